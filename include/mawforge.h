@@ -54,6 +54,11 @@ extern "C" {
 #define MF_Q4_0 2
 #define MF_Q8_0 8
 
+/* ---- types of activations, caches and logits (GGUF type ids) ---- */
+#define MF_F32 0
+#define MF_F16 1
+#define MF_BF16 30
+
 /* Access orders of a step with several tokens (mf_access_order). */
 #define MF_ORDER_FIRST_OCCURRENCE 0 /* distinct experts in (token, rank) first-occurrence order */
 #define MF_ORDER_RESIDENT_FIRST 1   /* the experts resident when the step starts first, then the rest */
@@ -347,6 +352,147 @@ int mf_expert_ffn_noalloc(const mf_model_t* model, const void* experts, const fl
  * when no call has run on the device).  Allocates nothing; MF_E_CUDA if the device cannot be
  * read. */
 int mf_expert_ffn_noalloc_check(void);
+
+/* ---- attention over a paged key/value cache, and sampling ----
+ *
+ * The rest of a serving step around mf_moe_forward: new tokens' keys and values appended to a
+ * paged cache (K(n) of the static plan; section "Static Budget Check"), attention from the new
+ * tokens over that cache, and the choice of the next token from the logits.  The paper's worker
+ * takes these from its runtime; it describes only their bytes. */
+
+/* Heads of an attention layer: n_heads query heads share n_kv_heads key/value heads (query head h
+ * reads kv head h / (n_heads / n_kv_heads)).  n_heads a multiple of n_kv_heads, at most 128 of
+ * them for each kv head; head_dim 64, 128 or 256; dtype MF_F16 or MF_BF16, of q, k, v, the cache
+ * and the output. */
+typedef struct mf_attn_shape {
+  int32_t n_heads, n_kv_heads, head_dim, dtype;
+} mf_attn_shape_t;
+
+/* A layer's cache, in the caller's device memory.  Element d of head h of line i of page p of the keys is at
+ * k + p * page_stride + i * token_stride + h * head_stride + d (in elements; the values the same
+ * from v), so a page may hold its lines token by token or head by head.  page_size >= 1 lines a
+ * page.  Pointers 16-byte aligned, strides multiples of 8. */
+typedef struct mf_kv_cache {
+  void *k, *v;
+  int64_t page_stride, token_stride, head_stride;
+  int32_t n_pages, page_size;
+} mf_kv_cache_t;
+
+/* The sequences of a step.  Sequence s adds the tokens q_start[s] .. q_start[s + 1] - 1 of the
+ * step's n_tokens (q_start device int32 [n_seqs + 1]; NULL: one token a sequence) and then has
+ * kv_len[s] lines in the cache (device int32 [n_seqs], the new ones counted): its new token i is
+ * line kv_len[s] - n + i of n new ones.  Line c is line c % page_size of page pages[s][c / page_size]
+ * (device int32 [n_seqs][pages_per_seq]).  max_q: no sequence adds more tokens than this (it bounds the
+ * launch; the lengths themselves stay on the device, so a captured step replays with new ones).
+ * Lengths, pages and positions out of range are taken as the nearest valid ones, never followed out of
+ * bounds, and reported by mf_attn_check. */
+typedef struct mf_step {
+  const int32_t *q_start, *kv_len, *pages;
+  int32_t n_seqs, n_tokens, max_q, pages_per_seq;
+} mf_step_t;
+
+/* Rotation by position.  Pair j < rot_dim / 2 of a head (elements j and j + rot_dim / 2, or 2j and 2j + 1
+ * when interleaved) turns by the angle whose cosine and sine are cos[p][j], sin[p][j] (device float
+ * [n_pos][rot_dim / 2], 16-byte aligned); the head's other elements stay.  p is the token's position on axis
+ * a, pos[a][t] (device int32 [n_axes][n_tokens]; NULL with n_axes = 1: its line in the cache), where
+ * the first section[0] pairs belong to axis 0, the next section[1] to axis 1, and so on (n_axes 1..4; the
+ * sections' sum is rot_dim / 2; ignored for one axis).  rot_dim a multiple of 16, at most head_dim. */
+typedef struct mf_rope {
+  const float *cos, *sin;
+  const int32_t* pos;
+  int32_t n_pos, rot_dim, interleaved, n_axes;
+  int32_t section[4];
+} mf_rope_t;
+
+/* New tokens of an append: q [n_tokens][n_heads][head_dim], k and v [n_tokens][n_kv_heads][head_dim]
+ * (device, of the shape's dtype), token t's row at t * stride elements, so they may be parts of one projection's rows.
+ * q and q_out are both NULL or both given; q_out may be q.  Pointers 16-byte aligned, strides multiples
+ * of 8. */
+typedef struct mf_append_args {
+  const void *q, *k, *v;
+  void* q_out;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;
+} mf_append_args_t;
+
+/* One attention call: out[t] = sum_j softmax_j(scale * q[t].k[j]) v[j] over the lines j that token t
+ * sees: j < kv_len; with causal != 0 only j <= its own line; with window > 0 only the last `window`
+ * lines up to its own.  lse (device float [n_tokens][n_heads], or NULL) receives log sum_j exp(scale * q.k[j]).
+ * A token that sees no line gets out = 0 and lse = -inf.  q and out as in mf_append_args; out may be q. */
+typedef struct mf_attn_args {
+  const void* q;
+  void* out;
+  float* lse;
+  int64_t q_stride, out_stride;
+  float scale;
+  int32_t window, causal, reserved;
+} mf_attn_args_t;
+
+typedef struct mf_attn mf_attn_t;
+
+/* Cache bytes K(n) of one sequence of n_tokens lines over n_layers layers, whole pages counted: what
+ * mf_plan_req's kv_bytes takes per stream.  MF_E_INVAL for an invalid shape, n_layers < 1, n_tokens < 0 or
+ * page_size < 1.  Host only. */
+int mf_kv_bytes(const mf_attn_shape_t* shape, int n_layers, int64_t n_tokens, int page_size, uint64_t* out);
+
+/* The workspace of attention calls of one shape on CUDA device `device`: steps of at most max_seqs
+ * sequences and max_tokens new tokens.  One handle serves all layers.  Its calls must follow one another (one stream, or ordered by
+ * events): they share the workspace.  MF_E_INVAL for an invalid shape or a size below 1; MF_E_OOM when
+ * the workspace cannot be allocated. */
+int mf_attn_create(mf_attn_t** out, const mf_attn_shape_t* shape, int max_seqs, int max_tokens, int device);
+
+/* Rotate the step's q (into q_out) and k by position and store k and v into their lines of the cache,
+ * stream-ordered on `stream` (a cudaStream_t).  rope NULL: no rotation.  Arithmetic in fp32, rounded once to
+ * the dtype.  A token whose line lies outside its sequence's pages, or on a page outside the pool, is not
+ * stored.  n_tokens = 0 does nothing.  MF_E_INVAL for NULL, misaligned or
+ * inconsistent arguments, or a step beyond the handle's sizes.  Returns after enqueueing. */
+int mf_kv_append(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step, const mf_rope_t* rope,
+                 const mf_append_args_t* args, void* stream);
+
+/* Attention of the step's tokens over the cache, which holds their own lines too, stream-ordered on
+ * `stream`.  The lines a token sees must hold finite values; what lies beyond a sequence's length, outside every
+ * window or on other pages may hold anything.  Scores, softmax and sums in fp32; the probabilities are rounded to the dtype for
+ * their product with v.  n_tokens = 0 does nothing.  Errors as for mf_kv_append. */
+int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step, const mf_attn_args_t* args,
+                    void* stream);
+
+/* Synchronise the device and report what the handle's kernels recorded since the last check, clearing it:
+ * MF_E_TIMEOUT if a bounded wait gave up (outputs since the last check are unreliable), MF_E_INVAL if a length,
+ * page or position was out of range, else MF_OK. */
+int mf_attn_check(mf_attn_t* attn);
+
+/* Release the handle (synchronises its device first).  NULL is a no-op. */
+void mf_attn_destroy(mf_attn_t* attn);
+
+/* One token from each row of logits.  With x the row in fp32 (NaN as -inf), M its largest value, T the
+ * row's temperature, and the entries in the order of falling x, the lower index first where x is equal:
+ *   z_i = 0 where x_i = M, else (x_i - M) / T, w_i = exp(z_i)
+ *   kept = the first top_k entries (top_k <= 0: all), of those the ones before which less than top_p of
+ *          their mass lies (top_p >= 1 or NaN: all), of those the ones with w_i >= min_p (above 1 it counts
+ *          as 1, NaN as 0); entries of -inf never, the first entry always
+ *   token = the kept i with the largest z_i + noise_i (the lowest such i; noise NaN as -inf),
+ *   logprob = z_token - log(sum of w over the kept)
+ * noise is the caller's random numbers: independent standard Gumbel values, -log(-log u) of uniform u,
+ * which make the token a draw from softmax over the kept (one value an entry, so that no token hangs on
+ * the rounding of a running sum).  T <= 0 or NaN keeps the first entry alone (greedy).  A row without a finite
+ * or +inf entry gives token -1 and logprob -inf.
+ *   logits  device [n_rows][vocab] of dtype (MF_F32, MF_F16 or MF_BF16), row r at r * logits_stride elements
+ *   noise   device float [n_rows][vocab], row r at r * noise_stride
+ *   temperature, top_p, min_p  device float [n_rows], top_k device int32 [n_rows]; NULL: 1, 1, 0, 0
+ *   token   device int32 [n_rows]; logprob device float [n_rows] or NULL
+ * vocab from 1 to 2^20.  Pointers aligned to their element; no workspace; n_rows = 0 does nothing. */
+typedef struct mf_sample_args {
+  const void* logits;
+  const float *noise, *temperature, *top_p, *min_p;
+  const int32_t* top_k;
+  int32_t* token;
+  float* logprob;
+  int64_t logits_stride, noise_stride;
+  int32_t n_rows, vocab, dtype, reserved;
+} mf_sample_args_t;
+
+/* Sample on the current device, stream-ordered on `stream`.  MF_E_INVAL for NULL or misaligned pointers, an unknown
+ * dtype, n_rows < 0, a vocab out of range or a stride below it. */
+int mf_sample(const mf_sample_args_t* args, void* stream);
 
 /* Release everything the context owns (synchronises its streams first). NULL is a no-op. */
 void mf_destroy(mf_ctx_t* ctx);

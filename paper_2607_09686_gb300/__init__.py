@@ -1,4 +1,5 @@
-"""GB300 routed-expert step of one MoE decoder layer (MawForge, arXiv 2607.09686).
+"""GB300 routed-expert step of one MoE decoder layer (MawForge, arXiv 2607.09686), with the paged
+attention and the sampling of a serving step around it.
 
 Thin ctypes binding of ``libmawforge.so`` (declared in ``include/mawforge.h``).  Every
 step of the path runs in the library's CUDA kernels; this module only marshals
@@ -21,10 +22,13 @@ __all__ = [
     "mf_expert_ffn_noalloc_check", "mf_pack_save", "mf_create_from_file", "mf_pack_file_stats",
     "mf_pack_file_direct", "mf_destroy",
     "mf_strerror", "mf_last_cuda_error",
+    "MF_F32", "MF_F16", "MF_BF16", "AttnShape", "KvCache", "Step", "Rope", "kv_cache", "step", "rope", "mf_kv_bytes",
+    "mf_attn_create", "mf_kv_append", "mf_attn_forward", "mf_attn_check", "mf_attn_destroy", "mf_sample",
 ]
 
 Q4_0 = 2
 Q8_0 = 8
+MF_F32, MF_F16, MF_BF16 = 0, 1, 30
 MF_OK, MF_E_INVAL, MF_E_BUDGET, MF_E_OOM, MF_E_CUDA, MF_E_STATE, MF_E_TIMEOUT, MF_E_IO = 0, -1, -2, -3, -4, -5, -6, -7
 KERNEL_CLASSES = ("router", "resolve", "materialize", "gateup_swiglu", "down_combine", "prefill_gemm", "ffn_fused")
 
@@ -73,6 +77,49 @@ class TunePoint(ctypes.Structure):
         return {name: getattr(self, name) for name, _ in self._fields_}
 
 
+class AttnShape(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+class KvCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32)]
+
+
+class Step(ctypes.Structure):
+    _fields_ = [("q_start", ctypes.c_void_p), ("kv_len", ctypes.c_void_p), ("pages", ctypes.c_void_p),
+                ("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("max_q", ctypes.c_int32),
+                ("pages_per_seq", ctypes.c_int32)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+                ("n_pos", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("n_axes", ctypes.c_int32), ("section", ctypes.c_int32 * 4)]
+
+
+class _AppendArgs(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_out", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("q_out_stride", ctypes.c_int64)]
+
+
+class _AttnArgs(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64), ("scale", ctypes.c_float),
+                ("window", ctypes.c_int32), ("causal", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class _SampleArgs(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("noise", ctypes.c_void_p), ("temperature", ctypes.c_void_p),
+                ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
+                ("token", ctypes.c_void_p), ("logprob", ctypes.c_void_p), ("logits_stride", ctypes.c_int64),
+                ("noise_stride", ctypes.c_int64), ("n_rows", ctypes.c_int32), ("vocab", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
 _vp, _i32, _u64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_uint64
 _sig = {
     "mf_payload_bytes": (_i32, [ctypes.POINTER(Model), ctypes.POINTER(_u64)]),
@@ -102,6 +149,14 @@ _sig = {
     "mf_pack_file_stats": (_i32, [_vp, ctypes.POINTER(_u64), ctypes.POINTER(_u64), ctypes.POINTER(ctypes.c_double)]),
     "mf_pack_file_direct": (_i32, [_vp]),
     "mf_destroy": (None, [_vp]),
+    "mf_kv_bytes": (_i32, [ctypes.POINTER(AttnShape), _i32, ctypes.c_int64, _i32, ctypes.POINTER(_u64)]),
+    "mf_attn_create": (_i32, [ctypes.POINTER(_vp), ctypes.POINTER(AttnShape), _i32, _i32, _i32]),
+    "mf_kv_append": (_i32, [_vp, ctypes.POINTER(KvCache), ctypes.POINTER(Step), ctypes.POINTER(Rope),
+                            ctypes.POINTER(_AppendArgs), _vp]),
+    "mf_attn_forward": (_i32, [_vp, ctypes.POINTER(KvCache), ctypes.POINTER(Step), ctypes.POINTER(_AttnArgs), _vp]),
+    "mf_attn_check": (_i32, [_vp]),
+    "mf_attn_destroy": (None, [_vp]),
+    "mf_sample": (_i32, [ctypes.POINTER(_SampleArgs), _vp]),
     "mf_strerror": (ctypes.c_char_p, [_i32]),
     "mf_last_cuda_error": (ctypes.c_char_p, []),
 }
@@ -340,3 +395,123 @@ def mf_expert_ffn_noalloc(model: Model, experts, g, x, y, stream=None) -> None:
 def mf_destroy(ctx: int) -> None:
     if ctx:
         _lib.mf_destroy(ctx)
+
+
+# ---- attention over a paged cache, and sampling (torch tensors; see mawforge.h for the layouts)
+
+def mf_kv_bytes(shape: AttnShape, n_layers: int, n_tokens: int, page_size: int) -> int:
+    """Cache bytes of one sequence over all layers, whole pages counted (PlanReq.kv_bytes per stream)."""
+    out = _u64()
+    _check(_lib.mf_kv_bytes(ctypes.byref(shape), n_layers, n_tokens, page_size, ctypes.byref(out)), "mf_kv_bytes")
+    return int(out.value)
+
+
+def kv_cache(k, v) -> KvCache:
+    """Describe a layer's cache: k and v of shape [pages][lines][kv heads][head_dim] with the same strides, the
+    last of them 1 (a page that holds its lines head by head is a transposed view)."""
+    st = k.stride()
+    if k.dim() != 4 or st != v.stride() or k.shape != v.shape or k.dtype != v.dtype or st[3] != 1:
+        raise ValueError("k and v must be [pages][lines][heads][dim] of one dtype and stride, dim contiguous")
+    c = KvCache(k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], k.shape[0], k.shape[1])
+    c.held = (k, v)
+    return c
+
+
+def _i32_tensor(t, name: str) -> None:
+    if t is not None and (str(t.dtype) != "torch.int32" or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous int32 tensor")
+
+
+def step(q_start, kv_len, pages, n_tokens: int, max_q: int) -> Step:
+    """Describe a step's sequences: q_start [n + 1] (None: one token each), kv_len [n], pages [n][pages a sequence],
+    contiguous int32 tensors on the device."""
+    for t, name in ((q_start, "q_start"), (kv_len, "kv_len"), (pages, "pages")):
+        _i32_tensor(t, name)
+    n = kv_len.shape[0]
+    if pages.dim() != 2 or pages.shape[0] != n or (q_start is not None and q_start.shape[0] != n + 1):
+        raise ValueError("q_start [n + 1], kv_len [n] and pages [n][...] must describe the same sequences")
+    s = Step(_addr(q_start), kv_len.data_ptr(), pages.data_ptr(), n, n_tokens, max_q, pages.shape[1])
+    s.held = (q_start, kv_len, pages)
+    return s
+
+
+def rope(cos, sin, pos=None, interleaved: bool = False, sections=None) -> Rope:
+    """Describe the rotation: cos and sin float [positions][pairs]; pos int32 [axes][tokens] or None (the cache
+    lines); sections: pairs of each axis."""
+    if cos.shape != sin.shape or not (cos.is_contiguous() and sin.is_contiguous()) or \
+            {str(cos.dtype), str(sin.dtype)} != {"torch.float32"}:
+        raise ValueError("cos and sin must be contiguous float32 tensors of one shape")
+    _i32_tensor(pos, "pos")
+    sections = tuple(sections) if sections is not None else (cos.shape[1],)
+    axes = 1 if pos is None or pos.dim() == 1 else pos.shape[0]
+    if len(sections) != axes or axes > 4:
+        raise ValueError("one section for each of at most 4 axes")
+    r = Rope(cos.data_ptr(), sin.data_ptr(), _addr(pos), cos.shape[0], 2 * cos.shape[1], int(interleaved), axes,
+             (ctypes.c_int32 * 4)(*sections))
+    r.held = (cos, sin, pos)
+    return r
+
+
+def mf_attn_create(shape: AttnShape, max_seqs: int, max_tokens: int, device: int = 0) -> int:
+    h = _vp()
+    _check(_lib.mf_attn_create(ctypes.byref(h), ctypes.byref(shape), max_seqs, max_tokens, device), "mf_attn_create")
+    return h.value
+
+
+def _row(t, where: str) -> int:
+    """Stride between tokens of a [tokens][heads][head_dim] tensor whose rows are contiguous."""
+    st = t.stride()
+    if len(st) != 3 or st[2] != 1 or st[1] != t.shape[2]:
+        raise MFError(MF_E_INVAL, where)
+    return st[0]
+
+
+def mf_kv_append(attn: int, cache: KvCache, step: Step, k, v, q=None, q_out=None, rope: Rope | None = None,
+                 stream=None) -> None:
+    """Rotate q (into q_out) and k by position, and store k and v into their lines of the cache."""
+    w = "mf_kv_append"
+    a = _AppendArgs(_addr(q), k.data_ptr(), v.data_ptr(), _addr(q_out), _row(q, w) if q is not None else 0, _row(k, w),
+                    _row(v, w), _row(q_out, w) if q_out is not None else 0)
+    rc = _lib.mf_kv_append(attn, cache, step, rope, a, _stream(stream))
+    if rc:
+        _check(rc, w)
+
+
+def mf_attn_forward(attn: int, cache: KvCache, step: Step, q, out, lse=None, scale: float = 1.0, window: int = 0,
+                    causal: bool = True, stream=None) -> None:
+    """Attention of the step's tokens over the cache."""
+    w = "mf_attn_forward"
+    a = _AttnArgs(q.data_ptr(), out.data_ptr(), _addr(lse), _row(q, w), _row(out, w), scale, window, causal, 0)
+    rc = _lib.mf_attn_forward(attn, cache, step, a, _stream(stream))
+    if rc:
+        _check(rc, w)
+
+
+def mf_attn_check(attn: int) -> int:
+    """0, MF_E_TIMEOUT, or MF_E_INVAL for a length, page or position out of range (returned, not raised)."""
+    rc = _lib.mf_attn_check(attn)
+    if rc not in (MF_OK, MF_E_TIMEOUT, MF_E_INVAL):
+        _check(rc, "mf_attn_check")
+    return rc
+
+
+def mf_attn_destroy(attn: int) -> None:
+    if attn:
+        _lib.mf_attn_destroy(attn)
+
+
+_LOGIT_TYPES = {"torch.float32": MF_F32, "torch.float16": MF_F16, "torch.bfloat16": MF_BF16}
+
+
+def mf_sample(logits, noise, token, logprob=None, temperature=None, top_k=None, top_p=None, min_p=None,
+              stream=None) -> None:
+    """One token from each row of logits [rows][vocab], with Gumbel noise of the same shape (see mawforge.h)."""
+    ls, ns = logits.stride(), noise.stride()
+    dtype = _LOGIT_TYPES.get(str(logits.dtype))
+    if dtype is None or len(ls) != 2 or ls[1] != 1 or ns[1] != 1 or noise.shape != logits.shape:
+        raise MFError(MF_E_INVAL, "mf_sample")
+    a = _SampleArgs(logits.data_ptr(), noise.data_ptr(), _addr(temperature), _addr(top_p), _addr(min_p), _addr(top_k),
+                    token.data_ptr(), _addr(logprob), ls[0], ns[0], logits.shape[0], logits.shape[1], dtype, 0)
+    rc = _lib.mf_sample(a, _stream(stream))
+    if rc:
+        _check(rc, "mf_sample")

@@ -16,10 +16,14 @@ namespace {
 
 thread_local char g_cuda_err[256] = "";
 
+}  // namespace
+
 int cuda_fail(cudaError_t e, const char* what) {
   snprintf(g_cuda_err, sizeof(g_cuda_err), "%s: %s", what, cudaGetErrorString(e));
   return e == cudaErrorMemoryAllocation ? MF_E_OOM : MF_E_CUDA;
 }
+
+namespace {
 
 #define MF_CUDA(call)                                 \
   do {                                                \

@@ -1,0 +1,281 @@
+// Attention over a paged key/value cache: entry points, and the append of new tokens.  Declarations and
+// contracts: mawforge.h.
+#include <cmath>
+#include <cstring>
+#include <new>
+
+#include "mf_attn.cuh"
+
+namespace mf {
+namespace {
+
+// ---- append: q and k rotated by position, k and v into their lines
+//
+// A pair (a, b) turned by an angle is (a cos - b sin, b cos + a sin).  Every element is read and written once,
+// so the kernel is a copy bounded by memory (few tokens: by its launch).  One block per token: the threads
+// count the sequences that end at or before it, then each takes pairs of 16-byte vectors of a head: the two halves of
+// eight rotated pairs (elements j.. and j + rot / 2.., or 16 neighbours when interleaved), or 16 neighbours
+// of what is only copied.
+struct AppendCall {
+  AttnStep st;
+  const void *q, *k, *v;
+  void *q_out, *kc, *vc;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;
+  const float *cos, *sin;
+  const int32_t* pos;
+  int n_pos, half, interleaved, n_axes;  // half = rot_dim / 2 (0: no rotation)
+  int end0, end1, end2;  // first pair after axes 0, 1, 2
+};
+
+constexpr int kAppendThreads = 256;
+
+template <class T>
+__global__ void __launch_bounds__(kAppendThreads) k_append(AppendCall c, int D) {
+  const AttnStep& st = c.st;
+  const int t = blockIdx.x;
+  int s = t;
+  if (st.q_start) {
+    s = 0;
+    for (int base = 0; base < st.n_seqs; base += kAppendThreads) {
+      const int i = base + threadIdx.x;
+      s += __syncthreads_count(i < st.n_seqs && __ldg(st.q_start + i + 1) <= t);
+    }
+  }
+  if (s >= st.n_seqs) {  // no sequence has the token
+    if (threadIdx.x == 0) attn_report(st, kAttnRange);
+    return;
+  }
+  const SeqSpan sp = seq_span(st, s);
+  const int line = sp.len - sp.n + t - sp.q0;
+  bool store = t >= sp.q0 && t < sp.q0 + sp.n && line >= 0;
+  int64_t at = 0;
+  if (store) {
+    const int pi = (int)fast_div((uint32_t)line, st.page_mul, st.page_shift);
+    const int page = __ldg(st.pages + (int64_t)s * st.pages_per_seq + pi);
+    store = page >= 0 && page < st.n_pages;
+    at = (int64_t)page * st.page_stride + (int64_t)(line - pi * st.page_size) * st.token_stride;
+  }
+  if (!store && threadIdx.x == 0) attn_report(st, kAttnRange);
+
+  const int per = D / 16, q_heads = c.q ? st.Hq : 0;
+  const int n_items = (q_heads + 2 * st.Hkv) * per;
+  for (int i = threadIdx.x; i < n_items; i += kAppendThreads) {
+    const int head = i / per, j = i % per;
+    const bool is_q = head < q_heads, is_v = head >= q_heads + st.Hkv;
+    const int h = is_q ? head : is_v ? head - q_heads - st.Hkv : head - q_heads;
+    if (!is_q && !store) continue;
+    const T* src = static_cast<const T*>(is_q ? c.q : is_v ? c.v : c.k) +
+                   (int64_t)t * (is_q ? c.q_stride : is_v ? c.v_stride : c.k_stride) + (int64_t)h * D;
+    T* dst = is_q ? static_cast<T*>(c.q_out) + (int64_t)t * c.q_out_stride + (int64_t)h * D
+                  : static_cast<T*>(is_v ? c.vc : c.kc) + at + (int64_t)h * st.head_stride;
+    const bool turn = !is_v && j * 8 < c.half;
+    const int e0 = turn && !c.interleaved ? j * 8 : j * 16, e1 = turn && !c.interleaved ? e0 + c.half : e0 + 8;
+    uint4 a = *reinterpret_cast<const uint4*>(src + e0), b = *reinterpret_cast<const uint4*>(src + e1);
+    if (turn) {
+      float co[8], si[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int pair = j * 8 + u;
+        int p = line;
+        if (c.pos) {
+          const int axis = c.n_axes == 1 ? 0 : (pair >= c.end0) + (pair >= c.end1) + (pair >= c.end2);
+          p = __ldg(c.pos + (int64_t)axis * st.n_tokens + t);
+        }
+        const int pc = min(max(p, 0), c.n_pos - 1);
+        if (pc != p) attn_report(st, kAttnRange);
+        co[u] = __ldg(c.cos + (int64_t)pc * c.half + pair);
+        si[u] = __ldg(c.sin + (int64_t)pc * c.half + pair);
+      }
+      uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
+      if (c.interleaved) {  // words hold (a, b) of pair u
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float2 x = Half2<T>::up(wa[u]), y = Half2<T>::up(wb[u]);
+          wa[u] = Half2<T>::down(x.x * co[u] - x.y * si[u], x.y * co[u] + x.x * si[u]);
+          wb[u] = Half2<T>::down(y.x * co[4 + u] - y.y * si[4 + u], y.y * co[4 + u] + y.x * si[4 + u]);
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float2 x = Half2<T>::up(wa[u]), y = Half2<T>::up(wb[u]);
+          wa[u] = Half2<T>::down(x.x * co[2 * u] - y.x * si[2 * u], x.y * co[2 * u + 1] - y.y * si[2 * u + 1]);
+          wb[u] = Half2<T>::down(y.x * co[2 * u] + x.x * si[2 * u], y.y * co[2 * u + 1] + x.y * si[2 * u + 1]);
+        }
+      }
+      a = make_uint4(wa[0], wa[1], wa[2], wa[3]);
+      b = make_uint4(wb[0], wb[1], wb[2], wb[3]);
+    }
+    *reinterpret_cast<uint4*>(dst + e0) = a;
+    *reinterpret_cast<uint4*>(dst + e1) = b;
+  }
+}
+
+// ---- arguments
+
+bool shape_ok(const mf_attn_shape_t* s) {
+  return s && s->n_kv_heads >= 1 && s->n_heads >= s->n_kv_heads && s->n_heads <= 65536 && s->n_heads % s->n_kv_heads == 0 &&
+         s->n_heads / s->n_kv_heads <= 128 && (s->head_dim == 64 || s->head_dim == 128 || s->head_dim == 256) &&
+         (s->dtype == MF_F16 || s->dtype == MF_BF16);
+}
+
+bool off16(const void* p) { return ((uintptr_t)p & 15) != 0; }
+bool bad_rows(const void* p, int64_t stride) { return !p || off16(p) || stride < 0 || stride % 8; }
+
+// false where the cache or the step does not fit the handle
+bool make_step(const mf_attn_t* h, const mf_kv_cache_t* c, const mf_step_t* t, AttnStep* st) {
+  if (!h || !c || !t || !c->k || !c->v || off16(c->k) || off16(c->v)) return false;
+  if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0 ||
+      (c->page_stride | c->token_stride | c->head_stride) % 8 || c->n_pages < 1 || c->page_size < 1)
+    return false;
+  if (t->n_seqs < 0 || t->n_tokens < 0 || t->n_seqs > h->max_seqs || t->n_tokens > h->max_tokens) return false;
+  if (t->n_tokens > 0 && (t->n_seqs < 1 || !t->kv_len || !t->pages || t->pages_per_seq < 1 || t->max_q < 1)) return false;
+  if (!t->q_start && t->n_tokens != t->n_seqs) return false;
+  st->q_start = t->q_start;
+  st->kv_len = t->kv_len;
+  st->pages = t->pages;
+  st->n_seqs = t->n_seqs;
+  st->n_tokens = t->n_tokens;
+  st->max_q = t->max_q < t->n_tokens ? t->max_q : t->n_tokens;
+  st->pages_per_seq = t->pages_per_seq;
+  st->page_size = c->page_size;
+  st->n_pages = c->n_pages;
+  const int64_t cap = (int64_t)t->pages_per_seq * c->page_size;
+  st->cap = cap < (1 << 30) ? (int)cap : 1 << 30;
+  const FastDiv fd = make_fast_div((uint32_t)c->page_size);
+  st->page_mul = fd.mul;
+  st->page_shift = fd.shift;
+  st->page_stride = c->page_stride;
+  st->token_stride = c->token_stride;
+  st->head_stride = c->head_stride;
+  st->Hq = h->shape.n_heads;
+  st->Hkv = h->shape.n_kv_heads;
+  st->G = st->Hq / st->Hkv;
+  st->err = h->err;
+  return true;
+}
+
+struct OnDevice {
+  int prev = -1;
+  bool ok;
+  explicit OnDevice(int dev) {
+    ok = cudaGetDevice(&prev) == cudaSuccess && (prev == dev || cudaSetDevice(dev) == cudaSuccess);
+    if (prev == dev) prev = -1;
+  }
+  ~OnDevice() {
+    if (prev >= 0) cudaSetDevice(prev);
+  }
+};
+
+}  // namespace
+}  // namespace mf
+
+using namespace mf;
+
+extern "C" int mf_kv_bytes(const mf_attn_shape_t* shape, int n_layers, int64_t n_tokens, int page_size, uint64_t* out) {
+  if (!shape_ok(shape) || !out || n_layers < 1 || n_tokens < 0 || page_size < 1) return MF_E_INVAL;
+  const uint64_t pages = ((uint64_t)n_tokens + (uint64_t)page_size - 1) / (uint64_t)page_size;
+  const unsigned __int128 b = (unsigned __int128)pages * (unsigned)page_size * 4u * (unsigned)shape->n_kv_heads *
+                              (unsigned)shape->head_dim * (unsigned)n_layers;
+  if (b >> 64) return MF_E_INVAL;
+  *out = (uint64_t)b;
+  return MF_OK;
+}
+
+extern "C" int mf_attn_create(mf_attn_t** out, const mf_attn_shape_t* shape, int max_seqs, int max_tokens, int device) {
+  if (!out) return MF_E_INVAL;
+  *out = nullptr;
+  if (!shape_ok(shape) || max_seqs < 1 || max_tokens < 1 || device < 0) return MF_E_INVAL;
+  OnDevice on(device);
+  if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
+  mf_attn_t* h = new (std::nothrow) mf_attn_t();
+  if (!h) return MF_E_OOM;
+  h->shape = *shape;
+  h->max_seqs = max_seqs;
+  h->max_tokens = max_tokens;
+  h->device = device;
+  cudaError_t e = cudaMalloc(&h->err, 256);
+  if (e == cudaSuccess) e = cudaMemset(h->err, 0, 256);
+  if (e == cudaSuccess) e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) {
+    const int rc = cuda_fail(e, "mf_attn_create");
+    cudaGetLastError();
+    cudaFree(h->err);
+    delete h;
+    return rc;
+  }
+  *out = h;
+  return MF_OK;
+}
+
+extern "C" int mf_kv_append(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step, const mf_rope_t* rope,
+                            const mf_append_args_t* args, void* stream) {
+  AppendCall c;
+  memset(&c, 0, sizeof(c));
+  if (!args || !make_step(attn, cache, step, &c.st)) return MF_E_INVAL;
+  const int D = attn->shape.head_dim;
+  if (rope) {
+    if (!rope->cos || !rope->sin || off16(rope->cos) || off16(rope->sin) || rope->n_pos < 1 || rope->rot_dim < 16 ||
+        rope->rot_dim % 16 || rope->rot_dim > D || rope->n_axes < 1 || rope->n_axes > 4 || (rope->n_axes > 1 && !rope->pos))
+      return MF_E_INVAL;
+    c.half = rope->rot_dim / 2;
+    int end[4] = {c.half, c.half, c.half, c.half}, at = 0;
+    for (int a = 0; a < rope->n_axes && rope->n_axes > 1; ++a) {
+      if (rope->section[a] < 0 || rope->section[a] > c.half - at) return MF_E_INVAL;
+      end[a] = at += rope->section[a];
+    }
+    if (rope->n_axes > 1 && at != c.half) return MF_E_INVAL;
+    c.end0 = end[0], c.end1 = end[1], c.end2 = end[2];
+    c.cos = rope->cos, c.sin = rope->sin, c.pos = rope->pos;
+    c.n_pos = rope->n_pos, c.interleaved = rope->interleaved != 0, c.n_axes = rope->n_axes;
+  }
+  if (c.st.n_tokens == 0) return MF_OK;
+  if (bad_rows(args->k, args->k_stride) || bad_rows(args->v, args->v_stride) || !args->q != !args->q_out) return MF_E_INVAL;
+  if (args->q && (bad_rows(args->q, args->q_stride) || bad_rows(args->q_out, args->q_out_stride))) return MF_E_INVAL;
+  c.q = args->q, c.k = args->k, c.v = args->v, c.q_out = args->q_out, c.kc = cache->k, c.vc = cache->v;
+  c.q_stride = args->q_stride, c.k_stride = args->k_stride, c.v_stride = args->v_stride, c.q_out_stride = args->q_out_stride;
+  OnDevice on(attn->device);
+  if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (attn->shape.dtype == MF_BF16)
+    k_append<__nv_bfloat16><<<c.st.n_tokens, kAppendThreads, 0, s>>>(c, D);
+  else
+    k_append<__half><<<c.st.n_tokens, kAppendThreads, 0, s>>>(c, D);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_kv_append");
+}
+
+extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step,
+                               const mf_attn_args_t* args, void* stream) {
+  AttnCall c;
+  memset(&c, 0, sizeof(c));
+  if (!args || !make_step(attn, cache, step, &c.st) || args->window < 0 || !std::isfinite(args->scale)) return MF_E_INVAL;
+  if (c.st.n_tokens == 0) return MF_OK;
+  if (bad_rows(args->q, args->q_stride) || bad_rows(args->out, args->out_stride) || ((uintptr_t)args->lse & 3)) return MF_E_INVAL;
+  c.k = cache->k, c.v = cache->v, c.q = args->q, c.out = args->out, c.lse = args->lse;
+  c.q_stride = args->q_stride, c.out_stride = args->out_stride;
+  c.scale = args->scale, c.window = args->window, c.causal = args->causal != 0;
+  OnDevice on(attn->device);
+  if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
+  const cudaError_t e = launch_attn(c, attn->shape.head_dim, attn->shape.dtype == MF_BF16, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_attn_forward");
+}
+
+extern "C" int mf_attn_check(mf_attn_t* attn) {
+  if (!attn) return MF_E_INVAL;
+  OnDevice on(attn->device);
+  unsigned err = 0;
+  cudaError_t e = on.ok ? cudaDeviceSynchronize() : cudaGetLastError();
+  if (e == cudaSuccess) e = cudaMemcpy(&err, attn->err, sizeof(err), cudaMemcpyDeviceToHost);
+  if (e == cudaSuccess && err) e = cudaMemset(attn->err, 0, sizeof(err));
+  if (e == cudaSuccess && err) e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) return cuda_fail(e, "mf_attn_check");
+  return err & kAttnTimeout ? MF_E_TIMEOUT : err ? MF_E_INVAL : MF_OK;
+}
+
+extern "C" void mf_attn_destroy(mf_attn_t* attn) {
+  if (!attn) return;
+  OnDevice on(attn->device);
+  cudaDeviceSynchronize();
+  cudaFree(attn->err);
+  delete attn;
+}

@@ -1,0 +1,118 @@
+// Internal declarations of the paged attention operators (not part of the C ABI).
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "mf_internal.cuh"
+
+namespace mf {
+
+// Bits of a handle's error word.
+constexpr unsigned kAttnRange = 1u, kAttnTimeout = 2u;
+
+// A step and the cache it works on, as the kernels take them (by value).
+struct AttnStep {
+  const int32_t *q_start, *kv_len, *pages;
+  int n_seqs, n_tokens, max_q, pages_per_seq;
+  int page_size, n_pages, cap;  // cap: lines a sequence's pages can hold
+  uint32_t page_mul, page_shift;  // line / page_size = (line * page_mul) >> (32 + page_shift), see fast_div
+  int64_t page_stride, token_stride, head_stride;
+  int Hq, Hkv, G;
+  unsigned* err;
+};
+
+// n / d for 0 <= n < 2^31 from a multiplier chosen on the host (Granlund and Montgomery, 1994: m = ceil(2^(32+l) / d)
+// with 2^l >= d fits 33 bits; its low 32 bits are kept and the top one added back by the sum below).
+struct FastDiv {
+  uint32_t mul, shift;
+};
+__host__ __device__ __forceinline__ uint32_t mulhi_u32(uint32_t a, uint32_t b) {
+#ifdef __CUDA_ARCH__
+  return __umulhi(a, b);
+#else
+  return (uint32_t)(((uint64_t)a * b) >> 32);
+#endif
+}
+inline FastDiv make_fast_div(uint32_t d) {
+  uint32_t l = 0;
+  while (l < 31 && (1u << l) < d) ++l;
+  const uint64_t m = ((uint64_t(1) << 32) * ((uint64_t(1) << l) - d)) / d + 1;
+  return {(uint32_t)m, l};
+}
+__host__ __device__ __forceinline__ uint32_t fast_div(uint32_t n, uint32_t mul, uint32_t shift) {
+  return (uint32_t)(((uint64_t)mulhi_u32(n, mul) + n) >> shift);
+}
+
+// One sequence's part of the step: its new tokens q0 .. q0 + n - 1 of the step, its lines in the cache.
+struct SeqSpan {
+  int q0, n, len;
+};
+
+__device__ __forceinline__ void attn_report(const AttnStep& a, unsigned bit) { atomicOr(a.err, bit); }
+
+__device__ __forceinline__ SeqSpan seq_span(const AttnStep& a, int s) {
+  int b = s, e = s + 1;
+  if (a.q_start) b = __ldg(a.q_start + s), e = __ldg(a.q_start + s + 1);
+  const int len0 = __ldg(a.kv_len + s);
+  const int q0 = min(max(b, 0), a.n_tokens), q1 = min(max(e, q0), a.n_tokens);
+  SeqSpan r = {q0, min(q1 - q0, a.max_q), min(max(len0, 0), a.cap)};
+  if (r.q0 != b || r.q0 + r.n != e || r.len != len0 || r.len < r.n) attn_report(a, kAttnRange);
+  return r;
+}
+
+// Element offset of line c of sequence s in the cache (head 0); a page outside the pool is taken as the nearest.
+__device__ __forceinline__ int64_t line_offset(const AttnStep& a, int s, int c) {
+  const int pi = (int)fast_div((uint32_t)c, a.page_mul, a.page_shift);
+  const int raw = __ldg(a.pages + (int64_t)s * a.pages_per_seq + pi), page = min(max(raw, 0), a.n_pages - 1);
+  if (page != raw) attn_report(a, kAttnRange);
+  return (int64_t)page * a.page_stride + (int64_t)(c - pi * a.page_size) * a.token_stride;
+}
+
+// An attention call.
+struct AttnCall {
+  AttnStep st;
+  const void *k, *v, *q;
+  void* out;
+  float* lse;
+  int64_t q_stride, out_stride;
+  float scale;
+  int window, causal;
+};
+
+// The lines [lo, hi) that the token at line `pos` of a sequence of `len` lines sees.
+__device__ __forceinline__ int vis_lo(const AttnCall& c, int pos) { return c.window > 0 ? max(0, pos - c.window + 1) : 0; }
+__device__ __forceinline__ int vis_hi(const AttnCall& c, int pos, int len) { return c.causal ? min(len, pos + 1) : len; }
+
+// The two 16-bit types.
+template <class T>
+struct Half2;
+template <>
+struct Half2<__half> {
+  using T2 = __half2;
+  static __device__ __forceinline__ float2 up(uint32_t w) { return __half22float2(*reinterpret_cast<__half2*>(&w)); }
+  static __device__ __forceinline__ uint32_t down(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+};
+template <>
+struct Half2<__nv_bfloat16> {
+  using T2 = __nv_bfloat162;
+  static __device__ __forceinline__ float2 up(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ uint32_t down(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+};
+
+cudaError_t launch_attn(const AttnCall& c, int head_dim, bool bf16, cudaStream_t s);
+
+}  // namespace mf
+
+struct mf_attn {
+  mf_attn_shape_t shape;
+  int max_seqs, max_tokens, device;
+  unsigned* err;  // device error word
+};

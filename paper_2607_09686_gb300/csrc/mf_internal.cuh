@@ -294,6 +294,9 @@ namespace mf {
 Layout make_layout(const mf_model_t& m);
 uint64_t canonical_payload_bytes(const mf_model_t& m);
 
+// record a failed CUDA call for mf_last_cuda_error; the MF_E_* code for it
+int cuda_fail(cudaError_t e, const char* what);
+
 // kernel launchers (each returns the launch status)
 // x and bias may be pinned host memory; with x_copy, the router also writes x there (device)
 // calls with at least this many tokens take the tiled router (W_r read once per 64 tokens)

@@ -1,0 +1,208 @@
+"""Sampling against the plain form in 64 bits.
+
+Inputs are such that no decision hangs on a rounding: borders of top-p lie between the mass of whole entries by more than
+1e-4 of the total, and the noise is drawn, so that two keys are never within 1e-4 of the best (the
+test checks this of its inputs before it compares)."""
+import math
+
+import pytest
+import torch
+
+import attn_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def mf():
+    import __graft_entry__
+    __graft_entry__.build()
+    import paper_2607_09686_gb300 as pkg
+    return pkg
+
+
+def gumbel(n, v, seed=0):
+    g = torch.Generator("cuda").manual_seed(seed + 99)
+    return -torch.log(-torch.log(torch.rand(n, v, device="cuda", generator=g).clamp_(1e-10, 1 - 1e-7)))
+
+
+def run(mf, x, noise, t=None, k=None, p=None, mp=None, logprob=True):
+    n = x.shape[0]
+
+    def vec(v, dt=torch.float32):
+        return None if v is None else torch.tensor([v] * n if not isinstance(v, list) else v, dtype=dt, device="cuda")
+
+    token = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+    lp = torch.full((n,), 7.0, device="cuda") if logprob else None
+    mf.mf_sample(x, noise, token, lp, vec(t), vec(k, torch.int32), vec(p), vec(mp))
+    return token.tolist(), lp.tolist() if logprob else None
+
+
+def check(mf, x, noise, t=None, k=None, p=None, mp=None):
+    got, lp = run(mf, x, noise, t, k, p, mp)
+    close = 0
+    for r in range(x.shape[0]):
+        def of(v, d):
+            return d if v is None else v[r] if isinstance(v, list) else v
+        kept, z = ref.kept64(x[r].float(), of(t, 1.0), of(k, 0), torch.tensor(of(p, 1.0)).item(), torch.tensor(of(mp, 0.0)).item())
+        if not kept:
+            assert got[r] == -1 and lp[r] == -math.inf
+            continue
+        g = noise[r].double().nan_to_num(-math.inf, math.inf, -math.inf).tolist()
+        key = sorted(((z[i] + g[i], -i) for i in kept), reverse=True)
+        if len(key) > 1 and key[0][0] - key[1][0] < 1e-4 * max(1.0, abs(key[0][0])) and key[0][0] != key[1][0]:
+            close += 1
+            assert got[r] in (-key[0][1], -key[1][1])
+            continue
+        assert got[r] == -key[0][1], (r, got[r], -key[0][1])
+        # the fp32 z and the sum's relative error (2^-20 covers exp and a tree over 2^20 entries)
+        want = z[got[r]] - math.log(math.fsum(math.exp(z[i]) for i in kept))
+        assert abs(lp[r] - want) <= 2.0 ** -22 * abs(z[got[r]]) + 2.0 ** -20 + 2.0 ** -23 * abs(want)
+    assert close <= 1 + x.shape[0] // 50
+    return got
+
+
+DT = [torch.float32, torch.float16, torch.bfloat16]
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("v", [1, 2, 31, 1000, 4096, 50001, 131072, 262147])
+def test_temperature_alone(mf, dtype, v):
+    g = torch.Generator("cuda").manual_seed(v)
+    x = (torch.randn(3, v, device="cuda", generator=g) * 3).to(dtype)
+    check(mf, x, gumbel(3, v, v), t=[1.0, 0.5, 1.7])
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("v", [1, 7, 1000, 50001, 262147])
+def test_top_k(mf, dtype, v):
+    g = torch.Generator("cuda").manual_seed(v + 1)
+    ks = [1, 2, 3, 20, 50, 1000, 5000, v - 1, v, v + 5, 0, -1]
+    x = (torch.randn(len(ks), v, device="cuda", generator=g) * 3).to(dtype)
+    check(mf, x, gumbel(len(ks), v, v), k=ks)
+
+
+def spaced(v, n, seed, ratio, dtype=torch.float32):
+    """Rows whose sorted probabilities fall by a fixed ratio: running masses are known and well apart."""
+    g = torch.Generator("cuda").manual_seed(seed)
+    perm = torch.stack([torch.randperm(v, device="cuda", generator=g) for _ in range(n)])
+    return (torch.arange(v, device="cuda").float()[perm] * math.log(ratio)).to(dtype)
+
+
+@pytest.mark.parametrize("v", [3, 1000, 50001])
+@pytest.mark.parametrize("ratio", [0.5, 0.9, 0.99])
+def test_top_p(mf, v, ratio):
+    ps = [0.0, -1.0, 0.3, 0.505, 0.9003, 0.95007, 1.0, 2.0, math.nan]
+    x = spaced(v, len(ps), v, ratio)
+    noise = gumbel(len(ps), v, v)
+    check(mf, x, noise, p=[1.0 if p != p else p for p in ps])
+    a, b = (run(mf, x, noise, p=q) for q in (ps, [1.0 if p != p else p for p in ps]))
+    assert a == b
+
+
+@pytest.mark.parametrize("v", [3, 1000, 50001])
+def test_min_p(mf, v):
+    ms = [0.0, -1.0, 0.0503, 0.5003, 1.0, 3.0]
+    x = spaced(v, len(ms), v, 0.9)
+    check(mf, x, gumbel(len(ms), v, v), mp=ms)
+
+
+@pytest.mark.parametrize("dtype", DT)
+def test_all_together(mf, dtype):
+    n, v = 40, 5003
+    g = torch.Generator("cuda").manual_seed(5)
+    x = (torch.randn(n, v, device="cuda", generator=g) * 2).to(dtype)
+    check(mf, x, gumbel(n, v), t=[0.7, 1.0, 0.0, 1.3] * 10, k=[0, 50, 7, 1000, 4000] * 8, p=[1.0, 0.9, 0.5003, 0.8] * 10,
+          mp=[0.0, 0.02, 0.3] * 13 + [0.0])
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("v", [40, 3001, 70000])
+def test_ties(mf, dtype, v):
+    """Few distinct values: the border falls among equal ones, which count in the order of their index."""
+    g = torch.Generator("cuda").manual_seed(v)
+    ks = [1, 2, 5, 17, 100, v // 3, v // 2 + 1, v - 1]
+    x = torch.randint(0, 4, (len(ks), v), device="cuda", generator=g).float().mul_(0.5).to(dtype)
+    check(mf, x, gumbel(len(ks), v), k=ks)
+    one = torch.zeros(len(ks), v, device="cuda", dtype=dtype)
+    check(mf, one, gumbel(len(ks), v, 3), k=ks)
+    # of equal entries top-p keeps the first ceil(p v)
+    p = [(j + 0.5) / v for j in (0, 1, 5, v // 2, v - 2)]
+    check(mf, one[:5], gumbel(5, v, 4), p=p)
+
+
+def test_greedy_takes_the_lowest_of_the_largest(mf):
+    x = torch.randn(6, 3000, device="cuda")
+    x[:, 700] = x[:, 699] = x[:, 2999] = 9.0
+    for t in (0.0, -1.0, math.nan):
+        got, lp = run(mf, x, gumbel(6, 3000), t=t, k=50, p=0.5, mp=0.1)
+        assert got == [699] * 6 and lp == [0.0] * 6
+
+
+@pytest.mark.parametrize("dtype", DT)
+def test_masked_rows(mf, dtype):
+    """Forbidden entries of -inf, NaN or the type's lowest value, rows of nothing else, +inf."""
+    n, v = 8, 2050
+    g = torch.Generator("cuda").manual_seed(8)
+    x = (torch.randn(n, v, device="cuda", generator=g) * 2).to(dtype)
+    x[0, ::2] = -math.inf
+    x[1] = -math.inf
+    x[2] = math.nan
+    x[3, 5:] = math.nan
+    x[4, 3:] = torch.finfo(dtype).min
+    x[5] = torch.finfo(dtype).min
+    x[6, 77] = math.inf
+    x[7, 10:40:3] = math.inf
+    noise = gumbel(n, v)
+    noise[0, 1:200:2] = math.nan
+    for kw in (dict(), dict(k=3), dict(p=0.9003), dict(mp=0.3003), dict(t=0.0), dict(t=0.7, k=100, p=0.7003)):
+        check(mf, x, noise, **kw)
+
+
+def test_equal_keys_take_the_lowest_index(mf):
+    x = torch.zeros(2, 5000, device="cuda")
+    noise = torch.zeros(2, 5000, device="cuda")
+    noise[1] = -math.inf
+    noise[1, 4000:] = math.nan
+    assert run(mf, x, noise)[0] == [0, 0]
+    noise[0, 1234] = noise[0, 4321] = 1.0
+    assert run(mf, x, noise)[0] == [1234, 0]
+
+
+def test_strides_and_odd_addresses(mf):
+    for dtype in DT:
+        big = torch.randn(5, 1013, device="cuda").to(dtype)
+        x, noise = big[:, 5:1006], gumbel(5, 1003)[:, 1:1002]
+        assert run(mf, x, noise, k=50) == run(mf, x.contiguous(), noise.contiguous(), k=50)
+
+
+def test_frequencies(mf):
+    """Drawn often enough, tokens come up as softmax says: within 5 standard deviations."""
+    n, v = 20000, 12
+    row = torch.tensor([0.0, 1.0, -1.0, 2.0, 0.5, -3.0, 1.5, -0.5, 0.2, 0.7, -2.0, 1.1], device="cuda")
+    got, _ = run(mf, row.expand(n, v).contiguous(), gumbel(n, v, 2), t=0.8)
+    p = torch.softmax(row.double() / 0.8, 0).tolist()
+    for i in range(v):
+        assert abs(got.count(i) - n * p[i]) <= 5 * math.sqrt(n * p[i] * (1 - p[i]))
+
+
+def test_same_every_time(mf):
+    x, noise = (torch.randn(64, 50001, device="cuda") * 2).bfloat16(), gumbel(64, 50001)
+    a = run(mf, x, noise, t=0.9, k=0, p=0.95)
+    for _ in range(5):
+        assert run(mf, x, noise, t=0.9, k=0, p=0.95) == a
+
+
+def test_refusals(mf):
+    x, noise, token = torch.zeros(2, 10, device="cuda"), torch.zeros(2, 10, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    for a in ((x.double(), noise, token), (x, noise[:, :9], token), (x[:, ::2], noise[:, ::2], token)):
+        with pytest.raises(mf.MFError):
+            mf.mf_sample(*a)
+    ok = dict(logits=x.data_ptr(), noise=noise.data_ptr(), token=token.data_ptr(), logits_stride=10, noise_stride=10, n_rows=2,
+              vocab=10, dtype=mf.MF_F32)
+    for bad in (dict(logits=None), dict(noise=None), dict(token=None), dict(logits=x.data_ptr() + 2), dict(noise=noise.data_ptr() + 1),
+                dict(vocab=0), dict(vocab=(1 << 20) + 1), dict(n_rows=-1), dict(dtype=8), dict(logits_stride=9), dict(noise_stride=9)):
+        with pytest.raises(mf.MFError) as e:
+            mf._check(mf._lib.mf_sample(mf._SampleArgs(**{**ok, **bad}), None), "mf_sample")
+        assert e.value.status == mf.MF_E_INVAL
+    mf._check(mf._lib.mf_sample(mf._SampleArgs(**{**ok, "n_rows": 0, "token": None}), None), "mf_sample")
