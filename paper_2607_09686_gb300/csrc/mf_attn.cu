@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(AppendCall c, int D) 
 // ---- arguments
 
 bool shape_ok(const mf_attn_shape_t* s) {
-  return s && s->n_kv_heads >= 1 && s->n_heads >= s->n_kv_heads && s->n_heads <= 65536 && s->n_heads % s->n_kv_heads == 0 &&
+  return s && s->n_kv_heads >= 1 && s->n_heads >= s->n_kv_heads && s->n_heads <= 4096 && s->n_heads % s->n_kv_heads == 0 &&
          s->n_heads / s->n_kv_heads <= 128 && (s->head_dim == 64 || s->head_dim == 128 || s->head_dim == 256) &&
          (s->dtype == MF_F16 || s->dtype == MF_BF16);
 }
@@ -193,7 +193,15 @@ extern "C" int mf_attn_create(mf_attn_t** out, const mf_attn_shape_t* shape, int
   h->max_seqs = max_seqs;
   h->max_tokens = max_tokens;
   h->device = device;
-  cudaError_t e = cudaMalloc(&h->err, 256);
+  cudaError_t e = cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, device);
+  const int n_parts = attn_few_parts(h->sms);
+  const size_t o_bytes = (size_t)n_parts * 16 * shape->head_dim * 4, ml_bytes = (size_t)n_parts * 16 * 8;
+  unsigned char* ws = nullptr;
+  if (e == cudaSuccess) e = cudaMalloc(&ws, 256 + o_bytes + ml_bytes + (size_t)max_seqs * shape->n_kv_heads * sizeof(int2));
+  h->err = reinterpret_cast<unsigned*>(ws);
+  h->parts.o = reinterpret_cast<float*>(ws + 256);
+  h->parts.ml = reinterpret_cast<float2*>(ws + 256 + o_bytes);
+  h->parts.rec = reinterpret_cast<int2*>(ws + 256 + o_bytes + ml_bytes);
   if (e == cudaSuccess) e = cudaMemset(h->err, 0, 256);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) {
@@ -256,7 +264,11 @@ extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, cons
   c.scale = args->scale, c.window = args->window, c.causal = args->causal != 0;
   OnDevice on(attn->device);
   if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
-  const cudaError_t e = launch_attn(c, attn->shape.head_dim, attn->shape.dtype == MF_BF16, static_cast<cudaStream_t>(stream));
+  const int D = attn->shape.head_dim;
+  const bool bf16 = attn->shape.dtype == MF_BF16;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = (int64_t)c.st.max_q * c.st.G <= kFewRows ? launch_attn_few(c, attn->parts, D, bf16, attn->sms, s)
+                                                                 : launch_attn(c, D, bf16, s);
   return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_attn_forward");
 }
 

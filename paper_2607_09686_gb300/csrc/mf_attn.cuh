@@ -88,7 +88,7 @@ template <class T>
 struct Half2;
 template <>
 struct Half2<__half> {
-  using T2 = __half2;
+  static constexpr bool kBf16 = false;
   static __device__ __forceinline__ float2 up(uint32_t w) { return __half22float2(*reinterpret_cast<__half2*>(&w)); }
   static __device__ __forceinline__ uint32_t down(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
@@ -97,7 +97,7 @@ struct Half2<__half> {
 };
 template <>
 struct Half2<__nv_bfloat16> {
-  using T2 = __nv_bfloat162;
+  static constexpr bool kBf16 = true;
   static __device__ __forceinline__ float2 up(uint32_t w) {
     return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
   }
@@ -107,6 +107,17 @@ struct Half2<__nv_bfloat16> {
   }
 };
 
+// What blocks leave of (sequence, kv head) pairs that they do not have whole: per part 16 rows of o (not yet
+// divided by l) and of (m, l); per pair the first block and the number of its pieces (0: one block had it whole).
+struct AttnParts {
+  float* o;     // [parts][16][head_dim]
+  float2* ml;   // [parts][16]  m in the log2 domain
+  int2* rec;    // [max_seqs][Hkv]
+};
+constexpr int kFewRows = 16;    // rows (token, head of the group) of a call for launch_attn_few
+constexpr int kMaxParts = 1024; // pieces of one pair
+int attn_few_parts(int sms);
+cudaError_t launch_attn_few(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int sms, cudaStream_t s);
 cudaError_t launch_attn(const AttnCall& c, int head_dim, bool bf16, cudaStream_t s);
 
 }  // namespace mf
@@ -114,5 +125,7 @@ cudaError_t launch_attn(const AttnCall& c, int head_dim, bool bf16, cudaStream_t
 struct mf_attn {
   mf_attn_shape_t shape;
   int max_seqs, max_tokens, device;
-  unsigned* err;  // device error word
+  int sms;
+  unsigned* err;  // device error word, at the workspace's start
+  mf::AttnParts parts;
 };

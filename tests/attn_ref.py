@@ -76,7 +76,7 @@ def attention64(c, scale, window=0, causal=True):
             lo = max(0, pos - window + 1) if window else 0
             hi = min(n, pos + 1) if causal else n
             if pos < 0:
-                hi = 0 if causal or window else n
+                hi = 0 if causal else n
             if hi <= lo:
                 continue
             q = c.q[t].double().view(c.hkv, c.hq // c.hkv, c.d)
