@@ -154,6 +154,15 @@ bool make_step(const mf_attn_t* h, const mf_kv_cache_t* c, const mf_step_t* t, A
   return true;
 }
 
+struct Carve {  // places in one allocation
+  size_t off = 0;
+  size_t take(size_t bytes) {
+    const size_t o = off;
+    off = (off + bytes + 255) & ~size_t(255);
+    return o;
+  }
+};
+
 struct OnDevice {
   int prev = -1;
   bool ok;
@@ -194,14 +203,21 @@ extern "C" int mf_attn_create(mf_attn_t** out, const mf_attn_shape_t* shape, int
   h->max_tokens = max_tokens;
   h->device = device;
   cudaError_t e = cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, device);
-  const int n_parts = attn_few_parts(h->sms);
-  const size_t o_bytes = (size_t)n_parts * 16 * shape->head_dim * 4, ml_bytes = (size_t)n_parts * 16 * 8;
+  // parts of either path (a step takes one): rows of a part times parts
+  const int G = shape->n_heads / shape->n_kv_heads, tile = attn_tile_rows(shape->head_dim);
+  const size_t few = (size_t)attn_few_blocks(h->sms) * 2 * kFewRows;
+  const size_t many = (int64_t)max_tokens * G > kFewRows ? (size_t)h->sms * 2 * tile : 0;
+  const size_t rows = few > many ? few : many, tiles = (size_t)((int64_t)max_tokens * G / tile) + max_seqs;
+  Carve w;
+  const size_t o_err = w.take(256), o_o = w.take(rows * shape->head_dim * 4), o_ml = w.take(rows * 8),
+               o_rec = w.take((size_t)attn_few_blocks(h->sms) * sizeof(AttnRec)), o_first = w.take(((size_t)max_seqs + 1) * 4),
+               o_seq = w.take(tiles * 4), o_before = w.take((tiles + 1) * 8);
   unsigned char* ws = nullptr;
-  if (e == cudaSuccess) e = cudaMalloc(&ws, 256 + o_bytes + ml_bytes + (size_t)max_seqs * shape->n_kv_heads * sizeof(int2));
-  h->err = reinterpret_cast<unsigned*>(ws);
-  h->parts.o = reinterpret_cast<float*>(ws + 256);
-  h->parts.ml = reinterpret_cast<float2*>(ws + 256 + o_bytes);
-  h->parts.rec = reinterpret_cast<int2*>(ws + 256 + o_bytes + ml_bytes);
+  if (e == cudaSuccess) e = tiles < (1u << 30) ? cudaMalloc(&ws, w.off) : cudaErrorMemoryAllocation;
+  h->err = reinterpret_cast<unsigned*>(ws + o_err);
+  h->parts = {reinterpret_cast<float*>(ws + o_o), reinterpret_cast<float2*>(ws + o_ml), reinterpret_cast<AttnRec*>(ws + o_rec)};
+  h->plan = {reinterpret_cast<int*>(ws + o_first), reinterpret_cast<int*>(ws + o_seq), reinterpret_cast<int64_t*>(ws + o_before),
+             (int)tiles, 0};
   if (e == cudaSuccess) e = cudaMemset(h->err, 0, 256);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) {
@@ -256,7 +272,9 @@ extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, cons
                                const mf_attn_args_t* args, void* stream) {
   AttnCall c;
   memset(&c, 0, sizeof(c));
-  if (!args || !make_step(attn, cache, step, &c.st) || args->window < 0 || !std::isfinite(args->scale)) return MF_E_INVAL;
+  if (!args || !make_step(attn, cache, step, &c.st) || args->window < 0 || !std::isfinite(args->scale) ||
+      !(args->scale > 0.f))
+    return MF_E_INVAL;
   if (c.st.n_tokens == 0) return MF_OK;
   if (bad_rows(args->q, args->q_stride) || bad_rows(args->out, args->out_stride) || ((uintptr_t)args->lse & 3)) return MF_E_INVAL;
   c.k = cache->k, c.v = cache->v, c.q = args->q, c.out = args->out, c.lse = args->lse;
@@ -268,7 +286,7 @@ extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, cons
   const bool bf16 = attn->shape.dtype == MF_BF16;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = (int64_t)c.st.max_q * c.st.G <= kFewRows ? launch_attn_few(c, attn->parts, D, bf16, attn->sms, s)
-                                                                 : launch_attn(c, D, bf16, s);
+                                                                 : launch_attn_many(c, attn->plan, attn->parts, D, bf16, attn->sms, s);
   return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_attn_forward");
 }
 

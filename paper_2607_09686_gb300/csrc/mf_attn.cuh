@@ -107,18 +107,37 @@ struct Half2<__nv_bfloat16> {
   }
 };
 
-// What blocks leave of (sequence, kv head) pairs that they do not have whole: per part 16 rows of o (not yet
-// divided by l) and of (m, l); per pair the first block and the number of its pieces (0: one block had it whole).
-struct AttnParts {
-  float* o;     // [parts][16][head_dim]
-  float2* ml;   // [parts][16]  m in the log2 domain
-  int2* rec;    // [max_seqs][Hkv]
+// A (sequence, kv head)'s rows that several blocks share: `rows` of them from row0 on (row r: token q0 + r / G of the
+// step, head r % G of kv head h's group), in n pieces of successive blocks (0: none starts here).
+struct AttnRec {
+  int q0, h, row0, rows, n;
 };
-constexpr int kFewRows = 16;    // rows (token, head of the group) of a call for launch_attn_few
-constexpr int kMaxParts = 1024; // pieces of one pair
-int attn_few_parts(int sms);
+// What blocks leave of work that they do not have whole.  Block b's last piece, where it starts the work, is part
+// 2b + 1 and rec[b] describes it; the pieces that go on with it are parts 2(b + 1), 2(b + 2), ...
+struct AttnParts {
+  float* o;     // [parts][rows][head_dim], not yet divided by l
+  float2* ml;   // [parts][rows]  running maximum (log2 domain) and sum
+  AttnRec* rec;  // [blocks]
+};
+constexpr int kFewRows = 16;    // rows (token, head of the group) of a part of launch_attn_few
+constexpr int kMaxParts = 1024; // pieces of one record
+int attn_few_blocks(int sms);
+int attn_tile_rows(int head_dim);  // rows of a part of launch_attn_many (one block per SM)
+
+// What k_attn_plan finds of a step for launch_attn_many: the row tiles of the sequences and the jobs before each.
+struct AttnPlan {
+  int* first;       // [max_seqs + 1]  first row tile of a sequence; then the number of tiles
+  int* seq_of;      // [max_tiles]     the tile's sequence
+  int64_t* before;  // [max_tiles + 1] jobs (of one kv head) before the tile
+  int max_tiles, tiles;
+};
+
 cudaError_t launch_attn_few(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int sms, cudaStream_t s);
-cudaError_t launch_attn(const AttnCall& c, int head_dim, bool bf16, cudaStream_t s);
+cudaError_t launch_attn_many(const AttnCall& c, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
+                             cudaStream_t s);
+// the records of `blocks` blocks joined; rows: rows of a part
+cudaError_t launch_attn_join(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int rows, int blocks,
+                             cudaStream_t s);
 
 }  // namespace mf
 
@@ -128,4 +147,5 @@ struct mf_attn {
   int sms;
   unsigned* err;  // device error word, at the workspace's start
   mf::AttnParts parts;
+  mf::AttnPlan plan;
 };

@@ -122,6 +122,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
   __syncthreads();
   total = (s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]) * st.Hkv;
   const int64_t B = min((int64_t)gridDim.x, total);  // every block that works has a tile
+  if (tid == 0) parts.rec[blockIdx.x].n = 0;
   if (blockIdx.x >= B) return;
   const int64_t t0 = total * blockIdx.x / B, t1 = total * (blockIdx.x + 1) / B;
   {
@@ -302,11 +303,11 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
       __syncthreads();
       const bool whole = j0 == 0 && cur.j + 1 == cur.sn.nt;
       const int part = blockIdx.x * 2 + (j0 == 0);  // a piece that starts before this block is its first
-      if (j0 == 0 && tid == 0)  // the piece that starts a (sequence, head) says how many follow
-        parts.rec[cur.s * st.Hkv + cur.h] =
-            whole ? make_int2(0, 0)
-                  : make_int2((int)blockIdx.x, (int)((B * (t0 + t - cur.j + cur.sn.nt) - 1) / total) - (int)blockIdx.x + 1);
       const int rows = cur.sn.sp.n * st.G;
+      if (j0 == 0 && !whole && tid == 0) {  // the block of the last tile has the last piece
+        const int64_t end = t0 + t - cur.j + cur.sn.nt;
+        parts.rec[blockIdx.x] = {cur.sn.sp.q0, cur.h, 0, rows, (int)((B * end - 1) / total) - (int)blockIdx.x + 1};
+      }
       for (int i = tid; i < rows * (D / 4); i += kThreads) {
         const int r = i / (D / 4), col = i % (D / 4) * 4;
         float mx = s_m[0][r];
@@ -342,76 +343,6 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
   }
 }
 
-// The pieces of each split (sequence, head) joined: block = (new token, query head); the threads hold four columns each,
-// several groups of them take the pieces in turn.
-template <class T, int D>
-__global__ void __launch_bounds__(128) k_attn_join(AttnCall c, AttnParts parts) {
-  constexpr int kCols = D / 4, kGroups = 128 / kCols;
-  __shared__ float s_w[kMaxParts];
-  __shared__ float4 s_o[128];
-  __shared__ float s_red[8];
-  const AttnStep& st = c.st;
-  const int t = blockIdx.x, head = blockIdx.y, tid = threadIdx.x, lane = tid & 31;
-  pdl_wait();
-  int s = t;
-  if (st.q_start) {
-    s = 0;
-    for (int base = 0; base < st.n_seqs; base += 128) {
-      const int i = base + tid;
-      s += __syncthreads_count(i < st.n_seqs && __ldg(st.q_start + i + 1) <= t);
-    }
-  }
-  if (s >= st.n_seqs) return;
-  const SeqSpan sp = seq_span(st, s);
-  if (t < sp.q0 || t >= sp.q0 + sp.n) return;
-  const int2 rec = parts.rec[s * st.Hkv + head / st.G];
-  const int n = rec.y;
-  if (n == 0) return;
-  const int r = (t - sp.q0) * st.G + head % st.G;
-  auto row_of = [&](int p) { return (p == 0 ? rec.x * 2 + 1 : (rec.x + p) * 2) * 16 + r; };
-  float mx = -INFINITY, ls = 0.f;
-  for (int p = tid; p < n; p += 128) mx = fmaxf(mx, parts.ml[row_of(p)].x);
-#pragma unroll
-  for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-  if (lane == 0) s_red[tid >> 5] = mx;
-  __syncthreads();
-  mx = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-  const float ms = mx == -INFINITY ? 0.f : mx;
-  for (int p = tid; p < n; p += 128) {
-    const float2 ml = parts.ml[row_of(p)];
-    const float w = exp2f(ml.x - ms);
-    s_w[p] = w;
-    ls += w * ml.y;
-  }
-#pragma unroll
-  for (int d = 16; d; d >>= 1) ls += __shfl_xor_sync(0xffffffffu, ls, d);
-  if (lane == 0) s_red[4 + (tid >> 5)] = ls;
-  __syncthreads();
-  ls = (s_red[4] + s_red[5]) + (s_red[6] + s_red[7]);
-  const int col = tid % kCols, g = tid / kCols;
-  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int p = g; p < n; p += kGroups) {
-    const float w = s_w[p];
-    const float4 v = *reinterpret_cast<const float4*>(parts.o + (int64_t)row_of(p) * D + col * 4);
-    sum.x += w * v.x, sum.y += w * v.y, sum.z += w * v.z, sum.w += w * v.w;
-  }
-  s_o[tid] = sum;
-  __syncthreads();
-  if (g == 0) {
-#pragma unroll
-    for (int i = 1; i < kGroups; ++i) {
-      const float4 v = s_o[i * kCols + col];
-      sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
-    }
-    const float inv = ls > 0.f ? 1.f / ls : 0.f;
-    T* out = static_cast<T*>(c.out) + (int64_t)t * c.out_stride + (int64_t)head * D + col * 4;
-    *reinterpret_cast<uint2*>(out) =
-        make_uint2(Half2<T>::down(sum.x * inv, sum.y * inv), Half2<T>::down(sum.z * inv, sum.w * inv));
-    if (c.lse && tid == 0) c.lse[(int64_t)t * st.Hq + head] = ls > 0.f ? (mx + log2f(ls)) * kLn2 : -INFINITY;
-  }
-}
-
 template <class T, int D>
 cudaError_t run(const AttnCall& c, const AttnParts& parts, int sms, cudaStream_t s) {
   // no more blocks than tiles there can be: the lengths are on the device, the pages they fit in are known
@@ -420,14 +351,13 @@ cudaError_t run(const AttnCall& c, const AttnParts& parts, int sms, cudaStream_t
   const unsigned grid = (unsigned)(most < fit ? most : fit);
   cudaError_t e = cudaFuncSetAttribute(k_attn_few<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Cfg<D>::kSmem);
   if (e == cudaSuccess) e = launch_pdl(false, k_attn_few<T, D>, dim3(grid), dim3(kThreads), Cfg<D>::kSmem, s, c, parts);
-  if (e == cudaSuccess && grid > 1)
-    e = launch_pdl(true, k_attn_join<T, D>, dim3((unsigned)c.st.n_tokens, (unsigned)c.st.Hq), dim3(128), 0, s, c, parts);
+  if (e == cudaSuccess && grid > 1) e = launch_attn_join(c, parts, D, Half2<T>::kBf16, kFewRows, (int)grid, s);
   return e;
 }
 
 }  // namespace
 
-int attn_few_parts(int sms) { return sms * 2 * 2; }
+int attn_few_blocks(int sms) { return sms * 2; }
 
 cudaError_t launch_attn_few(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int sms, cudaStream_t s) {
   if (bf16)

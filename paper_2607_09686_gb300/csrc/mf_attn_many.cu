@@ -1,0 +1,632 @@
+// Paged attention of many query rows (prefill chunks, verification batches) on the fifth-generation tensor cores.
+//
+// Rows.  The tokens of a sequence times the query heads that share a kv head are one list of rows (token major), cut into
+// row tiles of 128, so K and V are read once for the whole group and short chunks fill a tile with several heads.
+// A work item ("segment") is one or two row tiles of a (sequence, kv head) and the 128-line key tiles that
+// any of their rows sees; per key tile and row tile ("job")
+//   S = Q K^T (tcgen05, both operands in shared memory)  ->  tensor memory, 128 fp32 columns
+//   P = 2^(scale log2e S - m), rounded to the cache's type, written over S      (one thread a row)
+//   O += P V  (A from tensor memory, V read as it lies: its lines are the K dimension, an MN-major operand)
+// with a running maximum m and sum l per row.  O is rescaled only when m grows by more than 2^8 (until then the old m
+// serves: p stays below 2^8, and o and l carry the same factor); so most key tiles touch O not at all.
+//
+// Two jobs are always under way: while the tensor cores run one's products the softmax of the other is computed,
+// S and P in two buffers.  With head_dim 64 and 128 they are the two row tiles of a segment (they share K and V in
+// shared memory, which halves the cache's traffic), each with a warpgroup of its own; with head_dim 256, whose O fills
+// half of the tensor memory, or where a segment has one row tile, they are successive key tiles of it.  The
+// order in which the tensor cores work is S(0), S(1), then O(g), S(g + 2) for g = 0, 1, ..., across segments, so the next
+// segment's first scores run beside the last one's softmax.
+//
+// 12 warps: 0-3 and 4-7 softmax (thread = row; the maximum and the sum need no shuffles), 8 issues MMAs, 9-11 copy K, V and Q
+// lines with cp.async (a line's page is looked up per line, so any page size and stride will do; lines that no row of the
+// segment sees become zeros).  The ring holds units of 128 lines x 64 elements (16 KiB), ten of them beside Q.
+//
+// Split.  As for few rows: the step's jobs are one list shared out evenly over one block per SM; pieces of segments that
+// a block does not have whole are left as partials and joined in order.
+#include "mf_attn.cuh"
+#include "mf_tc.cuh"
+
+namespace mf {
+namespace {
+
+constexpr int kThreads = 384, kMmaWarp = 8, kLoadWarp0 = 9, kLoadWarps = 3;
+constexpr int kKeys = 128;                  // lines of a key tile
+constexpr uint32_t kUnitBytes = 128 * 128;  // 128 lines x 64 elements
+constexpr int kUnits = 10;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kGrow = 8.f;  // growth of the maximum (log2) that o is rescaled for
+
+template <int D>
+struct Cfg {
+  static constexpr int kU = D / 64;                   // units of a K or V tile
+  static constexpr int kRowTiles = D == 256 ? 1 : 2;  // row tiles of a segment
+  static constexpr int kRows = kRowTiles * 128;
+  static constexpr uint32_t kQBytes = kRowTiles * kU * kUnitBytes;
+  static constexpr uint32_t kSmem = kQBytes + kUnits * kUnitBytes + 1024;  // 1024: alignment
+};
+constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;
+
+// ---- the step's segments
+
+// row tile `qt` of a sequence: its rows and the lines that any of them sees
+struct Tile {
+  int rows, start, end, nt, jobs;  // jobs: row tiles (1 or 2) per key tile
+};
+template <int D>
+__device__ __forceinline__ Tile tile_of(const AttnCall& c, const SeqSpan& sp, int qt) {
+  const int G = c.st.G, R0 = qt * Cfg<D>::kRows;
+  Tile t;
+  t.rows = min(Cfg<D>::kRows, sp.n * G - R0);
+  const int first = sp.len - sp.n;
+  t.start = vis_lo(c, first + R0 / G);
+  t.end = max(0, vis_hi(c, first + (R0 + t.rows - 1) / G, sp.len));
+  t.nt = max(1, (t.end - t.start + kKeys - 1) / kKeys);
+  t.jobs = Cfg<D>::kRowTiles == 2 && t.rows > 128 ? 2 : 1;
+  return t;
+}
+
+// One block: for each sequence the index of its first row tile, for each row tile its sequence and the jobs before it.
+template <int D>
+__global__ void __launch_bounds__(1024) k_attn_plan(AttnCall c, AttnPlan p) {
+  __shared__ int64_t s_warp[32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_wait();
+  pdl_trigger();
+  auto scan = [&](int64_t v, int64_t& all) -> int64_t {  // exclusive prefix over the block, and the sum
+    int64_t x = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t o = __shfl_up_sync(0xffffffffu, x, d);
+      if (lane >= d) x += o;
+    }
+    __syncthreads();
+    if (lane == 31) s_warp[warp] = x;
+    __syncthreads();
+    int64_t before = 0;
+    all = 0;
+    for (int w = 0; w < 32; ++w) {
+      if (w < warp) before += s_warp[w];
+      all += s_warp[w];
+    }
+    return before + x - v;
+  };
+  int64_t done = 0;
+  for (int base = 0; base < c.st.n_seqs; base += 1024) {
+    const int s = base + tid;
+    int n = 0;
+    if (s < c.st.n_seqs) n = (seq_span(c.st, s).n * c.st.G + Cfg<D>::kRows - 1) / Cfg<D>::kRows;
+    int64_t all;
+    const int64_t at = done + scan(n, all);
+    if (s < c.st.n_seqs) p.first[s] = (int)min(at, (int64_t)p.max_tiles);
+    done += all;
+  }
+  const int tiles = (int)min(done, (int64_t)p.max_tiles);
+  if (tid == 0) p.first[c.st.n_seqs] = tiles;
+  __syncthreads();
+  int64_t jobs = 0;
+  for (int base = 0; base < tiles; base += 1024) {
+    const int i = base + tid;
+    int64_t n = 0;
+    if (i < tiles) {
+      int lo = 0, hi = c.st.n_seqs - 1;  // the last sequence whose first tile is at or before i
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.first[mid] <= i) lo = mid;
+        else hi = mid - 1;
+      }
+      const Tile t = tile_of<D>(c, seq_span(c.st, lo), i - p.first[lo]);
+      n = (int64_t)t.nt * t.jobs;
+      p.seq_of[i] = lo;
+    }
+    int64_t all;
+    const int64_t at = jobs + scan(n, all);
+    if (i < tiles) p.before[i] = at;
+    jobs += all;
+  }
+  if (tid == 0) p.before[tiles] = jobs;
+}
+
+// A segment as a block has it: key tiles j0 .. j1 - 1 of row tile `tile` (of all) and kv head h.
+struct Seg {
+  SeqSpan sp;
+  Tile t;
+  int s, h, tile, qt, j0, j1;
+  int64_t at;  // place of its first job in the list
+};
+// The walk over a block's segments.  The list is ordered by sequence, kv head, row tile.
+template <int D>
+struct Walk {
+  int64_t t0, t1;
+  Seg g;
+  bool more;  // g is a segment of this block
+
+  __device__ __forceinline__ void fill(const AttnCall& c, const AttnPlan& p) {
+    g.s = __ldg(p.seq_of + g.tile);
+    g.sp = seq_span(c.st, g.s);
+    g.qt = g.tile - __ldg(p.first + g.s);
+    g.t = tile_of<D>(c, g.sp, g.qt);
+    const int w = g.t.jobs;  // a key tile belongs to the block that its first job falls to
+    g.j0 = (int)max((int64_t)0, (t0 - g.at + w - 1) / w);
+    g.j1 = (int)min((int64_t)g.t.nt, (t1 - g.at + w - 1) / w);
+  }
+  __device__ __forceinline__ void advance(const AttnCall& c, const AttnPlan& p) {
+    g.at += (int64_t)g.t.nt * g.t.jobs;
+    if (g.at >= t1) {
+      more = false;
+      return;
+    }
+    const int first = __ldg(p.first + g.s);
+    int last = g.tile + 1;
+    // the sequence's tiles end where seq_of changes
+    if (last < p.tiles && __ldg(p.seq_of + last) == g.s) g.tile = last;
+    else if (++g.h < c.st.Hkv) g.tile = first;
+    else g.h = 0, g.tile = last;
+    fill(c, p);
+  }
+  __device__ __forceinline__ void skip_empty(const AttnCall& c, const AttnPlan& p) {
+    while (more && g.j0 >= g.j1) advance(c, p);
+  }
+  __device__ __forceinline__ void start(const AttnCall& c, const AttnPlan& p, int64_t a, int64_t b) {
+    t0 = a, t1 = b;
+    more = a < b;
+    if (!more) return;
+    // the last tile whose sequence starts at or before a, then the kv head, then the tile
+    int lo = 0, hi = p.tiles - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      const int first = __ldg(p.first + __ldg(p.seq_of + mid));
+      if (__ldg(p.before + first) * c.st.Hkv <= a) lo = mid;
+      else hi = mid - 1;
+    }
+    const int first = __ldg(p.first + __ldg(p.seq_of + lo)), end = lo + 1;
+    const int64_t b0 = __ldg(p.before + first), len = __ldg(p.before + end) - b0;
+    g.h = (int)((a - b0 * c.st.Hkv) / len);
+    const int64_t head = b0 * c.st.Hkv + g.h * len;
+    lo = first, hi = end - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (head + __ldg(p.before + mid) - b0 <= a) lo = mid;
+      else hi = mid - 1;
+    }
+    g.tile = lo;
+    g.at = head + __ldg(p.before + lo) - b0;
+    fill(c, p);
+    skip_empty(c, p);
+  }
+  __device__ __forceinline__ void next(const AttnCall& c, const AttnPlan& p) {
+    advance(c, p);
+    skip_empty(c, p);
+  }
+};
+
+// The jobs of the walk one by one: (key tile, row tile), row tile inner.
+template <int D>
+struct Jobs {
+  Walk<D> w;
+  int i, n;  // job in its segment, of n
+  __device__ __forceinline__ void begin() { i = 0, n = w.more ? (w.g.j1 - w.g.j0) * w.g.t.jobs : 0; }
+  __device__ __forceinline__ bool live() const { return w.more; }
+  __device__ __forceinline__ bool first_of_tile() const { return w.g.t.jobs == 1 || (i & 1) == 0; }
+  __device__ __forceinline__ bool last_of_tile() const { return w.g.t.jobs == 1 || (i & 1) == 1; }
+  __device__ __forceinline__ int row_tile() const { return w.g.t.jobs == 1 ? 0 : i & 1; }
+  __device__ __forceinline__ int key_tile() const { return w.g.j0 + (w.g.t.jobs == 1 ? i : i >> 1); }
+  __device__ __forceinline__ void next(const AttnCall& c, const AttnPlan& p) {
+    if (++i < n) return;
+    w.next(c, p);
+    begin();
+  }
+};
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// shared memory: [Q][ring], barriers
+constexpr int kBFull = 0, kBEmpty = kUnits, kBQFull = 2 * kUnits, kBQFree = kBQFull + 1, kBS = kBQFree + 1,
+              kBP = kBS + 4, kBO = kBP + 4, kBDrain = kBO + 2, kBars = kBDrain + 1;
+
+template <class T, int D>
+__global__ void __launch_bounds__(kThreads, 1) k_attn_many(AttnCall c, AttnPlan p, AttnParts parts) {
+  using C = Cfg<D>;
+  constexpr bool kBf = Half2<T>::kBf16;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ uint64_t bars[kBars];
+  __shared__ uint32_t s_tmem;
+  __shared__ volatile int s_flag;
+  const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u, ring0 = smem0 + C::kQBytes;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const AttnStep& st = c.st;
+  if (tid == 0) {
+    for (int i = 0; i < kUnits; ++i) mbar_init(&bars[kBFull + i], 1), mbar_init(&bars[kBEmpty + i], 1);
+    mbar_init(&bars[kBQFull], kLoadWarps);
+    mbar_init(&bars[kBQFree], 1);
+    for (int i = 0; i < 4; ++i) mbar_init(&bars[kBS + i], 1), mbar_init(&bars[kBP + i], 4);
+    for (int i = 0; i < 2; ++i) mbar_init(&bars[kBO + i], 1);
+    mbar_init(&bars[kBDrain], 1);
+    s_flag = 0;
+    mbar_fence_init();
+  }
+  if (warp == kMmaWarp) tc::alloc(&s_tmem, kTmemCols);
+  tc::fence_before();
+  __syncthreads();
+  tc::fence_after();
+  const uint32_t tmem = s_tmem;
+  pdl_wait();
+  pdl_trigger();
+
+  p.tiles = __ldg(p.first + st.n_seqs);
+  const int64_t total = p.tiles ? __ldg(p.before + p.tiles) * st.Hkv : 0;
+  // every block that works has at least two jobs, so that it has a key tile's start
+  const int64_t B = max((int64_t)1, min((int64_t)gridDim.x, total / 2));
+  const int64_t b = blockIdx.x;
+  const int64_t t0 = b < B ? total * b / B : 0, t1 = b < B ? total * (b + 1) / B : 0;
+
+  // bounded wait; false, with the block's flag and the error word set, once any wait gave up
+  auto wait = [&](int bar, uint32_t parity) -> bool {
+    if (mbar_try_wait(&bars[bar], parity)) return true;
+    if (s_flag) return false;
+    if (mbar_wait(&bars[bar], parity, kDefaultWaitNs)) return true;
+    s_flag = 1;
+    attn_report(st, kAttnTimeout);
+    return false;
+  };
+
+  auto wait_all = [&](int bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, wait(bar, parity)); };
+
+  if (warp < kMmaWarp) {
+    // ================= softmax: warpgroup wg has row tile wg of two, or (wg 0) the only one
+    const int wg = warp >> 2, row = tid & 127;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const float sc2 = c.scale * kLog2e;
+    Walk<D> w;
+    w.start(c, p, t0, t1);
+    int par = 0;                     // buffer of the segment's first job
+    uint32_t sph[2] = {0, 0};        // phases of this warpgroup's S barriers, by buffer
+    uint32_t opv = 0;                // products with V so far (phases of its O barrier)
+    int rec_n = 0;
+    bool alive = true;
+    for (; w.more && alive; w.next(c, p)) {
+      const Seg& g = w.g;
+      const int nj = g.j1 - g.j0, two = g.t.jobs == 2;
+      if (two || wg == 0) {
+        const int R = g.qt * C::kRows + wg * 128 + row, tok = R / st.G, pos = g.sp.len - g.sp.n + tok;
+        const bool ok = wg * 128 + row < g.t.rows;
+        const int lo = ok ? vis_lo(c, pos) : 0, hi = ok ? vis_hi(c, pos, g.sp.len) : 0;
+        const uint32_t col_o = tmem + lanes + kColO + (two ? wg * D : 0);
+        float m = -INFINITY, l = 0.f;
+        for (int j = 0; j < nj; ++j) {
+          const int buf = (par + (two ? wg : j)) & 1;
+          if (!(alive = wait_all(kBS + wg * 2 + buf, sph[buf] & 1))) break;
+          ++sph[buf];
+          __syncwarp();
+          tc::fence_after();
+          const uint32_t col_s = tmem + lanes + kColS + buf * 128;
+          float s[128];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tc::ld32(col_s + i * 32, reinterpret_cast<uint32_t*>(s) + i * 32);
+          tc::wait_ld();
+          const int k0 = g.t.start + (g.j0 + j) * kKeys, a = lo - k0, z = hi - k0;  // columns [a, z) are seen
+          if (__any_sync(0xffffffffu, a > 0 || z < kKeys)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int za = min(max(z - 32 * i, 0), 32), aa = min(max(a - 32 * i, 0), 32);
+              const uint32_t bits = (uint32_t)((1ull << za) - 1) & ~(uint32_t)((1ull << aa) - 1);
+#pragma unroll
+              for (int u = 0; u < 32; ++u) s[32 * i + u] = bits >> u & 1 ? s[32 * i + u] : -INFINITY;
+            }
+          }
+          float mx[4] = {m, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int i = 0; i < 128; i += 8)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) mx[u] = fmaxf(mx[u], fmaxf(s[i + 2 * u], s[i + 2 * u + 1]));
+          const float mn = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          bool waited = two || j == 0;  // two row tiles: S(g + 2) is formed after O(g)
+          if (j == 0) {
+            m = mn;
+          } else if (__any_sync(0xffffffffu, (mn - m) * sc2 > kGrow)) {
+            if (!waited) {
+              if (!(alive = wait_all(kBO + wg, (opv - 1) & 1))) break;
+              __syncwarp();
+              tc::fence_after();
+              waited = true;
+            }
+            const float f = mn == -INFINITY ? 1.f : ex2((m - mn) * sc2);
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) {
+              uint32_t o[32];
+              tc::ld32(col_o + i * 32, o);
+              tc::wait_ld();
+#pragma unroll
+              for (int u = 0; u < 32; ++u) o[u] = __float_as_uint(__uint_as_float(o[u]) * f);
+              tc::st32(col_o + i * 32, o);
+            }
+          }
+          const float ms = m == -INFINITY ? 0.f : m * sc2;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) {
+              const float e0 = ex2(fmaf(s[32 * i + 2 * u], sc2, -ms)), e1 = ex2(fmaf(s[32 * i + 2 * u + 1], sc2, -ms));
+              sum[u & 1] += e0, sum[2 + (u & 1)] += e1;
+              pk[u] = Half2<T>::down(e0, e1);
+            }
+            tc::st16(col_s + i * 16, pk);
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          tc::wait_st();
+          if (!waited && !(alive = wait_all(kBO + wg, (opv - 1) & 1))) break;  // keeps this barrier's phases in step
+          tc::fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars[kBP + wg * 2 + buf]);
+          ++opv;
+        }
+        if (!alive) break;
+        // ---- the piece's o
+        if (!(alive = wait_all(kBO + wg, (opv - 1) & 1))) break;
+        __syncwarp();
+        tc::fence_after();
+        const bool whole = g.j0 == 0 && g.j1 == g.t.nt;
+        const int64_t pr = ((int64_t)b * 2 + (g.j0 == 0)) * C::kRows + wg * 128 + row;
+        const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
+        const int head = g.h * st.G + R % st.G;
+        T* out = static_cast<T*>(c.out) + (int64_t)(g.sp.q0 + tok) * c.out_stride + (int64_t)head * D;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+          uint32_t o[32];
+          tc::ld32(col_o + i * 32, o);
+          tc::wait_ld();
+          if (!ok) continue;
+          if (whole) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              uint32_t v[4];
+#pragma unroll
+              for (int x = 0; x < 4; ++x)
+                v[x] = Half2<T>::down(__uint_as_float(o[8 * u + 2 * x]) * inv, __uint_as_float(o[8 * u + 2 * x + 1]) * inv);
+              *reinterpret_cast<uint4*>(out + i * 32 + u * 8) = make_uint4(v[0], v[1], v[2], v[3]);
+            }
+          } else {
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+              *reinterpret_cast<uint4*>(parts.o + pr * D + i * 32 + u * 4) =
+                  make_uint4(o[4 * u], o[4 * u + 1], o[4 * u + 2], o[4 * u + 3]);
+          }
+        }
+        if (ok) {
+          const float mm = m == -INFINITY ? m : m * sc2;
+          if (!whole) parts.ml[pr] = make_float2(mm, l);
+          else if (c.lse) c.lse[(int64_t)(g.sp.q0 + tok) * st.Hq + head] = l > 0.f ? (mm + log2f(l)) * kLn2 : -INFINITY;
+        }
+        if (tid == 0 && g.j0 == 0 && !whole) {
+          // the block of the segment's last key tile, by the place of its first job
+          const int64_t last = g.at + (int64_t)(g.t.nt - 1) * g.t.jobs;
+          rec_n = (int)((B * (last + 1) - 1) / total) - (int)b + 1;
+          parts.rec[b] = {g.sp.q0, g.h, g.qt * C::kRows, g.t.rows, rec_n};
+        }
+      }
+      par = (par + nj * g.t.jobs) & 1;
+    }
+    if (tid == 0 && rec_n == 0) parts.rec[b].n = 0;
+  } else if (warp == kMmaWarp) {
+    // ================= MMA issue: the whole warp walks the jobs, one elected lane issues
+    constexpr uint32_t kIdQk = tc::idesc_f16(kBf, 128, false), kNv = D == 64 ? 64 : 128,
+                       kIdPv = tc::idesc_f16(kBf, (int)kNv, true);
+    const uint32_t bars0 = __shfl_sync(0xffffffffu, smem_u32(bars), 0), tm = __shfl_sync(0xffffffffu, tmem, 0);
+    const uint32_t q0 = __shfl_sync(0xffffffffu, smem0, 0), r0 = __shfl_sync(0xffffffffu, ring0, 0);
+    Jobs<D> qk, pv;
+    qk.w.start(c, p, t0, t1);
+    qk.begin();
+    pv = qk;
+    uint32_t unit = 0, uph = 0;      // next ring unit to be used first, and its phase
+    uint32_t ku = 0, vu = 0;         // first unit of the current K and V tile
+    uint32_t gq = 0, gp = 0;         // jobs issued on either side: their buffers
+    uint32_t seg_ph = 0, pph[4] = {0, 0, 0, 0};
+    auto take = [&](uint32_t& first) -> bool {  // wait for the units of the next K or V tile
+      first = unit;
+      for (int i = 0; i < C::kU; ++i) {
+        if (!wait(kBFull + (int)unit, uph)) return false;
+        if (++unit == kUnits) unit = 0, uph ^= 1;
+      }
+      return true;
+    };
+    auto free_units = [&](uint32_t first) {
+      for (int i = 0; i < C::kU; ++i) {
+        const uint32_t u = first + i >= kUnits ? first + i - kUnits : first + i;
+        tc::commit(bars0 + (kBEmpty + u) * 8);
+      }
+    };
+    auto issue_qk = [&]() -> bool {
+      bool ok = qk.i != 0 || wait(kBQFull, seg_ph);
+      if (qk.i == 0) seg_ph ^= 1;
+      if (ok && qk.first_of_tile()) ok = take(ku);
+      if (!__all_sync(0xffffffffu, ok)) return false;
+      tc::fence_after();
+      const int x = qk.row_tile(), buf = gq & 1;
+      if (tc::elect_one()) {
+#pragma unroll
+        for (int u = 0; u < C::kU; ++u) {
+          const uint32_t un = ku + u >= kUnits ? ku + u - kUnits : ku + u;
+          const uint64_t a = tc::desc_sw128(q0 + (uint32_t)(x * C::kU + u) * kUnitBytes, 0),
+                         bd = tc::desc_sw128(r0 + un * kUnitBytes, 0);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)  // 16 elements: 32 bytes along the rows
+            tc::mma_ss(tm + kColS + buf * 128, a + k * 2, bd + k * 2, kIdQk, u + k > 0);
+        }
+        const int wg = qk.w.g.t.jobs == 2 ? x : 0;
+        tc::commit(bars0 + (kBS + wg * 2 + buf) * 8);
+        if (qk.last_of_tile()) free_units(ku);
+        if (qk.i == qk.n - 1) tc::commit(bars0 + kBQFree * 8);
+      }
+      __syncwarp();
+      ++gq;
+      qk.next(c, p);
+      return true;
+    };
+    bool ok = true;
+    for (int i = 0; i < 2 && ok && qk.live(); ++i) ok = issue_qk();
+    while (ok && pv.live()) {
+      const int two = pv.w.g.t.jobs == 2, x = pv.row_tile(), wg = two ? x : 0, buf = gp & 1;
+      if (pv.first_of_tile()) ok = take(vu);
+      ok = ok && wait(kBP + wg * 2 + buf, pph[wg * 2 + buf] & 1);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      ++pph[wg * 2 + buf];
+      tc::fence_after();
+      const uint32_t acc = pv.i >= (two ? 2 : 1);
+      if (tc::elect_one()) {
+#pragma unroll
+        for (int u = 0; u < C::kU; u += (D == 64 ? 1 : 2)) {
+          const uint32_t un = vu + u >= kUnits ? vu + u - kUnits : vu + u;
+          const uint64_t bd = tc::desc_sw128(r0 + un * kUnitBytes, kUnitBytes);
+#pragma unroll
+          for (int k = 0; k < 8; ++k)  // 16 lines: two groups of eight
+            tc::mma_ts(tm + kColO + (two ? x * D : 0) + u * 64, tm + kColS + buf * 128 + k * 8, bd + k * (2048 >> 4), kIdPv,
+                       acc | (k > 0));
+        }
+        tc::commit(bars0 + (kBO + wg) * 8);
+        if (pv.last_of_tile()) free_units(vu);
+      }
+      __syncwarp();
+      ++gp;
+      pv.next(c, p);
+      if (qk.live()) ok = issue_qk();
+    }
+    // nothing may be in flight when the tensor memory is freed
+    if (tc::elect_one()) tc::commit(bars0 + kBDrain * 8);
+    __syncwarp();
+    if (!mbar_wait(&bars[kBDrain], 0, kDefaultWaitNs)) attn_report(st, kAttnTimeout);
+  } else {
+    // ================= copies: the warps take the ring's units in turn, and Q's among them
+    const int me = warp - kLoadWarp0;
+    Jobs<D> qk, pv;
+    qk.w.start(c, p, t0, t1);
+    qk.begin();
+    pv = qk;
+    uint32_t unit = 0, uph = 1;  // next unit, and the parity of "it is free" (at first it is)
+    int turn = 0;                // unit count % kLoadWarps
+    uint32_t seg_ph = 1;
+    int pending = -1;            // barrier of the copies that are not announced yet
+    bool ok = true;
+    auto announce = [&](int left) {  // the copies of the pending barrier have landed once at most `left` groups fly
+      if (pending < 0) return;
+      if (left) asm volatile("cp.async.wait_group 1;" ::: "memory");
+      else asm volatile("cp.async.wait_group 0;" ::: "memory");
+      tc::fence_proxy();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars[pending]);
+      pending = -1;
+    };
+    auto wait_free = [&](int bar, uint32_t parity) -> bool {  // no copy stays unannounced while this warp sleeps
+      if (__all_sync(0xffffffffu, mbar_try_wait(&bars[bar], parity))) return true;
+      announce(0);
+      return __all_sync(0xffffffffu, wait(bar, parity));
+    };
+    auto copied = [&](int bar) {
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      announce(1);
+      pending = bar;
+    };
+    // 128 lines x 64 elements; `at`: element offsets of lines lane, lane + 32, ... (negative: a line of zeros)
+    auto copy_unit = [&](uint32_t dst, const T* base, const int64_t (&at)[4]) {
+      const int ch = lane & 7;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const int r = i * 4 + (lane >> 3);
+        const int64_t o = __shfl_sync(0xffffffffu, at[i >> 3], (i & 7) * 4 + (lane >> 3));
+        cp16(dst + r * 128 + ((ch ^ (r & 7)) << 4), base + (o < 0 ? 0 : o + ch * 8), o < 0 ? 0u : 16u);
+      }
+    };
+    auto load_tile = [&](const Jobs<D>& jb, const void* cache) {  // the units of a K or V tile
+      const Seg& g = jb.w.g;
+      const int k0 = g.t.start + jb.key_tile() * kKeys;
+      for (int u = 0; u < C::kU && ok; ++u) {
+        if (turn == me) {
+          int64_t at[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int line = k0 + i * 32 + lane;
+            at[i] = line < g.t.end ? line_offset(st, g.s, line) + (int64_t)g.h * st.head_stride : -1;
+          }
+          if (!(ok = wait_free(kBEmpty + (int)unit, uph))) return;
+          copy_unit(ring0 + unit * kUnitBytes, static_cast<const T*>(cache) + u * 64, at);
+          copied(kBFull + (int)unit);
+        }
+        if (++turn == kLoadWarps) turn = 0;
+        if (++unit == kUnits) unit = 0, uph ^= 1;
+      }
+    };
+    auto load_q = [&](const Seg& g) {
+      if (!(ok = wait_free(kBQFree, seg_ph))) return;
+      seg_ph ^= 1;
+      const int n = g.t.jobs * C::kU;
+      for (int v = me; v < n; v += kLoadWarps) {
+        const int x = v / C::kU, u = v % C::kU;
+        int64_t at[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = x * 128 + i * 32 + lane, R = g.qt * C::kRows + r;
+          at[i] = r < g.t.rows ? (int64_t)(g.sp.q0 + R / st.G) * c.q_stride + (int64_t)(g.h * st.G + R % st.G) * D : -1;
+        }
+        copy_unit(smem0 + (uint32_t)v * kUnitBytes, static_cast<const T*>(c.q) + u * 64, at);
+      }
+      copied(kBQFull);
+    };
+    auto on_qk = [&]() {
+      if (qk.i == 0) load_q(qk.w.g);
+      if (ok && qk.first_of_tile()) load_tile(qk, c.k);
+      qk.next(c, p);
+    };
+    for (int i = 0; i < 2 && ok && qk.live(); ++i) on_qk();
+    while (ok && pv.live()) {
+      if (pv.first_of_tile()) load_tile(pv, c.v);
+      pv.next(c, p);
+      if (ok && qk.live()) on_qk();
+    }
+    announce(0);
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  }
+  tc::fence_before();
+  __syncthreads();
+  tc::fence_after();
+  if (warp == kMmaWarp) tc::dealloc(tmem, kTmemCols);
+}
+
+template <class T, int D>
+cudaError_t run(const AttnCall& c, AttnPlan plan, const AttnParts& parts, int sms, cudaStream_t s) {
+  using C = Cfg<D>;
+  const int64_t rows = (int64_t)c.st.n_tokens * c.st.G;
+  const int64_t tiles = rows / C::kRows + c.st.n_seqs;
+  plan.max_tiles = tiles < plan.max_tiles ? (int)tiles : plan.max_tiles;
+  const int64_t most = tiles * c.st.Hkv * (((int64_t)c.st.cap + kKeys - 1) / kKeys);
+  const unsigned grid = (unsigned)(most < sms ? most : sms);
+  cudaError_t e = cudaFuncSetAttribute(k_attn_many<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
+  if (e == cudaSuccess) e = launch_pdl(false, k_attn_plan<D>, dim3(1), dim3(1024), 0, s, c, plan);
+  if (e == cudaSuccess) e = launch_pdl(true, k_attn_many<T, D>, dim3(grid), dim3(kThreads), C::kSmem, s, c, plan, parts);
+  if (e == cudaSuccess && grid > 1) e = launch_attn_join(c, parts, D, Half2<T>::kBf16, C::kRows, (int)grid, s);
+  return e;
+}
+
+}  // namespace
+
+int attn_tile_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
+
+cudaError_t launch_attn_many(const AttnCall& c, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
+                             cudaStream_t s) {
+  if (bf16)
+    return head_dim == 64    ? run<__nv_bfloat16, 64>(c, plan, parts, sms, s)
+           : head_dim == 128 ? run<__nv_bfloat16, 128>(c, plan, parts, sms, s)
+                             : run<__nv_bfloat16, 256>(c, plan, parts, sms, s);
+  return head_dim == 64    ? run<__half, 64>(c, plan, parts, sms, s)
+         : head_dim == 128 ? run<__half, 128>(c, plan, parts, sms, s)
+                           : run<__half, 256>(c, plan, parts, sms, s);
+}
+
+}  // namespace mf
