@@ -217,7 +217,7 @@ extern "C" int mf_attn_create(mf_attn_t** out, const mf_attn_shape_t* shape, int
   h->err = reinterpret_cast<unsigned*>(ws + o_err);
   h->parts = {reinterpret_cast<float*>(ws + o_o), reinterpret_cast<float2*>(ws + o_ml), reinterpret_cast<AttnRec*>(ws + o_rec)};
   h->plan = {reinterpret_cast<int*>(ws + o_first), reinterpret_cast<int*>(ws + o_seq), reinterpret_cast<int64_t*>(ws + o_before),
-             (int)tiles, 0};
+             (int)tiles};
   if (e == cudaSuccess) e = cudaMemset(h->err, 0, 256);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) {

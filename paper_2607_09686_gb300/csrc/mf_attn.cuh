@@ -129,7 +129,7 @@ struct AttnPlan {
   int* first;       // [max_seqs + 1]  first row tile of a sequence; then the number of tiles
   int* seq_of;      // [max_tiles]     the tile's sequence
   int64_t* before;  // [max_tiles + 1] jobs (of one kv head) before the tile
-  int max_tiles, tiles;
+  int max_tiles;
 };
 
 cudaError_t launch_attn_few(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int sms, cudaStream_t s);

@@ -133,92 +133,116 @@ struct Seg {
   int s, h, tile, qt, j0, j1;
   int64_t at;  // place of its first job in the list
 };
-// The walk over a block's segments.  The list is ordered by sequence, kv head, row tile.
-template <int D>
+// The walk over a block's segments.  The list is ordered by sequence, kv head, row tile.  Its steps are taken once a segment
+// and kept out of line: the roles' loops together have to fit the instruction cache (with everything inline two fifths
+// of the fetches missed and a job took five times as long).
 struct Walk {
   int64_t t0, t1;
   Seg g;
+  int tiles;
   bool more;  // g is a segment of this block
-
-  __device__ __forceinline__ void fill(const AttnCall& c, const AttnPlan& p) {
-    g.s = __ldg(p.seq_of + g.tile);
-    g.sp = seq_span(c.st, g.s);
-    g.qt = g.tile - __ldg(p.first + g.s);
-    g.t = tile_of<D>(c, g.sp, g.qt);
-    const int w = g.t.jobs;  // a key tile belongs to the block that its first job falls to
-    g.j0 = (int)max((int64_t)0, (t0 - g.at + w - 1) / w);
-    g.j1 = (int)min((int64_t)g.t.nt, (t1 - g.at + w - 1) / w);
-  }
-  __device__ __forceinline__ void advance(const AttnCall& c, const AttnPlan& p) {
+};
+template <int D>
+__device__ __forceinline__ void walk_fill(Walk& w, const AttnCall& c, const AttnPlan& p) {
+  Seg& g = w.g;
+  g.s = __ldg(p.seq_of + g.tile);
+  g.sp = seq_span(c.st, g.s);
+  g.qt = g.tile - __ldg(p.first + g.s);
+  g.t = tile_of<D>(c, g.sp, g.qt);
+  const int n = g.t.jobs;  // a key tile belongs to the block that its first job falls to
+  g.j0 = (int)max((int64_t)0, (w.t0 - g.at + n - 1) / n);
+  g.j1 = (int)min((int64_t)g.t.nt, (w.t1 - g.at + n - 1) / n);
+}
+template <int D>
+__device__ __noinline__ void walk_next(Walk& w, const AttnCall& c, const AttnPlan& p) {
+  Seg& g = w.g;
+  do {
     g.at += (int64_t)g.t.nt * g.t.jobs;
-    if (g.at >= t1) {
-      more = false;
+    if (g.at >= w.t1) {
+      w.more = false;
       return;
     }
-    const int first = __ldg(p.first + g.s);
-    int last = g.tile + 1;
-    // the sequence's tiles end where seq_of changes
-    if (last < p.tiles && __ldg(p.seq_of + last) == g.s) g.tile = last;
+    const int first = __ldg(p.first + g.s), end = __ldg(p.first + g.s + 1);
+    if (g.tile + 1 < end) ++g.tile;
     else if (++g.h < c.st.Hkv) g.tile = first;
-    else g.h = 0, g.tile = last;
-    fill(c, p);
+    else g.h = 0, g.tile = end;
+    walk_fill<D>(w, c, p);
+  } while (g.j0 >= g.j1);
+}
+template <int D>
+__device__ __noinline__ void walk_start(Walk& w, const AttnCall& c, const AttnPlan& p, int tiles, int64_t a, int64_t b) {
+  w.t0 = a, w.t1 = b, w.tiles = tiles;
+  w.more = a < b;
+  if (!w.more) return;
+  // the last tile whose sequence starts at or before a, then the kv head, then the tile
+  int lo = 0, hi = tiles - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    const int first = __ldg(p.first + __ldg(p.seq_of + mid));
+    if (__ldg(p.before + first) * c.st.Hkv <= a) lo = mid;
+    else hi = mid - 1;
   }
-  __device__ __forceinline__ void skip_empty(const AttnCall& c, const AttnPlan& p) {
-    while (more && g.j0 >= g.j1) advance(c, p);
+  const int first = __ldg(p.first + __ldg(p.seq_of + lo)), end = lo + 1;
+  const int64_t b0 = __ldg(p.before + first), len = __ldg(p.before + end) - b0;
+  w.g.h = (int)((a - b0 * c.st.Hkv) / len);
+  const int64_t head = b0 * c.st.Hkv + w.g.h * len;
+  lo = first, hi = end - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (head + __ldg(p.before + mid) - b0 <= a) lo = mid;
+    else hi = mid - 1;
   }
-  __device__ __forceinline__ void start(const AttnCall& c, const AttnPlan& p, int64_t a, int64_t b) {
-    t0 = a, t1 = b;
-    more = a < b;
-    if (!more) return;
-    // the last tile whose sequence starts at or before a, then the kv head, then the tile
-    int lo = 0, hi = p.tiles - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      const int first = __ldg(p.first + __ldg(p.seq_of + mid));
-      if (__ldg(p.before + first) * c.st.Hkv <= a) lo = mid;
-      else hi = mid - 1;
-    }
-    const int first = __ldg(p.first + __ldg(p.seq_of + lo)), end = lo + 1;
-    const int64_t b0 = __ldg(p.before + first), len = __ldg(p.before + end) - b0;
-    g.h = (int)((a - b0 * c.st.Hkv) / len);
-    const int64_t head = b0 * c.st.Hkv + g.h * len;
-    lo = first, hi = end - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (head + __ldg(p.before + mid) - b0 <= a) lo = mid;
-      else hi = mid - 1;
-    }
-    g.tile = lo;
-    g.at = head + __ldg(p.before + lo) - b0;
-    fill(c, p);
-    skip_empty(c, p);
-  }
-  __device__ __forceinline__ void next(const AttnCall& c, const AttnPlan& p) {
-    advance(c, p);
-    skip_empty(c, p);
-  }
-};
+  w.g.tile = lo;
+  w.g.at = head + __ldg(p.before + lo) - b0;
+  walk_fill<D>(w, c, p);
+  if (w.g.j0 >= w.g.j1) walk_next<D>(w, c, p);
+}
 
 // The jobs of the walk one by one: (key tile, row tile), row tile inner.
-template <int D>
 struct Jobs {
-  Walk<D> w;
-  int i, n;  // job in its segment, of n
-  __device__ __forceinline__ void begin() { i = 0, n = w.more ? (w.g.j1 - w.g.j0) * w.g.t.jobs : 0; }
-  __device__ __forceinline__ bool live() const { return w.more; }
-  __device__ __forceinline__ bool first_of_tile() const { return w.g.t.jobs == 1 || (i & 1) == 0; }
-  __device__ __forceinline__ bool last_of_tile() const { return w.g.t.jobs == 1 || (i & 1) == 1; }
-  __device__ __forceinline__ int row_tile() const { return w.g.t.jobs == 1 ? 0 : i & 1; }
-  __device__ __forceinline__ int key_tile() const { return w.g.j0 + (w.g.t.jobs == 1 ? i : i >> 1); }
-  __device__ __forceinline__ void next(const AttnCall& c, const AttnPlan& p) {
-    if (++i < n) return;
-    w.next(c, p);
-    begin();
+  int i, n, two;  // job in its segment, of n; two row tiles
+  bool live;
+  __device__ __forceinline__ void take(const Walk& w) {
+    live = w.more;
+    i = 0;
+    two = live && w.g.t.jobs == 2;
+    n = live ? (w.g.j1 - w.g.j0) * w.g.t.jobs : 0;
   }
+  __device__ __forceinline__ int row_tile() const { return two & i; }  // also: which of the tile's jobs
+  __device__ __forceinline__ bool first_of_tile() const { return !(two & i); }
+  __device__ __forceinline__ bool last_of_tile() const { return !two || (i & 1); }
+  __device__ __forceinline__ int key_tile() const { return i >> two; }  // from the segment's j0 on
 };
+
+// A wait whose first poll failed; false, with the block's flag and the error word set, once any wait gave up.
+__device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, volatile int* flag, unsigned* err) {
+  if (*flag) return false;
+  if (mbar_wait(bar, parity, kDefaultWaitNs)) return true;
+  *flag = 1;
+  atomicOr(err, kAttnTimeout);
+  return false;
+}
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+// 128 lines x 64 elements to `dst`, swizzled; a0..a3: element offsets of lines lane, lane + 32, ... (negative: a line of
+// zeros)
+template <class T>
+__device__ __noinline__ void copy_unit(uint32_t dst, const T* base, int64_t a0, int64_t a1, int64_t a2, int64_t a3) {
+  const int lane = threadIdx.x & 31, ch = lane & 7, sub = lane >> 3;
+  dst += sub * 128;
+  const uint32_t even = (uint32_t)(ch ^ sub) << 4, odd = (uint32_t)(ch ^ (sub + 4)) << 4;  // lines sub, sub + 4 of eight
+#pragma unroll 1
+  for (int q = 0; q < 4; ++q) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t o = __shfl_sync(0xffffffffu, a0, i * 4 + sub);
+      cp16(dst + i * 512 + (i & 1 ? odd : even), base + (o < 0 ? 0 : o + ch * 8), o < 0 ? 0u : 16u);
+    }
+    dst += 4096;
+    a0 = a1, a1 = a2, a2 = a3;
+  }
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -230,7 +254,8 @@ constexpr int kBFull = 0, kBEmpty = kUnits, kBQFull = 2 * kUnits, kBQFree = kBQF
               kBP = kBS + 4, kBO = kBP + 4, kBDrain = kBO + 2, kBars = kBDrain + 1;
 
 template <class T, int D>
-__global__ void __launch_bounds__(kThreads, 1) k_attn_many(AttnCall c, AttnPlan p, AttnParts parts) {
+__global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant__ AttnCall c, const __grid_constant__ AttnPlan p,
+                                                           const __grid_constant__ AttnParts parts) {
   using C = Cfg<D>;
   constexpr bool kBf = Half2<T>::kBf16;
   extern __shared__ unsigned char smem_raw[];
@@ -258,23 +283,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(AttnCall c, AttnPlan 
   pdl_wait();
   pdl_trigger();
 
-  p.tiles = __ldg(p.first + st.n_seqs);
-  const int64_t total = p.tiles ? __ldg(p.before + p.tiles) * st.Hkv : 0;
+  const int tiles = __ldg(p.first + st.n_seqs);
+  const int64_t total = tiles ? __ldg(p.before + tiles) * st.Hkv : 0;
   // every block that works has at least two jobs, so that it has a key tile's start
   const int64_t B = max((int64_t)1, min((int64_t)gridDim.x, total / 2));
   const int64_t b = blockIdx.x;
   const int64_t t0 = b < B ? total * b / B : 0, t1 = b < B ? total * (b + 1) / B : 0;
 
-  // bounded wait; false, with the block's flag and the error word set, once any wait gave up
-  auto wait = [&](int bar, uint32_t parity) -> bool {
-    if (mbar_try_wait(&bars[bar], parity)) return true;
-    if (s_flag) return false;
-    if (mbar_wait(&bars[bar], parity, kDefaultWaitNs)) return true;
-    s_flag = 1;
-    attn_report(st, kAttnTimeout);
-    return false;
+  auto wait = [&](int bar, uint32_t parity) -> bool {  // bounded
+    return mbar_try_wait(&bars[bar], parity) || wait_slow(&bars[bar], parity, &s_flag, st.err);
   };
-
   auto wait_all = [&](int bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, wait(bar, parity)); };
 
   if (warp < kMmaWarp) {
@@ -282,15 +300,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(AttnCall c, AttnPlan 
     const int wg = warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float sc2 = c.scale * kLog2e;
-    Walk<D> w;
-    w.start(c, p, t0, t1);
+    Walk w;
+    walk_start<D>(w, c, p, tiles, t0, t1);
     int par = 0;                     // buffer of the segment's first job
     uint32_t sph[2] = {0, 0};        // phases of this warpgroup's S barriers, by buffer
     uint32_t opv = 0;                // products with V so far (phases of its O barrier)
     int rec_n = 0;
     bool alive = true;
-    for (; w.more && alive; w.next(c, p)) {
-      const Seg& g = w.g;
+    for (; w.more && alive; walk_next<D>(w, c, p)) {
+      const Seg g = w.g;
       const int nj = g.j1 - g.j0, two = g.t.jobs == 2;
       if (two || wg == 0) {
         const int R = g.qt * C::kRows + wg * 128 + row, tok = R / st.G, pos = g.sp.len - g.sp.n + tok;
@@ -422,82 +440,87 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(AttnCall c, AttnPlan 
                        kIdPv = tc::idesc_f16(kBf, (int)kNv, true);
     const uint32_t bars0 = __shfl_sync(0xffffffffu, smem_u32(bars), 0), tm = __shfl_sync(0xffffffffu, tmem, 0);
     const uint32_t q0 = __shfl_sync(0xffffffffu, smem0, 0), r0 = __shfl_sync(0xffffffffu, ring0, 0);
-    Jobs<D> qk, pv;
-    qk.w.start(c, p, t0, t1);
-    qk.begin();
-    pv = qk;
+    Walk wq, wp;  // of the scores' side, two jobs ahead, and of the products' with V
+    walk_start<D>(wq, c, p, tiles, t0, t1);
+    wp = wq;
+    Jobs qk, pv;
+    qk.take(wq), pv.take(wp);
     uint32_t unit = 0, uph = 0;      // next ring unit to be used first, and its phase
     uint32_t ku = 0, vu = 0;         // first unit of the current K and V tile
-    uint32_t gq = 0, gp = 0;         // jobs issued on either side: their buffers
-    uint32_t seg_ph = 0, pph[4] = {0, 0, 0, 0};
+    uint32_t buf = 0;                // buffer of S and P: that of the jobs in turn
+    uint32_t seg_ph = 0, pph = 0;    // pph: phases of the four P barriers, a bit each
     auto take = [&](uint32_t& first) -> bool {  // wait for the units of the next K or V tile
       first = unit;
-      for (int i = 0; i < C::kU; ++i) {
-        if (!wait(kBFull + (int)unit, uph)) return false;
+      bool ok = true;
+#pragma unroll 1
+      for (int i = 0; i < C::kU && ok; ++i) {
+        ok = wait(kBFull + (int)unit, uph);
         if (++unit == kUnits) unit = 0, uph ^= 1;
       }
-      return true;
+      return ok;
     };
     auto free_units = [&](uint32_t first) {
-      for (int i = 0; i < C::kU; ++i) {
-        const uint32_t u = first + i >= kUnits ? first + i - kUnits : first + i;
-        tc::commit(bars0 + (kBEmpty + u) * 8);
-      }
-    };
-    auto issue_qk = [&]() -> bool {
-      bool ok = qk.i != 0 || wait(kBQFull, seg_ph);
-      if (qk.i == 0) seg_ph ^= 1;
-      if (ok && qk.first_of_tile()) ok = take(ku);
-      if (!__all_sync(0xffffffffu, ok)) return false;
-      tc::fence_after();
-      const int x = qk.row_tile(), buf = gq & 1;
-      if (tc::elect_one()) {
 #pragma unroll
-        for (int u = 0; u < C::kU; ++u) {
-          const uint32_t un = ku + u >= kUnits ? ku + u - kUnits : ku + u;
-          const uint64_t a = tc::desc_sw128(q0 + (uint32_t)(x * C::kU + u) * kUnitBytes, 0),
-                         bd = tc::desc_sw128(r0 + un * kUnitBytes, 0);
-#pragma unroll
-          for (int k = 0; k < 4; ++k)  // 16 elements: 32 bytes along the rows
-            tc::mma_ss(tm + kColS + buf * 128, a + k * 2, bd + k * 2, kIdQk, u + k > 0);
-        }
-        const int wg = qk.w.g.t.jobs == 2 ? x : 0;
-        tc::commit(bars0 + (kBS + wg * 2 + buf) * 8);
-        if (qk.last_of_tile()) free_units(ku);
-        if (qk.i == qk.n - 1) tc::commit(bars0 + kBQFree * 8);
-      }
-      __syncwarp();
-      ++gq;
-      qk.next(c, p);
-      return true;
+      for (int i = 0; i < C::kU; ++i) tc::commit(bars0 + (kBEmpty + (first + i >= kUnits ? first + i - kUnits : first + i)) * 8);
     };
     bool ok = true;
-    for (int i = 0; i < 2 && ok && qk.live(); ++i) ok = issue_qk();
-    while (ok && pv.live()) {
-      const int two = pv.w.g.t.jobs == 2, x = pv.row_tile(), wg = two ? x : 0, buf = gp & 1;
-      if (pv.first_of_tile()) ok = take(vu);
-      ok = ok && wait(kBP + wg * 2 + buf, pph[wg * 2 + buf] & 1);
-      if (!__all_sync(0xffffffffu, ok)) break;
-      ++pph[wg * 2 + buf];
-      tc::fence_after();
-      const uint32_t acc = pv.i >= (two ? 2 : 1);
-      if (tc::elect_one()) {
+#pragma unroll 1
+    for (int step = -2; pv.live; ++step, buf ^= 1) {
+      if (step >= 0) {  // O += P V of job `step`
+        const int x = pv.row_tile(), pb = x * 2 + (int)buf;
+        if (pv.first_of_tile()) ok = take(vu);
+        ok = ok && wait(kBP + pb, pph >> pb & 1);
+        if (!__all_sync(0xffffffffu, ok)) break;
+        pph ^= 1u << pb;
+        tc::fence_after();
+        const uint32_t acc = pv.i > pv.two;
+        if (tc::elect_one()) {
 #pragma unroll
-        for (int u = 0; u < C::kU; u += (D == 64 ? 1 : 2)) {
-          const uint32_t un = vu + u >= kUnits ? vu + u - kUnits : vu + u;
-          const uint64_t bd = tc::desc_sw128(r0 + un * kUnitBytes, kUnitBytes);
+          for (int u = 0; u < C::kU; u += (D == 64 ? 1 : 2)) {
+            const uint32_t un = vu + u >= kUnits ? vu + u - kUnits : vu + u;
+            const uint64_t bd = tc::desc_sw128(r0 + un * kUnitBytes, kUnitBytes);
 #pragma unroll
-          for (int k = 0; k < 8; ++k)  // 16 lines: two groups of eight
-            tc::mma_ts(tm + kColO + (two ? x * D : 0) + u * 64, tm + kColS + buf * 128 + k * 8, bd + k * (2048 >> 4), kIdPv,
-                       acc | (k > 0));
+            for (int k = 0; k < 8; ++k)  // 16 lines: two groups of eight
+              tc::mma_ts(tm + kColO + x * D + u * 64, tm + kColS + buf * 128 + k * 8, bd + k * (2048 >> 4), kIdPv, acc | (k > 0));
+          }
+          tc::commit(bars0 + (kBO + x) * 8);
+          if (pv.last_of_tile()) free_units(vu);
         }
-        tc::commit(bars0 + (kBO + wg) * 8);
-        if (pv.last_of_tile()) free_units(vu);
+        __syncwarp();
+        if (++pv.i == pv.n) {
+          walk_next<D>(wp, c, p);
+          pv.take(wp);
+        }
       }
-      __syncwarp();
-      ++gp;
-      pv.next(c, p);
-      if (qk.live()) ok = issue_qk();
+      if (qk.live) {  // S = Q K^T of job step + 2, into the buffer whose P is read by now
+        if (qk.i == 0) {
+          ok = wait(kBQFull, seg_ph);
+          seg_ph ^= 1;
+        }
+        if (ok && qk.first_of_tile()) ok = take(ku);
+        if (!__all_sync(0xffffffffu, ok)) break;
+        tc::fence_after();
+        const int x = qk.row_tile();
+        if (tc::elect_one()) {
+#pragma unroll
+          for (int u = 0; u < C::kU; ++u) {
+            const uint32_t un = ku + u >= kUnits ? ku + u - kUnits : ku + u;
+            const uint64_t a = tc::desc_sw128(q0 + (uint32_t)(x * C::kU + u) * kUnitBytes, 0),
+                           bd = tc::desc_sw128(r0 + un * kUnitBytes, 0);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)  // 16 elements: 32 bytes along the rows
+              tc::mma_ss(tm + kColS + buf * 128, a + k * 2, bd + k * 2, kIdQk, u + k > 0);
+          }
+          tc::commit(bars0 + (kBS + x * 2 + buf) * 8);
+          if (qk.last_of_tile()) free_units(ku);
+          if (qk.i == qk.n - 1) tc::commit(bars0 + kBQFree * 8);
+        }
+        __syncwarp();
+        if (++qk.i == qk.n) {
+          walk_next<D>(wq, c, p);
+          qk.take(wq);
+        }
+      }
     }
     // nothing may be in flight when the tensor memory is freed
     if (tc::elect_one()) tc::commit(bars0 + kBDrain * 8);
@@ -506,19 +529,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(AttnCall c, AttnPlan 
   } else {
     // ================= copies: the warps take the ring's units in turn, and Q's among them
     const int me = warp - kLoadWarp0;
-    Jobs<D> qk, pv;
-    qk.w.start(c, p, t0, t1);
-    qk.begin();
-    pv = qk;
+    Walk wk[2];  // [0] of the products with V, [1] of the scores, two jobs ahead
+    walk_start<D>(wk[0], c, p, tiles, t0, t1);
+    wk[1] = wk[0];
+    Jobs jb[2];
+    jb[0].take(wk[0]), jb[1].take(wk[1]);
     uint32_t unit = 0, uph = 1;  // next unit, and the parity of "it is free" (at first it is)
-    int turn = 0;                // unit count % kLoadWarps
+    int turn = me;               // units until this warp's next
     uint32_t seg_ph = 1;
     int pending = -1;            // barrier of the copies that are not announced yet
     bool ok = true;
-    auto announce = [&](int left) {  // the copies of the pending barrier have landed once at most `left` groups fly
+    auto announce = [&](bool last) {  // the copies of the pending barrier, once they have landed (last: the newest group's)
       if (pending < 0) return;
-      if (left) asm volatile("cp.async.wait_group 1;" ::: "memory");
-      else asm volatile("cp.async.wait_group 0;" ::: "memory");
+      if (last) asm volatile("cp.async.wait_group 0;" ::: "memory");
+      else asm volatile("cp.async.wait_group 1;" ::: "memory");
       tc::fence_proxy();
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars[pending]);
@@ -526,71 +550,64 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(AttnCall c, AttnPlan 
     };
     auto wait_free = [&](int bar, uint32_t parity) -> bool {  // no copy stays unannounced while this warp sleeps
       if (__all_sync(0xffffffffu, mbar_try_wait(&bars[bar], parity))) return true;
-      announce(0);
-      return __all_sync(0xffffffffu, wait(bar, parity));
+      announce(true);
+      return wait_all(bar, parity);
     };
     auto copied = [&](int bar) {
       asm volatile("cp.async.commit_group;" ::: "memory");
-      announce(1);
+      announce(false);
       pending = bar;
     };
-    // 128 lines x 64 elements; `at`: element offsets of lines lane, lane + 32, ... (negative: a line of zeros)
-    auto copy_unit = [&](uint32_t dst, const T* base, const int64_t (&at)[4]) {
-      const int ch = lane & 7;
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        const int r = i * 4 + (lane >> 3);
-        const int64_t o = __shfl_sync(0xffffffffu, at[i >> 3], (i & 7) * 4 + (lane >> 3));
-        cp16(dst + r * 128 + ((ch ^ (r & 7)) << 4), base + (o < 0 ? 0 : o + ch * 8), o < 0 ? 0u : 16u);
-      }
-    };
-    auto load_tile = [&](const Jobs<D>& jb, const void* cache) {  // the units of a K or V tile
-      const Seg& g = jb.w.g;
-      const int k0 = g.t.start + jb.key_tile() * kKeys;
-      for (int u = 0; u < C::kU && ok; ++u) {
-        if (turn == me) {
+#pragma unroll 1
+    for (int e = -3; ok; ++e) {  // events in the order of the MMAs: Q K^T of jobs 0, 1, then P V of g, Q K^T of g + 2, ...
+      const int side = e < 0 ? 1 : e & 1;
+      if (e == -1) continue;
+      if (side == 0 && !jb[0].live) break;
+      if (!jb[side].live) continue;
+      const Seg& g = wk[side].g;
+      if (side == 1 && jb[1].i == 0) {  // the segment's rows of q
+        if (!(ok = wait_free(kBQFree, seg_ph))) break;
+        seg_ph ^= 1;
+        const int n = g.t.jobs * C::kU;
+#pragma unroll 1
+        for (int v = me; v < n; v += kLoadWarps) {
           int64_t at[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const int line = k0 + i * 32 + lane;
-            at[i] = line < g.t.end ? line_offset(st, g.s, line) + (int64_t)g.h * st.head_stride : -1;
+            const int r = v / C::kU * 128 + i * 32 + lane, R = g.qt * C::kRows + r;
+            at[i] = r < g.t.rows ? (int64_t)(g.sp.q0 + R / st.G) * c.q_stride + (int64_t)(g.h * st.G + R % st.G) * D : -1;
           }
-          if (!(ok = wait_free(kBEmpty + (int)unit, uph))) return;
-          copy_unit(ring0 + unit * kUnitBytes, static_cast<const T*>(cache) + u * 64, at);
-          copied(kBFull + (int)unit);
+          copy_unit<T>(smem0 + (uint32_t)v * kUnitBytes, static_cast<const T*>(c.q) + v % C::kU * 64, at[0], at[1], at[2], at[3]);
         }
-        if (++turn == kLoadWarps) turn = 0;
-        if (++unit == kUnits) unit = 0, uph ^= 1;
+        copied(kBQFull);
       }
-    };
-    auto load_q = [&](const Seg& g) {
-      if (!(ok = wait_free(kBQFree, seg_ph))) return;
-      seg_ph ^= 1;
-      const int n = g.t.jobs * C::kU;
-      for (int v = me; v < n; v += kLoadWarps) {
-        const int x = v / C::kU, u = v % C::kU;
-        int64_t at[4];
+      if (jb[side].first_of_tile()) {  // the units of a K or V tile
+        const T* cache = static_cast<const T*>(side ? c.k : c.v);
+        const int k0 = g.t.start + (g.j0 + jb[side].key_tile()) * kKeys;
+#pragma unroll 1
+        for (int u = 0; u < C::kU; ++u) {
+          if (turn == 0) {
+            int64_t at[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = x * 128 + i * 32 + lane, R = g.qt * C::kRows + r;
-          at[i] = r < g.t.rows ? (int64_t)(g.sp.q0 + R / st.G) * c.q_stride + (int64_t)(g.h * st.G + R % st.G) * D : -1;
+            for (int i = 0; i < 4; ++i) {
+              const int line = k0 + i * 32 + lane;
+              at[i] = line < g.t.end ? line_offset(st, g.s, line) + (int64_t)g.h * st.head_stride : -1;
+            }
+            if (!(ok = wait_free(kBEmpty + (int)unit, uph))) break;
+            copy_unit<T>(ring0 + unit * kUnitBytes, cache + u * 64, at[0], at[1], at[2], at[3]);
+            copied(kBFull + (int)unit);
+            turn = kLoadWarps;
+          }
+          --turn;
+          if (++unit == kUnits) unit = 0, uph ^= 1;
         }
-        copy_unit(smem0 + (uint32_t)v * kUnitBytes, static_cast<const T*>(c.q) + u * 64, at);
       }
-      copied(kBQFull);
-    };
-    auto on_qk = [&]() {
-      if (qk.i == 0) load_q(qk.w.g);
-      if (ok && qk.first_of_tile()) load_tile(qk, c.k);
-      qk.next(c, p);
-    };
-    for (int i = 0; i < 2 && ok && qk.live(); ++i) on_qk();
-    while (ok && pv.live()) {
-      if (pv.first_of_tile()) load_tile(pv, c.v);
-      pv.next(c, p);
-      if (ok && qk.live()) on_qk();
+      if (++jb[side].i == jb[side].n) {
+        walk_next<D>(wk[side], c, p);
+        jb[side].take(wk[side]);
+      }
     }
-    announce(0);
+    announce(true);
     asm volatile("cp.async.wait_all;" ::: "memory");
   }
   tc::fence_before();
