@@ -285,8 +285,14 @@ extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, cons
   const int D = attn->shape.head_dim;
   const bool bf16 = attn->shape.dtype == MF_BF16;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = (int64_t)c.st.max_q * c.st.G <= kFewRows ? launch_attn_few(c, attn->parts, D, bf16, attn->sms, s)
-                                                                 : launch_attn_many(c, attn->plan, attn->parts, D, bf16, attn->sms, s);
+  cudaError_t e;
+  if ((int64_t)c.st.max_q * c.st.G <= kFewRows) {
+    e = launch_attn_few(c, attn->parts, D, bf16, attn->sms, s);
+  } else {
+    AttnMaps maps;
+    attn_maps(c, D, &maps);
+    e = launch_attn_many(c, maps, attn->plan, attn->parts, D, bf16, attn->sms, s);
+  }
   return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_attn_forward");
 }
 

@@ -77,6 +77,12 @@ struct AttnCall {
   int64_t q_stride, out_stride;
   float scale;
   int window, causal;
+  int box;  // lines of a tensor-map box (mf_attn_many.cu): a power of two that divides the page; 0: no tensor maps
+};
+
+// The caches as 4-D tensors (element, head, line, page), boxes of 64 elements x `box` lines, 128-byte swizzled.
+struct AttnMaps {
+  CUtensorMap k, v;
 };
 
 // The lines [lo, hi) that the token at line `pos` of a sequence of `len` lines sees.
@@ -133,7 +139,9 @@ struct AttnPlan {
 };
 
 cudaError_t launch_attn_few(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int sms, cudaStream_t s);
-cudaError_t launch_attn_many(const AttnCall& c, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
+// Fills `maps` and c.box where the cache can be described so (c.box = 0 where not).
+void attn_maps(AttnCall& c, int head_dim, AttnMaps* maps);
+cudaError_t launch_attn_many(const AttnCall& c, const AttnMaps& maps, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
                              cudaStream_t s);
 // the records of `blocks` blocks joined; rows: rows of a part
 cudaError_t launch_attn_join(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int rows, int blocks,

@@ -17,19 +17,24 @@
 // order in which the tensor cores work is S(0), S(1), then O(g), S(g + 2) for g = 0, 1, ..., across segments, so the next
 // segment's first scores run beside the last one's softmax.
 //
-// 12 warps: 0-3 and 4-7 softmax (thread = row; the maximum and the sum need no shuffles), 8 issues MMAs, 9-11 copy K, V and Q
-// lines with cp.async (a line's page is looked up per line, so any page size and stride will do; lines that no row of the
-// segment sees become zeros).  The ring holds units of 128 lines x 64 elements (16 KiB), ten of them beside Q.
+// 12 warps: 0-3 and 4-7 softmax (thread = row; the maximum and the sum need no shuffles), 8 issues MMAs, 9 copies K and V by
+// TMA, 10 and 11 copy Q, and K and V where TMA cannot: a box is as many lines as the largest power of two that divides the
+// page (8 to 128), and a tile that reaches past its sequence's lines (where anything may lie, NaN among it, which a product
+// with p = 0 would pass on) or before every window is copied line by line with cp.async, such lines becoming zeros.  So are
+// all tiles of pages that are no multiple of 8 lines.  The ring holds units of 128 lines x 64 elements (16 KiB), ten of them
+// beside Q.
 //
 // Split.  As for few rows: the step's jobs are one list shared out evenly over one block per SM; pieces of segments that
 // a block does not have whole are left as partials and joined in order.
+#include <cstring>
+
 #include "mf_attn.cuh"
 #include "mf_tc.cuh"
 
 namespace mf {
 namespace {
 
-constexpr int kThreads = 384, kMmaWarp = 8, kLoadWarp0 = 9, kLoadWarps = 3;
+constexpr int kThreads = 384, kMmaWarp = 8, kTmaWarp = 9, kCopyWarp0 = 10, kCopyWarps = 2;
 constexpr int kKeys = 128;                  // lines of a key tile
 constexpr uint32_t kUnitBytes = 128 * 128;  // 128 lines x 64 elements
 constexpr int kUnits = 10;
@@ -59,6 +64,7 @@ __device__ __forceinline__ Tile tile_of(const AttnCall& c, const SeqSpan& sp, in
   t.rows = min(Cfg<D>::kRows, sp.n * G - R0);
   const int first = sp.len - sp.n;
   t.start = vis_lo(c, first + R0 / G);
+  if (c.box) t.start &= ~(c.box - 1);
   t.end = max(0, vis_hi(c, first + (R0 + t.rows - 1) / G, sp.len));
   t.nt = max(1, (t.end - t.start + kKeys - 1) / kKeys);
   t.jobs = Cfg<D>::kRowTiles == 2 && t.rows > 128 ? 2 : 1;
@@ -131,6 +137,7 @@ struct Seg {
   SeqSpan sp;
   Tile t;
   int s, h, tile, qt, j0, j1;
+  int lo;      // the sequence's first line that any token of the step sees
   int64_t at;  // place of its first job in the list
 };
 // The walk over a block's segments.  The list is ordered by sequence, kv head, row tile.  Its steps are taken once a segment
@@ -149,6 +156,7 @@ __device__ __forceinline__ void walk_fill(Walk& w, const AttnCall& c, const Attn
   g.sp = seq_span(c.st, g.s);
   g.qt = g.tile - __ldg(p.first + g.s);
   g.t = tile_of<D>(c, g.sp, g.qt);
+  g.lo = vis_lo(c, g.sp.len - g.sp.n);
   const int n = g.t.jobs;  // a key tile belongs to the block that its first job falls to
   g.j0 = (int)max((int64_t)0, (w.t0 - g.at + n - 1) / n);
   g.j1 = (int)min((int64_t)g.t.nt, (w.t1 - g.at + n - 1) / n);
@@ -226,22 +234,29 @@ __device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, volatile 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, uint32_t bytes) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-// 128 lines x 64 elements to `dst`, swizzled; a0..a3: element offsets of lines lane, lane + 32, ... (negative: a line of
-// zeros)
+// 4-D tiled TMA load of the box at (element, head, line, page), completing on `bar`
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm, int x, int h, int line, int page, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+          dst),
+      "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(h), "r"(line), "r"(page), "r"(bar)
+      : "memory");
+}
+// 64 lines x 64 elements to `dst`, swizzled; a0, a1: element offsets of lines lane, lane + 32 (negative: a line of zeros)
 template <class T>
-__device__ __noinline__ void copy_unit(uint32_t dst, const T* base, int64_t a0, int64_t a1, int64_t a2, int64_t a3) {
+__device__ __noinline__ void copy_lines(uint32_t dst, const T* base, int64_t a0, int64_t a1) {
   const int lane = threadIdx.x & 31, ch = lane & 7, sub = lane >> 3;
   dst += sub * 128;
   const uint32_t even = (uint32_t)(ch ^ sub) << 4, odd = (uint32_t)(ch ^ (sub + 4)) << 4;  // lines sub, sub + 4 of eight
 #pragma unroll 1
-  for (int q = 0; q < 4; ++q) {
+  for (int q = 0; q < 2; ++q) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int64_t o = __shfl_sync(0xffffffffu, a0, i * 4 + sub);
       cp16(dst + i * 512 + (i & 1 ? odd : even), base + (o < 0 ? 0 : o + ch * 8), o < 0 ? 0u : 16u);
     }
     dst += 4096;
-    a0 = a1, a1 = a2, a2 = a3;
+    a0 = a1;
   }
 }
 __device__ __forceinline__ float ex2(float x) {
@@ -254,7 +269,8 @@ constexpr int kBFull = 0, kBEmpty = kUnits, kBQFull = 2 * kUnits, kBQFree = kBQF
               kBP = kBS + 4, kBO = kBP + 4, kBDrain = kBO + 2, kBars = kBDrain + 1;
 
 template <class T, int D>
-__global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant__ AttnCall c, const __grid_constant__ AttnPlan p,
+__global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant__ AttnCall c, const __grid_constant__ AttnMaps maps,
+                                                           const __grid_constant__ AttnPlan p,
                                                            const __grid_constant__ AttnParts parts) {
   using C = Cfg<D>;
   constexpr bool kBf = Half2<T>::kBf16;
@@ -266,8 +282,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const AttnStep& st = c.st;
   if (tid == 0) {
-    for (int i = 0; i < kUnits; ++i) mbar_init(&bars[kBFull + i], 1), mbar_init(&bars[kBEmpty + i], 1);
-    mbar_init(&bars[kBQFull], kLoadWarps);
+    // a unit is full when the TMA warp and both copying warps have done their part, which may be none: each of them
+    // sees every phase of every unit, so none can run ahead of the ring or fall behind it
+    for (int i = 0; i < kUnits; ++i) mbar_init(&bars[kBFull + i], 1 + kCopyWarps), mbar_init(&bars[kBEmpty + i], 1);
+    mbar_init(&bars[kBQFull], kCopyWarps);
     mbar_init(&bars[kBQFree], 1);
     for (int i = 0; i < 4; ++i) mbar_init(&bars[kBS + i], 1), mbar_init(&bars[kBP + i], 4);
     for (int i = 0; i < 2; ++i) mbar_init(&bars[kBO + i], 1);
@@ -527,88 +545,165 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     __syncwarp();
     if (!mbar_wait(&bars[kBDrain], 0, kDefaultWaitNs)) attn_report(st, kAttnTimeout);
   } else {
-    // ================= copies: the warps take the ring's units in turn, and Q's among them
-    const int me = warp - kLoadWarp0;
-    Walk wk[2];  // [0] of the products with V, [1] of the scores, two jobs ahead
-    walk_start<D>(wk[0], c, p, tiles, t0, t1);
-    wk[1] = wk[0];
-    Jobs jb[2];
-    jb[0].take(wk[0]), jb[1].take(wk[1]);
-    uint32_t unit = 0, uph = 1;  // next unit, and the parity of "it is free" (at first it is)
-    int turn = me;               // units until this warp's next
-    uint32_t seg_ph = 1;
-    int pending = -1;            // barrier of the copies that are not announced yet
-    bool ok = true;
-    auto announce = [&](bool last) {  // the copies of the pending barrier, once they have landed (last: the newest group's)
-      if (pending < 0) return;
-      if (last) asm volatile("cp.async.wait_group 0;" ::: "memory");
-      else asm volatile("cp.async.wait_group 1;" ::: "memory");
-      tc::fence_proxy();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bars[pending]);
-      pending = -1;
-    };
-    auto wait_free = [&](int bar, uint32_t parity) -> bool {  // no copy stays unannounced while this warp sleeps
-      if (__all_sync(0xffffffffu, mbar_try_wait(&bars[bar], parity))) return true;
-      announce(true);
-      return wait_all(bar, parity);
-    };
-    auto copied = [&](int bar) {
-      asm volatile("cp.async.commit_group;" ::: "memory");
-      announce(false);
-      pending = bar;
-    };
-#pragma unroll 1
-    for (int e = -3; ok; ++e) {  // events in the order of the MMAs: Q K^T of jobs 0, 1, then P V of g, Q K^T of g + 2, ...
-      const int side = e < 0 ? 1 : e & 1;
-      if (e == -1) continue;
-      if (side == 0 && !jb[0].live) break;
-      if (!jb[side].live) continue;
-      const Seg& g = wk[side].g;
-      if (side == 1 && jb[1].i == 0) {  // the segment's rows of q
-        if (!(ok = wait_free(kBQFree, seg_ph))) break;
-        seg_ph ^= 1;
-        const int n = g.t.jobs * C::kU;
-#pragma unroll 1
-        for (int v = me; v < n; v += kLoadWarps) {
-          int64_t at[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = v / C::kU * 128 + i * 32 + lane, R = g.qt * C::kRows + r;
-            at[i] = r < g.t.rows ? (int64_t)(g.sp.q0 + R / st.G) * c.q_stride + (int64_t)(g.h * st.G + R % st.G) * D : -1;
-          }
-          copy_unit<T>(smem0 + (uint32_t)v * kUnitBytes, static_cast<const T*>(c.q) + v % C::kU * 64, at[0], at[1], at[2], at[3]);
-        }
-        copied(kBQFull);
+    // ================= copies, in the order of the MMAs' first uses: (Q and) K of jobs 0 and 1, then V of job g, K of g + 2
+    struct Side {  // what a segment's K or V tiles need
+      Jobs jb;
+      int s, h, k0, lo, len, end;
+      __device__ __forceinline__ void take(const Walk& w) {
+        jb.take(w);
+        s = w.g.s, h = w.g.h, k0 = w.g.t.start + w.g.j0 * kKeys, lo = w.g.lo, len = w.g.sp.len, end = w.g.t.end;
       }
-      if (jb[side].first_of_tile()) {  // the units of a K or V tile
-        const T* cache = static_cast<const T*>(side ? c.k : c.v);
-        const int k0 = g.t.start + (g.j0 + jb[side].key_tile()) * kKeys;
+      // whether TMA copies the job's tile: all its lines are the sequence's, and seen by some token
+      __device__ __forceinline__ bool clean(int box) const {
+        const int a = k0 + jb.key_tile() * kKeys;
+        return box && a >= lo && a + kKeys <= len;
+      }
+    };
+    Walk wq, wp;
+    walk_start<D>(wq, c, p, tiles, t0, t1);
+    wp = wq;
+    Side qk, pv;
+    qk.take(wq), pv.take(wp);
+    uint32_t unit = 0, uph = 1;  // next unit, and the parity of "it is free" (at first it is)
+    bool ok = true;
+    if (warp == kTmaWarp) {
+      const uint32_t bars0 = smem_u32(bars);
+      const int n_box = c.box ? kKeys / c.box : 0;
+      auto tile = [&](const Side& sd, const CUtensorMap* tm) {
+        const bool mine = sd.clean(c.box);
+        int page = 0, line = 0;
+        if (mine && lane < n_box) {
+          const int at = sd.k0 + sd.jb.key_tile() * kKeys + lane * c.box;
+          const int pi = (int)fast_div((uint32_t)at, st.page_mul, st.page_shift);
+          const int raw = __ldg(st.pages + (int64_t)sd.s * st.pages_per_seq + pi);
+          page = min(max(raw, 0), st.n_pages - 1);
+          if (page != raw) attn_report(st, kAttnRange);
+          line = at - pi * st.page_size;
+        }
 #pragma unroll 1
         for (int u = 0; u < C::kU; ++u) {
-          if (turn == 0) {
-            int64_t at[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int line = k0 + i * 32 + lane;
-              at[i] = line < g.t.end ? line_offset(st, g.s, line) + (int64_t)g.h * st.head_stride : -1;
-            }
-            if (!(ok = wait_free(kBEmpty + (int)unit, uph))) break;
-            copy_unit<T>(ring0 + unit * kUnitBytes, cache + u * 64, at[0], at[1], at[2], at[3]);
-            copied(kBFull + (int)unit);
-            turn = kLoadWarps;
+          if (!(ok = wait_all(kBEmpty + (int)unit, uph))) return;
+          if (lane == 0) {
+            if (mine) mbar_arrive_tx(&bars[kBFull + unit], kUnitBytes);
+            else mbar_arrive(&bars[kBFull + unit]);
           }
-          --turn;
+          if (mine) {
+            __syncwarp();
+            if (lane < n_box)
+              tma_load_4d(ring0 + unit * kUnitBytes + lane * c.box * 128, tm, u * 64, sd.h, line, page, bars0 + (kBFull + unit) * 8);
+          }
           if (++unit == kUnits) unit = 0, uph ^= 1;
         }
+      };
+#pragma unroll 1
+      for (int g = -2; pv.jb.live; ++g) {
+        if (g >= 0) {
+          if (pv.jb.first_of_tile()) tile(pv, &maps.v);
+          if (++pv.jb.i == pv.jb.n) {
+            walk_next<D>(wp, c, p);
+            pv.take(wp);
+          }
+        }
+        if (!ok) break;
+        if (qk.jb.live) {
+          if (qk.jb.first_of_tile()) tile(qk, &maps.k);
+          if (++qk.jb.i == qk.jb.n) {
+            walk_next<D>(wq, c, p);
+            qk.take(wq);
+          }
+        }
+        if (!ok) break;
       }
-      if (++jb[side].i == jb[side].n) {
-        walk_next<D>(wk[side], c, p);
-        jb[side].take(wk[side]);
+      // no copy may be in flight when the block exits: the MMA warp has waited for every unit that it used, and uses all
+      // of them unless a wait gave up; then the last phases are waited for here
+      if (!ok)
+        for (int i = 0; i < kUnits; ++i) mbar_wait(&bars[kBFull + i], (i < (int)unit ? uph ^ 1 : uph), 1000000);
+    } else {
+      const int me = warp - kCopyWarp0;
+      uint32_t seg_ph = 1;
+      int pending = -1;  // barrier of the copies that are not announced yet
+      auto announce = [&](bool last) {  // the copies of the pending barrier, once they have landed (last: the newest group's)
+        if (pending < 0) return;
+        if (last) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        else asm volatile("cp.async.wait_group 1;" ::: "memory");
+        tc::fence_proxy();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[pending]);
+        pending = -1;
+      };
+      auto wait_free = [&](int bar, uint32_t parity) -> bool {  // no copy stays unannounced while this warp sleeps
+        if (__all_sync(0xffffffffu, mbar_try_wait(&bars[bar], parity))) return true;
+        announce(true);
+        return wait_all(bar, parity);
+      };
+      auto copied = [&](int bar) {
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        announce(false);
+        pending = bar;
+      };
+      auto tile = [&](const Side& sd, const void* cache) {
+        const bool skip = sd.clean(c.box);
+        int64_t at[2] = {-1, -1};
+        if (!skip) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int line = sd.k0 + sd.jb.key_tile() * kKeys + me * 64 + i * 32 + lane;
+            if (line >= sd.lo && line < sd.end) at[i] = line_offset(st, sd.s, line) + (int64_t)sd.h * st.head_stride;
+          }
+        }
+#pragma unroll 1
+        for (int u = 0; u < C::kU; ++u) {
+          if (!(ok = wait_free(kBEmpty + (int)unit, uph))) return;
+          if (skip) {
+            if (lane == 0) mbar_arrive(&bars[kBFull + unit]);
+          } else {
+            copy_lines<T>(ring0 + unit * kUnitBytes + me * 64 * 128, static_cast<const T*>(cache) + u * 64, at[0], at[1]);
+            copied(kBFull + (int)unit);
+          }
+          if (++unit == kUnits) unit = 0, uph ^= 1;
+        }
+      };
+      auto rows_of_q = [&](const Seg& g) {
+        if (!(ok = wait_free(kBQFree, seg_ph))) return;
+        seg_ph ^= 1;
+        const int n = 2 * g.t.jobs * C::kU;  // halves of units
+#pragma unroll 1
+        for (int v = me; v < n; v += kCopyWarps) {
+          const int x = (v >> 1) / C::kU, u = (v >> 1) % C::kU;
+          int64_t at[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int r = x * 128 + (v & 1) * 64 + i * 32 + lane, R = g.qt * C::kRows + r;
+            at[i] = r < g.t.rows ? (int64_t)(g.sp.q0 + R / st.G) * c.q_stride + (int64_t)(g.h * st.G + R % st.G) * D : -1;
+          }
+          copy_lines<T>(smem0 + (uint32_t)v * (kUnitBytes / 2), static_cast<const T*>(c.q) + u * 64, at[0], at[1]);
+        }
+        copied(kBQFull);
+        announce(true);
+      };
+#pragma unroll 1
+      for (int g = -2; pv.jb.live; ++g) {
+        if (g >= 0) {
+          if (pv.jb.first_of_tile()) tile(pv, c.v);
+          if (++pv.jb.i == pv.jb.n) {
+            walk_next<D>(wp, c, p);
+            pv.take(wp);
+          }
+        }
+        if (!ok) break;
+        if (qk.jb.live) {
+          if (qk.jb.i == 0) rows_of_q(wq.g);
+          if (ok && qk.jb.first_of_tile()) tile(qk, c.k);
+          if (++qk.jb.i == qk.jb.n) {
+            walk_next<D>(wq, c, p);
+            qk.take(wq);
+          }
+        }
+        if (!ok) break;
       }
+      announce(true);
+      asm volatile("cp.async.wait_all;" ::: "memory");
     }
-    announce(true);
-    asm volatile("cp.async.wait_all;" ::: "memory");
   }
   tc::fence_before();
   __syncthreads();
@@ -617,7 +712,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
 }
 
 template <class T, int D>
-cudaError_t run(const AttnCall& c, AttnPlan plan, const AttnParts& parts, int sms, cudaStream_t s) {
+cudaError_t run(const AttnCall& c, const AttnMaps& maps, AttnPlan plan, const AttnParts& parts, int sms, cudaStream_t s) {
   using C = Cfg<D>;
   const int64_t rows = (int64_t)c.st.n_tokens * c.st.G;
   const int64_t tiles = rows / C::kRows + c.st.n_seqs;
@@ -626,24 +721,51 @@ cudaError_t run(const AttnCall& c, AttnPlan plan, const AttnParts& parts, int sm
   const unsigned grid = (unsigned)(most < sms ? most : sms);
   cudaError_t e = cudaFuncSetAttribute(k_attn_many<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
   if (e == cudaSuccess) e = launch_pdl(false, k_attn_plan<D>, dim3(1), dim3(1024), 0, s, c, plan);
-  if (e == cudaSuccess) e = launch_pdl(true, k_attn_many<T, D>, dim3(grid), dim3(kThreads), C::kSmem, s, c, plan, parts);
+  if (e == cudaSuccess) e = launch_pdl(true, k_attn_many<T, D>, dim3(grid), dim3(kThreads), C::kSmem, s, c, maps, plan, parts);
   if (e == cudaSuccess && grid > 1) e = launch_attn_join(c, parts, D, Half2<T>::kBf16, C::kRows, (int)grid, s);
   return e;
 }
 
 }  // namespace
 
+void attn_maps(AttnCall& c, int head_dim, AttnMaps* maps) {
+  using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static const EncodeTiled encode = [] {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &q);
+    return e == cudaSuccess && q == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiled>(fn) : nullptr;
+  }();
+  memset(maps, 0, sizeof(*maps));
+  c.box = 0;
+  const AttnStep& st = c.st;
+  int box = kKeys;
+  while (st.page_size % box) box /= 2;
+  if (!encode || box < 8) return;
+  const cuuint64_t dims[4] = {(cuuint64_t)head_dim, (cuuint64_t)st.Hkv, (cuuint64_t)st.page_size, (cuuint64_t)st.n_pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)st.head_stride * 2, (cuuint64_t)st.token_stride * 2, (cuuint64_t)st.page_stride * 2};
+  const cuuint32_t boxes[4] = {64, 1, (cuuint32_t)box, 1}, ones[4] = {1, 1, 1, 1};
+  auto make = [&](CUtensorMap* tm, const void* base) {
+    return encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, const_cast<void*>(base), dims, strides, boxes, ones,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  if (make(&maps->k, c.k) && make(&maps->v, c.v)) c.box = box;
+}
+
 int attn_tile_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
 
-cudaError_t launch_attn_many(const AttnCall& c, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
+cudaError_t launch_attn_many(const AttnCall& c, const AttnMaps& maps, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
                              cudaStream_t s) {
   if (bf16)
-    return head_dim == 64    ? run<__nv_bfloat16, 64>(c, plan, parts, sms, s)
-           : head_dim == 128 ? run<__nv_bfloat16, 128>(c, plan, parts, sms, s)
-                             : run<__nv_bfloat16, 256>(c, plan, parts, sms, s);
-  return head_dim == 64    ? run<__half, 64>(c, plan, parts, sms, s)
-         : head_dim == 128 ? run<__half, 128>(c, plan, parts, sms, s)
-                           : run<__half, 256>(c, plan, parts, sms, s);
+    return head_dim == 64    ? run<__nv_bfloat16, 64>(c, maps, plan, parts, sms, s)
+           : head_dim == 128 ? run<__nv_bfloat16, 128>(c, maps, plan, parts, sms, s)
+                             : run<__nv_bfloat16, 256>(c, maps, plan, parts, sms, s);
+  return head_dim == 64    ? run<__half, 64>(c, maps, plan, parts, sms, s)
+         : head_dim == 128 ? run<__half, 128>(c, maps, plan, parts, sms, s)
+                           : run<__half, 256>(c, maps, plan, parts, sms, s);
 }
 
 }  // namespace mf

@@ -70,27 +70,32 @@ def attention64(c, scale, window=0, causal=True):
     tol, lse = torch.zeros_like(out), torch.full((c.tokens, c.hq), -math.inf, dtype=torch.float64, device="cuda")
     ltol = torch.zeros_like(lse)
     for s, n in enumerate(c.len):
-        k, v = (x[c.lines[s]].double() for x in (c.k, c.v))
-        for i in range(c.new[s]):
-            t, pos = c.start[s] + i, n - c.new[s] + i
-            lo = max(0, pos - window + 1) if window else 0
-            hi = min(n, pos + 1) if causal else n
-            if pos < 0:
-                hi = 0 if causal else n
-            if hi <= lo:
-                continue
-            q = c.q[t].double().view(c.hkv, c.hq // c.hkv, c.d)
-            x = torch.einsum("hgd,jhd->hgj", q, k[lo:hi]) * scale
-            mag = torch.einsum("hgd,jhd->hgj", q.abs(), k[lo:hi].abs()) * abs(scale)
+        lo = max(0, n - c.new[s] - window + 1) if window else 0  # lines before it may hold anything
+        k, v = (x[c.lines[s][0][lo:], c.lines[s][1][lo:]].double() for x in (c.k, c.v))
+        line = torch.arange(lo, n, device="cuda")
+        for i0 in range(0, c.new[s] if n else 0, 256):
+            i1 = min(i0 + 256, c.new[s])
+            t = slice(c.start[s] + i0, c.start[s] + i1)
+            pos = torch.arange(n - c.new[s] + i0, n - c.new[s] + i1, device="cuda")[:, None]
+            see = torch.ones(i1 - i0, n - lo, dtype=torch.bool, device="cuda")
+            if window:
+                see &= line > pos - window
+            if causal:
+                see &= line <= pos
+            num = see.sum(-1).double()[:, None, None]
+            q = c.q[t].double().unflatten(1, (c.hkv, c.hq // c.hkv))
+            x = torch.einsum("thgd,jhd->thgj", q, k) * scale
+            mag = (torch.einsum("thgd,jhd->thgj", q.abs(), k.abs()) * abs(scale)).masked_fill_(~see[:, None, None], 0)
+            x.masked_fill_(~see[:, None, None], -math.inf)
             z = torch.logsumexp(x, -1)
-            p = torch.exp(x - z[..., None])
-            o = torch.einsum("hgj,jhd->hgd", p, v[lo:hi])
-            rel = (c.d + 2) * 2.0 ** -24 * mag.amax(-1) + (hi - lo + 4) * 2.0 ** -24 + 2.0 ** -20
-            size = torch.einsum("hgj,jhd->hgd", p, v[lo:hi].abs())
-            tiny = (hi - lo) * 2.0 ** -25 * v[lo:hi].abs().amax() if c.dtype == "f16" else 0.0
-            out[t], lse[t] = o.reshape(c.hq, c.d), z.reshape(-1)
-            tol[t] = (u * (size + o.abs()) * 1.01 + 3 * rel[..., None] * size + tiny + 2.0 ** -24).reshape(c.hq, c.d)
-            ltol[t] = (2 * rel + 2.0 ** -22 * z.abs()).reshape(-1)
+            p = torch.exp(x - torch.where(z.isinf(), 0.0, z)[..., None])
+            o = torch.einsum("thgj,jhd->thgd", p, v)
+            rel = (c.d + 2) * 2.0 ** -24 * mag.amax(-1) + (num + 4) * 2.0 ** -24 + 2.0 ** -20
+            size = torch.einsum("thgj,jhd->thgd", p, v.abs())
+            tiny = num[..., None] * 2.0 ** -25 * v.abs().amax() if c.dtype == "f16" else 0.0
+            out[t], lse[t] = o.flatten(1, 2), z.flatten(1, 2)
+            tol[t] = (u * (size + o.abs()) * 1.01 + 3 * rel[..., None] * size + tiny + 2.0 ** -24).flatten(1, 2)
+            ltol[t] = (2 * rel + 2.0 ** -22 * z.abs()).flatten(1, 2).nan_to_num(0)
     return out, lse, tol, ltol
 
 

@@ -54,6 +54,14 @@ def test_chunks(mf, dtype, d, hq, hkv):
     check(mf, ref.Case([5, 1, 0, 130, 33, 64, 1], [0, 200, 9, 100, 31, 129, 0], hq, hkv, d, dtype))
 
 
+@pytest.mark.parametrize("page,heads_first", [(64, False), (16, True), (24, False), (5, False)])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_long_prompts(mf, d, page, heads_first):
+    """Blocks that walk many segments: tiles that are copied whole and by lines take turns in the ring."""
+    check(mf, ref.Case([1500, 3, 900, 1, 1999, 640], [0, 700, 37, 1300, 0, 2000], 16, 4, d, page=page, heads_first=heads_first))
+    check(mf, ref.Case([900, 1999], [300, 0], 16, 4, d, "f16", page=page, heads_first=heads_first), window=200)
+
+
 @pytest.mark.parametrize("new,ctx", [([1], [0]), ([1], [40000]), ([3], [9000]), ([700], [0]), ([257], [2000]), ([16], [112])])
 @pytest.mark.parametrize("d", [64, 128, 256])
 def test_one_sequence(mf, new, ctx, d):
