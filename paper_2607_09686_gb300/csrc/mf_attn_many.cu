@@ -21,8 +21,8 @@
 // TMA, 10 and 11 copy Q, and K and V where TMA cannot: a box is as many lines as the largest power of two that divides the
 // page (8 to 128), and a tile that reaches past its sequence's lines (where anything may lie, NaN among it, which a product
 // with p = 0 would pass on) or before every window is copied line by line with cp.async, such lines becoming zeros.  So are
-// all tiles of pages that are no multiple of 8 lines.  The ring holds units of 128 lines x 64 elements (16 KiB), ten of them
-// beside Q.
+// all tiles of pages that are no multiple of 8 lines.  The ring holds 160 KiB beside Q, in
+// slots of 128 lines x 64 elements (head_dim 64) or 128.
 //
 // Split.  As for few rows: the step's jobs are one list shared out evenly over one block per SM; pieces of segments that
 // a block does not have whole are left as partials and joined in order.
@@ -44,6 +44,9 @@ constexpr float kGrow = 8.f;  // growth of the maximum (log2) that o is rescaled
 template <int D>
 struct Cfg {
   static constexpr int kU = D / 64;                   // units of a K or V tile
+  static constexpr int kSlotU = D == 64 ? 1 : 2;      // units of a ring slot: what one barrier and one PV product cover
+  static constexpr int kSlots = kUnits / kSlotU, kTileSlots = kU / kSlotU;
+  static constexpr uint32_t kSlotBytes = kSlotU * kUnitBytes;
   static constexpr int kRowTiles = D == 256 ? 1 : 2;  // row tiles of a segment
   static constexpr int kRows = kRowTiles * 128;
   static constexpr uint32_t kQBytes = kRowTiles * kU * kUnitBytes;
@@ -282,9 +285,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const AttnStep& st = c.st;
   if (tid == 0) {
-    // a unit is full when the TMA warp and both copying warps have done their part, which may be none: each of them
-    // sees every phase of every unit, so none can run ahead of the ring or fall behind it
-    for (int i = 0; i < kUnits; ++i) mbar_init(&bars[kBFull + i], 1 + kCopyWarps), mbar_init(&bars[kBEmpty + i], 1);
+    // a slot is full when the TMA warp and both copying warps have done their part, which may be none: each of them
+    // sees every phase of every slot, so none can run ahead of the ring or fall behind it
+    for (int i = 0; i < C::kSlots; ++i) mbar_init(&bars[kBFull + i], 1 + kCopyWarps), mbar_init(&bars[kBEmpty + i], 1);
     mbar_init(&bars[kBQFull], kCopyWarps);
     mbar_init(&bars[kBQFree], 1);
     for (int i = 0; i < 4; ++i) mbar_init(&bars[kBS + i], 1), mbar_init(&bars[kBP + i], 4);
@@ -322,7 +325,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     walk_start<D>(w, c, p, tiles, t0, t1);
     int par = 0;                     // buffer of the segment's first job
     uint32_t sph[2] = {0, 0};        // phases of this warpgroup's S barriers, by buffer
-    uint32_t opv = 0;                // products with V so far (phases of its O barrier)
+    uint32_t oph = 0;                // phase of its O barrier
     int rec_n = 0;
     bool alive = true;
     for (; w.more && alive; walk_next<D>(w, c, p)) {
@@ -338,7 +341,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           const int buf = (par + (two ? wg : j)) & 1;
           if (!(alive = wait_all(kBS + wg * 2 + buf, sph[buf] & 1))) break;
           ++sph[buf];
-          __syncwarp();
           tc::fence_after();
           const uint32_t col_s = tmem + lanes + kColS + buf * 128;
           float s[128];
@@ -366,8 +368,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
             m = mn;
           } else if (__any_sync(0xffffffffu, (mn - m) * sc2 > kGrow)) {
             if (!waited) {
-              if (!(alive = wait_all(kBO + wg, (opv - 1) & 1))) break;
-              __syncwarp();
+              if (!(alive = wait_all(kBO + wg, oph))) break;
+              oph ^= 1;
               tc::fence_after();
               waited = true;
             }
@@ -385,30 +387,37 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
             }
           }
           const float ms = m == -INFINITY ? 0.f : m * sc2;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+          const uint64_t sc2x2 = tc::pack2(sc2, sc2), nms2 = tc::pack2(-ms, -ms);
+          uint64_t sum[2] = {0, 0};
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             uint32_t pk[16];
 #pragma unroll
             for (int u = 0; u < 16; ++u) {
-              const float e0 = ex2(fmaf(s[32 * i + 2 * u], sc2, -ms)), e1 = ex2(fmaf(s[32 * i + 2 * u + 1], sc2, -ms));
-              sum[u & 1] += e0, sum[2 + (u & 1)] += e1;
+              float e0, e1;
+              tc::unpack2(tc::fma2(tc::pack2(s[32 * i + 2 * u], s[32 * i + 2 * u + 1]), sc2x2, nms2), e0, e1);
+              e0 = ex2(e0), e1 = ex2(e1);
+              sum[u & 1] = tc::add2(sum[u & 1], tc::pack2(e0, e1));
               pk[u] = Half2<T>::down(e0, e1);
             }
             tc::st16(col_s + i * 16, pk);
           }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          float l0, l1;
+          tc::unpack2(tc::add2(sum[0], sum[1]), l0, l1);
+          l += l0 + l1;
           tc::wait_st();
-          if (!waited && !(alive = wait_all(kBO + wg, (opv - 1) & 1))) break;  // keeps this barrier's phases in step
+          if (!waited) {  // keeps this barrier's phases in step
+            if (!(alive = wait_all(kBO + wg, oph))) break;
+            oph ^= 1;
+          }
           tc::fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&bars[kBP + wg * 2 + buf]);
-          ++opv;
         }
         if (!alive) break;
         // ---- the piece's o
-        if (!(alive = wait_all(kBO + wg, (opv - 1) & 1))) break;
-        __syncwarp();
+        if (!(alive = wait_all(kBO + wg, oph))) break;
+        oph ^= 1;
         tc::fence_after();
         const bool whole = g.j0 == 0 && g.j1 == g.t.nt;
         const int64_t pr = ((int64_t)b * 2 + (g.j0 == 0)) * C::kRows + wg * 128 + row;
@@ -463,46 +472,50 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     wp = wq;
     Jobs qk, pv;
     qk.take(wq), pv.take(wp);
-    uint32_t unit = 0, uph = 0;      // next ring unit to be used first, and its phase
-    uint32_t ku = 0, vu = 0;         // first unit of the current K and V tile
+    uint32_t slot = 0, sph = 0;      // next ring slot to be used first, and its phase
+    uint32_t ks = 0, vs = 0;         // first slot of the current K and V tile
     uint32_t buf = 0;                // buffer of S and P: that of the jobs in turn
     uint32_t seg_ph = 0, pph = 0;    // pph: phases of the four P barriers, a bit each
-    auto take = [&](uint32_t& first) -> bool {  // wait for the units of the next K or V tile
-      first = unit;
+    auto take = [&](uint32_t& first) -> bool {  // wait for the slots of the next K or V tile
+      first = slot;
       bool ok = true;
-#pragma unroll 1
-      for (int i = 0; i < C::kU && ok; ++i) {
-        ok = wait(kBFull + (int)unit, uph);
-        if (++unit == kUnits) unit = 0, uph ^= 1;
+#pragma unroll
+      for (int i = 0; i < C::kTileSlots; ++i) {
+        ok = ok && wait_all(kBFull + (int)slot, sph);
+        if (++slot == C::kSlots) slot = 0, sph ^= 1;
       }
       return ok;
     };
-    auto free_units = [&](uint32_t first) {
-#pragma unroll
-      for (int i = 0; i < C::kU; ++i) tc::commit(bars0 + (kBEmpty + (first + i >= kUnits ? first + i - kUnits : first + i)) * 8);
-    };
-    bool ok = true;
+    // operands of an MMA come from uniform registers: what they derive from is read from one lane, so that the compiler
+    // knows it to be uniform (moved there one by one they cost as much as the products)
+    auto uniform = [](uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); };
+    auto slot_of = [](uint32_t first, int i) { return first + i >= C::kSlots ? first + i - C::kSlots : first + i; };
 #pragma unroll 1
     for (int step = -2; pv.live; ++step, buf ^= 1) {
       if (step >= 0) {  // O += P V of job `step`
-        const int x = pv.row_tile(), pb = x * 2 + (int)buf;
-        if (pv.first_of_tile()) ok = take(vu);
-        ok = ok && wait(kBP + pb, pph >> pb & 1);
-        if (!__all_sync(0xffffffffu, ok)) break;
+        const int pb = pv.row_tile() * 2 + (int)buf;
+        bool ok = true;
+        if (pv.first_of_tile()) ok = take(vs);
+        ok = ok && wait_all(kBP + pb, pph >> pb & 1);
+        if (!ok) break;
         pph ^= 1u << pb;
         tc::fence_after();
-        const uint32_t acc = pv.i > pv.two;
+        const uint32_t x = uniform(pv.row_tile()), b_ = uniform(buf), first = uniform(vs), acc = uniform(pv.i > pv.two);
+        // two row tiles: only their last product is waited for (S(g + 2) is formed after O(g)), else each one
+        const uint32_t tell = uniform(!pv.two || pv.i + 2 >= pv.n), last = uniform(pv.last_of_tile());
         if (tc::elect_one()) {
 #pragma unroll
-          for (int u = 0; u < C::kU; u += (D == 64 ? 1 : 2)) {
-            const uint32_t un = vu + u >= kUnits ? vu + u - kUnits : vu + u;
-            const uint64_t bd = tc::desc_sw128(r0 + un * kUnitBytes, kUnitBytes);
+          for (int u = 0; u < C::kTileSlots; ++u) {
+            const uint64_t bd = tc::desc_sw128(r0 + slot_of(first, u) * C::kSlotBytes, kUnitBytes);
 #pragma unroll
             for (int k = 0; k < 8; ++k)  // 16 lines: two groups of eight
-              tc::mma_ts(tm + kColO + x * D + u * 64, tm + kColS + buf * 128 + k * 8, bd + k * (2048 >> 4), kIdPv, acc | (k > 0));
+              tc::mma_ts(tm + kColO + x * D + u * 128, tm + kColS + b_ * 128 + k * 8, bd + k * (2048 >> 4), kIdPv, acc | (k > 0));
           }
-          tc::commit(bars0 + (kBO + x) * 8);
-          if (pv.last_of_tile()) free_units(vu);
+          if (tell) tc::commit(bars0 + (kBO + x) * 8);
+          if (last) {
+#pragma unroll
+            for (int u = 0; u < C::kTileSlots; ++u) tc::commit(bars0 + (kBEmpty + slot_of(first, u)) * 8);
+          }
         }
         __syncwarp();
         if (++pv.i == pv.n) {
@@ -511,27 +524,31 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         }
       }
       if (qk.live) {  // S = Q K^T of job step + 2, into the buffer whose P is read by now
+        bool ok = true;
         if (qk.i == 0) {
-          ok = wait(kBQFull, seg_ph);
+          ok = wait_all(kBQFull, seg_ph);
           seg_ph ^= 1;
         }
-        if (ok && qk.first_of_tile()) ok = take(ku);
-        if (!__all_sync(0xffffffffu, ok)) break;
+        if (qk.first_of_tile()) ok = ok && take(ks);
+        if (!ok) break;
         tc::fence_after();
-        const int x = qk.row_tile();
+        const uint32_t x = uniform(qk.row_tile()), b_ = uniform(buf), first = uniform(ks), end = uniform(qk.i == qk.n - 1),
+                       last = uniform(qk.last_of_tile());
         if (tc::elect_one()) {
 #pragma unroll
           for (int u = 0; u < C::kU; ++u) {
-            const uint32_t un = ku + u >= kUnits ? ku + u - kUnits : ku + u;
-            const uint64_t a = tc::desc_sw128(q0 + (uint32_t)(x * C::kU + u) * kUnitBytes, 0),
-                           bd = tc::desc_sw128(r0 + un * kUnitBytes, 0);
+            const uint64_t a = tc::desc_sw128(q0 + (x * C::kU + u) * kUnitBytes, 0),
+                           bd = tc::desc_sw128(r0 + slot_of(first, u / C::kSlotU) * C::kSlotBytes + u % C::kSlotU * kUnitBytes, 0);
 #pragma unroll
             for (int k = 0; k < 4; ++k)  // 16 elements: 32 bytes along the rows
-              tc::mma_ss(tm + kColS + buf * 128, a + k * 2, bd + k * 2, kIdQk, u + k > 0);
+              tc::mma_ss(tm + kColS + b_ * 128, a + k * 2, bd + k * 2, kIdQk, u + k > 0);
           }
-          tc::commit(bars0 + (kBS + x * 2 + buf) * 8);
-          if (qk.last_of_tile()) free_units(ku);
-          if (qk.i == qk.n - 1) tc::commit(bars0 + kBQFree * 8);
+          tc::commit(bars0 + (kBS + x * 2 + b_) * 8);
+          if (last) {
+#pragma unroll
+            for (int u = 0; u < C::kTileSlots; ++u) tc::commit(bars0 + (kBEmpty + slot_of(first, u)) * 8);
+          }
+          if (end) tc::commit(bars0 + kBQFree * 8);
         }
         __syncwarp();
         if (++qk.i == qk.n) {
@@ -564,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     wp = wq;
     Side qk, pv;
     qk.take(wq), pv.take(wp);
-    uint32_t unit = 0, uph = 1;  // next unit, and the parity of "it is free" (at first it is)
+    uint32_t slot = 0, sph = 1;  // next slot, and the parity of "it is free" (at first it is)
     bool ok = true;
     if (warp == kTmaWarp) {
       const uint32_t bars0 = smem_u32(bars);
@@ -572,8 +589,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
       auto tile = [&](const Side& sd, const CUtensorMap* tm) {
         const bool mine = sd.clean(c.box);
         int page = 0, line = 0;
-        if (mine && lane < n_box) {
-          const int at = sd.k0 + sd.jb.key_tile() * kKeys + lane * c.box;
+        const int un = lane / max(n_box, 1), bx = lane - un * n_box;  // lane: box bx of unit un of the slot
+        if (mine && un < C::kSlotU) {
+          const int at = sd.k0 + sd.jb.key_tile() * kKeys + bx * c.box;
           const int pi = (int)fast_div((uint32_t)at, st.page_mul, st.page_shift);
           const int raw = __ldg(st.pages + (int64_t)sd.s * st.pages_per_seq + pi);
           page = min(max(raw, 0), st.n_pages - 1);
@@ -581,18 +599,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           line = at - pi * st.page_size;
         }
 #pragma unroll 1
-        for (int u = 0; u < C::kU; ++u) {
-          if (!(ok = wait_all(kBEmpty + (int)unit, uph))) return;
+        for (int u = 0; u < C::kTileSlots; ++u) {
+          if (!(ok = wait_all(kBEmpty + (int)slot, sph))) return;
           if (lane == 0) {
-            if (mine) mbar_arrive_tx(&bars[kBFull + unit], kUnitBytes);
-            else mbar_arrive(&bars[kBFull + unit]);
+            if (mine) mbar_arrive_tx(&bars[kBFull + slot], C::kSlotBytes);
+            else mbar_arrive(&bars[kBFull + slot]);
           }
           if (mine) {
             __syncwarp();
-            if (lane < n_box)
-              tma_load_4d(ring0 + unit * kUnitBytes + lane * c.box * 128, tm, u * 64, sd.h, line, page, bars0 + (kBFull + unit) * 8);
+            if (un < C::kSlotU)
+              tma_load_4d(ring0 + slot * C::kSlotBytes + un * kUnitBytes + bx * c.box * 128, tm, (u * C::kSlotU + un) * 64, sd.h,
+                          line, page, bars0 + (kBFull + slot) * 8);
           }
-          if (++unit == kUnits) unit = 0, uph ^= 1;
+          if (++slot == C::kSlots) slot = 0, sph ^= 1;
         }
       };
 #pragma unroll 1
@@ -614,10 +633,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         }
         if (!ok) break;
       }
-      // no copy may be in flight when the block exits: the MMA warp has waited for every unit that it used, and uses all
+      // no copy may be in flight when the block exits: the MMA warp has waited for every slot that it used, and uses all
       // of them unless a wait gave up; then the last phases are waited for here
       if (!ok)
-        for (int i = 0; i < kUnits; ++i) mbar_wait(&bars[kBFull + i], (i < (int)unit ? uph ^ 1 : uph), 1000000);
+        for (int i = 0; i < C::kSlots; ++i) mbar_wait(&bars[kBFull + i], (i < (int)slot ? sph ^ 1 : sph), 1000000);
     } else {
       const int me = warp - kCopyWarp0;
       uint32_t seg_ph = 1;
@@ -652,15 +671,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           }
         }
 #pragma unroll 1
-        for (int u = 0; u < C::kU; ++u) {
-          if (!(ok = wait_free(kBEmpty + (int)unit, uph))) return;
+        for (int u = 0; u < C::kTileSlots; ++u) {
+          if (!(ok = wait_free(kBEmpty + (int)slot, sph))) return;
           if (skip) {
-            if (lane == 0) mbar_arrive(&bars[kBFull + unit]);
+            if (lane == 0) mbar_arrive(&bars[kBFull + slot]);
           } else {
-            copy_lines<T>(ring0 + unit * kUnitBytes + me * 64 * 128, static_cast<const T*>(cache) + u * 64, at[0], at[1]);
-            copied(kBFull + (int)unit);
+#pragma unroll 1
+            for (int x = 0; x < C::kSlotU; ++x)
+              copy_lines<T>(ring0 + slot * C::kSlotBytes + x * kUnitBytes + me * 64 * 128,
+                            static_cast<const T*>(cache) + (u * C::kSlotU + x) * 64, at[0], at[1]);
+            copied(kBFull + (int)slot);
           }
-          if (++unit == kUnits) unit = 0, uph ^= 1;
+          if (++slot == C::kSlots) slot = 0, sph ^= 1;
         }
       };
       auto rows_of_q = [&](const Seg& g) {
