@@ -78,11 +78,13 @@ struct AttnCall {
   float scale;
   int window, causal;
   int box;  // lines of a tensor-map box (mf_attn_many.cu): a power of two that divides the page; 0: no tensor maps
+  int q_box;  // Q has a tensor map
 };
 
 // The caches as 4-D tensors (element, head, line, page), boxes of 64 elements x `box` lines, 128-byte swizzled.
+// Q as a 3-D tensor (element, head, token), boxes of 64 elements x a group's heads x 128 / G tokens.
 struct AttnMaps {
-  CUtensorMap k, v;
+  CUtensorMap k, v, q;
 };
 
 // The lines [lo, hi) that the token at line `pos` of a sequence of `len` lines sees.
@@ -121,7 +123,7 @@ struct AttnRec {
 // What blocks leave of work that they do not have whole.  Block b's last piece, where it starts the work, is part
 // 2b + 1 and rec[b] describes it; the pieces that go on with it are parts 2(b + 1), 2(b + 2), ...
 struct AttnParts {
-  float* o;     // [parts][rows][head_dim], not yet divided by l
+  float* o;     // [parts][rows][head_dim] (16 rows) or [parts][head_dim / 4][rows][4] (tiles), not yet divided by l
   float2* ml;   // [parts][rows]  running maximum (log2 domain) and sum
   AttnRec* rec;  // [blocks]
 };
@@ -139,7 +141,7 @@ struct AttnPlan {
 };
 
 cudaError_t launch_attn_few(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int sms, cudaStream_t s);
-// Fills `maps` and c.box where the cache can be described so (c.box = 0 where not).
+// Fills `maps`, c.box and c.q_box where the cache and Q can be described so (0 where not).
 void attn_maps(AttnCall& c, int head_dim, AttnMaps* maps);
 cudaError_t launch_attn_many(const AttnCall& c, const AttnMaps& maps, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
                              cudaStream_t s);

@@ -14,14 +14,20 @@ struct Join {
   static constexpr int kCols = D / 4, kThreads = D == 256 ? 512 : 256, kGroups = kThreads / kCols;
 };
 
-template <class T, int D, bool kOneRow>
+template <class T, int D, bool kOneRow, bool kTiles>
 __global__ void __launch_bounds__(Join<D>::kThreads) k_attn_join(AttnCall c, AttnParts parts, int part_rows) {
   using J = Join<D>;
-  const int b = blockIdx.x, tid = threadIdx.x, col = tid % J::kCols, g = tid / J::kCols;
+  // many rows: neighbouring threads take neighbouring rows, which is how tiles leave them
+  const int b = blockIdx.x, tid = threadIdx.x, col = kOneRow ? tid % J::kCols : tid / J::kGroups,
+            g = kOneRow ? tid / J::kCols : tid % J::kGroups;
   pdl_wait();
   const AttnRec rec = parts.rec[b];
   const int r = kOneRow ? (int)blockIdx.y : (int)blockIdx.y * J::kGroups + g;
   if (rec.n == 0 || (kOneRow && r >= rec.rows)) return;
+  auto o_of = [&](int64_t row) -> const float4* {  // the row's four columns (kTiles: column group by column group)
+    const int64_t part0 = row - r;
+    return reinterpret_cast<const float4*>(parts.o + part0 * D + (kTiles ? (col * part_rows + r) * 4 : r * D + col * 4));
+  };
   auto row_of = [&](int p) { return (int64_t)(p == 0 ? b * 2 + 1 : (b + p) * 2) * part_rows + r; };
   float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
   float mx = -INFINITY, ls = 0.f;
@@ -53,7 +59,7 @@ __global__ void __launch_bounds__(Join<D>::kThreads) k_attn_join(AttnCall c, Att
 #pragma unroll 8
     for (int p = g; p < rec.n; p += J::kGroups) {
       const float w = s_w[p];
-      const float4 v = *reinterpret_cast<const float4*>(parts.o + row_of(p) * D + col * 4);
+      const float4 v = *o_of(row_of(p));
       sum.x += w * v.x, sum.y += w * v.y, sum.z += w * v.z, sum.w += w * v.w;
     }
     s_o[tid] = sum;
@@ -72,7 +78,7 @@ __global__ void __launch_bounds__(Join<D>::kThreads) k_attn_join(AttnCall c, Att
     for (int p = 0; p < rec.n; ++p) {
       const float2 ml = parts.ml[row_of(p)];
       const float w = exp2f(ml.x - ms);
-      const float4 v = *reinterpret_cast<const float4*>(parts.o + row_of(p) * D + col * 4);
+      const float4 v = *o_of(row_of(p));
       sum.x += w * v.x, sum.y += w * v.y, sum.z += w * v.z, sum.w += w * v.w;
       ls += w * ml.y;
     }
@@ -91,10 +97,10 @@ cudaError_t run(const AttnCall& c, const AttnParts& parts, int rows, int blocks,
   // up to 64 rows there may be many pieces of each; with more, a record has few pieces
   const int64_t most = (int64_t)c.st.max_q * c.st.G;
   const int held = (int)(most < rows ? most : rows);
-  if (held <= 64)
-    return launch_pdl(true, k_attn_join<T, D, true>, dim3(blocks, held), dim3(J::kThreads), 0, s, c, parts, rows);
-  return launch_pdl(true, k_attn_join<T, D, false>, dim3(blocks, (held + J::kGroups - 1) / J::kGroups), dim3(J::kThreads), 0, s,
-                    c, parts, rows);
+  const dim3 one(blocks, held), each(blocks, (held + J::kGroups - 1) / J::kGroups), threads(J::kThreads);
+  if (rows == kFewRows) return launch_pdl(true, k_attn_join<T, D, true, false>, one, threads, 0, s, c, parts, rows);
+  if (held <= 64) return launch_pdl(true, k_attn_join<T, D, true, true>, one, threads, 0, s, c, parts, rows);
+  return launch_pdl(true, k_attn_join<T, D, false, true>, each, threads, 0, s, c, parts, rows);
 }
 
 }  // namespace

@@ -13,16 +13,15 @@
 // Two jobs are always under way: while the tensor cores run one's products the softmax of the other is computed,
 // S and P in two buffers.  With head_dim 64 and 128 they are the two row tiles of a segment (they share K and V in
 // shared memory, which halves the cache's traffic), each with a warpgroup of its own; with head_dim 256, whose O fills
-// half of the tensor memory, or where a segment has one row tile, they are successive key tiles of it.  The
-// order in which the tensor cores work is S(0), S(1), then O(g), S(g + 2) for g = 0, 1, ..., across segments, so the next
-// segment's first scores run beside the last one's softmax.
+// half of the tensor memory, or where a segment has one row tile, they are successive key tiles of it.
 //
-// 12 warps: 0-3 and 4-7 softmax (thread = row; the maximum and the sum need no shuffles), 8 issues MMAs, 9 copies K and V by
-// TMA, 10 and 11 copy Q, and K and V where TMA cannot: a box is as many lines as the largest power of two that divides the
-// page (8 to 128), and a tile that reaches past its sequence's lines (where anything may lie, NaN among it, which a product
-// with p = 0 would pass on) or before every window is copied line by line with cp.async, such lines becoming zeros.  So are
-// all tiles of pages that are no multiple of 8 lines.  The ring holds 160 KiB beside Q, in
-// slots of 128 lines x 64 elements (head_dim 64) or 128.
+// 12 warps: 0-3 and 4-7 softmax (thread = row; the maximum and the sum need no shuffles), 8 issues the MMAs of S, 9 those of O
+// (one warp for both left the tensor cores idle while it waited between products: their queue covers a few hundred
+// cycles), 10 copies Q and K, 11 V, each into a ring of its own.  A barrier has one waiting role, which sees every phase of
+// it.  Copies are TMA boxes of as many lines as the largest power of two that divides the page (8 to 128); a tile that
+// reaches past its sequence's lines (where anything may lie, NaN among it, which a product with p = 0 would pass on)
+// or before every window is copied line by line with cp.async, such lines becoming zeros.  So are all tiles of pages that
+// are no multiple of 8 lines, and Q where the group does not divide 128.
 //
 // Split.  As for few rows: the step's jobs are one list shared out evenly over one block per SM; pieces of segments that
 // a block does not have whole are left as partials and joined in order.
@@ -34,23 +33,23 @@
 namespace mf {
 namespace {
 
-constexpr int kThreads = 384, kMmaWarp = 8, kTmaWarp = 9, kCopyWarp0 = 10, kCopyWarps = 2;
+constexpr int kThreads = 384, kQkWarp = 8, kPvWarp = 9, kKWarp = 10;
 constexpr int kKeys = 128;                  // lines of a key tile
 constexpr uint32_t kUnitBytes = 128 * 128;  // 128 lines x 64 elements
-constexpr int kUnits = 10;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kGrow = 8.f;  // growth of the maximum (log2) that o is rescaled for
 
 template <int D>
 struct Cfg {
   static constexpr int kU = D / 64;                   // units of a K or V tile
-  static constexpr int kSlotU = D == 64 ? 1 : 2;      // units of a ring slot: what one barrier and one PV product cover
-  static constexpr int kSlots = kUnits / kSlotU, kTileSlots = kU / kSlotU;
+  static constexpr int kSlotU = D == 64 ? 1 : 2;      // units of a ring slot: what one barrier and one product of O cover
+  static constexpr int kTileSlots = kU / kSlotU;
+  static constexpr int kKSlots = D == 64 ? 5 : 3, kVSlots = D == 64 ? 5 : 2;  // 160 KiB of rings
   static constexpr uint32_t kSlotBytes = kSlotU * kUnitBytes;
   static constexpr int kRowTiles = D == 256 ? 1 : 2;  // row tiles of a segment
   static constexpr int kRows = kRowTiles * 128;
   static constexpr uint32_t kQBytes = kRowTiles * kU * kUnitBytes;
-  static constexpr uint32_t kSmem = kQBytes + kUnits * kUnitBytes + 1024;  // 1024: alignment
+  static constexpr uint32_t kSmem = kQBytes + (kKSlots + kVSlots) * kSlotBytes + 1024;  // 1024: alignment
 };
 constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;
 
@@ -222,7 +221,6 @@ struct Jobs {
   __device__ __forceinline__ int row_tile() const { return two & i; }  // also: which of the tile's jobs
   __device__ __forceinline__ bool first_of_tile() const { return !(two & i); }
   __device__ __forceinline__ bool last_of_tile() const { return !two || (i & 1); }
-  __device__ __forceinline__ int key_tile() const { return i >> two; }  // from the segment's j0 on
 };
 
 // A wait whose first poll failed; false, with the block's flag and the error word set, once any wait gave up.
@@ -243,6 +241,13 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm,
       "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
           dst),
       "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(h), "r"(line), "r"(page), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          dst),
+      "l"(reinterpret_cast<uint64_t>(tm)), "r"(x), "r"(y), "r"(z), "r"(bar)
       : "memory");
 }
 // 64 lines x 64 elements to `dst`, swizzled; a0, a1: element offsets of lines lane, lane + 32 (negative: a line of zeros)
@@ -267,9 +272,10 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// shared memory: [Q][ring], barriers
-constexpr int kBFull = 0, kBEmpty = kUnits, kBQFull = 2 * kUnits, kBQFree = kBQFull + 1, kBS = kBQFree + 1,
-              kBP = kBS + 4, kBO = kBP + 4, kBDrain = kBO + 2, kBars = kBDrain + 1;
+// shared memory: [Q][ring of K][ring of V]; barriers: slots full and free, Q full and free, S and P by (warpgroup,
+// buffer), O by row tile, the buffers free again, the end of all MMAs
+constexpr int kBKFull = 0, kBKFree = 5, kBVFull = 10, kBVFree = 15, kBQFull = 20, kBQFree = 21, kBS = 22, kBP = 26, kBO = 30,
+              kBBuf = 32, kBDrain = 34, kBars = 36;
 
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant__ AttnCall c, const __grid_constant__ AttnMaps maps,
@@ -281,22 +287,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
   __shared__ uint64_t bars[kBars];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_flag;
-  const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u, ring0 = smem0 + C::kQBytes;
+  const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t kring = smem0 + C::kQBytes, vring = kring + C::kKSlots * C::kSlotBytes;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const AttnStep& st = c.st;
   if (tid == 0) {
-    // a slot is full when the TMA warp and both copying warps have done their part, which may be none: each of them
-    // sees every phase of every slot, so none can run ahead of the ring or fall behind it
-    for (int i = 0; i < C::kSlots; ++i) mbar_init(&bars[kBFull + i], 1 + kCopyWarps), mbar_init(&bars[kBEmpty + i], 1);
-    mbar_init(&bars[kBQFull], kCopyWarps);
-    mbar_init(&bars[kBQFree], 1);
-    for (int i = 0; i < 4; ++i) mbar_init(&bars[kBS + i], 1), mbar_init(&bars[kBP + i], 4);
-    for (int i = 0; i < 2; ++i) mbar_init(&bars[kBO + i], 1);
-    mbar_init(&bars[kBDrain], 1);
+    for (int i = 0; i < kBars; ++i) mbar_init(&bars[i], i >= kBP && i < kBP + 4 ? 4 : 1);
     s_flag = 0;
     mbar_fence_init();
   }
-  if (warp == kMmaWarp) tc::alloc(&s_tmem, kTmemCols);
+  if (warp == kQkWarp) tc::alloc(&s_tmem, kTmemCols);
   tc::fence_before();
   __syncthreads();
   tc::fence_after();
@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
   };
   auto wait_all = [&](int bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, wait(bar, parity)); };
 
-  if (warp < kMmaWarp) {
+  if (warp < kQkWarp) {
     // ================= softmax: warpgroup wg has row tile wg of two, or (wg 0) the only one
     const int wg = warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -420,8 +420,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         oph ^= 1;
         tc::fence_after();
         const bool whole = g.j0 == 0 && g.j1 == g.t.nt;
-        const int64_t pr = ((int64_t)b * 2 + (g.j0 == 0)) * C::kRows + wg * 128 + row;
+        // partials column group by column group, so that a warp's rows are neighbours
+        const int64_t pr0 = ((int64_t)b * 2 + (g.j0 == 0)) * C::kRows, pr = pr0 + wg * 128 + row;
+        float* po = parts.o + pr0 * D + (wg * 128 + row) * 4;
         const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
+        const bool wide = (((uintptr_t)c.out | (uintptr_t)(c.out_stride * 2)) & 31) == 0;  // 32-byte stores: whole sectors
         const int head = g.h * st.G + R % st.G;
         T* out = static_cast<T*>(c.out) + (int64_t)(g.sp.q0 + tok) * c.out_stride + (int64_t)head * D;
 #pragma unroll
@@ -432,17 +435,24 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           if (!ok) continue;
           if (whole) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              uint32_t v[4];
+            for (int u = 0; u < 2; ++u) {
+              uint32_t v[8];
 #pragma unroll
-              for (int x = 0; x < 4; ++x)
-                v[x] = Half2<T>::down(__uint_as_float(o[8 * u + 2 * x]) * inv, __uint_as_float(o[8 * u + 2 * x + 1]) * inv);
-              *reinterpret_cast<uint4*>(out + i * 32 + u * 8) = make_uint4(v[0], v[1], v[2], v[3]);
+              for (int x = 0; x < 8; ++x)
+                v[x] = Half2<T>::down(__uint_as_float(o[16 * u + 2 * x]) * inv, __uint_as_float(o[16 * u + 2 * x + 1]) * inv);
+              if (wide) {
+                asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(out + i * 32 + u * 16), "r"(v[0]), "r"(v[1]),
+                             "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                             : "memory");
+              } else {
+                *reinterpret_cast<uint4*>(out + i * 32 + u * 16) = make_uint4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<uint4*>(out + i * 32 + u * 16 + 8) = make_uint4(v[4], v[5], v[6], v[7]);
+              }
             }
           } else {
 #pragma unroll
             for (int u = 0; u < 8; ++u)
-              *reinterpret_cast<uint4*>(parts.o + pr * D + i * 32 + u * 4) =
+              *reinterpret_cast<uint4*>(po + (int64_t)(i * 8 + u) * (C::kRows * 4)) =
                   make_uint4(o[4 * u], o[4 * u + 1], o[4 * u + 2], o[4 * u + 3]);
           }
         }
@@ -461,276 +471,247 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
       par = (par + nj * g.t.jobs) & 1;
     }
     if (tid == 0 && rec_n == 0) parts.rec[b].n = 0;
-  } else if (warp == kMmaWarp) {
-    // ================= MMA issue: the whole warp walks the jobs, one elected lane issues
-    constexpr uint32_t kIdQk = tc::idesc_f16(kBf, 128, false), kNv = D == 64 ? 64 : 128,
-                       kIdPv = tc::idesc_f16(kBf, (int)kNv, true);
-    const uint32_t bars0 = __shfl_sync(0xffffffffu, smem_u32(bars), 0), tm = __shfl_sync(0xffffffffu, tmem, 0);
-    const uint32_t q0 = __shfl_sync(0xffffffffu, smem0, 0), r0 = __shfl_sync(0xffffffffu, ring0, 0);
-    Walk wq, wp;  // of the scores' side, two jobs ahead, and of the products' with V
-    walk_start<D>(wq, c, p, tiles, t0, t1);
-    wp = wq;
-    Jobs qk, pv;
-    qk.take(wq), pv.take(wp);
-    uint32_t slot = 0, sph = 0;      // next ring slot to be used first, and its phase
-    uint32_t ks = 0, vs = 0;         // first slot of the current K and V tile
-    uint32_t buf = 0;                // buffer of S and P: that of the jobs in turn
-    uint32_t seg_ph = 0, pph = 0;    // pph: phases of the four P barriers, a bit each
-    auto take = [&](uint32_t& first) -> bool {  // wait for the slots of the next K or V tile
-      first = slot;
-      bool ok = true;
-#pragma unroll
-      for (int i = 0; i < C::kTileSlots; ++i) {
-        ok = ok && wait_all(kBFull + (int)slot, sph);
-        if (++slot == C::kSlots) slot = 0, sph ^= 1;
-      }
-      return ok;
-    };
-    // operands of an MMA come from uniform registers: what they derive from is read from one lane, so that the compiler
-    // knows it to be uniform (moved there one by one they cost as much as the products)
+  } else if (warp <= kPvWarp) {
+    // ================= MMA issue: the whole warp walks the jobs, one elected lane issues.  Operands of an MMA come from
+    // uniform registers: what they derive from is read from one lane, so that the compiler knows it to be uniform (moved
+    // there one by one they cost as much as the products).
     auto uniform = [](uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); };
-    auto slot_of = [](uint32_t first, int i) { return first + i >= C::kSlots ? first + i - C::kSlots : first + i; };
+    const uint32_t bars0 = uniform(smem_u32(bars)), tm = uniform(tmem);
+    Walk w;
+    walk_start<D>(w, c, p, tiles, t0, t1);
+    Jobs jb;
+    jb.take(w);
+    uint32_t slot = 0, sph = 0, buf = 0, g = 0;  // next ring slot and its phase, buffer of S and P, job
+    if (warp == kQkWarp) {
+      constexpr uint32_t kId = tc::idesc_f16(kBf, 128, false);
+      const uint32_t q0 = uniform(smem0), r0 = uniform(kring);
+      uint32_t first = 0, seg_ph = 0;
 #pragma unroll 1
-    for (int step = -2; pv.live; ++step, buf ^= 1) {
-      if (step >= 0) {  // O += P V of job `step`
-        const int pb = pv.row_tile() * 2 + (int)buf;
+      for (; jb.live; ++g, buf ^= 1) {  // S = Q K^T
         bool ok = true;
-        if (pv.first_of_tile()) ok = take(vs);
+        if (jb.i == 0) {
+          ok = wait_all(kBQFull, seg_ph);
+          seg_ph ^= 1;
+        }
+        if (jb.first_of_tile()) {
+          first = slot;
+          if (C::kTileSlots == 1) {
+            ok = ok && wait_all(kBKFull + (int)slot, sph);
+            if (++slot == C::kKSlots) slot = 0, sph ^= 1;
+          }
+        }
+        if (g >= 2) ok = ok && wait_all(kBBuf + (int)buf, (g >> 1) + 1 & 1);  // P of job g - 2 has been read
+        if (!ok) break;
+        tc::fence_after();
+        const uint32_t x = uniform(jb.row_tile()), b_ = uniform(buf), end = uniform(jb.i == jb.n - 1),
+                       last = uniform(jb.last_of_tile()), f = uniform(first);
+#pragma unroll
+        for (int v = 0; v < C::kTileSlots; ++v) {
+          const uint32_t sl = f + v >= C::kKSlots ? f + v - C::kKSlots : f + v;
+          if (C::kTileSlots > 1) {  // slot by slot: one row tile, so each is used once
+            if (!(ok = wait_all(kBKFull + (int)slot, sph))) break;
+            if (++slot == C::kKSlots) slot = 0, sph ^= 1;
+            tc::fence_after();
+          }
+          if (tc::elect_one()) {
+#pragma unroll
+            for (int u = 0; u < C::kSlotU; ++u) {
+              const uint64_t a = tc::desc_sw128(q0 + (x * C::kU + v * C::kSlotU + u) * kUnitBytes, 0),
+                             bd = tc::desc_sw128(r0 + sl * C::kSlotBytes + u * kUnitBytes, 0);
+#pragma unroll
+              for (int k = 0; k < 4; ++k)  // 16 elements: 32 bytes along the rows
+                tc::mma_ss(tm + kColS + b_ * 128, a + k * 2, bd + k * 2, kId, v + u + k > 0);
+            }
+            if (v == C::kTileSlots - 1) {
+              tc::commit(bars0 + (kBS + x * 2 + b_) * 8);
+              if (end) tc::commit(bars0 + kBQFree * 8);
+            }
+            if (last) tc::commit(bars0 + (kBKFree + sl) * 8);
+          }
+          __syncwarp();
+        }
+        if (!ok) break;
+        if (++jb.i == jb.n) {
+          walk_next<D>(w, c, p);
+          jb.take(w);
+        }
+      }
+    } else {
+      constexpr uint32_t kId = tc::idesc_f16(kBf, D == 64 ? 64 : 128, true);
+      const uint32_t r0 = uniform(vring);
+      uint32_t first = 0, pph = 0;  // pph: phases of the four P barriers, a bit each
+#pragma unroll 1
+      for (; jb.live; ++g, buf ^= 1) {  // O += P V
+        bool ok = true;
+        if (jb.first_of_tile()) {
+          first = slot;
+          if (C::kTileSlots == 1) {
+            ok = wait_all(kBVFull + (int)slot, sph);
+            if (++slot == C::kVSlots) slot = 0, sph ^= 1;
+          }
+        }
+        const int pb = jb.row_tile() * 2 + (int)buf;
         ok = ok && wait_all(kBP + pb, pph >> pb & 1);
         if (!ok) break;
         pph ^= 1u << pb;
         tc::fence_after();
-        const uint32_t x = uniform(pv.row_tile()), b_ = uniform(buf), first = uniform(vs), acc = uniform(pv.i > pv.two);
-        // two row tiles: only their last product is waited for (S(g + 2) is formed after O(g)), else each one
-        const uint32_t tell = uniform(!pv.two || pv.i + 2 >= pv.n), last = uniform(pv.last_of_tile());
-        if (tc::elect_one()) {
+        const uint32_t x = uniform(jb.row_tile()), b_ = uniform(buf), acc = uniform(jb.i > jb.two), f = uniform(first);
+        // two row tiles: only their last product is waited for (their next S is formed after it), else each one
+        const uint32_t tell = uniform(!jb.two || jb.i + 2 >= jb.n), last = uniform(jb.last_of_tile());
 #pragma unroll
-          for (int u = 0; u < C::kTileSlots; ++u) {
-            const uint64_t bd = tc::desc_sw128(r0 + slot_of(first, u) * C::kSlotBytes, kUnitBytes);
+        for (int v = 0; v < C::kTileSlots; ++v) {
+          const uint32_t sl = f + v >= C::kVSlots ? f + v - C::kVSlots : f + v;
+          if (C::kTileSlots > 1) {
+            if (!(ok = wait_all(kBVFull + (int)slot, sph))) break;
+            if (++slot == C::kVSlots) slot = 0, sph ^= 1;
+            tc::fence_after();
+          }
+          if (tc::elect_one()) {
+            const uint64_t bd = tc::desc_sw128(r0 + sl * C::kSlotBytes, kUnitBytes);
 #pragma unroll
             for (int k = 0; k < 8; ++k)  // 16 lines: two groups of eight
-              tc::mma_ts(tm + kColO + x * D + u * 128, tm + kColS + b_ * 128 + k * 8, bd + k * (2048 >> 4), kIdPv, acc | (k > 0));
+              tc::mma_ts(tm + kColO + x * D + v * 128, tm + kColS + b_ * 128 + k * 8, bd + k * (2048 >> 4), kId, acc | (k > 0));
+            if (v == C::kTileSlots - 1) {
+              tc::commit(bars0 + (kBBuf + b_) * 8);
+              if (tell) tc::commit(bars0 + (kBO + x) * 8);
+            }
+            if (last) tc::commit(bars0 + (kBVFree + sl) * 8);
           }
-          if (tell) tc::commit(bars0 + (kBO + x) * 8);
-          if (last) {
-#pragma unroll
-            for (int u = 0; u < C::kTileSlots; ++u) tc::commit(bars0 + (kBEmpty + slot_of(first, u)) * 8);
-          }
+          __syncwarp();
         }
-        __syncwarp();
-        if (++pv.i == pv.n) {
-          walk_next<D>(wp, c, p);
-          pv.take(wp);
-        }
-      }
-      if (qk.live) {  // S = Q K^T of job step + 2, into the buffer whose P is read by now
-        bool ok = true;
-        if (qk.i == 0) {
-          ok = wait_all(kBQFull, seg_ph);
-          seg_ph ^= 1;
-        }
-        if (qk.first_of_tile()) ok = ok && take(ks);
         if (!ok) break;
-        tc::fence_after();
-        const uint32_t x = uniform(qk.row_tile()), b_ = uniform(buf), first = uniform(ks), end = uniform(qk.i == qk.n - 1),
-                       last = uniform(qk.last_of_tile());
-        if (tc::elect_one()) {
-#pragma unroll
-          for (int u = 0; u < C::kU; ++u) {
-            const uint64_t a = tc::desc_sw128(q0 + (x * C::kU + u) * kUnitBytes, 0),
-                           bd = tc::desc_sw128(r0 + slot_of(first, u / C::kSlotU) * C::kSlotBytes + u % C::kSlotU * kUnitBytes, 0);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)  // 16 elements: 32 bytes along the rows
-              tc::mma_ss(tm + kColS + b_ * 128, a + k * 2, bd + k * 2, kIdQk, u + k > 0);
-          }
-          tc::commit(bars0 + (kBS + x * 2 + b_) * 8);
-          if (last) {
-#pragma unroll
-            for (int u = 0; u < C::kTileSlots; ++u) tc::commit(bars0 + (kBEmpty + slot_of(first, u)) * 8);
-          }
-          if (end) tc::commit(bars0 + kBQFree * 8);
-        }
-        __syncwarp();
-        if (++qk.i == qk.n) {
-          walk_next<D>(wq, c, p);
-          qk.take(wq);
+        if (++jb.i == jb.n) {
+          walk_next<D>(w, c, p);
+          jb.take(w);
         }
       }
     }
     // nothing may be in flight when the tensor memory is freed
-    if (tc::elect_one()) tc::commit(bars0 + kBDrain * 8);
+    const int drain = kBDrain + warp - kQkWarp;
+    if (tc::elect_one()) tc::commit(bars0 + drain * 8);
     __syncwarp();
-    if (!mbar_wait(&bars[kBDrain], 0, kDefaultWaitNs)) attn_report(st, kAttnTimeout);
+    if (!mbar_wait(&bars[drain], 0, kDefaultWaitNs)) attn_report(st, kAttnTimeout);
   } else {
-    // ================= copies, in the order of the MMAs' first uses: (Q and) K of jobs 0 and 1, then V of job g, K of g + 2
-    struct Side {  // what a segment's K or V tiles need
-      Jobs jb;
-      int s, h, k0, lo, len, end;
-      __device__ __forceinline__ void take(const Walk& w) {
-        jb.take(w);
-        s = w.g.s, h = w.g.h, k0 = w.g.t.start + w.g.j0 * kKeys, lo = w.g.lo, len = w.g.sp.len, end = w.g.t.end;
-      }
-      // whether TMA copies the job's tile: all its lines are the sequence's, and seen by some token
-      __device__ __forceinline__ bool clean(int box) const {
-        const int a = k0 + jb.key_tile() * kKeys;
-        return box && a >= lo && a + kKeys <= len;
-      }
-    };
-    Walk wq, wp;
-    walk_start<D>(wq, c, p, tiles, t0, t1);
-    wp = wq;
-    Side qk, pv;
-    qk.take(wq), pv.take(wp);
-    uint32_t slot = 0, sph = 1;  // next slot, and the parity of "it is free" (at first it is)
+    // ================= copies: warp kKWarp Q and K, the next one V
+    const bool is_k = warp == kKWarp;
+    const uint32_t bars0 = smem_u32(bars), ring = is_k ? kring : vring;
+    const int full = is_k ? kBKFull : kBVFull, empty = is_k ? kBKFree : kBVFree, slots = is_k ? C::kKSlots : C::kVSlots;
+    const CUtensorMap* tm = is_k ? &maps.k : &maps.v;
+    const T* cache = static_cast<const T*>(is_k ? c.k : c.v);
+    const int n_box = c.box ? kKeys / c.box : 0;
+    int slot = 0, pending = -1;         // pending: barrier of the cp.async copies that are not announced yet
+    uint32_t sph = 1, seg_ph = 1;       // parities of "it is free" (at first it is)
+    uint32_t tx = 0;                    // slots that TMA has been asked to fill last
     bool ok = true;
-    if (warp == kTmaWarp) {
-      const uint32_t bars0 = smem_u32(bars);
-      const int n_box = c.box ? kKeys / c.box : 0;
-      auto tile = [&](const Side& sd, const CUtensorMap* tm) {
-        const bool mine = sd.clean(c.box);
+    auto announce = [&](bool last) {  // the copies of the pending barrier, once they have landed (last: the newest group's)
+      if (pending < 0) return;
+      if (last) asm volatile("cp.async.wait_group 0;" ::: "memory");
+      else asm volatile("cp.async.wait_group 1;" ::: "memory");
+      tc::fence_proxy();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars[pending]);
+      pending = -1;
+    };
+    auto wait_free = [&](int bar, uint32_t parity) -> bool {  // no copy stays unannounced while this warp sleeps
+      if (__all_sync(0xffffffffu, mbar_try_wait(&bars[bar], parity))) return true;
+      announce(true);
+      return wait_all(bar, parity);
+    };
+    auto copied = [&](int bar) {
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      announce(false);
+      pending = bar;
+    };
+    Walk w;
+    walk_start<D>(w, c, p, tiles, t0, t1);
+#pragma unroll 1
+    for (; w.more && ok; walk_next<D>(w, c, p)) {
+      const Seg g = w.g;
+      if (is_k) {  // the segment's rows of q
+        if (!(ok = wait_free(kBQFree, seg_ph))) break;
+        seg_ph ^= 1;
+        if (c.q_box) {
+          const int n = g.t.jobs * C::kU;
+          announce(true);
+          if (lane == 0) mbar_arrive_tx(&bars[kBQFull], n * kUnitBytes);
+          __syncwarp();
+          if (lane < n)
+            tma_load_3d(smem0 + lane * kUnitBytes, &maps.q, lane % C::kU * 64, g.h * st.G,
+                        g.sp.q0 + (g.qt * C::kRows + lane / C::kU * 128) / st.G, bars0 + kBQFull * 8);
+        } else {
+          const int n = 2 * g.t.jobs * C::kU;  // halves of units
+#pragma unroll 1
+          for (int v = 0; v < n; ++v) {
+            const int x = (v >> 1) / C::kU, u = (v >> 1) % C::kU;
+            int64_t at[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int r = x * 128 + (v & 1) * 64 + i * 32 + lane, R = g.qt * C::kRows + r;
+              at[i] = r < g.t.rows ? (int64_t)(g.sp.q0 + R / st.G) * c.q_stride + (int64_t)(g.h * st.G + R % st.G) * D : -1;
+            }
+            copy_lines<T>(smem0 + (uint32_t)v * (kUnitBytes / 2), static_cast<const T*>(c.q) + u * 64, at[0], at[1]);
+          }
+          copied(kBQFull);
+          announce(true);
+        }
+      }
+      const int un = lane / max(n_box, 1), bx = lane - un * n_box;  // TMA: this lane's box bx of unit un of a slot
+#pragma unroll 1
+      for (int j = g.j0; j < g.j1 && ok; ++j) {
+        const int k0 = g.t.start + j * kKeys;
+        // TMA where all the tile's lines are the sequence's, and seen by some token of the step
+        const bool tma = n_box && k0 >= g.lo && k0 + kKeys <= g.sp.len;
         int page = 0, line = 0;
-        const int un = lane / max(n_box, 1), bx = lane - un * n_box;  // lane: box bx of unit un of the slot
-        if (mine && un < C::kSlotU) {
-          const int at = sd.k0 + sd.jb.key_tile() * kKeys + bx * c.box;
-          const int pi = (int)fast_div((uint32_t)at, st.page_mul, st.page_shift);
-          const int raw = __ldg(st.pages + (int64_t)sd.s * st.pages_per_seq + pi);
-          page = min(max(raw, 0), st.n_pages - 1);
-          if (page != raw) attn_report(st, kAttnRange);
-          line = at - pi * st.page_size;
+        int64_t at[4] = {-1, -1, -1, -1};
+        if (tma) {
+          if (un < C::kSlotU) {
+            const int l0 = k0 + bx * c.box, pi = (int)fast_div((uint32_t)l0, st.page_mul, st.page_shift);
+            const int raw = __ldg(st.pages + (int64_t)g.s * st.pages_per_seq + pi);
+            page = min(max(raw, 0), st.n_pages - 1);
+            if (page != raw) attn_report(st, kAttnRange);
+            line = l0 - pi * st.page_size;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int l0 = k0 + i * 32 + lane;
+            if (l0 >= g.lo && l0 < g.t.end) at[i] = line_offset(st, g.s, l0) + (int64_t)g.h * st.head_stride;
+          }
         }
 #pragma unroll 1
         for (int u = 0; u < C::kTileSlots; ++u) {
-          if (!(ok = wait_all(kBEmpty + (int)slot, sph))) return;
-          if (lane == 0) {
-            if (mine) mbar_arrive_tx(&bars[kBFull + slot], C::kSlotBytes);
-            else mbar_arrive(&bars[kBFull + slot]);
-          }
-          if (mine) {
+          if (!(ok = wait_free(empty + slot, sph))) break;
+          const uint32_t dst = ring + slot * C::kSlotBytes;
+          if (tma) {
+            if (lane == 0) mbar_arrive_tx(&bars[full + slot], C::kSlotBytes);
             __syncwarp();
             if (un < C::kSlotU)
-              tma_load_4d(ring0 + slot * C::kSlotBytes + un * kUnitBytes + bx * c.box * 128, tm, (u * C::kSlotU + un) * 64, sd.h,
-                          line, page, bars0 + (kBFull + slot) * 8);
-          }
-          if (++slot == C::kSlots) slot = 0, sph ^= 1;
-        }
-      };
-#pragma unroll 1
-      for (int g = -2; pv.jb.live; ++g) {
-        if (g >= 0) {
-          if (pv.jb.first_of_tile()) tile(pv, &maps.v);
-          if (++pv.jb.i == pv.jb.n) {
-            walk_next<D>(wp, c, p);
-            pv.take(wp);
-          }
-        }
-        if (!ok) break;
-        if (qk.jb.live) {
-          if (qk.jb.first_of_tile()) tile(qk, &maps.k);
-          if (++qk.jb.i == qk.jb.n) {
-            walk_next<D>(wq, c, p);
-            qk.take(wq);
-          }
-        }
-        if (!ok) break;
-      }
-      // no copy may be in flight when the block exits: the MMA warp has waited for every slot that it used, and uses all
-      // of them unless a wait gave up; then the last phases are waited for here
-      if (!ok)
-        for (int i = 0; i < C::kSlots; ++i) mbar_wait(&bars[kBFull + i], (i < (int)slot ? sph ^ 1 : sph), 1000000);
-    } else {
-      const int me = warp - kCopyWarp0;
-      uint32_t seg_ph = 1;
-      int pending = -1;  // barrier of the copies that are not announced yet
-      auto announce = [&](bool last) {  // the copies of the pending barrier, once they have landed (last: the newest group's)
-        if (pending < 0) return;
-        if (last) asm volatile("cp.async.wait_group 0;" ::: "memory");
-        else asm volatile("cp.async.wait_group 1;" ::: "memory");
-        tc::fence_proxy();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bars[pending]);
-        pending = -1;
-      };
-      auto wait_free = [&](int bar, uint32_t parity) -> bool {  // no copy stays unannounced while this warp sleeps
-        if (__all_sync(0xffffffffu, mbar_try_wait(&bars[bar], parity))) return true;
-        announce(true);
-        return wait_all(bar, parity);
-      };
-      auto copied = [&](int bar) {
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        announce(false);
-        pending = bar;
-      };
-      auto tile = [&](const Side& sd, const void* cache) {
-        const bool skip = sd.clean(c.box);
-        int64_t at[2] = {-1, -1};
-        if (!skip) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int line = sd.k0 + sd.jb.key_tile() * kKeys + me * 64 + i * 32 + lane;
-            if (line >= sd.lo && line < sd.end) at[i] = line_offset(st, sd.s, line) + (int64_t)sd.h * st.head_stride;
-          }
-        }
-#pragma unroll 1
-        for (int u = 0; u < C::kTileSlots; ++u) {
-          if (!(ok = wait_free(kBEmpty + (int)slot, sph))) return;
-          if (skip) {
-            if (lane == 0) mbar_arrive(&bars[kBFull + slot]);
+              tma_load_4d(dst + un * kUnitBytes + bx * c.box * 128, tm, (u * C::kSlotU + un) * 64, g.h, line, page,
+                          bars0 + (full + slot) * 8);
+            tx |= 1u << slot;
           } else {
 #pragma unroll 1
-            for (int x = 0; x < C::kSlotU; ++x)
-              copy_lines<T>(ring0 + slot * C::kSlotBytes + x * kUnitBytes + me * 64 * 128,
-                            static_cast<const T*>(cache) + (u * C::kSlotU + x) * 64, at[0], at[1]);
-            copied(kBFull + (int)slot);
+            for (int x = 0; x < 2 * C::kSlotU; ++x)
+              copy_lines<T>(dst + x * (kUnitBytes / 2), cache + (u * C::kSlotU + (x >> 1)) * 64, at[x & 1 ? 2 : 0], at[x & 1 ? 3 : 1]);
+            copied(full + slot);
+            tx &= ~(1u << slot);
           }
-          if (++slot == C::kSlots) slot = 0, sph ^= 1;
+          if (++slot == slots) slot = 0, sph ^= 1;
         }
-      };
-      auto rows_of_q = [&](const Seg& g) {
-        if (!(ok = wait_free(kBQFree, seg_ph))) return;
-        seg_ph ^= 1;
-        const int n = 2 * g.t.jobs * C::kU;  // halves of units
-#pragma unroll 1
-        for (int v = me; v < n; v += kCopyWarps) {
-          const int x = (v >> 1) / C::kU, u = (v >> 1) % C::kU;
-          int64_t at[2];
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int r = x * 128 + (v & 1) * 64 + i * 32 + lane, R = g.qt * C::kRows + r;
-            at[i] = r < g.t.rows ? (int64_t)(g.sp.q0 + R / st.G) * c.q_stride + (int64_t)(g.h * st.G + R % st.G) * D : -1;
-          }
-          copy_lines<T>(smem0 + (uint32_t)v * (kUnitBytes / 2), static_cast<const T*>(c.q) + u * 64, at[0], at[1]);
-        }
-        copied(kBQFull);
-        announce(true);
-      };
-#pragma unroll 1
-      for (int g = -2; pv.jb.live; ++g) {
-        if (g >= 0) {
-          if (pv.jb.first_of_tile()) tile(pv, c.v);
-          if (++pv.jb.i == pv.jb.n) {
-            walk_next<D>(wp, c, p);
-            pv.take(wp);
-          }
-        }
-        if (!ok) break;
-        if (qk.jb.live) {
-          if (qk.jb.i == 0) rows_of_q(wq.g);
-          if (ok && qk.jb.first_of_tile()) tile(qk, c.k);
-          if (++qk.jb.i == qk.jb.n) {
-            walk_next<D>(wq, c, p);
-            qk.take(wq);
-          }
-        }
-        if (!ok) break;
       }
-      announce(true);
-      asm volatile("cp.async.wait_all;" ::: "memory");
     }
+    announce(true);
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    // no copy may be in flight when the block exits: the MMA warps have waited for every slot they used, and use all unless a
+    // wait gave up; then the slots' last phases are waited for here (the one before `slot` was filled in this turn)
+    if (!ok)
+      for (int i = 0; i < slots; ++i)
+        if (tx >> i & 1) mbar_wait(&bars[full + i], i < slot ? sph ^ 1 : sph, kDefaultWaitNs);
   }
   tc::fence_before();
   __syncthreads();
   tc::fence_after();
-  if (warp == kMmaWarp) tc::dealloc(tmem, kTmemCols);
+  if (warp == kQkWarp) tc::dealloc(tmem, kTmemCols);
 }
 
 template <class T, int D>
@@ -761,20 +742,31 @@ void attn_maps(AttnCall& c, int head_dim, AttnMaps* maps) {
     return e == cudaSuccess && q == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiled>(fn) : nullptr;
   }();
   memset(maps, 0, sizeof(*maps));
-  c.box = 0;
+  c.box = c.q_box = 0;
   const AttnStep& st = c.st;
-  int box = kKeys;
-  while (st.page_size % box) box /= 2;
-  if (!encode || box < 8) return;
-  const cuuint64_t dims[4] = {(cuuint64_t)head_dim, (cuuint64_t)st.Hkv, (cuuint64_t)st.page_size, (cuuint64_t)st.n_pages};
-  const cuuint64_t strides[3] = {(cuuint64_t)st.head_stride * 2, (cuuint64_t)st.token_stride * 2, (cuuint64_t)st.page_stride * 2};
-  const cuuint32_t boxes[4] = {64, 1, (cuuint32_t)box, 1}, ones[4] = {1, 1, 1, 1};
-  auto make = [&](CUtensorMap* tm, const void* base) {
-    return encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, const_cast<void*>(base), dims, strides, boxes, ones,
+  if (!encode) return;
+  auto make = [&](CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
+                  const cuuint32_t* box) {
+    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    return encode(tm, CU_TENSOR_MAP_DATA_TYPE_UINT16, rank, const_cast<void*>(base), dims, strides, box, ones,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
   };
-  if (make(&maps->k, c.k) && make(&maps->v, c.v)) c.box = box;
+  const cuuint64_t d = (cuuint64_t)head_dim;
+  int box = kKeys;
+  while (st.page_size % box) box /= 2;
+  if (box >= 8) {
+    const cuuint64_t dims[4] = {d, (cuuint64_t)st.Hkv, (cuuint64_t)st.page_size, (cuuint64_t)st.n_pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)st.head_stride * 2, (cuuint64_t)st.token_stride * 2, (cuuint64_t)st.page_stride * 2};
+    const cuuint32_t boxes[4] = {64, 1, (cuuint32_t)box, 1};
+    if (make(&maps->k, c.k, 4, dims, strides, boxes) && make(&maps->v, c.v, 4, dims, strides, boxes)) c.box = box;
+  }
+  if (128 % st.G == 0) {  // a row tile is the group's heads of 128 / G tokens
+    const cuuint64_t dims[3] = {d, (cuuint64_t)st.Hq, (cuuint64_t)st.n_tokens};
+    const cuuint64_t strides[2] = {d * 2, (cuuint64_t)c.q_stride * 2};
+    const cuuint32_t boxes[3] = {64, (cuuint32_t)st.G, (cuuint32_t)(128 / st.G)};
+    c.q_box = make(&maps->q, c.q, 3, dims, strides, boxes);
+  }
 }
 
 int attn_tile_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
