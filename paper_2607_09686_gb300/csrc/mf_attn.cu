@@ -211,12 +211,12 @@ extern "C" int mf_attn_create(mf_attn_t** out, const mf_attn_shape_t* shape, int
   Carve w;
   const size_t o_err = w.take(256), o_o = w.take(rows * shape->head_dim * 4), o_ml = w.take(rows * 8),
                o_rec = w.take((size_t)attn_few_blocks(h->sms) * sizeof(AttnRec)), o_first = w.take(((size_t)max_seqs + 1) * 4),
-               o_seq = w.take(tiles * 4), o_before = w.take((tiles + 1) * 8);
+               o_tile = w.take(tiles * 32), o_before = w.take((tiles + 1) * 8);
   unsigned char* ws = nullptr;
   if (e == cudaSuccess) e = tiles < (1u << 30) ? cudaMalloc(&ws, w.off) : cudaErrorMemoryAllocation;
   h->err = reinterpret_cast<unsigned*>(ws + o_err);
   h->parts = {reinterpret_cast<float*>(ws + o_o), reinterpret_cast<float2*>(ws + o_ml), reinterpret_cast<AttnRec*>(ws + o_rec)};
-  h->plan = {reinterpret_cast<int*>(ws + o_first), reinterpret_cast<int*>(ws + o_seq), reinterpret_cast<int64_t*>(ws + o_before),
+  h->plan = {reinterpret_cast<int*>(ws + o_first), reinterpret_cast<int4*>(ws + o_tile), reinterpret_cast<int64_t*>(ws + o_before),
              (int)tiles};
   if (e == cudaSuccess) e = cudaMemset(h->err, 0, 256);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();

@@ -135,7 +135,8 @@ int attn_tile_rows(int head_dim);  // rows of a part of launch_attn_many (one bl
 // What k_attn_plan finds of a step for launch_attn_many: the row tiles of the sequences and the jobs before each.
 struct AttnPlan {
   int* first;       // [max_seqs + 1]  first row tile of a sequence; then the number of tiles
-  int* seq_of;      // [max_tiles]     the tile's sequence
+  int4* tile;       // [max_tiles][2]  its sequence, that one's first new token, new tokens and lines; its place among the
+                    //                 sequence's tiles, rows, first and end of the lines that any of them sees
   int64_t* before;  // [max_tiles + 1] jobs (of one kv head) before the tile
   int max_tiles;
 };

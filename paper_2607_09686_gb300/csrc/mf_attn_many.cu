@@ -55,25 +55,7 @@ constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;
 
 // ---- the step's segments
 
-// row tile `qt` of a sequence: its rows and the lines that any of them sees
-struct Tile {
-  int rows, start, end, nt, jobs;  // jobs: row tiles (1 or 2) per key tile
-};
-template <int D>
-__device__ __forceinline__ Tile tile_of(const AttnCall& c, const SeqSpan& sp, int qt) {
-  const int G = c.st.G, R0 = qt * Cfg<D>::kRows;
-  Tile t;
-  t.rows = min(Cfg<D>::kRows, sp.n * G - R0);
-  const int first = sp.len - sp.n;
-  t.start = vis_lo(c, first + R0 / G);
-  if (c.box) t.start &= ~(c.box - 1);
-  t.end = max(0, vis_hi(c, first + (R0 + t.rows - 1) / G, sp.len));
-  t.nt = max(1, (t.end - t.start + kKeys - 1) / kKeys);
-  t.jobs = Cfg<D>::kRowTiles == 2 && t.rows > 128 ? 2 : 1;
-  return t;
-}
-
-// One block: for each sequence the index of its first row tile, for each row tile its sequence and the jobs before it.
+// One block: for each sequence the index of its first row tile, for each row tile its description and the jobs before it.
 template <int D>
 __global__ void __launch_bounds__(1024) k_attn_plan(AttnCall c, AttnPlan p) {
   __shared__ int64_t s_warp[32];
@@ -122,9 +104,15 @@ __global__ void __launch_bounds__(1024) k_attn_plan(AttnCall c, AttnPlan p) {
         if (p.first[mid] <= i) lo = mid;
         else hi = mid - 1;
       }
-      const Tile t = tile_of<D>(c, seq_span(c.st, lo), i - p.first[lo]);
-      n = (int64_t)t.nt * t.jobs;
-      p.seq_of[i] = lo;
+      const SeqSpan sp = seq_span(c.st, lo);
+      const int qt = i - p.first[lo], R0 = qt * Cfg<D>::kRows, G = c.st.G;
+      const int rows = min(Cfg<D>::kRows, sp.n * G - R0), first = sp.len - sp.n;
+      int start = vis_lo(c, first + R0 / G);
+      if (c.box) start &= ~(c.box - 1);
+      const int end = max(0, vis_hi(c, first + (R0 + rows - 1) / G, sp.len));
+      p.tile[2 * i] = make_int4(lo, sp.q0, sp.n, sp.len);
+      p.tile[2 * i + 1] = make_int4(qt, rows, start, end);
+      n = (int64_t)max(1, (end - start + kKeys - 1) / kKeys) << (Cfg<D>::kRowTiles == 2 && rows > 128);
     }
     int64_t all;
     const int64_t at = jobs + scan(n, all);
@@ -134,79 +122,84 @@ __global__ void __launch_bounds__(1024) k_attn_plan(AttnCall c, AttnPlan p) {
   if (tid == 0) p.before[tiles] = jobs;
 }
 
-// A segment as a block has it: key tiles j0 .. j1 - 1 of row tile `tile` (of all) and kv head h.
-struct Seg {
-  SeqSpan sp;
-  Tile t;
-  int s, h, tile, qt, j0, j1;
-  int lo;      // the sequence's first line that any token of the step sees
-  int64_t at;  // place of its first job in the list
-};
-// The walk over a block's segments.  The list is ordered by sequence, kv head, row tile.  Its steps are taken once a segment
-// and kept out of line: the roles' loops together have to fit the instruction cache (with everything inline two fifths
-// of the fetches missed and a job took five times as long).
+// The walk over a block's segments: key tiles j0 .. j1 - 1 of a row tile (of all: `tile`) and kv head h.  The list is
+// ordered by sequence, kv head, row tile.  The next tile's description is asked for when the walk comes to a segment, and
+// has long arrived when the segment ends.  The roles' loops together have to fit the instruction cache (with walks that
+// looked everything up inline, two fifths of the fetches missed and a job took five times as long).
 struct Walk {
-  int64_t t0, t1;
-  Seg g;
-  int tiles;
-  bool more;  // g is a segment of this block
+  int s, q0, n, len;          // the sequence: new tokens, lines
+  int qt, rows, start, end;   // the row tile: its place, rows, lines that any of them sees
+  int h, tile, j0, j1, nt;
+  int two;                    // 1: two row tiles, two jobs a key tile
+  int4 na, nb;                // the next tile's description
+  int64_t at, t0, t1;         // place of the segment's first job in the list; the block's share
+  bool more;                  // this is a segment of the block
+
+  __device__ __forceinline__ void set(int4 a, int4 b) {
+    s = a.x, q0 = a.y, n = a.z, len = a.w, qt = b.x, rows = b.y, start = b.z, end = b.w;
+    two = rows > 128;
+    nt = max(1, (end - start + kKeys - 1) / kKeys);
+    // a key tile belongs to the block that its first job falls to
+    const int64_t up0 = (t0 - at + two) >> two, up1 = (t1 - at + two) >> two;
+    j0 = (int)max((int64_t)0, up0);
+    j1 = (int)min((int64_t)nt, up1);
+  }
+  // the tile after this one in the list (of this kv head or the next)
+  __device__ __forceinline__ int following(const AttnCall& c, int tile_rows) const {
+    return (qt + 1) * tile_rows >= n * c.st.G && h + 1 < c.st.Hkv ? tile - qt : tile + 1;
+  }
+  __device__ __forceinline__ void ask(const AttnCall& c, const AttnPlan& p, int tile_rows) {
+    const int f = min(following(c, tile_rows), p.max_tiles - 1);  // (past the last tile: anything, not used)
+    na = __ldg(p.tile + 2 * f), nb = __ldg(p.tile + 2 * f + 1);
+  }
+  __device__ __forceinline__ void next(const AttnCall& c, const AttnPlan& p, int tile_rows) {
+#pragma unroll 1
+    do {
+      at += (int64_t)nt << two;
+      if (at >= t1) {
+        more = false;
+        return;
+      }
+      const int f = following(c, tile_rows);
+      if ((qt + 1) * tile_rows >= n * c.st.G) h = f > tile ? 0 : h + 1;
+      tile = f;
+      set(na, nb);
+      ask(c, p, tile_rows);
+    } while (j0 >= j1);
+  }
 };
-template <int D>
-__device__ __forceinline__ void walk_fill(Walk& w, const AttnCall& c, const AttnPlan& p) {
-  Seg& g = w.g;
-  g.s = __ldg(p.seq_of + g.tile);
-  g.sp = seq_span(c.st, g.s);
-  g.qt = g.tile - __ldg(p.first + g.s);
-  g.t = tile_of<D>(c, g.sp, g.qt);
-  g.lo = vis_lo(c, g.sp.len - g.sp.n);
-  const int n = g.t.jobs;  // a key tile belongs to the block that its first job falls to
-  g.j0 = (int)max((int64_t)0, (w.t0 - g.at + n - 1) / n);
-  g.j1 = (int)min((int64_t)g.t.nt, (w.t1 - g.at + n - 1) / n);
-}
-template <int D>
-__device__ __noinline__ void walk_next(Walk& w, const AttnCall& c, const AttnPlan& p) {
-  Seg& g = w.g;
-  do {
-    g.at += (int64_t)g.t.nt * g.t.jobs;
-    if (g.at >= w.t1) {
-      w.more = false;
-      return;
-    }
-    const int first = __ldg(p.first + g.s), end = __ldg(p.first + g.s + 1);
-    if (g.tile + 1 < end) ++g.tile;
-    else if (++g.h < c.st.Hkv) g.tile = first;
-    else g.h = 0, g.tile = end;
-    walk_fill<D>(w, c, p);
-  } while (g.j0 >= g.j1);
-}
-template <int D>
-__device__ __noinline__ void walk_start(Walk& w, const AttnCall& c, const AttnPlan& p, int tiles, int64_t a, int64_t b) {
-  w.t0 = a, w.t1 = b, w.tiles = tiles;
+// to the block's first segment
+__device__ __noinline__ void walk_start(Walk& w, const AttnCall& c, const AttnPlan& p, int tiles, int tile_rows, int64_t a,
+                                        int64_t b) {
+  w.t0 = a, w.t1 = b;
   w.more = a < b;
   if (!w.more) return;
   // the last tile whose sequence starts at or before a, then the kv head, then the tile
   int lo = 0, hi = tiles - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
-    const int first = __ldg(p.first + __ldg(p.seq_of + mid));
+    const int first = mid - __ldg(p.tile + 2 * mid + 1).x;
     if (__ldg(p.before + first) * c.st.Hkv <= a) lo = mid;
     else hi = mid - 1;
   }
-  const int first = __ldg(p.first + __ldg(p.seq_of + lo)), end = lo + 1;
+  const int first = lo - __ldg(p.tile + 2 * lo + 1).x, end = lo + 1;
   const int64_t b0 = __ldg(p.before + first), len = __ldg(p.before + end) - b0;
-  w.g.h = (int)((a - b0 * c.st.Hkv) / len);
-  const int64_t head = b0 * c.st.Hkv + w.g.h * len;
+  w.h = (int)((a - b0 * c.st.Hkv) / len);
+  const int64_t head = b0 * c.st.Hkv + w.h * len;
   lo = first, hi = end - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (head + __ldg(p.before + mid) - b0 <= a) lo = mid;
     else hi = mid - 1;
   }
-  w.g.tile = lo;
-  w.g.at = head + __ldg(p.before + lo) - b0;
-  walk_fill<D>(w, c, p);
-  if (w.g.j0 >= w.g.j1) walk_next<D>(w, c, p);
+  w.tile = lo;
+  w.at = head + __ldg(p.before + lo) - b0;
+  w.set(__ldg(p.tile + 2 * lo), __ldg(p.tile + 2 * lo + 1));
+  w.ask(c, p, tile_rows);
+  if (w.j0 >= w.j1) w.next(c, p, tile_rows);
 }
+
+__device__ __noinline__ void walk_next(Walk& w, const AttnCall& c, const AttnPlan& p, int tile_rows) { w.next(c, p, tile_rows); }
 
 // The jobs of the walk one by one: (key tile, row tile), row tile inner.
 struct Jobs {
@@ -215,8 +208,8 @@ struct Jobs {
   __device__ __forceinline__ void take(const Walk& w) {
     live = w.more;
     i = 0;
-    two = live && w.g.t.jobs == 2;
-    n = live ? (w.g.j1 - w.g.j0) * w.g.t.jobs : 0;
+    two = w.two;
+    n = (w.j1 - w.j0) << two;
   }
   __device__ __forceinline__ int row_tile() const { return two & i; }  // also: which of the tile's jobs
   __device__ __forceinline__ bool first_of_tile() const { return !(two & i); }
@@ -321,20 +314,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     const int wg = warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float sc2 = c.scale * kLog2e;
-    Walk w;
-    walk_start<D>(w, c, p, tiles, t0, t1);
+    Walk w;  // kept in memory: the scores need the registers
+    walk_start(w, c, p, tiles, C::kRows, t0, t1);
     int par = 0;                     // buffer of the segment's first job
     uint32_t sph[2] = {0, 0};        // phases of this warpgroup's S barriers, by buffer
     uint32_t oph = 0;                // phase of its O barrier
     int rec_n = 0;
     bool alive = true;
-    for (; w.more && alive; walk_next<D>(w, c, p)) {
-      const Seg g = w.g;
-      const int nj = g.j1 - g.j0, two = g.t.jobs == 2;
+    while (w.more && alive) {
+      const int nj = w.j1 - w.j0, two = w.two, k_start = w.start + w.j0 * kKeys, R0 = w.qt * C::kRows, rows = w.rows, h = w.h,
+                q0 = w.q0, first = w.len - w.n, len = w.len, nt = w.nt, j0 = w.j0;
+      const int64_t last = w.at + ((int64_t)(nt - 1) << two);  // place of the last key tile's first job
+      walk_next(w, c, p, C::kRows);
       if (two || wg == 0) {
-        const int R = g.qt * C::kRows + wg * 128 + row, tok = R / st.G, pos = g.sp.len - g.sp.n + tok;
-        const bool ok = wg * 128 + row < g.t.rows;
-        const int lo = ok ? vis_lo(c, pos) : 0, hi = ok ? vis_hi(c, pos, g.sp.len) : 0;
+        const int R = R0 + wg * 128 + row, tok = R / st.G, pos = first + tok;
+        const bool ok = wg * 128 + row < rows;
+        const int lo = ok ? vis_lo(c, pos) : 0, hi = ok ? vis_hi(c, pos, len) : 0;
         const uint32_t col_o = tmem + lanes + kColO + (two ? wg * D : 0);
         float m = -INFINITY, l = 0.f;
         for (int j = 0; j < nj; ++j) {
@@ -343,25 +338,34 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           ++sph[buf];
           tc::fence_after();
           const uint32_t col_s = tmem + lanes + kColS + buf * 128;
-          float s[128];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) tc::ld32(col_s + i * 32, reinterpret_cast<uint32_t*>(s) + i * 32);
+          // the row's scores: the first 64 stay in registers, the others are read again when their turn comes
+          uint32_t sa[64], sb[64];
+          tc::ld32(col_s, sa);
+          tc::ld32(col_s + 32, sa + 32);
+          tc::ld32(col_s + 64, sb);
+          tc::ld32(col_s + 96, sb + 32);
           tc::wait_ld();
-          const int k0 = g.t.start + (g.j0 + j) * kKeys, a = lo - k0, z = hi - k0;  // columns [a, z) are seen
-          if (__any_sync(0xffffffffu, a > 0 || z < kKeys)) {
+          tc::pin32(sa), tc::pin32(sa + 32), tc::pin32(sb), tc::pin32(sb + 32);
+          const int k0 = k_start + j * kKeys, a = lo - k0, z = hi - k0;  // columns [a, z) are seen
+          const bool cut = __any_sync(0xffffffffu, a > 0 || z < kKeys);
+          auto mask = [&](uint32_t* s, int col) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int za = min(max(z - 32 * i, 0), 32), aa = min(max(a - 32 * i, 0), 32);
+            for (int i = 0; i < 2; ++i) {
+              const int za = min(max(z - col - 32 * i, 0), 32), aa = min(max(a - col - 32 * i, 0), 32);
               const uint32_t bits = (uint32_t)((1ull << za) - 1) & ~(uint32_t)((1ull << aa) - 1);
 #pragma unroll
-              for (int u = 0; u < 32; ++u) s[32 * i + u] = bits >> u & 1 ? s[32 * i + u] : -INFINITY;
+              for (int u = 0; u < 32; ++u) s[32 * i + u] = bits >> u & 1 ? s[32 * i + u] : 0xFF800000u;  // -inf
             }
-          }
+          };
+          if (cut) mask(sa, 0), mask(sb, 64);
           float mx[4] = {m, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int i = 0; i < 128; i += 8)
+          for (int i = 0; i < 64; i += 4)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) mx[u] = fmaxf(mx[u], fmaxf(s[i + 2 * u], s[i + 2 * u + 1]));
+            for (int u = 0; u < 2; ++u) {
+              mx[u] = fmaxf(mx[u], fmaxf(__uint_as_float(sa[i + 2 * u]), __uint_as_float(sa[i + 2 * u + 1])));
+              mx[2 + u] = fmaxf(mx[2 + u], fmaxf(__uint_as_float(sb[i + 2 * u]), __uint_as_float(sb[i + 2 * u + 1])));
+            }
           const float mn = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
           bool waited = two || j == 0;  // two row tiles: S(g + 2) is formed after O(g)
           if (j == 0) {
@@ -381,6 +385,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
               uint32_t o[32];
               tc::ld32(col_o + i * 32, o);
               tc::wait_ld();
+              tc::pin32(o);
 #pragma unroll
               for (int u = 0; u < 32; ++u) o[u] = __float_as_uint(__uint_as_float(o[u]) * f);
               tc::st32(col_o + i * 32, o);
@@ -389,19 +394,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           const float ms = m == -INFINITY ? 0.f : m * sc2;
           const uint64_t sc2x2 = tc::pack2(sc2, sc2), nms2 = tc::pack2(-ms, -ms);
           uint64_t sum[2] = {0, 0};
+          auto exps = [&](uint32_t* s, uint32_t col) {  // 64 scores -> P, written over S
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t pk[16];
+            for (int i = 0; i < 2; ++i) {
+              uint32_t pk[16];
 #pragma unroll
-            for (int u = 0; u < 16; ++u) {
-              float e0, e1;
-              tc::unpack2(tc::fma2(tc::pack2(s[32 * i + 2 * u], s[32 * i + 2 * u + 1]), sc2x2, nms2), e0, e1);
-              e0 = ex2(e0), e1 = ex2(e1);
-              sum[u & 1] = tc::add2(sum[u & 1], tc::pack2(e0, e1));
-              pk[u] = Half2<T>::down(e0, e1);
+              for (int u = 0; u < 16; ++u) {
+                float e0, e1;
+                tc::unpack2(tc::fma2(tc::pack2(__uint_as_float(s[32 * i + 2 * u]), __uint_as_float(s[32 * i + 2 * u + 1])), sc2x2, nms2),
+                            e0, e1);
+                e0 = ex2(e0), e1 = ex2(e1);
+                sum[u & 1] = tc::add2(sum[u & 1], tc::pack2(e0, e1));
+                pk[u] = Half2<T>::down(e0, e1);
+              }
+              tc::st16(col_s + col + i * 16, pk);
             }
-            tc::st16(col_s + i * 16, pk);
-          }
+          };
+          tc::ld32(col_s + 64, sb);
+          tc::ld32(col_s + 96, sb + 32);
+          exps(sa, 0);
+          tc::wait_ld();
+          tc::pin32(sb), tc::pin32(sb + 32);
+          if (cut) mask(sb, 64);
+          exps(sb, 32);
           float l0, l1;
           tc::unpack2(tc::add2(sum[0], sum[1]), l0, l1);
           l += l0 + l1;
@@ -419,19 +434,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         if (!(alive = wait_all(kBO + wg, oph))) break;
         oph ^= 1;
         tc::fence_after();
-        const bool whole = g.j0 == 0 && g.j1 == g.t.nt;
+        const bool whole = nj == nt;
         // partials column group by column group, so that a warp's rows are neighbours
-        const int64_t pr0 = ((int64_t)b * 2 + (g.j0 == 0)) * C::kRows, pr = pr0 + wg * 128 + row;
+        const int64_t pr0 = ((int64_t)b * 2 + (j0 == 0)) * C::kRows, pr = pr0 + wg * 128 + row;
         float* po = parts.o + pr0 * D + (wg * 128 + row) * 4;
         const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
         const bool wide = (((uintptr_t)c.out | (uintptr_t)(c.out_stride * 2)) & 31) == 0;  // 32-byte stores: whole sectors
-        const int head = g.h * st.G + R % st.G;
-        T* out = static_cast<T*>(c.out) + (int64_t)(g.sp.q0 + tok) * c.out_stride + (int64_t)head * D;
+        const int head = h * st.G + R % st.G;
+        T* out = static_cast<T*>(c.out) + (int64_t)(q0 + tok) * c.out_stride + (int64_t)head * D;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
           uint32_t o[32];
           tc::ld32(col_o + i * 32, o);
           tc::wait_ld();
+          tc::pin32(o);
           if (!ok) continue;
           if (whole) {
 #pragma unroll
@@ -459,16 +475,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         if (ok) {
           const float mm = m == -INFINITY ? m : m * sc2;
           if (!whole) parts.ml[pr] = make_float2(mm, l);
-          else if (c.lse) c.lse[(int64_t)(g.sp.q0 + tok) * st.Hq + head] = l > 0.f ? (mm + log2f(l)) * kLn2 : -INFINITY;
+          else if (c.lse) c.lse[(int64_t)(q0 + tok) * st.Hq + head] = l > 0.f ? (mm + log2f(l)) * kLn2 : -INFINITY;
         }
-        if (tid == 0 && g.j0 == 0 && !whole) {
+        if (tid == 0 && j0 == 0 && !whole) {
           // the block of the segment's last key tile, by the place of its first job
-          const int64_t last = g.at + (int64_t)(g.t.nt - 1) * g.t.jobs;
           rec_n = (int)((B * (last + 1) - 1) / total) - (int)b + 1;
-          parts.rec[b] = {g.sp.q0, g.h, g.qt * C::kRows, g.t.rows, rec_n};
+          parts.rec[b] = {q0, h, R0, rows, rec_n};
         }
       }
-      par = (par + nj * g.t.jobs) & 1;
+      par = (par + (nj << two)) & 1;
     }
     if (tid == 0 && rec_n == 0) parts.rec[b].n = 0;
   } else if (warp <= kPvWarp) {
@@ -477,8 +492,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     // there one by one they cost as much as the products).
     auto uniform = [](uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); };
     const uint32_t bars0 = uniform(smem_u32(bars)), tm = uniform(tmem);
-    Walk w;
-    walk_start<D>(w, c, p, tiles, t0, t1);
+    Walk w0;
+    walk_start(w0, c, p, tiles, C::kRows, t0, t1);
+    Walk w = w0;
     Jobs jb;
     jb.take(w);
     uint32_t slot = 0, sph = 0, buf = 0, g = 0;  // next ring slot and its phase, buffer of S and P, job
@@ -532,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         }
         if (!ok) break;
         if (++jb.i == jb.n) {
-          walk_next<D>(w, c, p);
+          w.next(c, p, C::kRows);
           jb.take(w);
         }
       }
@@ -581,7 +597,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         }
         if (!ok) break;
         if (++jb.i == jb.n) {
-          walk_next<D>(w, c, p);
+          w.next(c, p, C::kRows);
           jb.take(w);
         }
       }
@@ -622,32 +638,32 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
       announce(false);
       pending = bar;
     };
-    Walk w;
-    walk_start<D>(w, c, p, tiles, t0, t1);
+    Walk w0;
+    walk_start(w0, c, p, tiles, C::kRows, t0, t1);
+    Walk w = w0;
 #pragma unroll 1
-    for (; w.more && ok; walk_next<D>(w, c, p)) {
-      const Seg g = w.g;
+    for (; w.more && ok; w.next(c, p, C::kRows)) {
       if (is_k) {  // the segment's rows of q
         if (!(ok = wait_free(kBQFree, seg_ph))) break;
         seg_ph ^= 1;
         if (c.q_box) {
-          const int n = g.t.jobs * C::kU;
+          const int n = (w.two + 1) * C::kU;
           announce(true);
           if (lane == 0) mbar_arrive_tx(&bars[kBQFull], n * kUnitBytes);
           __syncwarp();
           if (lane < n)
-            tma_load_3d(smem0 + lane * kUnitBytes, &maps.q, lane % C::kU * 64, g.h * st.G,
-                        g.sp.q0 + (g.qt * C::kRows + lane / C::kU * 128) / st.G, bars0 + kBQFull * 8);
+            tma_load_3d(smem0 + lane * kUnitBytes, &maps.q, lane % C::kU * 64, w.h * st.G,
+                        w.q0 + (w.qt * C::kRows + lane / C::kU * 128) / st.G, bars0 + kBQFull * 8);
         } else {
-          const int n = 2 * g.t.jobs * C::kU;  // halves of units
+          const int n = 2 * (w.two + 1) * C::kU;  // halves of units
 #pragma unroll 1
           for (int v = 0; v < n; ++v) {
             const int x = (v >> 1) / C::kU, u = (v >> 1) % C::kU;
             int64_t at[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              const int r = x * 128 + (v & 1) * 64 + i * 32 + lane, R = g.qt * C::kRows + r;
-              at[i] = r < g.t.rows ? (int64_t)(g.sp.q0 + R / st.G) * c.q_stride + (int64_t)(g.h * st.G + R % st.G) * D : -1;
+              const int r = x * 128 + (v & 1) * 64 + i * 32 + lane, R = w.qt * C::kRows + r;
+              at[i] = r < w.rows ? (int64_t)(w.q0 + R / st.G) * c.q_stride + (int64_t)(w.h * st.G + R % st.G) * D : -1;
             }
             copy_lines<T>(smem0 + (uint32_t)v * (kUnitBytes / 2), static_cast<const T*>(c.q) + u * 64, at[0], at[1]);
           }
@@ -655,18 +671,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           announce(true);
         }
       }
+      const int lo0 = vis_lo(c, w.len - w.n);  // the sequence's first line that any token of the step sees
       const int un = lane / max(n_box, 1), bx = lane - un * n_box;  // TMA: this lane's box bx of unit un of a slot
 #pragma unroll 1
-      for (int j = g.j0; j < g.j1 && ok; ++j) {
-        const int k0 = g.t.start + j * kKeys;
+      for (int j = w.j0; j < w.j1 && ok; ++j) {
+        const int k0 = w.start + j * kKeys;
         // TMA where all the tile's lines are the sequence's, and seen by some token of the step
-        const bool tma = n_box && k0 >= g.lo && k0 + kKeys <= g.sp.len;
+        const bool tma = n_box && k0 >= lo0 && k0 + kKeys <= w.len;
         int page = 0, line = 0;
         int64_t at[4] = {-1, -1, -1, -1};
         if (tma) {
           if (un < C::kSlotU) {
             const int l0 = k0 + bx * c.box, pi = (int)fast_div((uint32_t)l0, st.page_mul, st.page_shift);
-            const int raw = __ldg(st.pages + (int64_t)g.s * st.pages_per_seq + pi);
+            const int raw = __ldg(st.pages + (int64_t)w.s * st.pages_per_seq + pi);
             page = min(max(raw, 0), st.n_pages - 1);
             if (page != raw) attn_report(st, kAttnRange);
             line = l0 - pi * st.page_size;
@@ -675,7 +692,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int l0 = k0 + i * 32 + lane;
-            if (l0 >= g.lo && l0 < g.t.end) at[i] = line_offset(st, g.s, l0) + (int64_t)g.h * st.head_stride;
+            if (l0 >= lo0 && l0 < w.end) at[i] = line_offset(st, w.s, l0) + (int64_t)w.h * st.head_stride;
           }
         }
 #pragma unroll 1
@@ -686,7 +703,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
             if (lane == 0) mbar_arrive_tx(&bars[full + slot], C::kSlotBytes);
             __syncwarp();
             if (un < C::kSlotU)
-              tma_load_4d(dst + un * kUnitBytes + bx * c.box * 128, tm, (u * C::kSlotU + un) * 64, g.h, line, page,
+              tma_load_4d(dst + un * kUnitBytes + bx * c.box * 128, tm, (u * C::kSlotU + un) * 64, w.h, line, page,
                           bars0 + (full + slot) * 8);
             tx |= 1u << slot;
           } else {
