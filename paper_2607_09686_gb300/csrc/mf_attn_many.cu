@@ -5,7 +5,8 @@
 // A work item ("segment") is one or two row tiles of a (sequence, kv head) and the 128-line key tiles that
 // any of their rows sees; per key tile and row tile ("job")
 //   S = Q K^T (tcgen05, both operands in shared memory)  ->  tensor memory, 128 fp32 columns
-//   P = 2^(scale log2e S - m), rounded to the cache's type, written over S      (one thread a row)
+//   P = 2^(scale log2e S - m), rounded to the cache's type, written over S      (one thread a row; the first 64 lines'
+//                                                              products with V begin while the others are computed)
 //   O += P V  (A from tensor memory, V read as it lies: its lines are the K dimension, an MN-major operand)
 // with a running maximum m and sum l per row.  O is rescaled only when m grows by more than 2^8 (until then the old m
 // serves: p stays below 2^8, and o and l carry the same factor); so most key tiles touch O not at all.
@@ -266,9 +267,9 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 // shared memory: [Q][ring of K][ring of V]; barriers: slots full and free, Q full and free, S and P by (warpgroup,
-// buffer), O by row tile, the buffers free again, the end of all MMAs
+// buffer; kBP2: the second half of P), O by row tile, the buffers free again, the end of all MMAs
 constexpr int kBKFull = 0, kBKFree = 5, kBVFull = 10, kBVFree = 15, kBQFull = 20, kBQFree = 21, kBS = 22, kBP = 26, kBO = 30,
-              kBBuf = 32, kBDrain = 34, kBars = 36;
+              kBBuf = 32, kBDrain = 34, kBP2 = 36, kBars = 40;
 
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant__ AttnCall c, const __grid_constant__ AttnMaps maps,
@@ -285,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const AttnStep& st = c.st;
   if (tid == 0) {
-    for (int i = 0; i < kBars; ++i) mbar_init(&bars[i], i >= kBP && i < kBP + 4 ? 4 : 1);
+    for (int i = 0; i < kBars; ++i) mbar_init(&bars[i], (i >= kBP && i < kBP + 4) || i >= kBP2 ? 4 : 1);
     s_flag = 0;
     mbar_fence_init();
   }
@@ -338,6 +339,23 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           ++sph[buf];
           tc::fence_after();
           const uint32_t col_s = tmem + lanes + kColS + buf * 128;
+          const int k0 = k_start + j * kKeys, a = lo - k0, z = hi - k0;  // columns [a, z) are seen
+          if (__any_sync(0xffffffffu, a > 0 || z < kKeys)) {
+            // a tile at an edge (one or two of a segment): -inf written over the others
+#pragma unroll
+            for (int i = 0; i < 128; i += 32) {
+              uint32_t v[32];
+              tc::ld32(col_s + i, v);
+              tc::wait_ld();
+              tc::pin32(v);
+              const int za = min(max(z - i, 0), 32), aa = min(max(a - i, 0), 32);
+              const uint32_t bits = (uint32_t)((1ull << za) - 1) & ~(uint32_t)((1ull << aa) - 1);
+#pragma unroll
+              for (int u = 0; u < 32; ++u) v[u] = bits >> u & 1 ? v[u] : 0xFF800000u;
+              tc::st32(col_s + i, v);
+            }
+            tc::wait_st();
+          }
           // the row's scores: the first 64 stay in registers, the others are read again when their turn comes
           uint32_t sa[64], sb[64];
           tc::ld32(col_s, sa);
@@ -346,18 +364,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           tc::ld32(col_s + 96, sb + 32);
           tc::wait_ld();
           tc::pin32(sa), tc::pin32(sa + 32), tc::pin32(sb), tc::pin32(sb + 32);
-          const int k0 = k_start + j * kKeys, a = lo - k0, z = hi - k0;  // columns [a, z) are seen
-          const bool cut = __any_sync(0xffffffffu, a > 0 || z < kKeys);
-          auto mask = [&](uint32_t* s, int col) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int za = min(max(z - col - 32 * i, 0), 32), aa = min(max(a - col - 32 * i, 0), 32);
-              const uint32_t bits = (uint32_t)((1ull << za) - 1) & ~(uint32_t)((1ull << aa) - 1);
-#pragma unroll
-              for (int u = 0; u < 32; ++u) s[32 * i + u] = bits >> u & 1 ? s[32 * i + u] : 0xFF800000u;  // -inf
-            }
-          };
-          if (cut) mask(sa, 0), mask(sb, 64);
           float mx[4] = {m, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
           for (int i = 0; i < 64; i += 4)
@@ -413,13 +419,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           tc::ld32(col_s + 64, sb);
           tc::ld32(col_s + 96, sb + 32);
           exps(sa, 0);
-          tc::wait_ld();
-          tc::pin32(sb), tc::pin32(sb + 32);
-          if (cut) mask(sb, 64);
-          exps(sb, 32);
-          float l0, l1;
-          tc::unpack2(tc::add2(sum[0], sum[1]), l0, l1);
-          l += l0 + l1;
           tc::wait_st();
           if (!waited) {  // keeps this barrier's phases in step
             if (!(alive = wait_all(kBO + wg, oph))) break;
@@ -428,6 +427,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           tc::fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&bars[kBP + wg * 2 + buf]);
+          tc::wait_ld();
+          tc::pin32(sb), tc::pin32(sb + 32);
+          exps(sb, 32);
+          float l0, l1;
+          tc::unpack2(tc::add2(sum[0], sum[1]), l0, l1);
+          l += l0 + l1;
+          tc::wait_st();
+          tc::fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars[kBP2 + wg * 2 + buf]);
         }
         if (!alive) break;
         // ---- the piece's o
@@ -438,34 +447,65 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         // partials column group by column group, so that a warp's rows are neighbours
         const int64_t pr0 = ((int64_t)b * 2 + (j0 == 0)) * C::kRows, pr = pr0 + wg * 128 + row;
         float* po = parts.o + pr0 * D + (wg * 128 + row) * 4;
-        const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
-        const bool wide = (((uintptr_t)c.out | (uintptr_t)(c.out_stride * 2)) & 31) == 0;  // 32-byte stores: whole sectors
         const int head = h * st.G + R % st.G;
-        T* out = static_cast<T*>(c.out) + (int64_t)(q0 + tok) * c.out_stride + (int64_t)head * D;
+        if (whole) {
+          // 64 columns at a time: 32 bytes of a row and lane, transposed among four lanes, so that these store 128
+          // neighbouring bytes of one row after the other (a row a lane, the stores took 4000 cycles a segment)
+          const float inv = l > 0.f ? 1.f / l : 0.f;
+          const bool wide = (((uintptr_t)c.out | (uintptr_t)(c.out_stride * 2)) & 31) == 0;
+          const int64_t at = ok ? (int64_t)(q0 + tok) * c.out_stride + (int64_t)head * D : -1;
+          T* out[4];  // where the rows of this lane's four begin, this lane's quarter of 64 columns; null: no row
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-          uint32_t o[32];
-          tc::ld32(col_o + i * 32, o);
-          tc::wait_ld();
-          tc::pin32(o);
-          if (!ok) continue;
-          if (whole) {
+          for (int i = 0; i < 4; ++i) {
+            const int64_t o = __shfl_sync(0xffffffffu, at, (lane & ~3) + i);
+            out[i] = o < 0 ? nullptr : static_cast<T*>(c.out) + o + (lane & 3) * 16;
+          }
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              uint32_t v[8];
+          for (int i = 0; i < D / 64; ++i) {
+            uint32_t o[64], v[4][8];
+            tc::ld32(col_o + i * 64, o);
+            tc::ld32(col_o + i * 64 + 32, o + 32);
+            tc::wait_ld();
+            tc::pin32(o), tc::pin32(o + 32);
 #pragma unroll
-              for (int x = 0; x < 8; ++x)
-                v[x] = Half2<T>::down(__uint_as_float(o[16 * u + 2 * x]) * inv, __uint_as_float(o[16 * u + 2 * x + 1]) * inv);
-              if (wide) {
-                asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(out + i * 32 + u * 16), "r"(v[0]), "r"(v[1]),
-                             "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-                             : "memory");
-              } else {
-                *reinterpret_cast<uint4*>(out + i * 32 + u * 16) = make_uint4(v[0], v[1], v[2], v[3]);
-                *reinterpret_cast<uint4*>(out + i * 32 + u * 16 + 8) = make_uint4(v[4], v[5], v[6], v[7]);
+            for (int u = 0; u < 32; ++u) v[u >> 3][u & 7] = Half2<T>::down(__uint_as_float(o[2 * u]) * inv, __uint_as_float(o[2 * u + 1]) * inv);
+#pragma unroll
+            for (int bit = 1; bit <= 2; bit <<= 1) {
+              const bool up = lane & bit;
+#pragma unroll
+              for (int q = 0; q < 4; ++q) {
+                if (q & bit) continue;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {  // blocks q and q + bit: the one that belongs to the other lane changes places
+                  const uint32_t give = up ? v[q][x] : v[q + bit][x];
+                  const uint32_t got = __shfl_xor_sync(0xffffffffu, give, bit);
+                  if (up) v[q][x] = got;
+                  else v[q + bit][x] = got;
+                }
               }
             }
-          } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {  // v[r]: columns 16 (lane % 4) .. of the 64, row r of the four
+              if (!out[r]) continue;
+              T* to = out[r] + i * 64;
+              if (wide) {
+                asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(to), "r"(v[r][0]), "r"(v[r][1]), "r"(v[r][2]),
+                             "r"(v[r][3]), "r"(v[r][4]), "r"(v[r][5]), "r"(v[r][6]), "r"(v[r][7])
+                             : "memory");
+              } else {
+                *reinterpret_cast<uint4*>(to) = make_uint4(v[r][0], v[r][1], v[r][2], v[r][3]);
+                *reinterpret_cast<uint4*>(to + 8) = make_uint4(v[r][4], v[r][5], v[r][6], v[r][7]);
+              }
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i) {
+            uint32_t o[32];
+            tc::ld32(col_o + i * 32, o);
+            tc::wait_ld();
+            tc::pin32(o);
+            if (!ok) continue;
 #pragma unroll
             for (int u = 0; u < 8; ++u)
               *reinterpret_cast<uint4*>(po + (int64_t)(i * 8 + u) * (C::kRows * 4)) =
@@ -516,11 +556,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
             if (++slot == C::kKSlots) slot = 0, sph ^= 1;
           }
         }
+        const uint32_t x = uniform(jb.row_tile()), b_ = uniform(buf), end = uniform(jb.i == jb.n - 1),
+                       last = uniform(jb.last_of_tile()), f = uniform(first);
         if (g >= 2) ok = ok && wait_all(kBBuf + (int)buf, (g >> 1) + 1 & 1);  // P of job g - 2 has been read
         if (!ok) break;
         tc::fence_after();
-        const uint32_t x = uniform(jb.row_tile()), b_ = uniform(buf), end = uniform(jb.i == jb.n - 1),
-                       last = uniform(jb.last_of_tile()), f = uniform(first);
 #pragma unroll
         for (int v = 0; v < C::kTileSlots; ++v) {
           const uint32_t sl = f + v >= C::kKSlots ? f + v - C::kKSlots : f + v;
@@ -567,13 +607,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           }
         }
         const int pb = jb.row_tile() * 2 + (int)buf;
+        const uint32_t x = uniform(jb.row_tile()), b_ = uniform(buf), acc = uniform(jb.i > jb.two), f = uniform(first);
+        // two row tiles: only their last product is waited for (their next S is formed after it), else each one
+        const uint32_t tell = uniform(!jb.two || jb.i + 2 >= jb.n), last = uniform(jb.last_of_tile());
         ok = ok && wait_all(kBP + pb, pph >> pb & 1);
         if (!ok) break;
         pph ^= 1u << pb;
         tc::fence_after();
-        const uint32_t x = uniform(jb.row_tile()), b_ = uniform(buf), acc = uniform(jb.i > jb.two), f = uniform(first);
-        // two row tiles: only their last product is waited for (their next S is formed after it), else each one
-        const uint32_t tell = uniform(!jb.two || jb.i + 2 >= jb.n), last = uniform(jb.last_of_tile());
 #pragma unroll
         for (int v = 0; v < C::kTileSlots; ++v) {
           const uint32_t sl = f + v >= C::kVSlots ? f + v - C::kVSlots : f + v;
@@ -582,11 +622,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
             if (++slot == C::kVSlots) slot = 0, sph ^= 1;
             tc::fence_after();
           }
+          const uint64_t bd = tc::desc_sw128(r0 + sl * C::kSlotBytes, kUnitBytes);
           if (tc::elect_one()) {
-            const uint64_t bd = tc::desc_sw128(r0 + sl * C::kSlotBytes, kUnitBytes);
 #pragma unroll
-            for (int k = 0; k < 8; ++k)  // 16 lines: two groups of eight
+            for (int k = 0; k < 4; ++k)  // 16 lines: two groups of eight
               tc::mma_ts(tm + kColO + x * D + v * 128, tm + kColS + b_ * 128 + k * 8, bd + k * (2048 >> 4), kId, acc | (k > 0));
+          }
+          __syncwarp();
+          if (v == 0) {
+            if (!(ok = wait_all(kBP2 + pb, pph >> pb & 1 ^ 1))) break;
+            tc::fence_after();
+          }
+          if (tc::elect_one()) {
+#pragma unroll
+            for (int k = 4; k < 8; ++k)
+              tc::mma_ts(tm + kColO + x * D + v * 128, tm + kColS + b_ * 128 + k * 8, bd + k * (2048 >> 4), kId, 1);
             if (v == C::kTileSlots - 1) {
               tc::commit(bars0 + (kBBuf + b_) * 8);
               if (tell) tc::commit(bars0 + (kBO + x) * 8);
