@@ -217,6 +217,18 @@ struct Jobs {
   __device__ __forceinline__ bool last_of_tile() const { return !two || (i & 1); }
 };
 
+// What the softmax needs of a segment.  Each of its warps keeps this and the next one in shared memory: the registers
+// hold scores.
+struct Piece {
+  int nj, two, k_start, R0, rows, h, q0, first, len, nt, j0, more;
+  int64_t last;  // place of the last key tile's first job
+  __device__ __forceinline__ void take(const Walk& w, int tile_rows) {
+    more = w.more, two = w.two, nj = w.j1 - w.j0, k_start = w.start + w.j0 * kKeys, R0 = w.qt * tile_rows, rows = w.rows;
+    h = w.h, q0 = w.q0, first = w.len - w.n, len = w.len, nt = w.nt, j0 = w.j0;
+    last = w.at + ((int64_t)(nt - 1) << two);
+  }
+};
+
 // A wait whose first poll failed; false, with the block's flag and the error word set, once any wait gave up.
 __device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, volatile int* flag, unsigned* err) {
   if (*flag) return false;
@@ -279,6 +291,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
   constexpr bool kBf = Half2<T>::kBf16;
   extern __shared__ unsigned char smem_raw[];
   __shared__ uint64_t bars[kBars];
+  __shared__ Piece s_piece[8][2];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_flag;
   const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -322,15 +335,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     uint32_t oph = 0;                // phase of its O barrier
     int rec_n = 0;
     bool alive = true;
-    while (w.more && alive) {
-      const int nj = w.j1 - w.j0, two = w.two, k_start = w.start + w.j0 * kKeys, R0 = w.qt * C::kRows, rows = w.rows, h = w.h,
-                q0 = w.q0, first = w.len - w.n, len = w.len, nt = w.nt, j0 = w.j0;
-      const int64_t last = w.at + ((int64_t)(nt - 1) << two);  // place of the last key tile's first job
+    int at = 0;
+    if (lane == 0) s_piece[warp][0].take(w, C::kRows);
+    __syncwarp();
+    auto advance = [&]() {  // the next segment into the other place
       walk_next(w, c, p, C::kRows);
+      if (lane == 0) s_piece[warp][at ^ 1].take(w, C::kRows);
+      __syncwarp();
+    };
+    for (; s_piece[warp][at].more && alive; at ^= 1) {
+      const Piece& cur = s_piece[warp][at];
+      const int nj = cur.nj, two = cur.two, k_start = cur.k_start;
       if (two || wg == 0) {
-        const int R = R0 + wg * 128 + row, tok = R / st.G, pos = first + tok;
-        const bool ok = wg * 128 + row < rows;
-        const int lo = ok ? vis_lo(c, pos) : 0, hi = ok ? vis_hi(c, pos, len) : 0;
+        const bool ok = wg * 128 + row < cur.rows;
+        const int pos = cur.first + (cur.R0 + wg * 128 + row) / st.G;
+        const int lo = ok ? vis_lo(c, pos) : 0, hi = ok ? vis_hi(c, pos, cur.len) : 0;
         const uint32_t col_o = tmem + lanes + kColO + (two ? wg * D : 0);
         float m = -INFINITY, l = 0.f;
         for (int j = 0; j < nj; ++j) {
@@ -439,11 +458,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           if (lane == 0) mbar_arrive(&bars[kBP2 + wg * 2 + buf]);
         }
         if (!alive) break;
+        // the next segment is looked up while the last product runs: after the stores below its loads would queue
+        advance();
         // ---- the piece's o
         if (!(alive = wait_all(kBO + wg, oph))) break;
         oph ^= 1;
         tc::fence_after();
-        const bool whole = nj == nt;
+        const int R = cur.R0 + wg * 128 + row, tok = R / st.G, q0 = cur.q0, h = cur.h, j0 = cur.j0;
+        const bool whole = nj == cur.nt;
         // partials column group by column group, so that a warp's rows are neighbours
         const int64_t pr0 = ((int64_t)b * 2 + (j0 == 0)) * C::kRows, pr = pr0 + wg * 128 + row;
         float* po = parts.o + pr0 * D + (wg * 128 + row) * 4;
@@ -519,10 +541,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         }
         if (tid == 0 && j0 == 0 && !whole) {
           // the block of the segment's last key tile, by the place of its first job
-          rec_n = (int)((B * (last + 1) - 1) / total) - (int)b + 1;
-          parts.rec[b] = {q0, h, R0, rows, rec_n};
+          rec_n = (int)((B * (cur.last + 1) - 1) / total) - (int)b + 1;
+          parts.rec[b] = {q0, h, cur.R0, cur.rows, rec_n};
         }
       }
+      if (!two && wg == 1) advance();
       par = (par + (nj << two)) & 1;
     }
     if (tid == 0 && rec_n == 0) parts.rec[b].n = 0;
