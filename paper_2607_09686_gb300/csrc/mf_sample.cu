@@ -5,19 +5,20 @@
 // index: all entries with a larger x, and those equal to it up to that index (and w >= min_p, which needs no order).
 //
 // A cluster of 1 to 8 blocks has a row, each block a slice of it in shared memory: the logits cross the memory bus
-// once, whatever the steps that follow (a step reads shared memory, 64 entries a thread; noise is read for kept entries
-// alone).  Sums and choices of the blocks meet in distributed shared memory.  Steps:
-//   1. load, M = max.
-//   2. top-k: a histogram of counts over bins of 1/64 in z; the bin where the count passes k.  If the entries down to
-//      that bin are few (kList), they go to the leading block, which sorts them and finishes alone: top-p, min-p, argmax.
+// once, whatever the steps that follow.  Sums and choices of the blocks meet in distributed shared memory.  Steps:
+//   1. load (bulk copies; where nothing is cut the noise with it), M = max.
+//   2. top-k: the k-th largest of the threads' own maxima is a floor of the k-th largest entry, and hardly more than k
+//      entries reach it; these go to the leading block, which sorts them and finishes alone: top-p, min-p, argmax.  (Where k
+//      is large for that, a histogram of counts over bins of 1/64 in z takes the maxima's place.)
 //   3. top-p of what may be many entries: a histogram of masses.  A bin's mass is a sum of integers, w / e^(-bin / 64)
 //      in units of 2^-q, so it hangs on no order of additions; the border bin's entries are sorted as above.
 //      (Bits: a slice of 2^s entries leaves q = 31 - s; rounding to a unit is random and below 2^-16 of an entry.)
 //   4. a border bin that is too large is cut by bisection over the value's 32-bit key, and equal values by counting them
 //      in the order of their index.
-//   5. one pass over what is kept: sum of w, argmax of z + noise.
-// What bounds it: a few passes of some ten instructions an entry and the cluster's barriers, about 1 us each; not
-// the memory.
+//   5. what is kept: sum of w and the largest z + noise, with z as a product; then the entries that come near that one
+//      again, with z as the exact quotient.
+// What bounds it: with top-k the cluster's barriers and one pass over the slice; else passes of some ten to twenty
+// instructions an entry.
 #include <cooperative_groups.h>
 
 #include <cmath>
@@ -31,10 +32,9 @@ namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxVocab = 1 << 20;
-constexpr int kBins = 2048, kList = 4096;
+constexpr int kBins = 2048, kList = 4096, kShort = 256;
 constexpr float kBinsPerUnit = 64.f;
 constexpr size_t kResident = 128 * 1024;  // bytes of a slice that are kept in shared memory
-constexpr uint32_t kKeyNone = 0x007FFFFFu;  // the key of -inf
 
 struct SampleCall {
   const void* logits;
@@ -46,6 +46,7 @@ struct SampleCall {
   int vocab;
   int slice;  // entries of a block
   int qbits;  // bits of a mass unit
+  int keep;   // the slice's logits (1), and its noise too (2), lie in shared memory
 };
 
 // larger floats have larger keys (-0 and +0 compare equal as floats: one key)
@@ -55,7 +56,10 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
 __device__ __forceinline__ float z_of(float x, float m, float t) { return x == m ? 0.f : __fdiv_rn(x - m, t); }
-__device__ __forceinline__ int bin_of(float z) { return (int)fminf(-z * kBinsPerUnit, (float)(kBins - 1)); }
+// bin of an entry `d` = x - M; monotonic in d (inv: bins per unit of d)
+__device__ __forceinline__ int bin_of(float d, float inv) {
+  return d == 0.f ? 0 : (int)fminf(-d * inv, (float)(kBins - 1));  // (inv may be infinite)
+}
 
 struct Best {  // the largest z + noise so far, the lowest index where equal
   float v, z;
@@ -66,9 +70,10 @@ struct Best {  // the largest z + noise so far, the lowest index where equal
 };
 
 struct Shared {
-  float d[2][kWarps];    // sums of the warps
-  double pub[2];         // sums of the block, which the cluster reads
-  float f[kWarps + 1];
+  float d[kWarps];       // sums of the warps
+  float pub[2];          // sums of the block, which the cluster reads
+  float f[kWarps], mx;   // maxima of the warps, of the block
+  float top[2];          // the block's largest key
   int n[kWarps + 1];
   Best best[kWarps + 1];
   // the leading block's answers
@@ -78,10 +83,12 @@ struct Shared {
   uint32_t key;
   int index;
   int here;
+  uint64_t bar;  // the bulk copies' barrier
 };
 
-template <class T>
-__global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
+// kCut: some row may have top-k or top-p.  Without, a block needs fewer registers and three find room on an SM.
+template <class T, bool kCut>
+__global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c) {
   extern __shared__ __align__(16) unsigned char dyn[];
   __shared__ Shared sh;
   cg::cluster_group cl = cg::this_cluster();
@@ -95,51 +102,91 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   Shared* lead = cl.map_shared_rank(&sh, 0);
   unsigned long long* lead_list = cl.map_shared_rank(list, 0);
 
-  // ---- 1. the slice into shared memory (at the same place modulo 16 bytes, so that whole vectors are copied)
+  // ---- 1. the slice into shared memory, at the same place modulo 16 bytes: whole vectors by bulk copies, the ends by hand
+  auto up = [](T v) -> float { return fmaxf((float)v, -INFINITY); };  // NaN as -inf
   const T* src = row;
-  float mx = -INFINITY;
-  auto up = [](T v) -> float {  // NaN as -inf
-    const float x = (float)v;
-    return x == x ? x : -INFINITY;
-  };
-  if ((size_t)c.slice * sizeof(T) <= kResident) {
-    constexpr int kV = 16 / sizeof(T);
-    T* keep = reinterpret_cast<T*>(dyn + kBins * 4 + kList * 8) + (((uintptr_t)row & 15) / sizeof(T));
-    const int head = min(n, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T)), vecs = (n - head) / kV;
-    const uint4* from = reinterpret_cast<const uint4*>(row + head);
-    uint4* to = reinterpret_cast<uint4*>(keep + head);
-#pragma unroll 4
-    for (int i = tid; i < vecs; i += kThreads) {
-      const uint4 v = ld_stream(from + i);
-      to[i] = v;
-      const T* e = reinterpret_cast<const T*>(&v);
-#pragma unroll
-      for (int u = 0; u < kV; ++u) mx = fmaxf(mx, up(e[u]));
+  const float* gsrc = noise;
+  bool lost = false;  // a copy did not arrive in time: the row has no answer (as if it had no entry)
+  if (c.keep) {
+    unsigned char* room = dyn + (c.keep == 2 ? 0 : kBins * 4 + kList * 8);
+    T* x0 = reinterpret_cast<T*>(room + ((uintptr_t)row & 15));
+    float* g0 = reinterpret_cast<float*>(room + (((size_t)c.slice * sizeof(T) + 31) & ~size_t(15)) + ((uintptr_t)noise & 15));
+    auto ends = [&](const auto* from, auto* to, int& head, int& body) {
+      constexpr int kE = (int)sizeof(*from);
+      head = min(n, (int)((16 - ((uintptr_t)from & 15)) & 15) / kE);
+      body = (n - head) * kE / 16 * 16 / kE;
+      for (int i = tid; i < n - body; i += kThreads) {
+        const int at = i < head ? i : body + i;
+        to[at] = from[at];
+      }
+    };
+    int hx, bx, hg = 0, bg = 0;
+    if (tid == 0) {
+      mbar_init(&sh.bar, 1);
+      mbar_fence_init();
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    const int rest = head + vecs * kV;
-    for (int i = tid; i < head + n - rest; i += kThreads) {
-      const int at = i < head ? i : rest + i - head;
-      keep[at] = row[at];
-      mx = fmaxf(mx, up(row[at]));
+    ends(row, x0, hx, bx);
+    if (c.keep == 2) ends(noise, g0, hg, bg);
+    if (tid == 0) {
+      mbar_arrive_tx(&sh.bar, (uint32_t)(bx * sizeof(T) + bg * 4));
+      // pieces of 32 KiB: several copies in flight
+      auto copy = [&](unsigned char* to, const unsigned char* from, uint32_t bytes) {
+        for (uint32_t o = 0; o < bytes; o += 32768) bulk_g2s(to + o, from + o, min(bytes - o, 32768u), &sh.bar);
+      };
+      copy(reinterpret_cast<unsigned char*>(x0 + hx), reinterpret_cast<const unsigned char*>(row + hx), (uint32_t)(bx * sizeof(T)));
+      copy(reinterpret_cast<unsigned char*>(g0 + hg), reinterpret_cast<const unsigned char*>(noise + hg), (uint32_t)(bg * 4));
     }
-    src = keep;
-  } else {
-    for (int i = tid; i < n; i += kThreads) mx = fmaxf(mx, up(row[i]));
+    __syncthreads();
+    lost = __syncthreads_or(!mbar_wait(&sh.bar, 0, kDefaultWaitNs));
+    src = x0;
+    if (c.keep == 2) gsrc = g0;
   }
+  // every thread's entries: whole vectors of the slice where it lies in shared memory
+  auto for_each = [&](auto&& f) {
+    if (c.keep) {
+      constexpr int kV = 16 / sizeof(T);
+      const int lead_in = (int)(((uintptr_t)src & 15) / sizeof(T)), total = lead_in + n;
+      for (int v = tid; v * kV < total; v += kThreads) {
+        const uint4 q = reinterpret_cast<const uint4*>(src - lead_in)[v];
+        const T* e = reinterpret_cast<const T*>(&q);
+        const int i0 = v * kV - lead_in;
+        if (i0 >= 0 && i0 + kV <= n) {
+#pragma unroll
+          for (int u = 0; u < kV; ++u) f(i0 + u, up(e[u]));
+        } else {
+          for (int i = max(i0, 0); i < min(i0 + kV, n); ++i) f(i, up(src[i]));
+        }
+      }
+    } else {
+      for (int i = tid; i < n; i += kThreads) f(i, up(row[i]));
+    }
+  };
+  float mx = -INFINITY;
+  for_each([&](int, float x) { mx = fmaxf(mx, x); });
+  const float own_max = mx;
 #pragma unroll
   for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
   if (lane == 0) sh.f[warp] = mx;
   if (tid == 0) sh.listed = 0, sh.kmin = 0xFFFFFFFFu, sh.kmax = 0;
   __syncthreads();
-  if (warp == 0) {
-    mx = lane < kWarps ? sh.f[lane] : -INFINITY;
+  auto warp_max = [&](float v) -> float {
 #pragma unroll
-    for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-    if (lane == 0) sh.f[kWarps] = mx;
+    for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+  };
+  auto warp_sum = [&](float v) -> float {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+  };
+  if (warp == 0) {
+    mx = warp_max(lane < kWarps ? sh.f[lane] : -INFINITY);
+    if (lane == 0) sh.mx = lost ? NAN : mx;
   }
   cl.sync();
-  float m = -INFINITY;
-  for (int b = 0; b < C; ++b) m = fmaxf(m, cl.map_shared_rank(&sh, b)->f[kWarps]);
+  const float theirs = lane < C ? cl.map_shared_rank(&sh, lane)->mx : -INFINITY;
+  float m = __any_sync(0xffffffffu, theirs != theirs) ? -INFINITY : warp_max(theirs);
 
   const float temp = c.temperature ? c.temperature[r] : 1.f;
   const bool greedy = !(temp > 0.f);
@@ -147,28 +194,27 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   const int top_k = c.top_k && !greedy ? c.top_k[r] : 0;
   const float top_p = c.top_p && !greedy ? c.top_p[r] : 1.f;
   const float min_p = c.min_p && !greedy ? fminf(fmaxf(c.min_p[r], 0.f), 1.f) : 0.f;
-  uint32_t kc = kKeyNone;  // kept: larger keys, and this one up to index ic
+  const float inv = kBinsPerUnit / t;
+  float xc = -INFINITY;  // kept: larger entries, and equal ones up to index ic
   int ic = -1;
-  auto kept = [&](uint32_t k, int i) { return k > kc || (k == kc && i <= ic); };
+  auto kept = [&](float x, int i) { return x > xc || (x == xc && i <= ic); };
 
-  // a sum over the cluster, the same in every thread and whatever the order of execution (doubles only where one thread
-  // adds: there are few units for them)
+  // a sum and a maximum over the cluster, the same in every thread and whatever the order of execution
   int flip = 0;
-  auto cluster_sum = [&](float v) -> double {
-#pragma unroll
-    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    if (lane == 0) sh.d[flip][warp] = v;
+  auto cluster_sum = [&](float v, float& top) -> float {
+    v = warp_sum(v), top = warp_max(top);
     __syncthreads();
-    if (tid == 0) {
-      double s = 0;
-      for (int w = 0; w < kWarps; ++w) s += (double)sh.d[flip][w];
-      sh.pub[flip] = s;
+    if (lane == 0) sh.d[warp] = v, sh.f[warp] = top;
+    __syncthreads();
+    if (warp == 0) {
+      v = warp_sum(lane < kWarps ? sh.d[lane] : 0.f), top = warp_max(lane < kWarps ? sh.f[lane] : -INFINITY);
+      if (lane == 0) sh.pub[flip] = v, sh.top[flip] = top;
     }
     cl.sync();
-    double s = 0;
-    for (int b = 0; b < C; ++b) s += cl.map_shared_rank(&sh, b)->pub[flip];
+    const Shared* o = cl.map_shared_rank(&sh, lane < C ? lane : 0);
+    v = warp_sum(lane < C ? o->pub[flip] : 0.f), top = warp_max(o->top[flip]);
     flip ^= 1;
-    return s;
+    return v;
   };
   // exclusive prefix over the block's threads, and the sum
   auto block_scan = [&](float v, float& all) -> float {
@@ -179,40 +225,52 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       if (lane >= d) x += o;
     }
     __syncthreads();
-    if (lane == 31) sh.d[0][warp] = x;
+    if (lane == 31) sh.d[warp] = x;
     __syncthreads();
     float before = 0;
     all = 0;
     for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) before += sh.d[0][w];
-      all += sh.d[0][w];
+      if (w < warp) before += sh.d[w];
+      all += sh.d[w];
     }
     return before + x - v;
   };
-  // counts (or masses, in units of 2^-qbits) of the kept entries by bin; the leading block finds the first bin down to
+  // counts (or masses, in units of 2^-qbits) of the kept entries by bin, or counts of the threads' maxima; the leading block finds the first bin down to
   // which they reach `want` (mass: want * their total); then lead->bin, above, goal, and for counts count.  Counts are whole
   // numbers below 2^24: exact in fp32.
-  auto find_bin = [&](bool mass, float want) {
+  enum { kCounts, kMasses, kMaxima };
+  auto find_bin = [&](int what, float want) {
+    const bool mass = what == kMasses;
     for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
     __syncthreads();
     const float unit = (float)(1 << c.qbits);
-    for (int i = tid; i < n; i += kThreads) {
-      const float x = up(src[i]);
-      if (!kept(order_key(x), base + i)) continue;
-      const float z = z_of(x, m, t);
-      const int b = bin_of(z);
-      atomicAdd(hist + b, mass ? (uint32_t)(__expf(z + (float)b * (1.f / kBinsPerUnit)) * unit + 0.5f) : 1u);
+    if (what == kMaxima) {
+      if (own_max > -INFINITY) atomicAdd(hist + bin_of(own_max == m ? 0.f : own_max - m, inv), 1u);
+    } else {
+      for_each([&](int i, float x) {
+        if (!kept(x, base + i)) return;
+        const float d = x == m ? 0.f : x - m;
+        const int b = bin_of(d, inv);
+        // (w of the bin's upper end is e^(-bin / 64): what is left is below 1)
+        atomicAdd(hist + b, mass ? (uint32_t)((d == 0.f ? 1.f : __expf((d * inv + (float)b) * (1.f / kBinsPerUnit))) * unit + 0.5f) : 1u);
+      });
     }
     cl.sync();
     if (rank == 0) {
       constexpr int kPer = kBins / kThreads;
       float v[kPer], sum = 0, total;
+      static_assert(kPer == 4, "a vector of bins a thread");
+      uint4 h[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        h[q] = q < C ? reinterpret_cast<const uint4*>(cl.map_shared_rank(hist, q))[tid] : make_uint4(0, 0, 0, 0);
+      unsigned long long s[kPer] = {0, 0, 0, 0};
+#pragma unroll
+      for (int q = 0; q < 8; ++q) s[0] += h[q].x, s[1] += h[q].y, s[2] += h[q].z, s[3] += h[q].w;
 #pragma unroll
       for (int u = 0; u < kPer; ++u) {
         const int b = tid * kPer + u;
-        unsigned long long s = 0;
-        for (int q = 0; q < C; ++q) s += cl.map_shared_rank(hist, q)[b];
-        v[u] = mass ? (float)s * expf(-(float)b * (1.f / kBinsPerUnit)) : (float)s;
+        v[u] = mass ? (float)s[u] * expf(-(float)b * (1.f / kBinsPerUnit)) : (float)s[u];
         sum += v[u];
       }
       if (tid == 0) sh.bin = -1;
@@ -229,27 +287,20 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   };
   // the kept entries of bins lo .. hi onto the leading block's list (as many as there is room for; all are counted)
   auto gather = [&](int lo, int hi) {
-    for (int i0 = 0; i0 < n; i0 += kThreads) {
-      const int i = i0 + tid;
-      uint32_t k = 0;
-      bool in = false;
-      if (i < n) {
-        const float x = up(src[i]);
-        k = order_key(x);
-        if (kept(k, base + i)) {
-          const int b = bin_of(z_of(x, m, t));
-          in = b >= lo && b <= hi;
-        }
-      }
-      const unsigned who = __ballot_sync(0xffffffffu, in);
-      if (!who) continue;
+    for_each([&](int i, float x) {
+      const int b = bin_of(x == m ? 0.f : x - m, inv);
+      if (b < lo || b > hi || !kept(x, base + i)) return;
+      const uint32_t k = order_key(x);
+      // few come here: those of a warp that do take their places together
+      const unsigned who = __activemask();
+      const int first = __ffs(who) - 1;
       unsigned at = 0;
-      if (lane == 0) at = atomicAdd(&lead->listed, (unsigned)__popc(who));
-      at = __shfl_sync(0xffffffffu, at, 0) + __popc(who & ((1u << lane) - 1));
-      if (in && at < kList) lead_list[at] = (unsigned long long)k << 32 | (0xFFFFFFFFu - (unsigned)(base + i));
-      const unsigned kmin = __reduce_min_sync(0xffffffffu, in ? k : 0xFFFFFFFFu), kmax = __reduce_max_sync(0xffffffffu, in ? k : 0u);
-      if (lane == 0) atomicMin(&lead->kmin, kmin), atomicMax(&lead->kmax, kmax);
-    }
+      if (lane == first) at = atomicAdd(&lead->listed, (unsigned)__popc(who));
+      at = __shfl_sync(who, at, first) + __popc(who & ((1u << lane) - 1));
+      if (at < kList) lead_list[at] = (unsigned long long)k << 32 | (0xFFFFFFFFu - (unsigned)(base + i));
+      const unsigned kmin = __reduce_min_sync(who, k), kmax = __reduce_max_sync(who, k);
+      if (lane == first) atomicMin(&lead->kmin, kmin), atomicMax(&lead->kmax, kmax);
+    });
     cl.sync();
   };
   // the leading block's list sorted: keys falling, indices rising
@@ -268,17 +319,20 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       }
     __syncthreads();
   };
-  auto block_best = [&](Best b) -> Best {
+  auto warp_best = [&](Best b) -> Best {
 #pragma unroll
     for (int d = 16; d; d >>= 1)
       b.take(__shfl_xor_sync(0xffffffffu, b.v, d), __shfl_xor_sync(0xffffffffu, b.z, d), __shfl_xor_sync(0xffffffffu, b.i, d));
-    __syncthreads();
-    if (lane == 0) sh.best[warp] = b;
-    __syncthreads();
-    for (int w = 0; w < kWarps; ++w) b.take(sh.best[w].v, sh.best[w].z, sh.best[w].i);
     return b;
   };
   const Best none = {-INFINITY, 0.f, 0x7FFFFFFF};
+  auto block_best = [&](Best b) -> Best {  // (in warp 0)
+    b = warp_best(b);
+    __syncthreads();
+    if (lane == 0) sh.best[warp] = b;
+    __syncthreads();
+    return warp == 0 ? warp_best(lane < kWarps ? sh.best[lane] : none) : none;
+  };
   auto answer = [&](const Best& b, float sum) {
     c.token[r] = b.i;
     if (c.logprob) c.logprob[r] = b.z - logf(sum);
@@ -292,11 +346,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       for (int i = tid; i < n; i += kThreads) {
         const float x = up(src[i]);
         const uint32_t k = order_key(x);
-        if (k < from || !kept(k, base + i)) continue;
+        if (k < from || !kept(x, base + i)) continue;
         if (mass) part += expf(z_of(x, m, t));
         else ++cnt;
       }
-      return cluster_sum(mass ? part : (float)cnt);
+      float unused = 0.f;
+      return cluster_sum(mass ? part : (float)cnt, unused);
     };
     while (lo < hi) {
       const uint32_t mid = lo + (hi - lo + 1) / 2;
@@ -310,8 +365,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     const int seg = ((n + kWarps - 1) / kWarps + 31) & ~31, s0 = min(n, warp * seg), s1 = min(n, s0 + seg);
     int mine = 0;
     for (int i = s0 + lane; i < s1; i += 32) {
-      const uint32_t k = order_key(up(src[i]));
-      mine += k == lo && kept(k, base + i);
+      const float x = up(src[i]);
+      mine += order_key(x) == lo && kept(x, base + i);
     }
     mine = __reduce_add_sync(0xffffffffu, mine);
     __syncthreads();
@@ -335,11 +390,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     if (mine && before < nth && nth <= before + mine) {
       for (int i0 = s0; i0 < s1; i0 += 32) {
         const int i = i0 + lane;
-        uint32_t k = 0;
         bool in = false;
         if (i < s1) {
-          k = order_key(up(src[i]));
-          in = k == lo && kept(k, base + i);
+          const float x = up(src[i]);
+          in = order_key(x) == lo && kept(x, base + i);
         }
         const unsigned who = __ballot_sync(0xffffffffu, in);
         if (nth <= before + __popc(who)) {
@@ -354,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       }
     }
     cl.sync();
-    kc = lo;
+    xc = key_value(lo);
     ic = lead->index;
     cl.sync();
   };
@@ -367,15 +421,31 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     cl.sync();
     return;
   }
+  if constexpr (kCut) {
   if (!greedy && top_k > 0 && top_k < c.vocab) {
     // ---- 2. top-k
-    find_bin(false, (float)top_k);
-    const int bin = lead->bin, count = lead->count, above = bin < 0 ? 0 : (int)lead->above;
+    // The bin down to which top_k of the threads' maxima reach holds top_k entries at least; if the list has no room for all
+    // down to it, the bin that top_k entries reach.
+    bool few = false;
+    if (top_k <= kThreads * C / 2) {
+      find_bin(kMaxima, (float)top_k);
+      if (lead->bin >= 0) {
+        gather(0, lead->bin);
+        few = lead->listed <= kList;
+        cl.sync();
+        if (!few && rank == 0 && tid == 0) sh.listed = 0, sh.kmin = 0xFFFFFFFFu, sh.kmax = 0;
+      }
+    }
+    if (!few) find_bin(kCounts, (float)top_k);
+    const int bin = lead->bin, above = bin < 0 ? 0 : (int)lead->above;
     if (bin >= 0) {
-      const bool few = count <= kList;
-      gather(few ? 0 : bin, bin);
+      if (!few) {
+        few = lead->count <= kList;
+        gather(few ? 0 : bin, bin);
+      }
       if (few) {
         if (rank == 0) {
+          const int count = (int)sh.listed;
           sort_list(count);
           constexpr int kPer = kList / kThreads;
           const int len = min(top_k, count), per = (len + kThreads - 1) / kThreads;
@@ -419,7 +489,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
           }
         }
         cl.sync();
-        kc = lead->key, ic = lead->index;
+        xc = key_value(lead->key), ic = lead->index;
       } else {
         cut_by_key(false, (double)top_k, lead->kmin, lead->kmax);
       }
@@ -430,26 +500,98 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   if (!greedy && top_p < 1.f) {
     // ---- 3. top-p
     if (!(top_p > 0.f)) {  // the first entry alone: the lowest of the largest
-      kc = order_key(m);
+      xc = m;
       ic = -1;
     } else {
-      find_bin(true, top_p);
+      if (tid == 0 && n > 0) {  // most of the noise will be asked for: into the L2 cache meanwhile
+        const uintptr_t a = ((uintptr_t)noise + 15) & ~uintptr_t(15), e = (uintptr_t)(noise + n) & ~uintptr_t(15);
+        if (e > a) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a), "r"((uint32_t)(e - a)) : "memory");
+      }
+      find_bin(kMasses, top_p);
       const int bin = lead->bin;
       if (bin >= 0) {
         gather(bin, bin);
         const unsigned len = lead->listed;
         if (len <= kList) {
           if (rank == 0) {
-            sort_list((int)len);
+            // In units of an entry's w: the list's entries are cut down to those around the border, by histograms of masses over
+            // the range of their keys, then (equal keys) over that of their indices, until a short list is left to sort.
+            const float unit = 1.f / (float)(1 << c.qbits), want = sh.goal * unit;
+            float above = sh.above * unit;
+            uint32_t lo = sh.kmin, hi = sh.kmax;      // keys of the entries around the border
+            uint32_t i_lo = 0, i_hi = (uint32_t)c.vocab - 1;  // and their indices, once the keys are equal
+            int left = (int)len;
+            const float w_top = expf(z_of(key_value(hi), m, t));
+            auto around = [&](unsigned long long e) {
+              const uint32_t k = (uint32_t)(e >> 32), i = 0xFFFFFFFFu - (uint32_t)e;
+              return k >= lo && k <= hi && i >= i_lo && i <= i_hi;
+            };
+            while (left > kShort && (lo < hi || i_lo < i_hi)) {
+              const bool by_key = lo < hi;
+              const uint32_t range = by_key ? hi - lo : i_hi - i_lo;
+              const int shift = max(0, 32 - __clz(range) - 11);  // 2048 bins
+              for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
+              __syncthreads();
+              for (int i = tid; i < (int)len; i += kThreads) {
+                const unsigned long long e = list[i];
+                if (!around(e)) continue;
+                const uint32_t k = (uint32_t)(e >> 32), bin = (by_key ? hi - k : 0xFFFFFFFFu - (uint32_t)e - i_lo) >> shift;
+                // 19 bits of w against the largest of the list (of 2^12 entries), the low bit kept for "not empty"
+                atomicAdd(hist + bin, (uint32_t)(expf(z_of(key_value(k), m, t)) / w_top * 524287.f + 0.5f));
+              }
+              __syncthreads();
+              float v[4], sum = 0, all;
+#pragma unroll
+              for (int u = 0; u < 4; ++u) sum += v[u] = (float)hist[tid * 4 + u] * (w_top / 524287.f);
+              float at = above + block_scan(sum, all);
+              if (tid == 0) sh.here = -1;
+              __syncthreads();
+#pragma unroll
+              for (int u = 0; u < 4; ++u) {
+                if (at < want && at + v[u] >= want) sh.here = tid * 4 + u, sh.above = at;
+                at += v[u];
+              }
+              __syncthreads();
+              const int bin = sh.here;
+              if (bin < 0) break;  // (the sums' last bits: the border is the range's end; sorted below as it is)
+              above = sh.above;
+              if (by_key) {
+                const uint32_t top = hi - ((uint32_t)bin << shift), step = (1u << shift) - 1;
+                hi = top, lo = top - lo > step ? top - step : lo;
+              } else {
+                const uint32_t first = i_lo + ((uint32_t)bin << shift), step = (1u << shift) - 1;
+                i_lo = first, i_hi = i_hi - first > step ? first + step : i_hi;
+              }
+              int cnt = 0;
+              for (int i = tid; i < (int)len; i += kThreads) cnt += around(list[i]);
+              block_scan((float)cnt, all);
+              left = (int)all;
+            }
+            // those around the border to the list's front, sorted
+            unsigned long long mine[kList / kThreads];
+            int cnt = 0;
+#pragma unroll
+            for (int u = 0; u < kList / kThreads; ++u) {
+              const int i = tid + u * kThreads;
+              mine[u] = i < (int)len && around(list[i]) ? list[i] : 0;
+              cnt += mine[u] != 0;
+            }
+            float all;
+            int to = (int)block_scan((float)cnt, all);
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < kList / kThreads; ++u)
+              if (mine[u]) list[to++] = mine[u];
+            left = (int)all;
+            __syncthreads();
+            sort_list(left);
             constexpr int kPer = kList / kThreads;
-            const float unit = 1.f / (float)(1 << c.qbits), above = sh.above * unit, want = sh.goal * unit;
-            const int per = ((int)len + kThreads - 1) / kThreads;
-            float w[kPer];
-            float sum = 0, all;
+            const int per = (left + kThreads - 1) / kThreads;
+            float w[kPer], sum = 0;
 #pragma unroll
             for (int u = 0; u < kPer; ++u) {
               const int i = tid * per + u;
-              w[u] = u < per && i < (int)len ? expf(z_of(key_value((uint32_t)(list[i] >> 32)), m, t)) : 0.f;
+              w[u] = u < per && i < left ? expf(z_of(key_value((uint32_t)(list[i] >> 32)), m, t)) : 0.f;
               sum += w[u];
             }
             float at = above + block_scan(sum, all);
@@ -459,7 +601,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
 #pragma unroll
             for (int u = 0; u < kPer; ++u) {
               const int i = tid * per + u;
-              if (u < per && i < (int)len && at < want) lastk = i;
+              if (u < per && i < left && at < want) lastk = i;
               at += w[u];
             }
             if (lastk >= 0) atomicMax(&sh.here, lastk);
@@ -470,49 +612,76 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
             }
           }
           cl.sync();
-          kc = lead->key, ic = lead->index;
+          xc = key_value(lead->key), ic = lead->index;
         } else {
           // the bin's share of the mass, with sums in floating point throughout
           float part = 0.f;
           for (int i = tid; i < n; i += kThreads) {
             const float x = up(src[i]);
-            if (kept(order_key(x), base + i)) part += expf(z_of(x, m, t));
+            if (kept(x, base + i)) part += expf(z_of(x, m, t));
           }
-          const double total = cluster_sum(part);
+          float unused = 0.f;
+          const double total = cluster_sum(part, unused);
           cut_by_key(true, (double)top_p * total, lead->kmin, lead->kmax);
         }
       }
     }
   }
+  }
   // ---- 5. what is kept
   const bool first_only = greedy || top_p <= 0.f;
   Best b = none;
-  float part = 0.f;
+  float sum = 1.f;
   if (first_only) {
-    for (int i = tid; i < n; i += kThreads)
-      if (up(src[i]) == m) b.take(0.f, 0.f, base + i);
-    part = 0.f;
+    for_each([&](int i, float x) {
+      if (x == m) b.take(0.f, 0.f, base + i);
+    });
   } else {
+    const float inv_t = 1.f / t, inv_e = inv_t * 1.4426950408889634f;
+    // (d, z as a product, whether the entry is in): w >= min_p is decided on the exact w where the product's comes near
+    auto in_with = [&](float x, int i, float& d, float& near, float& w) -> bool {
+      d = x == m ? 0.f : x - m;
+      near = d == 0.f ? 0.f : d * inv_t;
+      w = d == 0.f ? 1.f : exp2f(d * inv_e);
+      bool in = kept(x, i) && w >= min_p;
+      if (min_p > 0.f && fabsf(w - min_p) <= 1e-4f * min_p) in = kept(x, i) && expf(z_of(x, m, t)) >= min_p;
+      return in;
+    };
+    float part = 0.f, top = -INFINITY, slack = 0.f;  // slack: the largest margin of this thread's keys
 #pragma unroll 4
     for (int i = tid; i < n; i += kThreads) {
-      const float x = up(src[i]);
-      if (!kept(order_key(x), base + i)) continue;
-      const float z = z_of(x, m, t), w = expf(z);
-      if (!(w >= min_p)) continue;
-      const float g = noise[i];
+      float d, near, w;
+      if (!in_with(up(src[i]), base + i, d, near, w)) continue;
+      const float g = gsrc[i];
       part += w;
-      b.take(g == g ? z + g : -INFINITY, z, base + i);
+      top = fmaxf(top, near + g);
+      slack = fmaxf(slack, 4e-6f * (fabsf(near) + fabsf(g)));
+    }
+    const float own_top = top;
+    sum = cluster_sum(part, top);  // top: the largest of the row, up to the products' rounding
+    // a key's two forms differ by less than 1e-6 (|z| + |noise|)
+    const float floor = top - 4e-6f * fabsf(top);
+    // (a thread whose largest key is far below has none near)
+    if (own_top >= top || own_top + slack >= floor || slack != slack)
+    for (int i = tid; i < n; i += kThreads) {
+      const float x = up(src[i]);
+      if (!kept(x, base + i)) continue;
+      float d, near, w;
+      d = x == m ? 0.f : x - m;
+      near = d == 0.f ? 0.f : d * inv_t;
+      const float g = fmaxf(gsrc[i], -INFINITY), key = near + g;
+      if (!(key >= top || key + 4e-6f * (fabsf(near) + fabsf(g)) >= floor)) continue;
+      if (!in_with(x, base + i, d, near, w)) continue;
+      const float z = z_of(x, m, t);
+      b.take(z + g, z, base + i);
     }
   }
   b = block_best(b);
   if (tid == 0) sh.best[kWarps] = b;
-  const double sum = cluster_sum(part);
-  if (rank == 0 && tid == 0) {
-    for (int q = 1; q < C; ++q) {
-      const Best o = cl.map_shared_rank(&sh, q)->best[kWarps];
-      b.take(o.v, o.z, o.i);
-    }
-    answer(b, first_only ? 1.f : (float)sum);
+  cl.sync();
+  if (rank == 0 && warp == 0) {
+    b = warp_best(lane < C ? cl.map_shared_rank(&sh, lane)->best[kWarps] : none);
+    if (lane == 0) answer(b, sum);
   }
   cl.sync();  // no block leaves while another reads its shared memory
 }
@@ -523,17 +692,20 @@ int ceil_log2(int v) {
   return l;
 }
 
-template <class T>
+template <class T, bool kCut>
 cudaError_t run(SampleCall c, int rows, cudaStream_t s) {
   // Blocks of a row: as many as leave each some ten thousand entries while they find room on the GPU at once (few rows),
-  // at least so many that the slices stay in shared memory.
+  // at least so many that the slices stay in shared memory.  Where nothing is cut, the noise of every entry is needed: it is
+  // loaded with the logits, in slices of at most 76 KiB together: three blocks an SM.
+  const size_t entry = sizeof(T) + (kCut ? 0 : 4), most = kCut ? 64 * 1024 : 76 * 1024;
   int C = 1;
-  while (C < 8 && ((size_t)((c.vocab + C - 1) / C) * sizeof(T) > 64 * 1024 || ((int64_t)rows * C < 152 && c.vocab / C > 8192))) C *= 2;
+  while (C < 8 && ((size_t)((c.vocab + C - 1) / C) * entry > most || ((int64_t)rows * C < 152 && c.vocab / C > 8192))) C *= 2;
   c.slice = (c.vocab + C - 1) / C;
   c.qbits = 31 - ceil_log2(c.slice > 32768 ? c.slice : 32768);
-  const size_t keep = (size_t)c.slice * sizeof(T);
-  const size_t smem = kBins * 4 + kList * 8 + (keep <= kResident ? keep + 32 : 0);
-  cudaError_t e = cudaFuncSetAttribute(k_sample<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kBins * 4 + kList * 8 + kResident + 32));
+  c.keep = (size_t)c.slice * entry > kResident ? 0 : kCut ? 1 : 2;
+  const size_t smem = (c.keep == 2 ? 0 : kBins * 4 + kList * 8) + (c.keep ? (size_t)c.slice * entry + 64 : 0);
+  const cudaError_t e = cudaFuncSetAttribute(k_sample<T, kCut>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)(kBins * 4 + kList * 8 + kResident + 64));
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)rows * (unsigned)C);
@@ -545,7 +717,7 @@ cudaError_t run(SampleCall c, int rows, cudaStream_t s) {
   attr[0].val.clusterDim = {(unsigned)C, 1, 1};
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_sample<T>, c);
+  return cudaLaunchKernelEx(&cfg, k_sample<T, kCut>, c);
 }
 
 }  // namespace
@@ -564,10 +736,12 @@ extern "C" int mf_sample(const mf_sample_args_t* a, void* stream) {
   if (a->n_rows > 1 && (a->logits_stride < a->vocab || a->noise_stride < a->vocab)) return MF_E_INVAL;
   if (a->n_rows > (1 << 27)) return MF_E_INVAL;
   SampleCall c = {a->logits, a->noise, a->temperature, a->top_p, a->min_p, a->top_k, a->token, a->logprob,
-                  a->logits_stride, a->noise_stride, a->vocab, 0, 0};
+                  a->logits_stride, a->noise_stride, a->vocab, 0, 0, 0};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = a->dtype == MF_F32   ? run<float>(c, a->n_rows, s)
-                        : a->dtype == MF_F16 ? run<__half>(c, a->n_rows, s)
-                                             : run<__nv_bfloat16>(c, a->n_rows, s);
+  const bool cut = a->top_k || a->top_p;
+  const int n = a->n_rows;
+  const cudaError_t e = a->dtype == MF_F32   ? (cut ? run<float, true>(c, n, s) : run<float, false>(c, n, s))
+                        : a->dtype == MF_F16 ? (cut ? run<__half, true>(c, n, s) : run<__half, false>(c, n, s))
+                                             : (cut ? run<__nv_bfloat16, true>(c, n, s) : run<__nv_bfloat16, false>(c, n, s));
   return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_sample");
 }
