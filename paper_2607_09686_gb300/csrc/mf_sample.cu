@@ -61,6 +61,12 @@ __device__ __forceinline__ int bin_of(float d, float inv) {
   return d == 0.f ? 0 : (int)fminf(-d * inv, (float)(kBins - 1));  // (inv may be infinite)
 }
 
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 struct Best {  // the largest z + noise so far, the lowest index where equal
   float v, z;
   int i;
@@ -80,6 +86,7 @@ struct Shared {
   float above, goal;
   int bin, count;             // border bin (-1: nothing is cut), entries down to it
   unsigned listed, kmin, kmax;  // entries put on the list, and their keys' range
+  unsigned mine;                // of this block
   uint32_t key;
   int index;
   int here;
@@ -285,22 +292,31 @@ __global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c)
     }
     cl.sync();
   };
-  // the kept entries of bins lo .. hi onto the leading block's list (as many as there is room for; all are counted)
+  // the kept entries of bins lo .. hi onto the leading block's list (as many as there is room for; all are counted): each
+  // block collects its own first, so that only whole runs and one counter cross to the leading block
   auto gather = [&](int lo, int hi) {
+    unsigned kmin = 0xFFFFFFFFu, kmax = 0;
+    if (tid == 0) sh.mine = 0;
+    __syncthreads();
     for_each([&](int i, float x) {
       const int b = bin_of(x == m ? 0.f : x - m, inv);
       if (b < lo || b > hi || !kept(x, base + i)) return;
       const uint32_t k = order_key(x);
-      // few come here: those of a warp that do take their places together
-      const unsigned who = __activemask();
-      const int first = __ffs(who) - 1;
-      unsigned at = 0;
-      if (lane == first) at = atomicAdd(&lead->listed, (unsigned)__popc(who));
-      at = __shfl_sync(who, at, first) + __popc(who & ((1u << lane) - 1));
-      if (at < kList) lead_list[at] = (unsigned long long)k << 32 | (0xFFFFFFFFu - (unsigned)(base + i));
-      const unsigned kmin = __reduce_min_sync(who, k), kmax = __reduce_max_sync(who, k);
-      if (lane == first) atomicMin(&lead->kmin, kmin), atomicMax(&lead->kmax, kmax);
+      const unsigned at = atomicAdd(&sh.mine, 1u);
+      if (at < kList) list[at] = (unsigned long long)k << 32 | (0xFFFFFFFFu - (unsigned)(base + i));
+      kmin = min(kmin, k), kmax = max(kmax, k);
     });
+    kmin = __reduce_min_sync(0xffffffffu, kmin), kmax = __reduce_max_sync(0xffffffffu, kmax);
+    if (lane == 0 && kmax) atomicMin(&lead->kmin, kmin), atomicMax(&lead->kmax, kmax);
+    __syncthreads();
+    const unsigned own = sh.mine;
+    cl.sync();
+    // every block's place follows from the others' numbers: the same whatever the order of execution
+    const unsigned num = lane < C ? cl.map_shared_rank(&sh, lane)->mine : 0u;
+    const unsigned before = __reduce_add_sync(0xffffffffu, lane < rank ? num : 0u), total = __reduce_add_sync(0xffffffffu, num);
+    if (rank != 0)
+      for (unsigned i = tid; i < own && before + i < kList; i += kThreads) lead_list[before + i] = list[i];
+    if (rank == 0 && tid == 0) sh.listed = total;
     cl.sync();
   };
   // the leading block's list sorted: keys falling, indices rising
@@ -642,27 +658,37 @@ __global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c)
     auto in_with = [&](float x, int i, float& d, float& near, float& w) -> bool {
       d = x == m ? 0.f : x - m;
       near = d == 0.f ? 0.f : d * inv_t;
-      w = d == 0.f ? 1.f : exp2f(d * inv_e);
+      w = d == 0.f ? 1.f : ex2(d * inv_e);
       bool in = kept(x, i) && w >= min_p;
       if (min_p > 0.f && fabsf(w - min_p) <= 1e-4f * min_p) in = kept(x, i) && expf(z_of(x, m, t)) >= min_p;
       return in;
     };
-    float part = 0.f, top = -INFINITY, slack = 0.f;  // slack: the largest margin of this thread's keys
-#pragma unroll 4
-    for (int i = tid; i < n; i += kThreads) {
-      float d, near, w;
-      if (!in_with(up(src[i]), base + i, d, near, w)) continue;
-      const float g = gsrc[i];
+    // sum of w; the largest key; the largest with its margin, that of the exact key: the two forms of a key differ by less
+    // than 1e-6 (|z| + |noise|), and 4e-6 is allowed for
+    float part = 0.f, top = -INFINITY, reach = -INFINITY;
+    auto add = [&](float near, float w, float g) {
+      const float key = near + g;
       part += w;
-      top = fmaxf(top, near + g);
-      slack = fmaxf(slack, 4e-6f * (fabsf(near) + fabsf(g)));
+      top = fmaxf(top, key);
+      reach = fmaxf(reach, fmaf(4e-6f, fabsf(near) + fabsf(g), key));
+    };
+    if (min_p > 0.f || m == INFINITY) {
+      for (int i = tid; i < n; i += kThreads) {
+        float d, near, w;
+        if (in_with(up(src[i]), base + i, d, near, w)) add(near, w, gsrc[i]);
+      }
+    } else {
+#pragma unroll 8
+      for (int i = tid; i < n; i += kThreads) {
+        const float x = up(src[i]), d = x - m;
+        if (!kCut || kept(x, base + i)) add(d * inv_t, ex2(d * inv_e), gsrc[i]);  // (-inf: nothing to the sum, no key)
+      }
     }
-    const float own_top = top;
-    sum = cluster_sum(part, top);  // top: the largest of the row, up to the products' rounding
-    // a key's two forms differ by less than 1e-6 (|z| + |noise|)
+    const float own_reach = reach;
+    sum = cluster_sum(part, top);
     const float floor = top - 4e-6f * fabsf(top);
-    // (a thread whose largest key is far below has none near)
-    if (own_top >= top || own_top + slack >= floor || slack != slack)
+    // the entries near the largest, in threads that have one (a reach or floor that is no number: in any)
+    if (!(own_reach < floor))
     for (int i = tid; i < n; i += kThreads) {
       const float x = up(src[i]);
       if (!kept(x, base + i)) continue;
@@ -670,7 +696,7 @@ __global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c)
       d = x == m ? 0.f : x - m;
       near = d == 0.f ? 0.f : d * inv_t;
       const float g = fmaxf(gsrc[i], -INFINITY), key = near + g;
-      if (!(key >= top || key + 4e-6f * (fabsf(near) + fabsf(g)) >= floor)) continue;
+      if (!(key >= top || !(key + 4e-6f * (fabsf(near) + fabsf(g)) < floor))) continue;
       if (!in_with(x, base + i, d, near, w)) continue;
       const float z = z_of(x, m, t);
       b.take(z + g, z, base + i);
