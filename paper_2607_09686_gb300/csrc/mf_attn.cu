@@ -205,8 +205,8 @@ extern "C" int mf_attn_create(mf_attn_t** out, const mf_attn_shape_t* shape, int
   cudaError_t e = cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, device);
   // parts of either path (a step takes one): rows of a part times parts
   const int G = shape->n_heads / shape->n_kv_heads, tile = attn_tile_rows(shape->head_dim);
-  const size_t few = (size_t)attn_few_blocks(h->sms) * 2 * kFewRows;
-  const size_t many = (int64_t)max_tokens * G > kFewRows ? (size_t)h->sms * 2 * tile : 0;
+  const size_t few = (size_t)attn_few_blocks(h->sms) * 2 * attn_few_rows(shape->head_dim);
+  const size_t many = (int64_t)max_tokens * G > attn_few_rows(shape->head_dim) ? (size_t)h->sms * 2 * tile : 0;
   const size_t rows = few > many ? few : many, tiles = (size_t)((int64_t)max_tokens * G / tile) + max_seqs;
   Carve w;
   const size_t o_err = w.take(256), o_o = w.take(rows * shape->head_dim * 4), o_ml = w.take(rows * 8),
@@ -286,7 +286,7 @@ extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, cons
   const bool bf16 = attn->shape.dtype == MF_BF16;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
-  if ((int64_t)c.st.max_q * c.st.G <= kFewRows) {
+  if ((int64_t)c.st.max_q * c.st.G <= attn_few_rows(D)) {
     e = launch_attn_few(c, attn->parts, D, bf16, attn->sms, s);
   } else {
     AttnMaps maps;

@@ -123,13 +123,13 @@ struct AttnRec {
 // What blocks leave of work that they do not have whole.  Block b's last piece, where it starts the work, is part
 // 2b + 1 and rec[b] describes it; the pieces that go on with it are parts 2(b + 1), 2(b + 2), ...
 struct AttnParts {
-  float* o;     // [parts][rows][head_dim] (16 rows) or [parts][head_dim / 4][rows][4] (tiles), not yet divided by l
+  float* o;     // [parts][rows][head_dim] (few rows) or [parts][head_dim / 4][rows][4] (tiles), not yet divided by l
   float2* ml;   // [parts][rows]  running maximum (log2 domain) and sum
   AttnRec* rec;  // [blocks]
 };
-constexpr int kFewRows = 16;    // rows (token, head of the group) of a part of launch_attn_few
 constexpr int kMaxParts = 1024; // pieces of one record
 int attn_few_blocks(int sms);
+int attn_few_rows(int head_dim);   // the most rows (token, head of the group) that launch_attn_few takes: rows of a part
 int attn_tile_rows(int head_dim);  // rows of a part of launch_attn_many (one block per SM)
 
 // What k_attn_plan finds of a step for launch_attn_many: the row tiles of the sequences and the jobs before each.
@@ -146,8 +146,8 @@ cudaError_t launch_attn_few(const AttnCall& c, const AttnParts& parts, int head_
 void attn_maps(AttnCall& c, int head_dim, AttnMaps* maps);
 cudaError_t launch_attn_many(const AttnCall& c, const AttnMaps& maps, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
                              cudaStream_t s);
-// the records of `blocks` blocks joined; rows: rows of a part
-cudaError_t launch_attn_join(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int rows, int blocks,
+// the records of `blocks` blocks joined; rows: rows of a part; tiles: left by launch_attn_many
+cudaError_t launch_attn_join(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int rows, bool tiles, int blocks,
                              cudaStream_t s);
 
 }  // namespace mf

@@ -92,28 +92,28 @@ __global__ void __launch_bounds__(Join<D>::kThreads) k_attn_join(AttnCall c, Att
 }
 
 template <class T, int D>
-cudaError_t run(const AttnCall& c, const AttnParts& parts, int rows, int blocks, cudaStream_t s) {
+cudaError_t run(const AttnCall& c, const AttnParts& parts, int rows, bool tiles, int blocks, cudaStream_t s) {
   using J = Join<D>;
   // up to 64 rows there may be many pieces of each; with more, a record has few pieces
   const int64_t most = (int64_t)c.st.max_q * c.st.G;
   const int held = (int)(most < rows ? most : rows);
   const dim3 one(blocks, held), each(blocks, (held + J::kGroups - 1) / J::kGroups), threads(J::kThreads);
-  if (rows == kFewRows) return launch_pdl(true, k_attn_join<T, D, true, false>, one, threads, 0, s, c, parts, rows);
+  if (!tiles) return launch_pdl(true, k_attn_join<T, D, true, false>, one, threads, 0, s, c, parts, rows);
   if (held <= 64) return launch_pdl(true, k_attn_join<T, D, true, true>, one, threads, 0, s, c, parts, rows);
   return launch_pdl(true, k_attn_join<T, D, false, true>, each, threads, 0, s, c, parts, rows);
 }
 
 }  // namespace
 
-cudaError_t launch_attn_join(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int rows, int blocks,
+cudaError_t launch_attn_join(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int rows, bool tiles, int blocks,
                              cudaStream_t s) {
   if (bf16)
-    return head_dim == 64    ? run<__nv_bfloat16, 64>(c, parts, rows, blocks, s)
-           : head_dim == 128 ? run<__nv_bfloat16, 128>(c, parts, rows, blocks, s)
-                             : run<__nv_bfloat16, 256>(c, parts, rows, blocks, s);
-  return head_dim == 64    ? run<__half, 64>(c, parts, rows, blocks, s)
-         : head_dim == 128 ? run<__half, 128>(c, parts, rows, blocks, s)
-                           : run<__half, 256>(c, parts, rows, blocks, s);
+    return head_dim == 64    ? run<__nv_bfloat16, 64>(c, parts, rows, tiles, blocks, s)
+           : head_dim == 128 ? run<__nv_bfloat16, 128>(c, parts, rows, tiles, blocks, s)
+                             : run<__nv_bfloat16, 256>(c, parts, rows, tiles, blocks, s);
+  return head_dim == 64    ? run<__half, 64>(c, parts, rows, tiles, blocks, s)
+         : head_dim == 128 ? run<__half, 128>(c, parts, rows, tiles, blocks, s)
+                           : run<__half, 256>(c, parts, rows, tiles, blocks, s);
 }
 
 }  // namespace mf
