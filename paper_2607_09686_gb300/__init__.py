@@ -192,10 +192,21 @@ def _addr(buf):
     raise TypeError(f"cannot take the address of {type(buf).__name__}")
 
 
+_raw_stream = None  # torch's current stream of a device as a handle, without making a Stream object
+
+
 def _stream(stream):
+    global _raw_stream
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _raw_stream is None:
+            import torch
+            get, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+            if get is None or device is None:
+                _raw_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+            else:
+                torch.cuda.current_stream()  # (initialises CUDA)
+                _raw_stream = lambda: get(device())  # noqa: E731
+        return _raw_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

@@ -12,10 +12,11 @@ namespace {
 // ---- append: q and k rotated by position, k and v into their lines
 //
 // A pair (a, b) turned by an angle is (a cos - b sin, b cos + a sin).  Every element is read and written once,
-// so the kernel is a copy bounded by memory (few tokens: by its launch).  One block per token: the threads
-// count the sequences that end at or before it, then each takes pairs of 16-byte vectors of a head: the two halves of
-// eight rotated pairs (elements j.. and j + rot / 2.., or 16 neighbours when interleaved), or 16 neighbours
-// of what is only copied.
+// so the kernel is a copy bounded by memory (few tokens: by its launch).  A block has kTB tokens (one where there are few
+// tokens, four else, so that a thread has several loads under way): a warp finds a token's sequence (the ends at or before
+// it are counted) and its line, the threads fetch the angles' cosines and sines once for all heads, then each takes pairs
+// of 16-byte vectors of a head: the two halves of eight rotated pairs (elements j.. and j + rot / 2.., or 16 neighbours when
+// interleaved), or 16 neighbours of what is only copied.
 struct AppendCall {
   AttnStep st;
   const void *q, *k, *v;
@@ -29,84 +30,116 @@ struct AppendCall {
 
 constexpr int kAppendThreads = 256;
 
-template <class T>
-__global__ void __launch_bounds__(kAppendThreads) k_append(AppendCall c, int D) {
+template <class T, int kTB>
+__global__ void __launch_bounds__(kAppendThreads) k_append(const __grid_constant__ AppendCall c, int D) {
   const AttnStep& st = c.st;
-  const int t = blockIdx.x;
-  int s = t;
-  if (st.q_start) {
-    s = 0;
-    for (int base = 0; base < st.n_seqs; base += kAppendThreads) {
-      const int i = base + threadIdx.x;
-      s += __syncthreads_count(i < st.n_seqs && __ldg(st.q_start + i + 1) <= t);
+  __shared__ int64_t s_at[kTB];
+  __shared__ int s_line[kTB];  // the token's line; -1: not stored
+  __shared__ float2 s_cs[kTB][128];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, t0 = blockIdx.x * kTB, tokens = min(kTB, st.n_tokens - t0);
+  pdl_wait();
+  if (warp < tokens) {
+    const int t = t0 + warp;
+    int s = t;
+    if (st.q_start) {
+      s = 0;
+      for (int base = 0; base < st.n_seqs; base += 32) {
+        const int i = base + lane;
+        s += __popc(__ballot_sync(0xffffffffu, i < st.n_seqs && __ldg(st.q_start + i + 1) <= t));
+      }
+    }
+    if (lane == 0) {
+      int line = -1;
+      int64_t at = 0;
+      if (s < st.n_seqs) {
+        const SeqSpan sp = seq_span(st, s);
+        const int x = sp.len - sp.n + t - sp.q0;
+        if (t >= sp.q0 && t < sp.q0 + sp.n && x >= 0) {
+          const int pi = (int)fast_div((uint32_t)x, st.page_mul, st.page_shift);
+          const int page = __ldg(st.pages + (int64_t)s * st.pages_per_seq + pi);
+          if (page >= 0 && page < st.n_pages) {
+            line = x;
+            at = (int64_t)page * st.page_stride + (int64_t)(x - pi * st.page_size) * st.token_stride;
+          }
+        }
+      }
+      if (line < 0) attn_report(st, kAttnRange);
+      s_line[warp] = line;
+      s_at[warp] = at;
     }
   }
-  if (s >= st.n_seqs) {  // no sequence has the token
-    if (threadIdx.x == 0) attn_report(st, kAttnRange);
-    return;
+  __syncthreads();
+  if (c.half) {
+    for (int i = tid; i < tokens * c.half; i += kAppendThreads) {
+      const int k = i / c.half, pair = i - k * c.half;
+      int p = s_line[k];
+      if (c.pos) {
+        const int axis = c.n_axes == 1 ? 0 : (pair >= c.end0) + (pair >= c.end1) + (pair >= c.end2);
+        p = __ldg(c.pos + (int64_t)axis * st.n_tokens + t0 + k);
+      }
+      const int pc = min(max(p, 0), c.n_pos - 1);
+      if (pc != p) attn_report(st, kAttnRange);
+      s_cs[k][pair] = make_float2(__ldg(c.cos + (int64_t)pc * c.half + pair), __ldg(c.sin + (int64_t)pc * c.half + pair));
+    }
+    __syncthreads();
   }
-  const SeqSpan sp = seq_span(st, s);
-  const int line = sp.len - sp.n + t - sp.q0;
-  bool store = t >= sp.q0 && t < sp.q0 + sp.n && line >= 0;
-  int64_t at = 0;
-  if (store) {
-    const int pi = (int)fast_div((uint32_t)line, st.page_mul, st.page_shift);
-    const int page = __ldg(st.pages + (int64_t)s * st.pages_per_seq + pi);
-    store = page >= 0 && page < st.n_pages;
-    at = (int64_t)page * st.page_stride + (int64_t)(line - pi * st.page_size) * st.token_stride;
-  }
-  if (!store && threadIdx.x == 0) attn_report(st, kAttnRange);
 
-  const int per = D / 16, q_heads = c.q ? st.Hq : 0;
-  const int n_items = (q_heads + 2 * st.Hkv) * per;
-  for (int i = threadIdx.x; i < n_items; i += kAppendThreads) {
-    const int head = i / per, j = i % per;
+  const int per = D / 16, q_heads = c.q ? st.Hq : 0, n_items = (q_heads + 2 * st.Hkv) * per;
+  struct Item {
+    T* dst;
+    uint4 a, b;
+    int e0, e1, k, j;  // elements of the two vectors; token, place in the head
+    bool turn, ok;
+  };
+  auto load = [&](int i, Item& it) {
+    it.ok = i < tokens * n_items;
+    if (!it.ok) return;
+    const int k = i / n_items, x = i - k * n_items, head = x / per, j = x - head * per, t = t0 + k;
     const bool is_q = head < q_heads, is_v = head >= q_heads + st.Hkv;
     const int h = is_q ? head : is_v ? head - q_heads - st.Hkv : head - q_heads;
-    if (!is_q && !store) continue;
+    it.ok = is_q || s_line[k] >= 0;
+    if (!it.ok) return;
     const T* src = static_cast<const T*>(is_q ? c.q : is_v ? c.v : c.k) +
                    (int64_t)t * (is_q ? c.q_stride : is_v ? c.v_stride : c.k_stride) + (int64_t)h * D;
-    T* dst = is_q ? static_cast<T*>(c.q_out) + (int64_t)t * c.q_out_stride + (int64_t)h * D
-                  : static_cast<T*>(is_v ? c.vc : c.kc) + at + (int64_t)h * st.head_stride;
-    const bool turn = !is_v && j * 8 < c.half;
-    const int e0 = turn && !c.interleaved ? j * 8 : j * 16, e1 = turn && !c.interleaved ? e0 + c.half : e0 + 8;
-    uint4 a = *reinterpret_cast<const uint4*>(src + e0), b = *reinterpret_cast<const uint4*>(src + e1);
-    if (turn) {
-      float co[8], si[8];
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int pair = j * 8 + u;
-        int p = line;
-        if (c.pos) {
-          const int axis = c.n_axes == 1 ? 0 : (pair >= c.end0) + (pair >= c.end1) + (pair >= c.end2);
-          p = __ldg(c.pos + (int64_t)axis * st.n_tokens + t);
-        }
-        const int pc = min(max(p, 0), c.n_pos - 1);
-        if (pc != p) attn_report(st, kAttnRange);
-        co[u] = __ldg(c.cos + (int64_t)pc * c.half + pair);
-        si[u] = __ldg(c.sin + (int64_t)pc * c.half + pair);
-      }
-      uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
-      if (c.interleaved) {  // words hold (a, b) of pair u
+    it.dst = is_q ? static_cast<T*>(c.q_out) + (int64_t)t * c.q_out_stride + (int64_t)h * D
+                  : static_cast<T*>(is_v ? c.vc : c.kc) + s_at[k] + (int64_t)h * st.head_stride;
+    it.turn = !is_v && j * 8 < c.half;
+    it.e0 = it.turn && !c.interleaved ? j * 8 : j * 16, it.e1 = it.turn && !c.interleaved ? it.e0 + c.half : it.e0 + 8;
+    it.k = k, it.j = j;
+    it.a = *reinterpret_cast<const uint4*>(src + it.e0), it.b = *reinterpret_cast<const uint4*>(src + it.e1);
+  };
+  auto store = [&](Item& it) {
+    if (!it.ok) return;
+    if (it.turn) {
+      uint32_t wa[4] = {it.a.x, it.a.y, it.a.z, it.a.w}, wb[4] = {it.b.x, it.b.y, it.b.z, it.b.w};
+      const float2* cs = &s_cs[it.k][it.j * 8];
+      if (c.interleaved) {  // words hold (a, b) of a pair
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const float2 x = Half2<T>::up(wa[u]), y = Half2<T>::up(wb[u]);
-          wa[u] = Half2<T>::down(x.x * co[u] - x.y * si[u], x.y * co[u] + x.x * si[u]);
-          wb[u] = Half2<T>::down(y.x * co[4 + u] - y.y * si[4 + u], y.y * co[4 + u] + y.x * si[4 + u]);
+          const float2 x = Half2<T>::up(wa[u]), y = Half2<T>::up(wb[u]), p = cs[u], q = cs[4 + u];
+          wa[u] = Half2<T>::down(x.x * p.x - x.y * p.y, x.y * p.x + x.x * p.y);
+          wb[u] = Half2<T>::down(y.x * q.x - y.y * q.y, y.y * q.x + y.x * q.y);
         }
       } else {
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const float2 x = Half2<T>::up(wa[u]), y = Half2<T>::up(wb[u]);
-          wa[u] = Half2<T>::down(x.x * co[2 * u] - y.x * si[2 * u], x.y * co[2 * u + 1] - y.y * si[2 * u + 1]);
-          wb[u] = Half2<T>::down(y.x * co[2 * u] + x.x * si[2 * u], y.y * co[2 * u + 1] + x.y * si[2 * u + 1]);
+          const float2 x = Half2<T>::up(wa[u]), y = Half2<T>::up(wb[u]), p = cs[2 * u], q = cs[2 * u + 1];
+          wa[u] = Half2<T>::down(x.x * p.x - y.x * p.y, x.y * q.x - y.y * q.y);
+          wb[u] = Half2<T>::down(y.x * p.x + x.x * p.y, y.y * q.x + x.y * q.y);
         }
       }
-      a = make_uint4(wa[0], wa[1], wa[2], wa[3]);
-      b = make_uint4(wb[0], wb[1], wb[2], wb[3]);
+      it.a = make_uint4(wa[0], wa[1], wa[2], wa[3]);
+      it.b = make_uint4(wb[0], wb[1], wb[2], wb[3]);
     }
-    *reinterpret_cast<uint4*>(dst + e0) = a;
-    *reinterpret_cast<uint4*>(dst + e1) = b;
+    *reinterpret_cast<uint4*>(it.dst + it.e0) = it.a;
+    *reinterpret_cast<uint4*>(it.dst + it.e1) = it.b;
+  };
+  for (int i = tid; i < tokens * n_items; i += 2 * kAppendThreads) {  // both items' loads before the first store
+    Item x, y;
+    load(i, x);
+    load(i + kAppendThreads, y);
+    store(x);
+    store(y);
   }
 }
 
@@ -260,11 +293,16 @@ extern "C" int mf_kv_append(mf_attn_t* attn, const mf_kv_cache_t* cache, const m
   OnDevice on(attn->device);
   if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  // (single tokens keep latency low; from some eight blocks an SM on there are blocks enough to give each more tokens)
+  const int T = c.st.n_tokens;
+  auto launch = [&](auto kernel, int tb) {
+    return launch_pdl(true, kernel, dim3((unsigned)((T + tb - 1) / tb)), dim3(kAppendThreads), 0, s, c, D);
+  };
+  cudaError_t e;
   if (attn->shape.dtype == MF_BF16)
-    k_append<__nv_bfloat16><<<c.st.n_tokens, kAppendThreads, 0, s>>>(c, D);
+    e = T < 8 * attn->sms ? launch(k_append<__nv_bfloat16, 1>, 1) : launch(k_append<__nv_bfloat16, 4>, 4);
   else
-    k_append<__half><<<c.st.n_tokens, kAppendThreads, 0, s>>>(c, D);
-  const cudaError_t e = cudaGetLastError();
+    e = T < 8 * attn->sms ? launch(k_append<__half, 1>, 1) : launch(k_append<__half, 4>, 4);
   return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_kv_append");
 }
 

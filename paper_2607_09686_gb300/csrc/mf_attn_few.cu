@@ -25,7 +25,7 @@ namespace {
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kUnit = 16;               // lines a warp takes at once
 constexpr int kTile = kWarps * kUnit;   // lines of a tile
-constexpr int kOver = 2;                // tiles that a (sequence, head) costs besides its own
+constexpr int kOver = 3;                // tiles that a (sequence, head) costs besides its own
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 template <int D>
@@ -176,10 +176,10 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
   // ---- the copies' side, kS units ahead
   const uint32_t slots = smem_u32(smem) + warp * (kS * C::kSlot);
   Cursor ld = cur;
-  // Where pages hold whole units (a multiple of 16 lines), lane L knows where unit L of 32 begins, from tile `win` of the
+  // Where pages hold a multiple of 8 lines, lane L knows where the halves of unit L of 32 begin, from tile `win` of the
   // (sequence, head) on, else lane L % 16 where that line of the unit to copy lies.
-  const bool whole_pages = st.page_size % kUnit == 0;
-  int64_t line_at = 0, unit_at = 0;
+  const bool whole_pages = st.page_size % 8 == 0;
+  int64_t line_at = 0, half_at = 0, unit_at[2] = {0, 0};
   int win = 0, lo_at = 0, hi_at = 0;  // lines of the unit from lo_at to hi_at are copied, others become zeros
   bool fresh_win = true;
   auto look_up = [&]() {
@@ -192,7 +192,10 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
         fresh_win = false;
         win = ld.j;
         const int line = line0 + lane * kTile;
-        if (line < len && ld.j + lane < ld.j_end) line_at = line_offset(st, ld.s, line) + (int64_t)ld.h * st.head_stride;
+        if (ld.j + lane < ld.j_end) {
+          if (line < len && line + 8 > lo) line_at = line_offset(st, ld.s, line) + (int64_t)ld.h * st.head_stride;
+          if (line + 8 < len) half_at = line_offset(st, ld.s, line + 8) + (int64_t)ld.h * st.head_stride;
+        }
       }
     } else {
       const int line = line0 + (lane & 15);
@@ -206,22 +209,32 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
     if (ld.live()) {
       const T* base = static_cast<const T*>(cache);
       if (whole_pages) {
-        if (!is_v) unit_at = __shfl_sync(0xffffffffu, line_at, ld.j - win) + lane_off;
-        const T* p = base + unit_at;
+        if (!is_v) {
+          unit_at[0] = __shfl_sync(0xffffffffu, line_at, ld.j - win) + lane_off;
+          unit_at[1] = __shfl_sync(0xffffffffu, half_at, ld.j - win) + lane_off;
+        }
         if (lo_at <= 0 && hi_at >= kUnit) {
 #pragma unroll
-          for (int i = 0; i < kUnit / kRowsPer; ++i) {
-            const int row = i * kRowsPer + sub;
-            cp16(dst + row * C::kRow + ((ch ^ (row & 7)) << 4), p, 16u);
-            p += step;
+          for (int half = 0; half < 2; ++half) {
+            const T* p = base + unit_at[half];
+#pragma unroll
+            for (int i = 0; i < 8 / kRowsPer; ++i) {
+              const int row = half * 8 + i * kRowsPer + sub;
+              cp16(dst + row * C::kRow + ((ch ^ (row & 7)) << 4), p, 16u);
+              p += step;
+            }
           }
         } else {
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const T* p = base + unit_at[half];
 #pragma unroll 1
-          for (int i = 0; i < kUnit / kRowsPer; ++i) {
-            const int row = i * kRowsPer + sub;
-            const bool in = row >= lo_at && row < hi_at;
-            cp16(dst + row * C::kRow + ((ch ^ (row & 7)) << 4), in ? p : base, in ? 16u : 0u);
-            p += step;
+            for (int i = 0; i < 8 / kRowsPer; ++i) {
+              const int row = half * 8 + i * kRowsPer + sub;
+              const bool in = row >= lo_at && row < hi_at;
+              cp16(dst + row * C::kRow + ((ch ^ (row & 7)) << 4), in ? p : base, in ? 16u : 0u);
+              p += step;
+            }
           }
         }
       } else {
@@ -457,7 +470,7 @@ cudaError_t run(const AttnCall& c, const AttnParts& parts, int sms, cudaStream_t
   const unsigned grid = (unsigned)(most < fit ? most : fit);
   constexpr size_t smem = Cfg<D>::kSmem + MT * 16 * Cfg<D>::kRow;  // the pipelines, the query rows
   cudaError_t e = cudaFuncSetAttribute(k_attn_few<T, D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e == cudaSuccess) e = launch_pdl(false, k_attn_few<T, D, MT>, dim3(grid), dim3(kThreads), smem, s, c, parts);
+  if (e == cudaSuccess) e = launch_pdl(true, k_attn_few<T, D, MT>, dim3(grid), dim3(kThreads), smem, s, c, parts);
   if (e == cudaSuccess && grid > 1) e = launch_attn_join(c, parts, D, Half2<T>::kBf16, MT * 16, false, (int)grid, s);
   return e;
 }

@@ -1,13 +1,14 @@
 // The partials of paged attention joined: out = sum_p 2^(m_p - M) o_p / sum_p 2^(m_p - M) l_p over a row's pieces in their
 // order, M the largest m_p.  A copy's work: bounded by the launch for the few pieces of a balanced split, by reading them
 // where one sequence is cut for all blocks.  Threads hold four columns each.  A block takes one row, its groups of threads
-// the pieces in turn (few rows, perhaps many pieces), or one row a group (many rows, few pieces).
+// the pieces in turn (many pieces), or one row a group (few pieces).
 #include "mf_attn.cuh"
 
 namespace mf {
 namespace {
 
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kFew = 8;  // pieces up to which a row is one group of threads' work
 
 template <int D>
 struct Join {
@@ -15,15 +16,10 @@ struct Join {
 };
 
 template <class T, int D, bool kOneRow, bool kTiles>
-__global__ void __launch_bounds__(Join<D>::kThreads) k_attn_join(AttnCall c, AttnParts parts, int part_rows) {
+__device__ __forceinline__ void join_row(const AttnCall& c, const AttnParts& parts, int part_rows, const AttnRec& rec, int b, int r,
+                                         int col, int g) {
   using J = Join<D>;
-  // many rows: neighbouring threads take neighbouring rows, which is how tiles leave them
-  const int b = blockIdx.x, tid = threadIdx.x, col = kOneRow ? tid % J::kCols : tid / J::kGroups,
-            g = kOneRow ? tid / J::kCols : tid % J::kGroups;
-  pdl_wait();
-  const AttnRec rec = parts.rec[b];
-  const int r = kOneRow ? (int)blockIdx.y : (int)blockIdx.y * J::kGroups + g;
-  if (rec.n == 0 || (kOneRow && r >= rec.rows)) return;
+  const int tid = threadIdx.x;
   auto o_of = [&](int64_t row) -> const float4* {  // the row's four columns (kTiles: column group by column group)
     const int64_t part0 = row - r;
     return reinterpret_cast<const float4*>(parts.o + part0 * D + (kTiles ? (col * part_rows + r) * 4 : r * D + col * 4));
@@ -32,6 +28,7 @@ __global__ void __launch_bounds__(Join<D>::kThreads) k_attn_join(AttnCall c, Att
   float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
   float mx = -INFINITY, ls = 0.f;
   if constexpr (kOneRow) {
+    __syncthreads();  // the row before this one has been read
     __shared__ float s_w[kMaxParts];
     __shared__ float4 s_o[J::kThreads];
     __shared__ float s_red[2][J::kThreads / 32];
@@ -71,7 +68,6 @@ __global__ void __launch_bounds__(Join<D>::kThreads) k_attn_join(AttnCall c, Att
       sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
     }
   } else {
-    if (r >= rec.rows) return;
     for (int p = 0; p < rec.n; ++p) mx = fmaxf(mx, parts.ml[row_of(p)].x);
     const float ms = mx == -INFINITY ? 0.f : mx;
 #pragma unroll 2
@@ -91,13 +87,31 @@ __global__ void __launch_bounds__(Join<D>::kThreads) k_attn_join(AttnCall c, Att
   if (c.lse && col == 0) c.lse[(int64_t)tok * c.st.Hq + head] = ls > 0.f ? (mx + log2f(ls)) * kLn2 : -INFINITY;
 }
 
+template <class T, int D, bool kOneRow, bool kTiles>
+__global__ void __launch_bounds__(Join<D>::kThreads, 2)
+    k_attn_join(const __grid_constant__ AttnCall c, const __grid_constant__ AttnParts parts, int part_rows) {
+  using J = Join<D>;
+  const int b = blockIdx.x, tid = threadIdx.x;
+  pdl_wait();
+  const AttnRec rec = parts.rec[b];
+  if (rec.n == 0) return;
+  if (kOneRow && rec.n > kFew) {
+    for (int r = blockIdx.y; r < rec.rows; r += gridDim.y)
+      join_row<T, D, true, kTiles>(c, parts, part_rows, rec, b, r, tid % J::kCols, tid / J::kCols);
+  } else {  // (neighbouring threads take what neighbours in memory: columns, or rows as tiles leave them)
+    const int col = kTiles ? tid / J::kGroups : tid % J::kCols, g = kTiles ? tid % J::kGroups : tid / J::kCols;
+    for (int r = blockIdx.y * J::kGroups + g; r < rec.rows; r += gridDim.y * J::kGroups)
+      join_row<T, D, false, kTiles>(c, parts, part_rows, rec, b, r, col, g);
+  }
+}
+
 template <class T, int D>
 cudaError_t run(const AttnCall& c, const AttnParts& parts, int rows, bool tiles, int blocks, cudaStream_t s) {
   using J = Join<D>;
   // up to 64 rows there may be many pieces of each; with more, a record has few pieces
   const int64_t most = (int64_t)c.st.max_q * c.st.G;
   const int held = (int)(most < rows ? most : rows);
-  const dim3 one(blocks, held), each(blocks, (held + J::kGroups - 1) / J::kGroups), threads(J::kThreads);
+  const dim3 one(blocks, held < 8 ? held : 8), each(blocks, (held + J::kGroups - 1) / J::kGroups), threads(J::kThreads);
   if (!tiles) return launch_pdl(true, k_attn_join<T, D, true, false>, one, threads, 0, s, c, parts, rows);
   if (held <= 64) return launch_pdl(true, k_attn_join<T, D, true, true>, one, threads, 0, s, c, parts, rows);
   return launch_pdl(true, k_attn_join<T, D, false, true>, each, threads, 0, s, c, parts, rows);

@@ -813,7 +813,7 @@ cudaError_t run(const AttnCall& c, const AttnMaps& maps, AttnPlan plan, const At
   const int64_t most = tiles * c.st.Hkv * (((int64_t)c.st.cap + kKeys - 1) / kKeys);
   const unsigned grid = (unsigned)(most < sms ? most : sms);
   cudaError_t e = cudaFuncSetAttribute(k_attn_many<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
-  if (e == cudaSuccess) e = launch_pdl(false, k_attn_plan<D>, dim3(1), dim3(1024), 0, s, c, plan);
+  if (e == cudaSuccess) e = launch_pdl(true, k_attn_plan<D>, dim3(1), dim3(1024), 0, s, c, plan);
   if (e == cudaSuccess) e = launch_pdl(true, k_attn_many<T, D>, dim3(grid), dim3(kThreads), C::kSmem, s, c, maps, plan, parts);
   if (e == cudaSuccess && grid > 1) e = launch_attn_join(c, parts, D, Half2<T>::kBf16, C::kRows, true, (int)grid, s);
   return e;
