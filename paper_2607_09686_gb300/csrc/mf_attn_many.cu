@@ -50,7 +50,7 @@ struct Cfg {
   static constexpr int kRowTiles = D == 256 ? 1 : 2;  // row tiles of a segment
   static constexpr int kRows = kRowTiles * 128;
   static constexpr uint32_t kQBytes = kRowTiles * kU * kUnitBytes;
-  static constexpr uint32_t kSmem = kQBytes + (kKSlots + kVSlots) * kSlotBytes + 1024;  // 1024: alignment
+  static constexpr uint32_t kTail = kQBytes + (kKSlots + kVSlots) * kSlotBytes;  // then a Tail
 };
 constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;
 
@@ -279,9 +279,18 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 // shared memory: [Q][ring of K][ring of V]; barriers: slots full and free, Q full and free, S and P by (warpgroup,
-// buffer; kBP2: the second half of P), O by row tile, the buffers free again, the end of all MMAs
+// buffer; kBP2: the second half of P), O by who reads it, the buffers free again, the end of all MMAs, and for segments of
+// one row tile m and l written, read, O read
 constexpr int kBKFull = 0, kBKFree = 5, kBVFull = 10, kBVFree = 15, kBQFull = 20, kBQFree = 21, kBS = 22, kBP = 26, kBO = 30,
-              kBBuf = 32, kBDrain = 34, kBP2 = 36, kBars = 40;
+              kBBuf = 32, kBDrain = 34, kBP2 = 36, kBStat = 40, kBStatFree = 41, kBOFree = 42, kBars = 43;
+
+struct Tail {
+  uint64_t bars[kBars];
+  Piece piece[8][2];
+  float2 stat[128];  // m and l of the rows of a segment of one row tile
+  uint32_t tmem;
+  int flag;
+};
 
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant__ AttnCall c, const __grid_constant__ AttnMaps maps,
@@ -289,12 +298,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
                                                            const __grid_constant__ AttnParts parts) {
   using C = Cfg<D>;
   constexpr bool kBf = Half2<T>::kBf16;
-  extern __shared__ unsigned char smem_raw[];
-  __shared__ uint64_t bars[kBars];
-  __shared__ Piece s_piece[8][2];
-  __shared__ uint32_t s_tmem;
-  __shared__ volatile int s_flag;
-  const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  extern __shared__ __align__(1024) unsigned char smem[];  // (nothing static beside it: it begins at a multiple of 1024)
+  Tail& tail = *reinterpret_cast<Tail*>(smem + C::kTail);
+  uint64_t* bars = tail.bars;
+  auto& s_piece = tail.piece;
+  uint32_t& s_tmem = tail.tmem;
+  volatile int& s_flag = tail.flag;
+  const uint32_t smem0 = smem_u32(smem);
   const uint32_t kring = smem0 + C::kQBytes, vring = kring + C::kKSlots * C::kSlotBytes;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const AttnStep& st = c.st;
@@ -324,7 +334,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
   auto wait_all = [&](int bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, wait(bar, parity)); };
 
   if (warp < kQkWarp) {
-    // ================= softmax: warpgroup wg has row tile wg of two, or (wg 0) the only one
+    // ================= softmax: warpgroup wg has row tile wg of two; of the only one, 0 the softmax and 1 the storing of
+    // O, while 0 has begun the next segment
     const int wg = warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float sc2 = c.scale * kLog2e;
@@ -332,7 +343,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     walk_start(w, c, p, tiles, C::kRows, t0, t1);
     int par = 0;                     // buffer of the segment's first job
     uint32_t sph[2] = {0, 0};        // phases of this warpgroup's S barriers, by buffer
-    uint32_t oph = 0;                // phase of its O barrier
+    uint32_t oph = 0, lph = wg ^ 1;      // phases of its O barrier, of that of m and l (0 waits for them to be read)
     int rec_n = 0;
     bool alive = true;
     int at = 0;
@@ -345,13 +356,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     };
     for (; s_piece[warp][at].more && alive; at ^= 1) {
       const Piece& cur = s_piece[warp][at];
-      const int nj = cur.nj, two = cur.two, k_start = cur.k_start;
+      const int nj = cur.nj, two = cur.two, k_start = cur.k_start, tile_row = (two ? wg * 128 : 0) + row;
+      const uint32_t col_o = tmem + lanes + kColO + (two ? wg * D : 0);
+      const bool ok = tile_row < cur.rows;
+      float m = -INFINITY, l = 0.f;
       if (two || wg == 0) {
-        const bool ok = wg * 128 + row < cur.rows;
-        const int pos = cur.first + (cur.R0 + wg * 128 + row) / st.G;
+        const int pos = cur.first + (cur.R0 + tile_row) / st.G;
         const int lo = ok ? vis_lo(c, pos) : 0, hi = ok ? vis_hi(c, pos, cur.len) : 0;
-        const uint32_t col_o = tmem + lanes + kColO + (two ? wg * D : 0);
-        float m = -INFINITY, l = 0.f;
         for (int j = 0; j < nj; ++j) {
           const int buf = (par + (two ? wg : j)) & 1;
           if (!(alive = wait_all(kBS + wg * 2 + buf, sph[buf] & 1))) break;
@@ -458,17 +469,38 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           if (lane == 0) mbar_arrive(&bars[kBP2 + wg * 2 + buf]);
         }
         if (!alive) break;
-        // the next segment is looked up while the last product runs: after the stores below its loads would queue
-        advance();
+        if (tid == 0 && cur.j0 == 0 && nj != cur.nt) {
+          // the block of the segment's last key tile, by the place of its first job
+          rec_n = (int)((B * (cur.last + 1) - 1) / total) - (int)b + 1;
+          parts.rec[b] = {cur.q0, cur.h, cur.R0, cur.rows, rec_n};
+        }
+        if (!two) {  // m and l to the other warpgroup
+          if (!(alive = wait_all(kBStatFree, lph))) break;
+          lph ^= 1;
+          tail.stat[row] = make_float2(m, l);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars[kBStat]);
+        }
+      } else {
+        if (!(alive = wait_all(kBStat, lph))) break;
+        lph ^= 1;
+        const float2 ml = tail.stat[row];
+        m = ml.x, l = ml.y;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[kBStatFree]);
+      }
+      // the next segment is looked up while the last product runs: after the stores below its loads would queue
+      advance();
+      if (two || wg == 1) {
         // ---- the piece's o
         if (!(alive = wait_all(kBO + wg, oph))) break;
         oph ^= 1;
         tc::fence_after();
-        const int R = cur.R0 + wg * 128 + row, tok = R / st.G, q0 = cur.q0, h = cur.h, j0 = cur.j0;
+        const int R = cur.R0 + tile_row, tok = R / st.G, q0 = cur.q0, h = cur.h, j0 = cur.j0;
         const bool whole = nj == cur.nt;
         // partials column group by column group, so that a warp's rows are neighbours
-        const int64_t pr0 = ((int64_t)b * 2 + (j0 == 0)) * C::kRows, pr = pr0 + wg * 128 + row;
-        float* po = parts.o + pr0 * D + (wg * 128 + row) * 4;
+        const int64_t pr0 = ((int64_t)b * 2 + (j0 == 0)) * C::kRows, pr = pr0 + tile_row;
+        float* po = parts.o + pr0 * D + tile_row * 4;
         const int head = h * st.G + R % st.G;
         if (whole) {
           // 64 columns at a time: 32 bytes of a row and lane, transposed among four lanes, so that these store 128
@@ -539,13 +571,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           if (!whole) parts.ml[pr] = make_float2(mm, l);
           else if (c.lse) c.lse[(int64_t)(q0 + tok) * st.Hq + head] = l > 0.f ? (mm + log2f(l)) * kLn2 : -INFINITY;
         }
-        if (tid == 0 && j0 == 0 && !whole) {
-          // the block of the segment's last key tile, by the place of its first job
-          rec_n = (int)((B * (cur.last + 1) - 1) / total) - (int)b + 1;
-          parts.rec[b] = {q0, h, cur.R0, cur.rows, rec_n};
+        if (!two) {  // O may be written again
+          tc::fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars[kBOFree]);
         }
       }
-      if (!two && wg == 1) advance();
       par = (par + (nj << two)) & 1;
     }
     if (tid == 0 && rec_n == 0) parts.rec[b].n = 0;
@@ -618,7 +649,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     } else {
       constexpr uint32_t kId = tc::idesc_f16(kBf, D == 64 ? 64 : 128, true);
       const uint32_t r0 = uniform(vring);
-      uint32_t first = 0, pph = 0;  // pph: phases of the four P barriers, a bit each
+      uint32_t first = 0, pph = 0, oph = 0;  // pph: phases of the four P barriers, a bit each
+      bool read_by_other = false;            // the last segment's O is read by warpgroup 1 while this one's P is formed
 #pragma unroll 1
       for (; jb.live; ++g, buf ^= 1) {  // O += P V
         bool ok = true;
@@ -629,10 +661,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
             if (++slot == C::kVSlots) slot = 0, sph ^= 1;
           }
         }
+        if (jb.i == 0) {
+          if (read_by_other) {
+            ok = ok && wait_all(kBOFree, oph);
+            oph ^= 1;
+          }
+          read_by_other = !jb.two;
+        }
         const int pb = jb.row_tile() * 2 + (int)buf;
         const uint32_t x = uniform(jb.row_tile()), b_ = uniform(buf), acc = uniform(jb.i > jb.two), f = uniform(first);
-        // two row tiles: only their last product is waited for (their next S is formed after it), else each one
-        const uint32_t tell = uniform(!jb.two || jb.i + 2 >= jb.n), last = uniform(jb.last_of_tile());
+        // two row tiles: only their last product is waited for (their next S is formed after it); one: each, the last by
+        // warpgroup 1
+        const uint32_t tell = uniform(!jb.two || jb.i + 2 >= jb.n), who = uniform(jb.two ? jb.row_tile() : jb.i == jb.n - 1), last = uniform(jb.last_of_tile());
         ok = ok && wait_all(kBP + pb, pph >> pb & 1);
         if (!ok) break;
         pph ^= 1u << pb;
@@ -662,7 +702,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
               tc::mma_ts(tm + kColO + x * D + v * 128, tm + kColS + b_ * 128 + k * 8, bd + k * (2048 >> 4), kId, 1);
             if (v == C::kTileSlots - 1) {
               tc::commit(bars0 + (kBBuf + b_) * 8);
-              if (tell) tc::commit(bars0 + (kBO + x) * 8);
+              if (tell) tc::commit(bars0 + (kBO + who) * 8);
             }
             if (last) tc::commit(bars0 + (kBVFree + sl) * 8);
           }
@@ -812,9 +852,11 @@ cudaError_t run(const AttnCall& c, const AttnMaps& maps, AttnPlan plan, const At
   plan.max_tiles = tiles < plan.max_tiles ? (int)tiles : plan.max_tiles;
   const int64_t most = tiles * c.st.Hkv * (((int64_t)c.st.cap + kKeys - 1) / kKeys);
   const unsigned grid = (unsigned)(most < sms ? most : sms);
-  cudaError_t e = cudaFuncSetAttribute(k_attn_many<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem);
+  constexpr size_t smem = C::kTail + sizeof(Tail);
+  static_assert(smem <= 232448, "shared memory of a block");
+  cudaError_t e = cudaFuncSetAttribute(k_attn_many<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e == cudaSuccess) e = launch_pdl(true, k_attn_plan<D>, dim3(1), dim3(1024), 0, s, c, plan);
-  if (e == cudaSuccess) e = launch_pdl(true, k_attn_many<T, D>, dim3(grid), dim3(kThreads), C::kSmem, s, c, maps, plan, parts);
+  if (e == cudaSuccess) e = launch_pdl(true, k_attn_many<T, D>, dim3(grid), dim3(kThreads), smem, s, c, maps, plan, parts);
   if (e == cudaSuccess && grid > 1) e = launch_attn_join(c, parts, D, Half2<T>::kBf16, C::kRows, true, (int)grid, s);
   return e;
 }
