@@ -200,8 +200,6 @@ __device__ __noinline__ void walk_start(Walk& w, const AttnCall& c, const AttnPl
   if (w.j0 >= w.j1) w.next(c, p, tile_rows);
 }
 
-__device__ __noinline__ void walk_next(Walk& w, const AttnCall& c, const AttnPlan& p, int tile_rows) { w.next(c, p, tile_rows); }
-
 // The jobs of the walk one by one: (key tile, row tile), row tile inner.
 struct Jobs {
   int i, n, two;  // job in its segment, of n; two row tiles
@@ -217,8 +215,8 @@ struct Jobs {
   __device__ __forceinline__ bool last_of_tile() const { return !two || (i & 1); }
 };
 
-// What the softmax needs of a segment.  Each of its warps keeps this and the next one in shared memory: the registers
-// hold scores.
+// What the softmax needs of a segment, told by the warp that copies K: it comes to a segment a few key tiles ahead, and the
+// softmax, which has no registers to walk with, finds it in shared memory.
 struct Piece {
   int nj, two, k_start, R0, rows, h, q0, first, len, nt, j0, more;
   int64_t last;  // place of the last key tile's first job
@@ -280,13 +278,15 @@ __device__ __forceinline__ float ex2(float x) {
 }
 // shared memory: [Q][ring of K][ring of V]; barriers: slots full and free, Q full and free, S and P by (warpgroup,
 // buffer; kBP2: the second half of P), O by who reads it, the buffers free again, the end of all MMAs, and for segments of
-// one row tile m and l written, read, O read
+// one row tile m and l written, read, O read; segments told, done with
 constexpr int kBKFull = 0, kBKFree = 5, kBVFull = 10, kBVFree = 15, kBQFull = 20, kBQFree = 21, kBS = 22, kBP = 26, kBO = 30,
-              kBBuf = 32, kBDrain = 34, kBP2 = 36, kBStat = 40, kBStatFree = 41, kBOFree = 42, kBars = 43;
+              kBBuf = 32, kBDrain = 34, kBP2 = 36, kBStat = 40, kBStatFree = 41, kBOFree = 42,
+              kBPiece = 43, kBPieceFree = 47, kBars = 51;
+constexpr int kPieces = 4;
 
 struct Tail {
   uint64_t bars[kBars];
-  Piece piece[8][2];
+  Piece piece[kPieces];
   float2 stat[128];  // m and l of the rows of a segment of one row tile
   uint32_t tmem;
   int flag;
@@ -301,7 +301,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
   extern __shared__ __align__(1024) unsigned char smem[];  // (nothing static beside it: it begins at a multiple of 1024)
   Tail& tail = *reinterpret_cast<Tail*>(smem + C::kTail);
   uint64_t* bars = tail.bars;
-  auto& s_piece = tail.piece;
   uint32_t& s_tmem = tail.tmem;
   volatile int& s_flag = tail.flag;
   const uint32_t smem0 = smem_u32(smem);
@@ -309,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const AttnStep& st = c.st;
   if (tid == 0) {
-    for (int i = 0; i < kBars; ++i) mbar_init(&bars[i], (i >= kBP && i < kBP + 4) || i >= kBP2 ? 4 : 1);
+    for (int i = 0; i < kBars; ++i) mbar_init(&bars[i], i >= kBPieceFree ? 8 : i >= kBPiece ? 1 : (i >= kBP && i < kBP + 4) || i >= kBP2 ? 4 : 1);
     s_flag = 0;
     mbar_fence_init();
   }
@@ -339,23 +338,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     const int wg = warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float sc2 = c.scale * kLog2e;
-    Walk w;  // kept in memory: the scores need the registers
-    walk_start(w, c, p, tiles, C::kRows, t0, t1);
     int par = 0;                     // buffer of the segment's first job
     uint32_t sph[2] = {0, 0};        // phases of this warpgroup's S barriers, by buffer
     uint32_t oph = 0, lph = wg ^ 1;      // phases of its O barrier, of that of m and l (0 waits for them to be read)
     int rec_n = 0;
     bool alive = true;
     int at = 0;
-    if (lane == 0) s_piece[warp][0].take(w, C::kRows);
-    __syncwarp();
-    auto advance = [&]() {  // the next segment into the other place
-      walk_next(w, c, p, C::kRows);
-      if (lane == 0) s_piece[warp][at ^ 1].take(w, C::kRows);
-      __syncwarp();
-    };
-    for (; s_piece[warp][at].more && alive; at ^= 1) {
-      const Piece& cur = s_piece[warp][at];
+    uint32_t pph = 0;
+    for (;;) {
+      if (!(alive = wait_all(kBPiece + at, pph))) break;
+      const Piece& cur = tail.piece[at];
+      if (!cur.more) break;
       const int nj = cur.nj, two = cur.two, k_start = cur.k_start, tile_row = (two ? wg * 128 : 0) + row;
       const uint32_t col_o = tmem + lanes + kColO + (two ? wg * D : 0);
       const bool ok = tile_row < cur.rows;
@@ -489,8 +482,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars[kBStatFree]);
       }
-      // the next segment is looked up while the last product runs: after the stores below its loads would queue
-      advance();
       if (two || wg == 1) {
         // ---- the piece's o
         if (!(alive = wait_all(kBO + wg, oph))) break;
@@ -578,6 +569,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         }
       }
       par = (par + (nj << two)) & 1;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars[kBPieceFree + at]);
+      if (++at == kPieces) at = 0, pph ^= 1;
     }
     if (tid == 0 && rec_n == 0) parts.rec[b].n = 0;
   } else if (warp <= kPvWarp) {
@@ -754,8 +748,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     Walk w0;
     walk_start(w0, c, p, tiles, C::kRows, t0, t1);
     Walk w = w0;
+    int told = 0;
+    uint32_t tph = 1;
+    auto tell = [&]() -> bool {  // the softmax what comes
+      if (!wait_free(kBPieceFree + told, tph)) return false;
+      if (lane == 0) {
+        tail.piece[told].take(w, C::kRows);
+        mbar_arrive(&bars[kBPiece + told]);
+      }
+      __syncwarp();
+      if (++told == kPieces) told = 0, tph ^= 1;
+      return true;
+    };
 #pragma unroll 1
     for (; w.more && ok; w.next(c, p, C::kRows)) {
+      if (is_k && !(ok = tell())) break;
       if (is_k) {  // the segment's rows of q
         if (!(ok = wait_free(kBQFree, seg_ph))) break;
         seg_ph ^= 1;
@@ -830,6 +837,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         }
       }
     }
+    if (is_k && ok) tell();  // the end
     announce(true);
     asm volatile("cp.async.wait_all;" ::: "memory");
     // no copy may be in flight when the block exits: the MMA warps have waited for every slot they used, and use all unless a
