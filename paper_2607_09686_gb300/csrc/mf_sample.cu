@@ -6,7 +6,7 @@
 //
 // A cluster of 1 to 8 blocks has a row, each block a slice of it in shared memory: the logits cross the memory bus
 // once, whatever the steps that follow.  Sums and choices of the blocks meet in distributed shared memory.  Steps:
-//   1. load (bulk copies; where nothing is cut the noise with it), M = max.
+//   1. load (bulk copies), M = max.
 //   2. top-k: the k-th largest of the threads' own maxima is a floor of the k-th largest entry, and hardly more than k
 //      entries reach it; these go to the leading block, which sorts them and finishes alone: top-p, min-p, argmax.  (Where k
 //      is large for that, a histogram of counts over bins of 1/64 in z takes the maxima's place.)
@@ -18,9 +18,10 @@
 //   5. what is kept: sum of w and the largest z + noise, with z as a product; then the entries that come near that one
 //      again, with z as the exact quotient.
 // What bounds it: with top-k the cluster's barriers and one pass over the slice; else passes of some ten to twenty
-// instructions an entry.
+// instructions an entry.  Rows by temperature alone have a kernel of their own, in one pass (k_sample_plain).
 #include <cooperative_groups.h>
 
+#include <cfloat>
 #include <cmath>
 
 #include "mf_attn.cuh"
@@ -46,7 +47,7 @@ struct SampleCall {
   int vocab;
   int slice;  // entries of a block
   int qbits;  // bits of a mass unit
-  int keep;   // the slice's logits (1), and its noise too (2), lie in shared memory
+  int keep;   // the slice's logits lie in shared memory
 };
 
 // larger floats have larger keys (-0 and +0 compare equal as floats: one key)
@@ -93,9 +94,8 @@ struct Shared {
   uint64_t bar;  // the bulk copies' barrier
 };
 
-// kCut: some row may have top-k or top-p.  Without, a block needs fewer registers and three find room on an SM.
-template <class T, bool kCut>
-__global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c) {
+template <class T>
+__global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   extern __shared__ __align__(16) unsigned char dyn[];
   __shared__ Shared sh;
   cg::cluster_group cl = cg::this_cluster();
@@ -109,45 +109,32 @@ __global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c)
   Shared* lead = cl.map_shared_rank(&sh, 0);
   unsigned long long* lead_list = cl.map_shared_rank(list, 0);
 
+  pdl_wait();
   // ---- 1. the slice into shared memory, at the same place modulo 16 bytes: whole vectors by bulk copies, the ends by hand
   auto up = [](T v) -> float { return fmaxf((float)v, -INFINITY); };  // NaN as -inf
   const T* src = row;
-  const float* gsrc = noise;
   bool lost = false;  // a copy did not arrive in time: the row has no answer (as if it had no entry)
   if (c.keep) {
-    unsigned char* room = dyn + (c.keep == 2 ? 0 : kBins * 4 + kList * 8);
-    T* x0 = reinterpret_cast<T*>(room + ((uintptr_t)row & 15));
-    float* g0 = reinterpret_cast<float*>(room + (((size_t)c.slice * sizeof(T) + 31) & ~size_t(15)) + ((uintptr_t)noise & 15));
-    auto ends = [&](const auto* from, auto* to, int& head, int& body) {
-      constexpr int kE = (int)sizeof(*from);
-      head = min(n, (int)((16 - ((uintptr_t)from & 15)) & 15) / kE);
-      body = (n - head) * kE / 16 * 16 / kE;
-      for (int i = tid; i < n - body; i += kThreads) {
-        const int at = i < head ? i : body + i;
-        to[at] = from[at];
-      }
-    };
-    int hx, bx, hg = 0, bg = 0;
+    T* x0 = reinterpret_cast<T*>(dyn + kBins * 4 + kList * 8 + ((uintptr_t)row & 15));
+    const int head = min(n, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T)),
+              body = (n - head) * (int)sizeof(T) / 16 * 16 / (int)sizeof(T);
     if (tid == 0) {
       mbar_init(&sh.bar, 1);
       mbar_fence_init();
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    }
-    ends(row, x0, hx, bx);
-    if (c.keep == 2) ends(noise, g0, hg, bg);
-    if (tid == 0) {
-      mbar_arrive_tx(&sh.bar, (uint32_t)(bx * sizeof(T) + bg * 4));
+      const uint32_t bytes = (uint32_t)(body * sizeof(T));
+      mbar_arrive_tx(&sh.bar, bytes);
       // pieces of 32 KiB: several copies in flight
-      auto copy = [&](unsigned char* to, const unsigned char* from, uint32_t bytes) {
-        for (uint32_t o = 0; o < bytes; o += 32768) bulk_g2s(to + o, from + o, min(bytes - o, 32768u), &sh.bar);
-      };
-      copy(reinterpret_cast<unsigned char*>(x0 + hx), reinterpret_cast<const unsigned char*>(row + hx), (uint32_t)(bx * sizeof(T)));
-      copy(reinterpret_cast<unsigned char*>(g0 + hg), reinterpret_cast<const unsigned char*>(noise + hg), (uint32_t)(bg * 4));
+      for (uint32_t o = 0; o < bytes; o += 32768)
+        bulk_g2s(reinterpret_cast<unsigned char*>(x0 + head) + o, reinterpret_cast<const unsigned char*>(row + head) + o, min(bytes - o, 32768u),
+                 &sh.bar);
+    }
+    for (int i = tid; i < n - body; i += kThreads) {
+      const int at = i < head ? i : body + i;
+      x0[at] = row[at];
     }
     __syncthreads();
     lost = __syncthreads_or(!mbar_wait(&sh.bar, 0, kDefaultWaitNs));
     src = x0;
-    if (c.keep == 2) gsrc = g0;
   }
   // every thread's entries: whole vectors of the slice where it lies in shared memory
   auto for_each = [&](auto&& f) {
@@ -294,13 +281,17 @@ __global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c)
   };
   // the kept entries of bins lo .. hi onto the leading block's list (as many as there is room for; all are counted): each
   // block collects its own first, so that only whole runs and one counter cross to the leading block
-  auto gather = [&](int lo, int hi) {
+  auto gather = [&](int lo, int hi, float floor) {  // (or, lo < 0: the entries from `floor` on)
     unsigned kmin = 0xFFFFFFFFu, kmax = 0;
     if (tid == 0) sh.mine = 0;
     __syncthreads();
     for_each([&](int i, float x) {
-      const int b = bin_of(x == m ? 0.f : x - m, inv);
-      if (b < lo || b > hi || !kept(x, base + i)) return;
+      if (lo < 0) {
+        if (x < floor) return;
+      } else {
+        const int b = bin_of(x == m ? 0.f : x - m, inv);
+        if (b < lo || b > hi || !kept(x, base + i)) return;
+      }
       const uint32_t k = order_key(x);
       const unsigned at = atomicAdd(&sh.mine, 1u);
       if (at < kList) list[at] = (unsigned long long)k << 32 | (0xFFFFFFFFu - (unsigned)(base + i));
@@ -437,7 +428,6 @@ __global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c)
     cl.sync();
     return;
   }
-  if constexpr (kCut) {
   if (!greedy && top_k > 0 && top_k < c.vocab) {
     // ---- 2. top-k
     // The bin down to which top_k of the threads' maxima reach holds top_k entries at least; if the list has no room for all
@@ -446,7 +436,9 @@ __global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c)
     if (top_k <= kThreads * C / 2) {
       find_bin(kMaxima, (float)top_k);
       if (lead->bin >= 0) {
-        gather(0, lead->bin);
+        // the bin's lower end, a little lower for the rounding (more entries than needed do no harm)
+        const float low = m - (float)(lead->bin + 1) * (1.f / inv) * 1.00001f;
+        gather(-1, 0, lead->bin < kBins - 1 && low > -INFINITY ? low : -FLT_MAX);
         few = lead->listed <= kList;
         cl.sync();
         if (!few && rank == 0 && tid == 0) sh.listed = 0, sh.kmin = 0xFFFFFFFFu, sh.kmax = 0;
@@ -457,7 +449,7 @@ __global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c)
     if (bin >= 0) {
       if (!few) {
         few = lead->count <= kList;
-        gather(few ? 0 : bin, bin);
+        gather(few ? 0 : bin, bin, 0.f);
       }
       if (few) {
         if (rank == 0) {
@@ -526,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c)
       find_bin(kMasses, top_p);
       const int bin = lead->bin;
       if (bin >= 0) {
-        gather(bin, bin);
+        gather(bin, bin, 0.f);
         const unsigned len = lead->listed;
         if (len <= kList) {
           if (rank == 0) {
@@ -643,7 +635,6 @@ __global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c)
       }
     }
   }
-  }
   // ---- 5. what is kept
   const bool first_only = greedy || top_p <= 0.f;
   Best b = none;
@@ -675,13 +666,13 @@ __global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c)
     if (min_p > 0.f || m == INFINITY) {
       for (int i = tid; i < n; i += kThreads) {
         float d, near, w;
-        if (in_with(up(src[i]), base + i, d, near, w)) add(near, w, gsrc[i]);
+        if (in_with(up(src[i]), base + i, d, near, w)) add(near, w, noise[i]);
       }
     } else {
 #pragma unroll 8
       for (int i = tid; i < n; i += kThreads) {
         const float x = up(src[i]), d = x - m;
-        if (!kCut || kept(x, base + i)) add(d * inv_t, ex2(d * inv_e), gsrc[i]);  // (-inf: nothing to the sum, no key)
+        if (kept(x, base + i)) add(d * inv_t, ex2(d * inv_e), noise[i]);
       }
     }
     const float own_reach = reach;
@@ -689,13 +680,14 @@ __global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c)
     const float floor = top - 4e-6f * fabsf(top);
     // the entries near the largest, in threads that have one (a reach or floor that is no number: in any)
     if (!(own_reach < floor))
+#pragma unroll 4
     for (int i = tid; i < n; i += kThreads) {
       const float x = up(src[i]);
       if (!kept(x, base + i)) continue;
       float d, near, w;
       d = x == m ? 0.f : x - m;
       near = d == 0.f ? 0.f : d * inv_t;
-      const float g = fmaxf(gsrc[i], -INFINITY), key = near + g;
+      const float g = fmaxf(noise[i], -INFINITY), key = near + g;
       if (!(key >= top || !(key + 4e-6f * (fabsf(near) + fabsf(g)) < floor))) continue;
       if (!in_with(x, base + i, d, near, w)) continue;
       const float z = z_of(x, m, t);
@@ -712,38 +704,195 @@ __global__ void __launch_bounds__(kThreads, kCut ? 2 : 3) k_sample(SampleCall c)
   cl.sync();  // no block leaves while another reads its shared memory
 }
 
+// ---- rows by temperature alone: no entry is cut, so that one pass over logits and noise will do
+//
+// Each thread keeps the running maximum of its logits and its sum of w against that (scaled when the maximum grows), and of
+// its keys, with M / T left in (x / T + noise), the largest and the largest with its margin: rounding aside the keys' order
+// needs no M.  With the row's M known, only threads whose keys come near the largest look at their entries again, with z as the
+// exact quotient.  Bounded by reading logits and noise once, and by two cluster barriers a row.
+struct PlainShared {
+  float m[kWarps], s[kWarps], top[kWarps];
+  int i[kWarps];
+  float bm, bs, btop;  // of the block
+  int bi;
+  float sum;
+  Best best[kWarps], block_best;
+};
+
+template <class T>
+__global__ void __launch_bounds__(kThreads, 2) k_sample_plain(SampleCall c) {
+  __shared__ PlainShared sh;
+  cg::cluster_group cl = cg::this_cluster();
+  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank(), r = blockIdx.x / C;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int base = rank * c.slice, n = max(0, min(c.slice, c.vocab - base));
+  const T* row = static_cast<const T*>(c.logits) + (int64_t)r * c.logits_stride + base;
+  const float* noise = c.noise + (int64_t)r * c.noise_stride + base;
+  pdl_wait();
+  const float temp = c.temperature ? c.temperature[r] : 1.f;
+  const bool greedy = !(temp > 0.f);
+  const float t = greedy ? 1.f : temp, inv_t = 1.f / t, inv_e = inv_t * 1.4426950408889634f;
+  auto up = [](T v) -> float { return fmaxf((float)v, -INFINITY); };  // NaN as -inf
+  auto scaled = [&](float s, float from, float to) { return from == to ? s : s * ex2((from - to) * inv_e); };
+  float m = -INFINITY, s = 0.f, top = -INFINITY, reach = -INFINITY;
+  int first = 0x7FFFFFFF;  // of this thread's largest
+  auto add = [&](float x, float g, int i) {
+    if (x > m) {
+      s = scaled(s, m, x) + 1.f;
+      m = x, first = i;
+    } else {
+      s += x == m ? 1.f : ex2((x - m) * inv_e);
+    }
+    const float near = x * inv_t, key = near + g;
+    top = fmaxf(top, key);
+    reach = fmaxf(reach, fmaf(4e-6f, fabsf(near) + fabsf(g), key));
+  };
+  constexpr int kU = 16;  // loads of an entry's logit and noise under way in each thread
+  int i = tid;
+  for (; i + (kU - 1) * kThreads < n; i += kU * kThreads) {
+    T x[kU];
+    float g[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) x[u] = row[i + u * kThreads], g[u] = noise[i + u * kThreads];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) add(up(x[u]), g[u], base + i + u * kThreads);
+  }
+  for (; i < n; i += kThreads) add(up(row[i]), noise[i], base + i);
+  if (m == -INFINITY) s = 0.f;
+
+  // the block's, then the row's
+  const float own_reach = reach;
+  auto join = [&](float& am, float& as, float& atop, int& ai, float bm, float bs, float btop, int bi) {
+    const float to = fmaxf(am, bm);
+    as = to == -INFINITY ? 0.f : scaled(as, am, to) + scaled(bs, bm, to);
+    ai = am == bm ? min(ai, bi) : am > bm ? ai : bi;
+    am = to, atop = fmaxf(atop, btop);
+  };
+  auto warp_join = [&](float& am, float& as, float& atop, int& ai) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1)
+      join(am, as, atop, ai, __shfl_xor_sync(0xffffffffu, am, d), __shfl_xor_sync(0xffffffffu, as, d),
+           __shfl_xor_sync(0xffffffffu, atop, d), __shfl_xor_sync(0xffffffffu, ai, d));
+  };
+  warp_join(m, s, top, first);
+  if (lane == 0) sh.m[warp] = m, sh.s[warp] = s, sh.top[warp] = top, sh.i[warp] = first;
+  __syncthreads();
+  if (warp == 0) {
+    const bool in = lane < kWarps;
+    m = in ? sh.m[lane] : -INFINITY, s = in ? sh.s[lane] : 0.f, top = in ? sh.top[lane] : -INFINITY, first = in ? sh.i[lane] : 0x7FFFFFFF;
+    warp_join(m, s, top, first);
+    if (lane == 0) sh.bm = m, sh.bs = s, sh.btop = top, sh.bi = first;
+  }
+  cl.sync();
+  {
+    const PlainShared* o = cl.map_shared_rank(&sh, lane < C ? lane : 0);
+    const bool in = lane < C;
+    m = in ? o->bm : -INFINITY, s = in ? o->bs : 0.f, top = in ? o->btop : -INFINITY, first = in ? o->bi : 0x7FFFFFFF;
+    warp_join(m, s, top, first);
+  }
+  Best b = {-INFINITY, 0.f, 0x7FFFFFFF};
+  if (!greedy && m == INFINITY) {  // the entries of +inf share the mass: their number, and the largest of their noise
+    float num = 0.f;
+    for (int k = tid; k < n; k += kThreads)
+      if ((float)row[k] == INFINITY) {
+        num += 1.f;
+        b.take(fmaxf(noise[k], -INFINITY), 0.f, base + k);
+      }
+#pragma unroll
+    for (int d = 16; d; d >>= 1) num += __shfl_xor_sync(0xffffffffu, num, d);
+    __syncthreads();
+    if (lane == 0) sh.s[warp] = num;
+    __syncthreads();
+    if (tid == 0) {
+      num = 0.f;
+      for (int w = 0; w < kWarps; ++w) num += sh.s[w];
+      sh.sum = num;
+    }
+  } else if (!greedy && m > -INFINITY) {
+    const float slack = 4e-6f * fabsf(m * inv_t), floor = top - 4e-6f * fabsf(top) - slack;
+    if (!(own_reach + slack < floor))  // (no number: look)
+      for (int k0 = tid; k0 < n; k0 += kU * kThreads) {
+        float x[kU], g[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {  // all loads before their use: few threads are here, and the row waits for them
+          const int k = k0 + u * kThreads;
+          x[u] = k < n ? up(row[k]) : -INFINITY, g[u] = k < n ? fmaxf(noise[k], -INFINITY) : -INFINITY;
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          if (x[u] == -INFINITY) continue;
+          const float near = x[u] * inv_t, key = near + g[u];
+          if (!(key >= top) && key + 4e-6f * (fabsf(near) + fabsf(g[u])) + slack < floor) continue;
+          const float z = z_of(x[u], m, t);
+          b.take(z + g[u], z, base + k0 + u * kThreads);
+        }
+      }
+  }
+  auto warp_best = [&](Best v) -> Best {
+#pragma unroll
+    for (int d = 16; d; d >>= 1)
+      v.take(__shfl_xor_sync(0xffffffffu, v.v, d), __shfl_xor_sync(0xffffffffu, v.z, d), __shfl_xor_sync(0xffffffffu, v.i, d));
+    return v;
+  };
+  const Best none = {-INFINITY, 0.f, 0x7FFFFFFF};
+  b = warp_best(b);
+  if (lane == 0) sh.best[warp] = b;
+  __syncthreads();
+  if (warp == 0) {
+    b = warp_best(lane < kWarps ? sh.best[lane] : none);
+    if (lane == 0) sh.block_best = b;
+  }
+  cl.sync();
+  if (rank == 0 && warp == 0) {
+    b = warp_best(lane < C ? cl.map_shared_rank(&sh, lane)->block_best : none);
+    if (lane == 0) {
+      if (m == INFINITY) {
+        s = 0.f;
+        for (int q = 0; q < C; ++q) s += cl.map_shared_rank(&sh, q)->sum;
+      }
+      c.token[r] = m == -INFINITY ? -1 : greedy ? first : b.i;
+      if (c.logprob) c.logprob[r] = m == -INFINITY ? -INFINITY : greedy ? 0.f : b.z - logf(s);
+    }
+  }
+  cl.sync();  // no block leaves while another reads its shared memory
+}
+
 int ceil_log2(int v) {
   int l = 0;
   while ((1 << l) < v) ++l;
   return l;
 }
 
-template <class T, bool kCut>
+template <class T>
 cudaError_t run(SampleCall c, int rows, cudaStream_t s) {
   // Blocks of a row: as many as leave each some ten thousand entries while they find room on the GPU at once (few rows),
-  // at least so many that the slices stay in shared memory.  Where nothing is cut, the noise of every entry is needed: it is
-  // loaded with the logits, in slices of at most 76 KiB together: three blocks an SM.
-  const size_t entry = sizeof(T) + (kCut ? 0 : 4), most = kCut ? 64 * 1024 : 76 * 1024;
+  // at least so many that the slices stay in shared memory.  By temperature alone: no more than find room at once (256
+  // rows of 50001: one block a row 32 us, four a row 42, whose barriers leave the memory idle).
+  const bool plain = !c.top_k && !c.top_p && !c.min_p;
   int C = 1;
-  while (C < 8 && ((size_t)((c.vocab + C - 1) / C) * entry > most || ((int64_t)rows * C < 152 && c.vocab / C > 8192))) C *= 2;
+  while (C < 8 && (plain ? (int64_t)rows * C * 2 <= 304 && c.vocab / C > 8192
+                         : (size_t)((c.vocab + C - 1) / C) * sizeof(T) > 64 * 1024 || ((int64_t)rows * C < 152 && c.vocab / C > 8192)))
+    C *= 2;
   c.slice = (c.vocab + C - 1) / C;
   c.qbits = 31 - ceil_log2(c.slice > 32768 ? c.slice : 32768);
-  c.keep = (size_t)c.slice * entry > kResident ? 0 : kCut ? 1 : 2;
-  const size_t smem = (c.keep == 2 ? 0 : kBins * 4 + kList * 8) + (c.keep ? (size_t)c.slice * entry + 64 : 0);
-  const cudaError_t e = cudaFuncSetAttribute(k_sample<T, kCut>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             (int)(kBins * 4 + kList * 8 + kResident + 64));
-  if (e != cudaSuccess) return e;
+  const size_t bytes = (size_t)c.slice * sizeof(T);
+  c.keep = bytes <= kResident;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)rows * (unsigned)C);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = plain ? 0 : kBins * 4 + kList * 8 + (c.keep ? bytes + 64 : 0);
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim = {(unsigned)C, 1, 1};
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k_sample<T, kCut>, c);
+  cfg.numAttrs = 2;
+  if (plain) return cudaLaunchKernelEx(&cfg, k_sample_plain<T>, c);
+  const cudaError_t e = cudaFuncSetAttribute(k_sample<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)(kBins * 4 + kList * 8 + kResident + 64));
+  return e == cudaSuccess ? cudaLaunchKernelEx(&cfg, k_sample<T>, c) : e;
 }
 
 }  // namespace
@@ -764,10 +913,8 @@ extern "C" int mf_sample(const mf_sample_args_t* a, void* stream) {
   SampleCall c = {a->logits, a->noise, a->temperature, a->top_p, a->min_p, a->top_k, a->token, a->logprob,
                   a->logits_stride, a->noise_stride, a->vocab, 0, 0, 0};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const bool cut = a->top_k || a->top_p;
-  const int n = a->n_rows;
-  const cudaError_t e = a->dtype == MF_F32   ? (cut ? run<float, true>(c, n, s) : run<float, false>(c, n, s))
-                        : a->dtype == MF_F16 ? (cut ? run<__half, true>(c, n, s) : run<__half, false>(c, n, s))
-                                             : (cut ? run<__nv_bfloat16, true>(c, n, s) : run<__nv_bfloat16, false>(c, n, s));
+  const cudaError_t e = a->dtype == MF_F32   ? run<float>(c, a->n_rows, s)
+                        : a->dtype == MF_F16 ? run<__half>(c, a->n_rows, s)
+                                             : run<__nv_bfloat16>(c, a->n_rows, s);
   return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_sample");
 }
