@@ -436,8 +436,8 @@ int mf_kv_bytes(const mf_attn_shape_t* shape, int n_layers, int64_t n_tokens, in
 
 /* The workspace of attention calls of one shape on CUDA device `device`: steps of at most max_seqs
  * sequences and max_tokens new tokens.  One handle serves all layers.  Its calls must follow one another (one stream, or ordered by
- * events): they share the workspace.  MF_E_INVAL for an invalid shape or a size below 1; MF_E_OOM when
- * the workspace cannot be allocated. */
+ * events): they share the workspace.  MF_E_INVAL for an invalid shape, a size below 1 or more than
+ * 2^30 tokens times heads of a group; MF_E_OOM when the workspace cannot be allocated. */
 int mf_attn_create(mf_attn_t** out, const mf_attn_shape_t* shape, int max_seqs, int max_tokens, int device);
 
 /* Rotate the step's q (into q_out) and k by position and store k and v into their lines of the cache,

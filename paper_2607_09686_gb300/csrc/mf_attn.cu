@@ -227,6 +227,7 @@ extern "C" int mf_attn_create(mf_attn_t** out, const mf_attn_shape_t* shape, int
   if (!out) return MF_E_INVAL;
   *out = nullptr;
   if (!shape_ok(shape) || max_seqs < 1 || max_tokens < 1 || device < 0) return MF_E_INVAL;
+  if ((int64_t)max_tokens * (shape->n_heads / shape->n_kv_heads) > (1 << 30)) return MF_E_INVAL;  // rows are counted in 32 bits
   OnDevice on(device);
   if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
   mf_attn_t* h = new (std::nothrow) mf_attn_t();

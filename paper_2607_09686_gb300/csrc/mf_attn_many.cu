@@ -50,6 +50,8 @@ struct Cfg {
   static constexpr int kRowTiles = D == 256 ? 1 : 2;  // row tiles of a segment
   static constexpr int kRows = kRowTiles * 128;
   static constexpr uint32_t kQBytes = kRowTiles * kU * kUnitBytes;
+  // jobs that a segment's beginning and end cost (first scores without a product beside them, O to memory)
+  static constexpr int kOver = kRowTiles == 2 ? 4 : 2;
   static constexpr uint32_t kTail = kQBytes + (kKSlots + kVSlots) * kSlotBytes;  // then a Tail
 };
 constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;
@@ -113,7 +115,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan(AttnCall c, AttnPlan p) {
       const int end = max(0, vis_hi(c, first + (R0 + rows - 1) / G, sp.len));
       p.tile[2 * i] = make_int4(lo, sp.q0, sp.n, sp.len);
       p.tile[2 * i + 1] = make_int4(qt, rows, start, end);
-      n = (int64_t)max(1, (end - start + kKeys - 1) / kKeys) << (Cfg<D>::kRowTiles == 2 && rows > 128);
+      n = ((int64_t)max(1, (end - start + kKeys - 1) / kKeys) << (Cfg<D>::kRowTiles == 2 && rows > 128)) + Cfg<D>::kOver;
     }
     int64_t all;
     const int64_t at = jobs + scan(n, all);
@@ -127,6 +129,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan(AttnCall c, AttnPlan p) {
 // ordered by sequence, kv head, row tile.  The next tile's description is asked for when the walk comes to a segment, and
 // has long arrived when the segment ends.  The roles' loops together have to fit the instruction cache (with walks that
 // looked everything up inline, two fifths of the fetches missed and a job took five times as long).
+template <int kRows, int kOver>
 struct Walk {
   int s, q0, n, len;          // the sequence: new tokens, lines
   int qt, rows, start, end;   // the row tile: its place, rows, lines that any of them sees
@@ -140,38 +143,38 @@ struct Walk {
     s = a.x, q0 = a.y, n = a.z, len = a.w, qt = b.x, rows = b.y, start = b.z, end = b.w;
     two = rows > 128;
     nt = max(1, (end - start + kKeys - 1) / kKeys);
-    // a key tile belongs to the block that its first job falls to
-    const int64_t up0 = (t0 - at + two) >> two, up1 = (t1 - at + two) >> two;
+    // a key tile belongs to the block that its first job falls to; the segment's kOver come before its jobs
+    const int64_t up0 = (t0 - at - kOver + two) >> two, up1 = (t1 - at - kOver + two) >> two;
     j0 = (int)max((int64_t)0, up0);
     j1 = (int)min((int64_t)nt, up1);
   }
   // the tile after this one in the list (of this kv head or the next)
-  __device__ __forceinline__ int following(const AttnCall& c, int tile_rows) const {
-    return (qt + 1) * tile_rows >= n * c.st.G && h + 1 < c.st.Hkv ? tile - qt : tile + 1;
+  __device__ __forceinline__ int following(const AttnCall& c) const {
+    return (qt + 1) * kRows >= n * c.st.G && h + 1 < c.st.Hkv ? tile - qt : tile + 1;
   }
-  __device__ __forceinline__ void ask(const AttnCall& c, const AttnPlan& p, int tile_rows) {
-    const int f = min(following(c, tile_rows), p.max_tiles - 1);  // (past the last tile: anything, not used)
+  __device__ __forceinline__ void ask(const AttnCall& c, const AttnPlan& p) {
+    const int f = min(following(c), p.max_tiles - 1);  // (past the last tile: anything, not used)
     na = __ldg(p.tile + 2 * f), nb = __ldg(p.tile + 2 * f + 1);
   }
-  __device__ __forceinline__ void next(const AttnCall& c, const AttnPlan& p, int tile_rows) {
+  __device__ __forceinline__ void next(const AttnCall& c, const AttnPlan& p) {
 #pragma unroll 1
     do {
-      at += (int64_t)nt << two;
+      at += ((int64_t)nt << two) + kOver;
       if (at >= t1) {
         more = false;
         return;
       }
-      const int f = following(c, tile_rows);
-      if ((qt + 1) * tile_rows >= n * c.st.G) h = f > tile ? 0 : h + 1;
+      const int f = following(c);
+      if ((qt + 1) * kRows >= n * c.st.G) h = f > tile ? 0 : h + 1;
       tile = f;
       set(na, nb);
-      ask(c, p, tile_rows);
+      ask(c, p);
     } while (j0 >= j1);
   }
 };
 // to the block's first segment
-__device__ __noinline__ void walk_start(Walk& w, const AttnCall& c, const AttnPlan& p, int tiles, int tile_rows, int64_t a,
-                                        int64_t b) {
+template <int kRows, int kOver>
+__device__ __noinline__ void walk_start(Walk<kRows, kOver>& w, const AttnCall& c, const AttnPlan& p, int tiles, int64_t a, int64_t b) {
   w.t0 = a, w.t1 = b;
   w.more = a < b;
   if (!w.more) return;
@@ -196,15 +199,16 @@ __device__ __noinline__ void walk_start(Walk& w, const AttnCall& c, const AttnPl
   w.tile = lo;
   w.at = head + __ldg(p.before + lo) - b0;
   w.set(__ldg(p.tile + 2 * lo), __ldg(p.tile + 2 * lo + 1));
-  w.ask(c, p, tile_rows);
-  if (w.j0 >= w.j1) w.next(c, p, tile_rows);
+  w.ask(c, p);
+  if (w.j0 >= w.j1) w.next(c, p);
 }
 
 // The jobs of the walk one by one: (key tile, row tile), row tile inner.
 struct Jobs {
   int i, n, two;  // job in its segment, of n; two row tiles
   bool live;
-  __device__ __forceinline__ void take(const Walk& w) {
+  template <class W>
+  __device__ __forceinline__ void take(const W& w) {
     live = w.more;
     i = 0;
     two = w.two;
@@ -220,10 +224,11 @@ struct Jobs {
 struct Piece {
   int nj, two, k_start, R0, rows, h, q0, first, len, nt, j0, more;
   int64_t last;  // place of the last key tile's first job
-  __device__ __forceinline__ void take(const Walk& w, int tile_rows) {
-    more = w.more, two = w.two, nj = w.j1 - w.j0, k_start = w.start + w.j0 * kKeys, R0 = w.qt * tile_rows, rows = w.rows;
+  template <int kRows, int kOver>
+  __device__ __forceinline__ void take(const Walk<kRows, kOver>& w) {
+    more = w.more, two = w.two, nj = w.j1 - w.j0, k_start = w.start + w.j0 * kKeys, R0 = w.qt * kRows, rows = w.rows;
     h = w.h, q0 = w.q0, first = w.len - w.n, len = w.len, nt = w.nt, j0 = w.j0;
-    last = w.at + ((int64_t)(nt - 1) << two);
+    last = w.at + kOver + ((int64_t)(nt - 1) << two);
   }
 };
 
@@ -580,10 +585,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     // there one by one they cost as much as the products).
     auto uniform = [](uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); };
     const uint32_t bars0 = uniform(smem_u32(bars)), tm = uniform(tmem);
-    Walk w0;
-    walk_start(w0, c, p, tiles, C::kRows, t0, t1);
-    Walk w = w0;
-    Jobs jb;
+    Walk<C::kRows, C::kOver> w0;
+    walk_start(w0, c, p, tiles, t0, t1);
+    Walk<C::kRows, C::kOver> w = w0;
+    Jobs jb{};
     jb.take(w);
     uint32_t slot = 0, sph = 0, buf = 0, g = 0;  // next ring slot and its phase, buffer of S and P, job
     if (warp == kQkWarp) {
@@ -636,7 +641,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         }
         if (!ok) break;
         if (++jb.i == jb.n) {
-          w.next(c, p, C::kRows);
+          w.next(c, p);
           jb.take(w);
         }
       }
@@ -704,7 +709,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         }
         if (!ok) break;
         if (++jb.i == jb.n) {
-          w.next(c, p, C::kRows);
+          w.next(c, p);
           jb.take(w);
         }
       }
@@ -745,15 +750,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
       announce(false);
       pending = bar;
     };
-    Walk w0;
-    walk_start(w0, c, p, tiles, C::kRows, t0, t1);
-    Walk w = w0;
+    Walk<C::kRows, C::kOver> w0;
+    walk_start(w0, c, p, tiles, t0, t1);
+    Walk<C::kRows, C::kOver> w = w0;
     int told = 0;
     uint32_t tph = 1;
     auto tell = [&]() -> bool {  // the softmax what comes
       if (!wait_free(kBPieceFree + told, tph)) return false;
       if (lane == 0) {
-        tail.piece[told].take(w, C::kRows);
+        tail.piece[told].take(w);
         mbar_arrive(&bars[kBPiece + told]);
       }
       __syncwarp();
@@ -761,7 +766,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
       return true;
     };
 #pragma unroll 1
-    for (; w.more && ok; w.next(c, p, C::kRows)) {
+    for (; w.more && ok; w.next(c, p)) {
       if (is_k && !(ok = tell())) break;
       if (is_k) {  // the segment's rows of q
         if (!(ok = wait_free(kBQFree, seg_ph))) break;

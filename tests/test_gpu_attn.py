@@ -167,6 +167,43 @@ def test_other_stream_and_graph(mf):
     mf.mf_attn_destroy(at)
 
 
+@pytest.mark.parametrize("new", [1, 70])
+def test_step_in_a_graph(mf, new):
+    """Append and attention captured together after other work, replayed with other lengths and tokens."""
+    c = ref.Case([new, new], [300, 20], 8, 2, 128)
+    at, cache, step = c.attn(mf), mf.kv_cache(c.k, c.v), c.step(mf)
+    out = torch.empty(c.tokens, 8, 128, dtype=c.q.dtype, device="cuda")
+    noise = torch.randn_like(c.new_k)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+
+    def body():
+        c.new_k.add_(noise)  # (another kernel, and a copy, before)
+        c.new_v.copy_(noise)
+        mf.mf_kv_append(at, cache, step, c.new_k, c.new_v)
+        mf.mf_attn_forward(at, cache, step, c.q, out, scale=0.1)
+
+    with torch.cuda.stream(s):
+        body()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            body()
+        full = list(c.lines)
+        for lens in (c.len, [new + 77, new], [new + 300, new + 1]):
+            c.kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+            g.replay()
+            c.len = lens
+            c.lines = [(a[:n], b[:n]) for (a, b), n in zip(full, lens)]
+            want, _, tol, _ = ref.attention64(c, 0.1)
+            s.synchronize()
+            for i, (pg, ln) in enumerate(c.lines):
+                rows = slice(c.start[i], c.start[i + 1])
+                assert torch.equal(c.k[pg[-new:], ln[-new:]], c.new_k[rows]) and torch.equal(c.v[pg[-new:], ln[-new:]], c.new_v[rows])
+            assert ((out.double() - want).abs() <= tol).all()
+    assert mf.mf_attn_check(at) == 0
+    mf.mf_attn_destroy(at)
+
+
 def test_same_bits_every_time(mf):
     for new, ctx in (([1] * 4, [3000, 7, 900, 64]), ([40, 200], [1000, 3])):
         c = ref.Case(new, ctx, 8, 2, 128)

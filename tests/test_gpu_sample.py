@@ -186,6 +186,38 @@ def test_frequencies(mf):
         assert abs(got.count(i) - n * p[i]) <= 5 * math.sqrt(n * p[i] * (1 - p[i]))
 
 
+@pytest.mark.parametrize("dtype", DT)
+def test_largest_vocabulary(mf, dtype):
+    """2^20 entries: slices that do not fit shared memory, settings that take every path."""
+    v = 1 << 20
+    g = torch.Generator("cuda").manual_seed(21)
+    x = (torch.randn(5, v, device="cuda", generator=g) * 3).to(dtype)
+    check(mf, x, gumbel(5, v), t=[1.0, 0.7, 0.0, 1.0, 1.0], k=[0, 40, 3, 60000, 0], p=[1.0, 0.9003, 0.5, 1.0, 0.3003], mp=[0.0, 0.0, 0.0, 0.0, 0.01])
+
+
+def test_in_a_graph(mf):
+    """Captured after another kernel, replayed with other logits and settings."""
+    x, noise = torch.randn(4, 5003, device="cuda") * 2, gumbel(4, 5003)
+    base, token = x.clone(), torch.empty(4, dtype=torch.int32, device="cuda")
+    k = torch.tensor([0, 50, 7, 1000], dtype=torch.int32, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        def body():
+            torch.mul(base, 1.5, out=x)
+            mf.mf_sample(x, noise, token, top_k=k)
+        body()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            body()
+        for seed in range(3):
+            base.copy_(torch.randn(4, 5003, device="cuda", generator=torch.Generator("cuda").manual_seed(seed)))
+            k.copy_(torch.tensor([seed, 50, 7, 1000]))
+            g.replay()
+            s.synchronize()
+            assert token.tolist() == run(mf, base * 1.5, noise, k=k.tolist())[0]
+
+
 def test_same_every_time(mf):
     x, noise = (torch.randn(64, 50001, device="cuda") * 2).bfloat16(), gumbel(64, 50001)
     a = run(mf, x, noise, t=0.9, k=0, p=0.95)
