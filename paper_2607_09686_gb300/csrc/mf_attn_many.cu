@@ -51,7 +51,7 @@ struct Cfg {
   static constexpr int kRows = kRowTiles * 128;
   static constexpr uint32_t kQBytes = kRowTiles * kU * kUnitBytes;
   // jobs that a segment's beginning and end cost (first scores without a product beside them, O to memory)
-  static constexpr int kOver = kRowTiles == 2 ? 4 : 2;
+  static constexpr int kOver = 4;
   static constexpr uint32_t kTail = kQBytes + (kKSlots + kVSlots) * kSlotBytes;  // then a Tail
 };
 constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;
