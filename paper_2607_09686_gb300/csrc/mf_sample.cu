@@ -33,8 +33,9 @@ namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxVocab = 1 << 20;
-constexpr int kBins = 2048, kList = 4096, kShort = 256;
+constexpr int kBins = 2048, kList = 4096, kShort = 512;
 constexpr float kBinsPerUnit = 64.f;
+constexpr size_t kListAt = (kBins + 4) * 4, kRowAt = kListAt + kList * 8;  // bytes of shared memory before the list, the row
 constexpr size_t kResident = 128 * 1024;  // bytes of a slice that are kept in shared memory
 
 struct SampleCall {
@@ -57,10 +58,12 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
 __device__ __forceinline__ float z_of(float x, float m, float t) { return x == m ? 0.f : __fdiv_rn(x - m, t); }
-// bin of an entry `d` = x - M; monotonic in d (inv: bins per unit of d)
-__device__ __forceinline__ int bin_of(float d, float inv) {
-  return d == 0.f ? 0 : (int)fminf(-d * inv, (float)(kBins - 1));  // (inv may be infinite)
+// bin of an entry `d` = x - M, the nearest of those at multiples of 1/64 in z; monotonic in d (inv: bins per unit of d).
+// Rounded by adding 2^23: conversions share a slow pipe with ex2.
+__device__ __forceinline__ float bin_at(float d, float inv) {
+  return (d == 0.f ? 0.f : fminf(-d * inv, (float)(kBins - 1))) + 8388608.f;  // (inv may be infinite)
 }
+__device__ __forceinline__ int bin_of(float d, float inv) { return (int)(__float_as_uint(bin_at(d, inv)) & (kBins - 1)); }
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -87,7 +90,7 @@ struct Shared {
   float above, goal;
   int bin, count;             // border bin (-1: nothing is cut), entries down to it
   unsigned listed, kmin, kmax;  // entries put on the list, and their keys' range
-  unsigned mine;                // of this block
+  unsigned place;               // of this block's entries on the leading block's list
   uint32_t key;
   int index;
   int here;
@@ -102,7 +105,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank(), r = blockIdx.x / C;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   uint32_t* hist = reinterpret_cast<uint32_t*>(dyn);
-  unsigned long long* list = reinterpret_cast<unsigned long long*>(dyn + kBins * 4);
+  unsigned long long* list = reinterpret_cast<unsigned long long*>(dyn + kListAt);
   const int base = rank * c.slice, n = max(0, min(c.slice, c.vocab - base));
   const T* row = static_cast<const T*>(c.logits) + (int64_t)r * c.logits_stride + base;
   const float* noise = c.noise + (int64_t)r * c.noise_stride + base;
@@ -115,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   const T* src = row;
   bool lost = false;  // a copy did not arrive in time: the row has no answer (as if it had no entry)
   if (c.keep) {
-    T* x0 = reinterpret_cast<T*>(dyn + kBins * 4 + kList * 8 + ((uintptr_t)row & 15));
+    T* x0 = reinterpret_cast<T*>(dyn + kRowAt + ((uintptr_t)row & 15));
     const int head = min(n, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T)),
               body = (n - head) * (int)sizeof(T) / 16 * 16 / (int)sizeof(T);
     if (tid == 0) {
@@ -156,6 +159,54 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       for (int i = tid; i < n; i += kThreads) f(i, up(row[i]));
     }
   };
+  // Those from lo to hi (a bound that is no number bounds nothing), where they are few: of 64 entries at a time a thread's are
+  // picked out first, then taken four by four, with what get() loads for them under way together.
+  auto for_some = [&](float lo, float hi, auto&& get, auto&& f) {
+    auto within = [&](float x) { return !(x < lo) && !(x > hi); };
+    if (c.keep) {
+      constexpr int kV = 16 / sizeof(T), kGroup = 64 / kV;
+      const int lead_in = (int)(((uintptr_t)src & 15) / sizeof(T)), total = lead_in + n;
+      const T* from = src - lead_in;
+      for (int v0 = tid; v0 * kV < total; v0 += kGroup * kThreads) {
+        uint32_t some[2] = {0, 0};
+#pragma unroll
+        for (int g = 0; g < kGroup; ++g) {
+          const int v = v0 + g * kThreads;
+          if (v * kV >= total) break;
+          const uint4 q = reinterpret_cast<const uint4*>(from)[v];
+          const T* e = reinterpret_cast<const T*>(&q);
+#pragma unroll
+          for (int u = 0; u < kV; ++u) some[g * kV / 32] |= (uint32_t)within((float)e[u]) << (g * kV % 32 + u);
+        }
+        unsigned long long left = (unsigned long long)some[1] << 32 | some[0];
+        while (left) {
+          int at[4];
+          float x[4], y[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int bit = __ffsll((long long)left) - 1;
+            at[u] = left ? (v0 + (bit / kV) * kThreads) * kV + bit % kV - lead_in : -1;
+            left &= left - 1;
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            if (at[u] >= n) at[u] = -1;
+            x[u] = at[u] >= 0 ? up(src[at[u]]) : 0.f;
+            y[u] = at[u] >= 0 ? get(at[u]) : 0.f;
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u)
+            if (at[u] >= 0) f(at[u], x[u], y[u]);
+        }
+      }
+    } else {
+      for (int i = tid; i < n; i += kThreads) {
+        const float x = up(row[i]);
+        if (within(x)) f(i, x, get(i));
+      }
+    }
+  };
+  auto get_none = [](int) { return 0.f; };
   float mx = -INFINITY;
   for_each([&](int, float x) { mx = fmaxf(mx, x); });
   const float own_max = mx;
@@ -229,24 +280,39 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     }
     return before + x - v;
   };
-  // counts (or masses, in units of 2^-qbits) of the kept entries by bin, or counts of the threads' maxima; the leading block finds the first bin down to
-  // which they reach `want` (mass: want * their total); then lead->bin, above, goal, and for counts count.  Counts are whole
-  // numbers below 2^24: exact in fp32.
+  // Counts (or masses, in units of 2^-qbits) of the kept entries by bin, or counts of the threads' maxima; the leading block finds
+  // the first bin down to which they reach `want` (mass: want * their total), and tells all blocks: bin, above, goal, and for
+  // counts count.  Counts are whole numbers below 2^24: exact in fp32.
+  // Masses: entries of less than (1 - want) / vocab of the largest one's cannot hold the border, whatever they are together;
+  // theirs is summed in units of 2^-30 (hist[kBins]) and joins the total alone.
   enum { kCounts, kMasses, kMaxima };
   auto find_bin = [&](int what, float want) {
     const bool mass = what == kMasses;
-    for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
+    for (int i = tid; i <= kBins; i += kThreads) hist[i] = 0;
     __syncthreads();
     const float unit = (float)(1 << c.qbits);
     if (what == kMaxima) {
       if (own_max > -INFINITY) atomicAdd(hist + bin_of(own_max == m ? 0.f : own_max - m, inv), 1u);
+    } else if (mass) {
+      float low = xc;
+      if (xc == -INFINITY) {
+        low = m + t * (logf((1.f - want) / (float)c.vocab) - 0.01f) - 1e-6f * fabsf(m);
+        const float inv_e = 1.4426950408889634f / t;
+        float rest = 0.f;
+        for_each([&](int, float x) { rest += x < low ? ex2((x - m) * inv_e) : 0.f; });
+        rest = warp_sum(rest);
+        if (lane == 0) atomicAdd(hist + kBins, (uint32_t)(fminf(rest, 1.f) * 1073741824.f / (float)(kWarps) + 0.5f));
+      }
+      for_some(low, INFINITY, get_none, [&](int i, float x, float) {
+        if (!kept(x, base + i)) return;
+        const float d = x == m ? 0.f : x - m, at = bin_at(d, inv);
+        // (w against that at the bin's middle: near 1)
+        const float w = d == 0.f ? 1.f : ex2(fmaf(d, inv, at - 8388608.f) * (1.4426950408889634f / kBinsPerUnit));
+        atomicAdd(hist + (__float_as_uint(at) & (kBins - 1)), __float_as_uint(fmaf(w, unit, 8388608.f)) & 0x7FFFFFu);
+      });
     } else {
       for_each([&](int i, float x) {
-        if (!kept(x, base + i)) return;
-        const float d = x == m ? 0.f : x - m;
-        const int b = bin_of(d, inv);
-        // (w of the bin's upper end is e^(-bin / 64): what is left is below 1)
-        atomicAdd(hist + b, mass ? (uint32_t)((d == 0.f ? 1.f : __expf((d * inv + (float)b) * (1.f / kBinsPerUnit))) * unit + 0.5f) : 1u);
+        if (kept(x, base + i)) atomicAdd(hist + bin_of(x == m ? 0.f : x - m, inv), 1u);
       });
     }
     cl.sync();
@@ -258,6 +324,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
 #pragma unroll
       for (int q = 0; q < 8; ++q)
         h[q] = q < C ? reinterpret_cast<const uint4*>(cl.map_shared_rank(hist, q))[tid] : make_uint4(0, 0, 0, 0);
+      const float rest = mass ? warp_sum(lane < C ? (float)cl.map_shared_rank(hist, lane)[kBins] : 0.f) * ((float)kWarps / 1073741824.f) : 0.f;
       unsigned long long s[kPer] = {0, 0, 0, 0};
 #pragma unroll
       for (int q = 0; q < 8; ++q) s[0] += h[q].x, s[1] += h[q].y, s[2] += h[q].z, s[3] += h[q].w;
@@ -269,62 +336,95 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       }
       if (tid == 0) sh.bin = -1;
       float at = block_scan(sum, total);
-      const float goal = mass ? want * total : want;
+      const float goal = mass ? want * (total + rest * unit) : want;
 #pragma unroll
       for (int u = 0; u < kPer; ++u) {
         if (at < goal && at + v[u] >= goal) sh.bin = tid * kPer + u, sh.above = at, sh.count = (int)(at + v[u]);
         at += v[u];
       }
       if (tid == 0) sh.goal = goal;
+      __syncthreads();
+      if (warp == 0 && lane > 0 && lane < C) {
+        Shared* o = cl.map_shared_rank(&sh, lane);
+        o->bin = sh.bin, o->above = sh.above, o->count = sh.count, o->goal = sh.goal;
+      }
     }
     cl.sync();
   };
-  // the kept entries of bins lo .. hi onto the leading block's list (as many as there is room for; all are counted): each
-  // block collects its own first, so that only whole runs and one counter cross to the leading block
-  auto gather = [&](int lo, int hi, float floor) {  // (or, lo < 0: the entries from `floor` on)
-    unsigned kmin = 0xFFFFFFFFu, kmax = 0;
-    if (tid == 0) sh.mine = 0;
+  // The entries from `lo` to `hi` that are wanted onto the leading block's list (as many as there is room for; all are
+  // counted), in no certain order: each block collects its own first, so that whole runs and one counter cross to the leading
+  // block.  kmin, kmax: the range of their keys.
+  auto gather = [&](float lo, float hi, auto&& wanted) {
+    if (rank != 0 && tid == 0) sh.listed = 0, sh.kmin = 0xFFFFFFFFu, sh.kmax = 0;
     __syncthreads();
-    for_each([&](int i, float x) {
-      if (lo < 0) {
-        if (x < floor) return;
-      } else {
-        const int b = bin_of(x == m ? 0.f : x - m, inv);
-        if (b < lo || b > hi || !kept(x, base + i)) return;
+    if (!(own_max < lo)) {
+      unsigned kmin = 0xFFFFFFFFu, kmax = 0;
+      for_some(lo, hi, get_none, [&](int i, float x, float) {
+        if (!wanted(x, base + i)) return;
+        const uint32_t k = order_key(x);
+        const unsigned at = atomicAdd(&sh.listed, 1u);
+        if (at < kList) list[at] = (unsigned long long)k << 32 | (0xFFFFFFFFu - (unsigned)(base + i));
+        kmin = min(kmin, k), kmax = max(kmax, k);
+      });
+      if (kmax) atomicMin(&sh.kmin, kmin), atomicMax(&sh.kmax, kmax);
+    }
+    __syncthreads();
+    const unsigned own = sh.listed;
+    if (rank != 0 && own) {
+      if (tid == 0) {
+        sh.place = atomicAdd(&lead->listed, own);
+        atomicMin(&lead->kmin, sh.kmin), atomicMax(&lead->kmax, sh.kmax);
       }
-      const uint32_t k = order_key(x);
-      const unsigned at = atomicAdd(&sh.mine, 1u);
-      if (at < kList) list[at] = (unsigned long long)k << 32 | (0xFFFFFFFFu - (unsigned)(base + i));
-      kmin = min(kmin, k), kmax = max(kmax, k);
-    });
-    kmin = __reduce_min_sync(0xffffffffu, kmin), kmax = __reduce_max_sync(0xffffffffu, kmax);
-    if (lane == 0 && kmax) atomicMin(&lead->kmin, kmin), atomicMax(&lead->kmax, kmax);
-    __syncthreads();
-    const unsigned own = sh.mine;
-    cl.sync();
-    // every block's place follows from the others' numbers: the same whatever the order of execution
-    const unsigned num = lane < C ? cl.map_shared_rank(&sh, lane)->mine : 0u;
-    const unsigned before = __reduce_add_sync(0xffffffffu, lane < rank ? num : 0u), total = __reduce_add_sync(0xffffffffu, num);
-    if (rank != 0)
-      for (unsigned i = tid; i < own && before + i < kList; i += kThreads) lead_list[before + i] = list[i];
-    if (rank == 0 && tid == 0) sh.listed = total;
+      __syncthreads();
+      for (unsigned i = tid; i < own && sh.place + i < kList; i += kThreads) lead_list[sh.place + i] = list[i];
+    }
     cl.sync();
   };
-  // the leading block's list sorted: keys falling, indices rising
+  // The leading block's list sorted: keys falling, indices rising.  Bitonic; entries up to 64 apart meet in the registers of a
+  // warp that has 128, without barriers.
   auto sort_list = [&](int len) {
-    int p2 = 1;
+    int p2 = 128;
     while (p2 < len) p2 <<= 1;
+    __syncthreads();
     for (int i = len + tid; i < p2; i += kThreads) list[i] = 0;
-    for (int k = 2; k <= p2; k <<= 1)
-      for (int j = k >> 1; j; j >>= 1) {
-        __syncthreads();
+    __syncthreads();
+    for (int k = 128; k <= p2; k <<= 1) {
+      for (int j = k >> 1; j > 64; j >>= 1) {
         for (int i = tid; i < p2 / 2; i += kThreads) {
           const int a = 2 * i - (i & (j - 1)), b = a + j;
           const unsigned long long x = list[a], y = list[b];
           if ((x < y) == ((a & k) == 0)) list[a] = y, list[b] = x;
         }
+        __syncthreads();
       }
-    __syncthreads();
+      for (int at = warp * 128 + lane * 4; at < p2; at += kWarps * 128) {  // four neighbours a lane
+        ulonglong2* mine = reinterpret_cast<ulonglong2*>(list + at);
+        const ulonglong2 lo = mine[0], hi = mine[1];
+        unsigned long long e[4] = {lo.x, lo.y, hi.x, hi.y};
+        auto meet = [&](int u, int w, bool fall) {
+          const unsigned long long x = e[u], y = e[w];
+          if ((x < y) == fall) e[u] = y, e[w] = x;
+        };
+        if (k == 128) meet(0, 1, true), meet(2, 3, false);
+        for (int k2 = k == 128 ? 4 : k; k2 <= k; k2 <<= 1) {
+          const bool fall = (at & k2) == 0;
+          for (int j = min(k2 >> 1, 64); j > 2; j >>= 1) {
+            const bool larger = fall == ((at & j) == 0);  // this lane keeps the larger ones
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const unsigned long long o = __shfl_xor_sync(0xffffffffu, e[u], j >> 2);
+              if ((e[u] < o) == larger) e[u] = o;
+            }
+          }
+          meet(0, 2, fall), meet(1, 3, fall), meet(0, 1, fall), meet(2, 3, fall);
+        }
+        mine[0] = make_ulonglong2(e[0], e[1]), mine[1] = make_ulonglong2(e[2], e[3]);
+      }
+      __syncthreads();
+    }
+  };
+  auto clear_list = [&]() {  // (after which a barrier of the cluster comes before the next gather: find_bin's)
+    if (rank == 0 && tid == 0) sh.listed = 0, sh.kmin = 0xFFFFFFFFu, sh.kmax = 0;
   };
   auto warp_best = [&](Best b) -> Best {
 #pragma unroll
@@ -435,23 +535,31 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     bool few = false;
     if (top_k <= kThreads * C / 2) {
       find_bin(kMaxima, (float)top_k);
-      if (lead->bin >= 0) {
+      if (sh.bin >= 0) {
         // the bin's lower end, a little lower for the rounding (more entries than needed do no harm)
-        const float low = m - (float)(lead->bin + 1) * (1.f / inv) * 1.00001f;
-        gather(-1, 0, lead->bin < kBins - 1 && low > -INFINITY ? low : -FLT_MAX);
+        const float low = m - ((float)sh.bin + 0.5f) * (1.f / inv) * 1.00001f;
+        gather(sh.bin < kBins - 1 && low > -INFINITY ? low : -FLT_MAX, INFINITY, [](float x, int) { return x > -INFINITY; });
         few = lead->listed <= kList;
-        cl.sync();
-        if (!few && rank == 0 && tid == 0) sh.listed = 0, sh.kmin = 0xFFFFFFFFu, sh.kmax = 0;
+        if (!few) {
+          cl.sync();
+          clear_list();
+        }
       }
     }
     if (!few) find_bin(kCounts, (float)top_k);
-    const int bin = lead->bin, above = bin < 0 ? 0 : (int)lead->above;
+    const int bin = sh.bin, above = bin < 0 ? 0 : (int)sh.above;
     if (bin >= 0) {
       if (!few) {
-        few = lead->count <= kList;
-        gather(few ? 0 : bin, bin, 0.f);
+        few = sh.count <= kList;
+        const int first = few ? 0 : bin;
+        gather(-INFINITY, INFINITY, [&](float x, int i) {
+          const int b = bin_of(x == m ? 0.f : x - m, inv);
+          return b >= first && b <= bin && kept(x, i);
+        });
       }
       if (few) {
+        // the other blocks are done: nothing of theirs is read any more, and the leading block waits for their last look at it
+        cl.barrier_arrive();
         if (rank == 0) {
           const int count = (int)sh.listed;
           sort_list(count);
@@ -485,7 +593,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
           b = block_best(b);
           if (tid == 0) answer(b, all);
         }
-        cl.sync();
+        cl.barrier_wait();
         return;
       }
       if (lead->listed <= kList) {
@@ -502,8 +610,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
         cut_by_key(false, (double)top_k, lead->kmin, lead->kmax);
       }
       cl.sync();
-      if (rank == 0 && tid == 0) sh.listed = 0, sh.kmin = 0xFFFFFFFFu, sh.kmax = 0;
+      clear_list();
     }
+  }
+  if (!greedy && tid == 0 && n > 0) {  // much of the noise will be asked for: into the L2 cache meanwhile
+    const uintptr_t a = ((uintptr_t)noise + 15) & ~uintptr_t(15), e = (uintptr_t)(noise + n) & ~uintptr_t(15);
+    if (e > a) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a), "r"((uint32_t)(e - a)) : "memory");
   }
   if (!greedy && top_p < 1.f) {
     // ---- 3. top-p
@@ -511,14 +623,13 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       xc = m;
       ic = -1;
     } else {
-      if (tid == 0 && n > 0) {  // most of the noise will be asked for: into the L2 cache meanwhile
-        const uintptr_t a = ((uintptr_t)noise + 15) & ~uintptr_t(15), e = (uintptr_t)(noise + n) & ~uintptr_t(15);
-        if (e > a) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a), "r"((uint32_t)(e - a)) : "memory");
-      }
       find_bin(kMasses, top_p);
-      const int bin = lead->bin;
+      const int bin = sh.bin;
       if (bin >= 0) {
-        gather(bin, bin, 0.f);
+        // the bin's ends, somewhat farther apart for the rounding
+        const float wide = 1e-5f * (float)(bin + 1) / inv + 1e-6f * fabsf(m);
+        gather(bin < kBins - 1 ? m - ((float)bin + 0.5f) / inv - wide : -INFINITY, m - ((float)bin - 0.5f) / inv + wide,
+               [&](float x, int i) { return bin_of(x == m ? 0.f : x - m, inv) == bin && kept(x, i); });
         const unsigned len = lead->listed;
         if (len <= kList) {
           if (rank == 0) {
@@ -645,53 +756,75 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     });
   } else {
     const float inv_t = 1.f / t, inv_e = inv_t * 1.4426950408889634f;
-    // (d, z as a product, whether the entry is in): w >= min_p is decided on the exact w where the product's comes near
-    auto in_with = [&](float x, int i, float& d, float& near, float& w) -> bool {
-      d = x == m ? 0.f : x - m;
+    // z as a product and w of an entry, and whether it is in: w >= min_p is decided on the exact w where the other comes near.
+    // (w is off by the rounding of z log2(e), by a few 2^-24 |z|, and by ex2's 2^-22.)
+    const float eps = 4e-7f * (8.f + fabsf(logf(fmaxf(min_p, FLT_MIN)))), p_hi = min_p * (1.f + eps), p_lo = min_p * (1.f - eps);
+    auto in_with = [&](float x, int i, float& near, float& w) -> bool {
+      const float d = x == m ? 0.f : x - m;
       near = d == 0.f ? 0.f : d * inv_t;
       w = d == 0.f ? 1.f : ex2(d * inv_e);
-      bool in = kept(x, i) && w >= min_p;
-      if (min_p > 0.f && fabsf(w - min_p) <= 1e-4f * min_p) in = kept(x, i) && expf(z_of(x, m, t)) >= min_p;
-      return in;
+      return kept(x, i) && w >= p_lo && (w >= p_hi || expf(z_of(x, m, t)) >= min_p);
     };
-    // sum of w; the largest key; the largest with its margin, that of the exact key: the two forms of a key differ by less
-    // than 1e-6 (|z| + |noise|), and 4e-6 is allowed for
-    float part = 0.f, top = -INFINITY, reach = -INFINITY;
-    auto add = [&](float near, float w, float g) {
-      const float key = near + g;
+    // sum of w; the largest key; the largest with its margin, that of the exact key (the two forms of a key differ by less
+    // than 1e-6 (|z| + |noise|), and 4e-6 is allowed for), whose it is, and the second largest of them
+    float part, top, reach, reach2;
+    int at;
+    auto clear = [&]() { part = 0.f, top = reach = reach2 = -INFINITY, at = -1; };
+    auto add = [&](float near, float w, float g, int i) {
+      const float key = near + g, far = fmaf(4e-6f, fabsf(near) + fabsf(g), key);
       part += w;
       top = fmaxf(top, key);
-      reach = fmaxf(reach, fmaf(4e-6f, fabsf(near) + fabsf(g), key));
+      reach2 = fmaxf(reach2, fminf(reach, far));
+      if (far > reach) reach = far, at = i;
     };
-    if (min_p > 0.f || m == INFINITY) {
-      for (int i = tid; i < n; i += kThreads) {
-        float d, near, w;
-        if (in_with(up(src[i]), base + i, d, near, w)) add(near, w, noise[i]);
-      }
-    } else {
+    clear();
+    // (the smallest x that may be in, somewhat less for the rounding)
+    const float low = fmaxf(xc, min_p > 0.f ? m + t * (logf(p_lo) - 1e-3f) - 1e-6f * fabsf(m) : -INFINITY);
+    const bool all = low == -INFINITY && m < INFINITY;  // nothing is cut
+    bool sure = m < INFINITY;
+    if (sure && !all) {  // (every pass gives a thread the same entries)
+      for_some(low, INFINITY, [&](int i) { return noise[i]; }, [&](int i, float x, float g) {
+        const float d = x - m, w = ex2(d * inv_e);
+        if (kept(x, base + i) && w >= p_lo) {
+          sure = sure && w >= p_hi;
+          add(d * inv_t, w, g, i);
+        }
+      });
+    } else if (sure) {
 #pragma unroll 8
       for (int i = tid; i < n; i += kThreads) {
         const float x = up(src[i]), d = x - m;
-        if (kept(x, base + i)) add(d * inv_t, ex2(d * inv_e), noise[i]);
+        if (x > -INFINITY) add(d * inv_t, ex2(d * inv_e), noise[i], i);
       }
     }
-    const float own_reach = reach;
+    if (!sure) {
+      clear();
+      for_some(low, INFINITY, [&](int i) { return noise[i]; }, [&](int i, float x, float g) {
+        float near, w;
+        if (in_with(x, base + i, near, w)) add(near, w, g, i);
+      });
+    }
     sum = cluster_sum(part, top);
     const float floor = top - 4e-6f * fabsf(top);
-    // the entries near the largest, in threads that have one (a reach or floor that is no number: in any)
-    if (!(own_reach < floor))
-#pragma unroll 4
-    for (int i = tid; i < n; i += kThreads) {
-      const float x = up(src[i]);
-      if (!kept(x, base + i)) continue;
-      float d, near, w;
-      d = x == m ? 0.f : x - m;
-      near = d == 0.f ? 0.f : d * inv_t;
-      const float g = fmaxf(noise[i], -INFINITY), key = near + g;
-      if (!(key >= top || !(key + 4e-6f * (fabsf(near) + fabsf(g)) < floor))) continue;
-      if (!in_with(x, base + i, d, near, w)) continue;
-      const float z = z_of(x, m, t);
-      b.take(z + g, z, base + i);
+    // the entries near the largest with z as the exact quotient: a thread has one at most, if its second is not near (a reach or
+    // floor that is no number: it looks at all)
+    if (!(reach2 < floor)) {
+      auto look = [&](int i, float x, float g) {
+        float near, w;
+        const bool in = in_with(x, base + i, near, w);
+        g = fmaxf(g, -INFINITY);
+        const float key = near + g;
+        if (!in || !(key >= top || !(key + 4e-6f * (fabsf(near) + fabsf(g)) < floor))) return;
+        const float z = z_of(x, m, t);
+        b.take(z + g, z, base + i);
+      };
+      if (all)
+        for (int i = tid; i < n; i += kThreads) look(i, up(src[i]), noise[i]);
+      else
+        for_some(low, INFINITY, [&](int i) { return noise[i]; }, look);
+    } else if (!(reach < floor)) {
+      const float z = z_of(up(src[at]), m, t);
+      b.take(z + noise[at], z, base + at);
     }
   }
   b = block_best(b);
@@ -880,7 +1013,7 @@ cudaError_t run(SampleCall c, int rows, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)rows * (unsigned)C);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = plain ? 0 : kBins * 4 + kList * 8 + (c.keep ? bytes + 64 : 0);
+  cfg.dynamicSmemBytes = plain ? 0 : kRowAt + (c.keep ? bytes + 64 : 0);
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -891,7 +1024,7 @@ cudaError_t run(SampleCall c, int rows, cudaStream_t s) {
   cfg.numAttrs = 2;
   if (plain) return cudaLaunchKernelEx(&cfg, k_sample_plain<T>, c);
   const cudaError_t e = cudaFuncSetAttribute(k_sample<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             (int)(kBins * 4 + kList * 8 + kResident + 64));
+                                             (int)(kRowAt + kResident + 64));
   return e == cudaSuccess ? cudaLaunchKernelEx(&cfg, k_sample<T>, c) : e;
 }
 
