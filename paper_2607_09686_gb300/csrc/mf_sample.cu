@@ -294,22 +294,22 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     if (what == kMaxima) {
       if (own_max > -INFINITY) atomicAdd(hist + bin_of(own_max == m ? 0.f : own_max - m, inv), 1u);
     } else if (mass) {
-      float low = xc;
-      if (xc == -INFINITY) {
-        low = m + t * (logf((1.f - want) / (float)c.vocab) - 0.01f) - 1e-6f * fabsf(m);
-        const float inv_e = 1.4426950408889634f / t;
-        float rest = 0.f;
-        for_each([&](int, float x) { rest += x < low ? ex2((x - m) * inv_e) : 0.f; });
-        rest = warp_sum(rest);
-        if (lane == 0) atomicAdd(hist + kBins, (uint32_t)(fminf(rest, 1.f) * 1073741824.f / (float)(kWarps) + 0.5f));
-      }
-      for_some(low, INFINITY, get_none, [&](int i, float x, float) {
-        if (!kept(x, base + i)) return;
-        const float d = x == m ? 0.f : x - m, at = bin_at(d, inv);
-        // (w against that at the bin's middle: near 1)
-        const float w = d == 0.f ? 1.f : ex2(fmaf(d, inv, at - 8388608.f) * (1.4426950408889634f / kBinsPerUnit));
-        atomicAdd(hist + (__float_as_uint(at) & (kBins - 1)), __float_as_uint(fmaf(w, unit, 8388608.f)) & 0x7FFFFFu);
+      const bool all = xc == -INFINITY;
+      const float low = all ? m + t * (logf((1.f - want) / (float)c.vocab) - 0.01f) - 1e-6f * fabsf(m) : xc;
+      const float inv_e = 1.4426950408889634f / t;
+      float rest = 0.f;
+      for_each([&](int i, float x) {
+        if (x < low) {
+          if (all) rest += ex2((x - m) * inv_e);
+        } else if (kept(x, base + i)) {
+          const float d = x == m ? 0.f : x - m, at = bin_at(d, inv);
+          // (w against that at the bin's middle: near 1)
+          const float w = d == 0.f ? 1.f : ex2(fmaf(d, inv, at - 8388608.f) * (1.4426950408889634f / kBinsPerUnit));
+          atomicAdd(hist + (__float_as_uint(at) & (kBins - 1)), __float_as_uint(fmaf(w, unit, 8388608.f)) & 0x7FFFFFu);
+        }
       });
+      rest = warp_sum(rest);
+      if (lane == 0 && rest > 0.f) atomicAdd(hist + kBins, (uint32_t)(fminf(rest, 1.f) * 1073741824.f / (float)(kWarps) + 0.5f));
     } else {
       for_each([&](int i, float x) {
         if (kept(x, base + i)) atomicAdd(hist + bin_of(x == m ? 0.f : x - m, inv), 1u);
@@ -380,12 +380,29 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     }
     cl.sync();
   };
-  // The leading block's list sorted: keys falling, indices rising.  Bitonic; entries up to 64 apart meet in the registers of a
-  // warp that has 128, without barriers.
+  // The leading block's list sorted: keys falling, indices rising.  A short one: each thread counts those before its entry (no
+  // two are equal).  Else bitonic; entries up to 64 apart meet in the registers of a warp that has 128, without barriers.
   auto sort_list = [&](int len) {
-    int p2 = 128;
-    while (p2 < len) p2 <<= 1;
     __syncthreads();
+    if (len <= kThreads) {
+      if (tid == 0) list[len] = 0;
+      __syncthreads();
+      const unsigned long long e = tid < len ? list[tid] : 0;
+      int before = 0;
+      if (warp * 32 < len) {
+#pragma unroll 4
+        for (int i = 0; i < len; i += 2) {
+          const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(list + i);
+          before += (int)(o.x > e) + (int)(o.y > e);
+        }
+      }
+      __syncthreads();
+      if (tid < len) list[before] = e;
+      __syncthreads();
+      return;
+    }
+    int p2 = 1024;
+    while (p2 < len) p2 <<= 1;
     for (int i = len + tid; i < p2; i += kThreads) list[i] = 0;
     __syncthreads();
     for (int k = 128; k <= p2; k <<= 1) {
