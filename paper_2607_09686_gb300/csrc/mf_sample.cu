@@ -857,9 +857,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
 // ---- rows by temperature alone: no entry is cut, so that one pass over logits and noise will do
 //
 // Each thread keeps the running maximum of its logits and its sum of w against that (scaled when the maximum grows), and of
-// its keys, with M / T left in (x / T + noise), the largest and the largest with its margin: rounding aside the keys' order
-// needs no M.  With the row's M known, only threads whose keys come near the largest look at their entries again, with z as the
-// exact quotient.  Bounded by reading logits and noise once, and by two cluster barriers a row.
+// its keys, with M / T left in (x / T + noise), the largest and the two largest with their margins: rounding aside the keys'
+// order needs no M.  With the row's M known, a thread whose key comes near the largest forms that one again, with z as the exact
+// quotient, or looks at all its entries where its second comes near too.  Bounded by reading logits and noise once, and by two cluster barriers a row.
 struct PlainShared {
   float m[kWarps], s[kWarps], top[kWarps];
   int i[kWarps];
@@ -884,8 +884,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_plain(SampleCall c) {
   const float t = greedy ? 1.f : temp, inv_t = 1.f / t, inv_e = inv_t * 1.4426950408889634f;
   auto up = [](T v) -> float { return fmaxf((float)v, -INFINITY); };  // NaN as -inf
   auto scaled = [&](float s, float from, float to) { return from == to ? s : s * ex2((from - to) * inv_e); };
-  float m = -INFINITY, s = 0.f, top = -INFINITY, reach = -INFINITY;
-  int first = 0x7FFFFFFF;  // of this thread's largest
+  float m = -INFINITY, s = 0.f, top = -INFINITY, reach = -INFINITY, reach2 = -INFINITY;
+  int first = 0x7FFFFFFF, at = 0;  // of this thread's largest, of its key with the largest reach
   auto add = [&](float x, float g, int i) {
     if (x > m) {
       s = scaled(s, m, x) + 1.f;
@@ -895,7 +895,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_plain(SampleCall c) {
     }
     const float near = x * inv_t, key = near + g;
     top = fmaxf(top, key);
-    reach = fmaxf(reach, fmaf(4e-6f, fabsf(near) + fabsf(g), key));
+    const float far = fmaf(4e-6f, fabsf(near) + fabsf(g), key);
+    reach2 = fmaxf(reach2, fminf(reach, far));
+    if (far > reach) reach = far, at = i;
   };
   constexpr int kU = 16;  // loads of an entry's logit and noise under way in each thread
   int i = tid;
@@ -911,7 +913,6 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_plain(SampleCall c) {
   if (m == -INFINITY) s = 0.f;
 
   // the block's, then the row's
-  const float own_reach = reach;
   auto join = [&](float& am, float& as, float& atop, int& ai, float bm, float bs, float btop, int bi) {
     const float to = fmaxf(am, bm);
     as = to == -INFINITY ? 0.f : scaled(as, am, to) + scaled(bs, bm, to);
@@ -960,7 +961,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_plain(SampleCall c) {
     }
   } else if (!greedy && m > -INFINITY) {
     const float slack = 4e-6f * fabsf(m * inv_t), floor = top - 4e-6f * fabsf(top) - slack;
-    if (!(own_reach + slack < floor))  // (no number: look)
+    if (!(reach2 + slack < floor)) {  // (no number: look)
       for (int k0 = tid; k0 < n; k0 += kU * kThreads) {
         float x[kU], g[kU];
 #pragma unroll
@@ -977,6 +978,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_plain(SampleCall c) {
           b.take(z + g[u], z, base + k0 + u * kThreads);
         }
       }
+    } else if (!(reach + slack < floor)) {
+      const float z = z_of(up(row[at - base]), m, t);
+      b.take(z + noise[at - base], z, at);
+    }
   }
   auto warp_best = [&](Best v) -> Best {
 #pragma unroll
