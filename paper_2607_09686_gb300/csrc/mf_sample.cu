@@ -791,8 +791,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       const float key = near + g, far = fmaf(4e-6f, fabsf(near) + fabsf(g), key);
       part += w;
       top = fmaxf(top, key);
-      reach2 = fmaxf(reach2, fminf(reach, far));
-      if (far > reach) reach = far, at = i;
+      const bool more = far > reach;
+      reach2 = fmaxf(reach2, more ? reach : far);
+      if (more) reach = far, at = i;
     };
     clear();
     // (the smallest x that may be in, somewhat less for the rounding)
@@ -886,31 +887,35 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_plain(SampleCall c) {
   auto scaled = [&](float s, float from, float to) { return from == to ? s : s * ex2((from - to) * inv_e); };
   float m = -INFINITY, s = 0.f, top = -INFINITY, reach = -INFINITY, reach2 = -INFINITY;
   int first = 0x7FFFFFFF, at = 0;  // of this thread's largest, of its key with the largest reach
-  auto add = [&](float x, float g, int i) {
-    if (x > m) {
-      s = scaled(s, m, x) + 1.f;
-      m = x, first = i;
-    } else {
-      s += x == m ? 1.f : ex2((x - m) * inv_e);
-    }
-    const float near = x * inv_t, key = near + g;
-    top = fmaxf(top, key);
-    const float far = fmaf(4e-6f, fabsf(near) + fabsf(g), key);
-    reach2 = fmaxf(reach2, fminf(reach, far));
-    if (far > reach) reach = far, at = i;
-  };
   constexpr int kU = 16;  // loads of an entry's logit and noise under way in each thread
-  int i = tid;
-  for (; i + (kU - 1) * kThreads < n; i += kU * kThreads) {
+  for (int k0 = tid; k0 < n; k0 += kU * kThreads) {
     T x[kU];
-    float g[kU];
+    float g[kU], most = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < kU; ++u) x[u] = row[i + u * kThreads], g[u] = noise[i + u * kThreads];
+    for (int u = 0; u < kU; ++u) {
+      const int k = k0 + u * kThreads;
+      x[u] = k < n ? row[k] : T(-INFINITY), g[u] = k < n ? noise[k] : 0.f;
+    }
 #pragma unroll
-    for (int u = 0; u < kU; ++u) add(up(x[u]), g[u], base + i + u * kThreads);
+    for (int u = 0; u < kU; ++u) most = fmaxf(most, up(x[u]));
+    if (most > m) {  // the sum is scaled once for all of them
+      s = m == -INFINITY ? 0.f : scaled(s, m, most);
+      m = most;
+#pragma unroll
+      for (int u = kU - 1; u >= 0; --u)
+        if ((float)x[u] == m) first = base + k0 + u * kThreads;
+    }
+    const float from = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const float v = up(x[u]), near = v * inv_t, key = near + g[u], far = fmaf(4e-6f, fabsf(near) + fabsf(g[u]), key);
+      s += ex2((v - from) * inv_e);
+      top = fmaxf(top, key);
+      const bool more = far > reach;
+      reach2 = fmaxf(reach2, more ? reach : far);
+      if (more) reach = far, at = base + k0 + u * kThreads;
+    }
   }
-  for (; i < n; i += kThreads) add(up(row[i]), noise[i], base + i);
-  if (m == -INFINITY) s = 0.f;
 
   // the block's, then the row's
   auto join = [&](float& am, float& as, float& atop, int& ai, float bm, float bs, float btop, int bi) {
