@@ -345,39 +345,66 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
     if (some) {
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
-        float sc[2][4];
+        if constexpr (kChains == 2)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[t][0][i >> 2][i & 3] += x[t][kChains - 1][i >> 2][i & 3];
+      }
+      // (step by step over all fragments: their chains of shuffles and exponentials run beside each other)
+      float f[MT][2], ms[MT][2];
+      bool grown = false;
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int line = line0 + n * 8 + (lane & 3) * 2 + (i & 1);
-            const float v = (kChains == 2 ? x[t][0][n][i] + x[t][kChains - 1][n][i] : x[t][0][n][i]) * scale;
-            sc[n][i] = line >= lo[t][i >> 1] && line < hi[t][i >> 1] ? v : -INFINITY;
+            float& v = x[t][0][n][i];
+            v = line >= lo[t][i >> 1] && line < hi[t][i >> 1] ? v * scale : -INFINITY;
           }
-        float f[2];
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          ms[t][u] = fmaxf(fmaxf(x[t][0][0][2 * u], x[t][0][0][2 * u + 1]), fmaxf(x[t][0][1][2 * u], x[t][0][1][2 * u + 1]));
+#pragma unroll
+      for (int d = 1; d <= 2; d <<= 1)
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) ms[t][u] = fmaxf(ms[t][u], __shfl_xor_sync(0xffffffffu, ms[t][u], d));
+#pragma unroll
+      for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          float mx = fmaxf(fmaxf(sc[0][2 * u], sc[0][2 * u + 1]), fmaxf(sc[1][2 * u], sc[1][2 * u + 1]));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-          const float mn = fmaxf(m[t][u], mx), ms = mn == -INFINITY ? 0.f : mn;
-          f[u] = ex2(m[t][u] - ms);
+          const float mn = fmaxf(m[t][u], ms[t][u]);
+          ms[t][u] = mn == -INFINITY ? 0.f : mn;
+          f[t][u] = ex2(m[t][u] - ms[t][u]);
           m[t][u] = mn;
+          grown |= f[t][u] != 1.f;
+        }
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
           float sum = 0.f;
 #pragma unroll
           for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) sum += sc[n][2 * u + i] = ex2(sc[n][2 * u + i] - ms);
-          l[t][u] = l[t][u] * f[u] + sum;
-        }
-        if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
-#pragma unroll
-          for (int i = 0; i < D / 8; ++i) o[t][i][0] *= f[0], o[t][i][1] *= f[0], o[t][i][2] *= f[1], o[t][i][3] *= f[1];
+            for (int i = 0; i < 2; ++i) sum += x[t][0][n][2 * u + i] = ex2(x[t][0][n][2 * u + i] - ms[t][u]);
+          l[t][u] = l[t][u] * f[t][u] + sum;
         }
         // the probabilities, rounded to the cache's type (an MMA multiplies equal types): the A operand's layout is
         // that of the scores
-        a[t][0] = Half2<T>::down(sc[0][0], sc[0][1]), a[t][1] = Half2<T>::down(sc[0][2], sc[0][3]);
-        a[t][2] = Half2<T>::down(sc[1][0], sc[1][1]), a[t][3] = Half2<T>::down(sc[1][2], sc[1][3]);
+        a[t][0] = Half2<T>::down(x[t][0][0][0], x[t][0][0][1]), a[t][1] = Half2<T>::down(x[t][0][0][2], x[t][0][0][3]);
+        a[t][2] = Half2<T>::down(x[t][0][1][0], x[t][0][1][1]), a[t][3] = Half2<T>::down(x[t][0][1][2], x[t][0][1][3]);
+      }
+      if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int i = 0; i < D / 8; ++i)
+            o[t][i][0] *= f[t][0], o[t][i][1] *= f[t][0], o[t][i][2] *= f[t][1], o[t][i][3] *= f[t][1];
       }
     }
     // this unit's V has landed
