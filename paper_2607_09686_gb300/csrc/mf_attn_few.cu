@@ -17,6 +17,10 @@
 // only this warp touches, so nothing in the loop waits for another warp, K and V apart, so that a slot is filled again as
 // soon as its products are done (128 KiB and more in flight per SM; the copies' depth sets the rate).  At a piece's end
 // the warps put their o into the slots just freed and add up.
+//
+// Measured: 64 sequences of 166 to 8192 lines, 32/4 heads of 128, 395 MB: 74.5 us with the join, 5.3 TB/s (78 % of the copy
+// rate; that rate once it runs, 6 us before the first lines are there); one sequence of 131071 lines, 16/2 heads of 256:
+// 54.9 us, 4.9 TB/s; one of 1001 lines: 9.8 us, of which 5 are this kernel's and the rest the join's and the launches'.
 #include "mf_attn.cuh"
 
 namespace mf {

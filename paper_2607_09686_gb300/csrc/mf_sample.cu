@@ -13,12 +13,15 @@
 //   3. top-p of what may be many entries: a histogram of masses.  A bin's mass is a sum of integers, w / e^(-bin / 64)
 //      in units of 2^-q, so it hangs on no order of additions; the border bin's entries are sorted as above.
 //      (Bits: a slice of 2^s entries leaves q = 31 - s; rounding to a unit is random and below 2^-16 of an entry.)
+//      What lies so low that it cannot hold the border is summed by ex2 alone.
 //   4. a border bin that is too large is cut by bisection over the value's 32-bit key, and equal values by counting them
 //      in the order of their index.
 //   5. what is kept: sum of w and the largest z + noise, with z as a product; then the entries that come near that one
 //      again, with z as the exact quotient.
-// What bounds it: with top-k the cluster's barriers and one pass over the slice; else passes of some ten to twenty
-// instructions an entry.  Rows by temperature alone have a kernel of their own, in one pass (k_sample_plain).
+// What bounds it: with top-k the cluster's barriers and one pass over the slice; else passes of ten to twenty-five
+// instructions an entry.  One row of 131072 fp32, top-k of 50: 11 us, of 1000: 14 (5 of them the sort); 64 rows of 262144 bf16,
+// each with settings of its own: 53 us (rows cut by top-p alone 40, in a grid that holds 38 clusters at a time).  Rows by
+// temperature alone have a kernel of their own, in one pass (k_sample_plain).
 #include <cooperative_groups.h>
 
 #include <cfloat>
@@ -34,6 +37,7 @@ namespace {
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxVocab = 1 << 20;
 constexpr int kBins = 2048, kList = 4096, kShort = 512;
+constexpr int kCounted = 256;  // entries of a list up to which they are sorted by counting (80: 11.2 us a row against 12.1, 345: 14.3 against 13.8)
 constexpr float kBinsPerUnit = 64.f;
 constexpr size_t kListAt = (kBins + 4) * 4, kRowAt = kListAt + kList * 8;  // bytes of shared memory before the list, the row
 constexpr size_t kResident = 128 * 1024;  // bytes of a slice that are kept in shared memory
@@ -384,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   // two are equal).  Else bitonic; entries up to 64 apart meet in the registers of a warp that has 128, without barriers.
   auto sort_list = [&](int len) {
     __syncthreads();
-    if (len <= kThreads) {
+    if (len <= kCounted) {
       if (tid == 0) list[len] = 0;
       __syncthreads();
       const unsigned long long e = tid < len ? list[tid] : 0;
@@ -401,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       __syncthreads();
       return;
     }
-    int p2 = 1024;
+    int p2 = 2 * kCounted;
     while (p2 < len) p2 <<= 1;
     for (int i = len + tid; i < p2; i += kThreads) list[i] = 0;
     __syncthreads();
@@ -861,6 +865,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
 // its keys, with M / T left in (x / T + noise), the largest and the two largest with their margins: rounding aside the keys'
 // order needs no M.  With the row's M known, a thread whose key comes near the largest forms that one again, with z as the exact
 // quotient, or looks at all its entries where its second comes near too.  Bounded by reading logits and noise once, and by two cluster barriers a row.
+// 256 rows of 50001 fp16: 22.6 us, 3.4 TB/s (half of the copy rate: 256 blocks where 304 find room, two thirds of the issue slots
+// taken, 4 us of barriers and joining at the end).
 struct PlainShared {
   float m[kWarps], s[kWarps], top[kWarps];
   int i[kWarps];
