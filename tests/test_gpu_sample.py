@@ -238,3 +238,61 @@ def test_refusals(mf):
             mf._check(mf._lib.mf_sample(mf._SampleArgs(**{**ok, **bad}), None), "mf_sample")
         assert e.value.status == mf.MF_E_INVAL
     mf._check(mf._lib.mf_sample(mf._SampleArgs(**{**ok, "n_rows": 0, "token": None}), None), "mf_sample")
+
+
+@pytest.mark.parametrize("v", [5003, 131072])
+def test_lists_of_all_lengths(mf, v):
+    """Entries that are sorted: from a few to as many as the list holds and more."""
+    ks = [60, 130, 250, 255, 256, 257, 300, 450, 511, 513, 700, 1400, 2100, 3500, 4090, 4097]
+    g = torch.Generator("cuda").manual_seed(v + 7)
+    x = torch.randn(len(ks), v, device="cuda", generator=g) * 3
+    check(mf, x, gumbel(len(ks), v, v), k=ks)
+    check(mf, x, gumbel(len(ks), v, v + 1), k=ks, p=0.9003, t=1.3)
+
+
+@pytest.mark.parametrize("v", [1000, 50001])
+@pytest.mark.parametrize("spread", [0.02, 1.0, 4.0, 20.0])
+def test_top_p_of_many(mf, v, spread):
+    """From rows where nearly all entries count to rows where most are too small to: p in the middle of an entry's mass.
+
+    Half an entry's share is 1e-5 and more of the total for v = 50001 with p to 0.99, sums and p err by some 1e-7."""
+    g = torch.Generator("cuda").manual_seed(v)
+    x = torch.randn(1, v, device="cuda", generator=g) * spread
+    w = torch.softmax(x[0].double(), 0).sort(descending=True).values
+    upto = w.cumsum(0)
+    ps = []
+    for share in (0.1, 0.5, 0.9, 0.95, 0.99):
+        j = int((upto < share).sum())
+        p = float(upto[j] - w[j] / 2)
+        if w[j] > 4e-6 and p not in ps:
+            ps.append(p)
+    assert ps
+    for mp in (None, [1e-4] * len(ps)):
+        check(mf, x.expand(len(ps), v).contiguous(), gumbel(len(ps), v, 3), p=ps, mp=mp)
+
+
+def test_min_p_close_to_its_entries(mf):
+    """Entries whose w is off min_p by 1.5e-6 of it, ten times what an exponential errs by: half are in."""
+    v = 3001
+    x = torch.full((2, v), math.log(0.5), device="cuda", dtype=torch.float64)
+    x[:, ::2] += 1.5e-6
+    x[:, 1::2] -= 1.5e-6
+    x[:, 1500] = 0.0
+    x[1] += 8.0 - x[1].max()  # (coarser logits: 8 + z in steps of 2^-21, the halves stay apart)
+    check(mf, x.float(), gumbel(2, v, 11), mp=[0.5, 0.5])
+
+
+def test_noise_without_bounds(mf):
+    """Noise of -inf and NaN rules entries out, one of +inf decides."""
+    n, v = 4, 40000
+    g = torch.Generator("cuda").manual_seed(31)
+    x = torch.randn(n, v, device="cuda", generator=g) * 2
+    noise = gumbel(n, v, 17)
+    noise[0, torch.rand(v, device="cuda", generator=g) < 0.9] = -math.inf
+    noise[1, ::2] = math.nan
+    best = int(x[2].argmax())
+    noise[2, best] = math.inf
+    noise[3, :] = -math.inf
+    noise[3, int(x[3].argmax())] = 0.5
+    for kw in (dict(), dict(k=5000), dict(k=100), dict(p=0.9003), dict(mp=0.01), dict(p=0.95007, mp=0.003)):
+        check(mf, x, noise, **kw)
