@@ -300,17 +300,16 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     } else if (mass) {
       const bool all = xc == -INFINITY;
       const float low = all ? m + t * (logf((1.f - want) / (float)c.vocab) - 0.01f) - 1e-6f * fabsf(m) : xc;
-      const float inv_e = 1.4426950408889634f / t;
+      const float inv_e = 1.4426950408889634f / t, inv_far = fminf(inv, FLT_MAX);
       float rest = 0.f;
-      for_each([&](int i, float x) {
-        if (x < low) {
-          if (all) rest += ex2((x - m) * inv_e);
-        } else if (kept(x, base + i)) {
-          const float d = x == m ? 0.f : x - m, at = bin_at(d, inv);
-          // (w against that at the bin's middle: near 1)
-          const float w = d == 0.f ? 1.f : ex2(fmaf(d, inv, at - 8388608.f) * (1.4426950408889634f / kBinsPerUnit));
+      for_each([&](int i, float x) {  // (without branches: both sides cost less than their divergence)
+        const bool below = x < low;
+        const float d = x == m ? 0.f : x - m, at = bin_at(d, inv);
+        // (w against that at the bin's middle: near 1)
+        const float w = ex2(fmaf(d, inv_far, at - 8388608.f) * (1.4426950408889634f / kBinsPerUnit)), tail = ex2(d * inv_e);
+        rest += below && all ? tail : 0.f;
+        if (!below && (all || kept(x, base + i)))
           atomicAdd(hist + (__float_as_uint(at) & (kBins - 1)), __float_as_uint(fmaf(w, unit, 8388608.f)) & 0x7FFFFFu);
-        }
       });
       rest = warp_sum(rest);
       if (lane == 0 && rest > 0.f) atomicAdd(hist + kBins, (uint32_t)(fminf(rest, 1.f) * 1073741824.f / (float)(kWarps) + 0.5f));
