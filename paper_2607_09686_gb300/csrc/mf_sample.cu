@@ -20,7 +20,7 @@
 //      again, with z as the exact quotient.
 // What bounds it: with top-k the cluster's barriers and one pass over the slice; else passes of ten to twenty-five
 // instructions an entry.  One row of 131072 fp32, top-k of 50: 11 us, of 1000: 14 (5 of them the sort); 64 rows of 262144 bf16,
-// each with settings of its own: 53 us (rows cut by top-p alone 40, in a grid that holds 38 clusters at a time).  Rows by
+// each with settings of its own: 52 us (rows cut by top-p alone 38, in a grid that holds 38 clusters at a time).  Rows by
 // temperature alone have a kernel of their own, in one pass (k_sample_plain).
 #include <cooperative_groups.h>
 
