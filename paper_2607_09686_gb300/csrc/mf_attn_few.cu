@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
   if (blockIdx.x >= B) return;
   const int64_t t0 = total * blockIdx.x / B, t1 = total * (blockIdx.x + 1) / B;
   {
-    int64_t before = 0;  // tiles of the sequences before this round's
+    int64_t before = 0;  // tiles of the sequences before these
     for (int base = 0; base < st.n_seqs; base += kThreads) {
       const int64_t nt = cost_of(base + tid) * st.Hkv;
       int64_t pre = nt;  // inclusive prefix
