@@ -321,7 +321,10 @@ extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, cons
   if (bad_rows(args->q, args->q_stride) || bad_rows(args->out, args->out_stride) || ((uintptr_t)args->lse & 3)) return MF_E_INVAL;
   c.k = cache->k, c.v = cache->v, c.q = args->q, c.out = args->out, c.lse = args->lse;
   c.q_stride = args->q_stride, c.out_stride = args->out_stride;
-  c.scale = args->scale, c.window = args->window, c.causal = args->causal != 0;
+  c.scale = args->scale, c.causal = args->causal != 0;
+  // a window of 2^30 lines holds every line there can be, and the line it begins at is counted in 32 bits also from a
+  // token whose own line would lie before the first (no more than 2^30 before it)
+  c.window = args->window < (1 << 30) ? args->window : 1 << 30;
   OnDevice on(attn->device);
   if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
   const int D = attn->shape.head_dim;

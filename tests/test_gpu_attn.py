@@ -359,3 +359,12 @@ def test_refusals(mf):
     mf.mf_kv_append(at, cache, empty, c.new_k, c.new_v)
     assert mf.mf_attn_check(at) == 0
     mf.mf_attn_destroy(at)
+
+
+@pytest.mark.parametrize("window", [2 ** 30 - 1, 2 ** 30, 2 ** 31 - 5, 2 ** 31 - 1])
+@pytest.mark.parametrize("new,total", [([1, 1, 4], [0, 5, 1]), ([20, 3, 200], [0, 5, 150])])
+@pytest.mark.parametrize("causal", [True, False])
+def test_largest_windows(mf, window, new, total, causal):
+    """Windows as long as their type allows hide nothing, also from tokens whose line would lie before the first."""
+    c = ref.Case(new, [t - n for t, n in zip(total, new)], 8, 2, 128)
+    assert torch.equal(check(mf, c, window=window, causal=causal), check(mf, c, causal=causal))
