@@ -284,6 +284,23 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     }
     return before + x - v;
   };
+  // The last bin that is not empty and begins below `goal`, of bins tid * 4 + u of v[u], this thread's first beginning at `at` (-1:
+  // none), in every thread; its owner gets its span.  A border that is sought so is found whatever the rounding: the ends of a
+  // thread's bins and the beginning of the next thread's are different sums, with gaps and overlaps of a last bit, in which no
+  // bin, or two, would hold the goal.  (sh.here is -1 before.)
+  auto last_below = [&](const float (&v)[4], float at, float goal, bool& own, float2& span) -> int {
+    int mine = -1;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (v[u] > 0.f && at < goal) mine = tid * 4 + u, span = make_float2(at, at + v[u]);
+      at += v[u];
+    }
+    const int most = __reduce_max_sync(0xffffffffu, mine);
+    if (lane == 0) atomicMax(&sh.here, most);
+    __syncthreads();
+    own = mine >= 0 && mine == sh.here;
+    return sh.here;
+  };
   // Counts (or masses, in units of 2^-qbits) of the kept entries by bin, or counts of the threads' maxima; the leading block finds
   // the first bin down to which they reach `want` (mass: want * their total), and tells all blocks: bin, above, goal, and for
   // counts count.  Counts are whole numbers below 2^24: exact in fp32.
@@ -337,14 +354,13 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
         v[u] = mass ? (float)s[u] * expf(-(float)b * (1.f / kBinsPerUnit)) : (float)s[u];
         sum += v[u];
       }
-      if (tid == 0) sh.bin = -1;
-      float at = block_scan(sum, total);
-      const float goal = mass ? want * (total + rest * unit) : want;
-#pragma unroll
-      for (int u = 0; u < kPer; ++u) {
-        if (at < goal && at + v[u] >= goal) sh.bin = tid * kPer + u, sh.above = at, sh.count = (int)(at + v[u]);
-        at += v[u];
-      }
+      if (tid == 0) sh.bin = sh.here = -1;
+      const float at = block_scan(sum, total), goal = mass ? want * (total + rest * unit) : want;
+      bool own;
+      float2 span;
+      const int bin = last_below(v, at, goal, own, span);
+      // (counts: fewer entries than are wanted cut nothing; a part of the mass is always reached)
+      if (own && (mass || total >= want)) sh.bin = bin, sh.above = span.x, sh.count = (int)span.y;
       if (tid == 0) sh.goal = goal;
       __syncthreads();
       if (warp == 0 && lane > 0 && lane < C) {
@@ -594,20 +610,33 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
             if (u < per && i < len) z[u] = z_of(key_value((uint32_t)(list[i] >> 32)), m, t), w[u] = expf(z[u]);
             sum += w[u];
           }
+          if (tid == 0) sh.here = 0;
           float at = block_scan(sum, all);
-          const float want = top_p * all;
+          int last = len - 1;  // kept by top-p
+          if (top_p < 1.f) {
+            const float want = top_p * all;
+            int mine = 0;
+#pragma unroll
+            for (int u = 0; u < kPer; ++u) {
+              if (u < per && tid * per + u < len && at < want) mine = tid * per + u;
+              at += w[u];
+            }
+            mine = __reduce_max_sync(0xffffffffu, mine);
+            if (lane == 0) atomicMax(&sh.here, mine);
+            __syncthreads();
+            last = sh.here;
+          }
           Best b = none;
           sum = 0;
 #pragma unroll
           for (int u = 0; u < kPer; ++u) {
             const int i = tid * per + u;
-            if (u < per && i < len && (i == 0 || ((!(top_p < 1.f) || at < want) && w[u] >= min_p))) {
+            if (u < per && i <= last && (i == 0 || w[u] >= min_p)) {
               const int idx = (int)(0xFFFFFFFFu - (uint32_t)list[i]);
               const float g = noise[idx];
               b.take(g == g ? z[u] + g : -INFINITY, z[u], idx);
               sum += w[u];
             }
-            at += w[u];
           }
           block_scan(sum, all);
           b = block_best(b);
@@ -682,17 +711,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
               float v[4], sum = 0, all;
 #pragma unroll
               for (int u = 0; u < 4; ++u) sum += v[u] = (float)hist[tid * 4 + u] * (w_top / 524287.f);
-              float at = above + block_scan(sum, all);
               if (tid == 0) sh.here = -1;
+              const float at = above + block_scan(sum, all);
+              bool own;
+              float2 span;
+              const int bin = last_below(v, at, want, own, span);
+              if (bin < 0) break;  // (the sums' last bits: the border is the range's beginning; sorted below as it is)
+              if (own) sh.above = span.x;
               __syncthreads();
-#pragma unroll
-              for (int u = 0; u < 4; ++u) {
-                if (at < want && at + v[u] >= want) sh.here = tid * 4 + u, sh.above = at;
-                at += v[u];
-              }
-              __syncthreads();
-              const int bin = sh.here;
-              if (bin < 0) break;  // (the sums' last bits: the border is the range's end; sorted below as it is)
               above = sh.above;
               if (by_key) {
                 const uint32_t top = hi - ((uint32_t)bin << shift), step = (1u << shift) - 1;

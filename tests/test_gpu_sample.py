@@ -296,3 +296,53 @@ def test_noise_without_bounds(mf):
     noise[3, int(x[3].argmax())] = 0.5
     for kw in (dict(), dict(k=5000), dict(k=100), dict(p=0.9003), dict(mp=0.01), dict(p=0.95007, mp=0.003)):
         check(mf, x, noise, **kw)
+
+
+@pytest.mark.parametrize("v", [4099, 50001])
+def test_top_p_is_cut_at_every_border(mf, v):
+    """p in steps of one ulp across the masses down to every fourth bin of 1/64 in z: the kept mass is p of the total each
+    time, less than an entry too much, and the same again.  (Masses in fp32 err by less than 1e-5 of the total.)"""
+    g = torch.Generator("cuda").manual_seed(v + 3)
+    x = torch.randn(v, device="cuda", generator=g) * 2
+    z = x.double() - x.double().max()
+    w, total = z.exp(), z.exp().sum()
+    upto = torch.zeros(2049, dtype=torch.float64, device="cuda").index_add_(0, (z * -64).round().clamp(max=2047).long() + 1, w).cumsum(0) / total
+    at = upto[::4]
+    at = at[(at > 0.03) & (at < 0.97)].float().unique()
+    p = (at.view(torch.int32)[:, None] + torch.arange(-24, 25, device="cuda", dtype=torch.int32)).view(-1).view(torch.float32)
+    noise = torch.zeros(v, device="cuda")
+    noise[x.argmax()] = 100.0
+    falling = w.sort(descending=True).values
+    before = falling.cumsum(0) - falling
+    for q in p.split(512):
+        n = len(q)
+        rows, token, lp = x.expand(n, v).contiguous(), torch.empty(2, n, dtype=torch.int32, device="cuda"), torch.empty(2, n, device="cuda")
+        for i in range(2):
+            mf.mf_sample(rows, noise.expand(n, v).contiguous(), token[i], lp[i], top_p=q)
+        assert torch.equal(lp[0], lp[1]) and (token == x.argmax()).all()
+        held, want = (-lp[0].double()).exp(), q.double() * total
+        entry = falling[(torch.searchsorted(before, want) - 2).clamp(min=0)]
+        assert (held >= want - 1e-5 * total).all() and (held <= want + 2 * entry + 1e-5 * total).all(), ((held - want) / total).abs().max()
+
+
+def test_top_p_among_the_first_is_a_prefix(mf):
+    """Under top-k too, p in steps of one ulp: the last kept entry (its noise is the largest) and the kept mass agree."""
+    v, k = 5003, 2000
+    g = torch.Generator("cuda").manual_seed(77)
+    x = torch.randn(v, device="cuda", generator=g)
+    order = x.argsort(descending=True)
+    noise = torch.full((v,), -1e4, device="cuda")
+    noise[order] = torch.arange(v, device="cuda").float() * 16  # later entries win whatever their z
+    w = (x.double() - x.double().max()).exp()[order][:k]
+    upto = w.cumsum(0)
+    for i in range(100, 1900, 100):
+        p = ((upto[i] / upto[-1]).float().view(torch.int32) + torch.arange(-16, 17, device="cuda", dtype=torch.int32)).view(torch.float32)
+        n = len(p)
+        token, lp = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(n, device="cuda")
+        mf.mf_sample(x.expand(n, v).contiguous(), noise.expand(n, v).contiguous(), token, lp, top_p=p,
+                     top_k=torch.full((n,), k, dtype=torch.int32, device="cuda"))
+        rank = torch.argsort(order)[token.long()]
+        # a sum in fp32 may move the border by an entry or two, what is kept ends there all the same
+        assert ((rank - i).abs() <= 2).all(), rank
+        held = ((x[token.long()].double() - x.double().max()) - lp.double()).exp()
+        assert ((held - upto[rank]).abs() <= 2e-6 * upto[-1]).all(), (rank, (held - upto[rank]) / upto[-1])
