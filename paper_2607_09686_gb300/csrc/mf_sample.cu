@@ -12,7 +12,10 @@
 //      is large for that, a histogram of counts over bins of 1/64 in z takes the maxima's place.)
 //   3. top-p of what may be many entries: a histogram of masses.  A bin's mass is a sum of integers, w / e^(-bin / 64)
 //      in units of 2^-q, so it hangs on no order of additions; the border bin's entries are sorted as above.
-//      (Bits: a slice of 2^s entries leaves q = 31 - s; rounding to a unit is random and below 2^-16 of an entry.)
+//      (Bits: a slice of 2^s entries, s >= 15, leaves q = 31 - s.  A mass is rounded up or down by a number that hangs on
+//      the entry's place alone, evenly spread: up as often as its fraction says.  So N equal logits, which to the nearest
+//      unit would all be rounded alike, N 2^-(q + 1) of an entry too much or too little, come to less than
+//      sqrt(8 N) 2^-(q + 1): 0.09 of an entry for the 2^20 of the largest vocabulary, whose q is 14, as a sum in fp32.)
 //      What lies so low that it cannot hold the border is summed by ex2 alone.
 //   4. a border bin that is too large is cut by bisection over the value's 32-bit key, and equal values by counting them
 //      in the order of their index.
@@ -143,7 +146,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     lost = __syncthreads_or(!mbar_wait(&sh.bar, 0, kDefaultWaitNs));
     src = x0;
   }
-  // every thread's entries: whole vectors of the slice where it lies in shared memory
+  // every thread's entries, f(index, logit, vector): whole vectors of the slice where it lies in shared memory
   auto for_each = [&](auto&& f) {
     if (c.keep) {
       constexpr int kV = 16 / sizeof(T);
@@ -154,13 +157,13 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
         const int i0 = v * kV - lead_in;
         if (i0 >= 0 && i0 + kV <= n) {
 #pragma unroll
-          for (int u = 0; u < kV; ++u) f(i0 + u, up(e[u]));
+          for (int u = 0; u < kV; ++u) f(i0 + u, up(e[u]), v);
         } else {
-          for (int i = max(i0, 0); i < min(i0 + kV, n); ++i) f(i, up(src[i]));
+          for (int i = max(i0, 0); i < min(i0 + kV, n); ++i) f(i, up(src[i]), v);
         }
       }
     } else {
-      for (int i = tid; i < n; i += kThreads) f(i, up(row[i]));
+      for (int i = tid; i < n; i += kThreads) f(i, up(row[i]), i);
     }
   };
   // Those from lo to hi (a bound that is no number bounds nothing), where they are few: of 64 entries at a time a thread's are
@@ -212,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   };
   auto get_none = [](int) { return 0.f; };
   float mx = -INFINITY;
-  for_each([&](int, float x) { mx = fmaxf(mx, x); });
+  for_each([&](int, float x, int) { mx = fmaxf(mx, x); });
   const float own_max = mx;
 #pragma unroll
   for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
@@ -318,20 +321,24 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       const bool all = xc == -INFINITY;
       const float low = all ? m + t * (logf((1.f - want) / (float)c.vocab) - 0.01f) - 1e-6f * fabsf(m) : xc;
       const float inv_e = 1.4426950408889634f / t, inv_far = fminf(inv, FLT_MAX);
+      const uint32_t seed = (uint32_t)rank * 0x85EBCA6Bu;
       float rest = 0.f;
-      for_each([&](int i, float x) {  // (without branches: both sides cost less than their divergence)
+      for_each([&](int i, float x, int v) {  // (without branches: both sides cost less than their divergence)
         const bool below = x < low;
         const float d = x == m ? 0.f : x - m, at = bin_at(d, inv);
         // (w against that at the bin's middle: near 1)
         const float w = ex2(fmaf(d, inv_far, at - 8388608.f) * (1.4426950408889634f / kBinsPerUnit)), tail = ex2(d * inv_e);
         rest += below && all ? tail : 0.f;
+        // rounded down after a number of [0, 1) is added, the vector's own (multiples of the golden ratio, their fractions):
+        // whole masses stay what they are
+        const float part = __uint_as_float(0x3F800000u | ((uint32_t)v * 0x9E3779B9u + seed) >> 9) - 1.f;
         if (!below && (all || kept(x, base + i)))
-          atomicAdd(hist + (__float_as_uint(at) & (kBins - 1)), __float_as_uint(fmaf(w, unit, 8388608.f)) & 0x7FFFFFu);
+          atomicAdd(hist + (__float_as_uint(at) & (kBins - 1)), __float_as_uint(__fadd_rd(__fmaf_rd(w, unit, part), 8388608.f)) & 0x7FFFFFu);
       });
       rest = warp_sum(rest);
       if (lane == 0 && rest > 0.f) atomicAdd(hist + kBins, (uint32_t)(fminf(rest, 1.f) * 1073741824.f / (float)(kWarps) + 0.5f));
     } else {
-      for_each([&](int i, float x) {
+      for_each([&](int i, float x, int) {
         if (kept(x, base + i)) atomicAdd(hist + bin_of(x == m ? 0.f : x - m, inv), 1u);
       });
     }
@@ -797,7 +804,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   Best b = none;
   float sum = 1.f;
   if (first_only) {
-    for_each([&](int i, float x) {
+    for_each([&](int i, float x, int) {
       if (x == m) b.take(0.f, 0.f, base + i);
     });
   } else {

@@ -346,3 +346,46 @@ def test_top_p_among_the_first_is_a_prefix(mf):
         assert ((rank - i).abs() <= 2).all(), rank
         held = ((x[token.long()].double() - x.double().max()) - lp.double()).exp()
         assert ((held - upto[rank]).abs() <= 2e-6 * upto[-1]).all(), (rank, (held - upto[rank]) / upto[-1])
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("v", [1 << 18, 1 << 19, 1 << 20])
+def test_top_p_beside_large_groups_of_equal_logits(mf, dtype, v):
+    """Two large groups of equal logits, one above the border and one below, whose masses a fixed number of bits would round the same
+    way entry by entry; the border falls among a few thousand smaller ones.  The noise is such that the last kept one wins.
+    Sums of fp32 numbers: 30 roundings of 2^-24 of the total and exponentials off by 2^-22 move the border by at
+    most 3e-6 of the total."""
+    g = torch.Generator("cuda").manual_seed(v)
+    perm = torch.randperm(v, device="cuda", generator=g)
+    n_top, n_mid = int(0.4 * v), 3000
+    mid = perm[n_top:n_top + n_mid].sort().values  # in the order of their index
+    x = torch.full((v,), -1.5, device="cuda")
+    noise = torch.full((v,), -100.0, device="cuda")
+    noise[mid] = torch.arange(n_mid, device="cuda") * 0.25
+    unit = 2.0 ** 34 / v  # of a mass rounded to whole units in slices of an eighth of the row, 2^31 units together
+    worst = 0.0
+    values = (torch.arange(1, 127, device="cuda") / -16384.0).to(dtype).double()  # of one 1/128 below the largest
+    off = (values.exp() * unit).round() - values.exp() * unit
+    low = (-1.5 + torch.arange(0, 64, device="cuda") / 4096.0).to(dtype).double()
+    place = low + ((low * -64).round() / 64)
+    off_low = (place.exp() * unit).round() - place.exp() * unit
+    for sign in (1, -1):
+        a, b = values[(off * sign).argmax()], low[(off_low * -sign).argmax()]
+        y = x.clone().double()
+        y[:] = b
+        y[perm[:n_top]] = a
+        y[mid] = -1.0
+        y[perm[-1]] = 0.0
+        y = y.to(dtype)
+        e = y.double().exp()
+        total, above = e.sum(), e[y.double() > -1.0].sum()
+        p = [float((above + (j + 0.5) * math.exp(-1.0)) / total) for j in (300, 1200, 1500, 2700)]
+        p = torch.tensor(p, dtype=torch.float32, device="cuda")
+        want = torch.ceil((p.double() * total - above) / math.exp(-1.0)) - 1  # rank of the last kept one
+        n = len(p)
+        token = torch.empty(n, dtype=torch.int32, device="cuda")
+        mf.mf_sample(y.expand(n, v).contiguous(), noise.expand(n, v).contiguous(), token, None, top_p=p)
+        rank = torch.searchsorted(mid, token.long())
+        assert torch.equal(mid[rank.clamp(max=n_mid - 1)], token.long())
+        worst = max(worst, float((rank - want).abs().max()))
+    assert worst <= 1 + 3e-6 * float(total) / math.exp(-1.0), worst
