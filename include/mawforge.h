@@ -465,7 +465,7 @@ void mf_attn_destroy(mf_attn_t* attn);
 
 /* One token from each row of logits.  With x the row in fp32 (NaN as -inf), M its largest value, T the
  * row's temperature, and the entries in the order of falling x, the lower index first where x is equal:
- *   z_i = 0 where x_i = M, else (x_i - M) / T, w_i = exp(z_i)
+ *   z_i = 0 where x_i = M, else (x_i - M) / T (-inf beside M = +inf, whatever T), w_i = exp(z_i)
  *   kept = the first top_k entries (top_k <= 0: all), of those the ones before which less than top_p of
  *          their mass lies (top_p >= 1 or NaN: all), of those the ones with w_i >= min_p (above 1 it counts
  *          as 1, NaN as 0); entries of -inf never, the first entry always
@@ -473,7 +473,8 @@ void mf_attn_destroy(mf_attn_t* attn);
  *   logprob = z_token - log(sum of w over the kept)
  * noise is the caller's random numbers: independent standard Gumbel values, -log(-log u) of uniform u,
  * which make the token a draw from softmax over the kept (one value an entry, so that no token hangs on
- * the rounding of a running sum).  T <= 0 or NaN keeps the first entry alone (greedy).  A row without a finite
+ * the rounding of a running sum).  T <= 0 or NaN keeps the first entry alone (greedy); T = +inf is any T so large that all z are
+ * 0; T between 0 and 2^-120 counts as 2^-120.  A row without a finite
  * or +inf entry gives token -1 and logprob -inf.
  *   logits  device [n_rows][vocab] of dtype (MF_F32, MF_F16 or MF_BF16), row r at r * logits_stride elements
  *   noise   device float [n_rows][vocab], row r at r * noise_stride

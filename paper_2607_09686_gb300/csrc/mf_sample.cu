@@ -64,11 +64,17 @@ __device__ __forceinline__ uint32_t order_key(float x) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
-__device__ __forceinline__ float z_of(float x, float m, float t) { return x == m ? 0.f : __fdiv_rn(x - m, t); }
+// The temperature and its inverse are kept where 0 and -inf times the inverse (also in units of log2 e and of bins) are 0 and
+// -inf: T from 2^-120 up (below it what differs from M weighs nothing, unless by less than 2^-113), the inverse above 0 for
+// T = inf (times the largest number it is below 1e-6).
+__device__ __forceinline__ float bounded(float t) { return fmaxf(t, 0x1p-120f); }
+__device__ __forceinline__ float inverse(float unit, float t) { return fmaxf(unit / t, 1e-45f); }
+// (what is no number, -inf / inf, is -inf)
+__device__ __forceinline__ float z_of(float x, float m, float t) { return x == m ? 0.f : fmaxf(__fdiv_rn(x - m, t), -INFINITY); }
 // bin of an entry `d` = x - M, the nearest of those at multiples of 1/64 in z; monotonic in d (inv: bins per unit of d).
 // Rounded by adding 2^23: conversions share a slow pipe with ex2.
 __device__ __forceinline__ float bin_at(float d, float inv) {
-  return (d == 0.f ? 0.f : fminf(-d * inv, (float)(kBins - 1))) + 8388608.f;  // (inv may be infinite)
+  return fminf(-d * inv, (float)(kBins - 1)) + 8388608.f;
 }
 __device__ __forceinline__ int bin_of(float d, float inv) { return (int)(__float_as_uint(bin_at(d, inv)) & (kBins - 1)); }
 
@@ -242,11 +248,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
 
   const float temp = c.temperature ? c.temperature[r] : 1.f;
   const bool greedy = !(temp > 0.f);
-  const float t = greedy ? 1.f : temp;
+  const float t = greedy ? 1.f : bounded(temp);
   const int top_k = c.top_k && !greedy ? c.top_k[r] : 0;
   const float top_p = c.top_p && !greedy ? c.top_p[r] : 1.f;
   const float min_p = c.min_p && !greedy ? fminf(fmaxf(c.min_p[r], 0.f), 1.f) : 0.f;
-  const float inv = kBinsPerUnit / t;
+  const float inv = inverse(kBinsPerUnit, t);
   float xc = -INFINITY;  // kept: larger entries, and equal ones up to index ic
   int ic = -1;
   auto kept = [&](float x, int i) { return x > xc || (x == xc && i <= ic); };
@@ -320,14 +326,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     } else if (mass) {
       const bool all = xc == -INFINITY;
       const float low = all ? m + t * (logf((1.f - want) / (float)c.vocab) - 0.01f) - 1e-6f * fabsf(m) : xc;
-      const float inv_e = 1.4426950408889634f / t, inv_far = fminf(inv, FLT_MAX);
+      const float inv_e = inverse(1.4426950408889634f, t);
       const uint32_t seed = (uint32_t)rank * 0x85EBCA6Bu;
       float rest = 0.f;
       for_each([&](int i, float x, int v) {  // (without branches: both sides cost less than their divergence)
         const bool below = x < low;
         const float d = x == m ? 0.f : x - m, at = bin_at(d, inv);
         // (w against that at the bin's middle: near 1)
-        const float w = ex2(fmaf(d, inv_far, at - 8388608.f) * (1.4426950408889634f / kBinsPerUnit)), tail = ex2(d * inv_e);
+        const float w = ex2(fmaf(d, inv, at - 8388608.f) * (1.4426950408889634f / kBinsPerUnit)), tail = ex2(d * inv_e);
         rest += below && all ? tail : 0.f;
         // rounded down after a number of [0, 1) is added, the vector's own (multiples of the golden ratio, their fractions):
         // whole masses stay what they are
@@ -808,14 +814,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       if (x == m) b.take(0.f, 0.f, base + i);
     });
   } else {
-    const float inv_t = 1.f / t, inv_e = inv_t * 1.4426950408889634f;
+    const float inv_t = inverse(1.f, t), inv_e = inv_t * 1.4426950408889634f;
     // z as a product and w of an entry, and whether it is in: w >= min_p is decided on the exact w where the other comes near.
     // (w is off by the rounding of z log2(e), by a few 2^-24 |z|, and by ex2's 2^-22.)
     const float eps = 4e-7f * (8.f + fabsf(logf(fmaxf(min_p, FLT_MIN)))), p_hi = min_p * (1.f + eps), p_lo = min_p * (1.f - eps);
     auto in_with = [&](float x, int i, float& near, float& w) -> bool {
       const float d = x == m ? 0.f : x - m;
-      near = d == 0.f ? 0.f : d * inv_t;
-      w = d == 0.f ? 1.f : ex2(d * inv_e);
+      near = d * inv_t;
+      w = ex2(d * inv_e);
       return kept(x, i) && w >= p_lo && (w >= p_hi || expf(z_of(x, m, t)) >= min_p);
     };
     // sum of w; the largest key; the largest with its margin, that of the exact key (the two forms of a key differ by less
@@ -920,7 +926,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_plain(SampleCall c) {
   pdl_wait();
   const float temp = c.temperature ? c.temperature[r] : 1.f;
   const bool greedy = !(temp > 0.f);
-  const float t = greedy ? 1.f : temp, inv_t = 1.f / t, inv_e = inv_t * 1.4426950408889634f;
+  const float t = greedy ? 1.f : bounded(temp), inv_t = inverse(1.f, t), inv_e = inv_t * 1.4426950408889634f;
   auto up = [](T v) -> float { return fmaxf((float)v, -INFINITY); };  // NaN as -inf
   auto scaled = [&](float s, float from, float to) { return from == to ? s : s * ex2((from - to) * inv_e); };
   float m = -INFINITY, s = 0.f, top = -INFINITY, reach = -INFINITY, reach2 = -INFINITY;

@@ -389,3 +389,39 @@ def test_top_p_beside_large_groups_of_equal_logits(mf, dtype, v):
         assert torch.equal(mid[rank.clamp(max=n_mid - 1)], token.long())
         worst = max(worst, float((rank - want).abs().max()))
     assert worst <= 1 + 3e-6 * float(total) / math.exp(-1.0), worst
+
+
+@pytest.mark.parametrize("dtype", DT)
+@pytest.mark.parametrize("v", [7, 4096, 5003, 50001])
+def test_ends_of_the_temperature(mf, dtype, v):
+    """From the smallest number above 0 to infinity, with forbidden entries, by temperature alone and with cuts."""
+    ts = [math.inf, 3e38, 1e38, 1e30, 1e-30, 2.0 ** -120, 1e-39, 1e-45]
+    ts = [torch.tensor(t, dtype=torch.float32).item() for t in ts]
+    n = len(ts)
+    g = torch.Generator("cuda").manual_seed(v + 5)
+    x = (torch.randn(n, v, device="cuda", generator=g) * 3).to(dtype)
+    x[:, 1::3] = -math.inf
+    x[:, 5] = x[:, 0] = x.max(-1).values  # two of the largest at least: noise decides
+    left = int((x[0] > -math.inf).sum())
+    half = (left // 2 + 0.5) / left
+    for kw in (dict(), dict(mp=[0.0] * n), dict(k=[left - 1] * n), dict(k=[max(1, left // 2)] * n), dict(p=[half] * n), dict(mp=[0.5003] * n),
+               dict(k=[left // 2 + 2] * n, p=[0.75] * n) if left > 8 else dict()):
+        check(mf, x, gumbel(n, v, v), t=ts, **kw)
+    x[:, 2] = torch.finfo(dtype).min
+    check(mf, x[:, 2:], gumbel(n, v - 2, v), t=ts)
+    check(mf, x[:, 2:], gumbel(n, v - 2, v), t=ts, mp=[0.0] * n)
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(mp=[0.0] * 8), dict(k=[3000] * 8), dict(p=[0.5] * 8)])
+def test_infinite_logits_at_the_ends_of_the_temperature(mf, kw):
+    """Entries of +inf share the row whatever the temperature."""
+    ts = [torch.tensor(t, dtype=torch.float32).item() for t in (math.inf, 3e38, 1.0, 1e-30, 1e-39, 1e-45, 0.0, 5.0)]
+    x = torch.randn(8, 4099, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    x[:, ::7] = -math.inf
+    x[:, 100::1000] = math.inf
+    noise = gumbel(8, 4099, 4)
+    got, lp = run(mf, x, noise, t=ts, **kw)
+    for r, t in enumerate(ts):
+        kept = [100, 1100, 2100, 3100][:1 if t == 0 else 2 if "p" in kw else 4]
+        assert got[r] == max(kept, key=lambda i: (noise[r, i].item(), -i))
+        assert abs(lp[r] + math.log(len(kept))) <= 2.0 ** -20
