@@ -824,18 +824,18 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       w = ex2(d * inv_e);
       return kept(x, i) && w >= p_lo && (w >= p_hi || expf(z_of(x, m, t)) >= min_p);
     };
-    // sum of w; the largest key; the largest with its margin, that of the exact key (the two forms of a key differ by less
-    // than 1e-6 (|z| + |noise|), and 4e-6 is allowed for), whose it is, and the second largest of them
-    float part, top, reach, reach2;
+    // sum of w; the largest key with its margin (the key and the exact one differ by less than 1e-6 (|z| + |noise|), and 4e-6 is
+    // allowed for), whose it is and its |z| + |noise|, and the second largest of them.  The key less its margin is a floor of the
+    // largest exact key; the sum of a large z and a large noise may be small, its margin is theirs.
+    float part, reach, reach2, size;
     int at;
-    auto clear = [&]() { part = 0.f, top = reach = reach2 = -INFINITY, at = -1; };
+    auto clear = [&]() { part = size = 0.f, reach = reach2 = -INFINITY, at = -1; };
     auto add = [&](float near, float w, float g, int i) {
-      const float key = near + g, far = fmaf(4e-6f, fabsf(near) + fabsf(g), key);
+      const float mag = fabsf(near) + fabsf(g), far = fmaf(4e-6f, mag, near + g);
       part += w;
-      top = fmaxf(top, key);
       const bool more = far > reach;
       reach2 = fmaxf(reach2, more ? reach : far);
-      if (more) reach = far, at = i;
+      if (more) reach = far, size = mag, at = i;
     };
     clear();
     // (the smallest x that may be in, somewhat less for the rounding)
@@ -864,8 +864,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
         if (in_with(x, base + i, near, w)) add(near, w, g, i);
       });
     }
-    sum = cluster_sum(part, top);
-    const float floor = top - 4e-6f * fabsf(top);
+    float floor = fmaf(-8e-6f, size, reach);
+    sum = cluster_sum(part, floor);
     // the entries near the largest with z as the exact quotient: a thread has one at most, if its second is not near (a reach or
     // floor that is no number: it looks at all)
     if (!(reach2 < floor)) {
@@ -873,8 +873,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
         float near, w;
         const bool in = in_with(x, base + i, near, w);
         g = fmaxf(g, -INFINITY);
-        const float key = near + g;
-        if (!in || !(key >= top || !(key + 4e-6f * (fabsf(near) + fabsf(g)) < floor))) return;
+        if (!in || fmaf(4e-6f, fabsf(near) + fabsf(g), near + g) < floor) return;
         const float z = z_of(x, m, t);
         b.take(z + g, z, base + i);
       };
@@ -900,7 +899,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
 // ---- rows by temperature alone: no entry is cut, so that one pass over logits and noise will do
 //
 // Each thread keeps the running maximum of its logits and its sum of w against that (scaled when the maximum grows), and of
-// its keys, with M / T left in (x / T + noise), the largest and the two largest with their margins: rounding aside the keys'
+// its keys, with M / T left in (x / T + noise), the two largest with their margins, as above: rounding aside the keys'
 // order needs no M.  With the row's M known, a thread whose key comes near the largest forms that one again, with z as the exact
 // quotient, or looks at all its entries where its second comes near too.  Bounded by reading logits and noise once, and by two cluster barriers a row.
 // 256 rows of 50001 fp16: 22.6 us, 3.4 TB/s (half of the copy rate: 256 blocks where 304 find room, two thirds of the issue slots
@@ -929,7 +928,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_plain(SampleCall c) {
   const float t = greedy ? 1.f : bounded(temp), inv_t = inverse(1.f, t), inv_e = inv_t * 1.4426950408889634f;
   auto up = [](T v) -> float { return fmaxf((float)v, -INFINITY); };  // NaN as -inf
   auto scaled = [&](float s, float from, float to) { return from == to ? s : s * ex2((from - to) * inv_e); };
-  float m = -INFINITY, s = 0.f, top = -INFINITY, reach = -INFINITY, reach2 = -INFINITY;
+  float m = -INFINITY, s = 0.f, reach = -INFINITY, reach2 = -INFINITY, size = 0.f;
   int first = 0x7FFFFFFF, at = 0;  // of this thread's largest, of its key with the largest reach
   constexpr int kU = 8;  // entries whose logits and noise are under way in each thread while it takes as many
   T x[kU], x2[kU];
@@ -959,14 +958,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_plain(SampleCall c) {
     const float from = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      const float v = up(x[u]), near = v * inv_t, key = near + g[u], far = fmaf(4e-6f, fabsf(near) + fabsf(g[u]), key);
+      const float v = up(x[u]), near = v * inv_t, mag = fabsf(near) + fabsf(g[u]), far = fmaf(4e-6f, mag, near + g[u]);
       s += ex2((v - from) * inv_e);
-      top = fmaxf(top, key);
       const bool more = far > reach;
       reach2 = fmaxf(reach2, more ? reach : far);
-      if (more) reach = far, at = base + k0 + u * kThreads;
+      if (more) reach = far, size = mag, at = base + k0 + u * kThreads;
     }
   }
+  float top = fmaf(-8e-6f, size, reach);  // a floor of the largest exact key
 
   // the block's, then the row's
   auto join = [&](float& am, float& as, float& atop, int& ai, float bm, float bs, float btop, int bi) {
@@ -1016,7 +1015,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_plain(SampleCall c) {
       sh.sum = num;
     }
   } else if (!greedy && m > -INFINITY) {
-    const float slack = 4e-6f * fabsf(m * inv_t), floor = top - 4e-6f * fabsf(top) - slack;
+    const float slack = 4e-6f * fabsf(m * inv_t), floor = top - slack;
     if (!(reach2 + slack < floor)) {  // (no number: look)
       for (int k0 = tid; k0 < n; k0 += kU * kThreads) {
         float x[kU], g[kU];
@@ -1028,8 +1027,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_plain(SampleCall c) {
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
           if (x[u] == -INFINITY) continue;
-          const float near = x[u] * inv_t, key = near + g[u];
-          if (!(key >= top) && key + 4e-6f * (fabsf(near) + fabsf(g[u])) + slack < floor) continue;
+          const float near = x[u] * inv_t;
+          if (fmaf(4e-6f, fabsf(near) + fabsf(g[u]), near + g[u]) + slack < floor) continue;
           const float z = z_of(x[u], m, t);
           b.take(z + g[u], z, base + k0 + u * kThreads);
         }

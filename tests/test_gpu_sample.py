@@ -425,3 +425,24 @@ def test_infinite_logits_at_the_ends_of_the_temperature(mf, kw):
         kept = [100, 1100, 2100, 3100][:1 if t == 0 else 2 if "p" in kw else 4]
         assert got[r] == max(kept, key=lambda i: (noise[r, i].item(), -i))
         assert abs(lp[r] + math.log(len(kept))) <= 2.0 ** -20
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(mp=[0.0] * 64), dict(k=[20000] * 64)])
+def test_large_z_and_noise_that_cancel(mf, kw):
+    """z + noise of a far entry comes near that of the largest although both are near 1000: what the products of z err by then is
+    a part of 1000, not of their sum."""
+    import numpy as np
+    n, v, t = 64, 50001, np.float32(1.1)
+    rng, far = np.random.default_rng(3), []
+    while len(far) < n:  # entries whose z as a product is an ulp (2^-14) above the quotient
+        x = np.float32(-rng.uniform(600, 700))
+        if np.float32(x * (np.float32(1) / t)) > np.float32(x / t):
+            far.append(x)
+    x = torch.full((n, v), -1000.0, device="cuda")
+    noise = torch.full((n, v), -100.0, device="cuda")
+    x[:, 4000], noise[:, 4000] = 0.0, 4.5e-5
+    for r, f in enumerate(far):
+        x[r, 77] = float(f)
+        noise[r, 77] = -float(np.float32(f / t))  # their sum is within half an ulp, 3.1e-5, of 0
+        assert float(f) / float(t) - float(np.float32(f / t)) < 3.2e-5
+    assert run(mf, x, noise, t=float(t), **kw)[0] == [4000] * n
