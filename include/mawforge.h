@@ -417,7 +417,7 @@ typedef struct mf_append_args {
 /* One attention call: out[t] = sum_j softmax_j(scale * q[t].k[j]) v[j] over the lines j that token t
  * sees: j < kv_len; with causal != 0 only j <= its own line; with window > 0 none that lies `window` or more
  * lines before its own.  lse (device float [n_tokens][n_heads], or NULL) receives log sum_j exp(scale * q.k[j]).
- * A token that sees no line gets out = 0 and lse = -inf.  scale is finite and above 0.  q and out as in mf_append_args; out may be q. */
+ * A token that sees no line gets out = 0 and lse = -inf, a head whose scores hold NaN (its q does) NaN in both.  scale is finite and above 0.  q and out as in mf_append_args; out may be q. */
 typedef struct mf_attn_args {
   const void* q;
   void* out;

@@ -471,12 +471,12 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
             ls += f * s_l[w][r];
           }
           if (whole) {
-            const float inv = ls > 0.f ? 1.f / ls : 0.f;
+            const float inv = ls == 0.f ? 0.f : 1.f / ls;  // (a NaN in the scores stays NaN)
             const int tok = cur.sn.sp.q0 + R / st.G, head = cur.h * st.G + R % st.G;
             T* out = static_cast<T*>(c.out) + (int64_t)tok * c.out_stride + (int64_t)head * D + col;
             *reinterpret_cast<uint2*>(out) =
                 make_uint2(Half2<T>::down(sum.x * inv, sum.y * inv), Half2<T>::down(sum.z * inv, sum.w * inv));
-            if (c.lse && col == 0) c.lse[(int64_t)tok * st.Hq + head] = ls > 0.f ? (mx + log2f(ls)) * kLn2 : -INFINITY;
+            if (c.lse && col == 0) c.lse[(int64_t)tok * st.Hq + head] = ls == 0.f ? -INFINITY : (mx + log2f(ls)) * kLn2;
           } else {
             *reinterpret_cast<float4*>(parts.o + ((int64_t)part * (MT * 16) + R) * D + col) = sum;
             if (col == 0) parts.ml[part * (MT * 16) + R] = make_float2(mx, ls);

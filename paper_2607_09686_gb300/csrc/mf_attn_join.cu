@@ -81,11 +81,11 @@ __device__ __forceinline__ void join_row(const AttnCall& c, const AttnParts& par
     }
   }
   const int R = rec.row0 + r, tok = rec.q0 + R / c.st.G, head = rec.h * c.st.G + R % c.st.G;
-  const float inv = ls > 0.f ? 1.f / ls : 0.f;
+  const float inv = ls == 0.f ? 0.f : 1.f / ls;  // (a NaN in the scores stays NaN)
   T* out = static_cast<T*>(c.out) + (int64_t)tok * c.out_stride + (int64_t)head * D + col * 4;
   *reinterpret_cast<uint2*>(out) =
       make_uint2(Half2<T>::down(sum.x * inv, sum.y * inv), Half2<T>::down(sum.z * inv, sum.w * inv));
-  if (c.lse && col == 0) c.lse[(int64_t)tok * c.st.Hq + head] = ls > 0.f ? (mx + log2f(ls)) * kLn2 : -INFINITY;
+  if (c.lse && col == 0) c.lse[(int64_t)tok * c.st.Hq + head] = ls == 0.f ? -INFINITY : (mx + log2f(ls)) * kLn2;
 }
 
 template <class T, int D, bool kOneRow, bool kTiles>

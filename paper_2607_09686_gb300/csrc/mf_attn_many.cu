@@ -506,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         if (whole) {
           // 64 columns at a time: 32 bytes of a row and lane, transposed among four lanes, so that these store 128
           // neighbouring bytes of one row after the other (a row a lane, the stores took 4000 cycles a segment)
-          const float inv = l > 0.f ? 1.f / l : 0.f;
+          const float inv = l == 0.f ? 0.f : 1.f / l;  // (a NaN in the scores stays NaN)
           const bool wide = (((uintptr_t)c.out | (uintptr_t)(c.out_stride * 2)) & 31) == 0;
           const int64_t at = ok ? (int64_t)(q0 + tok) * c.out_stride + (int64_t)head * D : -1;
           T* out[4];  // where the rows of this lane's four begin, this lane's quarter of 64 columns; null: no row
@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         if (ok) {
           const float mm = m == -INFINITY ? m : m * sc2;
           if (!whole) parts.ml[pr] = make_float2(mm, l);
-          else if (c.lse) c.lse[(int64_t)(q0 + tok) * st.Hq + head] = l > 0.f ? (mm + log2f(l)) * kLn2 : -INFINITY;
+          else if (c.lse) c.lse[(int64_t)(q0 + tok) * st.Hq + head] = l == 0.f ? -INFINITY : (mm + log2f(l)) * kLn2;
         }
         if (!two) {  // O may be written again
           tc::fence_before();

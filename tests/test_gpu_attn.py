@@ -368,3 +368,28 @@ def test_largest_windows(mf, window, new, total, causal):
     """Windows as long as their type allows hide nothing, also from tokens whose line would lie before the first."""
     c = ref.Case(new, [t - n for t, n in zip(total, new)], 8, 2, 128)
     assert torch.equal(check(mf, c, window=window, causal=causal), check(mf, c, causal=causal))
+
+
+@pytest.mark.parametrize("new,ctx", [([1, 1, 2], [40, 5, 900]), ([1], [5000]), ([90, 3, 200], [40, 5, 900]), ([40], [5000])])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_nan_in_q(mf, new, ctx, d):
+    """A token whose q holds NaN: its heads' out and lse are NaN (not the -inf of one that sees nothing), all others what they were."""
+    c = ref.Case(new, ctx, 8, 2, d)
+    at, cache, step = c.attn(mf), mf.kv_cache(c.k, c.v), c.step(mf)
+    want, _, tol, _ = ref.attention64(c, 0.1)
+    got = []
+    bad = [(0, 3), (c.tokens - 1, 0), (c.tokens // 2, 7)]
+    for _ in range(2):
+        out, lse = torch.empty(c.tokens, 8, d, dtype=c.q.dtype, device="cuda"), torch.empty(c.tokens, 8, device="cuda")
+        mf.mf_attn_forward(at, cache, step, c.q, out, lse, 0.1)
+        got.append((out, lse))
+        for t, h in bad:
+            c.q[t, h, 5] = math.nan
+    assert mf.mf_attn_check(at) == 0
+    mf.mf_attn_destroy(at)
+    hit = torch.zeros(c.tokens, 8, dtype=torch.bool, device="cuda")
+    for t, h in bad:
+        hit[t, h] = True
+    (_, lse0), (out1, lse1) = got
+    assert lse0.isfinite().all() and torch.equal(lse1.isnan(), hit) and (lse1 - lse0)[~hit].abs().max() < 1e-5
+    assert out1[hit].isnan().all() and ((out1.double() - want).abs() <= tol)[~hit].all()
