@@ -385,7 +385,9 @@ typedef struct mf_kv_cache {
  * (device int32 [n_seqs][pages_per_seq]).  max_q: no sequence adds more tokens than this (it bounds the
  * launch; the lengths themselves stay on the device, so a captured step replays with new ones).
  * Lengths, pages and positions out of range are taken as the nearest valid ones, never followed out of
- * bounds, and reported by mf_attn_check. */
+ * bounds, and reported by mf_attn_check.  So are tokens of no sequence (before q_start[0], from q_start[n_seqs] on, beyond max_q):
+ * mf_kv_append stores nothing of theirs, mf_attn_forward leaves their rows of out and lse as they are.  (A captured step
+ * with tokens to spare gives them to a sequence that has pages of its own.) */
 typedef struct mf_step {
   const int32_t *q_start, *kv_len, *pages;
   int32_t n_seqs, n_tokens, max_q, pages_per_seq;

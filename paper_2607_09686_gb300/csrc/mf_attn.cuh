@@ -56,7 +56,9 @@ __device__ __forceinline__ SeqSpan seq_span(const AttnStep& a, int s) {
   const int len0 = __ldg(a.kv_len + s);
   const int q0 = min(max(b, 0), a.n_tokens), q1 = min(max(e, q0), a.n_tokens);
   SeqSpan r = {q0, min(q1 - q0, a.max_q), min(max(len0, 0), a.cap)};
-  if (r.q0 != b || r.q0 + r.n != e || r.len != len0 || r.len < r.n) attn_report(a, kAttnRange);
+  // (tokens before the first sequence's or after the last one's are nobody's)
+  const bool nobodys = (s == 0 && b != 0) || (s + 1 == a.n_seqs && e != a.n_tokens);
+  if (r.q0 != b || r.q0 + r.n != e || r.len != len0 || r.len < r.n || nobodys) attn_report(a, kAttnRange);
   return r;
 }
 

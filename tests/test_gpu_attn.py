@@ -393,3 +393,27 @@ def test_nan_in_q(mf, new, ctx, d):
     (_, lse0), (out1, lse1) = got
     assert lse0.isfinite().all() and torch.equal(lse1.isnan(), hit) and (lse1 - lse0)[~hit].abs().max() < 1e-5
     assert out1[hit].isnan().all() and ((out1.double() - want).abs() <= tol)[~hit].all()
+
+
+@pytest.mark.parametrize("new", [[1, 3], [60, 70]])
+def test_tokens_of_no_sequence_are_reported(mf, new):
+    """Tokens before the first sequence's or after the last one's: the check says so after attention as it does after an append; their
+    rows stay, the others are right."""
+    c = ref.Case(new, [100, 7], 8, 2, 64)
+    want, _, tol, _ = ref.attention64(c, 0.1)
+    at = mf.mf_attn_create(mf.AttnShape(8, 2, 64, mf.MF_BF16), 2, c.tokens + 4, 0)
+    cache = mf.kv_cache(c.k, c.v)
+    for before, after in ((0, 4), (2, 0), (2, 2)):
+        n = before + c.tokens + after
+        q, k, v = (torch.cat((x[:before], x, x[:after])) for x in (c.q, c.new_k, c.new_v))
+        out, lse = torch.full((n, 8, 64), 7.0, dtype=c.q.dtype, device="cuda"), torch.full((n, 8), 7.0, device="cuda")
+        step = mf.step(c.q_start + before, c.kv_len, c.pages, n, c.max_q)
+        mf.mf_attn_forward(at, cache, step, q, out, lse, 0.1)
+        assert mf.mf_attn_check(at) == mf.MF_E_INVAL and mf.mf_attn_check(at) == 0
+        mine = slice(before, before + c.tokens)
+        assert ((out[mine].double() - want).abs() <= tol).all()
+        for x in (out, lse):
+            assert (x[:before] == 7).all() and (x[before + c.tokens:] == 7).all()
+        mf.mf_kv_append(at, mf.kv_cache(c.k.clone(), c.v.clone()), step, k, v)
+        assert mf.mf_attn_check(at) == mf.MF_E_INVAL
+    mf.mf_attn_destroy(at)
