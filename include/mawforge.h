@@ -497,6 +497,11 @@ typedef struct mf_sample_args {
  * dtype, n_rows < 0, a vocab out of range or a stride below it. */
 int mf_sample(const mf_sample_args_t* args, void* stream);
 
+/* Test hold of sampling.  hold = 1: blocks issue none of the copies of logits that they wait for, a second at most, in
+ * calls from now on.  A copy that does not arrive is no error: its logits are read without it, later, and the answer is the
+ * same.  hold = 0 (the default) restores normal operation.  MF_E_INVAL for other values.  Host only. */
+int mf_sample_test_hold(int hold);
+
 /* Release everything the context owns (synchronises its streams first). NULL is a no-op. */
 void mf_destroy(mf_ctx_t* ctx);
 

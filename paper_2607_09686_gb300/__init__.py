@@ -24,6 +24,7 @@ __all__ = [
     "mf_strerror", "mf_last_cuda_error",
     "MF_F32", "MF_F16", "MF_BF16", "AttnShape", "KvCache", "Step", "Rope", "kv_cache", "step", "rope", "mf_kv_bytes",
     "mf_attn_create", "mf_kv_append", "mf_attn_forward", "mf_attn_check", "mf_attn_destroy", "mf_sample",
+    "mf_sample_test_hold",
 ]
 
 Q4_0 = 2
@@ -157,6 +158,7 @@ _sig = {
     "mf_attn_check": (_i32, [_vp]),
     "mf_attn_destroy": (None, [_vp]),
     "mf_sample": (_i32, [ctypes.POINTER(_SampleArgs), _vp]),
+    "mf_sample_test_hold": (_i32, [_i32]),
     "mf_strerror": (ctypes.c_char_p, [_i32]),
     "mf_last_cuda_error": (ctypes.c_char_p, []),
 }
@@ -526,3 +528,8 @@ def mf_sample(logits, noise, token, logprob=None, temperature=None, top_k=None, 
     rc = _lib.mf_sample(a, _stream(stream))
     if rc:
         _check(rc, "mf_sample")
+
+
+def mf_sample_test_hold(hold: int) -> None:
+    """1: sampling issues none of the copies its blocks wait for (a second at most), for tests; 0: as usual."""
+    _check(_lib.mf_sample_test_hold(hold), "mf_sample_test_hold")

@@ -27,6 +27,7 @@
 // temperature alone have a kernel of their own, in one pass (k_sample_plain).
 #include <cooperative_groups.h>
 
+#include <atomic>
 #include <cfloat>
 #include <cmath>
 
@@ -56,6 +57,7 @@ struct SampleCall {
   int slice;  // entries of a block
   int qbits;  // bits of a mass unit
   int keep;   // the slice's logits lie in shared memory
+  int hold;   // (a test's) their copies are not issued
 };
 
 // larger floats have larger keys (-0 and +0 compare equal as floats: one key)
@@ -129,8 +131,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   // ---- 1. the slice into shared memory, at the same place modulo 16 bytes: whole vectors by bulk copies, the ends by hand
   auto up = [](T v) -> float { return fmaxf((float)v, -INFINITY); };  // NaN as -inf
   const T* src = row;
-  bool lost = false;  // a copy did not arrive in time: the row has no answer (as if it had no entry)
-  if (c.keep) {
+  // A copy that does not arrive in time costs time, no answer: the slice is read where it lies then.
+  bool keep = c.keep, lost = false;
+  if (keep) {
     T* x0 = reinterpret_cast<T*>(dyn + kRowAt + ((uintptr_t)row & 15));
     const int head = min(n, (int)((16 - ((uintptr_t)row & 15)) & 15) / (int)sizeof(T)),
               body = (n - head) * (int)sizeof(T) / 16 * 16 / (int)sizeof(T);
@@ -140,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       const uint32_t bytes = (uint32_t)(body * sizeof(T));
       mbar_arrive_tx(&sh.bar, bytes);
       // pieces of 32 KiB: several copies in flight
-      for (uint32_t o = 0; o < bytes; o += 32768)
+      for (uint32_t o = 0; o < bytes && !c.hold; o += 32768)
         bulk_g2s(reinterpret_cast<unsigned char*>(x0 + head) + o, reinterpret_cast<const unsigned char*>(row + head) + o, min(bytes - o, 32768u),
                  &sh.bar);
     }
@@ -150,11 +153,15 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     }
     __syncthreads();
     lost = __syncthreads_or(!mbar_wait(&sh.bar, 0, kDefaultWaitNs));
-    src = x0;
+    keep = !lost;
+    if (keep) src = x0;
   }
+  auto leave = [&]() {  // no copy may be in flight when the block exits
+    if (lost) mbar_wait(&sh.bar, 0, kDefaultWaitNs);
+  };
   // every thread's entries, f(index, logit, vector): whole vectors of the slice where it lies in shared memory
   auto for_each = [&](auto&& f) {
-    if (c.keep) {
+    if (keep) {
       constexpr int kV = 16 / sizeof(T);
       const int lead_in = (int)(((uintptr_t)src & 15) / sizeof(T)), total = lead_in + n;
       for (int v = tid; v * kV < total; v += kThreads) {
@@ -176,7 +183,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   // picked out first, then taken four by four, with what get() loads for them under way together.
   auto for_some = [&](float lo, float hi, auto&& get, auto&& f) {
     auto within = [&](float x) { return !(x < lo) && !(x > hi); };
-    if (c.keep) {
+    if (keep) {
       constexpr int kV = 16 / sizeof(T), kGroup = 64 / kV;
       const int lead_in = (int)(((uintptr_t)src & 15) / sizeof(T)), total = lead_in + n;
       const T* from = src - lead_in;
@@ -240,11 +247,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   };
   if (warp == 0) {
     mx = warp_max(lane < kWarps ? sh.f[lane] : -INFINITY);
-    if (lane == 0) sh.mx = lost ? NAN : mx;
+    if (lane == 0) sh.mx = mx;
   }
   cl.sync();
   const float theirs = lane < C ? cl.map_shared_rank(&sh, lane)->mx : -INFINITY;
-  float m = __any_sync(0xffffffffu, theirs != theirs) ? -INFINITY : warp_max(theirs);
+  const float m = warp_max(theirs);
 
   const float temp = c.temperature ? c.temperature[r] : 1.f;
   const bool greedy = !(temp > 0.f);
@@ -574,6 +581,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       c.token[r] = -1;
       if (c.logprob) c.logprob[r] = -INFINITY;
     }
+    leave();
     cl.sync();
     return;
   }
@@ -655,6 +663,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
           b = block_best(b);
           if (tid == 0) answer(b, all);
         }
+        leave();
         cl.barrier_wait();
         return;
       }
@@ -893,6 +902,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     b = warp_best(lane < C ? cl.map_shared_rank(&sh, lane)->best[kWarps] : none);
     if (lane == 0) answer(b, sum);
   }
+  leave();
   cl.sync();  // no block leaves while another reads its shared memory
 }
 
@@ -1067,6 +1077,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample_plain(SampleCall c) {
   cl.sync();  // no block leaves while another reads its shared memory
 }
 
+std::atomic<int> g_hold{0};  // mf_sample_test_hold
+
 int ceil_log2(int v) {
   int l = 0;
   while ((1 << l) < v) ++l;
@@ -1121,10 +1133,16 @@ extern "C" int mf_sample(const mf_sample_args_t* a, void* stream) {
   if (a->n_rows > 1 && (a->logits_stride < a->vocab || a->noise_stride < a->vocab)) return MF_E_INVAL;
   if (a->n_rows > (1 << 27)) return MF_E_INVAL;
   SampleCall c = {a->logits, a->noise, a->temperature, a->top_p, a->min_p, a->top_k, a->token, a->logprob,
-                  a->logits_stride, a->noise_stride, a->vocab, 0, 0, 0};
+                  a->logits_stride, a->noise_stride, a->vocab, 0, 0, 0, g_hold.load()};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t e = a->dtype == MF_F32   ? run<float>(c, a->n_rows, s)
                         : a->dtype == MF_F16 ? run<__half>(c, a->n_rows, s)
                                              : run<__nv_bfloat16>(c, a->n_rows, s);
   return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_sample");
+}
+
+extern "C" int mf_sample_test_hold(int hold) {
+  if (hold != 0 && hold != 1) return MF_E_INVAL;
+  g_hold = hold;
+  return MF_OK;
 }

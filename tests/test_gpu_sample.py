@@ -446,3 +446,30 @@ def test_large_z_and_noise_that_cancel(mf, kw):
         noise[r, 77] = -float(np.float32(f / t))  # their sum is within half an ulp, 3.1e-5, of 0
         assert float(f) / float(t) - float(np.float32(f / t)) < 3.2e-5
     assert run(mf, x, noise, t=float(t), **kw)[0] == [4000] * n
+
+
+def test_copies_that_do_not_arrive(mf):
+    """Logits that are not there within the wait's limit of a second are read without their copies: the same tokens."""
+    import time
+    n, v = 5, 50001
+    g = torch.Generator("cuda").manual_seed(41)
+    t, p, k = [1.0, 0.0, 0.8, 1.0, 1.3], [0.9003, 1.0, 0.95, 1.0, 0.5], [0, 0, 50, 5000, 0]
+    with pytest.raises(mf.MFError):
+        mf.mf_sample_test_hold(2)
+    for dtype in DT:
+        x, noise = (torch.randn(n, v, device="cuda", generator=g) * 3).to(dtype), gumbel(n, v, 6)
+        x[4] = -math.inf
+        got, took = [], []
+        for hold in range(2):
+            mf.mf_sample_test_hold(hold)
+            try:
+                t0 = time.perf_counter()
+                got.append(run(mf, x, noise, t=t, k=k, p=p))
+                took.append(time.perf_counter() - t0)
+            finally:
+                mf.mf_sample_test_hold(0)
+        assert took[0] < 0.5 and 0.9 < took[1] < 10, took
+        (token, lp), (held, held_lp) = got
+        # sums of the same numbers in another order: 2^6 additions in a thread and ten joins, each errs by 2^-24
+        assert token == held and all(a == b or abs(a - b) <= 2.0 ** -17 for a, b in zip(lp, held_lp))
+        assert token[4] == -1 and token[0] >= 0
