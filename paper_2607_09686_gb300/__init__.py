@@ -513,21 +513,47 @@ def mf_attn_destroy(attn: int) -> None:
         _lib.mf_attn_destroy(attn)
 
 
-_LOGIT_TYPES = {"torch.float32": MF_F32, "torch.float16": MF_F16, "torch.bfloat16": MF_BF16}
+class _Types:
+    """torch's types (torch is imported with the first call that takes tensors, not with this module)."""
+    f32 = i32 = None
+    codes: dict = {}
+
+    @classmethod
+    def load(cls):
+        import torch
+        cls.f32, cls.i32 = torch.float32, torch.int32
+        cls.codes = {torch.float32: MF_F32, torch.float16: MF_F16, torch.bfloat16: MF_BF16}
+
+
+def _vector(t, dtype, n: int, where: str):
+    """Address of n elements of a contiguous tensor that the GPU can reach (None and plain addresses as they are)."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not dtype or t.numel() < n or (n > 1 and not t.is_contiguous()) or not (t.is_cuda or t.is_pinned()):
+        raise MFError(MF_E_INVAL, where)
+    return t.data_ptr()
 
 
 def mf_sample(logits, noise, token, logprob=None, temperature=None, top_k=None, top_p=None, min_p=None,
               stream=None) -> None:
-    """One token from each row of logits [rows][vocab], with Gumbel noise of the same shape (see mawforge.h)."""
-    ls, ns = logits.stride(), noise.stride()
-    dtype = _LOGIT_TYPES.get(str(logits.dtype))
-    if dtype is None or len(ls) != 2 or ls[1] != 1 or ns[1] != 1 or noise.shape != logits.shape:
-        raise MFError(MF_E_INVAL, "mf_sample")
-    a = _SampleArgs(logits.data_ptr(), noise.data_ptr(), _addr(temperature), _addr(top_p), _addr(min_p), _addr(top_k),
-                    token.data_ptr(), _addr(logprob), ls[0], ns[0], logits.shape[0], logits.shape[1], dtype, 0)
+    """One token from each row of logits [rows][vocab], with Gumbel noise of the same shape (see mawforge.h).  noise,
+    temperature, top_p, min_p and logprob are float32, top_k and token int32; all but logits and noise contiguous, with an
+    element for each row at least."""
+    w = "mf_sample"
+    if not _Types.codes:
+        _Types.load()
+    f32, i32, shape, dtype = _Types.f32, _Types.i32, logits.shape, _Types.codes.get(logits.dtype)
+    if dtype is None or len(shape) != 2 or noise.shape != shape or noise.dtype is not f32:
+        raise MFError(MF_E_INVAL, w)
+    ls, ns, n = logits.stride(), noise.stride(), shape[0]
+    if ls[1] != 1 or ns[1] != 1 or not ((logits.is_cuda or logits.is_pinned()) and (noise.is_cuda or noise.is_pinned())):
+        raise MFError(MF_E_INVAL, w)
+    a = _SampleArgs(logits.data_ptr(), noise.data_ptr(), _vector(temperature, f32, n, w), _vector(top_p, f32, n, w),
+                    _vector(min_p, f32, n, w), _vector(top_k, i32, n, w), _vector(token, i32, n, w), _vector(logprob, f32, n, w),
+                    ls[0], ns[0], n, shape[1], dtype, 0)
     rc = _lib.mf_sample(a, _stream(stream))
     if rc:
-        _check(rc, "mf_sample")
+        _check(rc, w)
 
 
 def mf_sample_test_hold(hold: int) -> None:

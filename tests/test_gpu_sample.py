@@ -473,3 +473,36 @@ def test_copies_that_do_not_arrive(mf):
         # sums of the same numbers in another order: 2^6 additions in a thread and ten joins, each errs by 2^-24
         assert token == held and all(a == b or abs(a - b) <= 2.0 ** -17 for a, b in zip(lp, held_lp))
         assert token[4] == -1 and token[0] >= 0
+
+
+def test_tensors_that_do_not_fit_are_refused(mf):
+    """Other types, strides and lengths than the rows' (which would be read as what they are not, or past their end)."""
+    n, v = 4, 50
+    x, noise = torch.randn(n, v, device="cuda"), gumbel(n, v)
+    f, i = torch.ones(n, device="cuda"), torch.full((n,), 20, dtype=torch.int32, device="cuda")
+    ok = dict(logits=x, noise=noise, token=torch.full((n,), -7, dtype=torch.int32, device="cuda"), logprob=torch.empty(n, device="cuda"),
+              temperature=f, top_k=i, top_p=f * 0.9, min_p=f * 0)
+    bad = [dict(noise=noise.half()), dict(noise=noise.double()), dict(noise=noise[0]), dict(noise=noise.cpu()), dict(logits=x.cpu()),
+           dict(logits=x.int()), dict(logits=x[0])]
+    for name in ("token", "top_k"):
+        t = ok[name]
+        bad += [{name: y} for y in (t.long(), t.float(), t.short(), t[:n - 1], t.repeat_interleave(2)[::2], t[:1].expand(n), t.cpu())]
+    for name in ("logprob", "temperature", "top_p", "min_p"):
+        t = ok[name]
+        bad += [{name: y} for y in (t.double(), t.half(), t.int(), t[:n - 1], t.repeat_interleave(2)[::2], t[:1].expand(n), t.cpu())]
+    for kw in bad:
+        with pytest.raises(mf.MFError) as e:
+            mf.mf_sample(**{**ok, **kw})
+        assert e.value.status == mf.MF_E_INVAL
+    torch.cuda.synchronize()
+    assert (ok["token"] == -7).all()
+    mf.mf_sample(**ok)
+    want = ok["token"].tolist()
+    # longer ones, columns, and pinned settings serve
+    more = {k: torch.cat((t, t)) for k, t in ok.items() if t.dim() == 1}
+    mf.mf_sample(x, noise, **more)
+    column = torch.empty(n, 1, dtype=torch.int32, device="cuda")
+    mf.mf_sample(**{**ok, "token": column, "temperature": f.cpu().pin_memory()})
+    mf.mf_sample(**{**ok, "logits": x[:0], "noise": noise[:0]})
+    assert more["token"][:n].tolist() == column.view(-1).tolist() == want and (more["token"][n:] == torch.tensor(want, device="cuda")).logical_or(
+        more["token"][n:] == -7).all()
