@@ -87,6 +87,7 @@ class KvCache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
                 ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("n_pages", ctypes.c_int32),
                 ("page_size", ctypes.c_int32)]
+    kind = None  # kv heads, head_dim and type, where they are known (kv_cache)
 
 
 class Step(ctypes.Structure):
@@ -99,6 +100,7 @@ class Rope(ctypes.Structure):
     _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("pos", ctypes.c_void_p),
                 ("n_pos", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
                 ("n_axes", ctypes.c_int32), ("section", ctypes.c_int32 * 4)]
+    tokens = None  # positions of each axis, where they are known (rope)
 
 
 class _AppendArgs(ctypes.Structure):
@@ -419,20 +421,51 @@ def mf_kv_bytes(shape: AttnShape, n_layers: int, n_tokens: int, page_size: int) 
     return int(out.value)
 
 
+class _Types:
+    """torch's types (torch is imported with the first call that takes tensors, not with this module)."""
+    f32 = i32 = None
+    codes: dict = {}
+    of: dict = {}
+
+    @classmethod
+    def load(cls):
+        import torch
+        cls.f32, cls.i32 = torch.float32, torch.int32
+        cls.codes = {torch.float32: MF_F32, torch.float16: MF_F16, torch.bfloat16: MF_BF16}
+        cls.of = {code: dtype for dtype, code in cls.codes.items()}
+
+
+def _vector(t, dtype, n: int, where: str):
+    """Address of n elements of a contiguous tensor that the GPU can reach (None and plain addresses as they are)."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not dtype or t.numel() < n or (n > 1 and not t.is_contiguous()) or not (t.is_cuda or t.is_pinned()):
+        raise MFError(MF_E_INVAL, where)
+    return t.data_ptr()
+
+
 def kv_cache(k, v) -> KvCache:
     """Describe a layer's cache: k and v of shape [pages][lines][kv heads][head_dim] with the same strides, the
     last of them 1 (a page that holds its lines head by head is a transposed view)."""
     st = k.stride()
     if k.dim() != 4 or st != v.stride() or k.shape != v.shape or k.dtype != v.dtype or st[3] != 1:
         raise ValueError("k and v must be [pages][lines][heads][dim] of one dtype and stride, dim contiguous")
+    _on_gpu(k, v)
     c = KvCache(k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], k.shape[0], k.shape[1])
-    c.held = (k, v)
+    c.held, c.kind = (k, v), (k.shape[2], k.shape[3], k.dtype)
     return c
 
 
+def _on_gpu(*tensors) -> None:
+    if not all(t.is_cuda or t.is_pinned() for t in tensors):
+        raise ValueError("tensors must be on the GPU")
+
+
 def _i32_tensor(t, name: str) -> None:
-    if t is not None and (str(t.dtype) != "torch.int32" or not t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous int32 tensor")
+    if t is not None:
+        if str(t.dtype) != "torch.int32" or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 tensor")
+        _on_gpu(t)
 
 
 def step(q_start, kv_len, pages, n_tokens: int, max_q: int) -> Step:
@@ -454,6 +487,7 @@ def rope(cos, sin, pos=None, interleaved: bool = False, sections=None) -> Rope:
     if cos.shape != sin.shape or not (cos.is_contiguous() and sin.is_contiguous()) or \
             {str(cos.dtype), str(sin.dtype)} != {"torch.float32"}:
         raise ValueError("cos and sin must be contiguous float32 tensors of one shape")
+    _on_gpu(cos, sin)
     _i32_tensor(pos, "pos")
     sections = tuple(sections) if sections is not None else (cos.shape[1],)
     axes = 1 if pos is None or pos.dim() == 1 else pos.shape[0]
@@ -461,30 +495,56 @@ def rope(cos, sin, pos=None, interleaved: bool = False, sections=None) -> Rope:
         raise ValueError("one section for each of at most 4 axes")
     r = Rope(cos.data_ptr(), sin.data_ptr(), _addr(pos), cos.shape[0], 2 * cos.shape[1], int(interleaved), axes,
              (ctypes.c_int32 * 4)(*sections))
-    r.held = (cos, sin, pos)
+    r.held, r.tokens = (cos, sin, pos), None if pos is None else pos.shape[-1]
     return r
+
+
+_attn_kinds: dict = {}  # by handle: query heads, kv heads, head_dim, type; the kind of its caches
 
 
 def mf_attn_create(shape: AttnShape, max_seqs: int, max_tokens: int, device: int = 0) -> int:
     h = _vp()
     _check(_lib.mf_attn_create(ctypes.byref(h), ctypes.byref(shape), max_seqs, max_tokens, device), "mf_attn_create")
+    if not _Types.codes:
+        _Types.load()
+    dtype = _Types.of[shape.dtype]
+    _attn_kinds[h.value] = shape.n_heads, shape.n_kv_heads, shape.head_dim, dtype, (shape.n_kv_heads, shape.head_dim, dtype)
     return h.value
 
 
-def _row(t, where: str) -> int:
-    """Stride between tokens of a [tokens][heads][head_dim] tensor whose rows are contiguous."""
-    st = t.stride()
-    if len(st) != 3 or st[2] != 1 or st[1] != t.shape[2]:
+def _kind(attn: int, cache: KvCache, where: str):
+    """What is known of a handle, which the cache has to fit."""
+    kind = _attn_kinds.get(attn)
+    if kind is None or (cache.kind != kind[4] and cache.kind is not None):
         raise MFError(MF_E_INVAL, where)
-    return st[0]
+    return kind
+
+
+def _rows(t, n: int, heads: int, dim: int, dtype, where: str):
+    """(address, stride between tokens) of a [tokens][heads][head_dim] tensor of n tokens or more whose rows are contiguous."""
+    try:
+        (rows, h, d), (stride, head_stride, one) = t.shape, t.stride()
+    except ValueError:  # not three dimensions
+        raise MFError(MF_E_INVAL, where) from None
+    if rows < n or h != heads or d != dim or one != 1 or head_stride != d or t.dtype is not dtype or not (t.is_cuda or t.is_pinned()):
+        raise MFError(MF_E_INVAL, where)
+    return t.data_ptr(), stride
 
 
 def mf_kv_append(attn: int, cache: KvCache, step: Step, k, v, q=None, q_out=None, rope: Rope | None = None,
                  stream=None) -> None:
-    """Rotate q (into q_out) and k by position, and store k and v into their lines of the cache."""
+    """Rotate q (into q_out) and k by position, and store k and v into their lines of the cache.  q, q_out, k and v have
+    the handle's heads and type and the step's tokens (or more rows, which are not touched)."""
     w = "mf_kv_append"
-    a = _AppendArgs(_addr(q), k.data_ptr(), v.data_ptr(), _addr(q_out), _row(q, w) if q is not None else 0, _row(k, w),
-                    _row(v, w), _row(q_out, w) if q_out is not None else 0)
+    heads, kv_heads, dim, dtype, _ = _kind(attn, cache, w)
+    n = step.n_tokens
+    q_at, q_stride = _rows(q, n, heads, dim, dtype, w) if q is not None else (None, 0)
+    o_at, o_stride = _rows(q_out, n, heads, dim, dtype, w) if q_out is not None else (None, 0)
+    k_at, k_stride = _rows(k, n, kv_heads, dim, dtype, w)
+    v_at, v_stride = _rows(v, n, kv_heads, dim, dtype, w)
+    if rope is not None and rope.tokens is not None and (rope.tokens < n or (rope.n_axes > 1 and rope.tokens != n)):
+        raise MFError(MF_E_INVAL, w)
+    a = _AppendArgs(q_at, k_at, v_at, o_at, q_stride, k_stride, v_stride, o_stride)
     rc = _lib.mf_kv_append(attn, cache, step, rope, a, _stream(stream))
     if rc:
         _check(rc, w)
@@ -492,9 +552,14 @@ def mf_kv_append(attn: int, cache: KvCache, step: Step, k, v, q=None, q_out=None
 
 def mf_attn_forward(attn: int, cache: KvCache, step: Step, q, out, lse=None, scale: float = 1.0, window: int = 0,
                     causal: bool = True, stream=None) -> None:
-    """Attention of the step's tokens over the cache."""
+    """Attention of the step's tokens over the cache.  q and out as in mf_kv_append, lse contiguous float32 with an element for
+    each token and head at least."""
     w = "mf_attn_forward"
-    a = _AttnArgs(q.data_ptr(), out.data_ptr(), _addr(lse), _row(q, w), _row(out, w), scale, window, causal, 0)
+    heads, _, dim, dtype, _ = _kind(attn, cache, w)
+    n = step.n_tokens
+    q_at, q_stride = _rows(q, n, heads, dim, dtype, w)
+    o_at, o_stride = _rows(out, n, heads, dim, dtype, w)
+    a = _AttnArgs(q_at, o_at, _vector(lse, _Types.f32, n * heads, w), q_stride, o_stride, scale, window, causal, 0)
     rc = _lib.mf_attn_forward(attn, cache, step, a, _stream(stream))
     if rc:
         _check(rc, w)
@@ -510,28 +575,8 @@ def mf_attn_check(attn: int) -> int:
 
 def mf_attn_destroy(attn: int) -> None:
     if attn:
+        _attn_kinds.pop(attn, None)
         _lib.mf_attn_destroy(attn)
-
-
-class _Types:
-    """torch's types (torch is imported with the first call that takes tensors, not with this module)."""
-    f32 = i32 = None
-    codes: dict = {}
-
-    @classmethod
-    def load(cls):
-        import torch
-        cls.f32, cls.i32 = torch.float32, torch.int32
-        cls.codes = {torch.float32: MF_F32, torch.float16: MF_F16, torch.bfloat16: MF_BF16}
-
-
-def _vector(t, dtype, n: int, where: str):
-    """Address of n elements of a contiguous tensor that the GPU can reach (None and plain addresses as they are)."""
-    if t is None or isinstance(t, int):
-        return t
-    if t.dtype is not dtype or t.numel() < n or (n > 1 and not t.is_contiguous()) or not (t.is_cuda or t.is_pinned()):
-        raise MFError(MF_E_INVAL, where)
-    return t.data_ptr()
 
 
 def mf_sample(logits, noise, token, logprob=None, temperature=None, top_k=None, top_p=None, min_p=None,

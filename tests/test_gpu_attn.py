@@ -417,3 +417,49 @@ def test_tokens_of_no_sequence_are_reported(mf, new):
         mf.mf_kv_append(at, mf.kv_cache(c.k.clone(), c.v.clone()), step, k, v)
         assert mf.mf_attn_check(at) == mf.MF_E_INVAL
     mf.mf_attn_destroy(at)
+
+
+def test_tensors_that_do_not_fit_are_refused(mf):
+    """Other types, heads, sizes and lengths than the handle's and the step's, which would be read or written past their end."""
+    c = ref.Case([3, 1], [10, 5], 8, 2, 64)
+    at, cache, step = c.attn(mf), mf.kv_cache(c.k, c.v), c.step(mf)
+    out, lse = torch.empty(4, 8, 64, dtype=c.q.dtype, device="cuda"), torch.empty(4, 8, device="cuda")
+
+    def others(t):
+        return (t.float(), t.half(), t[:3], t[:, :-1], t[:, :, :32], t.cpu(), t.contiguous().view(4, t.shape[1] * 2, 32), t[0])
+
+    def refused(call, **kw):
+        with pytest.raises(mf.MFError) as e:
+            call(**kw)
+        assert e.value.status == mf.MF_E_INVAL
+
+    fwd = dict(attn=at, cache=cache, step=step, q=c.q, out=out, lse=lse, scale=0.1)
+    for name in ("q", "out"):
+        for t in others(fwd[name]):
+            refused(mf.mf_attn_forward, **{**fwd, name: t})
+    for t in (lse.double(), lse.half(), lse[:3], lse.repeat(1, 2)[:, ::2], lse.t().contiguous().t(), lse.cpu()):
+        refused(mf.mf_attn_forward, **{**fwd, "lse": t})
+    app = dict(attn=at, cache=cache, step=step, k=c.new_k, v=c.new_v, q=c.q, q_out=out)
+    for name in ("k", "v", "q", "q_out"):
+        for t in others(app[name]):
+            refused(mf.mf_kv_append, **{**app, name: t})
+    cos = torch.ones(64, 32, device="cuda")
+    for pos, sections in ((torch.zeros(3, dtype=torch.int32, device="cuda"), None), (torch.zeros(2, 3, dtype=torch.int32, device="cuda"), (16, 16)),
+                          (torch.zeros(2, 5, dtype=torch.int32, device="cuda"), (16, 16))):
+        refused(mf.mf_kv_append, rope=mf.rope(cos, cos, pos, sections=sections), **app)
+    for k, v in ((c.k[:, :, :1], c.v[:, :, :1]), (c.k[..., :32], c.v[..., :32]), (c.k.half(), c.v.half())):
+        refused(mf.mf_attn_forward, **{**fwd, "cache": mf.kv_cache(k, v)})
+        refused(mf.mf_kv_append, **{**app, "cache": mf.kv_cache(k, v)})
+    for make in (lambda: mf.kv_cache(c.k.cpu(), c.v.cpu()), lambda: mf.rope(cos.cpu(), cos.cpu()),
+                 lambda: mf.step(c.q_start, c.kv_len.cpu(), c.pages, 4, 3)):
+        with pytest.raises(ValueError):
+            make()
+    # more rows than the step has tokens are as good
+    want, _, tol, _ = ref.attention64(c, 0.1)
+    big = torch.full((9, 8, 64), 7.0, dtype=out.dtype, device="cuda")
+    mf.mf_attn_forward(at, cache, step, torch.cat((c.q, c.q)), big, torch.empty(100, device="cuda"), 0.1)
+    assert ((big[:4].double() - want).abs() <= tol).all() and (big[4:] == 7).all()
+    mf.mf_kv_append(at, cache, step, c.new_k, c.new_v, c.q, big, mf.rope(cos, cos, torch.zeros(9, dtype=torch.int32, device="cuda")))
+    assert mf.mf_attn_check(at) == 0
+    mf.mf_attn_destroy(at)
+    refused(mf.mf_attn_forward, **fwd)  # (a handle that is gone)
