@@ -526,7 +526,8 @@ def _rows(t, n: int, heads: int, dim: int, dtype, where: str):
         (rows, h, d), (stride, head_stride, one) = t.shape, t.stride()
     except ValueError:  # not three dimensions
         raise MFError(MF_E_INVAL, where) from None
-    if rows < n or h != heads or d != dim or one != 1 or head_stride != d or t.dtype is not dtype or not (t.is_cuda or t.is_pinned()):
+    if rows < n or h != heads or d != dim or one != 1 or (head_stride != d and h != 1) or t.dtype is not dtype or \
+            not (t.is_cuda or t.is_pinned()):
         raise MFError(MF_E_INVAL, where)
     return t.data_ptr(), stride
 

@@ -463,3 +463,14 @@ def test_tensors_that_do_not_fit_are_refused(mf):
     assert mf.mf_attn_check(at) == 0
     mf.mf_attn_destroy(at)
     refused(mf.mf_attn_forward, **fwd)  # (a handle that is gone)
+
+
+@pytest.mark.parametrize("hq,hkv", [(4, 1), (1, 1)])
+def test_one_head_of_any_head_stride(mf, hq, hkv):
+    """The stride between heads of a tensor that has one head means nothing: rows as a transpose of [head][token][dim] leaves them."""
+    c = ref.Case([3, 1], [10, 5], hq, hkv, 64)
+    turned = [x.transpose(0, 1).contiguous().transpose(0, 1) if x.shape[1] == 1 else x.contiguous() for x in (c.q, c.new_k, c.new_v)]
+    assert turned[1].stride() == (64, 256, 1)
+    c.q, c.new_k, c.new_v = turned
+    check(mf, c)
+    append(mf, c, 64)
