@@ -16,8 +16,8 @@ namespace {
 // tokens, four else, so that a thread has several loads under way): a warp finds a token's sequence (the ends at or before
 // it are counted) and its line, the threads fetch the angles' cosines and sines once for all heads, then each takes pairs
 // of 16-byte vectors of a head: the two halves of eight rotated pairs (elements j.. and j + rot / 2.., or 16 neighbours when
-// interleaved), or 16 neighbours of what is only copied.  5366 tokens of 16 + 2 x 4 heads of 256: 29.3 us, 4.6 TB/s; one
-// token: 2.6 us in a graph.
+// interleaved), or 16 neighbours of what is only copied.  5366 tokens of 16 + 2 x 4 heads of 256: 29.6 us, 4.5 TB/s; one
+// token: 2.6 to 2.8 us in a graph.
 struct AppendCall {
   AttnStep st;
   const void *q, *k, *v;
@@ -331,9 +331,11 @@ extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, cons
   const bool bf16 = attn->shape.dtype == MF_BF16;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
-  // (few rows: as many as their kernel's registers hold.  There it is the faster one: 16 sequences, window 1024, 32 rows
-  // of 128 36 us against 51, 40 rows of 64 28 against 39, 8 rows of 256 without a window 34 against 49; even, 41 against 39, for
-  // 40 rows of 64 without a window)
+  // (few rows: as many as their kernel's registers hold.  There it is the faster one, but for heads of 64 without a window.  16
+  // sequences of 4093 lines and 8 heads a kv head, in a graph, few against many, with a window of 1024 and without: 48 rows of 64
+  // 20.8 us against 31.1, 38.5 against 35.5; 32 rows of 128 21.7 against 33.2, 44.2 against 46.3; 16 rows of 256 24.2 against
+  // 42.7, 62.2 against 70.7.  One token a sequence more goes to the other kernel: 40 rows of 128 34.0 and 48.4, 24 rows of 256 43.3 and
+  // 71.9)
   if ((int64_t)c.st.max_q * c.st.G <= attn_few_rows(D)) {
     e = launch_attn_few(c, attn->parts, D, bf16, attn->sms, s);
   } else {

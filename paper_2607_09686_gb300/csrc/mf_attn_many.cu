@@ -29,8 +29,9 @@
 //
 // Measured: 2048 tokens over 14336 lines, 32/8 heads of 128, causal: 360 to 375 us, 1.4 PFLOP/s (72 % of the library's rate; the
 // tensor pipe is busy 66 % of the time, the rest is softmax and the waits between a job's two products); eight prompts of 1494 to
-// 4001 tokens, 32/4 heads of 128: 457 to 462 us, 1.13 PFLOP/s (beginnings and ends of segments); 8192 tokens, 16/8 heads of 256,
-// window 1024: 174 us, 0.74 PFLOP/s (segments of 9 to 10 key tiles, two of them masked).
+// 4001 tokens, 32/4 heads of 128: 457 to 464 us, 1.13 PFLOP/s (beginnings and ends of segments); 8192 tokens, 16/8 heads of 256,
+// window 1024: 173 us, 0.75 PFLOP/s (segments of 9 to 10 key tiles, two of them masked; 4096 tokens over 16384 without a window: 881 us,
+// 1.40 PFLOP/s).
 #include <cstring>
 
 #include "mf_attn.cuh"

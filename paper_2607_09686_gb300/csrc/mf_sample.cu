@@ -14,17 +14,18 @@
 //      in units of 2^-q, so it hangs on no order of additions; the border bin's entries are sorted as above.
 //      (Bits: a slice of 2^s entries, s >= 15, leaves q = 31 - s.  A mass is rounded up or down by a number that hangs on
 //      the entry's place alone, evenly spread: up as often as its fraction says.  So N equal logits, which to the nearest
-//      unit would all be rounded alike, N 2^-(q + 1) of an entry too much or too little, come to less than
-//      sqrt(8 N) 2^-(q + 1): 0.09 of an entry for the 2^20 of the largest vocabulary, whose q is 14, as a sum in fp32.)
+//      unit would all be rounded alike, up to N 2^-(q + 1) of an entry too much or too little, err by some sqrt(8 N) 2^-(q + 2)
+//      together: 0.05 of an entry for the 2^20 of the largest vocabulary, whose q is 14, as a sum in fp32 does.)
 //      What lies so low that it cannot hold the border is summed by ex2 alone.
 //   4. a border bin that is too large is cut by bisection over the value's 32-bit key, and equal values by counting them
 //      in the order of their index.
 //   5. what is kept: sum of w and the largest z + noise, with z as a product; then the entries that come near that one
 //      again, with z as the exact quotient.
 // What bounds it: with top-k the cluster's barriers and one pass over the slice; else passes of ten to twenty-five
-// instructions an entry.  One row of 131072 fp32, top-k of 50: 11 us, of 1000: 14 (5 of them the sort); 64 rows of 262144 bf16,
-// each with settings of its own: 52 us (rows cut by top-p alone 38, in a grid that holds 38 clusters at a time).  Rows by
-// temperature alone have a kernel of their own, in one pass (k_sample_plain).
+// instructions an entry.  One row of 131072 fp32, T = 0.8, in a graph: top-k of 50 11.2 us, of 1000 20.0 (a longer list to sort),
+// top-p of 0.9 21.9.  262144 bf16: one row 11.8, 20.5, 26.1; by top-p 38 rows, as many clusters as the GPU holds at a time, 51 and
+// 64 rows 67; 64 rows, each with settings of its own, 54.  Rows by temperature alone have a kernel of their own, in one pass
+// (k_sample_plain).
 #include <cooperative_groups.h>
 
 #include <atomic>
@@ -912,7 +913,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
 // its keys, with M / T left in (x / T + noise), the two largest with their margins, as above: rounding aside the keys'
 // order needs no M.  With the row's M known, a thread whose key comes near the largest forms that one again, with z as the exact
 // quotient, or looks at all its entries where its second comes near too.  Bounded by reading logits and noise once, and by two cluster barriers a row.
-// 256 rows of 50001 fp16: 22.6 us, 3.4 TB/s (half of the copy rate: 256 blocks where 304 find room, two thirds of the issue slots
+// 256 rows of 50001 fp16: 22.9 us, 3.4 TB/s (half of the copy rate: 256 blocks where 304 find room, two thirds of the issue slots
 // taken, 4 us of barriers and joining at the end).
 struct PlainShared {
   float m[kWarps], s[kWarps], top[kWarps];
@@ -1089,7 +1090,8 @@ template <class T>
 cudaError_t run(SampleCall c, int rows, cudaStream_t s) {
   // Blocks of a row: as many as leave each some ten thousand entries while they find room on the GPU at once (few rows),
   // at least so many that the slices stay in shared memory.  By temperature alone: no more than find room at once (256
-  // rows of 50001: one block a row 25 us, two a row 31, four 54, whose barriers leave the memory idle).
+  // rows of 50001: one block a row 25 us, two a row 31, four 54, whose barriers leave the memory idle).  152 and 304 are this
+  // GPU's SMs and the blocks that find room on them, two an SM.
   const bool plain = !c.top_k && !c.top_p && !c.min_p;
   int C = 1;
   while (C < 8 && (plain ? (int64_t)rows * C * 2 <= 304 && c.vocab / C > 8192
