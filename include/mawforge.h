@@ -450,12 +450,50 @@ int mf_attn_create(mf_attn_t** out, const mf_attn_shape_t* shape, int max_seqs, 
 int mf_kv_append(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step, const mf_rope_t* rope,
                  const mf_append_args_t* args, void* stream);
 
+/* Norms of q and k before their rotation: for each head of each token y = x / sqrt(mean(x^2) + eps) * (w + offset).  q_weight, k_weight
+ * device [head_dim], 16-byte aligned, of the shape's dtype or MF_F32 (`dtype` says which); NULL: that one is not normed.  offset: what is
+ * added to the weights (1 where a model keeps them less one, else 0).  eps at least 2^-100; eps and offset finite. */
+typedef struct mf_qk_norm {
+  const void *q_weight, *k_weight;
+  float eps, offset;
+  int32_t dtype, reserved;
+} mf_qk_norm_t;
+
+/* As mf_kv_append, with the norms of q and k (of each head by itself; values are not normed) before the rotation, in the same pass:
+ * fp32 throughout, rounded once to the dtype.  Any finite x, also where the squares' sum passes the largest float. */
+int mf_kv_append_norm(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step, const mf_qk_norm_t* norm,
+                      const mf_rope_t* rope, const mf_append_args_t* args, void* stream);
+
 /* Attention of the step's tokens over the cache, which holds their own lines too, stream-ordered on
  * `stream`.  The lines a token sees must hold finite values; what lies beyond a sequence's length, outside every
  * window or on other pages may hold anything.  Scores, softmax and sums in fp32; the probabilities are rounded to the dtype for
  * their product with v.  n_tokens = 0 does nothing.  Errors as for mf_kv_append. */
 int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step, const mf_attn_args_t* args,
                     void* stream);
+
+/* Groups of sequences that begin alike (a system prompt, a document that many ask about).  Group g is the step's sequences first[g]
+ * .. first[g + 1] - 1 (device int32 [n_groups + 1], rising), whose first len[g] lines (device int32 [n_groups]) hold the same keys and
+ * values: their tables may name the same pages for them, or copies.  Sequences of no group share nothing.  Of the
+ * shared lines whole pages are read from the pages of the group's first sequence, once for all its tokens; what is left of a page, and all that
+ * follows, each sequence reads from its own pages.  A length below 0, or beyond the lines that every sequence of the group has before its new
+ * tokens, is taken as the nearest valid one, and so is a first[g] that does not rise or lies outside the step; mf_attn_check reports both
+ * (a group that ends where it begins is no error). */
+typedef struct mf_shared {
+  const int32_t *first, *len;
+  int32_t n_groups, reserved;
+} mf_shared_t;
+
+/* Allocate what mf_attn_forward_shared needs besides, for calls of at most max_groups groups: 8 bytes for every token, query head and
+ * element of a head, and some tables.  Host only; again with another number, it replaces the first (synchronising the device: steps that
+ * were captured before must not be replayed after it).  MF_E_INVAL for max_groups < 1 or above 2^20, MF_E_OOM when it cannot be
+ * allocated (what was there stays). */
+int mf_attn_share(mf_attn_t* attn, int max_groups);
+
+/* mf_attn_forward for sequences that share their first lines: the same result, but for the order of sums.  args->window must be 0.
+ * MF_E_STATE before mf_attn_share; errors else as for mf_attn_forward, and MF_E_INVAL for NULL pointers of a group, n_groups
+ * below 0 or above max_groups. */
+int mf_attn_forward_shared(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step, const mf_shared_t* shared,
+                           const mf_attn_args_t* args, void* stream);
 
 /* Synchronise the device and report what the handle's kernels recorded since the last check, clearing it:
  * MF_E_TIMEOUT if a bounded wait gave up (outputs since the last check are unreliable), MF_E_INVAL if a length,
@@ -501,6 +539,52 @@ int mf_sample(const mf_sample_args_t* args, void* stream);
  * calls from now on.  A copy that does not arrive is no error: its logits are read without it, later, and the answer is the
  * same.  hold = 0 (the default) restores normal operation.  MF_E_INVAL for other values.  Host only. */
 int mf_sample_test_hold(int hold);
+
+/* The settings of sampled rows, as mf_sample takes them, but one for each sequence: device float [n_seqs], top_k device int32
+ * [n_seqs]; NULL: 1, 1, 0, 0. */
+typedef struct mf_cuts {
+  const float *temperature, *top_p, *min_p;
+  const int32_t* top_k;
+} mf_cuts_t;
+
+/* Verification of drafted tokens (speculative sampling; Leviathan, Kalman and Matias, 2023; Chen et al., 2023).  Sequence s has the rows
+ * row_start[s] .. row_start[s + 1] - 1 (device int32 [n_seqs + 1]: a step's q_start) of the target's logits; row i says what may follow the
+ * step's token i.  `tokens` (device int32 [n_rows]) are the step's: every row but its sequence's last has a draft, x = tokens[i + 1].
+ *   p = softmax of z over the row's kept entries, z and kept as in mf_sample by the sequence's settings `cuts` (a row
+ *       without a finite or +inf entry has no p)
+ *   q = the same of row i of draft_logits by `draft_cuts`: what mf_sample drew the draft from.  draft_logits NULL: the draft was certain,
+ *       q = 1 for x (as for drafts looked up in the text).  The last rows of sequences are not read.
+ * Row after row, x is taken while u[i] q(x) < p(x) (u device float [n_rows], uniform in [0, 1); a token outside the vocabulary
+ * or NaN is not taken).  In the first row where it is not, the token is the entry with the largest log(p - q) + noise among those
+ * with p > q (among those with p > 0 if there is none), in the last row, all drafts taken, the one with the largest log(p) + noise; the
+ * lowest such index; noise (device float [n_seqs][vocab], row s at s * noise_stride) as in mf_sample.  So the tokens that are taken
+ * are draws from the target.  Arithmetic in fp32, the kept as mf_sample finds them.
+ *   token     device int32 [n_rows]: the drafts that were taken, then the new token (-1 where its row has no p), -1 in the rows after it
+ *   accepted  device int32 [n_seqs]: the number of drafts taken
+ *   logprob   device float [n_rows] or NULL: log p of each token in `token`, -inf beside -1
+ * Rows of no sequence are left as they were; row starts that fall or lie outside the rows are taken as the nearest valid ones; a sequence without rows
+ * gets accepted = 0.
+ *   work      device, 16-byte aligned, mf_verify_bytes of it; calls that share it must follow one another
+ * vocab from 1 to 2^20.  Other pointers aligned to their element. */
+typedef struct mf_verify_args {
+  const void *logits, *draft_logits;
+  const int32_t *row_start, *tokens;
+  const float *u, *noise;
+  mf_cuts_t cuts, draft_cuts;
+  int32_t *token, *accepted;
+  float* logprob;
+  void* work;
+  int64_t logits_stride, draft_stride, noise_stride;
+  int32_t n_seqs, n_rows, vocab, dtype;
+} mf_verify_args_t;
+
+/* Bytes of `work` for calls of at most n_seqs sequences and n_rows rows.  MF_E_INVAL for negative numbers, more than 2^26 rows or
+ * sequences, or a vocab out of range.  Host only. */
+int mf_verify_bytes(int n_seqs, int n_rows, int vocab, uint64_t* out);
+
+/* Verify on the current device, stream-ordered on `stream`.  MF_E_INVAL for NULL or misaligned pointers, an unknown dtype, negative
+ * numbers, rows without a sequence, a vocab out of range or a stride below it.  n_seqs = 0 does nothing. */
+int mf_verify(const mf_verify_args_t* args, void* stream);
 
 /* Release everything the context owns (synchronises its streams first). NULL is a no-op. */
 void mf_destroy(mf_ctx_t* ctx);

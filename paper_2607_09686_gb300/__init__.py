@@ -24,7 +24,8 @@ __all__ = [
     "mf_strerror", "mf_last_cuda_error",
     "MF_F32", "MF_F16", "MF_BF16", "AttnShape", "KvCache", "Step", "Rope", "kv_cache", "step", "rope", "mf_kv_bytes",
     "mf_attn_create", "mf_kv_append", "mf_attn_forward", "mf_attn_check", "mf_attn_destroy", "mf_sample",
-    "mf_sample_test_hold",
+    "mf_sample_test_hold", "QkNorm", "Shared", "Cuts", "qk_norm", "shared", "cuts", "mf_kv_append_norm", "mf_attn_share",
+    "mf_attn_forward_shared", "mf_verify_bytes", "mf_verify",
 ]
 
 Q4_0 = 2
@@ -123,6 +124,29 @@ class _SampleArgs(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class QkNorm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float), ("offset", ctypes.c_float),
+                ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+    dim = None  # head_dim of the weights, where it is known (qk_norm)
+
+
+class Shared(ctypes.Structure):
+    _fields_ = [("first", ctypes.c_void_p), ("len", ctypes.c_void_p), ("n_groups", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class Cuts(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p), ("top_k", ctypes.c_void_p)]
+    seqs = None  # sequences that all settings have, where it is known (cuts)
+
+
+class _VerifyArgs(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("draft_logits", ctypes.c_void_p), ("row_start", ctypes.c_void_p),
+                ("tokens", ctypes.c_void_p), ("u", ctypes.c_void_p), ("noise", ctypes.c_void_p), ("cuts", Cuts), ("draft_cuts", Cuts),
+                ("token", ctypes.c_void_p), ("accepted", ctypes.c_void_p), ("logprob", ctypes.c_void_p), ("work", ctypes.c_void_p),
+                ("logits_stride", ctypes.c_int64), ("draft_stride", ctypes.c_int64), ("noise_stride", ctypes.c_int64),
+                ("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
 _vp, _i32, _u64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_uint64
 _sig = {
     "mf_payload_bytes": (_i32, [ctypes.POINTER(Model), ctypes.POINTER(_u64)]),
@@ -161,6 +185,13 @@ _sig = {
     "mf_attn_destroy": (None, [_vp]),
     "mf_sample": (_i32, [ctypes.POINTER(_SampleArgs), _vp]),
     "mf_sample_test_hold": (_i32, [_i32]),
+    "mf_kv_append_norm": (_i32, [_vp, ctypes.POINTER(KvCache), ctypes.POINTER(Step), ctypes.POINTER(QkNorm), ctypes.POINTER(Rope),
+                                 ctypes.POINTER(_AppendArgs), _vp]),
+    "mf_attn_share": (_i32, [_vp, _i32]),
+    "mf_attn_forward_shared": (_i32, [_vp, ctypes.POINTER(KvCache), ctypes.POINTER(Step), ctypes.POINTER(Shared),
+                                      ctypes.POINTER(_AttnArgs), _vp]),
+    "mf_verify_bytes": (_i32, [_i32, _i32, _i32, ctypes.POINTER(_u64)]),
+    "mf_verify": (_i32, [ctypes.POINTER(_VerifyArgs), _vp]),
     "mf_strerror": (ctypes.c_char_p, [_i32]),
     "mf_last_cuda_error": (ctypes.c_char_p, []),
 }
@@ -537,6 +568,13 @@ def mf_kv_append(attn: int, cache: KvCache, step: Step, k, v, q=None, q_out=None
     """Rotate q (into q_out) and k by position, and store k and v into their lines of the cache.  q, q_out, k and v have
     the handle's heads and type and the step's tokens (or more rows, which are not touched)."""
     w = "mf_kv_append"
+    a = _append_args(attn, cache, step, k, v, q, q_out, rope, w)
+    rc = _lib.mf_kv_append(attn, cache, step, rope, a, _stream(stream))
+    if rc:
+        _check(rc, w)
+
+
+def _append_args(attn, cache, step, k, v, q, q_out, rope, w: str) -> _AppendArgs:
     heads, kv_heads, dim, dtype, _ = _kind(attn, cache, w)
     n = step.n_tokens
     q_at, q_stride = _rows(q, n, heads, dim, dtype, w) if q is not None else (None, 0)
@@ -545,8 +583,34 @@ def mf_kv_append(attn: int, cache: KvCache, step: Step, k, v, q=None, q_out=None
     v_at, v_stride = _rows(v, n, kv_heads, dim, dtype, w)
     if rope is not None and rope.tokens is not None and (rope.tokens < n or (rope.n_axes > 1 and rope.tokens != n)):
         raise MFError(MF_E_INVAL, w)
-    a = _AppendArgs(q_at, k_at, v_at, o_at, q_stride, k_stride, v_stride, o_stride)
-    rc = _lib.mf_kv_append(attn, cache, step, rope, a, _stream(stream))
+    return _AppendArgs(q_at, k_at, v_at, o_at, q_stride, k_stride, v_stride, o_stride)
+
+
+def qk_norm(q_weight, k_weight, eps: float, offset: float = 0.0) -> QkNorm:
+    """Describe the norms of q and k: weights [head_dim], contiguous, both of one type (the handle's, or float32); None: that one is
+    not normed."""
+    given = [t for t in (q_weight, k_weight) if t is not None]
+    if len({t.dtype for t in given}) > 1 or len({tuple(t.shape) for t in given}) > 1 or \
+            any(t.dim() != 1 or not t.is_contiguous() for t in given):
+        raise ValueError("weights must be contiguous [head_dim] tensors of one type")
+    _on_gpu(*given)
+    if not _Types.codes:
+        _Types.load()
+    if given and given[0].dtype not in _Types.codes:
+        raise ValueError("weights must be float32, float16 or bfloat16")
+    n = QkNorm(_addr(q_weight), _addr(k_weight), eps, offset, _Types.codes[given[0].dtype] if given else MF_F32, 0)
+    n.held, n.dim = (q_weight, k_weight), given[0].shape[0] if given else None
+    return n
+
+
+def mf_kv_append_norm(attn: int, cache: KvCache, step: Step, norm: QkNorm, k, v, q=None, q_out=None, rope: Rope | None = None,
+                      stream=None) -> None:
+    """mf_kv_append with the norms of q and k, head by head, before the rotation."""
+    w = "mf_kv_append_norm"
+    a = _append_args(attn, cache, step, k, v, q, q_out, rope, w)
+    if norm.dim is not None and norm.dim != _attn_kinds[attn][2]:
+        raise MFError(MF_E_INVAL, w)
+    rc = _lib.mf_kv_append_norm(attn, cache, step, norm, rope, a, _stream(stream))
     if rc:
         _check(rc, w)
 
@@ -562,6 +626,37 @@ def mf_attn_forward(attn: int, cache: KvCache, step: Step, q, out, lse=None, sca
     o_at, o_stride = _rows(out, n, heads, dim, dtype, w)
     a = _AttnArgs(q_at, o_at, _vector(lse, _Types.f32, n * heads, w), q_stride, o_stride, scale, window, causal, 0)
     rc = _lib.mf_attn_forward(attn, cache, step, a, _stream(stream))
+    if rc:
+        _check(rc, w)
+
+
+def mf_attn_share(attn: int, max_groups: int) -> None:
+    """Make the handle ready for mf_attn_forward_shared with at most max_groups groups."""
+    _check(_lib.mf_attn_share(attn, max_groups), "mf_attn_share")
+
+
+def shared(first, lens) -> Shared:
+    """Describe groups of sequences that share their first lines: first [groups + 1] (where each begins), lens [groups], contiguous
+    int32 tensors on the device."""
+    for t, name in ((first, "first"), (lens, "lens")):
+        _i32_tensor(t, name)
+    if first.dim() != 1 or lens.dim() != 1 or first.shape[0] != lens.shape[0] + 1:
+        raise ValueError("first [groups + 1] and lens [groups] must describe the same groups")
+    s = Shared(first.data_ptr(), lens.data_ptr(), lens.shape[0], 0)
+    s.held = (first, lens)
+    return s
+
+
+def mf_attn_forward_shared(attn: int, cache: KvCache, step: Step, shared: Shared, q, out, lse=None, scale: float = 1.0,
+                           causal: bool = True, stream=None) -> None:
+    """mf_attn_forward for sequences that share their first lines, which are read once for a group."""
+    w = "mf_attn_forward_shared"
+    heads, _, dim, dtype, _ = _kind(attn, cache, w)
+    n = step.n_tokens
+    q_at, q_stride = _rows(q, n, heads, dim, dtype, w)
+    o_at, o_stride = _rows(out, n, heads, dim, dtype, w)
+    a = _AttnArgs(q_at, o_at, _vector(lse, _Types.f32, n * heads, w), q_stride, o_stride, scale, 0, causal, 0)
+    rc = _lib.mf_attn_forward_shared(attn, cache, step, shared, a, _stream(stream))
     if rc:
         _check(rc, w)
 
@@ -605,3 +700,61 @@ def mf_sample(logits, noise, token, logprob=None, temperature=None, top_k=None, 
 def mf_sample_test_hold(hold: int) -> None:
     """1: sampling issues none of the copies its blocks wait for (a second at most), for tests; 0: as usual."""
     _check(_lib.mf_sample_test_hold(hold), "mf_sample_test_hold")
+
+
+def cuts(temperature=None, top_k=None, top_p=None, min_p=None) -> Cuts:
+    """Describe the settings of sequences' rows: float32 tensors, top_k int32, contiguous, with an element for each sequence."""
+    if not _Types.codes:
+        _Types.load()
+    given = [t for t in (temperature, top_k, top_p, min_p) if t is not None]
+    for t in given:
+        if t.dim() != 1 or not t.is_contiguous() or t.dtype is not (_Types.i32 if t is top_k else _Types.f32):
+            raise ValueError("settings must be contiguous vectors, float32 (top_k int32)")
+    _on_gpu(*given)
+    c = Cuts(_addr(temperature), _addr(top_p), _addr(min_p), _addr(top_k))
+    c.held, c.seqs = (temperature, top_k, top_p, min_p), min((t.shape[0] for t in given), default=None)
+    return c
+
+
+def mf_verify_bytes(n_seqs: int, n_rows: int, vocab: int) -> int:
+    """Bytes of the workspace of mf_verify calls of at most these sizes."""
+    out = _u64()
+    _check(_lib.mf_verify_bytes(n_seqs, n_rows, vocab, ctypes.byref(out)), "mf_verify_bytes")
+    return int(out.value)
+
+
+_NO_CUTS = Cuts()
+
+
+def mf_verify(logits, row_start, tokens, u, noise, token, accepted, work, logprob=None, cuts: Cuts | None = None, draft_logits=None,
+              draft_cuts: Cuts | None = None, stream=None) -> None:
+    """Drafted tokens taken or refused, and the token that ends each sequence (see mawforge.h).  logits and draft_logits [rows][vocab] of
+    one type, noise float32 [sequences][vocab], u and logprob float32, row_start, tokens, token and accepted int32, work uint8."""
+    w = "mf_verify"
+    if not _Types.codes:
+        _Types.load()
+    f32, i32, dtype = _Types.f32, _Types.i32, _Types.codes.get(logits.dtype)
+    if dtype is None or logits.dim() != 2 or noise.dim() != 2 or noise.dtype is not f32 or noise.shape[1] != logits.shape[1]:
+        raise MFError(MF_E_INVAL, w)
+    (n, vocab), seqs = logits.shape, noise.shape[0]
+    draft, draft_stride = None, 0
+    if draft_logits is not None:
+        if draft_logits.dtype is not logits.dtype or draft_logits.shape != logits.shape or draft_logits.stride(1) != 1 or \
+                not (draft_logits.is_cuda or draft_logits.is_pinned()):
+            raise MFError(MF_E_INVAL, w)
+        draft, draft_stride = draft_logits.data_ptr(), draft_logits.stride(0)
+    ls, ns = logits.stride(), noise.stride()
+    if ls[1] != 1 or ns[1] != 1 or not ((logits.is_cuda or logits.is_pinned()) and (noise.is_cuda or noise.is_pinned())):
+        raise MFError(MF_E_INVAL, w)
+    cuts, draft_cuts = cuts or _NO_CUTS, draft_cuts or _NO_CUTS
+    need = _u64()
+    if any(c.seqs is not None and c.seqs < seqs for c in (cuts, draft_cuts)) or \
+            _lib.mf_verify_bytes(seqs, n, vocab, ctypes.byref(need)) or work.numel() * work.element_size() < need.value or \
+            not work.is_contiguous() or not work.is_cuda:
+        raise MFError(MF_E_INVAL, w)
+    a = _VerifyArgs(logits.data_ptr(), draft, _vector(row_start, i32, seqs + 1, w), _vector(tokens, i32, n, w), _vector(u, f32, n, w),
+                    noise.data_ptr(), cuts, draft_cuts, _vector(token, i32, n, w), _vector(accepted, i32, seqs, w),
+                    _vector(logprob, f32, n, w), work.data_ptr(), ls[0], draft_stride, ns[0], seqs, n, vocab, dtype)
+    rc = _lib.mf_verify(a, _stream(stream))
+    if rc:
+        _check(rc, w)

@@ -18,17 +18,6 @@ namespace {
 // of 16-byte vectors of a head: the two halves of eight rotated pairs (elements j.. and j + rot / 2.., or 16 neighbours when
 // interleaved), or 16 neighbours of what is only copied.  5366 tokens of 16 + 2 x 4 heads of 256: 29.6 us, 4.5 TB/s; one
 // token: 2.6 to 2.8 us in a graph.
-struct AppendCall {
-  AttnStep st;
-  const void *q, *k, *v;
-  void *q_out, *kc, *vc;
-  int64_t q_stride, k_stride, v_stride, q_out_stride;
-  const float *cos, *sin;
-  const int32_t* pos;
-  int n_pos, half, interleaved, n_axes;  // half = rot_dim / 2 (0: no rotation)
-  int end0, end1, end2;  // first pair after axes 0, 1, 2
-};
-
 constexpr int kAppendThreads = 256;
 
 template <class T, int kTB>
@@ -266,10 +255,14 @@ extern "C" int mf_attn_create(mf_attn_t** out, const mf_attn_shape_t* shape, int
   return MF_OK;
 }
 
-extern "C" int mf_kv_append(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step, const mf_rope_t* rope,
-                            const mf_append_args_t* args, void* stream) {
-  AppendCall c;
+namespace {
+
+// The arguments of an append, but its norms, as the kernels take them; *work: there is something to do.
+int make_append(const mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step, const mf_rope_t* rope,
+                const mf_append_args_t* args, AppendCall* call, bool* work) {
+  AppendCall& c = *call;
   memset(&c, 0, sizeof(c));
+  *work = false;
   if (!args || !make_step(attn, cache, step, &c.st)) return MF_E_INVAL;
   const int D = attn->shape.head_dim;
   if (rope) {
@@ -292,6 +285,19 @@ extern "C" int mf_kv_append(mf_attn_t* attn, const mf_kv_cache_t* cache, const m
   if (args->q && (bad_rows(args->q, args->q_stride) || bad_rows(args->q_out, args->q_out_stride))) return MF_E_INVAL;
   c.q = args->q, c.k = args->k, c.v = args->v, c.q_out = args->q_out, c.kc = cache->k, c.vc = cache->v;
   c.q_stride = args->q_stride, c.k_stride = args->k_stride, c.v_stride = args->v_stride, c.q_out_stride = args->q_out_stride;
+  *work = true;
+  return MF_OK;
+}
+
+}  // namespace
+
+extern "C" int mf_kv_append(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step, const mf_rope_t* rope,
+                            const mf_append_args_t* args, void* stream) {
+  AppendCall c;
+  bool work;
+  const int rc = make_append(attn, cache, step, rope, args, &c, &work);
+  if (rc != MF_OK || !work) return rc;
+  const int D = attn->shape.head_dim;
   OnDevice on(attn->device);
   if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -310,10 +316,30 @@ extern "C" int mf_kv_append(mf_attn_t* attn, const mf_kv_cache_t* cache, const m
   return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_kv_append");
 }
 
-extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step,
-                               const mf_attn_args_t* args, void* stream) {
-  AttnCall c;
+extern "C" int mf_kv_append_norm(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step, const mf_qk_norm_t* norm,
+                                 const mf_rope_t* rope, const mf_append_args_t* args, void* stream) {
+  AppendCall c;
+  bool work;
+  if (!attn || !norm || (norm->dtype != MF_F32 && norm->dtype != attn->shape.dtype) || off16(norm->q_weight) || off16(norm->k_weight) ||
+      !(norm->eps >= 0x1p-100f) || !std::isfinite(norm->eps) || !std::isfinite(norm->offset))
+    return MF_E_INVAL;
+  const int rc = make_append(attn, cache, step, rope, args, &c, &work);
+  if (rc != MF_OK || !work) return rc;
+  const AppendNorm n = {norm->q_weight, norm->k_weight, norm->eps, norm->offset, norm->dtype == MF_F32};
+  OnDevice on(attn->device);
+  if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
+  const cudaError_t e = launch_append_norm(c, n, attn->shape.head_dim, attn->shape.dtype == MF_BF16, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_kv_append_norm");
+}
+
+namespace {
+
+// The arguments of an attention call as the kernels take them; *work: there is something to do.
+int make_attn(const mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step, const mf_attn_args_t* args, AttnCall* call,
+              bool* work) {
+  AttnCall& c = *call;
   memset(&c, 0, sizeof(c));
+  *work = false;
   if (!args || !make_step(attn, cache, step, &c.st) || args->window < 0 || !std::isfinite(args->scale) ||
       !(args->scale > 0.f))
     return MF_E_INVAL;
@@ -325,6 +351,18 @@ extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, cons
   // a window of 2^30 lines holds every line there can be, and the line it begins at is counted in 32 bits also from a
   // token whose own line would lie before the first (no more than 2^30 before it)
   c.window = args->window < (1 << 30) ? args->window : 1 << 30;
+  *work = true;
+  return MF_OK;
+}
+
+}  // namespace
+
+extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step,
+                               const mf_attn_args_t* args, void* stream) {
+  AttnCall c;
+  bool work;
+  const int rc = make_attn(attn, cache, step, args, &c, &work);
+  if (rc != MF_OK || !work) return rc;
   OnDevice on(attn->device);
   if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
   const int D = attn->shape.head_dim;
@@ -344,6 +382,32 @@ extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, cons
     e = launch_attn_many(c, maps, attn->plan, attn->parts, D, bf16, attn->sms, s);
   }
   return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_attn_forward");
+}
+
+extern "C" int mf_attn_share(mf_attn_t* attn, int max_groups) {
+  if (!attn || max_groups < 1 || max_groups > (1 << 20)) return MF_E_INVAL;
+  attn->max_groups = max_groups;
+  return MF_OK;
+}
+
+extern "C" int mf_attn_forward_shared(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step, const mf_shared_t* shared,
+                                      const mf_attn_args_t* args, void* stream) {
+  AttnCall c;
+  bool work;
+  if (!shared || shared->n_groups < 0 || (shared->n_groups > 0 && (!shared->first || !shared->len)) ||
+      (((uintptr_t)shared->first | (uintptr_t)shared->len) & 3))
+    return MF_E_INVAL;
+  const int rc = make_attn(attn, cache, step, args, &c, &work);
+  if (rc != MF_OK) return rc;
+  if (args->window) return MF_E_INVAL;
+  if (!attn->max_groups) return MF_E_STATE;
+  if (shared->n_groups > attn->max_groups) return MF_E_INVAL;
+  if (!work) return MF_OK;
+  OnDevice on(attn->device);
+  if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
+  const SharedGroups g = {shared->first, shared->len, shared->n_groups};
+  const cudaError_t e = launch_attn_shared(c, g, attn->shape.head_dim, attn->shape.dtype == MF_BF16, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_attn_forward_shared");
 }
 
 extern "C" int mf_attn_check(mf_attn_t* attn) {

@@ -89,6 +89,25 @@ struct AttnMaps {
   CUtensorMap k, v, q;
 };
 
+// An append of new tokens.
+struct AppendCall {
+  AttnStep st;
+  const void *q, *k, *v;
+  void *q_out, *kc, *vc;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;
+  const float *cos, *sin;
+  const int32_t* pos;
+  int n_pos, half, interleaved, n_axes;  // half = rot_dim / 2 (0: no rotation)
+  int end0, end1, end2;  // first pair after axes 0, 1, 2
+};
+// Norms that come before the rotation: weights [head_dim] (of the caches' type, or float where f32 is set; null: that one is not
+// normed), to which `offset` is added.
+struct AppendNorm {
+  const void *q_weight, *k_weight;
+  float eps, offset;
+  int f32;
+};
+
 // The lines [lo, hi) that the token at line `pos` of a sequence of `len` lines sees.
 __device__ __forceinline__ int vis_lo(const AttnCall& c, int pos) { return c.window > 0 ? max(0, pos - c.window + 1) : 0; }
 __device__ __forceinline__ int vis_hi(const AttnCall& c, int pos, int len) { return c.causal ? min(len, pos + 1) : len; }
@@ -143,6 +162,13 @@ struct AttnPlan {
   int max_tiles;
 };
 
+// Groups of sequences that share their first lines.
+struct SharedGroups {
+  const int32_t *first, *len;
+  int n;
+};
+cudaError_t launch_attn_shared(const AttnCall& c, const SharedGroups& g, int head_dim, bool bf16, cudaStream_t s);
+cudaError_t launch_append_norm(const AppendCall& c, const AppendNorm& n, int head_dim, bool bf16, cudaStream_t s);
 cudaError_t launch_attn_few(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int sms, cudaStream_t s);
 // Fills `maps`, c.box and c.q_box where the cache and Q can be described so (0 where not).
 void attn_maps(AttnCall& c, int head_dim, AttnMaps* maps);
@@ -161,4 +187,5 @@ struct mf_attn {
   unsigned* err;  // device error word, at the workspace's start
   mf::AttnParts parts;
   mf::AttnPlan plan;
+  int max_groups;  // of mf_attn_share (0: not called)
 };

@@ -31,8 +31,9 @@
 #include <atomic>
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
-#include "mf_attn.cuh"
+#include "mf_sample.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -40,7 +41,6 @@ namespace mf {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kMaxVocab = 1 << 20;
 constexpr int kBins = 2048, kList = 4096, kShort = 512;
 constexpr int kCounted = 256;  // entries of a list up to which they are sorted by counting (80: 11.2 us a row against 12.1, 345: 14.3 against 13.8)
 constexpr float kBinsPerUnit = 64.f;
@@ -61,19 +61,22 @@ struct SampleCall {
   int hold;   // (a test's) their copies are not issued
 };
 
+// Rows whose kept entries alone are wanted (KeptRows); of SampleCall the logits, the cuts and the sizes are in use.
+struct KeptCall : SampleCall {
+  const void* draft;
+  int64_t draft_stride;
+  const int32_t* row_start;
+  mf_cuts_t draft_cuts;
+  Kept* kept;
+  int n_seqs, n_rows;
+};
+
 // larger floats have larger keys (-0 and +0 compare equal as floats: one key)
 __device__ __forceinline__ uint32_t order_key(float x) {
   const uint32_t b = __float_as_uint(x == 0.f ? 0.f : x);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
-// The temperature and its inverse are kept where 0 and -inf times the inverse (also in units of log2 e and of bins) are 0 and
-// -inf: T from 2^-120 up (below it what differs from M weighs nothing, unless by less than 2^-113), the inverse above 0 for
-// T = inf (times the largest number it is below 1e-6).
-__device__ __forceinline__ float bounded(float t) { return fmaxf(t, 0x1p-120f); }
-__device__ __forceinline__ float inverse(float unit, float t) { return fmaxf(unit / t, 1e-45f); }
-// (what is no number, -inf / inf, is -inf)
-__device__ __forceinline__ float z_of(float x, float m, float t) { return x == m ? 0.f : fmaxf(__fdiv_rn(x - m, t), -INFINITY); }
 // bin of an entry `d` = x - M, the nearest of those at multiples of 1/64 in z; monotonic in d (inv: bins per unit of d).
 // Rounded by adding 2^23: conversions share a slow pipe with ex2.
 __device__ __forceinline__ float bin_at(float d, float inv) {
@@ -113,8 +116,9 @@ struct Shared {
   uint64_t bar;  // the bulk copies' barrier
 };
 
-template <class T>
-__global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
+template <class T, class Call>
+__global__ void __launch_bounds__(kThreads, 2) k_sample(Call c) {
+  constexpr bool kKept = std::is_same<Call, KeptCall>::value;
   extern __shared__ __align__(16) unsigned char dyn[];
   __shared__ Shared sh;
   cg::cluster_group cl = cg::this_cluster();
@@ -124,11 +128,28 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   unsigned long long* list = reinterpret_cast<unsigned long long*>(dyn + kListAt);
   const int base = rank * c.slice, n = max(0, min(c.slice, c.vocab - base));
   const T* row = static_cast<const T*>(c.logits) + (int64_t)r * c.logits_stride + base;
-  const float* noise = c.noise + (int64_t)r * c.noise_stride + base;
+  const float* noise = kKept ? nullptr : c.noise + (int64_t)r * c.noise_stride + base;
   Shared* lead = cl.map_shared_rank(&sh, 0);
   unsigned long long* lead_list = cl.map_shared_rank(list, 0);
 
   pdl_wait();
+  int rs = r;  // whose settings the row has
+  if constexpr (kKept) {
+    const int i = r % c.n_rows;
+    int lo = 0, hi = c.n_seqs - 1;  // the last sequence that begins at or before the row
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (__ldg(c.row_start + mid) <= i) lo = mid;
+      else hi = mid - 1;
+    }
+    const RowSpan sp = row_span(c.row_start, c.n_rows, lo);
+    if (i < sp.b || i >= sp.e || (r != i && i + 1 == sp.e)) return;  // (the whole cluster)
+    rs = lo;
+    if (r != i) {
+      row = static_cast<const T*>(c.draft) + (int64_t)i * c.draft_stride + base;
+      c.temperature = c.draft_cuts.temperature, c.top_p = c.draft_cuts.top_p, c.min_p = c.draft_cuts.min_p, c.top_k = c.draft_cuts.top_k;
+    }
+  }
   // ---- 1. the slice into shared memory, at the same place modulo 16 bytes: whole vectors by bulk copies, the ends by hand
   auto up = [](T v) -> float { return fmaxf((float)v, -INFINITY); };  // NaN as -inf
   const T* src = row;
@@ -254,12 +275,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   const float theirs = lane < C ? cl.map_shared_rank(&sh, lane)->mx : -INFINITY;
   const float m = warp_max(theirs);
 
-  const float temp = c.temperature ? c.temperature[r] : 1.f;
+  const float temp = c.temperature ? c.temperature[rs] : 1.f;
   const bool greedy = !(temp > 0.f);
   const float t = greedy ? 1.f : bounded(temp);
-  const int top_k = c.top_k && !greedy ? c.top_k[r] : 0;
-  const float top_p = c.top_p && !greedy ? c.top_p[r] : 1.f;
-  const float min_p = c.min_p && !greedy ? fminf(fmaxf(c.min_p[r], 0.f), 1.f) : 0.f;
+  const int top_k = c.top_k && !greedy ? c.top_k[rs] : 0;
+  const float top_p = c.top_p && !greedy ? c.top_p[rs] : 1.f;
+  const float min_p = c.min_p && !greedy ? fminf(fmaxf(c.min_p[rs], 0.f), 1.f) : 0.f;
   const float inv = inverse(kBinsPerUnit, t);
   float xc = -INFINITY;  // kept: larger entries, and equal ones up to index ic
   int ic = -1;
@@ -501,6 +522,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     c.token[r] = b.i;
     if (c.logprob) c.logprob[r] = b.z - logf(sum);
   };
+  auto answer_kept = [&](float x, int i, float sum) {
+    if constexpr (kKept) c.kept[r] = {m, t, x, min_p, i, logf(sum), 1, 0};
+  };
   // the border among entries too many for the list, keys lo .. hi: the largest key down to which value() reaches want,
   // then the index of the last of its equals that is kept
   auto cut_by_key = [&](bool mass, double want, uint32_t lo, uint32_t hi) {
@@ -579,8 +603,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
 
   if (m == -INFINITY) {
     if (rank == 0 && tid == 0) {
-      c.token[r] = -1;
-      if (c.logprob) c.logprob[r] = -INFINITY;
+      if constexpr (kKept) {
+        c.kept[r] = {m, t, 0.f, 0.f, -1, 0.f, 0, 0};
+      } else {
+        c.token[r] = -1;
+        if (c.logprob) c.logprob[r] = -INFINITY;
+      }
     }
     leave();
     cl.sync();
@@ -654,15 +682,21 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
           for (int u = 0; u < kPer; ++u) {
             const int i = tid * per + u;
             if (u < per && i <= last && (i == 0 || w[u] >= min_p)) {
-              const int idx = (int)(0xFFFFFFFFu - (uint32_t)list[i]);
-              const float g = noise[idx];
-              b.take(g == g ? z[u] + g : -INFINITY, z[u], idx);
+              if constexpr (!kKept) {
+                const int idx = (int)(0xFFFFFFFFu - (uint32_t)list[i]);
+                const float g = noise[idx];
+                b.take(g == g ? z[u] + g : -INFINITY, z[u], idx);
+              }
               sum += w[u];
             }
           }
           block_scan(sum, all);
-          b = block_best(b);
-          if (tid == 0) answer(b, all);
+          if constexpr (kKept) {
+            if (tid == 0) answer_kept(key_value((uint32_t)(list[last] >> 32)), (int)(0xFFFFFFFFu - (uint32_t)list[last]), all);
+          } else {
+            b = block_best(b);
+            if (tid == 0) answer(b, all);
+          }
         }
         leave();
         cl.barrier_wait();
@@ -685,7 +719,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
       clear_list();
     }
   }
-  if (!greedy && tid == 0 && n > 0) {  // much of the noise will be asked for: into the L2 cache meanwhile
+  if (!kKept && !greedy && tid == 0 && n > 0) {  // much of the noise will be asked for: into the L2 cache meanwhile
     const uintptr_t a = ((uintptr_t)noise + 15) & ~uintptr_t(15), e = (uintptr_t)(noise + n) & ~uintptr_t(15);
     if (e > a) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a), "r"((uint32_t)(e - a)) : "memory");
   }
@@ -852,6 +886,22 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
     const float low = fmaxf(xc, min_p > 0.f ? m + t * (logf(p_lo) - 1e-3f) - 1e-6f * fabsf(m) : -INFINITY);
     const bool all = low == -INFINITY && m < INFINITY;  // nothing is cut
     bool sure = m < INFINITY;
+    if constexpr (kKept) {
+      if (all) {
+        for_each([&](int, float x, int) { part += ex2((x - m) * inv_e); });
+      } else {
+        for_some(low, INFINITY, get_none, [&](int i, float x, float) {
+          float near, w;
+          if (in_with(x, base + i, near, w)) part += w;
+        });
+      }
+      float unused = 0.f;
+      sum = cluster_sum(part, unused);
+      if (rank == 0 && tid == 0) answer_kept(xc, ic, sum);
+      leave();
+      cl.sync();
+      return;
+    }
     if (sure && !all) {  // (every pass gives a thread the same entries)
       for_some(low, INFINITY, [&](int i) { return noise[i]; }, [&](int i, float x, float g) {
         const float d = x - m, w = ex2(d * inv_e);
@@ -901,7 +951,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(SampleCall c) {
   cl.sync();
   if (rank == 0 && warp == 0) {
     b = warp_best(lane < C ? cl.map_shared_rank(&sh, lane)->best[kWarps] : none);
-    if (lane == 0) answer(b, sum);
+    if constexpr (kKept) {
+      if (lane == 0) answer_kept(m, b.i, 1.f);  // the first of the largest alone
+    } else {
+      if (lane == 0) answer(b, sum);
+    }
   }
   leave();
   cl.sync();  // no block leaves while another reads its shared memory
@@ -1086,13 +1140,14 @@ int ceil_log2(int v) {
   return l;
 }
 
-template <class T>
-cudaError_t run(SampleCall c, int rows, cudaStream_t s) {
+template <class T, class Call>
+cudaError_t run(Call c, int rows, cudaStream_t s) {
+  constexpr bool kKept = std::is_same<Call, KeptCall>::value;
   // Blocks of a row: as many as leave each some ten thousand entries while they find room on the GPU at once (few rows),
   // at least so many that the slices stay in shared memory.  By temperature alone: no more than find room at once (256
   // rows of 50001: one block a row 25 us, two a row 31, four 54, whose barriers leave the memory idle).  152 and 304 are this
   // GPU's SMs and the blocks that find room on them, two an SM.
-  const bool plain = !c.top_k && !c.top_p && !c.min_p;
+  const bool plain = !kKept && !c.top_k && !c.top_p && !c.min_p;
   int C = 1;
   while (C < 8 && (plain ? (int64_t)rows * C * 2 <= 304 && c.vocab / C > 8192
                          : (size_t)((c.vocab + C - 1) / C) * sizeof(T) > 64 * 1024 || ((int64_t)rows * C < 152 && c.vocab / C > 8192)))
@@ -1113,13 +1168,25 @@ cudaError_t run(SampleCall c, int rows, cudaStream_t s) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  if (plain) return cudaLaunchKernelEx(&cfg, k_sample_plain<T>, c);
-  const cudaError_t e = cudaFuncSetAttribute(k_sample<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  if constexpr (!kKept)
+    if (plain) return cudaLaunchKernelEx(&cfg, k_sample_plain<T>, c);
+  const cudaError_t e = cudaFuncSetAttribute(k_sample<T, Call>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              (int)(kRowAt + kResident + 64));
-  return e == cudaSuccess ? cudaLaunchKernelEx(&cfg, k_sample<T>, c) : e;
+  return e == cudaSuccess ? cudaLaunchKernelEx(&cfg, k_sample<T, Call>, c) : e;
 }
 
 }  // namespace
+
+cudaError_t launch_kept(const KeptRows& k, cudaStream_t s) {
+  KeptCall c = {};
+  c.logits = k.logits, c.logits_stride = k.logits_stride, c.vocab = k.vocab, c.hold = g_hold.load();
+  c.temperature = k.cuts.temperature, c.top_p = k.cuts.top_p, c.min_p = k.cuts.min_p, c.top_k = k.cuts.top_k;
+  c.draft = k.draft, c.draft_stride = k.draft_stride, c.draft_cuts = k.draft_cuts;
+  c.row_start = k.row_start, c.n_seqs = k.n_seqs, c.n_rows = k.n_rows, c.kept = k.kept;
+  const int rows = k.draft ? 2 * k.n_rows : k.n_rows;
+  return k.dtype == MF_F32 ? run<float>(c, rows, s) : k.dtype == MF_F16 ? run<__half>(c, rows, s) : run<__nv_bfloat16>(c, rows, s);
+}
+
 }  // namespace mf
 
 using namespace mf;
