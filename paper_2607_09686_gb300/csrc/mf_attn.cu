@@ -239,9 +239,9 @@ extern "C" int mf_attn_create(mf_attn_t** out, const mf_attn_shape_t* shape, int
   unsigned char* ws = nullptr;
   if (e == cudaSuccess) e = tiles < (1u << 30) ? cudaMalloc(&ws, w.off) : cudaErrorMemoryAllocation;
   h->err = reinterpret_cast<unsigned*>(ws + o_err);
-  h->parts = {reinterpret_cast<float*>(ws + o_o), reinterpret_cast<float2*>(ws + o_ml), reinterpret_cast<AttnRec*>(ws + o_rec)};
+  h->parts = {reinterpret_cast<float*>(ws + o_o), reinterpret_cast<float2*>(ws + o_ml), reinterpret_cast<AttnRec*>(ws + o_rec), nullptr, nullptr};
   h->plan = {reinterpret_cast<int*>(ws + o_first), reinterpret_cast<int4*>(ws + o_tile), reinterpret_cast<int64_t*>(ws + o_before),
-             (int)tiles};
+             (int)tiles, 0};
   if (e == cudaSuccess) e = cudaMemset(h->err, 0, 256);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) {
@@ -386,7 +386,35 @@ extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, cons
 
 extern "C" int mf_attn_share(mf_attn_t* attn, int max_groups) {
   if (!attn || max_groups < 1 || max_groups > (1 << 20)) return MF_E_INVAL;
-  attn->max_groups = max_groups;
+  OnDevice on(attn->device);
+  if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
+  const mf_attn_shape_t& sh = attn->shape;
+  const int64_t rows = (int64_t)attn->max_tokens * sh.n_heads, group_rows = rows / sh.n_kv_heads, tile = attn_tile_rows(sh.head_dim);
+  const int64_t tiles = 2 * (group_rows / tile) + attn->max_seqs + max_groups, part_rows = (int64_t)attn->sms * 2 * tile;
+  Carve w;
+  const size_t o_bound = w.take(((size_t)max_groups + 1) * 4), o_group = w.take((size_t)max_groups * 16),
+               o_seq = w.take((size_t)attn->max_seqs * 8), o_first = w.take(((size_t)attn->max_seqs + max_groups + 1) * 4),
+               o_tile = w.take((size_t)tiles * 32), o_before = w.take(((size_t)tiles + 1) * 8),
+               o_o = w.take((size_t)part_rows * sh.head_dim * 4), o_ml = w.take((size_t)part_rows * 8),
+               o_whole = w.take((size_t)rows * 2 * sh.head_dim * 4), o_whole_ml = w.take((size_t)rows * 2 * 8);
+  unsigned char* ws = nullptr;
+  cudaError_t e = tiles < (1 << 30) ? cudaMalloc(&ws, w.off) : cudaErrorMemoryAllocation;
+  if (e == cudaSuccess) e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) {
+    const int rc = cuda_fail(e, "mf_attn_share");
+    cudaGetLastError();
+    cudaFree(ws);
+    return rc;
+  }
+  cudaFree(attn->shared.mem);
+  AttnShared& a = attn->shared;
+  a.max_groups = max_groups;
+  a.mem = ws;
+  a.found = {reinterpret_cast<int*>(ws + o_bound), reinterpret_cast<int4*>(ws + o_group), reinterpret_cast<int2*>(ws + o_seq)};
+  a.plan = {reinterpret_cast<int*>(ws + o_first), reinterpret_cast<int4*>(ws + o_tile), reinterpret_cast<int64_t*>(ws + o_before),
+            (int)tiles, 0};
+  a.parts = {reinterpret_cast<float*>(ws + o_o), reinterpret_cast<float2*>(ws + o_ml), nullptr, reinterpret_cast<float*>(ws + o_whole),
+             reinterpret_cast<float2*>(ws + o_whole_ml)};
   return MF_OK;
 }
 
@@ -400,13 +428,16 @@ extern "C" int mf_attn_forward_shared(mf_attn_t* attn, const mf_kv_cache_t* cach
   const int rc = make_attn(attn, cache, step, args, &c, &work);
   if (rc != MF_OK) return rc;
   if (args->window) return MF_E_INVAL;
-  if (!attn->max_groups) return MF_E_STATE;
-  if (shared->n_groups > attn->max_groups) return MF_E_INVAL;
+  if (!attn->shared.max_groups) return MF_E_STATE;
+  if (shared->n_groups > attn->shared.max_groups) return MF_E_INVAL;
   if (!work) return MF_OK;
   OnDevice on(attn->device);
   if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
   const SharedGroups g = {shared->first, shared->len, shared->n_groups};
-  const cudaError_t e = launch_attn_shared(c, g, attn->shape.head_dim, attn->shape.dtype == MF_BF16, static_cast<cudaStream_t>(stream));
+  AttnMaps maps;
+  attn_maps(c, attn->shape.head_dim, &maps);
+  const cudaError_t e = launch_attn_shared(c, maps, g, attn->shared, attn->shape.head_dim, attn->shape.dtype == MF_BF16, attn->sms,
+                                           static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_attn_forward_shared");
 }
 
@@ -426,6 +457,7 @@ extern "C" void mf_attn_destroy(mf_attn_t* attn) {
   if (!attn) return;
   OnDevice on(attn->device);
   cudaDeviceSynchronize();
+  cudaFree(attn->shared.mem);
   cudaFree(attn->err);
   delete attn;
 }

@@ -147,6 +147,10 @@ struct AttnParts {
   float* o;     // [parts][rows][head_dim] (few rows) or [parts][head_dim / 4][rows][4] (tiles), not yet divided by l
   float2* ml;   // [parts][rows]  running maximum (log2 domain) and sum
   AttnRec* rec;  // [blocks]
+  // Of a step whose groups share lines, what blocks have whole of the groups' rows and then of the sequences', each [kv heads][tokens *
+  // heads of a group]: o of a row tile as [head_dim / 4][its rows][4] where its rows begin.
+  float* whole;
+  float2* whole_ml;
 };
 constexpr int kMaxParts = 1024; // pieces of one record
 int attn_few_blocks(int sms);
@@ -160,20 +164,35 @@ struct AttnPlan {
                     //                 sequence's tiles, rows, first and end of the lines that any of them sees
   int64_t* before;  // [max_tiles + 1] jobs (of one kv head) before the tile
   int max_tiles;
+  int groups;       // virtual sequences before the step's (k_attn_plan_shared)
 };
 
-// Groups of sequences that share their first lines.
+// Groups of sequences that share their first lines (mf_shared_t), and what k_attn_plan_shared finds of them.
 struct SharedGroups {
   const int32_t *first, *len;
   int n;
 };
-cudaError_t launch_attn_shared(const AttnCall& c, const SharedGroups& g, int head_dim, bool bf16, cudaStream_t s);
+struct SharedPlan {
+  int* bound;   // [max_groups + 1] first sequence of a group
+  int4* group;  // [max_groups]     that, its first token, tokens (0: nothing is shared), lines that are shared
+  int2* seq;    // [max_seqs]       a sequence's group (-1: none), the lines it shares
+};
+// What mf_attn_share allots.
+struct AttnShared {
+  int max_groups;  // 0: it was not called
+  unsigned char* mem;
+  SharedPlan found;
+  AttnPlan plan;
+  AttnParts parts;
+};
 cudaError_t launch_append_norm(const AppendCall& c, const AppendNorm& n, int head_dim, bool bf16, cudaStream_t s);
 cudaError_t launch_attn_few(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int sms, cudaStream_t s);
 // Fills `maps`, c.box and c.q_box where the cache and Q can be described so (0 where not).
 void attn_maps(AttnCall& c, int head_dim, AttnMaps* maps);
 cudaError_t launch_attn_many(const AttnCall& c, const AttnMaps& maps, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
                              cudaStream_t s);
+cudaError_t launch_attn_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& groups, const AttnShared& sh, int head_dim, bool bf16,
+                               int sms, cudaStream_t s);
 // the records of `blocks` blocks joined; rows: rows of a part; tiles: left by launch_attn_many
 cudaError_t launch_attn_join(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int rows, bool tiles, int blocks,
                              cudaStream_t s);
@@ -187,5 +206,5 @@ struct mf_attn {
   unsigned* err;  // device error word, at the workspace's start
   mf::AttnParts parts;
   mf::AttnPlan plan;
-  int max_groups;  // of mf_attn_share (0: not called)
+  mf::AttnShared shared;
 };

@@ -131,6 +131,140 @@ __global__ void __launch_bounds__(1024) k_attn_plan(AttnCall c, AttnPlan p) {
   if (tid == 0) p.before[tiles] = jobs;
 }
 
+// The same of a step whose groups of sequences share their first lines: as many virtual sequences as there are groups, with the rows of
+// all the group's tokens and the shared lines (whole pages of them), then the sequences, with what follows.  First the groups: bounds
+// that rise, lengths that all their sequences have; a group of one shares nothing.
+template <int D>
+__global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGroups g, AttnPlan p, SharedPlan sp) {
+  __shared__ int64_t s_warp[32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int V = g.n + c.st.n_seqs;
+  pdl_wait();
+  pdl_trigger();
+  auto scan = [&](int64_t v, int64_t& all) -> int64_t {  // exclusive prefix over the block, and the sum
+    int64_t x = v;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t o = __shfl_up_sync(0xffffffffu, x, d);
+      if (lane >= d) x += o;
+    }
+    __syncthreads();
+    if (lane == 31) s_warp[warp] = x;
+    __syncthreads();
+    int64_t before = 0;
+    all = 0;
+    for (int w = 0; w < 32; ++w) {
+      if (w < warp) before += s_warp[w];
+      all += s_warp[w];
+    }
+    return before + x - v;
+  };
+  // ---- the groups' bounds: the largest so far, inside the step
+  int from = 0;
+  for (int base = 0; base <= g.n; base += 1024) {
+    const int i = base + tid;
+    const int raw = i <= g.n && g.n ? __ldg(g.first + i) : 0;
+    int x = min(max(raw, 0), c.st.n_seqs);
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, x, d);
+      if (lane >= d) x = max(x, o);
+    }
+    __syncthreads();
+    if (lane == 31) s_warp[warp] = x;
+    __syncthreads();
+    int most = from;
+    for (int w = 0; w < 32; ++w) {
+      if (w < warp) x = max(x, (int)s_warp[w]);
+      most = max(most, (int)s_warp[w]);
+    }
+    x = max(x, from);
+    from = most;
+    if (i <= g.n) {
+      sp.bound[i] = x;
+      if (x != raw) attn_report(c.st, kAttnRange);
+    }
+  }
+  for (int s = tid; s < c.st.n_seqs; s += 1024) sp.seq[s] = make_int2(-1, 0);
+  __syncthreads();
+  // ---- their lengths: some lanes a group
+  int width = 32;
+  while (width > 1 && (int64_t)width * g.n > 1024) width >>= 1;
+  const int per = 1024 / width, sub = tid % width;
+  for (int base = 0; base < g.n; base += per) {
+    const int i = base + tid / width;
+    int a = 0, b = 0, least = 0x7FFFFFFF;
+    if (i < g.n) a = sp.bound[i], b = sp.bound[i + 1];
+    for (int s = a + sub; s < b; s += width) {
+      const SeqSpan q = seq_span(c.st, s);
+      least = min(least, q.len - q.n);
+    }
+    for (int d = 1; d < width; d <<= 1) least = min(least, __shfl_xor_sync(0xffffffffu, least, d));
+    if (i < g.n) {
+      const int asked = __ldg(g.len + i), len = max(0, min(asked, least));
+      if (len != asked && sub == 0 && a < b) attn_report(c.st, kAttnRange);
+      const int lines = b - a > 1 ? (int)fast_div((uint32_t)len, c.st.page_mul, c.st.page_shift) * c.st.page_size : 0;
+      int q0 = 0, n = 0;
+      if (lines) {
+        const SeqSpan x = seq_span(c.st, a), y = seq_span(c.st, b - 1);
+        q0 = x.q0, n = max(y.q0 + y.n - q0, 0);
+      }
+      if (sub == 0) sp.group[i] = make_int4(a, q0, n, lines);
+      for (int s = a + sub; s < b; s += width) sp.seq[s] = make_int2(n ? i : -1, n ? lines : 0);
+    }
+  }
+  __syncthreads();
+  // ---- row tiles of the virtual sequences
+  int64_t done = 0;
+  for (int base = 0; base < V; base += 1024) {
+    const int v = base + tid;
+    int64_t n = 0, all;
+    if (v < V) {
+      const int tokens = v < g.n ? sp.group[v].z : seq_span(c.st, v - g.n).n;
+      n = ((int64_t)tokens * c.st.G + Cfg<D>::kRows - 1) / Cfg<D>::kRows;
+    }
+    const int64_t at = done + scan(n, all);
+    if (v < V) p.first[v] = (int)min(at, (int64_t)p.max_tiles);
+    done += all;
+  }
+  const int tiles = (int)min(done, (int64_t)p.max_tiles);
+  if (tid == 0) p.first[V] = tiles;
+  __syncthreads();
+  int64_t jobs = 0;
+  for (int base = 0; base < tiles; base += 1024) {
+    const int i = base + tid;
+    int64_t n = 0;
+    if (i < tiles) {
+      int lo = 0, hi = V - 1;  // the last virtual sequence whose first tile is at or before i
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (p.first[mid] <= i) lo = mid;
+        else hi = mid - 1;
+      }
+      const int qt = i - p.first[lo], R0 = qt * Cfg<D>::kRows, G = c.st.G;
+      int s, start, end, rows;
+      SeqSpan q;
+      if (lo < g.n) {
+        const int4 x = sp.group[lo];
+        s = x.x, q = {x.y, x.z, x.w};
+        rows = min(Cfg<D>::kRows, q.n * G - R0), start = 0, end = x.w;
+      } else {
+        s = lo - g.n, q = seq_span(c.st, s);
+        rows = min(Cfg<D>::kRows, q.n * G - R0), start = sp.seq[s].y;
+        end = max(start, vis_hi(c, q.len - q.n + (R0 + rows - 1) / G, q.len));
+      }
+      p.tile[2 * i] = make_int4(s, q.q0, q.n, q.len);
+      p.tile[2 * i + 1] = make_int4(qt, rows, start, end);
+      n = ((int64_t)max(1, (end - start + kKeys - 1) / kKeys) << (Cfg<D>::kRowTiles == 2 && rows > 128)) + Cfg<D>::kOver;
+    }
+    int64_t all;
+    const int64_t at = jobs + scan(n, all);
+    if (i < tiles) p.before[i] = at;
+    jobs += all;
+  }
+  if (tid == 0) p.before[tiles] = jobs;
+}
+
 // The walk over a block's segments: key tiles j0 .. j1 - 1 of a row tile (of all: `tile`) and kv head h.  The list is
 // ordered by sequence, kv head, row tile.  The next tile's description is asked for when the walk comes to a segment, and
 // has long arrived when the segment ends.  The roles' loops together have to fit the instruction cache (with walks that
@@ -227,8 +361,10 @@ struct Jobs {
 
 // What the softmax needs of a segment, told by the warp that copies K: it comes to a segment a few key tiles ahead, and the
 // softmax, which has no registers to walk with, finds it in shared memory.
+constexpr int kGroupRows = 1 << 29;
 struct Piece {
   int nj, two, k_start, R0, rows, h, q0, first, len, nt, j0, more;
+  // (first: line of the sequence's first new token; kGroupRows: the rows are a group's, all of which see all its lines)
   int64_t last;  // place of the last key tile's first job
   template <int kRows, int kOver>
   __device__ __forceinline__ void take(const Walk<kRows, kOver>& w) {
@@ -303,7 +439,9 @@ struct Tail {
   int flag;
 };
 
-template <class T, int D>
+// kShared: a step whose groups share lines (k_attn_plan_shared).  Every piece is left as a partial, a whole one in its rows' place of
+// parts.whole, and k_attn_join_shared adds up those of the group's lines and those of the sequence's.
+template <class T, int D, bool kShared>
 __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant__ AttnCall c, const __grid_constant__ AttnMaps maps,
                                                            const __grid_constant__ AttnPlan p,
                                                            const __grid_constant__ AttnParts parts) {
@@ -331,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
   pdl_wait();
   pdl_trigger();
 
-  const int tiles = __ldg(p.first + st.n_seqs);
+  const int groups = kShared ? p.groups : 0, tiles = __ldg(p.first + groups + st.n_seqs);
   const int64_t total = tiles ? __ldg(p.before + tiles) * st.Hkv : 0;
   // every block that works has at least two jobs, so that it has a key tile's start
   const int64_t B = max((int64_t)1, min((int64_t)gridDim.x, total / 2));
@@ -473,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
           if (lane == 0) mbar_arrive(&bars[kBP2 + wg * 2 + buf]);
         }
         if (!alive) break;
-        if (tid == 0 && cur.j0 == 0 && nj != cur.nt) {
+        if (!kShared && tid == 0 && cur.j0 == 0 && nj != cur.nt) {
           // the block of the segment's last key tile, by the place of its first job
           rec_n = (int)((B * (cur.last + 1) - 1) / total) - (int)b + 1;
           parts.rec[b] = {cur.q0, cur.h, cur.R0, cur.rows, rec_n};
@@ -499,10 +637,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         oph ^= 1;
         tc::fence_after();
         const int R = cur.R0 + tile_row, tok = R / st.G, q0 = cur.q0, h = cur.h, j0 = cur.j0;
-        const bool whole = nj == cur.nt;
+        const bool whole = !kShared && nj == cur.nt, placed = kShared && nj == cur.nt;
         // partials column group by column group, so that a warp's rows are neighbours
         const int64_t pr0 = ((int64_t)b * 2 + (j0 == 0)) * C::kRows, pr = pr0 + tile_row;
         float* po = parts.o + pr0 * D + tile_row * 4;
+        int64_t po_step = C::kRows * 4, pm = pr;
+        if (placed) {  // the rows' place: kv head by kv head, token by token, a tile's like a partial of as many rows as it has
+          const int64_t base = (cur.first == kGroupRows ? 0 : (int64_t)st.n_tokens * st.Hq) + ((int64_t)h * st.n_tokens + q0) * st.G + cur.R0;
+          po = parts.whole + base * D + tile_row * 4;
+          po_step = cur.rows * 4;
+          pm = base + tile_row;
+        }
         const int head = h * st.G + R % st.G;
         if (whole) {
           // 64 columns at a time: 32 bytes of a row and lane, transposed among four lanes, so that these store 128
@@ -564,13 +709,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
             if (!ok) continue;
 #pragma unroll
             for (int u = 0; u < 8; ++u)
-              *reinterpret_cast<uint4*>(po + (int64_t)(i * 8 + u) * (C::kRows * 4)) =
+              *reinterpret_cast<uint4*>(po + (i * 8 + u) * po_step) =
                   make_uint4(o[4 * u], o[4 * u + 1], o[4 * u + 2], o[4 * u + 3]);
           }
         }
         if (ok) {
           const float mm = m == -INFINITY ? m : m * sc2;
-          if (!whole) parts.ml[pr] = make_float2(mm, l);
+          if (kShared) (placed ? parts.whole_ml : parts.ml)[pm] = make_float2(mm, l);
+          else if (!whole) parts.ml[pr] = make_float2(mm, l);
           else if (c.lse) c.lse[(int64_t)(q0 + tok) * st.Hq + head] = l == 0.f ? -INFINITY : (mm + log2f(l)) * kLn2;
         }
         if (!two) {  // O may be written again
@@ -584,7 +730,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
       if (lane == 0) mbar_arrive(&bars[kBPieceFree + at]);
       if (++at == kPieces) at = 0, pph ^= 1;
     }
-    if (tid == 0 && rec_n == 0) parts.rec[b].n = 0;
+    if (!kShared && tid == 0 && rec_n == 0) parts.rec[b].n = 0;
   } else if (warp <= kPvWarp) {
     // ================= MMA issue: the whole warp walks the jobs, one elected lane issues.  Operands of an MMA come from
     // uniform registers: what they derive from is read from one lane, so that the compiler knows it to be uniform (moved
@@ -760,11 +906,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     walk_start(w0, c, p, tiles, t0, t1);
     Walk<C::kRows, C::kOver> w = w0;
     int told = 0;
+    const int group_tiles = kShared ? __ldg(p.first + groups) : 0;
     uint32_t tph = 1;
     auto tell = [&]() -> bool {  // the softmax what comes
       if (!wait_free(kBPieceFree + told, tph)) return false;
       if (lane == 0) {
         tail.piece[told].take(w);
+        if (kShared && w.tile < group_tiles) tail.piece[told].first = kGroupRows;
         mbar_arrive(&bars[kBPiece + told]);
       }
       __syncwarp();
@@ -863,19 +1011,103 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
   if (warp == kQkWarp) tc::dealloc(tmem, kTmemCols);
 }
 
+// ---- the joined result of a step whose groups share lines
+
+// A block: some rows of a sequence's row tile and a kv head.  A row's pieces are the group's (in the order of the lines) and then the
+// sequence's own; where they lie follows from the plan: the block of a tile's first key tile to that of its last.  Four columns a thread.
+constexpr int kJoinRows = 16, kJoinThreads = 256;
 template <class T, int D>
-cudaError_t run(const AttnCall& c, const AttnMaps& maps, AttnPlan plan, const AttnParts& parts, int sms, cudaStream_t s) {
+__global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_constant__ AttnCall c, const __grid_constant__ AttnPlan p,
+                                                                   const __grid_constant__ SharedPlan sp,
+                                                                   const __grid_constant__ AttnParts parts, int blocks) {
+  using C = Cfg<D>;
+  const AttnStep& st = c.st;
+  const int h = blockIdx.y, r0 = blockIdx.z * kJoinRows, tid = threadIdx.x;
+  pdl_wait();
+  const int tile = __ldg(p.first + p.groups) + (int)blockIdx.x, tiles = __ldg(p.first + p.groups + st.n_seqs);
+  if (tile >= tiles) return;
+  const int4 ta = __ldg(p.tile + 2 * tile), tb = __ldg(p.tile + 2 * tile + 1);
+  const int rows = min(kJoinRows, tb.y - r0);
+  if (rows <= 0) return;
+  const int64_t total = __ldg(p.before + tiles) * st.Hkv, B = max((int64_t)1, min((int64_t)blocks, total / 2));
+  // the pieces of a tile: blocks b .. b + n - 1
+  struct Run {
+    int64_t b;
+    int n;
+  };
+  auto run_of = [&](int i, int v, int4 x) -> Run {
+    const int f = __ldg(p.first + v), e = __ldg(p.first + v + 1);
+    const int64_t b0 = __ldg(p.before + f), at = b0 * st.Hkv + h * (__ldg(p.before + e) - b0) + __ldg(p.before + i) - b0 + C::kOver;
+    const int nt = max(1, (x.w - x.z + kKeys - 1) / kKeys), two = x.y > 128;
+    const int64_t b = (B * (at + 1) - 1) / total, l = (B * (at + ((int64_t)(nt - 1) << two) + 1) - 1) / total;
+    return {b, (int)(l - b) + 1};
+  };
+  const Run own = run_of(tile, p.groups + ta.x, tb);
+  const int group = __ldg(&sp.seq[ta.x].x);
+  int4 g = make_int4(0, 0, 0, 0);
+  if (group >= 0) g = __ldg(sp.group + group);
+  for (int i = tid; i < rows * (D / 4); i += kJoinThreads) {
+    const int r = r0 + i % rows, col = i / rows, R = tb.x * C::kRows + r;
+    const int tok = ta.y + R / st.G, head = h * st.G + R % st.G;
+    float mx = -INFINITY, ls = 0.f;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float2 ml, float4 o) {
+      const float to = fmaxf(mx, ml.x), ms = to == -INFINITY ? 0.f : to, f = exp2f(mx - ms), w = exp2f(ml.x - ms);
+      sum.x = sum.x * f + w * o.x, sum.y = sum.y * f + w * o.y, sum.z = sum.z * f + w * o.z, sum.w = sum.w * f + w * o.w;
+      ls = ls * f + w * ml.y;
+      mx = to;
+    };
+    auto add_run = [&](const Run& run, int64_t place, int tile_rows, int row) {  // place: of the tile's rows, where it is whole
+      if (run.n == 1) {
+        add(parts.whole_ml[place + row], *reinterpret_cast<const float4*>(parts.whole + place * D + ((int64_t)col * tile_rows + row) * 4));
+      } else {
+#pragma unroll 4
+        for (int k = 0; k < run.n; ++k) {
+          const int64_t part = (k == 0 ? run.b * 2 + 1 : (run.b + k) * 2) * C::kRows;
+          add(parts.ml[part + row], *reinterpret_cast<const float4*>(parts.o + part * D + (col * C::kRows + row) * 4));
+        }
+      }
+    };
+    if (g.z) {
+      const int64_t at = (int64_t)(tok - g.y) * st.G + R % st.G;  // the row among the group's
+      const int qt = (int)(at / C::kRows), i0 = __ldg(p.first + group) + qt;
+      if (at >= 0 && at < (int64_t)g.z * st.G && i0 < __ldg(p.first + group + 1)) {
+        const int4 x = __ldg(p.tile + 2 * i0 + 1);
+        add_run(run_of(i0, group, x), ((int64_t)h * st.n_tokens + g.y) * st.G + (int64_t)qt * C::kRows, x.y, (int)(at - (int64_t)qt * C::kRows));
+      }
+    }
+    add_run(own, (int64_t)st.n_tokens * st.Hq + ((int64_t)h * st.n_tokens + ta.y) * st.G + tb.x * C::kRows, tb.y, r);
+    const float inv = ls == 0.f ? 0.f : 1.f / ls;  // (a NaN in the scores stays NaN)
+    T* out = static_cast<T*>(c.out) + (int64_t)tok * c.out_stride + (int64_t)head * D + col * 4;
+    *reinterpret_cast<uint2*>(out) = make_uint2(Half2<T>::down(sum.x * inv, sum.y * inv), Half2<T>::down(sum.z * inv, sum.w * inv));
+    if (c.lse && col == 0) c.lse[(int64_t)tok * st.Hq + head] = ls == 0.f ? -INFINITY : (mx + log2f(ls)) * kLn2;
+  }
+}
+
+template <class T, int D>
+cudaError_t run(const AttnCall& c, const AttnMaps& maps, AttnPlan plan, const AttnParts& parts, const SharedGroups* groups,
+                const SharedPlan* shared, int sms, cudaStream_t s) {
   using C = Cfg<D>;
   const int64_t rows = (int64_t)c.st.n_tokens * c.st.G;
-  const int64_t tiles = rows / C::kRows + c.st.n_seqs;
+  const int64_t own = rows / C::kRows + c.st.n_seqs, tiles = own + (groups ? rows / C::kRows + groups->n : 0);
   plan.max_tiles = tiles < plan.max_tiles ? (int)tiles : plan.max_tiles;
+  plan.groups = groups ? groups->n : 0;
   const int64_t most = tiles * c.st.Hkv * (((int64_t)c.st.cap + kKeys - 1) / kKeys);
   const unsigned grid = (unsigned)(most < sms ? most : sms);
   constexpr size_t smem = C::kTail + sizeof(Tail);
   static_assert(smem <= 232448, "shared memory of a block");
-  cudaError_t e = cudaFuncSetAttribute(k_attn_many<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e == cudaSuccess) e = launch_pdl(true, k_attn_plan<D>, dim3(1), dim3(1024), 0, s, c, plan);
-  if (e == cudaSuccess) e = launch_pdl(true, k_attn_many<T, D>, dim3(grid), dim3(kThreads), smem, s, c, maps, plan, parts);
+  auto kernel = groups ? k_attn_many<T, D, true> : k_attn_many<T, D, false>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e == cudaSuccess)
+    e = groups ? launch_pdl(true, k_attn_plan_shared<D>, dim3(1), dim3(1024), 0, s, c, *groups, plan, *shared)
+               : launch_pdl(true, k_attn_plan<D>, dim3(1), dim3(1024), 0, s, c, plan);
+  if (e == cudaSuccess) e = launch_pdl(true, kernel, dim3(grid), dim3(kThreads), smem, s, c, maps, plan, parts);
+  if (e == cudaSuccess && groups) {
+    const int64_t held = (int64_t)c.st.max_q * c.st.G;
+    const int in_tile = (int)(held < C::kRows ? held : C::kRows);
+    const dim3 g((unsigned)own, (unsigned)c.st.Hkv, (unsigned)((in_tile + kJoinRows - 1) / kJoinRows));
+    return launch_pdl(true, k_attn_join_shared<T, D>, g, dim3(kJoinThreads), 0, s, c, plan, *shared, parts, (int)grid);
+  }
   if (e == cudaSuccess && grid > 1) e = launch_attn_join(c, parts, D, Half2<T>::kBf16, C::kRows, true, (int)grid, s);
   return e;
 }
@@ -922,15 +1154,26 @@ void attn_maps(AttnCall& c, int head_dim, AttnMaps* maps) {
 
 int attn_tile_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
 
+namespace {
+cudaError_t pick(const AttnCall& c, const AttnMaps& maps, const AttnPlan& plan, const AttnParts& parts, const SharedGroups* groups,
+                 const SharedPlan* shared, int head_dim, bool bf16, int sms, cudaStream_t s) {
+  if (bf16)
+    return head_dim == 64    ? run<__nv_bfloat16, 64>(c, maps, plan, parts, groups, shared, sms, s)
+           : head_dim == 128 ? run<__nv_bfloat16, 128>(c, maps, plan, parts, groups, shared, sms, s)
+                             : run<__nv_bfloat16, 256>(c, maps, plan, parts, groups, shared, sms, s);
+  return head_dim == 64    ? run<__half, 64>(c, maps, plan, parts, groups, shared, sms, s)
+         : head_dim == 128 ? run<__half, 128>(c, maps, plan, parts, groups, shared, sms, s)
+                           : run<__half, 256>(c, maps, plan, parts, groups, shared, sms, s);
+}
+}  // namespace
+
 cudaError_t launch_attn_many(const AttnCall& c, const AttnMaps& maps, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
                              cudaStream_t s) {
-  if (bf16)
-    return head_dim == 64    ? run<__nv_bfloat16, 64>(c, maps, plan, parts, sms, s)
-           : head_dim == 128 ? run<__nv_bfloat16, 128>(c, maps, plan, parts, sms, s)
-                             : run<__nv_bfloat16, 256>(c, maps, plan, parts, sms, s);
-  return head_dim == 64    ? run<__half, 64>(c, maps, plan, parts, sms, s)
-         : head_dim == 128 ? run<__half, 128>(c, maps, plan, parts, sms, s)
-                           : run<__half, 256>(c, maps, plan, parts, sms, s);
+  return pick(c, maps, plan, parts, nullptr, nullptr, head_dim, bf16, sms, s);
+}
+cudaError_t launch_attn_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& groups, const AttnShared& sh, int head_dim, bool bf16,
+                               int sms, cudaStream_t s) {
+  return pick(c, maps, sh.plan, sh.parts, &groups, &sh.found, head_dim, bf16, sms, s);
 }
 
 }  // namespace mf
