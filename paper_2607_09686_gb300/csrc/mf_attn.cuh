@@ -164,7 +164,7 @@ struct AttnPlan {
                     //                 sequence's tiles, rows, first and end of the lines that any of them sees
   int64_t* before;  // [max_tiles + 1] jobs (of one kv head) before the tile
   int max_tiles;
-  int groups;       // virtual sequences before the step's (k_attn_plan_shared)
+  int groups, seqs;  // of a step whose groups share lines: the virtual sequences of the list, groups and then sequences
 };
 
 // Groups of sequences that share their first lines (mf_shared_t), and what k_attn_plan_shared finds of them.
@@ -176,16 +176,33 @@ struct SharedPlan {
   int* bound;   // [max_groups + 1] first sequence of a group
   int4* group;  // [max_groups]     that, its first token, tokens (0: nothing is shared), lines that are shared
   int2* seq;    // [max_seqs]       a sequence's group (-1: none), the lines it shares
+  // the list of launch_attn_few_shared: a (virtual) sequence's first new token, new tokens, end and beginning of its lines; the
+  // places before it
+  int4* span;       // [max_groups + max_seqs]
+  int64_t* before;  // [max_groups + max_seqs + 1]
 };
+// A step whose groups share lines, as launch_attn_few_shared takes it.
+struct FewShared {
+  const int4 *span, *group;
+  const int64_t* before;
+  int groups;  // virtual sequences before the step's
+  int wait;    // the kernel before this one is the plan
+  int blocks;
+};
+constexpr int kFewTile = 64, kFewOver = 3;  // lines of a tile, tiles that a (sequence, head) costs besides its own
 // What mf_attn_share allots.
 struct AttnShared {
   int max_groups;  // 0: it was not called
   unsigned char* mem;
   SharedPlan found;
   AttnPlan plan;
-  AttnParts parts;
+  AttnParts parts, few;  // of the two kernels, which may run side by side (what is whole: one place)
 };
 cudaError_t launch_append_norm(const AppendCall& c, const AppendNorm& n, int head_dim, bool bf16, cudaStream_t s);
+int attn_few_part_rows(int rows);            // rows of a part of launch_attn_few_shared for that many rows
+int attn_few_fit(int head_dim, int sms);     // its blocks that find room at once
+cudaError_t launch_attn_few_shared(const AttnCall& c, const AttnParts& parts, const FewShared& shared, int rows, int head_dim, bool bf16,
+                                   int sms, cudaStream_t s);
 cudaError_t launch_attn_few(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int sms, cudaStream_t s);
 // Fills `maps`, c.box and c.q_box where the cache and Q can be described so (0 where not).
 void attn_maps(AttnCall& c, int head_dim, AttnMaps* maps);

@@ -21,6 +21,8 @@
 // Measured: 64 sequences of 166 to 8192 lines, 32/4 heads of 128, 395 MB: 74.5 us with the join, 5.3 TB/s (78 % of the copy
 // rate; that rate once it runs, 6 us before the first lines are there); one sequence of 131071 lines, 16/2 heads of 256:
 // 54.9 us, 4.9 TB/s; one of 1001 lines: 9.8 us, of which 5 are this kernel's and the rest the join's and the launches'.
+#include <type_traits>
+
 #include "mf_attn.cuh"
 
 namespace mf {
@@ -29,7 +31,8 @@ namespace {
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kUnit = 16;               // lines a warp takes at once
 constexpr int kTile = kWarps * kUnit;   // lines of a tile
-constexpr int kOver = 3;                // tiles that a (sequence, head) costs besides its own
+constexpr int kOver = kFewOver;         // tiles that a (sequence, head) costs besides its own
+static_assert(kTile == kFewTile, "the plan of shared steps counts these tiles");
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 template <int D>
@@ -45,7 +48,10 @@ struct Cfg {
 struct Span {
   SeqSpan sp;
   int start, nt;
+  int skip, row;  // of a step whose groups share lines: lines before this one are the group's; whose row of the page table it has
 };
+// What such a step brings besides (FewShared); nothing for others.
+struct Alone {};
 __device__ __forceinline__ Span span_of(const AttnCall& c, int s) {
   Span r;
   r.sp = seq_span(c.st, s);
@@ -55,20 +61,33 @@ __device__ __forceinline__ Span span_of(const AttnCall& c, int s) {
   return r;
 }
 
+__device__ __forceinline__ Span span_of(const AttnCall& c, const Alone&, int s) { return span_of(c, s); }
+__device__ __forceinline__ Span span_of(const AttnCall&, const FewShared& f, int v) {
+  const int4 x = __ldg(f.span + v);
+  Span r;
+  r.sp = {x.x, x.y, x.z};
+  r.skip = x.w;
+  r.start = x.w & ~(kUnit - 1);
+  r.nt = x.y == 0 ? 0 : max(1, (x.z - r.start + kTile - 1) / kTile);
+  r.row = v < f.groups ? __ldg(f.group + v).x : v - f.groups;
+  return r;
+}
+
 // a place in a block's share of the list
+template <class Extra>
 struct Cursor {
   Span sn;
   int s, h, j, j_end;   // tile j of this (sequence, head), which the block has to j_end
   int64_t at, t1;       // the place of its first (empty) tile in the list, the end of the share
   __device__ __forceinline__ void limit() { j_end = (int)max((int64_t)0, min((int64_t)sn.nt, t1 - at - kOver)); }
-  __device__ __forceinline__ void next(const AttnCall& c) {
+  __device__ __forceinline__ void next(const AttnCall& c, const Extra& x) {
     if (++j < j_end) return;
     at += sn.nt + kOver;
     j = j_end = 0;
     if (at + kOver >= t1) return;  // (nothing of what follows is this block's)
     if (++h == c.st.Hkv) {
       h = 0;
-      do sn = span_of(c, ++s);  // (there is one with tiles: the list goes on)
+      do sn = span_of(c, x, ++s);  // (there is one with tiles: the list goes on)
       while (sn.nt == 0);
     }
     limit();
@@ -108,9 +127,10 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <class T, int D, int MT>
-__global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(AttnCall c, AttnParts parts) {
+template <class T, int D, int MT, class Extra>
+__global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(AttnCall c, AttnParts parts, Extra extra) {
   using C = Cfg<D>;
+  constexpr bool kShared = std::is_same<Extra, FewShared>::value;
   constexpr int kS = C::kStages, kSteps = D / 16, kChunks = D / 8, kRowsPer = 32 / (kChunks < 32 ? kChunks : 32);
   constexpr bool kQShared = MT * kSteps > 12;  // the query rows in shared memory, registers being short
   constexpr int kChains = MT == 1 ? 2 : 1;  // independent sums of a score: enough products in flight either way
@@ -121,65 +141,88 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
   __shared__ float s_m[kWarps][16], s_l[kWarps][16];
   const AttnStep& st = c.st;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  pdl_wait();
-
-  // ---- this block's share [t0, t1) of the list, and where it starts
-  auto cost_of = [&](int s) -> int64_t {  // of a kv head of sequence s
-    if (s >= st.n_seqs) return 0;
-    const int nt = span_of(c, s).nt;
-    return nt ? nt + kOver : 0;
-  };
-  int64_t total = 0;
-  for (int base = 0; base < st.n_seqs; base += kThreads) total += cost_of(base + tid);
-#pragma unroll
-  for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-  if (lane == 0) s_sum[warp] = total;
-  __syncthreads();
-  total = (s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]) * st.Hkv;
-  const int64_t B = min((int64_t)gridDim.x, total);
-  if (tid == 0) parts.rec[blockIdx.x].n = 0;
-  if (blockIdx.x >= B) return;
-  const int64_t t0 = total * blockIdx.x / B, t1 = total * (blockIdx.x + 1) / B;
-  {
-    int64_t before = 0;  // tiles of the sequences before these
-    for (int base = 0; base < st.n_seqs; base += kThreads) {
-      const int64_t nt = cost_of(base + tid) * st.Hkv;
-      int64_t pre = nt;  // inclusive prefix
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int64_t o = __shfl_up_sync(0xffffffffu, pre, d);
-        if (lane >= d) pre += o;
-      }
-      __syncthreads();
-      if (lane == 31) s_sum[warp] = pre;
-      __syncthreads();
-      int64_t round = 0, mine = before;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) mine += s_sum[w];
-        round += s_sum[w];
-      }
-      pre += mine;
-      if (nt && t0 >= pre - nt && t0 < pre) s_seq = base + tid, s_at = pre - nt;
-      before += round;
-      if (t0 < before) break;
+  int64_t total = 0, B, t0, t1;
+  if constexpr (kShared) {
+    // The plan, which was there before this launch's blocks could start, has the places of the (virtual) sequences.  Where the
+    // kernel before this one is that of the groups' lines, nothing of it is waited for until the end.
+    if (extra.wait) pdl_wait();
+    const int V = extra.groups + st.n_seqs;
+    total = __ldg(extra.before + V);
+    B = min((int64_t)gridDim.x, total);
+    if (blockIdx.x >= B) {
+      if (!extra.wait) pdl_wait();
+      return;
+    }
+    t0 = total * blockIdx.x / B, t1 = total * (blockIdx.x + 1) / B;
+    for (int v = tid; v < V; v += kThreads) {
+      const int64_t at = __ldg(extra.before + v);
+      if (t0 >= at && t0 < __ldg(extra.before + v + 1)) s_seq = v, s_at = at;
     }
     __syncthreads();
+  } else {
+    pdl_wait();
+
+    // ---- this block's share [t0, t1) of the list, and where it starts
+    auto cost_of = [&](int s) -> int64_t {  // of a kv head of sequence s
+      if (s >= st.n_seqs) return 0;
+      const int nt = span_of(c, s).nt;
+      return nt ? nt + kOver : 0;
+    };
+    for (int base = 0; base < st.n_seqs; base += kThreads) total += cost_of(base + tid);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+    if (lane == 0) s_sum[warp] = total;
+    __syncthreads();
+    total = (s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]) * st.Hkv;
+    B = min((int64_t)gridDim.x, total);
+    if (tid == 0) parts.rec[blockIdx.x].n = 0;
+    if (blockIdx.x >= B) return;
+    t0 = total * blockIdx.x / B, t1 = total * (blockIdx.x + 1) / B;
+    {
+      int64_t before = 0;  // tiles of the sequences before these
+      for (int base = 0; base < st.n_seqs; base += kThreads) {
+        const int64_t nt = cost_of(base + tid) * st.Hkv;
+        int64_t pre = nt;  // inclusive prefix
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+          const int64_t o = __shfl_up_sync(0xffffffffu, pre, d);
+          if (lane >= d) pre += o;
+        }
+        __syncthreads();
+        if (lane == 31) s_sum[warp] = pre;
+        __syncthreads();
+        int64_t round = 0, mine = before;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          if (w < warp) mine += s_sum[w];
+          round += s_sum[w];
+        }
+        pre += mine;
+        if (nt && t0 >= pre - nt && t0 < pre) s_seq = base + tid, s_at = pre - nt;
+        before += round;
+        if (t0 < before) break;
+      }
+      __syncthreads();
+    }
   }
-  Cursor cur;
+  Cursor<Extra> cur;
   cur.s = s_seq;
-  cur.sn = span_of(c, cur.s);
+  cur.sn = span_of(c, extra, cur.s);
   cur.h = (int)((t0 - s_at) / (cur.sn.nt + kOver));
   cur.at = s_at + (int64_t)cur.h * (cur.sn.nt + kOver);
   cur.t1 = t1;
   cur.j = (int)max((int64_t)0, t0 - cur.at - kOver);
   cur.limit();
   pdl_trigger();  // k_attn_join's blocks may start to wait
-  if (!cur.live()) return;  // (a share of empty tiles alone)
+  if (!cur.live()) {  // (a share of empty tiles alone)
+    if constexpr (kShared)
+      if (!extra.wait) pdl_wait();
+    return;
+  }
 
   // ---- the copies' side, kS units ahead
   const uint32_t slots = smem_u32(smem) + warp * (kS * C::kSlot);
-  Cursor ld = cur;
+  Cursor<Extra> ld = cur;
   // Where pages hold a multiple of 8 lines, lane L knows where the halves of unit L of 32 begin, from tile `win` of the
   // (sequence, head) on, else lane L % 16 where that line of the unit to copy lies.
   const bool whole_pages = st.page_size % 8 == 0;
@@ -189,7 +232,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
   auto look_up = [&]() {
     if (!ld.live()) return;
     const int line0 = ld.sn.start + ld.j * kTile + warp * kUnit, len = ld.sn.sp.len;
-    const int lo = c.window > 0 ? max(0, len - ld.sn.sp.n - c.window + 1) : 0;
+    const int lo = kShared ? ld.sn.skip : c.window > 0 ? max(0, len - ld.sn.sp.n - c.window + 1) : 0;
+    const int seq = kShared ? ld.sn.row : ld.s;
     lo_at = lo - line0, hi_at = len - line0;
     if (whole_pages) {
       if (fresh_win || ld.j - win >= 32) {
@@ -197,13 +241,13 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
         win = ld.j;
         const int line = line0 + lane * kTile;
         if (ld.j + lane < ld.j_end) {
-          if (line < len && line + 8 > lo) line_at = line_offset(st, ld.s, line) + (int64_t)ld.h * st.head_stride;
-          if (line + 8 < len) half_at = line_offset(st, ld.s, line + 8) + (int64_t)ld.h * st.head_stride;
+          if (line < len && line + 8 > lo) line_at = line_offset(st, seq, line) + (int64_t)ld.h * st.head_stride;
+          if (line + 8 < len) half_at = line_offset(st, seq, line + 8) + (int64_t)ld.h * st.head_stride;
         }
       }
     } else {
       const int line = line0 + (lane & 15);
-      if (line >= lo && line < len) line_at = line_offset(st, ld.s, line) + (int64_t)ld.h * st.head_stride;
+      if (line >= lo && line < len) line_at = line_offset(st, seq, line) + (int64_t)ld.h * st.head_stride;
     }
   };
   const int sub = lane / kChunks, ch = lane % kChunks;  // this lane's line (of kRowsPer) and chunk in a copy
@@ -252,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
       }
       if (is_v) {
         const int64_t was = ld.at;
-        ld.next(c);
+        ld.next(c, extra);
         if (ld.at != was) fresh_win = true;
         look_up();
       }
@@ -285,8 +329,10 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
         for (int u = 0; u < 2; ++u) {
           const int r = t * 16 + lane / 4 + 8 * u, i = r / st.G, pos = cur.sn.sp.len - cur.sn.sp.n + i;
           const bool ok = r < cur.sn.sp.n * st.G;
-          lo[t][u] = vis_lo(c, pos);
+          lo[t][u] = kShared ? cur.sn.skip : vis_lo(c, pos);
           hi[t][u] = ok ? vis_hi(c, pos, cur.sn.sp.len) : 0;
+          if constexpr (kShared)  // (a group's rows see all its lines)
+            if (ok && cur.s < extra.groups) hi[t][u] = cur.sn.sp.len;
           m[t][u] = -INFINITY, l[t][u] = 0.f;
           if constexpr (!kQShared) {
             const T* q = static_cast<const T*>(c.q) + (int64_t)(cur.sn.sp.q0 + (ok ? i : 0)) * c.q_stride +
@@ -434,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
       const bool whole = j0 == 0 && cur.j_end == cur.sn.nt;
       const int part = blockIdx.x * 2 + (j0 == 0);  // a piece that starts before this block is its first
       const int rows = cur.sn.sp.n * st.G;
-      if (j0 == 0 && !whole && tid == 0) {  // the block of the last tile has the last piece
+      if (!kShared && j0 == 0 && !whole && tid == 0) {  // the block of the last tile has the last piece
         const int64_t end = cur.at + kOver + cur.sn.nt;
         parts.rec[blockIdx.x] = {cur.sn.sp.q0, cur.h, 0, rows, (int)((B * end - 1) / total) - (int)blockIdx.x + 1};
       }
@@ -470,7 +516,16 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
             sum.x += f * v.x, sum.y += f * v.y, sum.z += f * v.z, sum.w += f * v.w;
             ls += f * s_l[w][r];
           }
-          if (whole) {
+          if constexpr (kShared) {
+            if (whole) {
+              const int64_t row = (cur.s < extra.groups ? 0 : (int64_t)st.n_tokens * st.Hq) + (int64_t)(cur.sn.sp.q0 + R / st.G) * st.Hq +
+                                  cur.h * st.G + R % st.G;
+              *reinterpret_cast<float4*>(parts.whole + row * D + col) = sum;
+              if (col == 0) parts.whole_ml[row] = make_float2(mx, ls);
+              continue;
+            }
+          }
+          if (!kShared && whole) {
             const float inv = ls == 0.f ? 0.f : 1.f / ls;  // (a NaN in the scores stays NaN)
             const int tok = cur.sn.sp.q0 + R / st.G, head = cur.h * st.G + R % st.G;
             T* out = static_cast<T*>(c.out) + (int64_t)tok * c.out_stride + (int64_t)head * D + col;
@@ -489,38 +544,56 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
     }
     copy_half(vb, c.v, true);
     if (++slot == kS) slot = 0;
-    cur.next(c);
+    cur.next(c, extra);
   }
+  if constexpr (kShared)
+    if (!extra.wait) pdl_wait();  // (what comes after this launch may rely on the one before it)
 }
 
 template <class T, int D, int MT>
-cudaError_t run(const AttnCall& c, const AttnParts& parts, int sms, cudaStream_t s) {
+cudaError_t run(const AttnCall& c, const AttnParts& parts, const FewShared* shared, int sms, cudaStream_t s) {
   // no more blocks than tiles there can be: the lengths are on the device, the pages they fit in are known
   const int64_t most = (int64_t)c.st.n_seqs * c.st.Hkv * (((int64_t)c.st.cap + kTile - 1) / kTile);
   const int64_t fit = (int64_t)sms * Cfg<D>::kBlocksPerSm;
-  const unsigned grid = (unsigned)(most < fit ? most : fit);
+  unsigned grid = (unsigned)(most < fit ? most : fit);
   constexpr size_t smem = Cfg<D>::kSmem + MT * 16 * Cfg<D>::kRow;  // the pipelines, the query rows
-  cudaError_t e = cudaFuncSetAttribute(k_attn_few<T, D, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e == cudaSuccess) e = launch_pdl(true, k_attn_few<T, D, MT>, dim3(grid), dim3(kThreads), smem, s, c, parts);
+  if (shared) {
+    auto kernel = k_attn_few<T, D, MT, FewShared>;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    return e == cudaSuccess ? launch_pdl(true, kernel, dim3((unsigned)shared->blocks), dim3(kThreads), smem, s, c, parts, *shared) : e;
+  }
+  auto kernel = k_attn_few<T, D, MT, Alone>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e == cudaSuccess) e = launch_pdl(true, kernel, dim3(grid), dim3(kThreads), smem, s, c, parts, Alone{});
   if (e == cudaSuccess && grid > 1) e = launch_attn_join(c, parts, D, Half2<T>::kBf16, MT * 16, false, (int)grid, s);
   return e;
 }
 
 template <class T>
-cudaError_t pick(const AttnCall& c, const AttnParts& parts, int head_dim, int sms, cudaStream_t s) {
-  const int rows = c.st.max_q * c.st.G;
-  if (head_dim == 256) return run<T, 256, 1>(c, parts, sms, s);
-  if (head_dim == 128) return rows <= 16 ? run<T, 128, 1>(c, parts, sms, s) : run<T, 128, 2>(c, parts, sms, s);
-  return rows <= 16 ? run<T, 64, 1>(c, parts, sms, s) : rows <= 32 ? run<T, 64, 2>(c, parts, sms, s) : run<T, 64, 3>(c, parts, sms, s);
+cudaError_t pick(const AttnCall& c, const AttnParts& parts, const FewShared* shared, int rows, int head_dim, int sms, cudaStream_t s) {
+  if (head_dim == 256) return run<T, 256, 1>(c, parts, shared, sms, s);
+  if (head_dim == 128) return rows <= 16 ? run<T, 128, 1>(c, parts, shared, sms, s) : run<T, 128, 2>(c, parts, shared, sms, s);
+  return rows <= 16   ? run<T, 64, 1>(c, parts, shared, sms, s)
+         : rows <= 32 ? run<T, 64, 2>(c, parts, shared, sms, s)
+                      : run<T, 64, 3>(c, parts, shared, sms, s);
 }
 
 }  // namespace
 
 int attn_few_blocks(int sms) { return sms * 2; }
 int attn_few_rows(int head_dim) { return head_dim == 256 ? 16 : head_dim == 128 ? 32 : 48; }
+int attn_few_part_rows(int rows) { return (rows + 15) / 16 * 16; }
+int attn_few_fit(int head_dim, int sms) {
+  return sms * (head_dim == 64 ? Cfg<64>::kBlocksPerSm : head_dim == 128 ? Cfg<128>::kBlocksPerSm : Cfg<256>::kBlocksPerSm);
+}
 
 cudaError_t launch_attn_few(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int sms, cudaStream_t s) {
-  return bf16 ? pick<__nv_bfloat16>(c, parts, head_dim, sms, s) : pick<__half>(c, parts, head_dim, sms, s);
+  const int rows = c.st.max_q * c.st.G;
+  return bf16 ? pick<__nv_bfloat16>(c, parts, nullptr, rows, head_dim, sms, s) : pick<__half>(c, parts, nullptr, rows, head_dim, sms, s);
+}
+cudaError_t launch_attn_few_shared(const AttnCall& c, const AttnParts& parts, const FewShared& shared, int rows, int head_dim, bool bf16,
+                                   int sms, cudaStream_t s) {
+  return bf16 ? pick<__nv_bfloat16>(c, parts, &shared, rows, head_dim, sms, s) : pick<__half>(c, parts, &shared, rows, head_dim, sms, s);
 }
 
 }  // namespace mf

@@ -133,12 +133,14 @@ __global__ void __launch_bounds__(1024) k_attn_plan(AttnCall c, AttnPlan p) {
 
 // The same of a step whose groups of sequences share their first lines: as many virtual sequences as there are groups, with the rows of
 // all the group's tokens and the shared lines (whole pages of them), then the sequences, with what follows.  First the groups: bounds
-// that rise, lengths that all their sequences have; a group of one shares nothing.
+// that rise, lengths that all their sequences have; a group of one shares nothing.  p.groups and p.seqs say which of them are in the list
+// of this file's kernel, few_groups and few_seqs which are in that of few rows.
 template <int D>
-__global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGroups g, AttnPlan p, SharedPlan sp) {
+__global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGroups g, AttnPlan p, SharedPlan sp, int few_groups,
+                                                           int few_seqs) {
   __shared__ int64_t s_warp[32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int V = g.n + c.st.n_seqs;
+  const int V = p.groups + p.seqs, few = few_groups + few_seqs;
   pdl_wait();
   pdl_trigger();
   auto scan = [&](int64_t v, int64_t& all) -> int64_t {  // exclusive prefix over the block, and the sum
@@ -214,13 +216,36 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     }
   }
   __syncthreads();
-  // ---- row tiles of the virtual sequences
+  // ---- the list of few rows
   int64_t done = 0;
+  for (int base = 0; base < few; base += 1024) {
+    const int v = base + tid;
+    int64_t n = 0, all;
+    if (v < few) {
+      int4 x;
+      if (v < few_groups) {
+        x = sp.group[v];
+        x = make_int4(x.y, x.z, x.w, 0);
+      } else {
+        const SeqSpan q = seq_span(c.st, v - few_groups);
+        x = make_int4(q.q0, q.n, q.len, sp.seq[v - few_groups].y);
+      }
+      sp.span[v] = x;
+      if (x.y) n = (int64_t)(max(1, (x.z - (x.w & ~15) + kFewTile - 1) / kFewTile) + kFewOver) * c.st.Hkv;
+    }
+    const int64_t at = done + scan(n, all);
+    if (v < few) sp.before[v] = at;
+    done += all;
+  }
+  if (tid == 0 && few) sp.before[few] = done;
+  if (V == 0) return;
+  // ---- row tiles of the virtual sequences
+  done = 0;
   for (int base = 0; base < V; base += 1024) {
     const int v = base + tid;
     int64_t n = 0, all;
     if (v < V) {
-      const int tokens = v < g.n ? sp.group[v].z : seq_span(c.st, v - g.n).n;
+      const int tokens = v < p.groups ? sp.group[v].z : seq_span(c.st, v - p.groups).n;
       n = ((int64_t)tokens * c.st.G + Cfg<D>::kRows - 1) / Cfg<D>::kRows;
     }
     const int64_t at = done + scan(n, all);
@@ -244,12 +269,12 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
       const int qt = i - p.first[lo], R0 = qt * Cfg<D>::kRows, G = c.st.G;
       int s, start, end, rows;
       SeqSpan q;
-      if (lo < g.n) {
+      if (lo < p.groups) {
         const int4 x = sp.group[lo];
         s = x.x, q = {x.y, x.z, x.w};
         rows = min(Cfg<D>::kRows, q.n * G - R0), start = 0, end = x.w;
       } else {
-        s = lo - g.n, q = seq_span(c.st, s);
+        s = lo - p.groups, q = seq_span(c.st, s);
         rows = min(Cfg<D>::kRows, q.n * G - R0), start = sp.seq[s].y;
         end = max(start, vis_hi(c, q.len - q.n + (R0 + rows - 1) / G, q.len));
       }
@@ -469,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
   pdl_wait();
   pdl_trigger();
 
-  const int groups = kShared ? p.groups : 0, tiles = __ldg(p.first + groups + st.n_seqs);
+  const int groups = kShared ? p.groups : 0, tiles = __ldg(p.first + (kShared ? groups + p.seqs : st.n_seqs));
   const int64_t total = tiles ? __ldg(p.before + tiles) * st.Hkv : 0;
   // every block that works has at least two jobs, so that it has a key tile's start
   const int64_t B = max((int64_t)1, min((int64_t)gridDim.x, total / 2));
@@ -1013,42 +1038,70 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
 
 // ---- the joined result of a step whose groups share lines
 
-// A block: some rows of a sequence's row tile and a kv head.  A row's pieces are the group's (in the order of the lines) and then the
-// sequence's own; where they lie follows from the plan: the block of a tile's first key tile to that of its last.  Four columns a thread.
+// A block: some rows of a sequence (of one of its row tiles, where they are many) and a kv head.  A row's pieces are the group's, in the order
+// of the lines, and then the sequence's own; where they lie follows from the plan: with the block that has the first key tile, to that of
+// the last.  Four columns a thread.  kFewGroups, kFewSeqs: the groups' lines, the sequences' own were the kernel's of few rows.
 constexpr int kJoinRows = 16, kJoinThreads = 256;
-template <class T, int D>
+template <class T, int D, bool kFewGroups, bool kFewSeqs>
 __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_constant__ AttnCall c, const __grid_constant__ AttnPlan p,
                                                                    const __grid_constant__ SharedPlan sp,
-                                                                   const __grid_constant__ AttnParts parts, int blocks) {
+                                                                   const __grid_constant__ AttnParts parts,
+                                                                   const __grid_constant__ AttnParts few, int blocks, int few_blocks,
+                                                                   int few_rows, int few_groups) {
   using C = Cfg<D>;
   const AttnStep& st = c.st;
   const int h = blockIdx.y, r0 = blockIdx.z * kJoinRows, tid = threadIdx.x;
   pdl_wait();
-  const int tile = __ldg(p.first + p.groups) + (int)blockIdx.x, tiles = __ldg(p.first + p.groups + st.n_seqs);
-  if (tile >= tiles) return;
-  const int4 ta = __ldg(p.tile + 2 * tile), tb = __ldg(p.tile + 2 * tile + 1);
-  const int rows = min(kJoinRows, tb.y - r0);
-  if (rows <= 0) return;
-  const int64_t total = __ldg(p.before + tiles) * st.Hkv, B = max((int64_t)1, min((int64_t)blocks, total / 2));
   // the pieces of a tile: blocks b .. b + n - 1
   struct Run {
     int64_t b;
     int n;
   };
-  auto run_of = [&](int i, int v, int4 x) -> Run {
+  const int64_t few_total = kFewGroups || kFewSeqs ? __ldg(sp.before + few_groups + st.n_seqs) : 0, few_B = min((int64_t)few_blocks, few_total);
+  auto few_run = [&](int v) -> Run {
+    const int4 x = __ldg(sp.span + v);
+    const int nt = max(1, (x.z - (x.w & ~15) + kFewTile - 1) / kFewTile);
+    const int64_t at = __ldg(sp.before + v) + (int64_t)h * (nt + kFewOver) + kFewOver;
+    const int64_t b = (few_B * (at + 1) - 1) / few_total, l = (few_B * (at + nt) - 1) / few_total;
+    return {b, (int)(l - b) + 1};
+  };
+  const int tiles = kFewGroups ? 0 : __ldg(p.first + p.groups + p.seqs);
+  const int64_t total = tiles ? __ldg(p.before + tiles) * st.Hkv : 0, B = max((int64_t)1, min((int64_t)blocks, total / 2));
+  auto many_run = [&](int i, int v, int4 x) -> Run {
     const int f = __ldg(p.first + v), e = __ldg(p.first + v + 1);
     const int64_t b0 = __ldg(p.before + f), at = b0 * st.Hkv + h * (__ldg(p.before + e) - b0) + __ldg(p.before + i) - b0 + C::kOver;
     const int nt = max(1, (x.w - x.z + kKeys - 1) / kKeys), two = x.y > 128;
     const int64_t b = (B * (at + 1) - 1) / total, l = (B * (at + ((int64_t)(nt - 1) << two) + 1) - 1) / total;
     return {b, (int)(l - b) + 1};
   };
-  const Run own = run_of(tile, p.groups + ta.x, tb);
-  const int group = __ldg(&sp.seq[ta.x].x);
+  int s, q0, rows, qt = 0, tile_rows = 0;
+  Run own;
+  if constexpr (kFewSeqs) {
+    s = blockIdx.x;
+    const int4 x = __ldg(sp.span + few_groups + s);
+    q0 = x.x, rows = x.y * st.G;
+    if (r0 >= rows) return;
+    own = few_run(few_groups + s);
+  } else {
+    const int tile = __ldg(p.first + p.groups) + (int)blockIdx.x;
+    if (tile >= tiles) return;
+    const int4 ta = __ldg(p.tile + 2 * tile), tb = __ldg(p.tile + 2 * tile + 1);
+    s = ta.x, q0 = ta.y, qt = tb.x, rows = tile_rows = tb.y;
+    if (r0 >= rows) return;
+    own = many_run(tile, p.groups + s, tb);
+  }
+  rows = min(kJoinRows, rows - r0);
+  const int group = __ldg(&sp.seq[s].x);
   int4 g = make_int4(0, 0, 0, 0);
-  if (group >= 0) g = __ldg(sp.group + group);
+  Run with = {0, 0};
+  if (group >= 0) {
+    g = __ldg(sp.group + group);
+    if (kFewGroups) with = few_run(group);
+  }
   for (int i = tid; i < rows * (D / 4); i += kJoinThreads) {
-    const int r = r0 + i % rows, col = i / rows, R = tb.x * C::kRows + r;
-    const int tok = ta.y + R / st.G, head = h * st.G + R % st.G;
+    // (neighbouring threads take what neighbours in memory: columns, or rows as tiles leave them)
+    const int r = r0 + (kFewGroups ? i / (D / 4) : i % rows), col = kFewGroups ? i % (D / 4) : i / rows, R = qt * C::kRows + r;
+    const int tok = q0 + R / st.G, head = h * st.G + R % st.G;
     float mx = -INFINITY, ls = 0.f;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     auto add = [&](float2 ml, float4 o) {
@@ -1057,9 +1110,9 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_
       ls = ls * f + w * ml.y;
       mx = to;
     };
-    auto add_run = [&](const Run& run, int64_t place, int tile_rows, int row) {  // place: of the tile's rows, where it is whole
+    auto add_many = [&](const Run& run, int64_t place, int of, int row) {  // place: of the tile's `of` rows, where it is whole
       if (run.n == 1) {
-        add(parts.whole_ml[place + row], *reinterpret_cast<const float4*>(parts.whole + place * D + ((int64_t)col * tile_rows + row) * 4));
+        add(parts.whole_ml[place + row], *reinterpret_cast<const float4*>(parts.whole + place * D + ((int64_t)col * of + row) * 4));
       } else {
 #pragma unroll 4
         for (int k = 0; k < run.n; ++k) {
@@ -1068,15 +1121,35 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_
         }
       }
     };
+    auto add_few = [&](const Run& run, int64_t half, int row) {
+      if (run.n == 1) {
+        const int64_t place = half + (int64_t)tok * st.Hq + head;
+        add(few.whole_ml[place], *reinterpret_cast<const float4*>(few.whole + place * D + col * 4));
+      } else {
+#pragma unroll 4
+        for (int k = 0; k < run.n; ++k) {
+          const int64_t at = (k == 0 ? run.b * 2 + 1 : (run.b + k) * 2) * few_rows + row;
+          add(few.ml[at], *reinterpret_cast<const float4*>(few.o + at * D + col * 4));
+        }
+      }
+    };
     if (g.z) {
       const int64_t at = (int64_t)(tok - g.y) * st.G + R % st.G;  // the row among the group's
-      const int qt = (int)(at / C::kRows), i0 = __ldg(p.first + group) + qt;
-      if (at >= 0 && at < (int64_t)g.z * st.G && i0 < __ldg(p.first + group + 1)) {
-        const int4 x = __ldg(p.tile + 2 * i0 + 1);
-        add_run(run_of(i0, group, x), ((int64_t)h * st.n_tokens + g.y) * st.G + (int64_t)qt * C::kRows, x.y, (int)(at - (int64_t)qt * C::kRows));
+      if (at >= 0 && at < (int64_t)g.z * st.G) {
+        if constexpr (kFewGroups) {
+          add_few(with, 0, (int)at);
+        } else {
+          const int t = (int)(at / C::kRows), i0 = __ldg(p.first + group) + t;
+          if (i0 < __ldg(p.first + group + 1)) {
+            const int4 x = __ldg(p.tile + 2 * i0 + 1);
+            add_many(many_run(i0, group, x), ((int64_t)h * st.n_tokens + g.y) * st.G + (int64_t)t * C::kRows, x.y, (int)(at - (int64_t)t * C::kRows));
+          }
+        }
       }
     }
-    add_run(own, (int64_t)st.n_tokens * st.Hq + ((int64_t)h * st.n_tokens + ta.y) * st.G + tb.x * C::kRows, tb.y, r);
+    const int64_t half = (int64_t)st.n_tokens * st.Hq;
+    if constexpr (kFewSeqs) add_few(own, half, r);
+    else add_many(own, half + ((int64_t)h * st.n_tokens + q0) * st.G + qt * C::kRows, tile_rows, r);
     const float inv = ls == 0.f ? 0.f : 1.f / ls;  // (a NaN in the scores stays NaN)
     T* out = static_cast<T*>(c.out) + (int64_t)tok * c.out_stride + (int64_t)head * D + col * 4;
     *reinterpret_cast<uint2*>(out) = make_uint2(Half2<T>::down(sum.x * inv, sum.y * inv), Half2<T>::down(sum.z * inv, sum.w * inv));
@@ -1084,32 +1157,60 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_
   }
 }
 
+constexpr size_t smem_of(size_t tail) { return tail + sizeof(Tail); }
+
 template <class T, int D>
-cudaError_t run(const AttnCall& c, const AttnMaps& maps, AttnPlan plan, const AttnParts& parts, const SharedGroups* groups,
-                const SharedPlan* shared, int sms, cudaStream_t s) {
+cudaError_t run(const AttnCall& c, const AttnMaps& maps, AttnPlan plan, const AttnParts& parts, int sms, cudaStream_t s) {
   using C = Cfg<D>;
   const int64_t rows = (int64_t)c.st.n_tokens * c.st.G;
-  const int64_t own = rows / C::kRows + c.st.n_seqs, tiles = own + (groups ? rows / C::kRows + groups->n : 0);
+  const int64_t tiles = rows / C::kRows + c.st.n_seqs;
   plan.max_tiles = tiles < plan.max_tiles ? (int)tiles : plan.max_tiles;
-  plan.groups = groups ? groups->n : 0;
   const int64_t most = tiles * c.st.Hkv * (((int64_t)c.st.cap + kKeys - 1) / kKeys);
   const unsigned grid = (unsigned)(most < sms ? most : sms);
-  constexpr size_t smem = C::kTail + sizeof(Tail);
+  constexpr size_t smem = smem_of(C::kTail);
   static_assert(smem <= 232448, "shared memory of a block");
-  auto kernel = groups ? k_attn_many<T, D, true> : k_attn_many<T, D, false>;
+  auto kernel = k_attn_many<T, D, false>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e == cudaSuccess)
-    e = groups ? launch_pdl(true, k_attn_plan_shared<D>, dim3(1), dim3(1024), 0, s, c, *groups, plan, *shared)
-               : launch_pdl(true, k_attn_plan<D>, dim3(1), dim3(1024), 0, s, c, plan);
+  if (e == cudaSuccess) e = launch_pdl(true, k_attn_plan<D>, dim3(1), dim3(1024), 0, s, c, plan);
   if (e == cudaSuccess) e = launch_pdl(true, kernel, dim3(grid), dim3(kThreads), smem, s, c, maps, plan, parts);
-  if (e == cudaSuccess && groups) {
-    const int64_t held = (int64_t)c.st.max_q * c.st.G;
-    const int in_tile = (int)(held < C::kRows ? held : C::kRows);
-    const dim3 g((unsigned)own, (unsigned)c.st.Hkv, (unsigned)((in_tile + kJoinRows - 1) / kJoinRows));
-    return launch_pdl(true, k_attn_join_shared<T, D>, g, dim3(kJoinThreads), 0, s, c, plan, *shared, parts, (int)grid);
-  }
   if (e == cudaSuccess && grid > 1) e = launch_attn_join(c, parts, D, Half2<T>::kBf16, C::kRows, true, (int)grid, s);
   return e;
+}
+
+// The plan, the groups' lines, the sequences' own, the join.  Rows that the kernel of few rows holds are its: all of them where a group cannot
+// have more (one launch), else those of the sequences (a launch that starts while the groups' ends).
+template <class T, int D>
+cudaError_t run_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& g, const AttnShared& sh, int sms, cudaStream_t s) {
+  using C = Cfg<D>;
+  constexpr bool kBf = Half2<T>::kBf16;
+  const int64_t rows = (int64_t)c.st.n_tokens * c.st.G, seq_rows = (int64_t)c.st.max_q * c.st.G;
+  const bool few_seqs = seq_rows <= attn_few_rows(D), few_groups = few_seqs && (rows <= attn_few_rows(D) || g.n == 0);
+  AttnPlan plan = sh.plan;
+  plan.groups = few_groups ? 0 : g.n, plan.seqs = few_seqs ? 0 : c.st.n_seqs;
+  const int64_t own = rows / C::kRows + c.st.n_seqs;  // row tiles of the sequences
+  const int64_t tiles = (plan.seqs ? own : 0) + (plan.groups ? rows / C::kRows + g.n : 0);
+  plan.max_tiles = tiles < plan.max_tiles ? (int)tiles : plan.max_tiles;
+  const int n_few_groups = few_groups ? g.n : 0;
+  cudaError_t e = launch_pdl(true, k_attn_plan_shared<D>, dim3(1), dim3(1024), 0, s, c, g, plan, sh.found, n_few_groups, few_seqs ? c.st.n_seqs : 0);
+  const int64_t most = tiles * c.st.Hkv * (((int64_t)c.st.cap + kKeys - 1) / kKeys);
+  const unsigned grid = (unsigned)(most < sms ? most : sms);
+  if (e == cudaSuccess && tiles) {
+    constexpr size_t smem = smem_of(C::kTail);
+    auto kernel = k_attn_many<T, D, true>;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e == cudaSuccess) e = launch_pdl(true, kernel, dim3(grid), dim3(kThreads), smem, s, c, maps, plan, sh.parts);
+  }
+  const int few_rows = (int)(few_groups && g.n ? rows : seq_rows), few_blocks = attn_few_fit(D, sms);
+  if (e == cudaSuccess && few_seqs) {
+    const FewShared f = {sh.found.span, sh.found.group, sh.found.before, n_few_groups, tiles == 0, few_blocks};
+    e = launch_attn_few_shared(c, sh.few, f, few_rows, D, kBf, sms, s);
+  }
+  if (e != cudaSuccess) return e;
+  const int64_t in_tile = few_seqs || seq_rows < C::kRows ? seq_rows : C::kRows;
+  const dim3 blocks((unsigned)(few_seqs ? c.st.n_seqs : own), (unsigned)c.st.Hkv, (unsigned)((in_tile + kJoinRows - 1) / kJoinRows));
+  auto join = few_groups ? k_attn_join_shared<T, D, true, true> : few_seqs ? k_attn_join_shared<T, D, false, true> : k_attn_join_shared<T, D, false, false>;
+  return launch_pdl(true, join, blocks, dim3(kJoinThreads), 0, s, c, plan, sh.found, sh.parts, sh.few, (int)grid, few_blocks,
+                    attn_few_part_rows(few_rows), n_few_groups);
 }
 
 }  // namespace
@@ -1154,26 +1255,25 @@ void attn_maps(AttnCall& c, int head_dim, AttnMaps* maps) {
 
 int attn_tile_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
 
-namespace {
-cudaError_t pick(const AttnCall& c, const AttnMaps& maps, const AttnPlan& plan, const AttnParts& parts, const SharedGroups* groups,
-                 const SharedPlan* shared, int head_dim, bool bf16, int sms, cudaStream_t s) {
-  if (bf16)
-    return head_dim == 64    ? run<__nv_bfloat16, 64>(c, maps, plan, parts, groups, shared, sms, s)
-           : head_dim == 128 ? run<__nv_bfloat16, 128>(c, maps, plan, parts, groups, shared, sms, s)
-                             : run<__nv_bfloat16, 256>(c, maps, plan, parts, groups, shared, sms, s);
-  return head_dim == 64    ? run<__half, 64>(c, maps, plan, parts, groups, shared, sms, s)
-         : head_dim == 128 ? run<__half, 128>(c, maps, plan, parts, groups, shared, sms, s)
-                           : run<__half, 256>(c, maps, plan, parts, groups, shared, sms, s);
-}
-}  // namespace
-
 cudaError_t launch_attn_many(const AttnCall& c, const AttnMaps& maps, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
                              cudaStream_t s) {
-  return pick(c, maps, plan, parts, nullptr, nullptr, head_dim, bf16, sms, s);
+  if (bf16)
+    return head_dim == 64    ? run<__nv_bfloat16, 64>(c, maps, plan, parts, sms, s)
+           : head_dim == 128 ? run<__nv_bfloat16, 128>(c, maps, plan, parts, sms, s)
+                             : run<__nv_bfloat16, 256>(c, maps, plan, parts, sms, s);
+  return head_dim == 64    ? run<__half, 64>(c, maps, plan, parts, sms, s)
+         : head_dim == 128 ? run<__half, 128>(c, maps, plan, parts, sms, s)
+                           : run<__half, 256>(c, maps, plan, parts, sms, s);
 }
-cudaError_t launch_attn_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& groups, const AttnShared& sh, int head_dim, bool bf16,
+cudaError_t launch_attn_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& g, const AttnShared& sh, int head_dim, bool bf16,
                                int sms, cudaStream_t s) {
-  return pick(c, maps, sh.plan, sh.parts, &groups, &sh.found, head_dim, bf16, sms, s);
+  if (bf16)
+    return head_dim == 64    ? run_shared<__nv_bfloat16, 64>(c, maps, g, sh, sms, s)
+           : head_dim == 128 ? run_shared<__nv_bfloat16, 128>(c, maps, g, sh, sms, s)
+                             : run_shared<__nv_bfloat16, 256>(c, maps, g, sh, sms, s);
+  return head_dim == 64    ? run_shared<__half, 64>(c, maps, g, sh, sms, s)
+         : head_dim == 128 ? run_shared<__half, 128>(c, maps, g, sh, sms, s)
+                           : run_shared<__half, 256>(c, maps, g, sh, sms, s);
 }
 
 }  // namespace mf
