@@ -164,7 +164,10 @@ struct AttnPlan {
                     //                 sequence's tiles, rows, first and end of the lines that any of them sees
   int64_t* before;  // [max_tiles + 1] jobs (of one kv head) before the tile
   int max_tiles;
-  int groups, seqs;  // of a step whose groups share lines: the virtual sequences of the list, groups and then sequences
+  // of a step whose groups share lines: the virtual sequences of the list, groups and then sequences, and for each row tile and kv
+  // head the block that has its first key tile and how many have one
+  int groups, seqs;
+  int2* runs;       // [max_tiles][kv heads]
 };
 
 // Groups of sequences that share their first lines (mf_shared_t), and what k_attn_plan_shared finds of them.
@@ -176,15 +179,20 @@ struct SharedPlan {
   int* bound;   // [max_groups + 1] first sequence of a group
   int4* group;  // [max_groups]     that, its first token, tokens (0: nothing is shared), lines that are shared
   int2* seq;    // [max_seqs]       a sequence's group (-1: none), the lines it shares
+  // for the join: a sequence's first token and tokens, its group's; the group's place in the list of few rows or its first row tile,
+  // its row tiles
+  int4* join;   // [max_seqs][2]
   // the list of launch_attn_few_shared: a (virtual) sequence's first new token, new tokens, end and beginning of its lines; the
-  // places before it
+  // places before it; for each and a kv head the block that has its first tile and how many have one
   int4* span;       // [max_groups + max_seqs]
   int64_t* before;  // [max_groups + max_seqs + 1]
+  int2* runs;       // [max_groups + max_seqs][kv heads]
 };
 // A step whose groups share lines, as launch_attn_few_shared takes it.
 struct FewShared {
   const int4 *span, *group;
   const int64_t* before;
+  int2* runs;
   int groups;  // virtual sequences before the step's
   int wait;    // the kernel before this one is the plan
   int blocks;

@@ -480,6 +480,11 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
       const bool whole = j0 == 0 && cur.j_end == cur.sn.nt;
       const int part = blockIdx.x * 2 + (j0 == 0);  // a piece that starts before this block is its first
       const int rows = cur.sn.sp.n * st.G;
+      if constexpr (kShared) {
+        if (j0 == 0 && tid == 0)
+          extra.runs[cur.s * st.Hkv + cur.h] = make_int2(
+              blockIdx.x, whole ? 1 : (int)((B * (cur.at + kOver + cur.sn.nt) - 1) / total) - (int)blockIdx.x + 1);
+      }
       if (!kShared && j0 == 0 && !whole && tid == 0) {  // the block of the last tile has the last piece
         const int64_t end = cur.at + kOver + cur.sn.nt;
         parts.rec[blockIdx.x] = {cur.sn.sp.q0, cur.h, 0, rows, (int)((B * end - 1) / total) - (int)blockIdx.x + 1};

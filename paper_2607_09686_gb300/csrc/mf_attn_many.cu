@@ -139,10 +139,22 @@ template <int D>
 __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGroups g, AttnPlan p, SharedPlan sp, int few_groups,
                                                            int few_seqs) {
   __shared__ int64_t s_warp[32];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  // what the phases hand on, in shared memory where it finds room: the sequences' spans and groups, the groups, first row tiles
+  constexpr int kSmall = 1024;
+  __shared__ SeqSpan s_span[kSmall];
+  __shared__ int2 s_seq[kSmall];
+  __shared__ int4 s_group[kSmall / 4];
+  __shared__ int s_bound[kSmall / 4 + 1], s_first[kSmall + 1];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_seqs = c.st.n_seqs;
   const int V = p.groups + p.seqs, few = few_groups + few_seqs;
+  const bool small_seqs = n_seqs <= kSmall, small_groups = g.n <= kSmall / 4, small = V <= kSmall;
+  int* bound = small_groups ? s_bound : sp.bound;
+  int4* group = small_groups ? s_group : sp.group;
+  int2* seq = small_seqs ? s_seq : sp.seq;
+  int* first = small ? s_first : p.first;
   pdl_wait();
   pdl_trigger();
+  auto span = [&](int s) -> SeqSpan { return small_seqs ? s_span[s] : seq_span(c.st, s); };
   auto scan = [&](int64_t v, int64_t& all) -> int64_t {  // exclusive prefix over the block, and the sum
     int64_t x = v;
 #pragma unroll
@@ -153,20 +165,25 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     __syncthreads();
     if (lane == 31) s_warp[warp] = x;
     __syncthreads();
-    int64_t before = 0;
-    all = 0;
-    for (int w = 0; w < 32; ++w) {
-      if (w < warp) before += s_warp[w];
-      all += s_warp[w];
+    int64_t mine = s_warp[lane], total = mine;  // (each warp adds up all of them)
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t o = __shfl_up_sync(0xffffffffu, total, d);
+      if (lane >= d) total += o;
     }
-    return before + x - v;
+    all = __shfl_sync(0xffffffffu, total, 31);
+    return __shfl_sync(0xffffffffu, total - mine, warp) + x - v;
   };
+  for (int s = tid; s < n_seqs; s += 1024) {
+    if (small_seqs) s_span[s] = seq_span(c.st, s);
+    seq[s] = make_int2(-1, 0);
+  }
   // ---- the groups' bounds: the largest so far, inside the step
   int from = 0;
   for (int base = 0; base <= g.n; base += 1024) {
     const int i = base + tid;
     const int raw = i <= g.n && g.n ? __ldg(g.first + i) : 0;
-    int x = min(max(raw, 0), c.st.n_seqs);
+    int x = min(max(raw, 0), n_seqs);
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const int o = __shfl_up_sync(0xffffffffu, x, d);
@@ -175,19 +192,14 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     __syncthreads();
     if (lane == 31) s_warp[warp] = x;
     __syncthreads();
-    int most = from;
-    for (int w = 0; w < 32; ++w) {
-      if (w < warp) x = max(x, (int)s_warp[w]);
-      most = max(most, (int)s_warp[w]);
-    }
-    x = max(x, from);
-    from = most;
+    const int theirs = (int)s_warp[lane];
+    x = max(max(x, from), __reduce_max_sync(0xffffffffu, lane < warp ? theirs : 0));
+    from = max(from, __reduce_max_sync(0xffffffffu, theirs));
     if (i <= g.n) {
-      sp.bound[i] = x;
+      bound[i] = x;
       if (x != raw) attn_report(c.st, kAttnRange);
     }
   }
-  for (int s = tid; s < c.st.n_seqs; s += 1024) sp.seq[s] = make_int2(-1, 0);
   __syncthreads();
   // ---- their lengths: some lanes a group
   int width = 32;
@@ -196,9 +208,9 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
   for (int base = 0; base < g.n; base += per) {
     const int i = base + tid / width;
     int a = 0, b = 0, least = 0x7FFFFFFF;
-    if (i < g.n) a = sp.bound[i], b = sp.bound[i + 1];
+    if (i < g.n) a = bound[i], b = bound[i + 1];
     for (int s = a + sub; s < b; s += width) {
-      const SeqSpan q = seq_span(c.st, s);
+      const SeqSpan q = span(s);
       least = min(least, q.len - q.n);
     }
     for (int d = 1; d < width; d <<= 1) least = min(least, __shfl_xor_sync(0xffffffffu, least, d));
@@ -208,11 +220,11 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
       const int lines = b - a > 1 ? (int)fast_div((uint32_t)len, c.st.page_mul, c.st.page_shift) * c.st.page_size : 0;
       int q0 = 0, n = 0;
       if (lines) {
-        const SeqSpan x = seq_span(c.st, a), y = seq_span(c.st, b - 1);
+        const SeqSpan x = span(a), y = span(b - 1);
         q0 = x.q0, n = max(y.q0 + y.n - q0, 0);
       }
-      if (sub == 0) sp.group[i] = make_int4(a, q0, n, lines);
-      for (int s = a + sub; s < b; s += width) sp.seq[s] = make_int2(n ? i : -1, n ? lines : 0);
+      if (sub == 0) group[i] = sp.group[i] = make_int4(a, q0, n, lines);
+      for (int s = a + sub; s < b; s += width) seq[s] = make_int2(n ? i : -1, n ? lines : 0);
     }
   }
   __syncthreads();
@@ -224,11 +236,11 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     if (v < few) {
       int4 x;
       if (v < few_groups) {
-        x = sp.group[v];
+        x = group[v];
         x = make_int4(x.y, x.z, x.w, 0);
       } else {
-        const SeqSpan q = seq_span(c.st, v - few_groups);
-        x = make_int4(q.q0, q.n, q.len, sp.seq[v - few_groups].y);
+        const SeqSpan q = span(v - few_groups);
+        x = make_int4(q.q0, q.n, q.len, seq[v - few_groups].y);
       }
       sp.span[v] = x;
       if (x.y) n = (int64_t)(max(1, (x.z - (x.w & ~15) + kFewTile - 1) / kFewTile) + kFewOver) * c.st.Hkv;
@@ -238,22 +250,21 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     done += all;
   }
   if (tid == 0 && few) sp.before[few] = done;
-  if (V == 0) return;
   // ---- row tiles of the virtual sequences
   done = 0;
   for (int base = 0; base < V; base += 1024) {
     const int v = base + tid;
     int64_t n = 0, all;
     if (v < V) {
-      const int tokens = v < p.groups ? sp.group[v].z : seq_span(c.st, v - p.groups).n;
+      const int tokens = v < p.groups ? group[v].z : span(v - p.groups).n;
       n = ((int64_t)tokens * c.st.G + Cfg<D>::kRows - 1) / Cfg<D>::kRows;
     }
     const int64_t at = done + scan(n, all);
-    if (v < V) p.first[v] = (int)min(at, (int64_t)p.max_tiles);
+    if (v < V) first[v] = p.first[v] = (int)min(at, (int64_t)p.max_tiles);
     done += all;
   }
   const int tiles = (int)min(done, (int64_t)p.max_tiles);
-  if (tid == 0) p.first[V] = tiles;
+  if (tid == 0 && V) first[V] = p.first[V] = tiles;
   __syncthreads();
   int64_t jobs = 0;
   for (int base = 0; base < tiles; base += 1024) {
@@ -263,19 +274,19 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
       int lo = 0, hi = V - 1;  // the last virtual sequence whose first tile is at or before i
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (p.first[mid] <= i) lo = mid;
+        if (first[mid] <= i) lo = mid;
         else hi = mid - 1;
       }
-      const int qt = i - p.first[lo], R0 = qt * Cfg<D>::kRows, G = c.st.G;
+      const int qt = i - first[lo], R0 = qt * Cfg<D>::kRows, G = c.st.G;
       int s, start, end, rows;
       SeqSpan q;
       if (lo < p.groups) {
-        const int4 x = sp.group[lo];
+        const int4 x = group[lo];
         s = x.x, q = {x.y, x.z, x.w};
         rows = min(Cfg<D>::kRows, q.n * G - R0), start = 0, end = x.w;
       } else {
-        s = lo - p.groups, q = seq_span(c.st, s);
-        rows = min(Cfg<D>::kRows, q.n * G - R0), start = sp.seq[s].y;
+        s = lo - p.groups, q = span(s);
+        rows = min(Cfg<D>::kRows, q.n * G - R0), start = seq[s].y;
         end = max(start, vis_hi(c, q.len - q.n + (R0 + rows - 1) / G, q.len));
       }
       p.tile[2 * i] = make_int4(s, q.q0, q.n, q.len);
@@ -287,7 +298,21 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     if (i < tiles) p.before[i] = at;
     jobs += all;
   }
-  if (tid == 0) p.before[tiles] = jobs;
+  if (tid == 0 && V) p.before[tiles] = jobs;
+  // ---- what the join asks for
+  for (int s = tid; s < n_seqs; s += 1024) {
+    const SeqSpan q = span(s);
+    const int gi = seq[s].x;
+    int4 x = make_int4(0, 0, 0, 0);
+    int at = 0, many = 0;
+    if (gi >= 0) {
+      x = group[gi];
+      at = few_groups ? gi : first[gi];
+      if (!few_groups) many = first[gi + 1] - at;
+    }
+    sp.join[2 * s] = make_int4(q.q0, q.n, x.y, x.z);
+    sp.join[2 * s + 1] = make_int4(at, many, 0, 0);
+  }
 }
 
 // The walk over a block's segments: key tiles j0 .. j1 - 1 of a row tile (of all: `tile`) and kv head h.  The list is
@@ -939,6 +964,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
         tail.piece[told].take(w);
         if (kShared && w.tile < group_tiles) tail.piece[told].first = kGroupRows;
         mbar_arrive(&bars[kBPiece + told]);
+        if (kShared && w.more && w.j0 == 0)  // (the block of the last key tile, by the place of its first job)
+          p.runs[(int64_t)w.tile * st.Hkv + w.h] = make_int2(
+              (int)b, w.j1 == w.nt ? 1 : (int)((B * (w.at + C::kOver + ((int64_t)(w.nt - 1) << w.two) + 1) - 1) / total) - (int)b + 1);
       }
       __syncwarp();
       if (++told == kPieces) told = 0, tph ^= 1;
@@ -1039,68 +1067,50 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
 // ---- the joined result of a step whose groups share lines
 
 // A block: some rows of a sequence (of one of its row tiles, where they are many) and a kv head.  A row's pieces are the group's, in the order
-// of the lines, and then the sequence's own; where they lie follows from the plan: with the block that has the first key tile, to that of
-// the last.  Four columns a thread.  kFewGroups, kFewSeqs: the groups' lines, the sequences' own were the kernel's of few rows.
-constexpr int kJoinRows = 16, kJoinThreads = 256;
+// of the lines, and then the sequence's own; the blocks that have them were noted by the one that had the first.  A thread has
+// four columns of a row, and where the rows are few every P-th piece.  kFewGroups, kFewSeqs: the groups' lines, the sequences' own were
+// the kernel's of few rows.
+constexpr int kJoinThreads = 256;
+template <bool kFewSeqs>
+constexpr int kJoinRows = kFewSeqs ? 2 : 16;
 template <class T, int D, bool kFewGroups, bool kFewSeqs>
 __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_constant__ AttnCall c, const __grid_constant__ AttnPlan p,
                                                                    const __grid_constant__ SharedPlan sp,
                                                                    const __grid_constant__ AttnParts parts,
-                                                                   const __grid_constant__ AttnParts few, int blocks, int few_blocks,
-                                                                   int few_rows, int few_groups) {
+                                                                   const __grid_constant__ AttnParts few, int few_rows, int few_groups) {
   using C = Cfg<D>;
+  constexpr int kR = kJoinRows<kFewSeqs>, kCols = D / 4;
+  __shared__ float4 s_o[kJoinThreads];
+  __shared__ float2 s_ml[kJoinThreads];
   const AttnStep& st = c.st;
-  const int h = blockIdx.y, r0 = blockIdx.z * kJoinRows, tid = threadIdx.x;
+  const int h = blockIdx.y, r0 = blockIdx.z * kR, tid = threadIdx.x;
   pdl_wait();
-  // the pieces of a tile: blocks b .. b + n - 1
-  struct Run {
-    int64_t b;
-    int n;
-  };
-  const int64_t few_total = kFewGroups || kFewSeqs ? __ldg(sp.before + few_groups + st.n_seqs) : 0, few_B = min((int64_t)few_blocks, few_total);
-  auto few_run = [&](int v) -> Run {
-    const int4 x = __ldg(sp.span + v);
-    const int nt = max(1, (x.z - (x.w & ~15) + kFewTile - 1) / kFewTile);
-    const int64_t at = __ldg(sp.before + v) + (int64_t)h * (nt + kFewOver) + kFewOver;
-    const int64_t b = (few_B * (at + 1) - 1) / few_total, l = (few_B * (at + nt) - 1) / few_total;
-    return {b, (int)(l - b) + 1};
-  };
-  const int tiles = kFewGroups ? 0 : __ldg(p.first + p.groups + p.seqs);
-  const int64_t total = tiles ? __ldg(p.before + tiles) * st.Hkv : 0, B = max((int64_t)1, min((int64_t)blocks, total / 2));
-  auto many_run = [&](int i, int v, int4 x) -> Run {
-    const int f = __ldg(p.first + v), e = __ldg(p.first + v + 1);
-    const int64_t b0 = __ldg(p.before + f), at = b0 * st.Hkv + h * (__ldg(p.before + e) - b0) + __ldg(p.before + i) - b0 + C::kOver;
-    const int nt = max(1, (x.w - x.z + kKeys - 1) / kKeys), two = x.y > 128;
-    const int64_t b = (B * (at + 1) - 1) / total, l = (B * (at + ((int64_t)(nt - 1) << two) + 1) - 1) / total;
-    return {b, (int)(l - b) + 1};
-  };
-  int s, q0, rows, qt = 0, tile_rows = 0;
-  Run own;
+  int s, qt = 0, of = 0;
+  int2 own;
   if constexpr (kFewSeqs) {
     s = blockIdx.x;
-    const int4 x = __ldg(sp.span + few_groups + s);
-    q0 = x.x, rows = x.y * st.G;
-    if (r0 >= rows) return;
-    own = few_run(few_groups + s);
+    own = __ldg(sp.runs + (few_groups + s) * st.Hkv + h);
   } else {
     const int tile = __ldg(p.first + p.groups) + (int)blockIdx.x;
-    if (tile >= tiles) return;
-    const int4 ta = __ldg(p.tile + 2 * tile), tb = __ldg(p.tile + 2 * tile + 1);
-    s = ta.x, q0 = ta.y, qt = tb.x, rows = tile_rows = tb.y;
-    if (r0 >= rows) return;
-    own = many_run(tile, p.groups + s, tb);
+    if (tile >= __ldg(p.first + p.groups + p.seqs)) return;
+    s = __ldg(&p.tile[2 * tile].x);
+    const int4 x = __ldg(p.tile + 2 * tile + 1);
+    qt = x.x, of = x.y;
+    own = __ldg(p.runs + (int64_t)tile * st.Hkv + h);
   }
-  rows = min(kJoinRows, rows - r0);
-  const int group = __ldg(&sp.seq[s].x);
-  int4 g = make_int4(0, 0, 0, 0);
-  Run with = {0, 0};
-  if (group >= 0) {
-    g = __ldg(sp.group + group);
-    if (kFewGroups) with = few_run(group);
-  }
-  for (int i = tid; i < rows * (D / 4); i += kJoinThreads) {
+  const int4 ja = __ldg(sp.join + 2 * s), jb = __ldg(sp.join + 2 * s + 1);
+  const int q0 = ja.x, all_rows = kFewSeqs ? ja.y * st.G : of;
+  if (r0 >= all_rows) return;
+  const int rows = min(kR, all_rows - r0), items = rows * kCols;
+  const int P = items < kJoinThreads ? kJoinThreads / items : 1;
+  int2 with = make_int2(0, 0);
+  if (kFewGroups && ja.w) with = __ldg(sp.runs + jb.x * st.Hkv + h);
+  const int64_t half = (int64_t)st.n_tokens * st.Hq;
+  for (int i0 = 0; i0 < items; i0 += kJoinThreads) {
+    const int pg = P > 1 ? tid / items : 0, i = P > 1 ? tid - pg * items : i0 + tid;
+    const bool in = i < items && pg < P;
     // (neighbouring threads take what neighbours in memory: columns, or rows as tiles leave them)
-    const int r = r0 + (kFewGroups ? i / (D / 4) : i % rows), col = kFewGroups ? i % (D / 4) : i / rows, R = qt * C::kRows + r;
+    const int r = r0 + (kFewGroups ? i / kCols : i % rows), col = kFewGroups ? i % kCols : i / rows, R = qt * C::kRows + r;
     const int tok = q0 + R / st.G, head = h * st.G + R % st.G;
     float mx = -INFINITY, ls = 0.f;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -1110,46 +1120,55 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_
       ls = ls * f + w * ml.y;
       mx = to;
     };
-    auto add_many = [&](const Run& run, int64_t place, int of, int row) {  // place: of the tile's `of` rows, where it is whole
-      if (run.n == 1) {
-        add(parts.whole_ml[place + row], *reinterpret_cast<const float4*>(parts.whole + place * D + ((int64_t)col * of + row) * 4));
+    int turn = pg;  // of this thread's next piece among those that are left
+    auto add_many = [&](int2 run, int64_t place, int tile_rows, int row) {  // place: of the tile's rows, where it is whole
+      if (run.y == 1) {
+        if (turn == 0)
+          add(parts.whole_ml[place + row], *reinterpret_cast<const float4*>(parts.whole + place * D + ((int64_t)col * tile_rows + row) * 4));
       } else {
 #pragma unroll 4
-        for (int k = 0; k < run.n; ++k) {
-          const int64_t part = (k == 0 ? run.b * 2 + 1 : (run.b + k) * 2) * C::kRows;
+        for (int k = turn; k < run.y; k += P) {
+          const int64_t part = (int64_t)(k == 0 ? run.x * 2 + 1 : (run.x + k) * 2) * C::kRows;
           add(parts.ml[part + row], *reinterpret_cast<const float4*>(parts.o + part * D + (col * C::kRows + row) * 4));
         }
       }
+      turn = ((turn - run.y) % P + P) % P;
     };
-    auto add_few = [&](const Run& run, int64_t half, int row) {
-      if (run.n == 1) {
-        const int64_t place = half + (int64_t)tok * st.Hq + head;
-        add(few.whole_ml[place], *reinterpret_cast<const float4*>(few.whole + place * D + col * 4));
+    auto add_few = [&](int2 run, int64_t from, int row) {
+      if (run.y == 1) {
+        const int64_t place = from + (int64_t)tok * st.Hq + head;
+        if (turn == 0) add(few.whole_ml[place], *reinterpret_cast<const float4*>(few.whole + place * D + col * 4));
       } else {
 #pragma unroll 4
-        for (int k = 0; k < run.n; ++k) {
-          const int64_t at = (k == 0 ? run.b * 2 + 1 : (run.b + k) * 2) * few_rows + row;
+        for (int k = turn; k < run.y; k += P) {
+          const int64_t at = (int64_t)(k == 0 ? run.x * 2 + 1 : (run.x + k) * 2) * few_rows + row;
           add(few.ml[at], *reinterpret_cast<const float4*>(few.o + at * D + col * 4));
         }
       }
+      turn = ((turn - run.y) % P + P) % P;
     };
-    if (g.z) {
-      const int64_t at = (int64_t)(tok - g.y) * st.G + R % st.G;  // the row among the group's
-      if (at >= 0 && at < (int64_t)g.z * st.G) {
+    if (in) {
+      const int64_t at = (int64_t)(tok - ja.z) * st.G + R % st.G;  // the row among the group's
+      if (at >= 0 && at < (int64_t)ja.w * st.G) {
         if constexpr (kFewGroups) {
           add_few(with, 0, (int)at);
         } else {
-          const int t = (int)(at / C::kRows), i0 = __ldg(p.first + group) + t;
-          if (i0 < __ldg(p.first + group + 1)) {
-            const int4 x = __ldg(p.tile + 2 * i0 + 1);
-            add_many(many_run(i0, group, x), ((int64_t)h * st.n_tokens + g.y) * st.G + (int64_t)t * C::kRows, x.y, (int)(at - (int64_t)t * C::kRows));
-          }
+          const int t = (int)(at / C::kRows);
+          if (t < jb.y)
+            add_many(__ldg(p.runs + (int64_t)(jb.x + t) * st.Hkv + h), ((int64_t)h * st.n_tokens + ja.z) * st.G + (int64_t)t * C::kRows,
+                     (int)min((int64_t)C::kRows, (int64_t)ja.w * st.G - (int64_t)t * C::kRows), (int)(at - (int64_t)t * C::kRows));
         }
       }
+      if constexpr (kFewSeqs) add_few(own, half, r);
+      else add_many(own, half + ((int64_t)h * st.n_tokens + q0) * st.G + qt * C::kRows, of, r);
     }
-    const int64_t half = (int64_t)st.n_tokens * st.Hq;
-    if constexpr (kFewSeqs) add_few(own, half, r);
-    else add_many(own, half + ((int64_t)h * st.n_tokens + q0) * st.G + qt * C::kRows, tile_rows, r);
+    if (P > 1) {  // (one round: the other parts of the row)
+      s_o[tid] = sum, s_ml[tid] = make_float2(mx, ls);
+      __syncthreads();
+      if (pg != 0) return;
+      for (int k = 1; k < P; ++k) add(s_ml[tid + k * items], s_o[tid + k * items]);
+    }
+    if (!in) continue;
     const float inv = ls == 0.f ? 0.f : 1.f / ls;  // (a NaN in the scores stays NaN)
     T* out = static_cast<T*>(c.out) + (int64_t)tok * c.out_stride + (int64_t)head * D + col * 4;
     *reinterpret_cast<uint2*>(out) = make_uint2(Half2<T>::down(sum.x * inv, sum.y * inv), Half2<T>::down(sum.z * inv, sum.w * inv));
@@ -1202,15 +1221,16 @@ cudaError_t run_shared(const AttnCall& c, const AttnMaps& maps, const SharedGrou
   }
   const int few_rows = (int)(few_groups && g.n ? rows : seq_rows), few_blocks = attn_few_fit(D, sms);
   if (e == cudaSuccess && few_seqs) {
-    const FewShared f = {sh.found.span, sh.found.group, sh.found.before, n_few_groups, tiles == 0, few_blocks};
+    const FewShared f = {sh.found.span, sh.found.group, sh.found.before, sh.found.runs, n_few_groups, tiles == 0, few_blocks};
     e = launch_attn_few_shared(c, sh.few, f, few_rows, D, kBf, sms, s);
   }
   if (e != cudaSuccess) return e;
+  const int join_rows = few_seqs ? kJoinRows<true> : kJoinRows<false>;
   const int64_t in_tile = few_seqs || seq_rows < C::kRows ? seq_rows : C::kRows;
-  const dim3 blocks((unsigned)(few_seqs ? c.st.n_seqs : own), (unsigned)c.st.Hkv, (unsigned)((in_tile + kJoinRows - 1) / kJoinRows));
+  const dim3 blocks((unsigned)(few_seqs ? c.st.n_seqs : own), (unsigned)c.st.Hkv, (unsigned)((in_tile + join_rows - 1) / join_rows));
   auto join = few_groups ? k_attn_join_shared<T, D, true, true> : few_seqs ? k_attn_join_shared<T, D, false, true> : k_attn_join_shared<T, D, false, false>;
-  return launch_pdl(true, join, blocks, dim3(kJoinThreads), 0, s, c, plan, sh.found, sh.parts, sh.few, (int)grid, few_blocks,
-                    attn_few_part_rows(few_rows), n_few_groups);
+  return launch_pdl(true, join, blocks, dim3(kJoinThreads), 0, s, c, plan, sh.found, sh.parts, sh.few, attn_few_part_rows(few_rows),
+                    n_few_groups);
 }
 
 }  // namespace
