@@ -241,7 +241,7 @@ extern "C" int mf_attn_create(mf_attn_t** out, const mf_attn_shape_t* shape, int
   h->err = reinterpret_cast<unsigned*>(ws + o_err);
   h->parts = {reinterpret_cast<float*>(ws + o_o), reinterpret_cast<float2*>(ws + o_ml), reinterpret_cast<AttnRec*>(ws + o_rec), nullptr, nullptr};
   h->plan = {reinterpret_cast<int*>(ws + o_first), reinterpret_cast<int4*>(ws + o_tile), reinterpret_cast<int64_t*>(ws + o_before),
-             (int)tiles, 0, 0, nullptr};
+             (int)tiles, 0, 0, nullptr, nullptr};
   if (e == cudaSuccess) e = cudaMemset(h->err, 0, 256);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();
   if (e != cudaSuccess) {
@@ -401,6 +401,7 @@ extern "C" int mf_attn_share(mf_attn_t* attn, int max_groups) {
                o_span = w.take(((size_t)max_groups + attn->max_seqs) * 16), o_fbefore = w.take(((size_t)max_groups + attn->max_seqs + 1) * 8),
                o_join = w.take((size_t)attn->max_seqs * 32), o_runs = w.take((size_t)tiles * sh.n_kv_heads * 8),
                o_fruns = w.take(((size_t)max_groups + attn->max_seqs) * sh.n_kv_heads * 8),
+               o_start = w.take((size_t)attn->sms * 48), o_fstart = w.take((size_t)attn_few_blocks(attn->sms) * 64),
                o_whole = w.take((size_t)rows * 2 * sh.head_dim * 4), o_whole_ml = w.take((size_t)rows * 2 * 8);
   unsigned char* ws = nullptr;
   cudaError_t e = tiles < (1 << 30) ? cudaMalloc(&ws, w.off) : cudaErrorMemoryAllocation;
@@ -420,9 +421,9 @@ extern "C" int mf_attn_share(mf_attn_t* attn, int max_groups) {
   a.mem = ws;
   a.found = {reinterpret_cast<int*>(ws + o_bound), reinterpret_cast<int4*>(ws + o_group), reinterpret_cast<int2*>(ws + o_seq),
              reinterpret_cast<int4*>(ws + o_join), reinterpret_cast<int4*>(ws + o_span), reinterpret_cast<int64_t*>(ws + o_fbefore),
-             reinterpret_cast<int2*>(ws + o_fruns)};
+             reinterpret_cast<int2*>(ws + o_fruns), reinterpret_cast<int4*>(ws + o_fstart)};
   a.plan = {reinterpret_cast<int*>(ws + o_first), reinterpret_cast<int4*>(ws + o_tile), reinterpret_cast<int64_t*>(ws + o_before),
-            (int)tiles, 0, 0, reinterpret_cast<int2*>(ws + o_runs)};
+            (int)tiles, 0, 0, reinterpret_cast<int2*>(ws + o_runs), reinterpret_cast<longlong2*>(ws + o_start)};
   a.parts = {reinterpret_cast<float*>(ws + o_o), reinterpret_cast<float2*>(ws + o_ml), nullptr, reinterpret_cast<float*>(ws + o_whole),
              reinterpret_cast<float2*>(ws + o_whole_ml)};
   a.few = {reinterpret_cast<float*>(ws + o_few), reinterpret_cast<float2*>(ws + o_few_ml), nullptr, a.parts.whole, a.parts.whole_ml};

@@ -168,6 +168,8 @@ struct AttnPlan {
   // head the block that has its first key tile and how many have one
   int groups, seqs;
   int2* runs;       // [max_tiles][kv heads]
+  // where each block begins: {row tile, kv head, blocks that have work, -}, {place of the tile's segment, beginning of the share}, {its end, all}
+  longlong2* start;  // [blocks][3]
 };
 
 // Groups of sequences that share their first lines (mf_shared_t), and what k_attn_plan_shared finds of them.
@@ -187,11 +189,13 @@ struct SharedPlan {
   int4* span;       // [max_groups + max_seqs]
   int64_t* before;  // [max_groups + max_seqs + 1]
   int2* runs;       // [max_groups + max_seqs][kv heads]
+  // where its blocks begin: {sequence, kv head, row of the page table, blocks that have work}, its span, {place, beginning of the share}, {its
+  // end, all}
+  int4* start;      // [blocks][4]
 };
 // A step whose groups share lines, as launch_attn_few_shared takes it.
 struct FewShared {
-  const int4 *span, *group;
-  const int64_t* before;
+  const int4 *span, *group, *start;
   int2* runs;
   int groups;  // virtual sequences before the step's
   int wait;    // the kernel before this one is the plan

@@ -62,15 +62,17 @@ __device__ __forceinline__ Span span_of(const AttnCall& c, int s) {
 }
 
 __device__ __forceinline__ Span span_of(const AttnCall& c, const Alone&, int s) { return span_of(c, s); }
-__device__ __forceinline__ Span span_of(const AttnCall&, const FewShared& f, int v) {
-  const int4 x = __ldg(f.span + v);
+__device__ __forceinline__ Span span_of(int4 x, int row) {
   Span r;
   r.sp = {x.x, x.y, x.z};
   r.skip = x.w;
   r.start = x.w & ~(kUnit - 1);
   r.nt = x.y == 0 ? 0 : max(1, (x.z - r.start + kTile - 1) / kTile);
-  r.row = v < f.groups ? __ldg(f.group + v).x : v - f.groups;
+  r.row = row;
   return r;
+}
+__device__ __forceinline__ Span span_of(const AttnCall&, const FewShared& f, int v) {
+  return span_of(f.span[v], v < f.groups ? f.group[v].x : v - f.groups);
 }
 
 // a place in a block's share of the list
@@ -141,24 +143,11 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
   __shared__ float s_m[kWarps][16], s_l[kWarps][16];
   const AttnStep& st = c.st;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  int64_t total = 0, B, t0, t1;
+  int64_t total = 0, B, t0, t1;  // the list, the blocks that have work, this one's share
   if constexpr (kShared) {
-    // The plan, which was there before this launch's blocks could start, has the places of the (virtual) sequences.  Where the
-    // kernel before this one is that of the groups' lines, nothing of it is waited for until the end.
+    // The plan, which was there before this launch's blocks could start, says where each begins.  Where the kernel before this one
+    // is that of the groups' lines, nothing of it is waited for until the end.
     if (extra.wait) pdl_wait();
-    const int V = extra.groups + st.n_seqs;
-    total = __ldg(extra.before + V);
-    B = min((int64_t)gridDim.x, total);
-    if (blockIdx.x >= B) {
-      if (!extra.wait) pdl_wait();
-      return;
-    }
-    t0 = total * blockIdx.x / B, t1 = total * (blockIdx.x + 1) / B;
-    for (int v = tid; v < V; v += kThreads) {
-      const int64_t at = __ldg(extra.before + v);
-      if (t0 >= at && t0 < __ldg(extra.before + v + 1)) s_seq = v, s_at = at;
-    }
-    __syncthreads();
   } else {
     pdl_wait();
 
@@ -206,10 +195,20 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
     }
   }
   Cursor<Extra> cur;
-  cur.s = s_seq;
-  cur.sn = span_of(c, extra, cur.s);
-  cur.h = (int)((t0 - s_at) / (cur.sn.nt + kOver));
-  cur.at = s_at + (int64_t)cur.h * (cur.sn.nt + kOver);
+  if constexpr (kShared) {
+    // (ordinary loads: read-only ones may be moved ahead of the wait)
+    const int4* at = extra.start + blockIdx.x * 4;
+    const int4 x = at[0], y = at[1];
+    const longlong2 u = *reinterpret_cast<const longlong2*>(at + 2), w = *reinterpret_cast<const longlong2*>(at + 3);
+    B = x.w, total = w.y, t0 = u.y, t1 = w.x;
+    cur.s = x.x, cur.h = x.y, cur.at = u.x;
+    cur.sn = span_of(y, x.z);
+  } else {
+    cur.s = s_seq;
+    cur.sn = span_of(c, extra, cur.s);
+    cur.h = (int)((t0 - s_at) / (cur.sn.nt + kOver));
+    cur.at = s_at + (int64_t)cur.h * (cur.sn.nt + kOver);
+  }
   cur.t1 = t1;
   cur.j = (int)max((int64_t)0, t0 - cur.at - kOver);
   cur.limit();

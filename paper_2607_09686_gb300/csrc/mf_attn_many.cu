@@ -134,10 +134,11 @@ __global__ void __launch_bounds__(1024) k_attn_plan(AttnCall c, AttnPlan p) {
 // The same of a step whose groups of sequences share their first lines: as many virtual sequences as there are groups, with the rows of
 // all the group's tokens and the shared lines (whole pages of them), then the sequences, with what follows.  First the groups: bounds
 // that rise, lengths that all their sequences have; a group of one shares nothing.  p.groups and p.seqs say which of them are in the list
-// of this file's kernel, few_groups and few_seqs which are in that of few rows.
+// of this file's kernel, few_groups and few_seqs which are in that of few rows.  Two blocks, both of which find the groups: the first lays out this
+// file's list and says where its kernel's blocks begin, the second the other list, and what the join asks for.
 template <int D>
 __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGroups g, AttnPlan p, SharedPlan sp, int few_groups,
-                                                           int few_seqs) {
+                                                           int few_seqs, int blocks, int few_blocks) {
   __shared__ int64_t s_warp[32];
   // what the phases hand on, in shared memory where it finds room: the sequences' spans and groups, the groups, first row tiles
   constexpr int kSmall = 1024;
@@ -145,6 +146,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
   __shared__ int2 s_seq[kSmall];
   __shared__ int4 s_group[kSmall / 4];
   __shared__ int s_bound[kSmall / 4 + 1], s_first[kSmall + 1];
+  __shared__ int64_t s_before[kSmall + 1];  // of row tiles, or of the list of few rows
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_seqs = c.st.n_seqs;
   const int V = p.groups + p.seqs, few = few_groups + few_seqs;
   const bool small_seqs = n_seqs <= kSmall, small_groups = g.n <= kSmall / 4, small = V <= kSmall;
@@ -152,6 +154,8 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
   int4* group = small_groups ? s_group : sp.group;
   int2* seq = small_seqs ? s_seq : sp.seq;
   int* first = small ? s_first : p.first;
+  const bool lists = blockIdx.x == 0;
+  if (lists && V == 0) return;
   pdl_wait();
   pdl_trigger();
   auto span = [&](int s) -> SeqSpan { return small_seqs ? s_span[s] : seq_span(c.st, s); };
@@ -182,7 +186,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
   int from = 0;
   for (int base = 0; base <= g.n; base += 1024) {
     const int i = base + tid;
-    const int raw = i <= g.n && g.n ? __ldg(g.first + i) : 0;
+    const int raw = i <= g.n && g.n ? g.first[i] : 0;
     int x = min(max(raw, 0), n_seqs);
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -215,7 +219,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     }
     for (int d = 1; d < width; d <<= 1) least = min(least, __shfl_xor_sync(0xffffffffu, least, d));
     if (i < g.n) {
-      const int asked = __ldg(g.len + i), len = max(0, min(asked, least));
+      const int asked = g.len[i], len = max(0, min(asked, least));
       if (len != asked && sub == 0 && a < b) attn_report(c.st, kAttnRange);
       const int lines = b - a > 1 ? (int)fast_div((uint32_t)len, c.st.page_mul, c.st.page_shift) * c.st.page_size : 0;
       int q0 = 0, n = 0;
@@ -228,8 +232,92 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     }
   }
   __syncthreads();
-  // ---- the list of few rows
+  // ---- row tiles of the virtual sequences
   int64_t done = 0;
+  for (int base = 0; base < V; base += 1024) {
+    const int v = base + tid;
+    int64_t n = 0, all;
+    if (v < V) {
+      const int tokens = v < p.groups ? group[v].z : span(v - p.groups).n;
+      n = ((int64_t)tokens * c.st.G + Cfg<D>::kRows - 1) / Cfg<D>::kRows;
+    }
+    const int64_t at = done + scan(n, all);
+    if (v < V) first[v] = p.first[v] = (int)min(at, (int64_t)p.max_tiles);
+    done += all;
+  }
+  const int tiles = (int)min(done, (int64_t)p.max_tiles);
+  if (tid == 0 && V) first[V] = p.first[V] = tiles;
+  __syncthreads();
+  if (lists) {
+    int64_t* before = tiles <= kSmall ? s_before : p.before;
+    int64_t jobs = 0;
+    for (int base = 0; base < tiles; base += 1024) {
+      const int i = base + tid;
+      int64_t n = 0;
+      if (i < tiles) {
+        int lo = 0, hi = V - 1;  // the last virtual sequence whose first tile is at or before i
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) >> 1;
+          if (first[mid] <= i) lo = mid;
+          else hi = mid - 1;
+        }
+        const int qt = i - first[lo], R0 = qt * Cfg<D>::kRows, G = c.st.G;
+        int s, start, end, rows;
+        SeqSpan q;
+        if (lo < p.groups) {
+          const int4 x = group[lo];
+          s = x.x, q = {x.y, x.z, x.w};
+          rows = min(Cfg<D>::kRows, q.n * G - R0), start = 0, end = x.w;
+        } else {
+          s = lo - p.groups, q = span(s);
+          rows = min(Cfg<D>::kRows, q.n * G - R0), start = seq[s].y;
+          end = max(start, vis_hi(c, q.len - q.n + (R0 + rows - 1) / G, q.len));
+        }
+        p.tile[2 * i] = make_int4(s, q.q0, q.n, q.len);
+        p.tile[2 * i + 1] = make_int4(qt, rows, start, end);
+        n = ((int64_t)max(1, (end - start + kKeys - 1) / kKeys) << (Cfg<D>::kRowTiles == 2 && rows > 128)) + Cfg<D>::kOver;
+      }
+      int64_t all;
+      const int64_t at = jobs + scan(n, all);
+      if (i < tiles) before[i] = at;
+      jobs += all;
+    }
+    if (tid == 0) before[tiles] = jobs;
+    __syncthreads();
+    // ---- where the blocks begin: every one that works has two jobs at least, so that it has a key tile's start
+    const int64_t total = jobs * c.st.Hkv, B = max((int64_t)1, min((int64_t)blocks, total / 2));
+    for (int b = tid; b < blocks; b += 1024) {
+      const int64_t t0 = b < B ? total * b / B : 0, t1 = b < B ? total * (b + 1) / B : 0;
+      int tile = 0, h = 0;
+      int64_t at = 0;
+      if (t0 < t1) {
+        int lo = 0, hi = V - 1;  // the last virtual sequence that begins at or before t0, then the kv head, then the tile
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) >> 1;
+          if (first[mid] < tiles && before[first[mid]] * c.st.Hkv <= t0) lo = mid;
+          else hi = mid - 1;
+        }
+        const int f = first[lo];
+        const int64_t b0 = before[f], len = before[first[lo + 1]] - b0;
+        h = (int)((t0 - b0 * c.st.Hkv) / len);
+        const int64_t head = b0 * c.st.Hkv + h * len;
+        int x = f, y = first[lo + 1] - 1;
+        while (x < y) {
+          const int mid = (x + y + 1) >> 1;
+          if (head + before[mid] - b0 <= t0) x = mid;
+          else y = mid - 1;
+        }
+        tile = x, at = head + before[x] - b0;
+      }
+      longlong2* to = p.start + 3 * b;
+      *reinterpret_cast<int4*>(to) = make_int4(tile, h, (int)B, 0);
+      to[1] = make_longlong2(at, t0), to[2] = make_longlong2(t1, total);
+    }
+    return;
+  }
+  // ---- the list of few rows
+  int64_t* before = few <= kSmall ? s_before : sp.before;
+  done = 0;
   for (int base = 0; base < few; base += 1024) {
     const int v = base + tid;
     int64_t n = 0, all;
@@ -246,59 +334,40 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
       if (x.y) n = (int64_t)(max(1, (x.z - (x.w & ~15) + kFewTile - 1) / kFewTile) + kFewOver) * c.st.Hkv;
     }
     const int64_t at = done + scan(n, all);
-    if (v < few) sp.before[v] = at;
+    if (v < few) before[v] = at;
     done += all;
   }
-  if (tid == 0 && few) sp.before[few] = done;
-  // ---- row tiles of the virtual sequences
-  done = 0;
-  for (int base = 0; base < V; base += 1024) {
-    const int v = base + tid;
-    int64_t n = 0, all;
-    if (v < V) {
-      const int tokens = v < p.groups ? group[v].z : span(v - p.groups).n;
-      n = ((int64_t)tokens * c.st.G + Cfg<D>::kRows - 1) / Cfg<D>::kRows;
-    }
-    const int64_t at = done + scan(n, all);
-    if (v < V) first[v] = p.first[v] = (int)min(at, (int64_t)p.max_tiles);
-    done += all;
-  }
-  const int tiles = (int)min(done, (int64_t)p.max_tiles);
-  if (tid == 0 && V) first[V] = p.first[V] = tiles;
+  if (tid == 0 && few) before[few] = done;
   __syncthreads();
-  int64_t jobs = 0;
-  for (int base = 0; base < tiles; base += 1024) {
-    const int i = base + tid;
-    int64_t n = 0;
-    if (i < tiles) {
-      int lo = 0, hi = V - 1;  // the last virtual sequence whose first tile is at or before i
+  const int64_t B = min((int64_t)few_blocks, done);
+  for (int b = tid; b < few_blocks && few; b += 1024) {
+    const int64_t t0 = b < B ? done * b / B : 0, t1 = b < B ? done * (b + 1) / B : 0;
+    int v = 0, h = 0, row = 0;
+    int64_t at = 0;
+    int4 x = make_int4(0, 0, 0, 0);
+    if (t0 < t1) {
+      int lo = 0, hi = few - 1;  // the last one that begins at or before t0 (none of those after it that begin there too is empty)
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (first[mid] <= i) lo = mid;
+        if (before[mid] <= t0) lo = mid;
         else hi = mid - 1;
       }
-      const int qt = i - first[lo], R0 = qt * Cfg<D>::kRows, G = c.st.G;
-      int s, start, end, rows;
-      SeqSpan q;
-      if (lo < p.groups) {
-        const int4 x = group[lo];
-        s = x.x, q = {x.y, x.z, x.w};
-        rows = min(Cfg<D>::kRows, q.n * G - R0), start = 0, end = x.w;
+      v = lo;
+      if (v < few_groups) {
+        const int4 y = group[v];
+        x = make_int4(y.y, y.z, y.w, 0), row = y.x;
       } else {
-        s = lo - p.groups, q = span(s);
-        rows = min(Cfg<D>::kRows, q.n * G - R0), start = seq[s].y;
-        end = max(start, vis_hi(c, q.len - q.n + (R0 + rows - 1) / G, q.len));
+        const SeqSpan q = span(v - few_groups);
+        x = make_int4(q.q0, q.n, q.len, seq[v - few_groups].y), row = v - few_groups;
       }
-      p.tile[2 * i] = make_int4(s, q.q0, q.n, q.len);
-      p.tile[2 * i + 1] = make_int4(qt, rows, start, end);
-      n = ((int64_t)max(1, (end - start + kKeys - 1) / kKeys) << (Cfg<D>::kRowTiles == 2 && rows > 128)) + Cfg<D>::kOver;
+      const int64_t len = (before[v + 1] - before[v]) / c.st.Hkv;
+      h = (int)((t0 - before[v]) / len);
+      at = before[v] + h * len;
     }
-    int64_t all;
-    const int64_t at = jobs + scan(n, all);
-    if (i < tiles) p.before[i] = at;
-    jobs += all;
+    int4* to = sp.start + 4 * b;
+    to[0] = make_int4(v, h, row, (int)B), to[1] = x;
+    reinterpret_cast<longlong2*>(to)[2] = make_longlong2(at, t0), reinterpret_cast<longlong2*>(to)[3] = make_longlong2(t1, done);
   }
-  if (tid == 0 && V) p.before[tiles] = jobs;
   // ---- what the join asks for
   for (int s = tid; s < n_seqs; s += 1024) {
     const SeqSpan q = span(s);
@@ -389,6 +458,17 @@ __device__ __noinline__ void walk_start(Walk<kRows, kOver>& w, const AttnCall& c
   w.tile = lo;
   w.at = head + __ldg(p.before + lo) - b0;
   w.set(__ldg(p.tile + 2 * lo), __ldg(p.tile + 2 * lo + 1));
+  w.ask(c, p);
+  if (w.j0 >= w.j1) w.next(c, p);
+}
+
+// the same where the plan has found it
+template <int kRows, int kOver>
+__device__ __forceinline__ void walk_from(Walk<kRows, kOver>& w, const AttnCall& c, const AttnPlan& p, int4 x, longlong2 u, int64_t t1) {
+  w.t0 = u.y, w.t1 = t1, w.at = u.x, w.tile = x.x, w.h = x.y;
+  w.more = w.t0 < w.t1;
+  if (!w.more) return;
+  w.set(__ldg(p.tile + 2 * w.tile), __ldg(p.tile + 2 * w.tile + 1));
   w.ask(c, p);
   if (w.j0 >= w.j1) w.next(c, p);
 }
@@ -519,12 +599,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
   pdl_wait();
   pdl_trigger();
 
-  const int groups = kShared ? p.groups : 0, tiles = __ldg(p.first + (kShared ? groups + p.seqs : st.n_seqs));
-  const int64_t total = tiles ? __ldg(p.before + tiles) * st.Hkv : 0;
-  // every block that works has at least two jobs, so that it has a key tile's start
-  const int64_t B = max((int64_t)1, min((int64_t)gridDim.x, total / 2));
+  int tiles = 0;
+  int64_t total, B, t0, t1;
   const int64_t b = blockIdx.x;
-  const int64_t t0 = b < B ? total * b / B : 0, t1 = b < B ? total * (b + 1) / B : 0;
+  int4 start_x = make_int4(0, 0, 0, 0);
+  longlong2 start_u = make_longlong2(0, 0);
+  if constexpr (kShared) {
+    // (ordinary loads: read-only ones may be moved ahead of the wait)
+    start_x = *reinterpret_cast<const int4*>(p.start + 3 * b);
+    start_u = p.start[3 * b + 1];
+    const longlong2 w = p.start[3 * b + 2];
+    total = w.y, B = start_x.z, t0 = start_u.y, t1 = w.x;
+  } else {
+    tiles = __ldg(p.first + st.n_seqs);
+    total = tiles ? __ldg(p.before + tiles) * st.Hkv : 0;
+    // every block that works has at least two jobs, so that it has a key tile's start
+    B = max((int64_t)1, min((int64_t)gridDim.x, total / 2));
+    t0 = b < B ? total * b / B : 0, t1 = b < B ? total * (b + 1) / B : 0;
+  }
+  auto walk_begin = [&](Walk<C::kRows, C::kOver>& w) {
+    if constexpr (kShared) walk_from(w, c, p, start_x, start_u, t1);
+    else walk_start(w, c, p, tiles, t0, t1);
+  };
 
   auto wait = [&](int bar, uint32_t parity) -> bool {  // bounded
     return mbar_try_wait(&bars[bar], parity) || wait_slow(&bars[bar], parity, &s_flag, st.err);
@@ -788,7 +884,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     auto uniform = [](uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); };
     const uint32_t bars0 = uniform(smem_u32(bars)), tm = uniform(tmem);
     Walk<C::kRows, C::kOver> w0;
-    walk_start(w0, c, p, tiles, t0, t1);
+    walk_begin(w0);
     Walk<C::kRows, C::kOver> w = w0;
     Jobs jb{};
     jb.take(w);
@@ -953,10 +1049,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
       pending = bar;
     };
     Walk<C::kRows, C::kOver> w0;
-    walk_start(w0, c, p, tiles, t0, t1);
+    walk_begin(w0);
     Walk<C::kRows, C::kOver> w = w0;
     int told = 0;
-    const int group_tiles = kShared ? __ldg(p.first + groups) : 0;
+    const int group_tiles = kShared ? p.first[p.groups] : 0;
     uint32_t tph = 1;
     auto tell = [&]() -> bool {  // the softmax what comes
       if (!wait_free(kBPieceFree + told, tph)) return false;
@@ -1066,113 +1162,148 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
 
 // ---- the joined result of a step whose groups share lines
 
-// A block: some rows of a sequence (of one of its row tiles, where they are many) and a kv head.  A row's pieces are the group's, in the order
-// of the lines, and then the sequence's own; the blocks that have them were noted by the one that had the first.  A thread has
-// four columns of a row, and where the rows are few every P-th piece.  kFewGroups, kFewSeqs: the groups' lines, the sequences' own were
-// the kernel's of few rows.
-constexpr int kJoinThreads = 256;
-template <bool kFewSeqs>
-constexpr int kJoinRows = kFewSeqs ? 2 : 16;
+// A block: eight rows of a sequence (of one of its row tiles, where they are many) and a kv head.  A row's pieces are the group's, in the
+// order of the lines, and then the sequence's own; the blocks that have them were noted by the one that had the first.  A warp forms the weights
+// of a row's pieces; then a thread has four columns of a row and, where rows times columns are fewer than threads, every P-th
+// piece.  kFewGroups, kFewSeqs: the groups' lines, the sequences' own were the kernel's of few rows.
+constexpr int kJoinThreads = 256, kJoinRows = kJoinThreads / 32, kJoinPieces = 640;
+struct JoinRun {  // a row's n pieces: four columns of piece k at o + k * step + column * next, of the first `first` farther on
+  const float* o;
+  int64_t step, first;
+  int next, n;
+};
 template <class T, int D, bool kFewGroups, bool kFewSeqs>
 __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_constant__ AttnCall c, const __grid_constant__ AttnPlan p,
                                                                    const __grid_constant__ SharedPlan sp,
                                                                    const __grid_constant__ AttnParts parts,
                                                                    const __grid_constant__ AttnParts few, int few_rows, int few_groups) {
   using C = Cfg<D>;
-  constexpr int kR = kJoinRows<kFewSeqs>, kCols = D / 4;
+  constexpr int kCols = D / 4;
+  __shared__ float s_w[kJoinRows][kJoinPieces];
   __shared__ float4 s_o[kJoinThreads];
-  __shared__ float2 s_ml[kJoinThreads];
+  __shared__ JoinRun s_run[kJoinRows][2];
+  __shared__ float s_inv[kJoinRows];
   const AttnStep& st = c.st;
-  const int h = blockIdx.y, r0 = blockIdx.z * kR, tid = threadIdx.x;
+  const int h = blockIdx.y, r0 = blockIdx.z * kJoinRows, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
   int s, qt = 0, of = 0;
   int2 own;
   if constexpr (kFewSeqs) {
     s = blockIdx.x;
-    own = __ldg(sp.runs + (few_groups + s) * st.Hkv + h);
+    own = sp.runs[(few_groups + s) * st.Hkv + h];
   } else {
-    const int tile = __ldg(p.first + p.groups) + (int)blockIdx.x;
-    if (tile >= __ldg(p.first + p.groups + p.seqs)) return;
-    s = __ldg(&p.tile[2 * tile].x);
-    const int4 x = __ldg(p.tile + 2 * tile + 1);
+    const int tile = p.first[p.groups] + (int)blockIdx.x;
+    if (tile >= p.first[p.groups + p.seqs]) return;
+    s = p.tile[2 * tile].x;
+    const int4 x = p.tile[2 * tile + 1];
     qt = x.x, of = x.y;
-    own = __ldg(p.runs + (int64_t)tile * st.Hkv + h);
+    own = p.runs[(int64_t)tile * st.Hkv + h];
   }
-  const int4 ja = __ldg(sp.join + 2 * s), jb = __ldg(sp.join + 2 * s + 1);
+  const int4 ja = sp.join[2 * s], jb = sp.join[2 * s + 1];
   const int q0 = ja.x, all_rows = kFewSeqs ? ja.y * st.G : of;
   if (r0 >= all_rows) return;
-  const int rows = min(kR, all_rows - r0), items = rows * kCols;
-  const int P = items < kJoinThreads ? kJoinThreads / items : 1;
-  int2 with = make_int2(0, 0);
-  if (kFewGroups && ja.w) with = __ldg(sp.runs + jb.x * st.Hkv + h);
-  const int64_t half = (int64_t)st.n_tokens * st.Hq;
+  const int rows = min(kJoinRows, all_rows - r0);
+  if (warp < rows) {
+    const int r = r0 + warp, R = qt * C::kRows + r, tok = q0 + R / st.G, head = h * st.G + R % st.G;
+    const int64_t half = (int64_t)st.n_tokens * st.Hq;
+    JoinRun run[2] = {{nullptr, 0, 0, 0, 0}, {nullptr, 0, 0, 0, 0}};
+    const float2* ml[2] = {nullptr, nullptr};
+    int ml_step[2] = {0, 0}, ml_first[2] = {0, 0};
+    auto set_many = [&](int u, int2 x, int64_t place, int tile_rows, int row) {  // place: of the tile's rows, where it is whole
+      if (x.y == 1) {
+        run[u] = {parts.whole + place * D + row * 4, 0, 0, tile_rows * 4, 1};
+        ml[u] = parts.whole_ml + place + row;
+      } else {
+        const int64_t part = (int64_t)x.x * 2 * C::kRows;
+        run[u] = {parts.o + part * D + row * 4, 2 * C::kRows * D, C::kRows * D, C::kRows * 4, x.y};
+        ml[u] = parts.ml + part + row, ml_step[u] = 2 * C::kRows, ml_first[u] = C::kRows;
+      }
+    };
+    auto set_few = [&](int u, int2 x, int64_t place, int row) {
+      if (x.y == 1) {
+        run[u] = {few.whole + place * D, 0, 0, 4, 1};
+        ml[u] = few.whole_ml + place;
+      } else {
+        const int64_t at = (int64_t)x.x * 2 * few_rows + row;
+        run[u] = {few.o + at * D, (int64_t)2 * few_rows * D, (int64_t)few_rows * D, 4, x.y};
+        ml[u] = few.ml + at, ml_step[u] = 2 * few_rows, ml_first[u] = few_rows;
+      }
+    };
+    const int64_t at = (int64_t)(tok - ja.z) * st.G + R % st.G;  // the row among the group's
+    if (at >= 0 && at < (int64_t)ja.w * st.G) {
+      if constexpr (kFewGroups) {
+        set_few(0, sp.runs[jb.x * st.Hkv + h], (int64_t)tok * st.Hq + head, (int)at);
+      } else {
+        const int t = (int)(at / C::kRows);
+        if (t < jb.y)
+          set_many(0, p.runs[(int64_t)(jb.x + t) * st.Hkv + h], ((int64_t)h * st.n_tokens + ja.z) * st.G + (int64_t)t * C::kRows,
+                   (int)min((int64_t)C::kRows, (int64_t)ja.w * st.G - (int64_t)t * C::kRows), (int)(at - (int64_t)t * C::kRows));
+      }
+    }
+    if constexpr (kFewSeqs) set_few(1, own, half + (int64_t)tok * st.Hq + head, r);
+    else set_many(1, own, half + ((int64_t)h * st.n_tokens + q0) * st.G + qt * C::kRows, of, r);
+    float mx = -INFINITY, ls = 0.f;
+    const int n0 = run[0].n, n = n0 + run[1].n;
+#pragma unroll 2
+    for (int k = lane; k < n; k += 32) {
+      const int u = k >= n0, i = u ? k - n0 : k;
+      const float2 x = (u ? ml[1] : ml[0])[(int64_t)i * (u ? ml_step[1] : ml_step[0]) + (i == 0 ? (u ? ml_first[1] : ml_first[0]) : 0)];
+      s_w[warp][k] = x.x;
+      const float to = fmaxf(mx, x.x), ms = to == -INFINITY ? 0.f : to;
+      ls = ls * exp2f(mx - ms) + exp2f(x.x - ms) * x.y;
+      mx = to;
+    }
+    float all = mx;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, d));
+    const float ms = all == -INFINITY ? 0.f : all;
+    ls *= exp2f(mx - ms);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) ls += __shfl_xor_sync(0xffffffffu, ls, d);
+    for (int k = lane; k < n; k += 32) s_w[warp][k] = exp2f(s_w[warp][k] - ms);
+    if (lane == 0) {
+      s_run[warp][0] = run[0], s_run[warp][1] = run[1];
+      s_inv[warp] = ls == 0.f ? 0.f : 1.f / ls;  // (a NaN in the scores stays NaN)
+      if (c.lse) c.lse[(int64_t)tok * st.Hq + head] = ls == 0.f ? -INFINITY : (all + log2f(ls)) * kLn2;
+    }
+  }
+  __syncthreads();
+  const int items = rows * kCols, P = items < kJoinThreads ? kJoinThreads / items : 1;
   for (int i0 = 0; i0 < items; i0 += kJoinThreads) {
     const int pg = P > 1 ? tid / items : 0, i = P > 1 ? tid - pg * items : i0 + tid;
-    const bool in = i < items && pg < P;
     // (neighbouring threads take what neighbours in memory: columns, or rows as tiles leave them)
-    const int r = r0 + (kFewGroups ? i / kCols : i % rows), col = kFewGroups ? i % kCols : i / rows, R = qt * C::kRows + r;
-    const int tok = q0 + R / st.G, head = h * st.G + R % st.G;
-    float mx = -INFINITY, ls = 0.f;
+    const int w = kFewGroups ? i / kCols : i % rows, col = kFewGroups ? i % kCols : i / rows;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    auto add = [&](float2 ml, float4 o) {
-      const float to = fmaxf(mx, ml.x), ms = to == -INFINITY ? 0.f : to, f = exp2f(mx - ms), w = exp2f(ml.x - ms);
-      sum.x = sum.x * f + w * o.x, sum.y = sum.y * f + w * o.y, sum.z = sum.z * f + w * o.z, sum.w = sum.w * f + w * o.w;
-      ls = ls * f + w * ml.y;
-      mx = to;
-    };
-    int turn = pg;  // of this thread's next piece among those that are left
-    auto add_many = [&](int2 run, int64_t place, int tile_rows, int row) {  // place: of the tile's rows, where it is whole
-      if (run.y == 1) {
-        if (turn == 0)
-          add(parts.whole_ml[place + row], *reinterpret_cast<const float4*>(parts.whole + place * D + ((int64_t)col * tile_rows + row) * 4));
-      } else {
-#pragma unroll 4
-        for (int k = turn; k < run.y; k += P) {
-          const int64_t part = (int64_t)(k == 0 ? run.x * 2 + 1 : (run.x + k) * 2) * C::kRows;
-          add(parts.ml[part + row], *reinterpret_cast<const float4*>(parts.o + part * D + (col * C::kRows + row) * 4));
+    if (i < items && pg < P) {
+      int turn = pg, done = 0;  // this thread's next piece among those that are left; those behind
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const JoinRun run = s_run[w][u];
+        const float* o = run.o + (int64_t)col * run.next;
+        int k = turn;
+#pragma unroll 8
+        for (; k < run.n; k += P) {
+          const float f = s_w[w][done + k];
+          const float4 v = *reinterpret_cast<const float4*>(o + (int64_t)k * run.step + (k == 0 ? run.first : 0));
+          sum.x += f * v.x, sum.y += f * v.y, sum.z += f * v.z, sum.w += f * v.w;
         }
+        turn = k - run.n, done += run.n;
       }
-      turn = ((turn - run.y) % P + P) % P;
-    };
-    auto add_few = [&](int2 run, int64_t from, int row) {
-      if (run.y == 1) {
-        const int64_t place = from + (int64_t)tok * st.Hq + head;
-        if (turn == 0) add(few.whole_ml[place], *reinterpret_cast<const float4*>(few.whole + place * D + col * 4));
-      } else {
-#pragma unroll 4
-        for (int k = turn; k < run.y; k += P) {
-          const int64_t at = (int64_t)(k == 0 ? run.x * 2 + 1 : (run.x + k) * 2) * few_rows + row;
-          add(few.ml[at], *reinterpret_cast<const float4*>(few.o + at * D + col * 4));
-        }
-      }
-      turn = ((turn - run.y) % P + P) % P;
-    };
-    if (in) {
-      const int64_t at = (int64_t)(tok - ja.z) * st.G + R % st.G;  // the row among the group's
-      if (at >= 0 && at < (int64_t)ja.w * st.G) {
-        if constexpr (kFewGroups) {
-          add_few(with, 0, (int)at);
-        } else {
-          const int t = (int)(at / C::kRows);
-          if (t < jb.y)
-            add_many(__ldg(p.runs + (int64_t)(jb.x + t) * st.Hkv + h), ((int64_t)h * st.n_tokens + ja.z) * st.G + (int64_t)t * C::kRows,
-                     (int)min((int64_t)C::kRows, (int64_t)ja.w * st.G - (int64_t)t * C::kRows), (int)(at - (int64_t)t * C::kRows));
-        }
-      }
-      if constexpr (kFewSeqs) add_few(own, half, r);
-      else add_many(own, half + ((int64_t)h * st.n_tokens + q0) * st.G + qt * C::kRows, of, r);
     }
     if (P > 1) {  // (one round: the other parts of the row)
-      s_o[tid] = sum, s_ml[tid] = make_float2(mx, ls);
+      s_o[tid] = sum;
       __syncthreads();
       if (pg != 0) return;
-      for (int k = 1; k < P; ++k) add(s_ml[tid + k * items], s_o[tid + k * items]);
+      for (int k = 1; k < P; ++k) {
+        const float4 v = s_o[tid + k * items];
+        sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+      }
     }
-    if (!in) continue;
-    const float inv = ls == 0.f ? 0.f : 1.f / ls;  // (a NaN in the scores stays NaN)
-    T* out = static_cast<T*>(c.out) + (int64_t)tok * c.out_stride + (int64_t)head * D + col * 4;
+    if (i >= items) continue;
+    const int R = qt * C::kRows + r0 + w;
+    const float inv = s_inv[w];
+    T* out = static_cast<T*>(c.out) + (int64_t)(q0 + R / st.G) * c.out_stride + (int64_t)(h * st.G + R % st.G) * D + col * 4;
     *reinterpret_cast<uint2*>(out) = make_uint2(Half2<T>::down(sum.x * inv, sum.y * inv), Half2<T>::down(sum.z * inv, sum.w * inv));
-    if (c.lse && col == 0) c.lse[(int64_t)tok * st.Hq + head] = ls == 0.f ? -INFINITY : (mx + log2f(ls)) * kLn2;
   }
 }
 
@@ -1209,25 +1340,26 @@ cudaError_t run_shared(const AttnCall& c, const AttnMaps& maps, const SharedGrou
   const int64_t own = rows / C::kRows + c.st.n_seqs;  // row tiles of the sequences
   const int64_t tiles = (plan.seqs ? own : 0) + (plan.groups ? rows / C::kRows + g.n : 0);
   plan.max_tiles = tiles < plan.max_tiles ? (int)tiles : plan.max_tiles;
-  const int n_few_groups = few_groups ? g.n : 0;
-  cudaError_t e = launch_pdl(true, k_attn_plan_shared<D>, dim3(1), dim3(1024), 0, s, c, g, plan, sh.found, n_few_groups, few_seqs ? c.st.n_seqs : 0);
+  const int n_few_groups = few_groups ? g.n : 0, few_blocks = attn_few_fit(D, sms);
+  if (few_blocks + sms + 2 > kJoinPieces) return cudaErrorInvalidConfiguration;  // (a row's pieces: no more than blocks, and one of each list)
   const int64_t most = tiles * c.st.Hkv * (((int64_t)c.st.cap + kKeys - 1) / kKeys);
   const unsigned grid = (unsigned)(most < sms ? most : sms);
+  cudaError_t e = launch_pdl(true, k_attn_plan_shared<D>, dim3(2), dim3(1024), 0, s, c, g, plan, sh.found, n_few_groups, few_seqs ? c.st.n_seqs : 0,
+                             (int)grid, few_blocks);
   if (e == cudaSuccess && tiles) {
     constexpr size_t smem = smem_of(C::kTail);
     auto kernel = k_attn_many<T, D, true>;
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e == cudaSuccess) e = launch_pdl(true, kernel, dim3(grid), dim3(kThreads), smem, s, c, maps, plan, sh.parts);
   }
-  const int few_rows = (int)(few_groups && g.n ? rows : seq_rows), few_blocks = attn_few_fit(D, sms);
+  const int few_rows = (int)(few_groups && g.n ? rows : seq_rows);
   if (e == cudaSuccess && few_seqs) {
-    const FewShared f = {sh.found.span, sh.found.group, sh.found.before, sh.found.runs, n_few_groups, tiles == 0, few_blocks};
+    const FewShared f = {sh.found.span, sh.found.group, sh.found.start, sh.found.runs, n_few_groups, tiles == 0, few_blocks};
     e = launch_attn_few_shared(c, sh.few, f, few_rows, D, kBf, sms, s);
   }
   if (e != cudaSuccess) return e;
-  const int join_rows = few_seqs ? kJoinRows<true> : kJoinRows<false>;
   const int64_t in_tile = few_seqs || seq_rows < C::kRows ? seq_rows : C::kRows;
-  const dim3 blocks((unsigned)(few_seqs ? c.st.n_seqs : own), (unsigned)c.st.Hkv, (unsigned)((in_tile + join_rows - 1) / join_rows));
+  const dim3 blocks((unsigned)(few_seqs ? c.st.n_seqs : own), (unsigned)c.st.Hkv, (unsigned)((in_tile + kJoinRows - 1) / kJoinRows));
   auto join = few_groups ? k_attn_join_shared<T, D, true, true> : few_seqs ? k_attn_join_shared<T, D, false, true> : k_attn_join_shared<T, D, false, false>;
   return launch_pdl(true, join, blocks, dim3(kJoinThreads), 0, s, c, plan, sh.found, sh.parts, sh.few, attn_few_part_rows(few_rows),
                     n_few_groups);
