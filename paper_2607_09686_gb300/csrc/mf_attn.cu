@@ -404,7 +404,8 @@ extern "C" int mf_attn_share(mf_attn_t* attn, int max_groups) {
                o_start = w.take((size_t)attn->sms * 48), o_fstart = w.take((size_t)attn_few_blocks(attn->sms) * 64),
                o_whole = w.take((size_t)rows * 2 * sh.head_dim * 4), o_whole_ml = w.take((size_t)rows * 2 * 8);
   unsigned char* ws = nullptr;
-  cudaError_t e = tiles < (1 << 30) ? cudaMalloc(&ws, w.off) : cudaErrorMemoryAllocation;
+  // (the join counts its vectors in 32 bits)
+  cudaError_t e = tiles < (1 << 30) && w.off < ((size_t)1 << 36) ? cudaMalloc(&ws, w.off) : cudaErrorMemoryAllocation;
   // (runs that no call wrote, for lack of tiles where a step's bounds overlap, have no pieces)
   if (e == cudaSuccess) e = cudaMemset(ws + o_runs, 0, (size_t)tiles * sh.n_kv_heads * 8);
   if (e == cudaSuccess) e = cudaMemset(ws + o_fruns, 0, ((size_t)max_groups + attn->max_seqs) * sh.n_kv_heads * 8);
@@ -448,7 +449,7 @@ extern "C" int mf_attn_forward_shared(mf_attn_t* attn, const mf_kv_cache_t* cach
   const SharedGroups g = {shared->first, shared->len, shared->n_groups};
   AttnMaps maps;
   attn_maps(c, attn->shape.head_dim, &maps);
-  const cudaError_t e = launch_attn_shared(c, maps, g, attn->shared, attn->shape.head_dim, attn->shape.dtype == MF_BF16, attn->sms,
+  const cudaError_t e = launch_attn_shared(c, maps, g, attn->shared, attn->parts, attn->shape.head_dim, attn->shape.dtype == MF_BF16, attn->sms,
                                            static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_attn_forward_shared");
 }

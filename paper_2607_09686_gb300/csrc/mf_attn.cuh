@@ -220,8 +220,9 @@ cudaError_t launch_attn_few(const AttnCall& c, const AttnParts& parts, int head_
 void attn_maps(AttnCall& c, int head_dim, AttnMaps* maps);
 cudaError_t launch_attn_many(const AttnCall& c, const AttnMaps& maps, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
                              cudaStream_t s);
-cudaError_t launch_attn_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& groups, const AttnShared& sh, int head_dim, bool bf16,
-                               int sms, cudaStream_t s);
+// parts: the handle's own, for sequences that share nothing after all
+cudaError_t launch_attn_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& groups, const AttnShared& sh, const AttnParts& parts,
+                               int head_dim, bool bf16, int sms, cudaStream_t s);
 // the records of `blocks` blocks joined; rows: rows of a part; tiles: left by launch_attn_many
 cudaError_t launch_attn_join(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int rows, bool tiles, int blocks,
                              cudaStream_t s);

@@ -135,10 +135,11 @@ __global__ void __launch_bounds__(1024) k_attn_plan(AttnCall c, AttnPlan p) {
 // all the group's tokens and the shared lines (whole pages of them), then the sequences, with what follows.  First the groups: bounds
 // that rise, lengths that all their sequences have; a group of one shares nothing.  p.groups and p.seqs say which of them are in the list
 // of this file's kernel, few_groups and few_seqs which are in that of few rows.  Two blocks, both of which find the groups: the first lays out this
-// file's list and says where its kernel's blocks begin, the second the other list, and what the join asks for.
+// file's list and says where its kernel's blocks begin, the second the other list, and what the join asks for.  alone: nothing is shared
+// after all, the list is k_attn_plan's.
 template <int D>
 __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGroups g, AttnPlan p, SharedPlan sp, int few_groups,
-                                                           int few_seqs, int blocks, int few_blocks) {
+                                                           int few_seqs, int blocks, int few_blocks, int alone) {
   __shared__ int64_t s_warp[32];
   // what the phases hand on, in shared memory where it finds room: the sequences' spans and groups, the groups, first row tiles
   constexpr int kSmall = 1024;
@@ -221,7 +222,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     if (i < g.n) {
       const int asked = g.len[i], len = max(0, min(asked, least));
       if (len != asked && sub == 0 && a < b) attn_report(c.st, kAttnRange);
-      const int lines = b - a > 1 ? (int)fast_div((uint32_t)len, c.st.page_mul, c.st.page_shift) * c.st.page_size : 0;
+      const int lines = b - a > 1 && !alone ? (int)fast_div((uint32_t)len, c.st.page_mul, c.st.page_shift) * c.st.page_size : 0;
       int q0 = 0, n = 0;
       if (lines) {
         const SeqSpan x = span(a), y = span(b - 1);
@@ -249,7 +250,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
   if (tid == 0 && V) first[V] = p.first[V] = tiles;
   __syncthreads();
   if (lists) {
-    int64_t* before = tiles <= kSmall ? s_before : p.before;
+    int64_t* before = tiles <= kSmall && !alone ? s_before : p.before;
     int64_t jobs = 0;
     for (int base = 0; base < tiles; base += 1024) {
       const int i = base + tid;
@@ -283,6 +284,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
       jobs += all;
     }
     if (tid == 0) before[tiles] = jobs;
+    if (alone) return;
     __syncthreads();
     // ---- where the blocks begin: every one that works has two jobs at least, so that it has a key tile's start
     const int64_t total = jobs * c.st.Hkv, B = max((int64_t)1, min((int64_t)blocks, total / 2));
@@ -315,6 +317,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     }
     return;
   }
+  if (alone) return;
   // ---- the list of few rows
   int64_t* before = few <= kSmall ? s_before : sp.before;
   done = 0;
@@ -1166,23 +1169,25 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
 // order of the lines, and then the sequence's own; the blocks that have them were noted by the one that had the first.  A warp forms the weights
 // of a row's pieces; then a thread has four columns of a row and, where rows times columns are fewer than threads, every P-th
 // piece.  kFewGroups, kFewSeqs: the groups' lines, the sequences' own were the kernel's of few rows.
-constexpr int kJoinThreads = 256, kJoinRows = kJoinThreads / 32, kJoinPieces = 640;
-struct JoinRun {  // a row's n pieces: four columns of piece k at o + k * step + column * next, of the first `first` farther on
-  const float* o;
-  int64_t step, first;
-  int next, n;
+constexpr int kJoinThreads = 512, kJoinRows = 8, kJoinPieces = 512;
+struct JoinPiece {
+  uint32_t at;  // 16-byte vectors from the workspace's beginning to the row's first columns
+  float w;
+};
+struct JoinRow {
+  int n0, n, next0, next1;  // pieces of the group's lines, of all; vectors from four columns to the next, in the group's pieces and the own
+  float inv;
 };
 template <class T, int D, bool kFewGroups, bool kFewSeqs>
 __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_constant__ AttnCall c, const __grid_constant__ AttnPlan p,
                                                                    const __grid_constant__ SharedPlan sp,
                                                                    const __grid_constant__ AttnParts parts,
-                                                                   const __grid_constant__ AttnParts few, int few_rows, int few_groups) {
+                                                                   const __grid_constant__ AttnParts few, const float* mem, int few_rows, int few_groups) {
   using C = Cfg<D>;
   constexpr int kCols = D / 4;
-  __shared__ float s_w[kJoinRows][kJoinPieces];
+  __shared__ JoinPiece s_piece[kJoinRows][kJoinPieces + 1];  // (rows in other banks)
   __shared__ float4 s_o[kJoinThreads];
-  __shared__ JoinRun s_run[kJoinRows][2];
-  __shared__ float s_inv[kJoinRows];
+  __shared__ JoinRow s_row[kJoinRows];
   const AttnStep& st = c.st;
   const int h = blockIdx.y, r0 = blockIdx.z * kJoinRows, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
@@ -1206,27 +1211,29 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_
   if (warp < rows) {
     const int r = r0 + warp, R = qt * C::kRows + r, tok = q0 + R / st.G, head = h * st.G + R % st.G;
     const int64_t half = (int64_t)st.n_tokens * st.Hq;
-    JoinRun run[2] = {{nullptr, 0, 0, 0, 0}, {nullptr, 0, 0, 0, 0}};
-    const float2* ml[2] = {nullptr, nullptr};
-    int ml_step[2] = {0, 0}, ml_first[2] = {0, 0};
+    // the pieces: n of them, the first's row of partials, from each to the next, and what the first lies farther on
+    struct {
+      const float* o;
+      const float2* ml;
+      int n, step, first, next, d;  // next: vectors between columns; d: vectors of a row step
+    } run[2] = {};
     auto set_many = [&](int u, int2 x, int64_t place, int tile_rows, int row) {  // place: of the tile's rows, where it is whole
+      run[u].n = x.y;
       if (x.y == 1) {
-        run[u] = {parts.whole + place * D + row * 4, 0, 0, tile_rows * 4, 1};
-        ml[u] = parts.whole_ml + place + row;
+        run[u].o = parts.whole + place * D + row * 4, run[u].ml = parts.whole_ml + place + row, run[u].next = tile_rows;
       } else {
         const int64_t part = (int64_t)x.x * 2 * C::kRows;
-        run[u] = {parts.o + part * D + row * 4, 2 * C::kRows * D, C::kRows * D, C::kRows * 4, x.y};
-        ml[u] = parts.ml + part + row, ml_step[u] = 2 * C::kRows, ml_first[u] = C::kRows;
+        run[u].o = parts.o + part * D + row * 4, run[u].ml = parts.ml + part + row, run[u].next = C::kRows;
+        run[u].step = 2 * C::kRows, run[u].first = C::kRows;
       }
     };
     auto set_few = [&](int u, int2 x, int64_t place, int row) {
+      run[u].n = x.y, run[u].next = 1;
       if (x.y == 1) {
-        run[u] = {few.whole + place * D, 0, 0, 4, 1};
-        ml[u] = few.whole_ml + place;
+        run[u].o = few.whole + place * D, run[u].ml = few.whole_ml + place;
       } else {
         const int64_t at = (int64_t)x.x * 2 * few_rows + row;
-        run[u] = {few.o + at * D, (int64_t)2 * few_rows * D, (int64_t)few_rows * D, 4, x.y};
-        ml[u] = few.ml + at, ml_step[u] = 2 * few_rows, ml_first[u] = few_rows;
+        run[u].o = few.o + at * D, run[u].ml = few.ml + at, run[u].step = 2 * few_rows, run[u].first = few_rows;
       }
     };
     const int64_t at = (int64_t)(tok - ja.z) * st.G + R % st.G;  // the row among the group's
@@ -1243,12 +1250,13 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_
     if constexpr (kFewSeqs) set_few(1, own, half + (int64_t)tok * st.Hq + head, r);
     else set_many(1, own, half + ((int64_t)h * st.n_tokens + q0) * st.G + qt * C::kRows, of, r);
     float mx = -INFINITY, ls = 0.f;
-    const int n0 = run[0].n, n = n0 + run[1].n;
+    const int n0 = run[0].n, n = min(n0 + run[1].n, kJoinPieces);
+    const uint32_t o0 = (uint32_t)((run[0].o - mem) >> 2), o1 = (uint32_t)((run[1].o - mem) >> 2);
 #pragma unroll 2
     for (int k = lane; k < n; k += 32) {
-      const int u = k >= n0, i = u ? k - n0 : k;
-      const float2 x = (u ? ml[1] : ml[0])[(int64_t)i * (u ? ml_step[1] : ml_step[0]) + (i == 0 ? (u ? ml_first[1] : ml_first[0]) : 0)];
-      s_w[warp][k] = x.x;
+      const int u = k >= n0, i = u ? k - n0 : k, rows_on = i * (u ? run[1].step : run[0].step) + (i == 0 ? (u ? run[1].first : run[0].first) : 0);
+      const float2 x = (u ? run[1].ml : run[0].ml)[rows_on];
+      s_piece[warp][k] = {(u ? o1 : o0) + (uint32_t)rows_on * kCols, x.x};
       const float to = fmaxf(mx, x.x), ms = to == -INFINITY ? 0.f : to;
       ls = ls * exp2f(mx - ms) + exp2f(x.x - ms) * x.y;
       mx = to;
@@ -1260,34 +1268,36 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_
     ls *= exp2f(mx - ms);
 #pragma unroll
     for (int d = 16; d; d >>= 1) ls += __shfl_xor_sync(0xffffffffu, ls, d);
-    for (int k = lane; k < n; k += 32) s_w[warp][k] = exp2f(s_w[warp][k] - ms);
+    for (int k = lane; k < n; k += 32) s_piece[warp][k].w = exp2f(s_piece[warp][k].w - ms);
     if (lane == 0) {
-      s_run[warp][0] = run[0], s_run[warp][1] = run[1];
-      s_inv[warp] = ls == 0.f ? 0.f : 1.f / ls;  // (a NaN in the scores stays NaN)
+      s_row[warp] = {n0, n, run[0].next, run[1].next, ls == 0.f ? 0.f : 1.f / ls};  // (a NaN in the scores stays NaN)
       if (c.lse) c.lse[(int64_t)tok * st.Hq + head] = ls == 0.f ? -INFINITY : (all + log2f(ls)) * kLn2;
     }
   }
   __syncthreads();
   const int items = rows * kCols, P = items < kJoinThreads ? kJoinThreads / items : 1;
+  const float4* vectors = reinterpret_cast<const float4*>(mem);
   for (int i0 = 0; i0 < items; i0 += kJoinThreads) {
     const int pg = P > 1 ? tid / items : 0, i = P > 1 ? tid - pg * items : i0 + tid;
     // (neighbouring threads take what neighbours in memory: columns, or rows as tiles leave them)
     const int w = kFewGroups ? i / kCols : i % rows, col = kFewGroups ? i % kCols : i / rows;
     float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
     if (i < items && pg < P) {
-      int turn = pg, done = 0;  // this thread's next piece among those that are left; those behind
+      const JoinRow row = s_row[w];
+      constexpr int kU = 8;  // pieces under way
+      for (int k0 = pg; k0 < row.n; k0 += kU * P) {
+        float4 v[kU];
+        float f[kU];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const JoinRun run = s_run[w][u];
-        const float* o = run.o + (int64_t)col * run.next;
-        int k = turn;
-#pragma unroll 8
-        for (; k < run.n; k += P) {
-          const float f = s_w[w][done + k];
-          const float4 v = *reinterpret_cast<const float4*>(o + (int64_t)k * run.step + (k == 0 ? run.first : 0));
-          sum.x += f * v.x, sum.y += f * v.y, sum.z += f * v.z, sum.w += f * v.w;
+        for (int u = 0; u < kU; ++u) {
+          const int k = k0 + u * P;
+          const JoinPiece x = s_piece[w][min(k, row.n - 1)];
+          f[u] = k < row.n ? x.w : 0.f;
+          v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (k < row.n) v[u] = vectors[(size_t)x.at + (size_t)(col * (k < row.n0 ? row.next0 : row.next1))];
         }
-        turn = k - run.n, done += run.n;
+#pragma unroll
+        for (int u = 0; u < kU; ++u) sum.x += f[u] * v[u].x, sum.y += f[u] * v[u].y, sum.z += f[u] * v[u].z, sum.w += f[u] * v[u].w;
       }
     }
     if (P > 1) {  // (one round: the other parts of the row)
@@ -1301,7 +1311,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_
     }
     if (i >= items) continue;
     const int R = qt * C::kRows + r0 + w;
-    const float inv = s_inv[w];
+    const float inv = s_row[w].inv;
     T* out = static_cast<T*>(c.out) + (int64_t)(q0 + R / st.G) * c.out_stride + (int64_t)(h * st.G + R % st.G) * D + col * 4;
     *reinterpret_cast<uint2*>(out) = make_uint2(Half2<T>::down(sum.x * inv, sum.y * inv), Half2<T>::down(sum.z * inv, sum.w * inv));
   }
@@ -1310,7 +1320,8 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_
 constexpr size_t smem_of(size_t tail) { return tail + sizeof(Tail); }
 
 template <class T, int D>
-cudaError_t run(const AttnCall& c, const AttnMaps& maps, AttnPlan plan, const AttnParts& parts, int sms, cudaStream_t s) {
+cudaError_t run(const AttnCall& c, const AttnMaps& maps, AttnPlan plan, const AttnParts& parts, const SharedGroups* groups,
+                const SharedPlan* found, int sms, cudaStream_t s) {  // groups: given, they are looked at and not used
   using C = Cfg<D>;
   const int64_t rows = (int64_t)c.st.n_tokens * c.st.G;
   const int64_t tiles = rows / C::kRows + c.st.n_seqs;
@@ -1321,20 +1332,29 @@ cudaError_t run(const AttnCall& c, const AttnMaps& maps, AttnPlan plan, const At
   static_assert(smem <= 232448, "shared memory of a block");
   auto kernel = k_attn_many<T, D, false>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e == cudaSuccess) e = launch_pdl(true, k_attn_plan<D>, dim3(1), dim3(1024), 0, s, c, plan);
+  plan.groups = 0, plan.seqs = c.st.n_seqs;
+  if (e == cudaSuccess)
+    e = groups ? launch_pdl(true, k_attn_plan_shared<D>, dim3(2), dim3(1024), 0, s, c, *groups, plan, *found, 0, 0, (int)grid, 0, 1)
+               : launch_pdl(true, k_attn_plan<D>, dim3(1), dim3(1024), 0, s, c, plan);
   if (e == cudaSuccess) e = launch_pdl(true, kernel, dim3(grid), dim3(kThreads), smem, s, c, maps, plan, parts);
   if (e == cudaSuccess && grid > 1) e = launch_attn_join(c, parts, D, Half2<T>::kBf16, C::kRows, true, (int)grid, s);
   return e;
 }
 
 // The plan, the groups' lines, the sequences' own, the join.  Rows that the kernel of few rows holds are its: all of them where a group cannot
-// have more (one launch), else those of the sequences (a launch that starts while the groups' ends).
+// have more (one launch), else those of the sequences (a launch that starts while the groups' ends).  Where the sequences have rows
+// enough to fill tiles of their own, a group's tiles spare no products and hardly any reading (the tiles of a head read the shared lines
+// from the L2 cache), and the partials cost: then each sequence reads all its lines itself, from its own pages, which hold the same (8
+// sequences of 100 and 8192 shared lines, 8 heads a kv head, shared against alone: heads of 128, rows of a sequence on the average 58
+// 31.8 us and 38.1, 77 40.3 and 39.0, 154 58.6 and 54.1; of 64, 77 52.2 and 51.4; of 256, 77 51.6 and 55.2, 154 65.5 and 75.2, 3400 430 and 376).
 template <class T, int D>
-cudaError_t run_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& g, const AttnShared& sh, int sms, cudaStream_t s) {
+cudaError_t run_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& g, const AttnShared& sh, const AttnParts& parts, int sms,
+                       cudaStream_t s) {
   using C = Cfg<D>;
   constexpr bool kBf = Half2<T>::kBf16;
   const int64_t rows = (int64_t)c.st.n_tokens * c.st.G, seq_rows = (int64_t)c.st.max_q * c.st.G;
   const bool few_seqs = seq_rows <= attn_few_rows(D), few_groups = few_seqs && (rows <= attn_few_rows(D) || g.n == 0);
+  if (!few_seqs && rows >= (int64_t)(D == 256 ? 256 : 72) * c.st.n_seqs) return run<T, D>(c, maps, sh.plan, parts, &g, &sh.found, sms, s);
   AttnPlan plan = sh.plan;
   plan.groups = few_groups ? 0 : g.n, plan.seqs = few_seqs ? 0 : c.st.n_seqs;
   const int64_t own = rows / C::kRows + c.st.n_seqs;  // row tiles of the sequences
@@ -1345,7 +1365,7 @@ cudaError_t run_shared(const AttnCall& c, const AttnMaps& maps, const SharedGrou
   const int64_t most = tiles * c.st.Hkv * (((int64_t)c.st.cap + kKeys - 1) / kKeys);
   const unsigned grid = (unsigned)(most < sms ? most : sms);
   cudaError_t e = launch_pdl(true, k_attn_plan_shared<D>, dim3(2), dim3(1024), 0, s, c, g, plan, sh.found, n_few_groups, few_seqs ? c.st.n_seqs : 0,
-                             (int)grid, few_blocks);
+                             (int)grid, few_blocks, 0);
   if (e == cudaSuccess && tiles) {
     constexpr size_t smem = smem_of(C::kTail);
     auto kernel = k_attn_many<T, D, true>;
@@ -1361,7 +1381,7 @@ cudaError_t run_shared(const AttnCall& c, const AttnMaps& maps, const SharedGrou
   const int64_t in_tile = few_seqs || seq_rows < C::kRows ? seq_rows : C::kRows;
   const dim3 blocks((unsigned)(few_seqs ? c.st.n_seqs : own), (unsigned)c.st.Hkv, (unsigned)((in_tile + kJoinRows - 1) / kJoinRows));
   auto join = few_groups ? k_attn_join_shared<T, D, true, true> : few_seqs ? k_attn_join_shared<T, D, false, true> : k_attn_join_shared<T, D, false, false>;
-  return launch_pdl(true, join, blocks, dim3(kJoinThreads), 0, s, c, plan, sh.found, sh.parts, sh.few, attn_few_part_rows(few_rows),
+  return launch_pdl(true, join, blocks, dim3(kJoinThreads), 0, s, c, plan, sh.found, sh.parts, sh.few, reinterpret_cast<const float*>(sh.mem), attn_few_part_rows(few_rows),
                     n_few_groups);
 }
 
@@ -1410,22 +1430,22 @@ int attn_tile_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
 cudaError_t launch_attn_many(const AttnCall& c, const AttnMaps& maps, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
                              cudaStream_t s) {
   if (bf16)
-    return head_dim == 64    ? run<__nv_bfloat16, 64>(c, maps, plan, parts, sms, s)
-           : head_dim == 128 ? run<__nv_bfloat16, 128>(c, maps, plan, parts, sms, s)
-                             : run<__nv_bfloat16, 256>(c, maps, plan, parts, sms, s);
-  return head_dim == 64    ? run<__half, 64>(c, maps, plan, parts, sms, s)
-         : head_dim == 128 ? run<__half, 128>(c, maps, plan, parts, sms, s)
-                           : run<__half, 256>(c, maps, plan, parts, sms, s);
+    return head_dim == 64    ? run<__nv_bfloat16, 64>(c, maps, plan, parts, nullptr, nullptr, sms, s)
+           : head_dim == 128 ? run<__nv_bfloat16, 128>(c, maps, plan, parts, nullptr, nullptr, sms, s)
+                             : run<__nv_bfloat16, 256>(c, maps, plan, parts, nullptr, nullptr, sms, s);
+  return head_dim == 64    ? run<__half, 64>(c, maps, plan, parts, nullptr, nullptr, sms, s)
+         : head_dim == 128 ? run<__half, 128>(c, maps, plan, parts, nullptr, nullptr, sms, s)
+                           : run<__half, 256>(c, maps, plan, parts, nullptr, nullptr, sms, s);
 }
-cudaError_t launch_attn_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& g, const AttnShared& sh, int head_dim, bool bf16,
-                               int sms, cudaStream_t s) {
+cudaError_t launch_attn_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& g, const AttnShared& sh, const AttnParts& parts,
+                               int head_dim, bool bf16, int sms, cudaStream_t s) {
   if (bf16)
-    return head_dim == 64    ? run_shared<__nv_bfloat16, 64>(c, maps, g, sh, sms, s)
-           : head_dim == 128 ? run_shared<__nv_bfloat16, 128>(c, maps, g, sh, sms, s)
-                             : run_shared<__nv_bfloat16, 256>(c, maps, g, sh, sms, s);
-  return head_dim == 64    ? run_shared<__half, 64>(c, maps, g, sh, sms, s)
-         : head_dim == 128 ? run_shared<__half, 128>(c, maps, g, sh, sms, s)
-                           : run_shared<__half, 256>(c, maps, g, sh, sms, s);
+    return head_dim == 64    ? run_shared<__nv_bfloat16, 64>(c, maps, g, sh, parts, sms, s)
+           : head_dim == 128 ? run_shared<__nv_bfloat16, 128>(c, maps, g, sh, parts, sms, s)
+                             : run_shared<__nv_bfloat16, 256>(c, maps, g, sh, parts, sms, s);
+  return head_dim == 64    ? run_shared<__half, 64>(c, maps, g, sh, parts, sms, s)
+         : head_dim == 128 ? run_shared<__half, 128>(c, maps, g, sh, parts, sms, s)
+                           : run_shared<__half, 256>(c, maps, g, sh, parts, sms, s);
 }
 
 }  // namespace mf
