@@ -69,6 +69,7 @@ struct KeptCall : SampleCall {
   mf_cuts_t draft_cuts;
   Kept* kept;
   int n_seqs, n_rows;
+  int row0;  // of the target's rows and then the drafter's
 };
 
 // larger floats have larger keys (-0 and +0 compare equal as floats: one key)
@@ -122,7 +123,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(Call c) {
   extern __shared__ __align__(16) unsigned char dyn[];
   __shared__ Shared sh;
   cg::cluster_group cl = cg::this_cluster();
-  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank(), r = blockIdx.x / C;
+  const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+  int r = blockIdx.x / C;
+  if constexpr (kKept) r += c.row0;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   uint32_t* hist = reinterpret_cast<uint32_t*>(dyn);
   unsigned long long* list = reinterpret_cast<unsigned long long*>(dyn + kListAt);
@@ -134,6 +137,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(Call c) {
 
   pdl_wait();
   int rs = r;  // whose settings the row has
+  bool drafters = false;
   if constexpr (kKept) {
     const int i = r % c.n_rows;
     int lo = 0, hi = c.n_seqs - 1;  // the last sequence that begins at or before the row
@@ -147,7 +151,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(Call c) {
     rs = lo;
     if (r != i) {
       row = static_cast<const T*>(c.draft) + (int64_t)i * c.draft_stride + base;
-      c.temperature = c.draft_cuts.temperature, c.top_p = c.draft_cuts.top_p, c.min_p = c.draft_cuts.min_p, c.top_k = c.draft_cuts.top_k;
+      drafters = true;
     }
   }
   // ---- 1. the slice into shared memory, at the same place modulo 16 bytes: whole vectors by bulk copies, the ends by hand
@@ -275,12 +279,15 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(Call c) {
   const float theirs = lane < C ? cl.map_shared_rank(&sh, lane)->mx : -INFINITY;
   const float m = warp_max(theirs);
 
-  const float temp = c.temperature ? c.temperature[rs] : 1.f;
+  mf_cuts_t cuts = {c.temperature, c.top_p, c.min_p, c.top_k};
+  if constexpr (kKept)
+    if (drafters) cuts = c.draft_cuts;
+  const float temp = cuts.temperature ? cuts.temperature[rs] : 1.f;
   const bool greedy = !(temp > 0.f);
   const float t = greedy ? 1.f : bounded(temp);
-  const int top_k = c.top_k && !greedy ? c.top_k[rs] : 0;
-  const float top_p = c.top_p && !greedy ? c.top_p[rs] : 1.f;
-  const float min_p = c.min_p && !greedy ? fminf(fmaxf(c.min_p[rs], 0.f), 1.f) : 0.f;
+  const int top_k = cuts.top_k && !greedy ? cuts.top_k[rs] : 0;
+  const float top_p = cuts.top_p && !greedy ? cuts.top_p[rs] : 1.f;
+  const float min_p = cuts.min_p && !greedy ? fminf(fmaxf(cuts.min_p[rs], 0.f), 1.f) : 0.f;
   const float inv = inverse(kBinsPerUnit, t);
   float xc = -INFINITY;  // kept: larger entries, and equal ones up to index ic
   int ic = -1;
@@ -1183,7 +1190,8 @@ cudaError_t launch_kept(const KeptRows& k, cudaStream_t s) {
   c.temperature = k.cuts.temperature, c.top_p = k.cuts.top_p, c.min_p = k.cuts.min_p, c.top_k = k.cuts.top_k;
   c.draft = k.draft, c.draft_stride = k.draft_stride, c.draft_cuts = k.draft_cuts;
   c.row_start = k.row_start, c.n_seqs = k.n_seqs, c.n_rows = k.n_rows, c.kept = k.kept;
-  const int rows = k.draft ? 2 * k.n_rows : k.n_rows;
+  c.row0 = k.target ? 0 : k.n_rows;
+  const int rows = (k.target ? k.n_rows : 0) + (k.draft ? k.n_rows : 0);
   return k.dtype == MF_F32 ? run<float>(c, rows, s) : k.dtype == MF_F16 ? run<__half>(c, rows, s) : run<__nv_bfloat16>(c, rows, s);
 }
 

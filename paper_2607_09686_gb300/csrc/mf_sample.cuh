@@ -24,15 +24,15 @@ struct Kept {
   int unused;
 };
 
-// Rows of several sequences: the target's and, where draft is given, the drafter's (not the last of a sequence), with settings by
-// sequence.  The n_rows target rows' sets are left in kept, the drafter's behind them.
+// Rows of several sequences: the target's (where `target` is set) and, where draft is given, the drafter's (not the last of a sequence),
+// with settings by sequence.  The n_rows target rows' sets are left in kept, the drafter's behind their place.
 struct KeptRows {
   const void *logits, *draft;
   int64_t logits_stride, draft_stride;
   const int32_t* row_start;
   mf_cuts_t cuts, draft_cuts;
   Kept* kept;
-  int n_seqs, n_rows, vocab, dtype;
+  int n_seqs, n_rows, vocab, dtype, target;
 };
 cudaError_t launch_kept(const KeptRows& rows, cudaStream_t s);
 

@@ -1,12 +1,16 @@
 // Verification of drafted tokens: the drafts that the target takes, and the token that ends each sequence.  Contract: mawforge.h.
 //
-// Two launches.  The first finds what each row of the target's logits keeps and the sum of its weights (k_sample's steps, without the
-// draw), and the same of the drafter's rows, so that p and q of any entry are a few operations on its logit.  In the second
-// a cluster of 1 to 8 blocks has a sequence: the drafts' p and q, one row a thread, the first row whose draft is not taken; then one
-// pass over that row for the largest log(p - q) + noise.
+// First what each row of the target's logits keeps and the sum of its weights, and the same of the drafter's rows, so that p and q of any entry are a
+// few operations on its logit: by k_sample's steps without the draw where rows are cut, else (k_rows) by maxima and sums of
+// slices, a block each.  Then (k_verify) a cluster of 1 to 8 blocks has a sequence: a warp a draft, p and q of it; the first row whose
+// draft is not taken; one pass over that row for the largest log(p - q) + noise.  In that pass log p + noise, a bound of it that
+// takes no exponential, is compared with the largest key so far, and only what lies above it is worked out.
+// What bounds it: reading the logits (k_rows), then of the rows that decide the logits again and the noise.
 #include <cooperative_groups.h>
 
+#include <cfloat>
 #include <cmath>
+#include <cstring>
 
 #include "mf_sample.cuh"
 
@@ -17,16 +21,111 @@ namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 
+// Of a slice of a row: the largest logit, its first index (rows without a temperature), the sum of w against it.
+struct Slice {
+  float m, s;
+  int first, unused;
+};
+
 struct VerifyCall {
   const void *logits, *draft;
   int64_t logits_stride, draft_stride, noise_stride;
   const int32_t *row_start, *tokens;
   const float *u, *noise;
+  const float* temperature[2];  // the target's, the drafter's
   int32_t *token, *accepted;
   float* logprob;
-  const Kept* kept;
-  int n_rows, vocab, slice;
+  const Kept* kept;   // [2][rows], of rows that are cut
+  Slice* slices;      // [2][rows][n_slices], of others
+  int whole[2];       // the target's, the drafter's are not cut
+  int n_seqs, n_rows, vocab, n_slices, slice;  // slice: entries of a block of k_verify
 };
+
+// ---- rows that are not cut
+//
+// A block has a slice: kVecs 16-byte vectors a thread, all asked for at once (those of a row's ends entry by entry).  Bounded by
+// reading the logits once; of an entry's some six instructions one is an exponential.
+constexpr int kRowThreads = 256, kVecs = 8;
+template <class T>
+constexpr int kSliceEntries = kRowThreads * kVecs * 16 / (int)sizeof(T);
+
+template <class T>
+__global__ void __launch_bounds__(kRowThreads) k_rows(const __grid_constant__ VerifyCall c, int side0) {
+  constexpr int kV = 16 / sizeof(T), kW = kRowThreads / 32;
+  __shared__ float s_m[kW], s_s[kW];
+  __shared__ int s_i[kW];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int q = blockIdx.x % c.n_slices, unit = blockIdx.x / c.n_slices, side = side0 + (unit >= c.n_rows), row = unit >= c.n_rows ? unit - c.n_rows : unit;
+  pdl_wait();
+  pdl_trigger();
+  const T* x = side ? static_cast<const T*>(c.draft) + (int64_t)row * c.draft_stride : static_cast<const T*>(c.logits) + (int64_t)row * c.logits_stride;
+  const int lead_in = (int)(((uintptr_t)x & 15) / sizeof(T)), v0 = q * (kRowThreads * kVecs) + tid;
+  uint4 raw[kVecs];
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k) {
+    const int i = (v0 + k * kRowThreads) * kV - lead_in;
+    if (i >= 0 && i + kV <= c.vocab) {
+      raw[k] = *reinterpret_cast<const uint4*>(x + i);
+    } else {
+      T e[kV];
+#pragma unroll
+      for (int u = 0; u < kV; ++u) e[u] = i + u >= 0 && i + u < c.vocab ? x[i + u] : T(-INFINITY);
+      memcpy(&raw[k], e, 16);
+    }
+  }
+  int lo = 0, hi = c.n_seqs - 1;  // the last sequence that begins at or before the row
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (__ldg(c.row_start + mid) <= row) lo = mid;
+    else hi = mid - 1;
+  }
+  const RowSpan sp = row_span(c.row_start, c.n_rows, lo);
+  if (row < sp.b || row >= sp.e || (side && row + 1 == sp.e)) return;
+  const float temp = c.temperature[side] ? c.temperature[side][lo] : 1.f;
+  const bool greedy = !(temp > 0.f);
+  const float inv_e = inverse(1.4426950408889634f, greedy ? 1.f : bounded(temp));
+  float m = -INFINITY;
+  auto each = [&](auto&& f) {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      T e[kV];
+      memcpy(e, &raw[k], 16);
+#pragma unroll
+      for (int u = 0; u < kV; ++u) f((float)e[u], (v0 + k * kRowThreads) * kV - lead_in + u);
+    }
+  };
+  each([&](float v, int) { m = fmaxf(m, v); });  // (a NaN is passed over)
+#pragma unroll
+  for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  if (lane == 0) s_m[warp] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kW; ++w) m = fmaxf(m, s_m[w]);
+  float s = 0.f;
+  int first = 0x7FFFFFFF;
+  if (greedy) {
+    each([&](float v, int i) {
+      if (v == m) first = min(first, i);
+    });
+  } else if (m == INFINITY) {
+    each([&](float v, int) { s += v == INFINITY ? 1.f : 0.f; });
+  } else if (m > -INFINITY) {
+    each([&](float v, int) {
+      float y;
+      asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"((fmaxf(v, -INFINITY) - m) * inv_e));
+      s += y;
+    });
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+  first = __reduce_min_sync(0xffffffffu, first);
+  if (lane == 0) s_s[warp] = s, s_i[warp] = first;
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 1; w < kW; ++w) s += s_s[w], first = min(first, s_i[w]);
+    c.slices[((int64_t)side * c.n_rows + row) * c.n_slices + q] = {m, s, first, 0};
+  }
+}
 
 // log p of the entry of index i, -inf where it is not kept
 __device__ __forceinline__ float log_p(const Kept& k, float x, int i) {
@@ -45,8 +144,9 @@ struct Best {  // the largest key so far, the lowest index where equal
 };
 
 template <class T>
-__global__ void __launch_bounds__(kThreads) k_verify(const __grid_constant__ VerifyCall c) {
+__global__ void __launch_bounds__(kThreads, 2) k_verify(const __grid_constant__ VerifyCall c) {
   __shared__ Best s_best[kWarps + 1];
+  __shared__ Kept s_kept[2];
   __shared__ int s_stop;
   cg::cluster_group cl = cg::this_cluster();
   const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank(), s = blockIdx.x / C;
@@ -60,32 +160,67 @@ __global__ void __launch_bounds__(kThreads) k_verify(const __grid_constant__ Ver
   const int drafts = sp.e - sp.b - 1;
   const T* logits = static_cast<const T*>(c.logits);
   const T* draft = static_cast<const T*>(c.draft);
-  auto draft_log_p = [&](int row) -> float {
-    const int x = __ldg(c.tokens + row + 1);
-    if (x < 0 || x >= c.vocab) return -INFINITY;
-    return log_p(c.kept[row], (float)logits[(int64_t)row * c.logits_stride + x], x);
+  // what a row keeps, in every lane of a warp (ordinary loads: read-only ones may be moved ahead of the wait)
+  auto kept_of = [&](int side, int row) -> Kept {
+    if (!c.whole[side]) return c.kept[(int64_t)side * c.n_rows + row];
+    const Slice* sl = c.slices + ((int64_t)side * c.n_rows + row) * c.n_slices;
+    const float temp = c.temperature[side] ? c.temperature[side][s] : 1.f;
+    const bool greedy = !(temp > 0.f);
+    const float t = greedy ? 1.f : bounded(temp), inv_e = inverse(1.4426950408889634f, t);
+    float m = -INFINITY, sum = 0.f;
+    int first = 0x7FFFFFFF;
+    auto join = [&](float om, float os, int oi) {
+      const float to = fmaxf(m, om);
+      sum = to == -INFINITY ? 0.f : sum * (m == to ? 1.f : exp2f((m - to) * inv_e)) + os * (om == to ? 1.f : exp2f((om - to) * inv_e));
+      first = m == om ? min(first, oi) : m > om ? first : oi;
+      m = to;
+    };
+    for (int q = lane; q < c.n_slices; q += 32) {
+      const Slice x = sl[q];
+      join(x.m, x.s, x.first);
+    }
+#pragma unroll
+    for (int d = 16; d; d >>= 1)
+      join(__shfl_xor_sync(0xffffffffu, m, d), __shfl_xor_sync(0xffffffffu, sum, d), __shfl_xor_sync(0xffffffffu, first, d));
+    return {m, t, greedy ? m : -INFINITY, 0.f, greedy ? first : 0x7FFFFFFF, greedy ? 0.f : logf(sum), m > -INFINITY, 0};
   };
   // ---- the drafts that are taken
   if (tid == 0) s_stop = drafts;
   __syncthreads();
-  for (int j = tid; j < drafts; j += kThreads) {
-    const int row = sp.b + j, x = __ldg(c.tokens + row + 1);
-    const float p = expf(draft_log_p(row));
+  for (int j = warp; j < drafts; j += kWarps) {
+    const int row = sp.b + j, x = c.tokens[row + 1];
+    const bool there = x >= 0 && x < c.vocab;
+    const float vp = there ? (float)logits[(int64_t)row * c.logits_stride + x] : -INFINITY,
+                vq = there && draft ? (float)draft[(int64_t)row * c.draft_stride + x] : -INFINITY;
+    const Kept kp = kept_of(0, row);
+    const float lp = log_p(kp, vp, x);
     float q = 1.f;
-    if (draft && x >= 0 && x < c.vocab) q = expf(log_p(c.kept[c.n_rows + row], (float)draft[(int64_t)row * c.draft_stride + x], x));
-    if (!(__ldg(c.u + row) * q < p)) atomicMin(&s_stop, j);
+    if (draft) q = expf(log_p(kept_of(1, row), vq, x));
+    if (lane == 0) {
+      if (!(c.u[row] * q < expf(lp))) atomicMin(&s_stop, j);
+      if (rank == 0) {  // (what is not taken after all is written over below)
+        c.token[row] = x;
+        if (c.logprob) c.logprob[row] = lp;
+      }
+    }
   }
   __syncthreads();
-  const int stop = s_stop, row = sp.b + stop, one = stop < drafts && !draft ? __ldg(c.tokens + row + 1) : -1;
-  const Kept kp = c.kept[row];
+  const int stop = s_stop, row = sp.b + stop, one = stop < drafts && !draft ? c.tokens[row + 1] : -1;
   const bool less = stop < drafts && draft;
-  Kept kq = {};
-  if (less) kq = c.kept[c.n_rows + row];
+  if (warp == 0) {
+    const Kept k = kept_of(0, row);
+    if (lane == 0) s_kept[0] = k;
+  } else if (warp == 1 && less) {
+    const Kept k = kept_of(1, row);
+    if (lane == 0) s_kept[1] = k;
+  }
+  __syncthreads();
+  const Kept kp = s_kept[0], kq = s_kept[1];
 
   // ---- the token after them
   const int i0 = rank * c.slice, i1 = min(c.vocab, i0 + c.slice);
   const T* x = logits + (int64_t)row * c.logits_stride;
-  const T* y = less ? draft + (int64_t)row * c.draft_stride : nullptr;
+  const T* y = less ? draft + (int64_t)row * c.draft_stride : x;
   const float* noise = c.noise + (int64_t)s * c.noise_stride;
   const Best none = {-INFINITY, -INFINITY, 0x7FFFFFFF};
   auto warp_best = [&](Best b) -> Best {
@@ -94,25 +229,48 @@ __global__ void __launch_bounds__(kThreads) k_verify(const __grid_constant__ Ver
       b.take(__shfl_xor_sync(0xffffffffu, b.v, d), __shfl_xor_sync(0xffffffffu, b.lp, d), __shfl_xor_sync(0xffffffffu, b.i, d));
     return b;
   };
+  const float inv_t = inverse(1.f, kp.t), low = fmaxf(kp.xc, -FLT_MAX);  // (NaN and -inf are never kept)
   Best b;
   for (int turn = 0; turn < 2; ++turn) {  // (the second where no entry has p > q: with p alone)
     b = none;
-    for (int i = i0 + tid; i < i1; i += kThreads) {
-      const float lp = log_p(kp, (float)x[i], i);
-      if (lp == -INFINITY) continue;
-      float key = lp;
-      if (turn == 0) {
-        if (i == one) continue;
-        if (less) {
-          const float lq = log_p(kq, (float)y[i], i);
+    const bool minus = less && turn == 0;
+    constexpr int kU = 8;  // entries of a thread that are under way together
+    float floor = -INFINITY;
+    for (int kb = i0; kb < i1; kb += kU * kThreads) {  // (a warp's lanes together)
+      const int k0 = kb + tid;
+      T vx[kU], vy[kU];
+      float g[kU];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int i = k0 + u * kThreads;
+        const bool in = i < i1;
+        vx[u] = in ? x[i] : T(-INFINITY), g[u] = in ? noise[i] : -INFINITY;
+        if (minus) vy[u] = in ? y[i] : T(-INFINITY);
+      }
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int i = k0 + u * kThreads;
+        const float v = (float)vx[u], d = v - kp.m, z = d * inv_t;
+        // The bound: z as a product differs from the quotient by a few 2^-24 of it; the margin is several times that of all
+        // roundings.  (A bound that is no number is looked at.)
+        if (!(v >= low) || fmaf(4e-6f, fabsf(z) + fabsf(kp.log_sum) + fabsf(g[u]) + 1.f, z - kp.log_sum + g[u]) < floor) continue;
+        if (i >= i1 || (turn == 0 && i == one)) continue;
+        const float lp = log_p(kp, v, i);
+        if (lp == -INFINITY) continue;
+        float key = lp;
+        if (minus) {
+          const float lq = log_p(kq, (float)vy[u], i);
           if (lq > -INFINITY) {
-            const float d = expf(lp) - expf(lq);
-            if (!(d > 0.f)) continue;
-            key = logf(d);
+            const float rest = expf(lp) - expf(lq);
+            if (!(rest > 0.f)) continue;
+            key = logf(rest);
           }
         }
+        b.take(fmaxf(key + g[u], -INFINITY), lp, i);
       }
-      b.take(fmaxf(key + noise[i], -INFINITY), lp, i);
+      floor = b.v;  // the warp's largest key
+#pragma unroll
+      for (int d = 16; d; d >>= 1) floor = fmaxf(floor, __shfl_xor_sync(0xffffffffu, floor, d));
     }
     b = warp_best(b);
     __syncthreads();
@@ -129,17 +287,25 @@ __global__ void __launch_bounds__(kThreads) k_verify(const __grid_constant__ Ver
   }
 
   if (rank != 0) return;
-  for (int j = tid; j <= drafts; j += kThreads) {
+  const bool empty = b.i == none.i;
+  for (int j = stop + tid; j <= drafts; j += kThreads) {
     const int at = sp.b + j;
-    const bool empty = b.i == none.i;
-    c.token[at] = j < stop ? __ldg(c.tokens + at + 1) : j > stop || empty ? -1 : b.i;
-    if (c.logprob) c.logprob[at] = j < stop ? draft_log_p(at) : j > stop || empty ? -INFINITY : b.lp;
+    c.token[at] = j > stop || empty ? -1 : b.i;
+    if (c.logprob) c.logprob[at] = j > stop || empty ? -INFINITY : b.lp;
   }
   if (tid == 0) c.accepted[s] = stop;
 }
 
 template <class T>
-cudaError_t run(VerifyCall c, int n_seqs, cudaStream_t s) {
+cudaError_t run(VerifyCall c, cudaStream_t s) {
+  const int n_seqs = c.n_seqs;
+  if (c.n_rows > 0 && (c.whole[0] || (c.draft && c.whole[1]))) {
+    c.n_slices = (c.vocab + 16 / (int)sizeof(T) - 1 + kSliceEntries<T> - 1) / kSliceEntries<T>;  // (a row may begin anywhere in a vector)
+    const int sides = c.whole[0] + (c.draft && c.whole[1]);
+    const cudaError_t e = launch_pdl(true, k_rows<T>, dim3((unsigned)(sides * c.n_rows) * (unsigned)c.n_slices), dim3(kRowThreads), 0, s, c,
+                                     c.whole[0] ? 0 : 1);
+    if (e != cudaSuccess) return e;
+  }
   int C = 1;
   while (C < 8 && (int64_t)n_seqs * C < 304 && c.vocab / C > 8192) C *= 2;
   c.slice = (c.vocab + C - 1) / C;
@@ -167,7 +333,8 @@ using namespace mf;
 
 extern "C" int mf_verify_bytes(int n_seqs, int n_rows, int vocab, uint64_t* out) {
   if (!out || n_seqs < 0 || n_rows < 0 || n_seqs > (1 << 26) || n_rows > (1 << 26) || vocab < 1 || vocab > kMaxVocab) return MF_E_INVAL;
-  *out = (uint64_t)(n_rows > 0 ? n_rows : 1) * 2 * sizeof(Kept);
+  const uint64_t slices = ((uint64_t)vocab + kSliceEntries<float> + 2) / kSliceEntries<float>;
+  *out = (uint64_t)(n_rows > 0 ? n_rows : 1) * 2 * (sizeof(Kept) + slices * sizeof(Slice));
   return MF_OK;
 }
 
@@ -188,15 +355,18 @@ extern "C" int mf_verify(const mf_verify_args_t* a, void* stream) {
     if (a->n_seqs > 1 && a->noise_stride < a->vocab) return MF_E_INVAL;
   }
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  auto whole = [](const mf_cuts_t& c) { return !c.top_p && !c.min_p && !c.top_k; };
+  const bool whole_p = whole(a->cuts), whole_q = whole(a->draft_cuts);
   Kept* kept = static_cast<Kept*>(a->work);
-  const KeptRows rows = {a->logits, a->draft_logits, a->logits_stride, a->draft_stride, a->row_start, a->cuts, a->draft_cuts,
-                         kept,      a->n_seqs,       a->n_rows,        a->vocab,        a->dtype};
-  const VerifyCall c = {a->logits, a->draft_logits, a->logits_stride, a->draft_stride, a->noise_stride, a->row_start, a->tokens, a->u,
-                        a->noise,  a->token,        a->accepted,      a->logprob,      kept,            a->n_rows,    a->vocab,  0};
-  cudaError_t e = a->n_rows > 0 ? launch_kept(rows, s) : cudaSuccess;
-  if (e == cudaSuccess)
-    e = a->dtype == MF_F32   ? run<float>(c, a->n_seqs, s)
-        : a->dtype == MF_F16 ? run<__half>(c, a->n_seqs, s)
-                             : run<__nv_bfloat16>(c, a->n_seqs, s);
+  const VerifyCall c = {a->logits, a->draft_logits, a->logits_stride, a->draft_stride, a->noise_stride, a->row_start, a->tokens, a->u, a->noise,
+                        {a->cuts.temperature, a->draft_cuts.temperature}, a->token, a->accepted, a->logprob, kept,
+                        reinterpret_cast<Slice*>(kept + 2 * (int64_t)a->n_rows), {whole_p, whole_q}, a->n_seqs, a->n_rows, a->vocab, 0, 0};
+  cudaError_t e = cudaSuccess;
+  if (a->n_rows > 0 && (!whole_p || (a->draft_logits && !whole_q))) {
+    const KeptRows rows = {a->logits,  whole_q ? nullptr : a->draft_logits, a->logits_stride, a->draft_stride, a->row_start, a->cuts, a->draft_cuts, kept,
+                           a->n_seqs, a->n_rows, a->vocab, a->dtype, !whole_p};
+    e = launch_kept(rows, s);
+  }
+  if (e == cudaSuccess) e = a->dtype == MF_F32 ? run<float>(c, s) : a->dtype == MF_F16 ? run<__half>(c, s) : run<__nv_bfloat16>(c, s);
   return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_verify");
 }
