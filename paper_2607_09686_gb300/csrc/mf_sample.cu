@@ -1184,6 +1184,8 @@ cudaError_t run(Call c, int rows, cudaStream_t s) {
 
 }  // namespace
 
+int sample_hold() { return g_hold.load(); }
+
 cudaError_t launch_kept(const KeptRows& k, cudaStream_t s) {
   KeptCall c = {};
   c.logits = k.logits, c.logits_stride = k.logits_stride, c.vocab = k.vocab, c.hold = g_hold.load();

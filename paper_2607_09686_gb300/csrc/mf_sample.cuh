@@ -35,6 +35,7 @@ struct KeptRows {
   int n_seqs, n_rows, vocab, dtype, target;
 };
 cudaError_t launch_kept(const KeptRows& rows, cudaStream_t s);
+int sample_hold();  // mf_sample_test_hold
 
 // The rows of a sequence, inside [0, n_rows].
 struct RowSpan {

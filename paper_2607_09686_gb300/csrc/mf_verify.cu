@@ -40,6 +40,7 @@ struct VerifyCall {
   Piece* pieces;      // [2][rows][n_units], of others
   int whole[2];       // the target's, the drafter's are not cut
   int n_seqs, n_rows, vocab, n_units, slice;  // units of a row (k_rows); slice: entries of a block of k_verify
+  int hold;  // (a test's) copies are not issued
 };
 
 // ---- rows that are not cut
@@ -172,86 +173,140 @@ struct Best {  // the largest key so far, the lowest index where equal
   }
 };
 
+// ---- the drafts and the token that follows
+//
+// The pass over the row that decides goes through a ring of chunks in shared memory, filled by bulk copies: logits, the drafter's
+// where they count, and the noise (of a row that is cut the few entries' that are kept are asked for one by one instead).  A copy
+// covers whole 16-byte vectors inside its row; what is left of a row's ends, and chunks whose copies do not arrive in time, are read where
+// they lie.
+constexpr int kU = 8, kChunk = kU * kThreads;  // entries of a thread, of a chunk
+constexpr int kTogether = kWarps / 2;                       // rows that are looked at together, two warps each
+template <class T>
+struct Stage {
+  static constexpr int kStages = sizeof(T) == 2 ? 3 : 2;  // of the ring: two blocks an SM
+  static constexpr uint32_t kLogits = kChunk * sizeof(T) + 128, kNoise = 2 * kLogits, kBytes = kNoise + kChunk * 4 + 128;
+};
+
+// A row's entries e0 .. e1 - 1 in a buffer: entry e at place + (e - e0) * sizeof(E), those from lo to hi - 1 by a copy.
+template <class E>
+struct Part {
+  const E* row;
+  uint32_t place;
+  int lo, hi;
+  // (n: entries of the row)
+  __device__ __forceinline__ void set(const E* r, int n, int e0, int e1, uint32_t buffer) {
+    row = r;
+    const uintptr_t p = (uintptr_t)r, first = (p + 15) & ~uintptr_t(15), last = (uintptr_t)(r + n) & ~uintptr_t(15);  // whole vectors
+    const uintptr_t a = (uintptr_t)(r + e0) & ~uintptr_t(15), b = ((uintptr_t)(r + e1) + 15) & ~uintptr_t(15);
+    const uintptr_t from = a > first ? a : first, to = b < last ? b : last;
+    place = buffer + (uint32_t)((uintptr_t)(r + e0) & 15);
+    lo = to > from ? (int)((int64_t)(from - p) / (int)sizeof(E)) : 0;  // (from may lie before e0)
+    hi = to > from ? (int)((int64_t)(to - p) / (int)sizeof(E)) : 0;
+  }
+  __device__ __forceinline__ uint32_t bytes() const { return (uint32_t)(hi - lo) * (uint32_t)sizeof(E); }
+  __device__ __forceinline__ void copy(unsigned char* smem, int e0, uint64_t* bar) const {
+    if (hi > lo) bulk_g2s(smem + (int)place + (lo - e0) * (int)sizeof(E), row + lo, bytes(), bar);
+  }
+  __device__ __forceinline__ E at(const unsigned char* smem, int e, int e0, bool there) const {
+    return there && e >= lo && e < hi ? *reinterpret_cast<const E*>(smem + place + (uint32_t)(e - e0) * (uint32_t)sizeof(E)) : row[e];
+  }
+};
+
 template <class T>
 __global__ void __launch_bounds__(kThreads, 2) k_verify(const __grid_constant__ VerifyCall c) {
-  __shared__ Best s_best[kWarps + 1];
-  __shared__ Kept s_kept[2];
-  __shared__ int s_stop;
+  extern __shared__ __align__(128) unsigned char ring[];
+  __shared__ Best s_best[kWarps], s_all[2][8];  // of the warps; of the cluster's blocks, by turn
+  __shared__ Kept s_kept[2][kTogether];
+  __shared__ float s_lp[2][kTogether];
+  constexpr int kStages = Stage<T>::kStages;
+  __shared__ uint64_t s_full[kStages], s_free[kStages];
+  __shared__ volatile int s_lost;
   cg::cluster_group cl = cg::this_cluster();
   const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank(), s = blockIdx.x / C;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) mbar_init(&s_full[i], 1), mbar_init(&s_free[i], kWarps);
+    s_lost = 0;
+    mbar_fence_init();
+  }
   pdl_wait();
   const RowSpan sp = row_span(c.row_start, c.n_rows, s);
   if (sp.b == sp.e) {
     if (rank == 0 && tid == 0) c.accepted[s] = 0;
     return;
   }
+  cl.barrier_arrive();  // (before any block writes to another's shared memory that one has to run: waited for below)
   const int drafts = sp.e - sp.b - 1;
   const T* logits = static_cast<const T*>(c.logits);
   const T* draft = static_cast<const T*>(c.draft);
+  const int i0 = rank * c.slice, i1 = min(c.vocab, i0 + c.slice);
+  const float* noise = c.noise + (int64_t)s * c.noise_stride;
+  if (tid == 32 && c.whole[0] && i1 > i0) {  // all of the noise will be asked for: into the L2 cache meanwhile
+    const uintptr_t a = ((uintptr_t)(noise + i0) + 15) & ~uintptr_t(15), e = (uintptr_t)(noise + i1) & ~uintptr_t(15);
+    if (e > a) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a), "r"((uint32_t)(e - a)) : "memory");
+  }
   // what a row keeps, in every lane of a warp (ordinary loads: read-only ones may be moved ahead of the wait)
   auto kept_of = [&](int side, int row) -> Kept {
     if (!c.whole[side]) return c.kept[(int64_t)side * c.n_rows + row];
     const Piece* pieces = c.pieces + ((int64_t)side * c.n_rows + row) * c.n_units;
-    const int n = min(max(pieces->n, 0), c.n_units);
+    Piece x = {-INFINITY, 0.f, 0x7FFFFFFF, 0};
+    if (lane < c.n_units) x = pieces[lane];  // (asked for before their number is known)
+    const int n = min(max(__shfl_sync(0xffffffffu, x.n, 0), 0), c.n_units);
+    if (lane >= n) x = {-INFINITY, 0.f, 0x7FFFFFFF, 0};
     const float temp = c.temperature[side] ? c.temperature[side][s] : 1.f;
     const bool greedy = !(temp > 0.f);
     const float t = greedy ? 1.f : bounded(temp), inv_e = inverse(1.4426950408889634f, t);
-    float m = -INFINITY, sum = 0.f;
-    int first = 0x7FFFFFFF;
-    auto join = [&](float om, float os, int oi) {
-      const float to = fmaxf(m, om);
-      sum = to == -INFINITY ? 0.f : sum * (m == to ? 1.f : exp2f((m - to) * inv_e)) + os * (om == to ? 1.f : exp2f((om - to) * inv_e));
-      first = m == om ? min(first, oi) : m > om ? first : oi;
-      m = to;
-    };
-    for (int q = lane; q < n; q += 32) {
-      const Piece x = pieces[q];
-      join(x.m, x.s, x.first);
+    for (int q = lane + 32; q < n; q += 32) {
+      const Piece y = pieces[q];
+      const float to = fmaxf(x.m, y.m);
+      x.s = to == -INFINITY ? 0.f : x.s * (x.m == to ? 1.f : exp2f((x.m - to) * inv_e)) + y.s * (y.m == to ? 1.f : exp2f((y.m - to) * inv_e));
+      x.first = x.m == y.m ? min(x.first, y.first) : x.m > y.m ? x.first : y.first;
+      x.m = to;
     }
+    float m = x.m;
 #pragma unroll
-    for (int d = 16; d; d >>= 1)
-      join(__shfl_xor_sync(0xffffffffu, m, d), __shfl_xor_sync(0xffffffffu, sum, d), __shfl_xor_sync(0xffffffffu, first, d));
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    float sum = x.m == m ? x.s : x.m == -INFINITY ? 0.f : x.s * exp2f((x.m - m) * inv_e);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    const int first = __reduce_min_sync(0xffffffffu, x.m == m ? x.first : 0x7FFFFFFF);
     return {m, t, greedy ? m : -INFINITY, 0.f, greedy ? first : 0x7FFFFFFF, greedy ? 0.f : logf(sum), m > -INFINITY, 0};
   };
-  // ---- the drafts that are taken
-  if (tid == 0) s_stop = drafts;
-  __syncthreads();
-  for (int j = warp; j < drafts; j += kWarps) {
-    const int row = sp.b + j, x = c.tokens[row + 1];
-    const bool there = x >= 0 && x < c.vocab;
-    const float vp = there ? (float)logits[(int64_t)row * c.logits_stride + x] : -INFINITY,
-                vq = there && draft ? (float)draft[(int64_t)row * c.draft_stride + x] : -INFINITY;
-    const Kept kp = kept_of(0, row);
-    const float lp = log_p(kp, vp, x);
-    float q = 1.f;
-    if (draft) q = expf(log_p(kept_of(1, row), vq, x));
-    if (lane == 0) {
-      if (!(c.u[row] * q < expf(lp))) atomicMin(&s_stop, j);
-      if (rank == 0) {  // (what is not taken after all is written over below)
-        c.token[row] = x;
-        if (c.logprob) c.logprob[row] = lp;
-      }
+  // ---- the drafts that are taken: kTogether rows at a time, until one stops
+  int stop = drafts, j0 = 0;
+  for (;; j0 += kTogether) {
+    const int j = j0 + (warp >> 1), side = warp & 1, row = sp.b + j;
+    if (j <= drafts && (side == 0 || (draft && j < drafts))) {
+      const int x = j < drafts ? c.tokens[row + 1] : -1;
+      const T* from = side ? draft + (int64_t)row * c.draft_stride : logits + (int64_t)row * c.logits_stride;
+      const float v = x >= 0 && x < c.vocab ? (float)from[x] : -INFINITY;
+      const Kept k = kept_of(side, row);
+      if (lane == 0) s_kept[side][warp >> 1] = k, s_lp[side][warp >> 1] = log_p(k, v, x);
     }
+    __syncthreads();
+    if (lane < kTogether && j0 + lane < drafts) {  // (in every warp)
+      const float q = draft ? expf(s_lp[1][lane]) : 1.f;
+      if (!(c.u[sp.b + j0 + lane] * q < expf(s_lp[0][lane]))) stop = j0 + lane;
+    }
+    stop = __reduce_min_sync(0xffffffffu, stop);
+    if (rank == 0 && tid < kTogether && j0 + tid < stop) {
+      const int at = sp.b + j0 + tid;
+      c.token[at] = c.tokens[at + 1];
+      if (c.logprob) c.logprob[at] = s_lp[0][tid];
+    }
+    if (stop < j0 + kTogether) break;
+    __syncthreads();
   }
-  __syncthreads();
-  const int stop = s_stop, row = sp.b + stop, one = stop < drafts && !draft ? c.tokens[row + 1] : -1;
+  const int row = sp.b + stop, one = stop < drafts && !draft ? c.tokens[row + 1] : -1;
   const bool less = stop < drafts && draft;
-  if (warp == 0) {
-    const Kept k = kept_of(0, row);
-    if (lane == 0) s_kept[0] = k;
-  } else if (warp == 1 && less) {
-    const Kept k = kept_of(1, row);
-    if (lane == 0) s_kept[1] = k;
-  }
-  __syncthreads();
-  const Kept kp = s_kept[0], kq = s_kept[1];
+  const Kept kp = s_kept[0][stop - j0], kq = less ? s_kept[1][stop - j0] : Kept{};
 
   // ---- the token after them
-  const int i0 = rank * c.slice, i1 = min(c.vocab, i0 + c.slice);
   const T* x = logits + (int64_t)row * c.logits_stride;
   const T* y = less ? draft + (int64_t)row * c.draft_stride : x;
-  const float* noise = c.noise + (int64_t)s * c.noise_stride;
+  const bool some = !c.whole[0];  // of the row: noise and the drafter's logits entry by entry
+  const float inv_t = inverse(1.f, kp.t), low = fmaxf(kp.xc, -FLT_MAX);  // (NaN and -inf are never kept)
+  const int chunks = i1 > i0 && kp.any ? (i1 - i0 + kChunk - 1) / kChunk : 0;
   const Best none = {-INFINITY, -INFINITY, 0x7FFFFFFF};
   auto warp_best = [&](Best b) -> Best {
 #pragma unroll
@@ -259,87 +314,148 @@ __global__ void __launch_bounds__(kThreads, 2) k_verify(const __grid_constant__ 
       b.take(__shfl_xor_sync(0xffffffffu, b.v, d), __shfl_xor_sync(0xffffffffu, b.lp, d), __shfl_xor_sync(0xffffffffu, b.i, d));
     return b;
   };
-  const float inv_t = inverse(1.f, kp.t), low = fmaxf(kp.xc, -FLT_MAX);  // (NaN and -inf are never kept)
+  struct Parts {
+    Part<T> x, y;
+    Part<float> g;
+  };
+  auto parts_of = [&](int k) -> Parts {
+    const int e0 = i0 + k * kChunk, e1 = min(i1, e0 + kChunk);
+    const uint32_t at = (uint32_t)(k % kStages) * Stage<T>::kBytes;
+    Parts p;
+    p.x.set(x, c.vocab, e0, e1, at + 64);
+    p.y.set(y, c.vocab, e0, e1, at + Stage<T>::kLogits + 64);
+    p.g.set(noise, c.vocab, e0, e1, at + Stage<T>::kNoise + 64);
+    if (some || !less) p.y.lo = p.y.hi = 0;
+    if (some) p.g.lo = p.g.hi = 0;
+    return p;
+  };
+  auto fill = [&](int k) {  // (one thread)
+    const Parts p = parts_of(k);
+    const int e0 = i0 + k * kChunk;
+    uint64_t* bar = &s_full[k % kStages];
+    mbar_arrive_tx(bar, c.hold ? 1 : p.x.bytes() + p.y.bytes() + p.g.bytes());
+    if (c.hold) return;
+    p.x.copy(ring, e0, bar), p.y.copy(ring, e0, bar), p.g.copy(ring, e0, bar);
+  };
+  if (tid == 0)
+    for (int k = 0; k < min(chunks, kStages); ++k) fill(k);
+  // chunks that are copied whole: entries from in_lo to in_hi; an entry's place in its chunk's buffer (the same in all chunks)
+  int in_lo, in_hi;
+  {
+    Part<T> a;
+    Part<float> g;
+    a.set(x, c.vocab, 0, c.vocab, 0), g.set(noise, c.vocab, 0, c.vocab, 0);
+    in_lo = some ? a.lo : max(a.lo, g.lo), in_hi = min(i1, some ? a.hi : min(a.hi, g.hi));
+  }
+  const uint32_t x_off = 64 + (uint32_t)((uintptr_t)(x + i0) & 15), g_off = Stage<T>::kNoise + 64 + (uint32_t)((uintptr_t)(noise + i0) & 15);
+  // The bound of a key is z + noise - log_sum with a margin several times that of all roundings, 4e-6 of their sizes and of M / T; what
+  // of it is the same for all entries is taken off the other side.
+  const float shift = -kp.m * inv_t - kp.log_sum, slack = 4e-6f * (1.f + 2.f * fabsf(kp.log_sum) + 4.f * fabsf(kp.m * inv_t));
+  const bool by_bound = fabsf(kp.m) < INFINITY;  // (else every entry is looked at)
   Best b;
-  for (int turn = 0; turn < 2; ++turn) {  // (the second where no entry has p > q: with p alone)
+  for (int turn = 0; turn < 2; ++turn) {  // (the second where no entry has p > q: with p alone, from where the rows lie)
     b = none;
     const bool minus = less && turn == 0;
-    constexpr int kU = 4;  // entries of a thread that are under way while it takes as many
     float floor = -INFINITY;
-    T vx[kU], vy[kU], wx[kU], wy[kU];
-    float g[kU], h[kU];
-    auto load = [&](T* ax, T* ay, float* ag, int k0) {
+    for (int k = 0; k < chunks; ++k) {  // (a warp's lanes together)
+      const int e0 = i0 + k * kChunk, e1 = min(i1, e0 + kChunk), stage = k % kStages;
+      bool there = turn == 0 && !s_lost;
+      if (there && !mbar_wait(&s_full[stage], (uint32_t)(k / kStages) & 1, kDefaultWaitNs)) there = false, s_lost = 1;
+      const unsigned char* buf = ring + stage * Stage<T>::kBytes;
+      T vx[kU];
+      float g[kU];
+      if (there && e0 >= in_lo && e0 + kChunk <= in_hi) {
+        const T* px = reinterpret_cast<const T*>(buf + x_off) + tid;
 #pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        const int i = k0 + u * kThreads;
-        const bool in = i < i1;
-        ax[u] = in ? x[i] : T(-INFINITY), ag[u] = in ? noise[i] : -INFINITY;
-        ay[u] = in && minus ? y[i] : T(-INFINITY);
-      }
-    };
-    load(wx, wy, h, i0 + tid);
-    for (int kb = i0; kb < i1; kb += kU * kThreads) {  // (a warp's lanes together)
-      const int k0 = kb + tid;
+        for (int u = 0; u < kU; ++u) vx[u] = px[u * kThreads];
+        if (!some) {
+          const float* pg = reinterpret_cast<const float*>(buf + g_off) + tid;
 #pragma unroll
-      for (int u = 0; u < kU; ++u) vx[u] = wx[u], vy[u] = wy[u], g[u] = h[u];
-      load(wx, wy, h, k0 + kU * kThreads);
-      // The bound of a key: z as a product differs from the quotient by a few 2^-24 of it; the margin is several times that of all
-      // roundings.  (A bound that is no number is looked at.)
-      float ub[kU];
-#pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        const float v = (float)vx[u], z = (v - kp.m) * inv_t;
-        const int i = k0 + u * kThreads;
-        ub[u] = fmaf(4e-6f, fabsf(z) + fabsf(kp.log_sum) + fabsf(g[u]) + 1.f, z - kp.log_sum + g[u]);
-        ub[u] = ub[u] != ub[u] ? INFINITY : fmaxf(ub[u], -FLT_MAX);
-        if (!(v >= low) || i >= i1 || (turn == 0 && i == one)) ub[u] = -INFINITY;
-      }
-      // each thread's most promising entry in turn, until none of the warp's reaches its largest key
-      for (;;) {
-        float most = -INFINITY, cg = 0.f;
-        T cx = T(0.f), cy = T(0.f);
-        int ci = -1;
-#pragma unroll
-        for (int u = 0; u < kU; ++u)
-          if (ub[u] > most) most = ub[u], cx = vx[u], cy = vy[u], cg = g[u], ci = u;
-        const bool look = ci >= 0 && !(most < floor);
-        if (!__any_sync(0xffffffffu, look)) break;
-        if (look) {
-#pragma unroll
-          for (int u = 0; u < kU; ++u)
-            if (u == ci) ub[u] = -INFINITY;
-          const int i = k0 + ci * kThreads;
-          const float lp = log_p(kp, (float)cx, i);
-          float key = lp;
-          bool in = lp > -INFINITY;
-          if (in && minus) {
-            const float lq = log_p(kq, (float)cy, i);
-            if (lq > -INFINITY) {
-              const float rest = expf(lp) - expf(lq);
-              in = rest > 0.f;
-              key = logf(rest);
-            }
-          }
-          if (in) b.take(fmaxf(key + cg, -INFINITY), lp, i);
+          for (int u = 0; u < kU; ++u) g[u] = pg[u * kThreads];
         }
-        floor = b.v;
+      } else {
+        const Parts p = parts_of(k);
 #pragma unroll
-        for (int d = 16; d; d >>= 1) floor = fmaxf(floor, __shfl_xor_sync(0xffffffffu, floor, d));
+        for (int u = 0; u < kU; ++u) {
+          const int e = e0 + u * kThreads + tid;
+          vx[u] = e < e1 ? p.x.at(ring, e, e0, there) : T(-INFINITY);
+          if (!some) g[u] = e < e1 ? p.g.at(ring, e, e0, there) : 0.f;
+        }
+      }
+      if (some) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) g[u] = (float)vx[u] >= low ? noise[e0 + u * kThreads + tid] : 0.f;
+      }
+      const float over = floor - slack;
+      bool any = false;
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const float v = (float)vx[u], a = fmaf(v, inv_t, shift);
+        any |= v >= low && !(fmaf(4e-6f, fabsf(a) + fabsf(g[u]), a + g[u]) < over);
+      }
+      if (__any_sync(0xffffffffu, any)) {
+        // each thread's most promising entry in turn, until none of the warp's reaches its largest key
+        uint32_t left = (1u << kU) - 1;
+        for (;;) {
+          float most = -INFINITY, cg = 0.f;
+          T cx = T(0.f);
+          int ci = -1;
+#pragma unroll
+          for (int u = 0; u < kU; ++u) {
+            const float v = (float)vx[u], a = fmaf(v, inv_t, shift);
+            float ub = fmaf(4e-6f, fabsf(a) + fabsf(g[u]), a + g[u]) + slack;
+            ub = by_bound && ub == ub ? fmaxf(ub, -FLT_MAX) : INFINITY;  // (a bound that is no number is looked at)
+            if (v >= low && (left >> u & 1) && ub > most) most = ub, cx = vx[u], cg = g[u], ci = u;
+          }
+          const bool look = ci >= 0 && !(most < floor);
+          if (!__any_sync(0xffffffffu, look)) break;
+          if (look) {
+            left &= ~(1u << ci);
+            const int e = e0 + ci * kThreads + tid;
+            const float lp = log_p(kp, (float)cx, e);
+            float key = lp;
+            bool in = lp > -INFINITY && !(turn == 0 && e == one);
+            if (in && minus) {
+              const float lq = log_p(kq, (float)(there && !some ? parts_of(k).y.at(ring, e, e0, true) : y[e]), e);
+              if (lq > -INFINITY) {
+                const float rest = expf(lp) - expf(lq);
+                in = rest > 0.f;
+                key = logf(rest);
+              }
+            }
+            if (in) b.take(fmaxf(key + cg, -INFINITY), lp, e);
+          }
+          floor = b.v;
+#pragma unroll
+          for (int d = 16; d; d >>= 1) floor = fmaxf(floor, __shfl_xor_sync(0xffffffffu, floor, d));
+        }
+      }
+      if (turn == 0) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s_free[stage]);
+        if (tid == 0 && k + kStages < chunks && !s_lost) {
+          if (mbar_wait(&s_free[stage], (uint32_t)(k / kStages) & 1, kDefaultWaitNs)) fill(k + kStages);
+          else s_lost = 1;
+        }
       }
     }
+    // the block's, then the cluster's: every block tells every other
     b = warp_best(b);
-    __syncthreads();
     if (lane == 0) s_best[warp] = b;
     __syncthreads();
+    if (turn == 0) cl.barrier_wait();
     if (warp == 0) {
       b = warp_best(lane < kWarps ? s_best[lane] : none);
-      if (lane == 0) s_best[kWarps] = b;
+      if (lane < C) cl.map_shared_rank(&s_all[turn][0], lane)[rank] = b;
     }
     cl.sync();
-    b = warp_best(lane < C ? cl.map_shared_rank(s_best, lane)[kWarps] : none);
-    cl.sync();  // no block writes its best again, or leaves, while another reads it
+    b = none;
+    for (int q = 0; q < C; ++q) b.take(s_all[turn][q].v, s_all[turn][q].lp, s_all[turn][q].i);
     if (b.i != none.i) break;
   }
+  // no copy may be in flight when the block exits (one that was not waited for: its chunk was read without it)
+  if (tid == 0 && s_lost && !c.hold)
+    for (int i = 0; i < kStages; ++i) mbar_wait(&s_full[i], 0, kDefaultWaitNs), mbar_wait(&s_full[i], 1, kDefaultWaitNs);
 
   if (rank != 0) return;
   const bool empty = b.i == none.i;
@@ -368,6 +484,7 @@ cudaError_t run(VerifyCall c, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)n_seqs * (unsigned)C);
   cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Stage<T>::kStages * Stage<T>::kBytes;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -376,7 +493,8 @@ cudaError_t run(VerifyCall c, cudaStream_t s) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, k_verify<T>, c);
+  const cudaError_t e = cudaFuncSetAttribute(k_verify<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+  return e == cudaSuccess ? cudaLaunchKernelEx(&cfg, k_verify<T>, c) : e;
 }
 
 bool bad_word(const void* p) { return ((uintptr_t)p & 3) != 0; }
@@ -416,7 +534,7 @@ extern "C" int mf_verify(const mf_verify_args_t* a, void* stream) {
   Kept* kept = static_cast<Kept*>(a->work);
   const VerifyCall c = {a->logits, a->draft_logits, a->logits_stride, a->draft_stride, a->noise_stride, a->row_start, a->tokens, a->u, a->noise,
                         {a->cuts.temperature, a->draft_cuts.temperature}, a->token, a->accepted, a->logprob, kept,
-                        reinterpret_cast<Piece*>(kept + 2 * (int64_t)a->n_rows), {whole_p, whole_q}, a->n_seqs, a->n_rows, a->vocab, 0, 0};
+                        reinterpret_cast<Piece*>(kept + 2 * (int64_t)a->n_rows), {whole_p, whole_q}, a->n_seqs, a->n_rows, a->vocab, 0, 0, sample_hold()};
   cudaError_t e = cudaSuccess;
   if (a->n_rows > 0 && (!whole_p || (a->draft_logits && !whole_q))) {
     const KeptRows rows = {a->logits,  whole_q ? nullptr : a->draft_logits, a->logits_stride, a->draft_stride, a->row_start, a->cuts, a->draft_cuts, kept,
