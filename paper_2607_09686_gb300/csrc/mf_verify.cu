@@ -19,7 +19,7 @@ namespace cg = cooperative_groups;
 namespace mf {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
 
 // Of a piece of a row: the largest logit, its first index (rows without a temperature), the sum of w against it; in a row's first piece
 // their number.
@@ -47,9 +47,10 @@ struct VerifyCall {
 //
 // The rows' units of 128 16-byte vectors are one list, shared out evenly: a warp takes a run of units, four vectors a lane at a time while the
 // next four are under way, with a running maximum and sum a lane, and leaves a piece where a row or its run ends (which depends on
-// the sizes alone).  Neighbouring runs lie on different SMs: some rows are not needed, and what is left stays evenly spread.  Bounded by
+// the row starts alone).  The list has the target's rows and those of the drafter's that have a draft: every block adds up the sequences' rows
+// in shared memory (of more than kSeqs sequences, or bounds that overlap: all rows, of which some are passed over).  Bounded by
 // reading the logits once; of an entry's some six instructions one is an exponential.
-constexpr int kRowThreads = 256, kUnit = 128, kVecs = kUnit / 32;
+constexpr int kRowThreads = 256, kUnit = 128, kVecs = kUnit / 32, kSeqs = 2048;
 template <class T>
 constexpr int kUnitEntries = kUnit * 16 / (int)sizeof(T);
 
@@ -57,21 +58,67 @@ template <class T>
 __global__ void __launch_bounds__(kRowThreads, 3) k_rows(const __grid_constant__ VerifyCall c, int side0, int rows) {
   constexpr int kV = 16 / sizeof(T);
   const int lane = threadIdx.x & 31;
-  // runs: no more than units, so that each has one and a row no more pieces than units
-  const int64_t U = (int64_t)rows * c.n_units, S = min((int64_t)gridDim.x * (kRowThreads / 32), U);
-  const int64_t w = (int64_t)(threadIdx.x >> 5) * gridDim.x + blockIdx.x, u0 = w < S ? U * w / S : 0, u1 = w < S ? U * (w + 1) / S : 0;
+  // rows before a sequence: the target's, the drafter's
+  __shared__ int s_rows[kSeqs + 1], s_drafts[kSeqs + 1];
+  __shared__ int2 s_sum[kRowThreads / 32];
   pdl_wait();
   pdl_trigger();
+  int listed = rows, target = side0 ? 0 : c.n_rows;  // rows of the list; the target's among them
+  bool packed = c.n_seqs <= kSeqs;
+  if (packed) {
+    int64_t all = 0;
+    int2 done = make_int2(0, 0);
+    for (int base = 0; base < c.n_seqs; base += kRowThreads) {
+      const int q = base + (int)threadIdx.x;
+      int n = 0;
+      if (q < c.n_seqs) {
+        const RowSpan sp = row_span(c.row_start, c.n_rows, q);
+        n = sp.e - sp.b;
+      }
+      int2 x = make_int2(n, max(n - 1, 0));  // inclusive prefixes
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int2 o = make_int2(__shfl_up_sync(0xffffffffu, x.x, d), __shfl_up_sync(0xffffffffu, x.y, d));
+        if (lane >= d) x.x += o.x, x.y += o.y;
+      }
+      __syncthreads();
+      if (lane == 31) s_sum[threadIdx.x >> 5] = x;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kRowThreads / 32; ++i) {
+        const int2 o = s_sum[i];
+        if (i < (int)(threadIdx.x >> 5)) x.x += o.x, x.y += o.y;
+        all += o.x;
+      }
+      if (q < c.n_seqs) s_rows[q + 1] = done.x + x.x, s_drafts[q + 1] = done.y + x.y;
+      if (all > c.n_rows) break;
+      for (int i = 0; i < kRowThreads / 32; ++i) done.x += s_sum[i].x, done.y += s_sum[i].y;
+    }
+    if (threadIdx.x == 0) s_rows[0] = s_drafts[0] = 0;
+    packed = all <= c.n_rows;
+    __syncthreads();
+    if (packed) {
+      target = side0 ? 0 : s_rows[c.n_seqs];
+      listed = target + (rows > c.n_rows || side0 ? s_drafts[c.n_seqs] : 0);
+    }
+  }
+  // runs: no more than units, so that each has one and a row no more pieces than units
+  const int64_t U = (int64_t)listed * c.n_units, S = min((int64_t)gridDim.x * (kRowThreads / 32), U);
+  const int64_t w = (int64_t)(threadIdx.x >> 5) * gridDim.x + blockIdx.x, u0 = w < S ? U * w / S : 0, u1 = w < S ? U * (w + 1) / S : 0;
   if (u0 >= u1) return;
   const float none = -INFINITY;
   int at = (int)(u0 / c.n_units), q = (int)(u0 - (int64_t)at * c.n_units);  // row of the list, unit of the row
   const T* x = nullptr;
   int lead_in = 0;
-  auto row_of = [&](int r) {  // where a row of the list begins
-    const bool second = side0 || r >= c.n_rows;
-    const int row = r >= c.n_rows ? r - c.n_rows : r;
-    x = second ? static_cast<const T*>(c.draft) + (int64_t)row * c.draft_stride : static_cast<const T*>(c.logits) + (int64_t)row * c.logits_stride;
-    lead_in = (int)(((uintptr_t)x & 15) / sizeof(T));
+  // the last sequence that has a place at or before i (of those that begin there too: the last, which has rows)
+  auto search = [&](const int* before, int i) {
+    int lo = 0, hi = c.n_seqs - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (before[mid] <= i) lo = mid;
+      else hi = mid - 1;
+    }
+    return lo;
   };
   auto load = [&](uint4 (&v)[kVecs], int unit) {
 #pragma unroll
@@ -88,19 +135,22 @@ __global__ void __launch_bounds__(kRowThreads, 3) k_rows(const __grid_constant__
     }
   };
   for (int64_t u = u0; u < u1; ++at, q = 0) {  // row by row
-    const int end = (int)min((int64_t)c.n_units, q + u1 - u), side = side0 || at >= c.n_rows, row = at >= c.n_rows ? at - c.n_rows : at;
+    const int end = (int)min((int64_t)c.n_units, q + u1 - u), side = side0 || at >= target, i = at >= target ? at - target : at;
     u += end - q;
     uint4 v[kVecs], next[kVecs];
-    row_of(at);
-    load(next, q);
-    int lo = 0, hi = c.n_seqs - 1;  // the last sequence that begins at or before the row
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (c.row_start[mid] <= row) lo = mid;
-      else hi = mid - 1;
+    int row = i, lo;
+    if (packed) {
+      lo = search(side ? s_drafts : s_rows, i);
+      row = row_span(c.row_start, c.n_rows, lo).b + i - (side ? s_drafts : s_rows)[lo];
     }
-    const RowSpan sp = row_span(c.row_start, c.n_rows, lo);
-    if (row < sp.b || row >= sp.e || (side && row + 1 == sp.e)) continue;
+    x = side ? static_cast<const T*>(c.draft) + (int64_t)row * c.draft_stride : static_cast<const T*>(c.logits) + (int64_t)row * c.logits_stride;
+    lead_in = (int)(((uintptr_t)x & 15) / sizeof(T));
+    load(next, q);
+    if (!packed) {
+      lo = search(c.row_start, row);
+      const RowSpan sp = row_span(c.row_start, c.n_rows, lo);
+      if (row < sp.b || row >= sp.e || (side && row + 1 == sp.e)) continue;
+    }
     const float temp = c.temperature[side] ? c.temperature[side][lo] : 1.f;
     const bool greedy = !(temp > 0.f);
     const float inv_e = inverse(1.4426950408889634f, greedy ? 1.f : bounded(temp));
@@ -175,15 +225,17 @@ struct Best {  // the largest key so far, the lowest index where equal
 
 // ---- the drafts and the token that follows
 //
-// The pass over the row that decides goes through a ring of chunks in shared memory, filled by bulk copies: logits, the drafter's
-// where they count, and the noise (of a row that is cut the few entries' that are kept are asked for one by one instead).  A copy
-// covers whole 16-byte vectors inside its row; what is left of a row's ends, and chunks whose copies do not arrive in time, are read where
-// they lie.
+// The pass over the row that decides goes through a ring of chunks in shared memory that a warp of its own fills by bulk copies: logits, the
+// drafter's where they count, and the noise.  A copy covers whole 16-byte vectors inside its row; what is left of a row's ends, and
+// chunks whose copies do not arrive in time, are read where they lie.  Each thread keeps the two largest bounds of its keys: log p + noise
+// + log(1 - q / p) by approximate exponentials, with a margin for all roundings; an entry that the drafter may not have kept counts as if it had
+// not.  With the largest bound's key worked out, no entry whose bound lies below the block's largest key can be the one; a thread whose second does
+// not looks at all its entries.
 constexpr int kU = 8, kChunk = kU * kThreads;  // entries of a thread, of a chunk
-constexpr int kTogether = kWarps / 2;                       // rows that are looked at together, two warps each
+constexpr int kTogether = kWarps;               // rows that are looked at together, a warp each
 template <class T>
 struct Stage {
-  static constexpr int kStages = sizeof(T) == 2 ? 3 : 2;  // of the ring: two blocks an SM
+  static constexpr int kStages = sizeof(T) == 2 ? 3 : 2;  // of the ring: three blocks an SM and more
   static constexpr uint32_t kLogits = kChunk * sizeof(T) + 128, kNoise = 2 * kLogits, kBytes = kNoise + kChunk * 4 + 128;
 };
 
@@ -213,7 +265,7 @@ struct Part {
 };
 
 template <class T>
-__global__ void __launch_bounds__(kThreads, 2) k_verify(const __grid_constant__ VerifyCall c) {
+__global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_constant__ VerifyCall c) {
   extern __shared__ __align__(128) unsigned char ring[];
   __shared__ Best s_best[kWarps], s_all[2][8];  // of the warps; of the cluster's blocks, by turn
   __shared__ Kept s_kept[2][kTogether];
@@ -245,43 +297,48 @@ __global__ void __launch_bounds__(kThreads, 2) k_verify(const __grid_constant__ 
     const uintptr_t a = ((uintptr_t)(noise + i0) + 15) & ~uintptr_t(15), e = (uintptr_t)(noise + i1) & ~uintptr_t(15);
     if (e > a) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a), "r"((uint32_t)(e - a)) : "memory");
   }
-  // what a row keeps, in every lane of a warp (ordinary loads: read-only ones may be moved ahead of the wait)
+  // what a row keeps, in 16 lanes of the target's and 16 of the drafter's, all lanes together (ordinary loads: read-only ones may be moved
+  // ahead of the wait)
   auto kept_of = [&](int side, int row) -> Kept {
-    if (!c.whole[side]) return c.kept[(int64_t)side * c.n_rows + row];
+    if (!c.whole[0] && !c.whole[1]) return c.kept[(int64_t)side * c.n_rows + row];
+    const int sub = lane & 15;
     const Piece* pieces = c.pieces + ((int64_t)side * c.n_rows + row) * c.n_units;
     Piece x = {-INFINITY, 0.f, 0x7FFFFFFF, 0};
-    if (lane < c.n_units) x = pieces[lane];  // (asked for before their number is known)
-    const int n = min(max(__shfl_sync(0xffffffffu, x.n, 0), 0), c.n_units);
-    if (lane >= n) x = {-INFINITY, 0.f, 0x7FFFFFFF, 0};
+    if (c.whole[side] && sub < c.n_units) x = pieces[sub];  // (asked for before their number is known)
+    const int n = min(max(__shfl_sync(0xffffffffu, x.n, lane & 16), 0), c.n_units);
+    if (sub >= n) x = {-INFINITY, 0.f, 0x7FFFFFFF, 0};
     const float temp = c.temperature[side] ? c.temperature[side][s] : 1.f;
     const bool greedy = !(temp > 0.f);
     const float t = greedy ? 1.f : bounded(temp), inv_e = inverse(1.4426950408889634f, t);
-    for (int q = lane + 32; q < n; q += 32) {
+    for (int q = sub + 16; q < n; q += 16) {
       const Piece y = pieces[q];
       const float to = fmaxf(x.m, y.m);
       x.s = to == -INFINITY ? 0.f : x.s * (x.m == to ? 1.f : exp2f((x.m - to) * inv_e)) + y.s * (y.m == to ? 1.f : exp2f((y.m - to) * inv_e));
       x.first = x.m == y.m ? min(x.first, y.first) : x.m > y.m ? x.first : y.first;
       x.m = to;
     }
+    __syncwarp();
     float m = x.m;
 #pragma unroll
-    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    for (int d = 8; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
     float sum = x.m == m ? x.s : x.m == -INFINITY ? 0.f : x.s * exp2f((x.m - m) * inv_e);
+    int first = x.m == m ? x.first : 0x7FFFFFFF;
 #pragma unroll
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    const int first = __reduce_min_sync(0xffffffffu, x.m == m ? x.first : 0x7FFFFFFF);
+    for (int d = 8; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d), first = min(first, __shfl_xor_sync(0xffffffffu, first, d));
+    if (!c.whole[side]) return c.kept[(int64_t)side * c.n_rows + row];
     return {m, t, greedy ? m : -INFINITY, 0.f, greedy ? first : 0x7FFFFFFF, greedy ? 0.f : logf(sum), m > -INFINITY, 0};
   };
   // ---- the drafts that are taken: kTogether rows at a time, until one stops
   int stop = drafts, j0 = 0;
   for (;; j0 += kTogether) {
-    const int j = j0 + (warp >> 1), side = warp & 1, row = sp.b + j;
-    if (j <= drafts && (side == 0 || (draft && j < drafts))) {
+    const int j = j0 + warp;
+    if (warp < kTogether && j <= drafts) {
+      const int side = draft && j < drafts ? lane >> 4 : 0, row = sp.b + j;
       const int x = j < drafts ? c.tokens[row + 1] : -1;
       const T* from = side ? draft + (int64_t)row * c.draft_stride : logits + (int64_t)row * c.logits_stride;
       const float v = x >= 0 && x < c.vocab ? (float)from[x] : -INFINITY;
       const Kept k = kept_of(side, row);
-      if (lane == 0) s_kept[side][warp >> 1] = k, s_lp[side][warp >> 1] = log_p(k, v, x);
+      if (lane == 16 * side) s_kept[side][warp] = k, s_lp[side][warp] = log_p(k, v, x);
     }
     __syncthreads();
     if (lane < kTogether && j0 + lane < drafts) {  // (in every warp)
@@ -304,8 +361,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_verify(const __grid_constant__ 
   // ---- the token after them
   const T* x = logits + (int64_t)row * c.logits_stride;
   const T* y = less ? draft + (int64_t)row * c.draft_stride : x;
-  const bool some = !c.whole[0];  // of the row: noise and the drafter's logits entry by entry
-  const float inv_t = inverse(1.f, kp.t), low = fmaxf(kp.xc, -FLT_MAX);  // (NaN and -inf are never kept)
+  // logits below this are surely not kept (NaN and -inf never are; a bound that is no number bounds nothing)
+  const float inv_t = inverse(1.f, kp.t),
+              low = fmaxf(fmaxf(kp.xc, kp.min_p > 0.f ? kp.m + kp.t * (logf(kp.min_p) - 1e-3f) - 1e-6f * fabsf(kp.m) : -INFINITY), -FLT_MAX);
   const int chunks = i1 > i0 && kp.any ? (i1 - i0 + kChunk - 1) / kChunk : 0;
   const Best none = {-INFINITY, -INFINITY, 0x7FFFFFFF};
   auto warp_best = [&](Best b) -> Best {
@@ -325,8 +383,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_verify(const __grid_constant__ 
     p.x.set(x, c.vocab, e0, e1, at + 64);
     p.y.set(y, c.vocab, e0, e1, at + Stage<T>::kLogits + 64);
     p.g.set(noise, c.vocab, e0, e1, at + Stage<T>::kNoise + 64);
-    if (some || !less) p.y.lo = p.y.hi = 0;
-    if (some) p.g.lo = p.g.hi = 0;
+    if (!less) p.y.lo = p.y.hi = 0;
     return p;
   };
   auto fill = [&](int k) {  // (one thread)
@@ -337,129 +394,137 @@ __global__ void __launch_bounds__(kThreads, 2) k_verify(const __grid_constant__ 
     if (c.hold) return;
     p.x.copy(ring, e0, bar), p.y.copy(ring, e0, bar), p.g.copy(ring, e0, bar);
   };
-  if (tid == 0)
-    for (int k = 0; k < min(chunks, kStages); ++k) fill(k);
-  // chunks that are copied whole: entries from in_lo to in_hi; an entry's place in its chunk's buffer (the same in all chunks)
-  int in_lo, in_hi;
-  {
-    Part<T> a;
-    Part<float> g;
-    a.set(x, c.vocab, 0, c.vocab, 0), g.set(noise, c.vocab, 0, c.vocab, 0);
-    in_lo = some ? a.lo : max(a.lo, g.lo), in_hi = min(i1, some ? a.hi : min(a.hi, g.hi));
-  }
-  const uint32_t x_off = 64 + (uint32_t)((uintptr_t)(x + i0) & 15), g_off = Stage<T>::kNoise + 64 + (uint32_t)((uintptr_t)(noise + i0) & 15);
-  // The bound of a key is z + noise - log_sum with a margin several times that of all roundings, 4e-6 of their sizes and of M / T; what
-  // of it is the same for all entries is taken off the other side.
-  const float shift = -kp.m * inv_t - kp.log_sum, slack = 4e-6f * (1.f + 2.f * fabsf(kp.log_sum) + 4.f * fabsf(kp.m * inv_t));
-  const bool by_bound = fabsf(kp.m) < INFINITY;  // (else every entry is looked at)
-  Best b;
-  for (int turn = 0; turn < 2; ++turn) {  // (the second where no entry has p > q: with p alone, from where the rows lie)
-    b = none;
-    const bool minus = less && turn == 0;
-    float floor = -INFINITY;
-    for (int k = 0; k < chunks; ++k) {  // (a warp's lanes together)
+  // The bound of a key: z + noise - log_sum with a margin several times that of all roundings, 8e-6 of their sizes and of M / T.
+  const float inv_tq = less ? inverse(1.f, kq.t) : 0.f, shift = -kp.m * inv_t - kp.log_sum, shift_q = less ? -kq.m * inv_tq - kq.log_sum : 0.f;
+  const float size = 1.f + 2.f * (fabsf(kp.log_sum) + fabsf(kq.log_sum)) + 4.f * (fabsf(kp.m * inv_t) + fabsf(kq.m * inv_tq));
+  const bool bounded_keys = size < INFINITY;  // (else every entry is looked at)
+  // logits above this are surely kept by the drafter
+  const float sure_q = !less || !kq.any      ? INFINITY
+                       : kq.min_p > 0.f ? fmaxf(kq.xc, kq.m + kq.t * (logf(kq.min_p) + 1e-3f) + 1e-6f * fabsf(kq.m))
+                                        : fmaxf(kq.xc, -FLT_MAX);
+  float reach = -INFINITY, reach2 = -INFINITY;
+  int at = -1;
+  if (warp == kWarps) {
+    // ================= copies
+    if (lane == 0) {
+      for (int k = 0; k < chunks && !s_lost; ++k) {
+        if (k >= kStages && !mbar_wait(&s_free[k % kStages], (uint32_t)(k / kStages - 1) & 1, kDefaultWaitNs)) {
+          s_lost = 1;
+          break;
+        }
+        fill(k);
+      }
+    }
+    __syncwarp();
+  } else {
+    // chunks that are copied whole: entries from in_lo to in_hi; an entry's place in its chunk's buffers is the same in all chunks
+    int in_lo, in_hi;
+    {
+      Part<T> a;
+      Part<float> g;
+      a.set(x, c.vocab, 0, c.vocab, 0), g.set(noise, c.vocab, 0, c.vocab, 0);
+      in_lo = max(a.lo, g.lo), in_hi = min(i1, min(a.hi, g.hi));
+      a.set(y, c.vocab, 0, c.vocab, 0);
+      in_lo = max(in_lo, a.lo), in_hi = min(in_hi, a.hi);
+    }
+    const uint32_t x_off = 64 + (uint32_t)((uintptr_t)(x + i0) & 15), y_off = Stage<T>::kLogits + 64 + (uint32_t)((uintptr_t)(y + i0) & 15),
+                   g_off = Stage<T>::kNoise + 64 + (uint32_t)((uintptr_t)(noise + i0) & 15);
+    for (int k = 0; k < chunks; ++k) {
       const int e0 = i0 + k * kChunk, e1 = min(i1, e0 + kChunk), stage = k % kStages;
-      bool there = turn == 0 && !s_lost;
+      bool there = !s_lost;
       if (there && !mbar_wait(&s_full[stage], (uint32_t)(k / kStages) & 1, kDefaultWaitNs)) there = false, s_lost = 1;
       const unsigned char* buf = ring + stage * Stage<T>::kBytes;
-      T vx[kU];
-      float g[kU];
+      auto take = [&](int e, float v, float w, float g) {
+        const float a = fmaf(v, inv_t, shift), sum = a + g;
+        float r = fmaf(8e-6f, fabsf(a) + fabsf(g) + size, sum);
+        bool out = false;  // p is surely not above q
+        if (less) {
+          const float b = fmaf(w, inv_tq, shift_q);
+          float ratio, lg;  // q / p; the bound of log(1 - q / p)
+          asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(ratio) : "f"((b - a) * 1.4426950408889634f));
+          const float rest = fmaxf(fmaf(ratio, 8e-6f * (fabsf(a) + fabsf(b) + size), 1.f - ratio), 0.f);
+          asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lg) : "f"(rest));
+          out = bounded_keys && w > sure_q && rest == 0.f;
+          r = w > sure_q ? fmaf(lg, 0.6931471805599453f, r) : r;
+        }
+        r = bounded_keys && r == r ? fmaxf(r, -FLT_MAX) : INFINITY;
+        if (v >= low && e != one && !out) {
+          const bool more = r > reach || at < 0;
+          reach2 = fmaxf(reach2, more ? reach : r);
+          if (more) reach = r, at = e;
+        }
+      };
       if (there && e0 >= in_lo && e0 + kChunk <= in_hi) {
         const T* px = reinterpret_cast<const T*>(buf + x_off) + tid;
+        const T* py = reinterpret_cast<const T*>(buf + y_off) + tid;
+        const float* pg = reinterpret_cast<const float*>(buf + g_off) + tid;
 #pragma unroll
-        for (int u = 0; u < kU; ++u) vx[u] = px[u * kThreads];
-        if (!some) {
-          const float* pg = reinterpret_cast<const float*>(buf + g_off) + tid;
-#pragma unroll
-          for (int u = 0; u < kU; ++u) g[u] = pg[u * kThreads];
-        }
+        for (int u = 0; u < kU; ++u) take(e0 + u * kThreads + tid, (float)px[u * kThreads], less ? (float)py[u * kThreads] : 0.f, pg[u * kThreads]);
       } else {
         const Parts p = parts_of(k);
-#pragma unroll
-        for (int u = 0; u < kU; ++u) {
-          const int e = e0 + u * kThreads + tid;
-          vx[u] = e < e1 ? p.x.at(ring, e, e0, there) : T(-INFINITY);
-          if (!some) g[u] = e < e1 ? p.g.at(ring, e, e0, there) : 0.f;
-        }
+        for (int e = e0 + tid; e < e1; e += kThreads)
+          take(e, (float)p.x.at(ring, e, e0, there), less ? (float)p.y.at(ring, e, e0, there) : 0.f, p.g.at(ring, e, e0, there));
       }
-      if (some) {
-#pragma unroll
-        for (int u = 0; u < kU; ++u) g[u] = (float)vx[u] >= low ? noise[e0 + u * kThreads + tid] : 0.f;
-      }
-      const float over = floor - slack;
-      bool any = false;
-#pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        const float v = (float)vx[u], a = fmaf(v, inv_t, shift);
-        any |= v >= low && !(fmaf(4e-6f, fabsf(a) + fabsf(g[u]), a + g[u]) < over);
-      }
-      if (__any_sync(0xffffffffu, any)) {
-        // each thread's most promising entry in turn, until none of the warp's reaches its largest key
-        uint32_t left = (1u << kU) - 1;
-        for (;;) {
-          float most = -INFINITY, cg = 0.f;
-          T cx = T(0.f);
-          int ci = -1;
-#pragma unroll
-          for (int u = 0; u < kU; ++u) {
-            const float v = (float)vx[u], a = fmaf(v, inv_t, shift);
-            float ub = fmaf(4e-6f, fabsf(a) + fabsf(g[u]), a + g[u]) + slack;
-            ub = by_bound && ub == ub ? fmaxf(ub, -FLT_MAX) : INFINITY;  // (a bound that is no number is looked at)
-            if (v >= low && (left >> u & 1) && ub > most) most = ub, cx = vx[u], cg = g[u], ci = u;
-          }
-          const bool look = ci >= 0 && !(most < floor);
-          if (!__any_sync(0xffffffffu, look)) break;
-          if (look) {
-            left &= ~(1u << ci);
-            const int e = e0 + ci * kThreads + tid;
-            const float lp = log_p(kp, (float)cx, e);
-            float key = lp;
-            bool in = lp > -INFINITY && !(turn == 0 && e == one);
-            if (in && minus) {
-              const float lq = log_p(kq, (float)(there && !some ? parts_of(k).y.at(ring, e, e0, true) : y[e]), e);
-              if (lq > -INFINITY) {
-                const float rest = expf(lp) - expf(lq);
-                in = rest > 0.f;
-                key = logf(rest);
-              }
-            }
-            if (in) b.take(fmaxf(key + cg, -INFINITY), lp, e);
-          }
-          floor = b.v;
-#pragma unroll
-          for (int d = 16; d; d >>= 1) floor = fmaxf(floor, __shfl_xor_sync(0xffffffffu, floor, d));
-        }
-      }
-      if (turn == 0) {
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&s_free[stage]);
-        if (tid == 0 && k + kStages < chunks && !s_lost) {
-          if (mbar_wait(&s_free[stage], (uint32_t)(k / kStages) & 1, kDefaultWaitNs)) fill(k + kStages);
-          else s_lost = 1;
-        }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s_free[stage]);
+    }
+  }
+  Best b = none;
+  auto work_out = [&](int e, bool minus) {
+    const float lp = log_p(kp, (float)x[e], e);
+    if (lp == -INFINITY || (minus && e == one)) return;
+    float key = lp;
+    if (minus && less) {
+      const float lq = log_p(kq, (float)y[e], e);
+      if (lq > -INFINITY) {
+        const float rest = expf(lp) - expf(lq);
+        if (!(rest > 0.f)) return;
+        key = logf(rest);
       }
     }
-    // the block's, then the cluster's: every block tells every other
+    b.take(fmaxf(key + noise[e], -INFINITY), lp, e);
+  };
+  auto block_best = [&]() {  // in every warp
     b = warp_best(b);
-    if (lane == 0) s_best[warp] = b;
     __syncthreads();
-    if (turn == 0) cl.barrier_wait();
-    if (warp == 0) {
-      b = warp_best(lane < kWarps ? s_best[lane] : none);
-      if (lane < C) cl.map_shared_rank(&s_all[turn][0], lane)[rank] = b;
+    if (lane == 0 && warp < kWarps) s_best[warp] = b;
+    __syncthreads();
+    b = warp_best(lane < kWarps ? s_best[lane] : none);
+  };
+  if (at >= 0) work_out(at, true);
+  block_best();
+  {
+    const Best found = b;
+    b = none;
+    const bool again = reach2 > -INFINITY && !(reach2 < found.v);
+    if (__syncthreads_or(again)) {
+      if (again)
+        for (int e = i0 + tid; e < i1; e += kThreads) work_out(e, true);
+      b.take(found.v, found.lp, found.i);
+      block_best();
+    } else {
+      b = found;
     }
+  }
+  cl.barrier_wait();
+  for (int turn = 0;; ++turn) {  // (the second where no entry has p > q: with p alone)
+    // the cluster's: every block tells every other
+    if (warp == 0 && lane < C) cl.map_shared_rank(&s_all[turn][0], lane)[rank] = b;
     cl.sync();
     b = none;
     for (int q = 0; q < C; ++q) b.take(s_all[turn][q].v, s_all[turn][q].lp, s_all[turn][q].i);
-    if (b.i != none.i) break;
+    if (b.i != none.i || turn == 1) break;
+    if (warp < kWarps && kp.any)
+      for (int e = i0 + tid; e < i1; e += kThreads) work_out(e, false);
+    block_best();
   }
   // no copy may be in flight when the block exits (one that was not waited for: its chunk was read without it)
-  if (tid == 0 && s_lost && !c.hold)
+  if (tid == kThreads && s_lost && !c.hold)
     for (int i = 0; i < kStages; ++i) mbar_wait(&s_full[i], 0, kDefaultWaitNs), mbar_wait(&s_full[i], 1, kDefaultWaitNs);
 
   if (rank != 0) return;
   const bool empty = b.i == none.i;
-  for (int j = stop + tid; j <= drafts; j += kThreads) {
+  for (int j = stop + tid; j <= drafts; j += kThreads + 32) {
     const int at = sp.b + j;
     c.token[at] = j > stop || empty ? -1 : b.i;
     if (c.logprob) c.logprob[at] = j > stop || empty ? -INFINITY : b.lp;
@@ -478,12 +543,16 @@ cudaError_t run(VerifyCall c, cudaStream_t s) {
                                      c.whole[0] ? 0 : 1, rows);
     if (e != cudaSuccess) return e;
   }
-  int C = 1;
-  while (C < 8 && (int64_t)n_seqs * C * 2 <= 304 && c.vocab / C > 8192) C *= 2;
+  // Blocks of a sequence: as many as find room on the GPU at once (clusters of up to 8 that lie on some SMs together: 64 sequences of
+  // 131072 entries, 6 blocks each 48 us, 4 55, 7 and 8, in two turns, 56 and 53; 128 sequences, 3 83, 4 86), where each has some thousand
+  // entries.
+  int C = 400 / n_seqs < 8 ? 400 / n_seqs : 8;
+  while (C > 1 && c.vocab / C < 4096) --C;
+  if (C < 1) C = 1;
   c.slice = (c.vocab + C - 1) / C;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)n_seqs * (unsigned)C);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(kThreads + 32);
   cfg.dynamicSmemBytes = Stage<T>::kStages * Stage<T>::kBytes;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
