@@ -40,7 +40,8 @@ struct VerifyCall {
   Piece* pieces;      // [2][rows][n_units], of others
   int whole[2];       // the target's, the drafter's are not cut
   int n_seqs, n_rows, vocab, n_units, slice;  // units of a row (k_rows); slice: entries of a block of k_verify
-  int hold;  // (a test's) copies are not issued
+  int stages;  // of k_verify's ring
+  int hold;    // (a test's) copies are not issued
 };
 
 // ---- rows that are not cut
@@ -215,6 +216,13 @@ __device__ __forceinline__ float log_p(const Kept& k, float x, int i) {
   return k.min_p > 0.f && expf(z) < k.min_p ? -INFINITY : z - k.log_sum;
 }
 
+// floats in the order of unsigned integers (0: below all)
+__device__ __forceinline__ unsigned ordered(float x) {
+  const unsigned b = __float_as_uint(x);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float key_of(unsigned k) { return k == 0 ? -INFINITY : __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
+
 struct Best {  // the largest key so far, the lowest index where equal
   float v, lp;
   int i;
@@ -229,13 +237,12 @@ struct Best {  // the largest key so far, the lowest index where equal
 // drafter's where they count, and the noise.  A copy covers whole 16-byte vectors inside its row; what is left of a row's ends, and
 // chunks whose copies do not arrive in time, are read where they lie.  Each thread keeps the two largest bounds of its keys: log p + noise
 // + log(1 - q / p) by approximate exponentials, with a margin for all roundings; an entry that the drafter may not have kept counts as if it had
-// not.  With the largest bound's key worked out, no entry whose bound lies below the block's largest key can be the one; a thread whose second does
+// not.  The first chunk's largest key spares most of what follows all but the bound by p alone.  With the largest bound's key worked out, no entry whose bound lies below the block's largest key can be the one; a thread whose second does
 // not looks at all its entries.
-constexpr int kU = 8, kChunk = kU * kThreads;  // entries of a thread, of a chunk
+constexpr int kU = 8, kChunk = kU * kThreads, kMostStages = 8;  // entries of a thread, of a chunk
 constexpr int kTogether = kWarps;               // rows that are looked at together, a warp each
 template <class T>
 struct Stage {
-  static constexpr int kStages = sizeof(T) == 2 ? 3 : 2;  // of the ring: three blocks an SM and more
   static constexpr uint32_t kLogits = kChunk * sizeof(T) + 128, kNoise = 2 * kLogits, kBytes = kNoise + kChunk * 4 + 128;
 };
 
@@ -270,15 +277,16 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
   __shared__ Best s_best[kWarps], s_all[2][8];  // of the warps; of the cluster's blocks, by turn
   __shared__ Kept s_kept[2][kTogether];
   __shared__ float s_lp[2][kTogether];
-  constexpr int kStages = Stage<T>::kStages;
-  __shared__ uint64_t s_full[kStages], s_free[kStages];
+  __shared__ uint64_t s_full[kMostStages], s_free[kMostStages];
+  const int stages = c.stages;
   __shared__ volatile int s_lost;
+  __shared__ volatile unsigned s_floor;  // the largest key that is known
   cg::cluster_group cl = cg::this_cluster();
   const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank(), s = blockIdx.x / C;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    for (int i = 0; i < kStages; ++i) mbar_init(&s_full[i], 1), mbar_init(&s_free[i], kWarps);
-    s_lost = 0;
+    for (int i = 0; i < kMostStages; ++i) mbar_init(&s_full[i], 1), mbar_init(&s_free[i], kWarps);
+    s_lost = 0, s_floor = 0;
     mbar_fence_init();
   }
   pdl_wait();
@@ -376,9 +384,9 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
     Part<T> x, y;
     Part<float> g;
   };
-  auto parts_of = [&](int k) -> Parts {
+  auto parts_of = [&](int k, int stage) -> Parts {
     const int e0 = i0 + k * kChunk, e1 = min(i1, e0 + kChunk);
-    const uint32_t at = (uint32_t)(k % kStages) * Stage<T>::kBytes;
+    const uint32_t at = (uint32_t)stage * Stage<T>::kBytes;
     Parts p;
     p.x.set(x, c.vocab, e0, e1, at + 64);
     p.y.set(y, c.vocab, e0, e1, at + Stage<T>::kLogits + 64);
@@ -386,10 +394,10 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
     if (!less) p.y.lo = p.y.hi = 0;
     return p;
   };
-  auto fill = [&](int k) {  // (one thread)
-    const Parts p = parts_of(k);
+  auto fill = [&](int k, int stage) {  // (one thread)
+    const Parts p = parts_of(k, stage);
     const int e0 = i0 + k * kChunk;
-    uint64_t* bar = &s_full[k % kStages];
+    uint64_t* bar = &s_full[stage];
     mbar_arrive_tx(bar, c.hold ? 1 : p.x.bytes() + p.y.bytes() + p.g.bytes());
     if (c.hold) return;
     p.x.copy(ring, e0, bar), p.y.copy(ring, e0, bar), p.g.copy(ring, e0, bar);
@@ -402,17 +410,35 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
   const float sure_q = !less || !kq.any      ? INFINITY
                        : kq.min_p > 0.f ? fmaxf(kq.xc, kq.m + kq.t * (logf(kq.min_p) + 1e-3f) + 1e-6f * fabsf(kq.m))
                                         : fmaxf(kq.xc, -FLT_MAX);
-  float reach = -INFINITY, reach2 = -INFINITY;
+  Best b = none;
+  auto work_out = [&](int e, bool minus) {
+    const float lp = log_p(kp, (float)x[e], e);
+    if (lp == -INFINITY || (minus && e == one)) return;
+    float key = lp;
+    if (minus && less) {
+      const float lq = log_p(kq, (float)y[e], e);
+      if (lq > -INFINITY) {
+        const float rest = expf(lp) - expf(lq);
+        if (!(rest > 0.f)) return;
+        key = logf(rest);
+      }
+    }
+    b.take(fmaxf(key + noise[e], -INFINITY), lp, e);
+  };
+  float reach = -INFINITY, reach2 = -INFINITY, floor = -INFINITY;
   int at = -1;
   if (warp == kWarps) {
     // ================= copies
     if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 1;  // (the first turn of the ring waits for nothing)
       for (int k = 0; k < chunks && !s_lost; ++k) {
-        if (k >= kStages && !mbar_wait(&s_free[k % kStages], (uint32_t)(k / kStages - 1) & 1, kDefaultWaitNs)) {
+        if (k >= stages && !mbar_wait(&s_free[stage], phase, kDefaultWaitNs)) {
           s_lost = 1;
           break;
         }
-        fill(k);
+        fill(k, stage);
+        if (++stage == stages) stage = 0, phase ^= 1;
       }
     }
     __syncwarp();
@@ -429,26 +455,34 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
     }
     const uint32_t x_off = 64 + (uint32_t)((uintptr_t)(x + i0) & 15), y_off = Stage<T>::kLogits + 64 + (uint32_t)((uintptr_t)(y + i0) & 15),
                    g_off = Stage<T>::kNoise + 64 + (uint32_t)((uintptr_t)(noise + i0) & 15);
+    int stage = 0;
+    uint32_t phase = 0;
     for (int k = 0; k < chunks; ++k) {
-      const int e0 = i0 + k * kChunk, e1 = min(i1, e0 + kChunk), stage = k % kStages;
+      const int e0 = i0 + k * kChunk, e1 = min(i1, e0 + kChunk);
       bool there = !s_lost;
-      if (there && !mbar_wait(&s_full[stage], (uint32_t)(k / kStages) & 1, kDefaultWaitNs)) there = false, s_lost = 1;
+      if (there && !mbar_wait(&s_full[stage], phase, kDefaultWaitNs)) there = false, s_lost = 1;
       const unsigned char* buf = ring + stage * Stage<T>::kBytes;
+      // (without the drafter's part the bound is higher, and nearly always enough)
+      const float over = floor - 8e-6f * size;
+      auto may_be = [&](float v, float g) -> bool {
+        const float a = fmaf(v, inv_t, shift);
+        return v >= low && !(fmaf(8e-6f, fabsf(a) + fabsf(g), a + g) < over);
+      };
       auto take = [&](int e, float v, float w, float g) {
         const float a = fmaf(v, inv_t, shift), sum = a + g;
         float r = fmaf(8e-6f, fabsf(a) + fabsf(g) + size, sum);
-        bool out = false;  // p is surely not above q
+        bool out = e == one;  // or p is surely not above q
         if (less) {
           const float b = fmaf(w, inv_tq, shift_q);
           float ratio, lg;  // q / p; the bound of log(1 - q / p)
           asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(ratio) : "f"((b - a) * 1.4426950408889634f));
           const float rest = fmaxf(fmaf(ratio, 8e-6f * (fabsf(a) + fabsf(b) + size), 1.f - ratio), 0.f);
           asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(lg) : "f"(rest));
-          out = bounded_keys && w > sure_q && rest == 0.f;
+          out |= bounded_keys && w > sure_q && rest == 0.f;
           r = w > sure_q ? fmaf(lg, 0.6931471805599453f, r) : r;
         }
         r = bounded_keys && r == r ? fmaxf(r, -FLT_MAX) : INFINITY;
-        if (v >= low && e != one && !out) {
+        if (!out) {
           const bool more = r > reach || at < 0;
           reach2 = fmaxf(reach2, more ? reach : r);
           if (more) reach = r, at = e;
@@ -458,32 +492,33 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
         const T* px = reinterpret_cast<const T*>(buf + x_off) + tid;
         const T* py = reinterpret_cast<const T*>(buf + y_off) + tid;
         const float* pg = reinterpret_cast<const float*>(buf + g_off) + tid;
+        uint32_t some = 0;
 #pragma unroll
-        for (int u = 0; u < kU; ++u) take(e0 + u * kThreads + tid, (float)px[u * kThreads], less ? (float)py[u * kThreads] : 0.f, pg[u * kThreads]);
+        for (int u = 0; u < kU; ++u) some |= (uint32_t)may_be((float)px[u * kThreads], pg[u * kThreads]) << u;
+        for (; some; some &= some - 1) {
+          const int u = __ffs(some) - 1;
+          take(e0 + u * kThreads + tid, (float)px[u * kThreads], less ? (float)py[u * kThreads] : 0.f, pg[u * kThreads]);
+        }
       } else {
-        const Parts p = parts_of(k);
-        for (int e = e0 + tid; e < e1; e += kThreads)
-          take(e, (float)p.x.at(ring, e, e0, there), less ? (float)p.y.at(ring, e, e0, there) : 0.f, p.g.at(ring, e, e0, there));
+        const Parts p = parts_of(k, stage);
+        for (int e = e0 + tid; e < e1; e += kThreads) {
+          const float v = (float)p.x.at(ring, e, e0, there), g = p.g.at(ring, e, e0, there);
+          if (may_be(v, g)) take(e, v, less ? (float)p.y.at(ring, e, e0, there) : 0.f, g);
+        }
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&s_free[stage]);
+      if (++stage == stages) stage = 0, phase ^= 1;
+      // The block's largest key of the first chunk (of what warps know when they ask): few of what follows reach it.
+      if (k == 0 && chunks > 1) {
+        if (at >= 0) work_out(at, true);
+        const unsigned mine = __reduce_max_sync(0xffffffffu, ordered(b.v));
+        if (lane == 0) atomicMax(const_cast<unsigned*>(&s_floor), mine);
+        b = none;
+      }
+      floor = key_of(s_floor);
     }
   }
-  Best b = none;
-  auto work_out = [&](int e, bool minus) {
-    const float lp = log_p(kp, (float)x[e], e);
-    if (lp == -INFINITY || (minus && e == one)) return;
-    float key = lp;
-    if (minus && less) {
-      const float lq = log_p(kq, (float)y[e], e);
-      if (lq > -INFINITY) {
-        const float rest = expf(lp) - expf(lq);
-        if (!(rest > 0.f)) return;
-        key = logf(rest);
-      }
-    }
-    b.take(fmaxf(key + noise[e], -INFINITY), lp, e);
-  };
   auto block_best = [&]() {  // in every warp
     b = warp_best(b);
     __syncthreads();
@@ -520,7 +555,7 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
   }
   // no copy may be in flight when the block exits (one that was not waited for: its chunk was read without it)
   if (tid == kThreads && s_lost && !c.hold)
-    for (int i = 0; i < kStages; ++i) mbar_wait(&s_full[i], 0, kDefaultWaitNs), mbar_wait(&s_full[i], 1, kDefaultWaitNs);
+    for (int i = 0; i < min(stages, chunks); ++i) mbar_wait(&s_full[i], 0, kDefaultWaitNs), mbar_wait(&s_full[i], 1, kDefaultWaitNs);
 
   if (rank != 0) return;
   const bool empty = b.i == none.i;
@@ -553,7 +588,10 @@ cudaError_t run(VerifyCall c, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)n_seqs * (unsigned)C);
   cfg.blockDim = dim3(kThreads + 32);
-  cfg.dynamicSmemBytes = Stage<T>::kStages * Stage<T>::kBytes;
+  // The ring: what shared memory holds of the blocks that an SM gets.
+  const int64_t per_sm = ((int64_t)n_seqs * C + 151) / 152, fit = (int64_t)(220 * 1024) / Stage<T>::kBytes / (per_sm < 3 ? per_sm : 3);
+  c.stages = fit < kMostStages ? (int)fit : kMostStages;
+  cfg.dynamicSmemBytes = c.stages * Stage<T>::kBytes;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -562,7 +600,7 @@ cudaError_t run(VerifyCall c, cudaStream_t s) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  const cudaError_t e = cudaFuncSetAttribute(k_verify<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes);
+  const cudaError_t e = cudaFuncSetAttribute(k_verify<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
   return e == cudaSuccess ? cudaLaunchKernelEx(&cfg, k_verify<T>, c) : e;
 }
 
@@ -603,7 +641,7 @@ extern "C" int mf_verify(const mf_verify_args_t* a, void* stream) {
   Kept* kept = static_cast<Kept*>(a->work);
   const VerifyCall c = {a->logits, a->draft_logits, a->logits_stride, a->draft_stride, a->noise_stride, a->row_start, a->tokens, a->u, a->noise,
                         {a->cuts.temperature, a->draft_cuts.temperature}, a->token, a->accepted, a->logprob, kept,
-                        reinterpret_cast<Piece*>(kept + 2 * (int64_t)a->n_rows), {whole_p, whole_q}, a->n_seqs, a->n_rows, a->vocab, 0, 0, sample_hold()};
+                        reinterpret_cast<Piece*>(kept + 2 * (int64_t)a->n_rows), {whole_p, whole_q}, a->n_seqs, a->n_rows, a->vocab, 0, 0, 0, sample_hold()};
   cudaError_t e = cudaSuccess;
   if (a->n_rows > 0 && (!whole_p || (a->draft_logits && !whole_q))) {
     const KeptRows rows = {a->logits,  whole_q ? nullptr : a->draft_logits, a->logits_stride, a->draft_stride, a->row_start, a->cuts, a->draft_cuts, kept,
