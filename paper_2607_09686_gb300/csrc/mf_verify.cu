@@ -289,9 +289,11 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
     s_lost = 0, s_floor = 0;
     mbar_fence_init();
   }
-  pdl_wait();
+  // The kernels before this one let it start when what comes before them is done: the call's inputs may be read, what they find not yet.
+  if (c.n_rows == 0) pdl_wait();  // (there are none)
   const RowSpan sp = row_span(c.row_start, c.n_rows, s);
   if (sp.b == sp.e) {
+    pdl_wait();
     if (rank == 0 && tid == 0) c.accepted[s] = 0;
     return;
   }
@@ -305,6 +307,15 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
     const uintptr_t a = ((uintptr_t)(noise + i0) + 15) & ~uintptr_t(15), e = (uintptr_t)(noise + i1) & ~uintptr_t(15);
     if (e > a) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a), "r"((uint32_t)(e - a)) : "memory");
   }
+  // the drafts of the first kTogether rows, and their logits
+  const int my_side = draft && warp < drafts ? lane >> 4 : 0;
+  const int my_x = warp < min(kTogether, drafts) ? c.tokens[sp.b + warp + 1] : -1;
+  auto logit_of = [&](int side, int row, int x) -> float {
+    const T* from = side ? draft + (int64_t)row * c.draft_stride : logits + (int64_t)row * c.logits_stride;
+    return x >= 0 && x < c.vocab ? (float)from[x] : -INFINITY;
+  };
+  const float my_v = logit_of(my_side, sp.b + warp, my_x);
+  pdl_wait();
   // what a row keeps, in 16 lanes of the target's and 16 of the drafter's, all lanes together (ordinary loads: read-only ones may be moved
   // ahead of the wait)
   auto kept_of = [&](int side, int row) -> Kept {
@@ -342,9 +353,8 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
     const int j = j0 + warp;
     if (warp < kTogether && j <= drafts) {
       const int side = draft && j < drafts ? lane >> 4 : 0, row = sp.b + j;
-      const int x = j < drafts ? c.tokens[row + 1] : -1;
-      const T* from = side ? draft + (int64_t)row * c.draft_stride : logits + (int64_t)row * c.logits_stride;
-      const float v = x >= 0 && x < c.vocab ? (float)from[x] : -INFINITY;
+      const int x = j0 == 0 ? my_x : j < drafts ? c.tokens[row + 1] : -1;
+      const float v = j0 == 0 ? my_v : logit_of(side, row, x);
       const Kept k = kept_of(side, row);
       if (lane == 16 * side) s_kept[side][warp] = k, s_lp[side][warp] = log_p(k, v, x);
     }
