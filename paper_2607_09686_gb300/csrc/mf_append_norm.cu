@@ -3,204 +3,199 @@
 //
 // Everything is read and written once: a copy, bounded by memory (few tokens: by its launch and a chain of look-ups).  A head's
 // 4, 8 or 16 lanes hold it whole, 16 elements each (two 16-byte vectors: the two halves of eight rotated pairs, or 16
-// neighbours when interleaved or not rotated), so that the mean is a few shuffles.  A row is 32 lanes' worth of a token's heads, 1 KiB; the
-// step's rows are one list, shared out evenly over all warps that find room.  A warp copies its rows ahead, kAhead of them under way, into shared
-// memory that each lane reads back itself, so nothing waits for another lane: 24 warps of 8 KiB an SM.  (Loads into registers, four rows a
-// warp and a warp for each four rows: 106 registers, 16 warps an SM, whose heads were under way for a third of their time; 8192 tokens of 40
-// heads of 128 49.6 us.)  At a new token a warp looks up where it goes, its sequence (the ends at or before it are counted), its
-// line and its page, and its lanes' angles: a lane has the same place in each of its heads.
+// neighbours when interleaved or not rotated), so that the mean is a few shuffles.  A block has kTB tokens, as in the append without norms: its
+// threads ask for their first vectors, then a warp a token looks up where it goes, the weights and the tokens' angles come into
+// shared memory, laid out as the lanes read them, and each thread takes two items at a time.  Arithmetic on pairs of floats (f32x2).
 #include "mf_attn.cuh"
+#include "mf_tc.cuh"
 
 namespace mf {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32, kAhead = 8;
-constexpr uint32_t kRowBytes = 1024;
+constexpr int kThreads = 256;
 
-template <class T, int D>
-__global__ void __launch_bounds__(kThreads, 3) k_append_norm(const __grid_constant__ AppendCall c, const __grid_constant__ AppendNorm n,
-                                                             int per_token) {
-  constexpr int kPer = D / 16, kHeads = 32 / kPer;  // lanes of a head, heads of a row
-  extern __shared__ __align__(128) unsigned char smem[];
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t neg2(uint64_t a) { return a ^ 0x8000000080000000ull; }
+
+template <class T, int D, int kTB>
+__global__ void __launch_bounds__(kThreads, 4) k_append_norm(const __grid_constant__ AppendCall c, const __grid_constant__ AppendNorm n) {
+  constexpr int kPer = D / 16;  // lanes of a head
   const AttnStep& st = c.st;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  // this warp's rows of the list, neighbouring runs on different SMs
-  const int64_t total = (int64_t)st.n_tokens * per_token, W = min((int64_t)gridDim.x * kWarps, total);
-  const int64_t w = (int64_t)warp * gridDim.x + blockIdx.x, f0 = w < W ? total * w / W : 0, f1 = w < W ? total * (w + 1) / W : 0;
+  __shared__ int64_t s_at[kTB];
+  __shared__ int s_line[kTB];  // the token's line; -1: not stored
+  __shared__ float4 s_angle[kTB][4][16];  // (cos, cos, sin, sin) of pairs 2u and 2u + 1 of a lane's eight, by u and lane
+  __shared__ float4 s_weight[2][4][16];   // four of a lane's 16 weights of q, of k, offset added
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, t0 = blockIdx.x * kTB, tokens = min(kTB, st.n_tokens - t0);
+  const int q_heads = c.q ? st.Hq : 0, n_items = (q_heads + 2 * st.Hkv) * kPer, total = tokens * n_items;
   pdl_wait();
-  if (f0 >= f1) return;
-  const int j = lane % kPer, q_heads = c.q ? st.Hq : 0, heads = q_heads + 2 * st.Hkv;
-  const bool turned = j * 8 < c.half, split = turned && !c.interleaved;
-  const int e0 = split ? j * 8 : j * 16, e1 = split ? e0 + c.half : e0 + 8;
-  unsigned char* mine = smem + warp * (kAhead * kRowBytes) + lane * 16;
-  const uint32_t mine_s = smem_u32(mine);
 
-  // ---- the copies' side
-  int rows = (int)(f1 - f0), lt = (int)(f0 / per_token), lr = (int)(f0 - (int64_t)lt * per_token), asked = 0;
-  auto ask = [&]() {  // the next row, if there is one; a group either way
-    const int head = lr * kHeads + lane / kPer;
-    if (asked < rows && head < heads) {
-      const bool is_q = head < q_heads, is_v = head >= q_heads + st.Hkv;
-      const T* src = is_q   ? static_cast<const T*>(c.q) + (int64_t)lt * c.q_stride + (int64_t)head * D
-                     : is_v ? static_cast<const T*>(c.v) + (int64_t)lt * c.v_stride + (int64_t)(head - q_heads - st.Hkv) * D
-                            : static_cast<const T*>(c.k) + (int64_t)lt * c.k_stride + (int64_t)(head - q_heads) * D;
-      const uint32_t dst = mine_s + (uint32_t)(asked % kAhead) * kRowBytes;
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src + e0) : "memory");
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + 512), "l"(src + e1) : "memory");
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    ++asked;
-    if (++lr == per_token) lr = 0, ++lt;
+  struct Item {
+    uint4 a, b;
+    int64_t at;          // element of the destination (a head of a cache line: from the line's beginning)
+    int e0, e1, k, j;    // elements of the two vectors; token, place in the head
+    int kind;            // 0: q, 1: k, 2: v, 3: none
   };
-#pragma unroll 1
-  for (int i = 0; i < kAhead; ++i) ask();
-
-  int t = (int)(f0 / per_token), r = (int)(f0 - (int64_t)t * per_token), line = -1;
-  int64_t at = 0;
-  float co[8], si[8];
-  bool fresh = true;
-#pragma unroll 1
-  for (int i = 0; i < rows; ++i) {
-    if (fresh) {
-      fresh = false;
-      // ---- the token's line and where that lies (every lane the same)
-      line = -1, at = 0;
-      int s = t;
-      if (st.q_start) {
-        s = 0;
-        for (int base = 0; base < st.n_seqs; base += 32) {
-          const int q = base + lane;
-          s += __popc(__ballot_sync(0xffffffffu, q < st.n_seqs && __ldg(st.q_start + q + 1) <= t));
-        }
-      }
-      if (s < st.n_seqs) {
-        const SeqSpan sp = seq_span(st, s);
-        const int x = sp.len - sp.n + t - sp.q0;
-        if (t >= sp.q0 && t < sp.q0 + sp.n && x >= 0) {
-          const int pi = (int)fast_div((uint32_t)x, st.page_mul, st.page_shift);
-          const int page = __ldg(st.pages + (int64_t)s * st.pages_per_seq + pi);
-          if (page >= 0 && page < st.n_pages) {
-            line = x;
-            at = (int64_t)page * st.page_stride + (int64_t)(x - pi * st.page_size) * st.token_stride;
-          }
-        }
-      }
-      if (line < 0 && lane == 0) attn_report(st, kAttnRange);
-      // ---- this lane's eight angles
-      if (turned) {
-        auto clamped = [&](int p) {
-          const int pc = min(max(p, 0), c.n_pos - 1);
-          if (pc != p) attn_report(st, kAttnRange);
-          return (int64_t)pc * c.half;
-        };
-        if (c.n_axes == 1) {
-          const int64_t row = clamped(c.pos ? __ldg(c.pos + t) : line) + j * 8;
-#pragma unroll
-          for (int u = 0; u < 8; u += 4) {
-            *reinterpret_cast<float4*>(co + u) = __ldg(reinterpret_cast<const float4*>(c.cos + row + u));
-            *reinterpret_cast<float4*>(si + u) = __ldg(reinterpret_cast<const float4*>(c.sin + row + u));
-          }
-        } else {
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const int pair = j * 8 + u, axis = (pair >= c.end0) + (pair >= c.end1) + (pair >= c.end2);
-            const int64_t row = clamped(__ldg(c.pos + (int64_t)axis * st.n_tokens + t));
-            co[u] = __ldg(c.cos + row + pair), si[u] = __ldg(c.sin + row + pair);
-          }
-        }
-      }
-    }
-    const int head = r * kHeads + lane / kPer;
-    const bool in = head < heads, is_q = head < q_heads, is_v = head >= q_heads + st.Hkv;
-    asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 1) : "memory");
-    const unsigned char* slot = mine + (i % kAhead) * kRowBytes;
-    const uint4 a = *reinterpret_cast<const uint4*>(slot), b = *reinterpret_cast<const uint4*>(slot + 512);
-    uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wb[4] = {b.x, b.y, b.z, b.w};
-    ask();
-    float x[8], y[8];
+  auto load = [&](int i, Item& it) {
+    it.kind = 3, it.a = it.b = make_uint4(0, 0, 0, 0), it.k = 0, it.j = i % kPer;
+    const bool split = it.j * 8 < c.half && !c.interleaved;
+    it.e0 = split ? it.j * 8 : it.j * 16, it.e1 = split ? it.e0 + c.half : it.e0 + 8;
+    if (i >= total) return;
+    const int k = kTB == 1 ? 0 : i / n_items, head = (i - k * n_items) / kPer;
+    it.k = k;
+    it.kind = head < q_heads ? 0 : head < q_heads + st.Hkv ? 1 : 2;
+    const int h = it.kind == 0 ? head : it.kind == 1 ? head - q_heads : head - q_heads - st.Hkv;
+    const T* src = static_cast<const T*>(it.kind == 0 ? c.q : it.kind == 1 ? c.k : c.v) +
+                   (int64_t)(t0 + k) * (it.kind == 0 ? c.q_stride : it.kind == 1 ? c.k_stride : c.v_stride) + h * D;
+    it.at = it.kind == 0 ? (int64_t)(t0 + k) * c.q_out_stride + h * D : (int64_t)h * st.head_stride;
+    it.a = *reinterpret_cast<const uint4*>(src + it.e0), it.b = *reinterpret_cast<const uint4*>(src + it.e1);
+  };
+  auto store = [&](Item& it) {  // (every lane of the warp)
+    uint32_t wa[4] = {it.a.x, it.a.y, it.a.z, it.a.w}, wb[4] = {it.b.x, it.b.y, it.b.z, it.b.w};
+    const bool normed = it.kind == 0 ? n.q_weight != nullptr : it.kind == 1 && n.k_weight, turn = it.kind < 2 && it.j * 8 < c.half;
+    uint64_t x[4], y[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const float2 p = Half2<T>::up(in ? wa[u] : 0u), q = Half2<T>::up(in ? wb[u] : 0u);
-      x[2 * u] = p.x, x[2 * u + 1] = p.y, y[2 * u] = q.x, y[2 * u + 1] = q.y;
+      const float2 f = Half2<T>::up(wa[u]), g = Half2<T>::up(wb[u]);
+      x[u] = tc::pack2(f.x, f.y), y[u] = tc::pack2(g.x, g.y);
     }
-    const void* weight = is_q ? n.q_weight : n.k_weight;
-    const bool normed = in && !is_v && weight;
     // the sum of squares in fp32 (a tree: its error is some 20 roundings'); where it passes the largest float the values are
     // taken times 2^-70, whose squares fit, and eps is nothing beside them
     auto sum_of = [&](float f) {
-      float ss = 0.f, s2 = 0.f;
+      const uint64_t f2 = tc::pack2(f, f);
+      uint64_t s0 = 0, s1 = 0;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) ss = fmaf(x[u] * f, x[u] * f, ss), s2 = fmaf(y[u] * f, y[u] * f, s2);
-      ss += s2;
+      for (int u = 0; u < 4; ++u) {
+        const uint64_t v = mul2(x[u], f2), z = mul2(y[u], f2);
+        s0 = tc::fma2(v, v, s0), s1 = tc::fma2(z, z, s1);
+      }
+      float lo, hi;
+      tc::unpack2(tc::add2(s0, s1), lo, hi);
+      float ss = lo + hi;
 #pragma unroll
       for (int d = 1; d < kPer; d <<= 1) ss += __shfl_xor_sync(0xffffffffu, ss, d);
       return ss;
     };
-    float ss = sum_of(1.f), rs = rsqrtf(ss * (1.f / D) + n.eps);
+    const float ss = sum_of(1.f);
+    float rs = rsqrtf(ss * (1.f / D) + n.eps);
     if (__any_sync(0xffffffffu, ss == INFINITY)) {
       const float big = sum_of(0x1p-70f);
       if (ss == INFINITY) rs = rsqrtf(big * (1.f / D)) * 0x1p-70f;
     }
+    if (it.kind == 3 || (it.kind > 0 && s_line[it.k] < 0)) return;
     if (normed) {
-      auto scaled = [&](float (&v)[8], int e) {
-        if (n.f32) {
-          const float* q = static_cast<const float*>(weight) + e;
+      const uint64_t rs2 = tc::pack2(rs, rs);
 #pragma unroll
-          for (int u = 0; u < 8; ++u) v[u] = v[u] * rs * (__ldg(q + u) + n.offset);
-        } else {
-          const uint4 q = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(weight) + e));
-          const uint32_t ws[4] = {q.x, q.y, q.z, q.w};
+      for (int u = 0; u < 2; ++u) {
+        const ulonglong2 p = *reinterpret_cast<const ulonglong2*>(&s_weight[it.kind][u][it.j]),
+                         q = *reinterpret_cast<const ulonglong2*>(&s_weight[it.kind][2 + u][it.j]);
+        x[2 * u] = mul2(mul2(x[2 * u], rs2), p.x), x[2 * u + 1] = mul2(mul2(x[2 * u + 1], rs2), p.y);
+        y[2 * u] = mul2(mul2(y[2 * u], rs2), q.x), y[2 * u + 1] = mul2(mul2(y[2 * u + 1], rs2), q.y);
+      }
+    }
+    if (turn && !c.interleaved) {  // (a, b): (a cos - b sin, b cos + a sin)
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const float2 f = Half2<T>::up(ws[u]);
-            v[2 * u] = v[2 * u] * rs * (f.x + n.offset), v[2 * u + 1] = v[2 * u + 1] * rs * (f.y + n.offset);
+      for (int u = 0; u < 4; ++u) {
+        const ulonglong2 cs = *reinterpret_cast<const ulonglong2*>(&s_angle[it.k][u][it.j]);
+        const uint64_t v = tc::fma2(x[u], cs.x, neg2(mul2(y[u], cs.y)));
+        y[u] = tc::fma2(y[u], cs.x, mul2(x[u], cs.y));
+        x[u] = v;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      float p0, p1, q0, q1;
+      tc::unpack2(x[u], p0, p1), tc::unpack2(y[u], q0, q1);
+      if (turn && c.interleaved) {  // each word is a pair
+        const float4 f = s_angle[it.k][u >> 1][it.j], g = s_angle[it.k][2 + (u >> 1)][it.j];
+        const float cp = u & 1 ? f.y : f.x, sp = u & 1 ? f.w : f.z, cq = u & 1 ? g.y : g.x, sq = u & 1 ? g.w : g.z;
+        const float v = p0 * cp - p1 * sp, z = q0 * cq - q1 * sq;
+        p1 = p1 * cp + p0 * sp, q1 = q1 * cq + q0 * sq;
+        p0 = v, q0 = z;
+      }
+      if (normed || turn) wa[u] = Half2<T>::down(p0, p1), wb[u] = Half2<T>::down(q0, q1);
+    }
+    T* to = static_cast<T*>(it.kind == 0 ? c.q_out : it.kind == 1 ? c.kc : c.vc) + it.at + (it.kind == 0 ? 0 : s_at[it.k]);
+    *reinterpret_cast<uint4*>(to + it.e0) = make_uint4(wa[0], wa[1], wa[2], wa[3]);
+    *reinterpret_cast<uint4*>(to + it.e1) = make_uint4(wb[0], wb[1], wb[2], wb[3]);
+  };
+
+  Item x, y;  // both items' loads before the first store, the first ones' before the look-ups
+  load(tid, x);
+  load(tid + kThreads, y);
+  if (warp < tokens) {
+    const int t = t0 + warp;
+    int s = t;
+    if (st.q_start) {
+      s = 0;
+      for (int base = 0; base < st.n_seqs; base += 32) {
+        const int i = base + lane;
+        s += __popc(__ballot_sync(0xffffffffu, i < st.n_seqs && __ldg(st.q_start + i + 1) <= t));
+      }
+    }
+    if (lane == 0) {
+      int line = -1;
+      int64_t at = 0;
+      if (s < st.n_seqs) {
+        const SeqSpan sp = seq_span(st, s);
+        const int at_line = sp.len - sp.n + t - sp.q0;
+        if (t >= sp.q0 && t < sp.q0 + sp.n && at_line >= 0) {
+          const int pi = (int)fast_div((uint32_t)at_line, st.page_mul, st.page_shift);
+          const int page = __ldg(st.pages + (int64_t)s * st.pages_per_seq + pi);
+          if (page >= 0 && page < st.n_pages) {
+            line = at_line;
+            at = (int64_t)page * st.page_stride + (int64_t)(at_line - pi * st.page_size) * st.token_stride;
           }
         }
-      };
-      scaled(x, e0), scaled(y, e1);
-    }
-    if (turned && !is_v) {
-      if (c.interleaved) {
-#pragma unroll
-        for (int u = 0; u < 8; u += 2) {
-          const float p = x[u] * co[u / 2] - x[u + 1] * si[u / 2], q = y[u] * co[4 + u / 2] - y[u + 1] * si[4 + u / 2];
-          x[u + 1] = x[u + 1] * co[u / 2] + x[u] * si[u / 2], y[u + 1] = y[u + 1] * co[4 + u / 2] + y[u] * si[4 + u / 2];
-          x[u] = p, y[u] = q;
-        }
-      } else {
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const float p = x[u] * co[u] - y[u] * si[u];
-          y[u] = y[u] * co[u] + x[u] * si[u];
-          x[u] = p;
-        }
       }
+      if (line < 0) attn_report(st, kAttnRange);
+      s_line[warp] = line;
+      s_at[warp] = at;
     }
-    if (in && (is_q || line >= 0)) {
-      if (normed || (turned && !is_v)) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) wa[u] = Half2<T>::down(x[2 * u], x[2 * u + 1]), wb[u] = Half2<T>::down(y[2 * u], y[2 * u + 1]);
-      }
-      T* dst = is_q   ? static_cast<T*>(c.q_out) + (int64_t)t * c.q_out_stride + (int64_t)head * D
-               : is_v ? static_cast<T*>(c.vc) + at + (int64_t)(head - q_heads - st.Hkv) * st.head_stride
-                      : static_cast<T*>(c.kc) + at + (int64_t)(head - q_heads) * st.head_stride;
-      *reinterpret_cast<uint4*>(dst + e0) = make_uint4(wa[0], wa[1], wa[2], wa[3]);
-      *reinterpret_cast<uint4*>(dst + e1) = make_uint4(wb[0], wb[1], wb[2], wb[3]);
+  } else {
+    for (int i = tid - 32 * tokens; i < 2 * D; i += kThreads - 32 * tokens) {
+      const int kind = i / D, e = i % D;  // which lane's, which of its elements
+      const bool low = e < 2 * c.half && !c.interleaved, second = low && e >= c.half;
+      const int j = low ? (second ? e - c.half : e) / 8 : e / 16, u = low ? (second ? 8 : 0) + e % 8 : e % 16;
+      const void* from = kind ? n.k_weight : n.q_weight;
+      const float f = !from ? 0.f : n.f32 ? __ldg(static_cast<const float*>(from) + e) : (float)static_cast<const T*>(from)[e];
+      reinterpret_cast<float*>(&s_weight[kind][u >> 2][j])[u & 3] = f + n.offset;
     }
-    if (++r == per_token) r = 0, ++t, fresh = true;
   }
-  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+  if (c.half) {
+    for (int i = tid; i < tokens * c.half; i += kThreads) {
+      const int k = i / c.half, pair = i - k * c.half;
+      int p = s_line[k];
+      if (c.pos) {
+        const int axis = c.n_axes == 1 ? 0 : (pair >= c.end0) + (pair >= c.end1) + (pair >= c.end2);
+        p = __ldg(c.pos + (int64_t)axis * st.n_tokens + t0 + k);
+      }
+      const int pc = min(max(p, 0), c.n_pos - 1);
+      if (pc != p) attn_report(st, kAttnRange);
+      float* to = reinterpret_cast<float*>(&s_angle[k][(pair & 7) >> 1][pair >> 3]) + (pair & 1);
+      to[0] = __ldg(c.cos + (int64_t)pc * c.half + pair), to[2] = __ldg(c.sin + (int64_t)pc * c.half + pair);
+    }
+    __syncthreads();
+  }
+  for (int i = tid;;) {  // (a warp's lanes together)
+    store(x);
+    store(y);
+    i += 2 * kThreads;
+    if (i - lane >= total) break;
+    load(i, x);
+    load(i + kThreads, y);
+  }
 }
 
 template <class T, int D>
 cudaError_t run(const AppendCall& c, const AppendNorm& n, cudaStream_t s) {
-  constexpr int kHeads = 32 * 16 / D;
-  constexpr size_t smem = kWarps * kAhead * kRowBytes;
-  const int per_token = ((c.q ? c.st.Hq : 0) + 2 * c.st.Hkv + kHeads - 1) / kHeads;
-  const int64_t blocks = ((int64_t)c.st.n_tokens * per_token + kWarps - 1) / kWarps, fit = 3 * 152;  // (this GPU's SMs)
-  const cudaError_t e = cudaFuncSetAttribute(k_append_norm<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  return e == cudaSuccess ? launch_pdl(true, k_append_norm<T, D>, dim3((unsigned)(blocks < fit ? blocks : fit)), dim3(kThreads), smem, s, c, n, per_token)
-                          : e;
+  const int t = c.st.n_tokens;
+  auto launch = [&](auto kernel, int tb) { return launch_pdl(true, kernel, dim3((unsigned)((t + tb - 1) / tb)), dim3(kThreads), 0, s, c, n); };
+  return t < 8 * 152 ? launch(k_append_norm<T, D, 1>, 1) : launch(k_append_norm<T, D, 4>, 4);
 }
 
 }  // namespace
