@@ -602,28 +602,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
   pdl_wait();
   pdl_trigger();
 
-  int tiles = 0;
-  int64_t total, B, t0, t1;
-  const int64_t b = blockIdx.x;
+  // where the plan says that the block begins, of a step whose groups share lines (ordinary loads: read-only ones may be moved ahead of the
+  // wait)
   int4 start_x = make_int4(0, 0, 0, 0);
-  longlong2 start_u = make_longlong2(0, 0);
+  longlong2 start_u = make_longlong2(0, 0), start_w = make_longlong2(0, 0);
   if constexpr (kShared) {
-    // (ordinary loads: read-only ones may be moved ahead of the wait)
-    start_x = *reinterpret_cast<const int4*>(p.start + 3 * b);
-    start_u = p.start[3 * b + 1];
-    const longlong2 w = p.start[3 * b + 2];
-    total = w.y, B = start_x.z, t0 = start_u.y, t1 = w.x;
-  } else {
-    tiles = __ldg(p.first + st.n_seqs);
-    total = tiles ? __ldg(p.before + tiles) * st.Hkv : 0;
-    // every block that works has at least two jobs, so that it has a key tile's start
-    B = max((int64_t)1, min((int64_t)gridDim.x, total / 2));
-    t0 = b < B ? total * b / B : 0, t1 = b < B ? total * (b + 1) / B : 0;
+    start_x = *reinterpret_cast<const int4*>(p.start + 3 * blockIdx.x);
+    start_u = p.start[3 * blockIdx.x + 1], start_w = p.start[3 * blockIdx.x + 2];
   }
-  auto walk_begin = [&](Walk<C::kRows, C::kOver>& w) {
-    if constexpr (kShared) walk_from(w, c, p, start_x, start_u, t1);
-    else walk_start(w, c, p, tiles, t0, t1);
-  };
+  const int tiles = kShared ? 0 : __ldg(p.first + st.n_seqs);
+  const int64_t total = kShared ? start_w.y : tiles ? __ldg(p.before + tiles) * st.Hkv : 0;
+  // every block that works has at least two jobs, so that it has a key tile's start
+  const int64_t B = kShared ? start_x.z : max((int64_t)1, min((int64_t)gridDim.x, total / 2));
+  const int64_t b = blockIdx.x;
+  const int64_t t0 = kShared ? start_u.y : b < B ? total * b / B : 0, t1 = kShared ? start_w.x : b < B ? total * (b + 1) / B : 0;
 
   auto wait = [&](int bar, uint32_t parity) -> bool {  // bounded
     return mbar_try_wait(&bars[bar], parity) || wait_slow(&bars[bar], parity, &s_flag, st.err);
@@ -887,7 +879,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
     auto uniform = [](uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); };
     const uint32_t bars0 = uniform(smem_u32(bars)), tm = uniform(tmem);
     Walk<C::kRows, C::kOver> w0;
-    walk_begin(w0);
+    if constexpr (kShared) walk_from(w0, c, p, start_x, start_u, t1);
+    else walk_start(w0, c, p, tiles, t0, t1);
     Walk<C::kRows, C::kOver> w = w0;
     Jobs jb{};
     jb.take(w);
@@ -1052,7 +1045,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
       pending = bar;
     };
     Walk<C::kRows, C::kOver> w0;
-    walk_begin(w0);
+    if constexpr (kShared) walk_from(w0, c, p, start_x, start_u, t1);
+    else walk_start(w0, c, p, tiles, t0, t1);
     Walk<C::kRows, C::kOver> w = w0;
     int told = 0;
     const int group_tiles = kShared ? p.first[p.groups] : 0;

@@ -94,6 +94,14 @@ def test_one_group(mf, n, prefix, own, d):
     check(mf, c, [0, n], [prefix])
 
 
+@pytest.mark.parametrize("d,hq,hkv,new", [(64, 16, 2, [8, 7, 6, 1, 8]), (128, 16, 1, [3, 4, 2, 3, 4]), (128, 8, 4, [20, 33, 17, 40, 1]),
+                                          (256, 16, 2, [9, 16, 31, 4, 2]), (256, 5, 1, [12, 40, 9, 50, 33])])
+def test_rows_between(mf, d, hq, hkv, new):
+    """More rows a sequence than the kernel of few rows holds, fewer than fill tiles of their own."""
+    check(mf, ref.Case(new, [600, 580, 700, 577, 1300], hq, hkv, d, page=16), [0, 3, 5], [576, 570])
+    check(mf, ref.Case(new, [600, 580, 700, 577, 1300], hq, hkv, d, "f16", page=7), [0, 5], [577], causal=False)
+
+
 def test_many_tokens(mf):
     """Prompts behind a prefix: tiles of the group that hold several sequences' tokens."""
     check(mf, ref.Case([700, 3, 511, 1, 64, 900], [1030, 1100, 1025, 1024, 1500, 1024], 16, 4, 128), [0, 6], [1024])
