@@ -355,6 +355,21 @@ int make_attn(const mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t
   return MF_OK;
 }
 
+// Each sequence from its own pages.
+cudaError_t each_alone(const mf_attn_t* attn, AttnCall& c, cudaStream_t s) {
+  const int D = attn->shape.head_dim;
+  const bool bf16 = attn->shape.dtype == MF_BF16;
+  // (few rows: as many as their kernel's registers hold.  There it is the faster one, but for heads of 64 without a window.  16
+  // sequences of 4093 lines and 8 heads a kv head, in a graph, few against many, with a window of 1024 and without: 48 rows of 64
+  // 20.8 us against 31.1, 38.5 against 35.5; 32 rows of 128 21.7 against 33.2, 44.2 against 46.3; 16 rows of 256 24.2 against
+  // 42.7, 62.2 against 70.7.  One token a sequence more goes to the other kernel: 40 rows of 128 34.0 and 48.4, 24 rows of 256 43.3 and
+  // 71.9)
+  if ((int64_t)c.st.max_q * c.st.G <= attn_few_rows(D)) return launch_attn_few(c, attn->parts, D, bf16, attn->sms, s);
+  AttnMaps maps;
+  attn_maps(c, D, &maps);
+  return launch_attn_many(c, maps, attn->plan, attn->parts, D, bf16, attn->sms, s);
+}
+
 }  // namespace
 
 extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step,
@@ -365,22 +380,7 @@ extern "C" int mf_attn_forward(mf_attn_t* attn, const mf_kv_cache_t* cache, cons
   if (rc != MF_OK || !work) return rc;
   OnDevice on(attn->device);
   if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
-  const int D = attn->shape.head_dim;
-  const bool bf16 = attn->shape.dtype == MF_BF16;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t e;
-  // (few rows: as many as their kernel's registers hold.  There it is the faster one, but for heads of 64 without a window.  16
-  // sequences of 4093 lines and 8 heads a kv head, in a graph, few against many, with a window of 1024 and without: 48 rows of 64
-  // 20.8 us against 31.1, 38.5 against 35.5; 32 rows of 128 21.7 against 33.2, 44.2 against 46.3; 16 rows of 256 24.2 against
-  // 42.7, 62.2 against 70.7.  One token a sequence more goes to the other kernel: 40 rows of 128 34.0 and 48.4, 24 rows of 256 43.3 and
-  // 71.9)
-  if ((int64_t)c.st.max_q * c.st.G <= attn_few_rows(D)) {
-    e = launch_attn_few(c, attn->parts, D, bf16, attn->sms, s);
-  } else {
-    AttnMaps maps;
-    attn_maps(c, D, &maps);
-    e = launch_attn_many(c, maps, attn->plan, attn->parts, D, bf16, attn->sms, s);
-  }
+  const cudaError_t e = each_alone(attn, c, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_attn_forward");
 }
 
@@ -447,10 +447,26 @@ extern "C" int mf_attn_forward_shared(mf_attn_t* attn, const mf_kv_cache_t* cach
   OnDevice on(attn->device);
   if (!on.ok) return cuda_fail(cudaGetLastError(), "cudaSetDevice");
   const SharedGroups g = {shared->first, shared->len, shared->n_groups};
-  AttnMaps maps;
-  attn_maps(c, attn->shape.head_dim, &maps);
-  const cudaError_t e = launch_attn_shared(c, maps, g, attn->shared, attn->parts, attn->shape.head_dim, attn->shape.dtype == MF_BF16, attn->sms,
-                                           static_cast<cudaStream_t>(stream));
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  // Sharing costs a plan, a launch and a longer join.  Where all that the sequences' tables can hold is soon read (of lines that share pages
+  // most come from the L2 cache), or the sequences have rows enough to fill tiles of their own (a group's tiles then spare no products
+  // and hardly any reading, and the partials cost), each sequence reads all its lines itself, from its own pages, which hold the same.
+  // Shared against alone, 4 kv heads with 8 heads each, in a graph: one token a sequence, 2 to 64 sequences, 66 MB 22 to 27 us and 20 to 22, 100
+  // MB 24 to 30 and 21 to 25, 131 MB 25 to 29 and 25 to 29; heads of 64 17 MB 18 and 13, 99 MB 22 and 26.  8 sequences of 100 and
+  // 8192 shared lines, rows of a sequence on the average: heads of 128, 58 32 us and 38, 77 40 and 39, 154 59 and 54; of 64, 77 52 and 51;
+  // of 256, 77 52 and 55, 154 66 and 75, 3400 430 and 376.
+  const int D = attn->shape.head_dim;
+  const int64_t rows = (int64_t)c.st.n_tokens * c.st.G, held = (int64_t)c.st.n_seqs * c.st.cap * c.st.Hkv * D * 4;
+  cudaError_t e;
+  if (held <= (D == 64 ? 80 : 128) * (int64_t)1000000 ||
+      ((int64_t)c.st.max_q * c.st.G > attn_few_rows(D) && rows >= (int64_t)attn_alone_rows(D) * c.st.n_seqs)) {
+    c.look = g;
+    e = each_alone(attn, c, s);
+  } else {
+    AttnMaps maps;
+    attn_maps(c, D, &maps);
+    e = launch_attn_shared(c, maps, g, attn->shared, D, attn->shape.dtype == MF_BF16, attn->sms, s);
+  }
   return e == cudaSuccess ? MF_OK : cuda_fail(e, "mf_attn_forward_shared");
 }
 

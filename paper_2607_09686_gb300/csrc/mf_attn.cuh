@@ -70,6 +70,12 @@ __device__ __forceinline__ int64_t line_offset(const AttnStep& a, int s, int c) 
   return (int64_t)page * a.page_stride + (int64_t)(c - pi * a.page_size) * a.token_stride;
 }
 
+// Groups of sequences that share their first lines (mf_shared_t).
+struct SharedGroups {
+  const int32_t *first, *len;
+  int n;
+};
+
 // An attention call.
 struct AttnCall {
   AttnStep st;
@@ -81,6 +87,7 @@ struct AttnCall {
   int window, causal;
   int box;  // lines of a tensor-map box (mf_attn_many.cu): a power of two that divides the page; 0: no tensor maps
   int q_box;  // Q has a tensor map
+  SharedGroups look;  // groups that are looked at (are bounds and lengths in range?) and not used; n = 0: none
 };
 
 // The caches as 4-D tensors (element, head, line, page), boxes of 64 elements x `box` lines, 128-byte swizzled.
@@ -172,11 +179,7 @@ struct AttnPlan {
   longlong2* start;  // [blocks][3]
 };
 
-// Groups of sequences that share their first lines (mf_shared_t), and what k_attn_plan_shared finds of them.
-struct SharedGroups {
-  const int32_t *first, *len;
-  int n;
-};
+// What k_attn_plan_shared finds of groups of sequences that share their first lines.
 struct SharedPlan {
   int* bound;   // [max_groups + 1] first sequence of a group
   int4* group;  // [max_groups]     that, its first token, tokens (0: nothing is shared), lines that are shared
@@ -220,9 +223,11 @@ cudaError_t launch_attn_few(const AttnCall& c, const AttnParts& parts, int head_
 void attn_maps(AttnCall& c, int head_dim, AttnMaps* maps);
 cudaError_t launch_attn_many(const AttnCall& c, const AttnMaps& maps, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
                              cudaStream_t s);
-// parts: the handle's own, for sequences that share nothing after all
-cudaError_t launch_attn_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& groups, const AttnShared& sh, const AttnParts& parts,
-                               int head_dim, bool bf16, int sms, cudaStream_t s);
+cudaError_t launch_attn_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& groups, const AttnShared& sh, int head_dim, bool bf16,
+                               int sms, cudaStream_t s);
+// Rows of a sequence, on the average, from which launch_attn_many does not gain by shared lines.
+int attn_alone_rows(int head_dim);
+cudaError_t launch_look(const AttnCall& c, cudaStream_t s);  // c.look, where no join does it
 // the records of `blocks` blocks joined; rows: rows of a part; tiles: left by launch_attn_many
 cudaError_t launch_attn_join(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int rows, bool tiles, int blocks,
                              cudaStream_t s);

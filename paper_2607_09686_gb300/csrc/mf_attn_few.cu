@@ -570,6 +570,7 @@ cudaError_t run(const AttnCall& c, const AttnParts& parts, const FewShared* shar
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e == cudaSuccess) e = launch_pdl(true, kernel, dim3(grid), dim3(kThreads), smem, s, c, parts, Alone{});
   if (e == cudaSuccess && grid > 1) e = launch_attn_join(c, parts, D, Half2<T>::kBf16, MT * 16, false, (int)grid, s);
+  else if (e == cudaSuccess && c.look.n) e = launch_look(c, s);
   return e;
 }
 

@@ -88,12 +88,45 @@ __device__ __forceinline__ void join_row(const AttnCall& c, const AttnParts& par
   if (c.lse && col == 0) c.lse[(int64_t)tok * c.st.Hq + head] = ls == 0.f ? -INFINITY : (mx + log2f(ls)) * kLn2;
 }
 
-template <class T, int D, bool kOneRow, bool kTiles>
+// Bounds of groups that fall or lie outside the step, and lengths that a sequence of the group does not have, are reported.
+__device__ void look_at_groups(const AttnStep& st, const SharedGroups& g) {
+  bool bad = false;
+  for (int i = threadIdx.x; i <= g.n; i += blockDim.x) {
+    const int x = g.first[i];
+    bad |= x < 0 || x > st.n_seqs || (i > 0 && x < g.first[i - 1]);
+  }
+  if (!__syncthreads_or(bad)) {
+    for (int s = threadIdx.x; s < st.n_seqs; s += blockDim.x) {
+      int lo = -1, hi = g.n - 1;  // the last group that begins at or before the sequence
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (g.first[mid] <= s) lo = mid;
+        else hi = mid - 1;
+      }
+      if (lo < 0 || s >= g.first[lo + 1]) continue;
+      const SeqSpan sp = seq_span(st, s);
+      const int len = g.len[lo];
+      bad |= len < 0 || len > max(sp.len - sp.n, 0);
+    }
+  }
+  if (bad) attn_report(st, kAttnRange);
+}
+__global__ void __launch_bounds__(256) k_look(const __grid_constant__ AttnCall c) {
+  pdl_wait();
+  look_at_groups(c.st, c.look);
+}
+
+// kLook: the last block looks at the call's groups.
+template <class T, int D, bool kOneRow, bool kTiles, bool kLook>
 __global__ void __launch_bounds__(Join<D>::kThreads, 2)
     k_attn_join(const __grid_constant__ AttnCall c, const __grid_constant__ AttnParts parts, int part_rows) {
   using J = Join<D>;
   const int b = blockIdx.x, tid = threadIdx.x;
   pdl_wait();
+  if (kLook && b + 1 == gridDim.x) {
+    if (blockIdx.y == 0) look_at_groups(c.st, c.look);
+    return;
+  }
   const AttnRec rec = parts.rec[b];
   if (rec.n == 0) return;
   if (kOneRow && rec.n > kFew) {
@@ -106,16 +139,22 @@ __global__ void __launch_bounds__(Join<D>::kThreads, 2)
   }
 }
 
-template <class T, int D>
+template <class T, int D, bool kLook>
 cudaError_t run(const AttnCall& c, const AttnParts& parts, int rows, bool tiles, int blocks, cudaStream_t s) {
   using J = Join<D>;
   // up to 64 rows there may be many pieces of each; with more, a record has few pieces
   const int64_t most = (int64_t)c.st.max_q * c.st.G;
   const int held = (int)(most < rows ? most : rows);
-  const dim3 one(blocks, held < 8 ? held : 8), each(blocks, (held + J::kGroups - 1) / J::kGroups), threads(J::kThreads);
-  if (!tiles) return launch_pdl(true, k_attn_join<T, D, true, false>, one, threads, 0, s, c, parts, rows);
-  if (held <= 64) return launch_pdl(true, k_attn_join<T, D, true, true>, one, threads, 0, s, c, parts, rows);
-  return launch_pdl(true, k_attn_join<T, D, false, true>, each, threads, 0, s, c, parts, rows);
+  const int x = blocks + kLook;
+  const dim3 one(x, held < 8 ? held : 8), each(x, (held + J::kGroups - 1) / J::kGroups), threads(J::kThreads);
+  if (!tiles) return launch_pdl(true, k_attn_join<T, D, true, false, kLook>, one, threads, 0, s, c, parts, rows);
+  if (held <= 64) return launch_pdl(true, k_attn_join<T, D, true, true, kLook>, one, threads, 0, s, c, parts, rows);
+  return launch_pdl(true, k_attn_join<T, D, false, true, kLook>, each, threads, 0, s, c, parts, rows);
+}
+
+template <class T, int D>
+cudaError_t pick(const AttnCall& c, const AttnParts& parts, int rows, bool tiles, int blocks, cudaStream_t s) {
+  return c.look.n ? run<T, D, true>(c, parts, rows, tiles, blocks, s) : run<T, D, false>(c, parts, rows, tiles, blocks, s);
 }
 
 }  // namespace
@@ -123,12 +162,14 @@ cudaError_t run(const AttnCall& c, const AttnParts& parts, int rows, bool tiles,
 cudaError_t launch_attn_join(const AttnCall& c, const AttnParts& parts, int head_dim, bool bf16, int rows, bool tiles, int blocks,
                              cudaStream_t s) {
   if (bf16)
-    return head_dim == 64    ? run<__nv_bfloat16, 64>(c, parts, rows, tiles, blocks, s)
-           : head_dim == 128 ? run<__nv_bfloat16, 128>(c, parts, rows, tiles, blocks, s)
-                             : run<__nv_bfloat16, 256>(c, parts, rows, tiles, blocks, s);
-  return head_dim == 64    ? run<__half, 64>(c, parts, rows, tiles, blocks, s)
-         : head_dim == 128 ? run<__half, 128>(c, parts, rows, tiles, blocks, s)
-                           : run<__half, 256>(c, parts, rows, tiles, blocks, s);
+    return head_dim == 64    ? pick<__nv_bfloat16, 64>(c, parts, rows, tiles, blocks, s)
+           : head_dim == 128 ? pick<__nv_bfloat16, 128>(c, parts, rows, tiles, blocks, s)
+                             : pick<__nv_bfloat16, 256>(c, parts, rows, tiles, blocks, s);
+  return head_dim == 64    ? pick<__half, 64>(c, parts, rows, tiles, blocks, s)
+         : head_dim == 128 ? pick<__half, 128>(c, parts, rows, tiles, blocks, s)
+                           : pick<__half, 256>(c, parts, rows, tiles, blocks, s);
 }
+
+cudaError_t launch_look(const AttnCall& c, cudaStream_t s) { return launch_pdl(true, k_look, dim3(1), dim3(256), 0, s, c); }
 
 }  // namespace mf

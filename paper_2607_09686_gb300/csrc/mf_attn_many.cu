@@ -135,11 +135,10 @@ __global__ void __launch_bounds__(1024) k_attn_plan(AttnCall c, AttnPlan p) {
 // all the group's tokens and the shared lines (whole pages of them), then the sequences, with what follows.  First the groups: bounds
 // that rise, lengths that all their sequences have; a group of one shares nothing.  p.groups and p.seqs say which of them are in the list
 // of this file's kernel, few_groups and few_seqs which are in that of few rows.  Two blocks, both of which find the groups: the first lays out this
-// file's list and says where its kernel's blocks begin, the second the other list, and what the join asks for.  alone: nothing is shared
-// after all, the list is k_attn_plan's.
+// file's list and says where its kernel's blocks begin, the second the other list, and what the join asks for.
 template <int D>
 __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGroups g, AttnPlan p, SharedPlan sp, int few_groups,
-                                                           int few_seqs, int blocks, int few_blocks, int alone) {
+                                                           int few_seqs, int blocks, int few_blocks) {
   __shared__ int64_t s_warp[32];
   // what the phases hand on, in shared memory where it finds room: the sequences' spans and groups, the groups, first row tiles
   constexpr int kSmall = 1024;
@@ -222,7 +221,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     if (i < g.n) {
       const int asked = g.len[i], len = max(0, min(asked, least));
       if (len != asked && sub == 0 && a < b) attn_report(c.st, kAttnRange);
-      const int lines = b - a > 1 && !alone ? (int)fast_div((uint32_t)len, c.st.page_mul, c.st.page_shift) * c.st.page_size : 0;
+      const int lines = b - a > 1 ? (int)fast_div((uint32_t)len, c.st.page_mul, c.st.page_shift) * c.st.page_size : 0;
       int q0 = 0, n = 0;
       if (lines) {
         const SeqSpan x = span(a), y = span(b - 1);
@@ -250,7 +249,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
   if (tid == 0 && V) first[V] = p.first[V] = tiles;
   __syncthreads();
   if (lists) {
-    int64_t* before = tiles <= kSmall && !alone ? s_before : p.before;
+    int64_t* before = tiles <= kSmall ? s_before : p.before;
     int64_t jobs = 0;
     for (int base = 0; base < tiles; base += 1024) {
       const int i = base + tid;
@@ -284,7 +283,6 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
       jobs += all;
     }
     if (tid == 0) before[tiles] = jobs;
-    if (alone) return;
     __syncthreads();
     // ---- where the blocks begin: every one that works has two jobs at least, so that it has a key tile's start
     const int64_t total = jobs * c.st.Hkv, B = max((int64_t)1, min((int64_t)blocks, total / 2));
@@ -317,7 +315,6 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     }
     return;
   }
-  if (alone) return;
   // ---- the list of few rows
   int64_t* before = few <= kSmall ? s_before : sp.before;
   done = 0;
@@ -1314,8 +1311,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_
 constexpr size_t smem_of(size_t tail) { return tail + sizeof(Tail); }
 
 template <class T, int D>
-cudaError_t run(const AttnCall& c, const AttnMaps& maps, AttnPlan plan, const AttnParts& parts, const SharedGroups* groups,
-                const SharedPlan* found, int sms, cudaStream_t s) {  // groups: given, they are looked at and not used
+cudaError_t run(const AttnCall& c, const AttnMaps& maps, AttnPlan plan, const AttnParts& parts, int sms, cudaStream_t s) {
   using C = Cfg<D>;
   const int64_t rows = (int64_t)c.st.n_tokens * c.st.G;
   const int64_t tiles = rows / C::kRows + c.st.n_seqs;
@@ -1326,29 +1322,21 @@ cudaError_t run(const AttnCall& c, const AttnMaps& maps, AttnPlan plan, const At
   static_assert(smem <= 232448, "shared memory of a block");
   auto kernel = k_attn_many<T, D, false>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  plan.groups = 0, plan.seqs = c.st.n_seqs;
-  if (e == cudaSuccess)
-    e = groups ? launch_pdl(true, k_attn_plan_shared<D>, dim3(2), dim3(1024), 0, s, c, *groups, plan, *found, 0, 0, (int)grid, 0, 1)
-               : launch_pdl(true, k_attn_plan<D>, dim3(1), dim3(1024), 0, s, c, plan);
+  if (e == cudaSuccess) e = launch_pdl(true, k_attn_plan<D>, dim3(1), dim3(1024), 0, s, c, plan);
   if (e == cudaSuccess) e = launch_pdl(true, kernel, dim3(grid), dim3(kThreads), smem, s, c, maps, plan, parts);
   if (e == cudaSuccess && grid > 1) e = launch_attn_join(c, parts, D, Half2<T>::kBf16, C::kRows, true, (int)grid, s);
+  else if (e == cudaSuccess && c.look.n) e = launch_look(c, s);
   return e;
 }
 
 // The plan, the groups' lines, the sequences' own, the join.  Rows that the kernel of few rows holds are its: all of them where a group cannot
-// have more (one launch), else those of the sequences (a launch that starts while the groups' ends).  Where the sequences have rows
-// enough to fill tiles of their own, a group's tiles spare no products and hardly any reading (the tiles of a head read the shared lines
-// from the L2 cache), and the partials cost: then each sequence reads all its lines itself, from its own pages, which hold the same (8
-// sequences of 100 and 8192 shared lines, 8 heads a kv head, shared against alone: heads of 128, rows of a sequence on the average 58
-// 31.8 us and 38.1, 77 40.3 and 39.0, 154 58.6 and 54.1; of 64, 77 52.2 and 51.4; of 256, 77 51.6 and 55.2, 154 65.5 and 75.2, 3400 430 and 376).
+// have more (one launch), else those of the sequences (a launch that starts while the groups' ends).
 template <class T, int D>
-cudaError_t run_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& g, const AttnShared& sh, const AttnParts& parts, int sms,
-                       cudaStream_t s) {
+cudaError_t run_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& g, const AttnShared& sh, int sms, cudaStream_t s) {
   using C = Cfg<D>;
   constexpr bool kBf = Half2<T>::kBf16;
   const int64_t rows = (int64_t)c.st.n_tokens * c.st.G, seq_rows = (int64_t)c.st.max_q * c.st.G;
   const bool few_seqs = seq_rows <= attn_few_rows(D), few_groups = few_seqs && (rows <= attn_few_rows(D) || g.n == 0);
-  if (!few_seqs && rows >= (int64_t)(D == 256 ? 256 : 72) * c.st.n_seqs) return run<T, D>(c, maps, sh.plan, parts, &g, &sh.found, sms, s);
   AttnPlan plan = sh.plan;
   plan.groups = few_groups ? 0 : g.n, plan.seqs = few_seqs ? 0 : c.st.n_seqs;
   const int64_t own = rows / C::kRows + c.st.n_seqs;  // row tiles of the sequences
@@ -1359,7 +1347,7 @@ cudaError_t run_shared(const AttnCall& c, const AttnMaps& maps, const SharedGrou
   const int64_t most = tiles * c.st.Hkv * (((int64_t)c.st.cap + kKeys - 1) / kKeys);
   const unsigned grid = (unsigned)(most < sms ? most : sms);
   cudaError_t e = launch_pdl(true, k_attn_plan_shared<D>, dim3(2), dim3(1024), 0, s, c, g, plan, sh.found, n_few_groups, few_seqs ? c.st.n_seqs : 0,
-                             (int)grid, few_blocks, 0);
+                             (int)grid, few_blocks);
   if (e == cudaSuccess && tiles) {
     constexpr size_t smem = smem_of(C::kTail);
     auto kernel = k_attn_many<T, D, true>;
@@ -1419,27 +1407,28 @@ void attn_maps(AttnCall& c, int head_dim, AttnMaps* maps) {
   }
 }
 
+int attn_alone_rows(int head_dim) { return head_dim == 256 ? 256 : 72; }
 int attn_tile_rows(int head_dim) { return head_dim == 256 ? 128 : 256; }
 
 cudaError_t launch_attn_many(const AttnCall& c, const AttnMaps& maps, const AttnPlan& plan, const AttnParts& parts, int head_dim, bool bf16, int sms,
                              cudaStream_t s) {
   if (bf16)
-    return head_dim == 64    ? run<__nv_bfloat16, 64>(c, maps, plan, parts, nullptr, nullptr, sms, s)
-           : head_dim == 128 ? run<__nv_bfloat16, 128>(c, maps, plan, parts, nullptr, nullptr, sms, s)
-                             : run<__nv_bfloat16, 256>(c, maps, plan, parts, nullptr, nullptr, sms, s);
-  return head_dim == 64    ? run<__half, 64>(c, maps, plan, parts, nullptr, nullptr, sms, s)
-         : head_dim == 128 ? run<__half, 128>(c, maps, plan, parts, nullptr, nullptr, sms, s)
-                           : run<__half, 256>(c, maps, plan, parts, nullptr, nullptr, sms, s);
+    return head_dim == 64    ? run<__nv_bfloat16, 64>(c, maps, plan, parts, sms, s)
+           : head_dim == 128 ? run<__nv_bfloat16, 128>(c, maps, plan, parts, sms, s)
+                             : run<__nv_bfloat16, 256>(c, maps, plan, parts, sms, s);
+  return head_dim == 64    ? run<__half, 64>(c, maps, plan, parts, sms, s)
+         : head_dim == 128 ? run<__half, 128>(c, maps, plan, parts, sms, s)
+                           : run<__half, 256>(c, maps, plan, parts, sms, s);
 }
-cudaError_t launch_attn_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& g, const AttnShared& sh, const AttnParts& parts,
-                               int head_dim, bool bf16, int sms, cudaStream_t s) {
+cudaError_t launch_attn_shared(const AttnCall& c, const AttnMaps& maps, const SharedGroups& g, const AttnShared& sh, int head_dim, bool bf16,
+                               int sms, cudaStream_t s) {
   if (bf16)
-    return head_dim == 64    ? run_shared<__nv_bfloat16, 64>(c, maps, g, sh, parts, sms, s)
-           : head_dim == 128 ? run_shared<__nv_bfloat16, 128>(c, maps, g, sh, parts, sms, s)
-                             : run_shared<__nv_bfloat16, 256>(c, maps, g, sh, parts, sms, s);
-  return head_dim == 64    ? run_shared<__half, 64>(c, maps, g, sh, parts, sms, s)
-         : head_dim == 128 ? run_shared<__half, 128>(c, maps, g, sh, parts, sms, s)
-                           : run_shared<__half, 256>(c, maps, g, sh, parts, sms, s);
+    return head_dim == 64    ? run_shared<__nv_bfloat16, 64>(c, maps, g, sh, sms, s)
+           : head_dim == 128 ? run_shared<__nv_bfloat16, 128>(c, maps, g, sh, sms, s)
+                             : run_shared<__nv_bfloat16, 256>(c, maps, g, sh, sms, s);
+  return head_dim == 64    ? run_shared<__half, 64>(c, maps, g, sh, sms, s)
+         : head_dim == 128 ? run_shared<__half, 128>(c, maps, g, sh, sms, s)
+                           : run_shared<__half, 256>(c, maps, g, sh, sms, s);
 }
 
 }  // namespace mf

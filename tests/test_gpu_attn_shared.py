@@ -17,10 +17,22 @@ def mf():
     return pkg
 
 
-def share(c, first, lens, copies=False):
+ALL_READ_ALONE = 128e6  # bytes that the tables can hold, up to which every sequence is read by itself
+
+
+def widen(c):
+    """Room in the page tables for so many more lines that the shared ones are read for the group."""
+    have, line = c.pages.shape[1], len(c.len) * c.hkv * c.d * 4
+    want = max(have, int(ALL_READ_ALONE / (line * c.page)) + 2)
+    c.pages = torch.nn.functional.pad(c.pages, (0, want - have)).contiguous()
+
+
+def share(c, first, lens, copies=False, wide=True):
     """Let groups of the case's sequences begin alike: sequences name the pages of their group's first one (whole pages), or hold
     copies; what is left of a page is copied.  The pages that are no longer named hold NaN."""
     gone = set()
+    if wide:
+        widen(c)
     for a, b, n in zip(first, first[1:], lens):
         whole = 0 if copies else n // c.page
         for s in range(a + 1, b):
@@ -40,6 +52,7 @@ def share(c, first, lens, copies=False):
 
 def check(mf, c, first, lens, causal=True, scale=None, lse=True, copies=False, status=0, stream=None, q_start=True, lens_given=None):
     scale = 1 / math.sqrt(c.d) if scale is None else scale
+    pages = c.pages.shape[1]
     f, n = share(c, first, lens, copies)
     if lens_given is not None:
         n = torch.tensor(lens_given, dtype=torch.int32, device="cuda")
@@ -48,18 +61,21 @@ def check(mf, c, first, lens, causal=True, scale=None, lse=True, copies=False, s
         mf.mf_attn_share(at, max(1, len(lens)))
         out = torch.full((c.tokens, c.hq, c.d), 7.0, dtype=c.q.dtype, device="cuda")
         le = torch.full((c.tokens, c.hq), 7.0, device="cuda") if lse else None
-        step = c.step(mf) if q_start else c.step(mf, q_start=None)
-        for _ in range(2):  # a second call on the same handle finds the workspace as the first left it
-            mf.mf_attn_forward_shared(at, mf.kv_cache(c.k, c.v), step, mf.shared(f, n), c.q, out, le, scale, causal=causal, stream=stream)
-        assert mf.mf_attn_check(at) == status
+        want, wl, tol, ltol = ref.attention64(c, scale, 0, causal)
+        wide = c.pages
+        for c.pages in (wide[:, :pages].contiguous(), wide):  # few lines in the tables: each sequence by itself
+            out.fill_(7.0)
+            step = c.step(mf) if q_start else c.step(mf, q_start=None)
+            for _ in range(2):  # a second call on the same handle finds the workspace as the first left it
+                mf.mf_attn_forward_shared(at, mf.kv_cache(c.k, c.v), step, mf.shared(f, n), c.q, out, le, scale, causal=causal, stream=stream)
+            assert mf.mf_attn_check(at) == status
+            far = (out.double() - want).abs() - tol
+            assert not out.isnan().any() and far.max() <= 0, (far.max().item(), (far > 0).sum().item())
+            if lse:
+                assert torch.equal(le.isinf(), wl.isinf())
+                assert ((le.double() - wl).abs() - ltol).nan_to_num(-1).max() <= 0
     finally:
         mf.mf_attn_destroy(at)
-    want, wl, tol, ltol = ref.attention64(c, scale, 0, causal)
-    far = (out.double() - want).abs() - tol
-    assert not out.isnan().any() and far.max() <= 0, (far.max().item(), (far > 0).sum().item())
-    if lse:
-        assert torch.equal(le.isinf(), wl.isinf())
-        assert ((le.double() - wl).abs() - ltol).nan_to_num(-1).max() <= 0
     return out
 
 
