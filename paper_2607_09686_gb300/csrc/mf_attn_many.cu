@@ -131,6 +131,11 @@ __global__ void __launch_bounds__(1024) k_attn_plan(AttnCall c, AttnPlan p) {
   if (tid == 0) p.before[tiles] = jobs;
 }
 
+// a / b of numbers that are mostly small (64-bit divisions take some hundred instructions)
+__device__ __forceinline__ int64_t quick_div(int64_t a, int64_t b) {
+  return (uint64_t)(a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
+
 // The same of a step whose groups of sequences share their first lines: as many virtual sequences as there are groups, with the rows of
 // all the group's tokens and the shared lines (whole pages of them), then the sequences, with what follows.  First the groups: bounds
 // that rise, lengths that all their sequences have; a group of one shares nothing.  p.groups and p.seqs say which of them are in the list
@@ -178,6 +183,10 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     all = __shfl_sync(0xffffffffu, total, 31);
     return __shfl_sync(0xffffffffu, total - mine, warp) + x - v;
   };
+  int width = 32;
+  while (width > 1 && (int64_t)width * g.n > 1024) width >>= 1;
+  const int per = 1024 / width, sub = tid % width;
+  const int first_raw = g.n && tid <= g.n ? g.first[tid] : 0, len_raw = tid / width < g.n ? g.len[tid / width] : 0;  // (with the spans)
   for (int s = tid; s < n_seqs; s += 1024) {
     if (small_seqs) s_span[s] = seq_span(c.st, s);
     seq[s] = make_int2(-1, 0);
@@ -186,7 +195,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
   int from = 0;
   for (int base = 0; base <= g.n; base += 1024) {
     const int i = base + tid;
-    const int raw = i <= g.n && g.n ? g.first[i] : 0;
+    const int raw = base == 0 ? first_raw : i <= g.n ? g.first[i] : 0;
     int x = min(max(raw, 0), n_seqs);
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -206,9 +215,6 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
   }
   __syncthreads();
   // ---- their lengths: some lanes a group
-  int width = 32;
-  while (width > 1 && (int64_t)width * g.n > 1024) width >>= 1;
-  const int per = 1024 / width, sub = tid % width;
   for (int base = 0; base < g.n; base += per) {
     const int i = base + tid / width;
     int a = 0, b = 0, least = 0x7FFFFFFF;
@@ -219,7 +225,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     }
     for (int d = 1; d < width; d <<= 1) least = min(least, __shfl_xor_sync(0xffffffffu, least, d));
     if (i < g.n) {
-      const int asked = g.len[i], len = max(0, min(asked, least));
+      const int asked = base == 0 ? len_raw : g.len[i], len = max(0, min(asked, least));
       if (len != asked && sub == 0 && a < b) attn_report(c.st, kAttnRange);
       const int lines = b - a > 1 ? (int)fast_div((uint32_t)len, c.st.page_mul, c.st.page_shift) * c.st.page_size : 0;
       int q0 = 0, n = 0;
@@ -287,7 +293,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     // ---- where the blocks begin: every one that works has two jobs at least, so that it has a key tile's start
     const int64_t total = jobs * c.st.Hkv, B = max((int64_t)1, min((int64_t)blocks, total / 2));
     for (int b = tid; b < blocks; b += 1024) {
-      const int64_t t0 = b < B ? total * b / B : 0, t1 = b < B ? total * (b + 1) / B : 0;
+      const int64_t t0 = b < B ? quick_div(total * b, B) : 0, t1 = b < B ? quick_div(total * (b + 1), B) : 0;
       int tile = 0, h = 0;
       int64_t at = 0;
       if (t0 < t1) {
@@ -299,7 +305,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
         }
         const int f = first[lo];
         const int64_t b0 = before[f], len = before[first[lo + 1]] - b0;
-        h = (int)((t0 - b0 * c.st.Hkv) / len);
+        h = (int)quick_div(t0 - b0 * c.st.Hkv, len);
         const int64_t head = b0 * c.st.Hkv + h * len;
         int x = f, y = first[lo + 1] - 1;
         while (x < y) {
@@ -341,7 +347,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
   __syncthreads();
   const int64_t B = min((int64_t)few_blocks, done);
   for (int b = tid; b < few_blocks && few; b += 1024) {
-    const int64_t t0 = b < B ? done * b / B : 0, t1 = b < B ? done * (b + 1) / B : 0;
+    const int64_t t0 = b < B ? quick_div(done * b, B) : 0, t1 = b < B ? quick_div(done * (b + 1), B) : 0;
     int v = 0, h = 0, row = 0;
     int64_t at = 0;
     int4 x = make_int4(0, 0, 0, 0);
@@ -360,8 +366,8 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
         const SeqSpan q = span(v - few_groups);
         x = make_int4(q.q0, q.n, q.len, seq[v - few_groups].y), row = v - few_groups;
       }
-      const int64_t len = (before[v + 1] - before[v]) / c.st.Hkv;
-      h = (int)((t0 - before[v]) / len);
+      const int64_t len = quick_div(before[v + 1] - before[v], c.st.Hkv);
+      h = (int)quick_div(t0 - before[v], len);
       at = before[v] + h * len;
     }
     int4* to = sp.start + 4 * b;
