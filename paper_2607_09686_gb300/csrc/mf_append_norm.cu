@@ -22,7 +22,8 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
 __device__ __forceinline__ uint64_t neg2(uint64_t a) { return a ^ 0x8000000080000000ull; }
 
 template <class T, int D, int kTB>
-__global__ void __launch_bounds__(kThreads, 4) k_append_norm(const __grid_constant__ AppendCall c, const __grid_constant__ AppendNorm n) {
+__global__ void __launch_bounds__(kThreads, 4) k_append_norm(const __grid_constant__ AppendCall c, const __grid_constant__ AppendNorm n,
+                                                             FastDiv by_items) {
   constexpr int kPer = D / 16;  // lanes of a head
   const AttnStep& st = c.st;
   __shared__ int64_t s_at[kTB];
@@ -44,7 +45,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_append_norm(const __grid_consta
     const bool split = it.j * 8 < c.half && !c.interleaved;
     it.e0 = split ? it.j * 8 : it.j * 16, it.e1 = split ? it.e0 + c.half : it.e0 + 8;
     if (i >= total) return;
-    const int k = kTB == 1 ? 0 : i / n_items, head = (i - k * n_items) / kPer;
+    const int k = kTB == 1 ? 0 : (int)fast_div((uint32_t)i, by_items.mul, by_items.shift), head = (i - k * n_items) / kPer;
     it.k = k;
     it.kind = head < q_heads ? 0 : head < q_heads + st.Hkv ? 1 : 2;
     const int h = it.kind == 0 ? head : it.kind == 1 ? head - q_heads : head - q_heads - st.Hkv;
@@ -194,7 +195,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_append_norm(const __grid_consta
 template <class T, int D>
 cudaError_t run(const AppendCall& c, const AppendNorm& n, cudaStream_t s) {
   const int t = c.st.n_tokens;
-  auto launch = [&](auto kernel, int tb) { return launch_pdl(true, kernel, dim3((unsigned)((t + tb - 1) / tb)), dim3(kThreads), 0, s, c, n); };
+  const FastDiv by_items = make_fast_div((uint32_t)(((c.q ? c.st.Hq : 0) + 2 * c.st.Hkv) * (D / 16)));
+  auto launch = [&](auto kernel, int tb) { return launch_pdl(true, kernel, dim3((unsigned)((t + tb - 1) / tb)), dim3(kThreads), 0, s, c, n, by_items); };
   return t < 8 * 152 ? launch(k_append_norm<T, D, 1>, 1) : launch(k_append_norm<T, D, 4>, 4);
 }
 

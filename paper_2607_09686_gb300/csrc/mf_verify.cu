@@ -11,8 +11,10 @@
 #include <cfloat>
 #include <cmath>
 #include <cstring>
+#include <type_traits>
 
 #include "mf_sample.cuh"
+#include "mf_tc.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -50,10 +52,48 @@ struct VerifyCall {
 // next four are under way, with a running maximum and sum a lane, and leaves a piece where a row or its run ends (which depends on
 // the row starts alone).  The list has the target's rows and those of the drafter's that have a draft: every block adds up the sequences' rows
 // in shared memory (of more than kSeqs sequences, or bounds that overlap: all rows, of which some are passed over).  Bounded by
-// reading the logits once; of an entry's some six instructions one is an exponential.
+// reading the logits once; of an entry's four instructions (pairs of floats) one is an exponential.
 constexpr int kRowThreads = 256, kUnit = 128, kVecs = kUnit / 32, kSeqs = 2048;
 template <class T>
 constexpr int kUnitEntries = kUnit * 16 / (int)sizeof(T);
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+// the largest of the vectors' numbers (-inf: there is none)
+template <class T>
+__device__ __forceinline__ float largest(const uint4 (&v)[kVecs]) {
+  if constexpr (sizeof(T) == 4) {
+    float most = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k)
+      most = fmaxf(most, fmaxf(fmaxf(__uint_as_float(v[k].x), __uint_as_float(v[k].y)), fmaxf(__uint_as_float(v[k].z), __uint_as_float(v[k].w))));
+    return most;
+  } else {  // pair by pair, as they are
+    using P = typename std::conditional<Half2<T>::kBf16, __nv_bfloat162, __half2>::type;
+    const uint32_t low = Half2<T>::kBf16 ? 0xFF80FF80u : 0xFC00FC00u;
+    P most;
+    memcpy(&most, &low, 4);
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      P e[4];
+      memcpy(e, &v[k], 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) most = __hmax2(most, e[i]);
+    }
+    uint32_t w;
+    memcpy(&w, &most, 4);
+    const float2 f = Half2<T>::up(w);
+    return fmaxf(f.x, f.y);
+  }
+}
 
 template <class T>
 __global__ void __launch_bounds__(kRowThreads, 3) k_rows(const __grid_constant__ VerifyCall c, int side0, int rows) {
@@ -161,7 +201,6 @@ __global__ void __launch_bounds__(kRowThreads, 3) k_rows(const __grid_constant__
 #pragma unroll
       for (int k = 0; k < kVecs; ++k) v[k] = next[k];
       if (j + 1 < end) load(next, j + 1);
-      float most = none;
       auto each = [&](auto&& f) {
 #pragma unroll
         for (int k = 0; k < kVecs; ++k) {
@@ -171,7 +210,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) k_rows(const __grid_constant__
           for (int i = 0; i < kV; ++i) f((float)e[i], (j * kUnit + k * 32 + lane) * kV - lead_in + i);
         }
       };
-      each([&](float y, int) { most = fmaxf(most, y); });  // (a NaN is passed over)
+      const float most = largest<T>(v);  // (a NaN is passed over)
       if (most > m) {
         if (m > none) s *= exp2f((m - most) * inv_e);
         m = most;
@@ -184,13 +223,30 @@ __global__ void __launch_bounds__(kRowThreads, 3) k_rows(const __grid_constant__
       } else if (m == INFINITY) {  // (what came before it, and is finite, weighs nothing)
         each([&](float y, int) { s += y == INFINITY ? 1.f : 0.f; });
       } else if (m > none) {
-        float part[2] = {0.f, 0.f};
-        each([&](float y, int i) {
-          float z;
-          asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(z) : "f"((fmaxf(y, none) - m) * inv_e));
-          part[i & 1] += z;
-        });
-        s += part[0] + part[1];
+        // (pairs of floats; where a NaN among them spoils the sum, once more with -inf in its place)
+        const uint64_t by = tc::pack2(-m, -m), inv2 = tc::pack2(inv_e, inv_e);
+        uint64_t part[2] = {0, 0};
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) {
+          const uint32_t word[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+          for (int i = 0; i < kV / 2; ++i) {
+            float2 y;
+            if constexpr (sizeof(T) == 2) y = Half2<T>::up(word[i]);
+            else y = make_float2(__uint_as_float(word[2 * i]), __uint_as_float(word[2 * i + 1]));
+            float y0, y1;
+            tc::unpack2(mul2(tc::add2(tc::pack2(y.x, y.y), by), inv2), y0, y1);
+            part[i & 1] = tc::add2(part[i & 1], tc::pack2(ex2(y0), ex2(y1)));
+          }
+        }
+        float s0, s1;
+        tc::unpack2(tc::add2(part[0], part[1]), s0, s1);
+        s0 += s1;
+        if (s0 != s0) {
+          s0 = 0.f;
+          each([&](float y, int) { s0 += ex2((fmaxf(y, none) - m) * inv_e); });
+        }
+        s += s0;
       }
     }
     float all = m;
