@@ -535,7 +535,7 @@ typedef struct mf_sample_args {
  * dtype, n_rows < 0, a vocab out of range or a stride below it. */
 int mf_sample(const mf_sample_args_t* args, void* stream);
 
-/* Test hold of sampling.  hold = 1: blocks issue none of the copies of logits that they wait for, a second at most, in
+/* Test hold of sampling and verification.  hold = 1: blocks issue none of the copies of logits that they wait for, a second at most, in
  * calls from now on.  A copy that does not arrive is no error: its logits are read without it, later, and the answer is the
  * same.  hold = 0 (the default) restores normal operation.  MF_E_INVAL for other values.  Host only. */
 int mf_sample_test_hold(int hold);
@@ -562,7 +562,7 @@ typedef struct mf_cuts {
  *   token     device int32 [n_rows]: the drafts that were taken, then the new token (-1 where its row has no p), -1 in the rows after it
  *   accepted  device int32 [n_seqs]: the number of drafts taken
  *   logprob   device float [n_rows] or NULL: log p of each token in `token`, -inf beside -1
- * Rows of no sequence are left as they were; row starts that fall or lie outside the rows are taken as the nearest valid ones; a sequence without rows
+ * Outputs overlap no input.  Rows of no sequence are left as they were; row starts that fall or lie outside the rows are taken as the nearest valid ones; a sequence without rows
  * gets accepted = 0.
  *   work      device, 16-byte aligned, mf_verify_bytes of it; calls that share it must follow one another
  * vocab from 1 to 2^20.  Other pointers aligned to their element. */

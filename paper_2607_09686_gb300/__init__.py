@@ -1,5 +1,5 @@
 """GB300 routed-expert step of one MoE decoder layer (MawForge, arXiv 2607.09686), with the paged
-attention and the sampling of a serving step around it.
+attention, the sampling and the verification of drafts of a serving step around it.
 
 Thin ctypes binding of ``libmawforge.so`` (declared in ``include/mawforge.h``).  Every
 step of the path runs in the library's CUDA kernels; this module only marshals
@@ -454,14 +454,14 @@ def mf_kv_bytes(shape: AttnShape, n_layers: int, n_tokens: int, page_size: int) 
 
 class _Types:
     """torch's types (torch is imported with the first call that takes tensors, not with this module)."""
-    f32 = i32 = None
+    f32 = i32 = device = None
     codes: dict = {}
     of: dict = {}
 
     @classmethod
     def load(cls):
         import torch
-        cls.f32, cls.i32 = torch.float32, torch.int32
+        cls.f32, cls.i32, cls.device = torch.float32, torch.int32, torch.cuda.current_device
         cls.codes = {torch.float32: MF_F32, torch.float16: MF_F16, torch.bfloat16: MF_BF16}
         cls.of = {code: dtype for dtype, code in cls.codes.items()}
 
@@ -729,7 +729,8 @@ _NO_CUTS = Cuts()
 def mf_verify(logits, row_start, tokens, u, noise, token, accepted, work, logprob=None, cuts: Cuts | None = None, draft_logits=None,
               draft_cuts: Cuts | None = None, stream=None) -> None:
     """Drafted tokens taken or refused, and the token that ends each sequence (see mawforge.h).  logits and draft_logits [rows][vocab] of
-    one type, noise float32 [sequences][vocab], u and logprob float32, row_start, tokens, token and accepted int32, work uint8."""
+    one type on the current device, noise float32 [sequences][vocab], u and logprob float32, row_start, tokens, token and accepted
+    int32, work uint8."""
     w = "mf_verify"
     if not _Types.codes:
         _Types.load()
@@ -745,6 +746,8 @@ def mf_verify(logits, row_start, tokens, u, noise, token, accepted, work, logpro
         draft, draft_stride = draft_logits.data_ptr(), draft_logits.stride(0)
     ls, ns = logits.stride(), noise.stride()
     if ls[1] != 1 or ns[1] != 1 or not ((logits.is_cuda or logits.is_pinned()) and (noise.is_cuda or noise.is_pinned())):
+        raise MFError(MF_E_INVAL, w)
+    if logits.is_cuda and logits.get_device() != _Types.device():
         raise MFError(MF_E_INVAL, w)
     cuts, draft_cuts = cuts or _NO_CUTS, draft_cuts or _NO_CUTS
     need = _u64()

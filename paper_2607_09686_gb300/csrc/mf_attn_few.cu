@@ -62,6 +62,18 @@ __device__ __forceinline__ Span span_of(const AttnCall& c, int s) {
 }
 
 __device__ __forceinline__ Span span_of(const AttnCall& c, const Alone&, int s) { return span_of(c, s); }
+// What the plan of such a step left, read where the kernel does not wait for the one before it: past the L1 cache, and in its place in
+// the program.
+__device__ __forceinline__ int4 planned(const int4* p) {
+  int4 v;
+  asm volatile("ld.global.cg.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ longlong2 planned2(const int4* p) {
+  longlong2 v;
+  asm volatile("ld.global.cg.v2.s64 {%0, %1}, [%2];" : "=l"(v.x), "=l"(v.y) : "l"(p) : "memory");
+  return v;
+}
 __device__ __forceinline__ Span span_of(int4 x, int row) {
   Span r;
   r.sp = {x.x, x.y, x.z};
@@ -72,7 +84,7 @@ __device__ __forceinline__ Span span_of(int4 x, int row) {
   return r;
 }
 __device__ __forceinline__ Span span_of(const AttnCall&, const FewShared& f, int v) {
-  return span_of(f.span[v], v < f.groups ? f.group[v].x : v - f.groups);
+  return span_of(planned(f.span + v), v < f.groups ? planned(f.group + v).x : v - f.groups);
 }
 
 // a place in a block's share of the list
@@ -196,10 +208,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
   }
   Cursor<Extra> cur;
   if constexpr (kShared) {
-    // (ordinary loads: read-only ones may be moved ahead of the wait)
     const int4* at = extra.start + blockIdx.x * 4;
-    const int4 x = at[0], y = at[1];
-    const longlong2 u = *reinterpret_cast<const longlong2*>(at + 2), w = *reinterpret_cast<const longlong2*>(at + 3);
+    const int4 x = planned(at), y = planned(at + 1);
+    const longlong2 u = planned2(at + 2), w = planned2(at + 3);
     B = x.w, total = w.y, t0 = u.y, t1 = w.x;
     cur.s = x.x, cur.h = x.y, cur.at = u.x;
     cur.sn = span_of(y, x.z);
@@ -481,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<D>::kBlocksPerSm) k_attn_few(Att
       const int rows = cur.sn.sp.n * st.G;
       if constexpr (kShared) {
         if (j0 == 0 && tid == 0)
-          extra.runs[cur.s * st.Hkv + cur.h] = make_int2(
+          extra.runs[(int64_t)cur.s * st.Hkv + cur.h] = make_int2(
               blockIdx.x, whole ? 1 : (int)((B * (cur.at + kOver + cur.sn.nt) - 1) / total) - (int)blockIdx.x + 1);
       }
       if (!kShared && j0 == 0 && !whole && tid == 0) {  // the block of the last tile has the last piece

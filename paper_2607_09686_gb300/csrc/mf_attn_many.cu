@@ -1192,7 +1192,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_
   int2 own;
   if constexpr (kFewSeqs) {
     s = blockIdx.x;
-    own = sp.runs[(few_groups + s) * st.Hkv + h];
+    own = sp.runs[(int64_t)(few_groups + s) * st.Hkv + h];
   } else {
     const int tile = p.first[p.groups] + (int)blockIdx.x;
     if (tile >= p.first[p.groups + p.seqs]) return;
@@ -1236,7 +1236,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_
     const int64_t at = (int64_t)(tok - ja.z) * st.G + R % st.G;  // the row among the group's
     if (at >= 0 && at < (int64_t)ja.w * st.G) {
       if constexpr (kFewGroups) {
-        set_few(0, sp.runs[jb.x * st.Hkv + h], (int64_t)tok * st.Hq + head, (int)at);
+        set_few(0, sp.runs[(int64_t)jb.x * st.Hkv + h], (int64_t)tok * st.Hq + head, (int)at);
       } else {
         const int t = (int)(at / C::kRows);
         if (t < jb.y)
