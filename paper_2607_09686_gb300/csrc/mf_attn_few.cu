@@ -21,6 +21,7 @@
 // Measured: 64 sequences of 166 to 8192 lines, 32/4 heads of 128, 395 MB: 74.5 us with the join, 5.3 TB/s (78 % of the copy
 // rate; that rate once it runs, 6 us before the first lines are there); one sequence of 131071 lines, 16/2 heads of 256:
 // 54.9 us, 4.9 TB/s; one of 1001 lines: 9.8 us, of which 5 are this kernel's and the rest the join's and the launches'.
+// Lines that follow shared ones (FewShared): 64 sequences of up to 1000, 46 MB, 14 us, 2.5 until the first copies are asked for.
 #include <type_traits>
 
 #include "mf_attn.cuh"
