@@ -1169,7 +1169,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_attn_many(const __grid_constant
 // of a row's pieces; then a thread has four columns of a row and, where rows times columns are fewer than threads, every P-th
 // piece.  kFewGroups, kFewSeqs: the groups' lines, the sequences' own were the kernel's of few rows.
 // Bounded by the latency of 20 pieces a row, 16 bytes a thread each, eight under way: 2048 rows of 128 columns (22 MB) 9 us.
-constexpr int kJoinThreads = 512, kJoinRows = 8, kJoinPieces = 512;
+constexpr int kJoinRows = 8, kJoinThreads = 512, kJoinPieces = 512;
 struct JoinPiece {
   uint32_t at;  // 16-byte vectors from the workspace's beginning to the row's first columns
   float w;
@@ -1185,6 +1185,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_
                                                                    const __grid_constant__ AttnParts few, const float* mem, int few_rows, int few_groups) {
   using C = Cfg<D>;
   constexpr int kCols = D / 4;
+  static_assert(kJoinThreads / 2 >= 32 * kJoinRows, "a warp for each row's weights");
   __shared__ JoinPiece s_piece[kJoinRows][kJoinPieces + 1];  // (rows in other banks)
   __shared__ float4 s_o[kJoinThreads];
   __shared__ JoinRow s_row[kJoinRows];
@@ -1275,9 +1276,9 @@ __global__ void __launch_bounds__(kJoinThreads) k_attn_join_shared(const __grid_
     }
   }
   __syncthreads();
-  const int items = rows * kCols, P = items < kJoinThreads ? kJoinThreads / items : 1;
+  const int threads = blockDim.x, items = rows * kCols, P = items < threads ? threads / items : 1;
   const float4* vectors = reinterpret_cast<const float4*>(mem);
-  for (int i0 = 0; i0 < items; i0 += kJoinThreads) {
+  for (int i0 = 0; i0 < items; i0 += threads) {
     const int pg = P > 1 ? tid / items : 0, i = P > 1 ? tid - pg * items : i0 + tid;
     // (neighbouring threads take what neighbours in memory: columns, or rows as tiles leave them)
     const int w = kFewGroups ? i / kCols : i % rows, col = kFewGroups ? i % kCols : i / rows;
@@ -1371,8 +1372,12 @@ cudaError_t run_shared(const AttnCall& c, const AttnMaps& maps, const SharedGrou
   if (e != cudaSuccess) return e;
   const int64_t in_tile = few_seqs || seq_rows < C::kRows ? seq_rows : C::kRows;
   const dim3 blocks((unsigned)(few_seqs ? c.st.n_seqs : own), (unsigned)c.st.Hkv, (unsigned)((in_tile + kJoinRows - 1) / kJoinRows));
+  // Few blocks: threads, for the latency of a row's pieces; more than two an SM: room for others.  512 and 256 threads, 32/4 heads of 128, a
+  // group's 16384 lines, in a graph: 16 sequences 36.9 us and 42.8, 64 (256 blocks) 49.8 and 53.3, two groups of 64 74.9 and 72.5, eight 204
+  // and 197; 48 sequences of up to 5 tokens, 32/8 heads of 64, 49.4 and 46.1.
+  const int join_threads = (int64_t)blocks.x * blocks.y * blocks.z <= 2 * sms ? kJoinThreads : kJoinThreads / 2;
   auto join = few_groups ? k_attn_join_shared<T, D, true, true> : few_seqs ? k_attn_join_shared<T, D, false, true> : k_attn_join_shared<T, D, false, false>;
-  return launch_pdl(true, join, blocks, dim3(kJoinThreads), 0, s, c, plan, sh.found, sh.parts, sh.few, reinterpret_cast<const float*>(sh.mem), attn_few_part_rows(few_rows),
+  return launch_pdl(true, join, blocks, dim3(join_threads), 0, s, c, plan, sh.found, sh.parts, sh.few, reinterpret_cast<const float*>(sh.mem), attn_few_part_rows(few_rows),
                     n_few_groups);
 }
 
