@@ -141,12 +141,14 @@ __device__ __forceinline__ int64_t quick_div(int64_t a, int64_t b) {
 // that rise, lengths that all their sequences have; a group of one shares nothing.  p.groups and p.seqs say which of them are in the list
 // of this file's kernel, few_groups and few_seqs which are in that of few rows.  Two blocks, both of which find the groups: the first lays out this
 // file's list and says where its kernel's blocks begin, the second the other list, and what the join asks for.  Its time is a chain of
-// loads and scans: 64 sequences, one group, 6 us.  Then the step of 64 tokens behind 16384 lines, 32/4 heads of 128: the group's 2048
-// jobs from 6.5 to 24 us (4.5 until the first scores, 13 for 13.5 jobs a block), the sequences' own lines to 38 (few rows), the join to 47.
+// loads and scans: 64 sequences, one group, 5 us (blocks of 512 threads; of 1024 a microsecond more, of 256 half of one).  Then the step of
+// 64 tokens behind 16384 lines, 32/4 heads of 128: the group's 2048 jobs from 5.5 to 23 us (4.5 until the first scores, 13 for 13.5 jobs
+// a block), the sequences' own lines to 37 (few rows), the join to 46.
+constexpr int kPlanThreads = 512;
 template <int D>
-__global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGroups g, AttnPlan p, SharedPlan sp, int few_groups,
+__global__ void __launch_bounds__(kPlanThreads) k_attn_plan_shared(AttnCall c, SharedGroups g, AttnPlan p, SharedPlan sp, int few_groups,
                                                            int few_seqs, int blocks, int few_blocks) {
-  __shared__ int64_t s_warp[32];
+  __shared__ int64_t s_warp[kPlanThreads / 32];
   // what the phases hand on, in shared memory where it finds room: the sequences' spans and groups, the groups, first row tiles
   constexpr int kSmall = 1024;
   __shared__ SeqSpan s_span[kSmall];
@@ -176,7 +178,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     __syncthreads();
     if (lane == 31) s_warp[warp] = x;
     __syncthreads();
-    int64_t mine = s_warp[lane], total = mine;  // (each warp adds up all of them)
+    int64_t mine = lane < kPlanThreads / 32 ? s_warp[lane] : 0, total = mine;  // (each warp adds up all of them)
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const int64_t o = __shfl_up_sync(0xffffffffu, total, d);
@@ -186,16 +188,16 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     return __shfl_sync(0xffffffffu, total - mine, warp) + x - v;
   };
   int width = 32;
-  while (width > 1 && (int64_t)width * g.n > 1024) width >>= 1;
-  const int per = 1024 / width, sub = tid % width;
+  while (width > 1 && (int64_t)width * g.n > kPlanThreads) width >>= 1;
+  const int per = kPlanThreads / width, sub = tid % width;
   const int first_raw = g.n && tid <= g.n ? g.first[tid] : 0, len_raw = tid / width < g.n ? g.len[tid / width] : 0;  // (with the spans)
-  for (int s = tid; s < n_seqs; s += 1024) {
+  for (int s = tid; s < n_seqs; s += kPlanThreads) {
     if (small_seqs) s_span[s] = seq_span(c.st, s);
     seq[s] = make_int2(-1, 0);
   }
   // ---- the groups' bounds: the largest so far, inside the step
   int from = 0;
-  for (int base = 0; base <= g.n; base += 1024) {
+  for (int base = 0; base <= g.n; base += kPlanThreads) {
     const int i = base + tid;
     const int raw = base == 0 ? first_raw : i <= g.n ? g.first[i] : 0;
     int x = min(max(raw, 0), n_seqs);
@@ -207,7 +209,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     __syncthreads();
     if (lane == 31) s_warp[warp] = x;
     __syncthreads();
-    const int theirs = (int)s_warp[lane];
+    const int theirs = lane < kPlanThreads / 32 ? (int)s_warp[lane] : 0;
     x = max(max(x, from), __reduce_max_sync(0xffffffffu, lane < warp ? theirs : 0));
     from = max(from, __reduce_max_sync(0xffffffffu, theirs));
     if (i <= g.n) {
@@ -242,7 +244,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
   __syncthreads();
   // ---- row tiles of the virtual sequences
   int64_t done = 0;
-  for (int base = 0; base < V; base += 1024) {
+  for (int base = 0; base < V; base += kPlanThreads) {
     const int v = base + tid;
     int64_t n = 0, all;
     if (v < V) {
@@ -259,7 +261,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
   if (lists) {
     int64_t* before = tiles <= kSmall ? s_before : p.before;
     int64_t jobs = 0;
-    for (int base = 0; base < tiles; base += 1024) {
+    for (int base = 0; base < tiles; base += kPlanThreads) {
       const int i = base + tid;
       int64_t n = 0;
       if (i < tiles) {
@@ -294,7 +296,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     __syncthreads();
     // ---- where the blocks begin: every one that works has two jobs at least, so that it has a key tile's start
     const int64_t total = jobs * c.st.Hkv, B = max((int64_t)1, min((int64_t)blocks, total / 2));
-    for (int b = tid; b < blocks; b += 1024) {
+    for (int b = tid; b < blocks; b += kPlanThreads) {
       const int64_t t0 = b < B ? quick_div(total * b, B) : 0, t1 = b < B ? quick_div(total * (b + 1), B) : 0;
       int tile = 0, h = 0;
       int64_t at = 0;
@@ -326,7 +328,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
   // ---- the list of few rows
   int64_t* before = few <= kSmall ? s_before : sp.before;
   done = 0;
-  for (int base = 0; base < few; base += 1024) {
+  for (int base = 0; base < few; base += kPlanThreads) {
     const int v = base + tid;
     int64_t n = 0, all;
     if (v < few) {
@@ -348,7 +350,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
   if (tid == 0 && few) before[few] = done;
   __syncthreads();
   const int64_t B = min((int64_t)few_blocks, done);
-  for (int b = tid; b < few_blocks && few; b += 1024) {
+  for (int b = tid; b < few_blocks && few; b += kPlanThreads) {
     const int64_t t0 = b < B ? quick_div(done * b, B) : 0, t1 = b < B ? quick_div(done * (b + 1), B) : 0;
     int v = 0, h = 0, row = 0;
     int64_t at = 0;
@@ -377,7 +379,7 @@ __global__ void __launch_bounds__(1024) k_attn_plan_shared(AttnCall c, SharedGro
     reinterpret_cast<longlong2*>(to)[2] = make_longlong2(at, t0), reinterpret_cast<longlong2*>(to)[3] = make_longlong2(t1, done);
   }
   // ---- what the join asks for
-  for (int s = tid; s < n_seqs; s += 1024) {
+  for (int s = tid; s < n_seqs; s += kPlanThreads) {
     const SeqSpan q = span(s);
     const int gi = seq[s].x;
     int4 x = make_int4(0, 0, 0, 0);
@@ -1356,7 +1358,7 @@ cudaError_t run_shared(const AttnCall& c, const AttnMaps& maps, const SharedGrou
   if (few_blocks + sms + 2 > kJoinPieces) return cudaErrorInvalidConfiguration;  // (a row's pieces: no more than blocks, and one of each list)
   const int64_t most = tiles * c.st.Hkv * (((int64_t)c.st.cap + kKeys - 1) / kKeys);
   const unsigned grid = (unsigned)(most < sms ? most : sms);
-  cudaError_t e = launch_pdl(true, k_attn_plan_shared<D>, dim3(2), dim3(1024), 0, s, c, g, plan, sh.found, n_few_groups, few_seqs ? c.st.n_seqs : 0,
+  cudaError_t e = launch_pdl(true, k_attn_plan_shared<D>, dim3(2), dim3(kPlanThreads), 0, s, c, g, plan, sh.found, n_few_groups, few_seqs ? c.st.n_seqs : 0,
                              (int)grid, few_blocks);
   if (e == cudaSuccess && tiles) {
     constexpr size_t smem = smem_of(C::kTail);
