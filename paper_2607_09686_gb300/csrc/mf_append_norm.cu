@@ -8,9 +8,9 @@
 // shared memory, laid out as the lanes read them, and each thread takes two items at a time.  Arithmetic on pairs of floats (f32x2).
 //
 // Measured, in a graph: 8192 tokens of 32 + 2 x 4 heads of 128 (168 MB and the angles) 38.2 us, 4.5 TB/s, 65 % of the issue slots (the
-// append without norms 36.2); three prompts, 5400 tokens in all, of 16 + 2 x 4 heads of 256, fp16, a quarter rotated by three axes 35.0 us, 3.8 TB/s (28.5); one
-// token 3.1 us, 64 tokens 3.9.  Four tokens a block where that gives two blocks an SM (two tokens 45.6 and 39.7 us, eight 36.6 and 38.9), else
-// one, for latency; four blocks an SM (three 43.8 and 35.7, five, with registers spilled, 40.1 and 35.0).
+// append without norms 36.2); three prompts, 5400 tokens in all, of 16 + 2 x 4 heads of 256, fp16, a quarter rotated by three axes 35.0
+// us, 3.8 TB/s (28.5); one token 3.1 us, 64 tokens 3.9.  Four tokens a block where that gives two blocks an SM (two tokens 45.6 and 39.7
+// us, eight 36.6 and 38.9), else one, for latency; four blocks an SM (three 43.8 and 35.7, five, with registers spilled, 40.1 and 35.0).
 #include "mf_attn.cuh"
 #include "mf_tc.cuh"
 

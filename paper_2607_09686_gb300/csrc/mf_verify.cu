@@ -298,8 +298,8 @@ struct Best {  // the largest key so far, the lowest index where equal
 // drafter's where they count, and the noise.  A copy covers whole 16-byte vectors inside its row; what is left of a row's ends, and
 // chunks whose copies do not arrive in time, are read where they lie.  Each thread keeps the two largest bounds of its keys: log p + noise
 // + log(1 - q / p) by approximate exponentials, with a margin for all roundings; an entry that the drafter may not have kept counts as if it had
-// not.  The first chunk's largest key spares most of what follows all but the bound by p alone.  With the largest bound's key worked out, no entry whose bound lies below the block's largest key can be the one; a thread whose second does
-// not looks at all its entries.
+// not.  The first chunk's largest key spares most of what follows all but the bound by p alone.  With the largest bound's key worked out, no
+// entry whose bound lies below the block's largest key can be the one; a thread whose second does not looks at all its entries.
 constexpr int kU = 8, kChunk = kU * kThreads, kMostStages = 8;  // entries of a thread, of a chunk
 constexpr int kTogether = kWarps;               // rows that are looked at together, a warp each
 template <class T>
