@@ -393,7 +393,7 @@ extern "C" int mf_attn_share(mf_attn_t* attn, int max_groups) {
   const int64_t tiles = 2 * (group_rows / tile) + attn->max_seqs + max_groups, part_rows = (int64_t)attn->sms * 2 * tile;
   Carve w;
   const size_t o_bound = w.take(((size_t)max_groups + 1) * 4), o_group = w.take((size_t)max_groups * 16),
-               o_seq = w.take((size_t)attn->max_seqs * 8), o_first = w.take(((size_t)attn->max_seqs + max_groups + 1) * 4),
+               o_seq = w.take((size_t)attn->max_seqs * 16), o_first = w.take(((size_t)attn->max_seqs + max_groups + 1) * 4),
                o_tile = w.take((size_t)tiles * 32), o_before = w.take(((size_t)tiles + 1) * 8),
                o_o = w.take((size_t)part_rows * sh.head_dim * 4), o_ml = w.take((size_t)part_rows * 8),
                o_few = w.take((size_t)attn_few_blocks(attn->sms) * 2 * attn_few_rows(sh.head_dim) * sh.head_dim * 4),

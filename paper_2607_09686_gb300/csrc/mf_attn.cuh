@@ -183,7 +183,7 @@ struct AttnPlan {
 struct SharedPlan {
   int* bound;   // [max_groups + 1] first sequence of a group
   int4* group;  // [max_groups]     that, its first token, tokens (0: nothing is shared), lines that are shared
-  int2* seq;    // [max_seqs]       a sequence's group (-1: none), the lines it shares
+  int2* seq;    // [2][max_seqs]    a sequence's group (-1: none), the lines it shares, for each of the plan's blocks
   // for the join: a sequence's first token and tokens, its group's; the group's place in the list of few rows or its first row tile,
   // its row tiles
   int4* join;   // [max_seqs][2]

@@ -140,7 +140,8 @@ __device__ __forceinline__ int64_t quick_div(int64_t a, int64_t b) {
 // all the group's tokens and the shared lines (whole pages of them), then the sequences, with what follows.  First the groups: bounds
 // that rise, lengths that all their sequences have; a group of one shares nothing.  p.groups and p.seqs say which of them are in the list
 // of this file's kernel, few_groups and few_seqs which are in that of few rows.  Two blocks, both of which find the groups: the first lays out this
-// file's list and says where its kernel's blocks begin, the second the other list, and what the join asks for.  Its time is a chain of
+// file's list and says where its kernel's blocks begin, the second the other list, and what the join asks for.  Nothing orders the two: what both
+// write to one place (bounds, groups, first row tiles, of steps too large for shared memory) is written once, with the same value.  Its time is a chain of
 // loads and scans: 64 sequences, one group, 5 us (blocks of 512 threads; of 1024 a microsecond more, of 256 half of one).  Then the step of
 // 64 tokens behind 16384 lines, 32/4 heads of 128: the group's 2048 jobs from 5.5 to 23 us (4.5 until the first scores, 13 for 13.5 jobs
 // a block), the sequences' own lines to 37 (few rows), the join to 46.
@@ -161,7 +162,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_attn_plan_shared(AttnCall c, S
   const bool small_seqs = n_seqs <= kSmall, small_groups = g.n <= kSmall / 4, small = V <= kSmall;
   int* bound = small_groups ? s_bound : sp.bound;
   int4* group = small_groups ? s_group : sp.group;
-  int2* seq = small_seqs ? s_seq : sp.seq;
+  int2* seq = small_seqs ? s_seq : sp.seq + (int64_t)blockIdx.x * n_seqs;  // (written twice: a block's own)
   int* first = small ? s_first : p.first;
   const bool lists = blockIdx.x == 0;
   if (lists && V == 0) return;

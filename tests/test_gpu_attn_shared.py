@@ -325,3 +325,30 @@ def test_refusals(mf):
             make()
     assert mf.mf_attn_check(at) == 0
     mf.mf_attn_destroy(at)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [lambda i: 1, lambda i: 30 if i % 50 == 0 else 1 + (i % 7 == 0), lambda i: int(i % 60 == 1)],
+                         ids=["single tokens", "some with many rows", "most without tokens"])
+def test_many_sequences_that_share(mf, d, new):
+    """More sequences than the plan holds in shared memory, with lines in common: those of few rows, of many, and groups that have few rows
+    themselves.  The same bits again, also beside another stream's kernels, which let the plan's blocks begin at different times."""
+    n, first, lens = 1100, [0, 3, 400, 1090], [70, 33, 100]
+    of = [sum(i >= f for f in first[1:]) for i in range(n)]
+    c = ref.Case([new(i) for i in range(n)], [(lens + [0])[of[i]] + (i * 37) % 50 for i in range(n)], 4, 2, d, "f16")
+    want = check(mf, c, first, lens)
+    at, i32 = c.attn(mf), dict(dtype=torch.int32, device="cuda")
+    mf.mf_attn_share(at, 3)
+    groups = mf.shared(torch.tensor(first, **i32), torch.tensor(lens, **i32))
+    outs = torch.full((40, *want.shape), 7.0, dtype=want.dtype, device="cuda")
+    other, x = torch.cuda.Stream(), torch.randn(2048, 2048, device="cuda")
+    other.wait_stream(torch.cuda.current_stream())
+    for out in outs:
+        with torch.cuda.stream(other):
+            for _ in range(3):
+                x.mul_(0.5)
+        mf.mf_attn_forward_shared(at, mf.kv_cache(c.k, c.v), c.step(mf), groups, c.q, out, scale=1 / math.sqrt(d))
+    torch.cuda.synchronize()
+    assert mf.mf_attn_check(at) == 0
+    mf.mf_attn_destroy(at)
+    assert (outs.view(torch.int16) == want.view(torch.int16)).all()
