@@ -497,7 +497,7 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
     b.take(fmaxf(key + noise[e], -INFINITY), lp, e);
   };
   float reach = -INFINITY, reach2 = -INFINITY, floor = -INFINITY;
-  int at = -1;
+  int at = -1, filled = 0;  // chunks whose copies were issued
   if (warp == kWarps) {
     // ================= copies
     if (lane == 0) {
@@ -508,7 +508,9 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
           s_lost = 1;
           break;
         }
+        if (s_lost) break;  // (let go without its copies, which may be on their way)
         fill(k, stage);
+        ++filled;
         if (++stage == stages) stage = 0, phase ^= 1;
       }
     }
@@ -626,7 +628,7 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
   }
   // no copy may be in flight when the block exits (one that was not waited for: its chunk was read without it)
   if (tid == kThreads && s_lost && !c.hold)
-    for (int i = 0; i < min(stages, chunks); ++i) mbar_wait(&s_full[i], 0, kDefaultWaitNs), mbar_wait(&s_full[i], 1, kDefaultWaitNs);
+    for (int k = max(0, filled - stages); k < filled; ++k) mbar_wait(&s_full[k % stages], (k / stages) & 1, kDefaultWaitNs);
 
   if (rank != 0) return;
   const bool empty = b.i == none.i;

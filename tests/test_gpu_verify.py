@@ -393,3 +393,43 @@ def test_tensors_that_do_not_fit_are_refused(mf):
     refused(draft_cuts=short)
     mf.mf_verify(**good)
     torch.cuda.synchronize()
+
+
+def refused_at_once(b, token, accepted, lp):
+    """Every first draft was refused (u above 1): the tokens against the formula, by torch in 64 bits.  A key is right to 2e-5 of p + q over
+    p - q and 1e-6 of the noise (see above): the one that is taken may lie below the largest by both keys' part of that."""
+    for s in range(b.n):
+        row = b.starts[s]
+        p = torch.softmax(b.logits[row].double(), 0)
+        if b.draft is None:
+            q = torch.zeros_like(p)
+            q[b.tokens[row + 1].long()] = 1
+        else:
+            q = torch.softmax(b.draft[row].double(), 0)
+        rest, g = p - q, b.noise[s].double()
+        key = torch.where(rest > 0, rest.clamp_min(1e-300).log() + g, -math.inf)
+        off = torch.where(rest > 0, 2e-5 * (p + q) / rest.clamp_min(1e-300) + 1e-6 * g.abs(), 0.0)
+        t, best = int(token[row]), int(key.argmax())
+        assert rest[t] > 0 and key[t] >= key[best] - off[t] - off[best], (s, t, best)
+        assert abs(float(lp[row]) - float(p[t].log())) <= 2e-5 * max(1.0, abs(float(p[t].log())))
+        assert (token[row + 1:b.starts[s + 1]] == -1).all()
+    assert accepted.tolist() == [0] * b.n
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("model", [True, False])
+def test_copies_of_more_chunks_than_the_ring_holds_that_do_not_arrive(mf, model, dtype):
+    """Nothing is cut, so that only the pass over the deciding row copies: 16 chunks a block, 8 stages.  Stages whose copies were given up are
+    not filled again."""
+    b = Batch([1, 2], 1 << 18, dtype, model)
+    b.u.fill_(1.5)
+    want = b.run(mf)
+    refused_at_once(b, *want)
+    mf.mf_sample_test_hold(1)
+    try:
+        got = b.run(mf)
+        torch.cuda.synchronize()
+    finally:
+        mf.mf_sample_test_hold(0)
+    assert all(torch.equal(p, q) for p, q in zip(want, got))
+    assert all(torch.equal(p, q) for p, q in zip(want, b.run(mf)))
