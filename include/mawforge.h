@@ -562,8 +562,8 @@ typedef struct mf_cuts {
  *   token     device int32 [n_rows]: the drafts that were taken, then the new token (-1 where its row has no p), -1 in the rows after it
  *   accepted  device int32 [n_seqs]: the number of drafts taken
  *   logprob   device float [n_rows] or NULL: log p of each token in `token`, -inf beside -1
- * Outputs overlap no input.  Rows of no sequence are left as they were; row starts that fall or lie outside the rows are taken as the
- * nearest valid ones; a sequence without rows gets accepted = 0.
+ * Outputs overlap no input.  Rows of no sequence are left as they were; row starts that lie outside the rows, or below an
+ * earlier one, are taken as the nearest valid ones (the largest so far); a sequence without rows gets accepted = 0.
  *   work      device, 16-byte aligned, mf_verify_bytes of it; calls that share it must follow one another
  * vocab from 1 to 2^20.  Other pointers aligned to their element. */
 typedef struct mf_verify_args {

@@ -70,6 +70,7 @@ struct KeptCall : SampleCall {
   const int32_t* row_start;
   mf_cuts_t draft_cuts;
   Kept* kept;
+  int* fall;
   int n_seqs, n_rows;
   int row0;  // of the target's rows and then the drafter's
 };
@@ -119,6 +120,15 @@ struct Shared {
   uint64_t bar;  // the bulk copies' barrier
 };
 
+// By one warp: whether row starts fall.
+__device__ __noinline__ void note_fall(const int32_t* row_start, int n_seqs, int* out) {
+  bool fall = false;
+#pragma unroll 4
+  for (int i = threadIdx.x & 31; i < n_seqs; i += 32) fall |= __ldg(row_start + i) > __ldg(row_start + i + 1);
+  fall = __any_sync(0xffffffffu, fall);
+  if ((threadIdx.x & 31) == 0) *out = fall;
+}
+
 template <class T, class Call>
 __global__ void __launch_bounds__(kThreads, 2) k_sample(Call c) {
   constexpr bool kKept = std::is_same<Call, KeptCall>::value;
@@ -142,15 +152,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(Call c) {
   bool drafters = false;
   if constexpr (kKept) {
     const int i = r % c.n_rows;
-    int lo = 0, hi = c.n_seqs - 1;  // the last sequence that begins at or before the row
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (__ldg(c.row_start + mid) <= i) lo = mid;
-      else hi = mid - 1;
-    }
-    const RowSpan sp = row_span(c.row_start, c.n_rows, lo);
-    if (i < sp.b || i >= sp.e || (r != i && i + 1 == sp.e)) return;  // (the whole cluster)
-    rs = lo;
+    if (blockIdx.x == 0 && warp == kWarps - 1 && c.n_seqs > 1) note_fall(c.row_start, c.n_seqs, c.fall);
+    const int2 own = row_owner_any(c.row_start, c.n_rows, c.n_seqs, i);
+    if (own.x < 0 || (r != i && i + 1 == own.y)) return;  // (the whole cluster)
+    rs = own.x;
     if (r != i) {
       row = static_cast<const T*>(c.draft) + (int64_t)i * c.draft_stride + base;
       drafters = true;
@@ -1193,7 +1198,7 @@ cudaError_t launch_kept(const KeptRows& k, cudaStream_t s) {
   c.logits = k.logits, c.logits_stride = k.logits_stride, c.vocab = k.vocab, c.hold = g_hold.load();
   c.temperature = k.cuts.temperature, c.top_p = k.cuts.top_p, c.min_p = k.cuts.min_p, c.top_k = k.cuts.top_k;
   c.draft = k.draft, c.draft_stride = k.draft_stride, c.draft_cuts = k.draft_cuts;
-  c.row_start = k.row_start, c.n_seqs = k.n_seqs, c.n_rows = k.n_rows, c.kept = k.kept;
+  c.row_start = k.row_start, c.n_seqs = k.n_seqs, c.n_rows = k.n_rows, c.kept = k.kept, c.fall = k.fall;
   c.row0 = k.target ? 0 : k.n_rows;
   const int rows = (k.target ? k.n_rows : 0) + (k.draft ? k.n_rows : 0);
   return k.dtype == MF_F32 ? run<float>(c, rows, s) : k.dtype == MF_F16 ? run<__half>(c, rows, s) : run<__nv_bfloat16>(c, rows, s);

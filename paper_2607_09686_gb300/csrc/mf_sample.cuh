@@ -32,18 +32,71 @@ struct KeptRows {
   const int32_t* row_start;
   mf_cuts_t cuts, draft_cuts;
   Kept* kept;
+  int* fall;  // is set to whether a start lies below the one before it
   int n_seqs, n_rows, vocab, dtype, target;
 };
 cudaError_t launch_kept(const KeptRows& rows, cudaStream_t s);
 int sample_hold();  // mf_sample_test_hold
 
-// The rows of a sequence, inside [0, n_rows].
+// The rows of a sequence, inside [0, n_rows], where the starts rise.
 struct RowSpan {
   int b, e;
 };
+__device__ __forceinline__ int row_at(const int32_t* row_start, int n_rows, int i) { return min(max(__ldg(row_start + i), 0), n_rows); }
 __device__ __forceinline__ RowSpan row_span(const int32_t* row_start, int n_rows, int s) {
-  const int b = min(max(__ldg(row_start + s), 0), n_rows);
-  return {b, min(max(__ldg(row_start + s + 1), b), n_rows)};
+  const int b = row_at(row_start, n_rows, s);
+  return {b, max(row_at(row_start, n_rows, s + 1), b)};
+}
+// Where they do not, a start is the largest so far, and rows still have one sequence at most.  Whether one of starts 1 .. n lies below
+// the one before it, as far as this thread of the block looks.
+__device__ __forceinline__ bool starts_fall(const int32_t* row_start, int n) {
+  bool fall = false;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < n; i += blockDim.x) fall |= __ldg(row_start + i) > __ldg(row_start + i + 1);
+  return fall;
+}
+// Then the rows of a sequence (every lane of the warp).
+static __device__ __noinline__ RowSpan row_span_fallen(const int32_t* row_start, int n_rows, int s) {
+  int b = 0;
+  for (int i = threadIdx.x & 31; i <= s; i += 32) b = max(b, row_at(row_start, n_rows, i));
+  b = __reduce_max_sync(0xffffffffu, b);
+  return {b, max(b, row_at(row_start, n_rows, s + 1))};
+}
+// A row's sequence (-1: none), which is the last that begins at or before it, the one before the first that begins behind it where starts
+// fall, and where that ends (every lane of the warp).
+static __device__ __noinline__ int2 row_owner(const int32_t* row_start, int n_rows, int n_seqs, int row, bool fall) {
+  if (!fall) {
+    int lo = 0, hi = n_seqs - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (__ldg(row_start + mid) <= row) lo = mid;
+      else hi = mid - 1;
+    }
+    const RowSpan sp = row_span(row_start, n_rows, lo);
+    return make_int2(row >= sp.b && row < sp.e ? lo : -1, sp.e);
+  }
+  for (int base = 0; base <= n_seqs; base += 32) {
+    const int i = base + (int)(threadIdx.x & 31), at = i <= n_seqs ? row_at(row_start, n_rows, i) : 0;
+    const unsigned behind = __ballot_sync(0xffffffffu, at > row);
+    if (behind) return make_int2(base + __ffs(behind) - 2, __shfl_sync(0xffffffffu, at, __ffs(behind) - 1));
+  }
+  return make_int2(-1, 0);
+}
+// The same in either case, by every thread of the block: of few sequences all starts are read at once.
+constexpr int kFewStarts = 4 * 32;
+__device__ __forceinline__ int2 row_owner_any(const int32_t* row_start, int n_rows, int n_seqs, int row) {
+  if (n_seqs >= kFewStarts) return row_owner(row_start, n_rows, n_seqs, row, __syncthreads_or(starts_fall(row_start, n_seqs)));
+  const int lane = threadIdx.x & 31;
+  int at[kFewStarts / 32];
+#pragma unroll
+  for (int k = 0; k < kFewStarts / 32; ++k) at[k] = 32 * k + lane <= n_seqs ? row_at(row_start, n_rows, 32 * k + lane) : 0;
+  int2 own = make_int2(-1, 0);
+#pragma unroll
+  for (int k = kFewStarts / 32 - 1; k >= 0; --k) {
+    const unsigned behind = __ballot_sync(0xffffffffu, at[k] > row);
+    if (behind) own = make_int2(32 * k + __ffs(behind) - 2, __shfl_sync(0xffffffffu, at[k], __ffs(behind) - 1));
+  }
+  return own;
 }
 
 }  // namespace mf

@@ -45,6 +45,7 @@ struct VerifyCall {
   float* logprob;
   const Kept* kept;   // [2][rows], of rows that are cut
   Piece* pieces;      // [2][rows][n_units], of others
+  int* fall;          // the kernels before k_verify set it to whether row starts fall (of one sequence: they cannot matter)
   int whole[2];       // the target's, the drafter's are not cut
   int n_seqs, n_rows, vocab, n_units, slice;  // units of a row (k_rows); slice: entries of a block of k_verify
   int stages;  // of k_verify's ring
@@ -56,7 +57,7 @@ struct VerifyCall {
 // The rows' units of 128 16-byte vectors are one list, shared out evenly: a warp takes a run of units, four vectors a lane at a time while the
 // next four are under way, with a running maximum and sum a lane, and leaves a piece where a row or its run ends (which depends on
 // the row starts alone).  The list has the target's rows and those of the drafter's that have a draft: every block adds up the sequences' rows
-// in shared memory (of more than kSeqs sequences, or bounds that overlap: all rows, of which some are passed over).  Bounded by
+// in shared memory (of more than kSeqs sequences, or starts that fall: all rows, of which some are passed over).  Bounded by
 // reading the logits once; of an entry's four instructions (pairs of floats) one is an exponential.
 constexpr int kRowThreads = 256, kUnit = 128, kVecs = kUnit / 32, kSeqs = 2048;
 template <class T>
@@ -110,9 +111,8 @@ __global__ void __launch_bounds__(kRowThreads, 3) k_rows(const __grid_constant__
   pdl_wait();
   pdl_trigger();
   int listed = rows, target = side0 ? 0 : c.n_rows;  // rows of the list; the target's among them
-  bool packed = c.n_seqs <= kSeqs;
+  bool packed = c.n_seqs <= kSeqs, fall = !packed && starts_fall(c.row_start, c.n_seqs);
   if (packed) {
-    int64_t all = 0;
     int2 done = make_int2(0, 0);
     for (int base = 0; base < c.n_seqs; base += kRowThreads) {
       const int q = base + (int)threadIdx.x;
@@ -120,6 +120,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) k_rows(const __grid_constant__
       if (q < c.n_seqs) {
         const RowSpan sp = row_span(c.row_start, c.n_rows, q);
         n = sp.e - sp.b;
+        fall |= __ldg(c.row_start + q) > __ldg(c.row_start + q + 1);
       }
       int2 x = make_int2(n, max(n - 1, 0));  // inclusive prefixes
 #pragma unroll
@@ -134,19 +135,18 @@ __global__ void __launch_bounds__(kRowThreads, 3) k_rows(const __grid_constant__
       for (int i = 0; i < kRowThreads / 32; ++i) {
         const int2 o = s_sum[i];
         if (i < (int)(threadIdx.x >> 5)) x.x += o.x, x.y += o.y;
-        all += o.x;
       }
       if (q < c.n_seqs) s_rows[q + 1] = done.x + x.x, s_drafts[q + 1] = done.y + x.y;
-      if (all > c.n_rows) break;
       for (int i = 0; i < kRowThreads / 32; ++i) done.x += s_sum[i].x, done.y += s_sum[i].y;
     }
     if (threadIdx.x == 0) s_rows[0] = s_drafts[0] = 0;
-    packed = all <= c.n_rows;
-    __syncthreads();
-    if (packed) {
-      target = side0 ? 0 : s_rows[c.n_seqs];
-      listed = target + (rows > c.n_rows || side0 ? s_drafts[c.n_seqs] : 0);
-    }
+  }
+  fall = __syncthreads_or(fall);
+  packed = packed && !fall;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *c.fall = fall;
+  if (packed) {
+    target = side0 ? 0 : s_rows[c.n_seqs];
+    listed = target + (rows > c.n_rows || side0 ? s_drafts[c.n_seqs] : 0);
   }
   // runs: no more than units, so that each has one and a row no more pieces than units
   const int64_t U = (int64_t)listed * c.n_units, S = min((int64_t)gridDim.x * (kRowThreads / 32), U);
@@ -193,9 +193,9 @@ __global__ void __launch_bounds__(kRowThreads, 3) k_rows(const __grid_constant__
     lead_in = (int)(((uintptr_t)x & 15) / sizeof(T));
     load(next, q);
     if (!packed) {
-      lo = search(c.row_start, row);
-      const RowSpan sp = row_span(c.row_start, c.n_rows, lo);
-      if (row < sp.b || row >= sp.e || (side && row + 1 == sp.e)) continue;
+      const int2 own = row_owner(c.row_start, c.n_rows, c.n_seqs, row, fall);
+      if (own.x < 0 || (side && row + 1 == own.y)) continue;
+      lo = own.x;
     }
     const float temp = c.temperature[side] ? c.temperature[side][lo] : 1.f;
     const bool greedy = !(temp > 0.f);
@@ -352,14 +352,14 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
   }
   // The kernels before this one let it start when what comes before them is done: the call's inputs may be read, what they find not yet.
   if (c.n_rows == 0) pdl_wait();  // (there are none)
-  const RowSpan sp = row_span(c.row_start, c.n_rows, s);
+  RowSpan sp = row_span(c.row_start, c.n_rows, s);  // (where starts fall it begins later or has no rows: looked at below)
   if (sp.b == sp.e) {
     pdl_wait();
     if (rank == 0 && tid == 0) c.accepted[s] = 0;
     return;
   }
   cl.barrier_arrive();  // (before any block writes to another's shared memory that one has to run: waited for below)
-  const int drafts = sp.e - sp.b - 1;
+  int drafts = sp.e - sp.b - 1;
   const T* logits = static_cast<const T*>(c.logits);
   const T* draft = static_cast<const T*>(c.draft);
   const int i0 = rank * c.slice, i1 = min(c.vocab, i0 + c.slice);
@@ -370,13 +370,14 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
   }
   // the drafts of the first kTogether rows, and their logits
   const int my_side = draft && warp < drafts ? lane >> 4 : 0;
-  const int my_x = warp < min(kTogether, drafts) ? c.tokens[sp.b + warp + 1] : -1;
+  int my_x = warp < min(kTogether, drafts) ? c.tokens[sp.b + warp + 1] : -1;
   auto logit_of = [&](int side, int row, int x) -> float {
     const T* from = side ? draft + (int64_t)row * c.draft_stride : logits + (int64_t)row * c.logits_stride;
     return x >= 0 && x < c.vocab ? (float)from[x] : -INFINITY;
   };
-  const float my_v = logit_of(my_side, sp.b + warp, my_x);
+  float my_v = logit_of(my_side, sp.b + warp, my_x);
   pdl_wait();
+  bool fall = s > 0 && *c.fall != 0;
   // what a row keeps, in 16 lanes of the target's and 16 of the drafter's, all lanes together (ordinary loads: read-only ones may be moved
   // ahead of the wait)
   auto kept_of = [&](int side, int row) -> Kept {
@@ -420,6 +421,21 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
       if (lane == 16 * side) s_kept[side][warp] = k, s_lp[side][warp] = log_p(k, v, x);
     }
     __syncthreads();
+    if (fall) {  // once more with the rows that the sequence has
+      fall = false;
+      sp = row_span_fallen(c.row_start, c.n_rows, s);
+      if (sp.b == sp.e) {
+        cl.barrier_wait();
+        if (rank == 0 && tid == 0) c.accepted[s] = 0;
+        return;
+      }
+      stop = drafts = sp.e - sp.b - 1;
+      my_x = warp < min(kTogether, drafts) ? c.tokens[sp.b + warp + 1] : -1;
+      my_v = logit_of(draft && warp < drafts ? lane >> 4 : 0, sp.b + warp, my_x);
+      j0 = -kTogether;
+      __syncthreads();
+      continue;
+    }
     if (lane < kTogether && j0 + lane < drafts) {  // (in every warp)
       const float q = draft ? expf(s_lp[1][lane]) : 1.f;
       if (!(c.u[sp.b + j0 + lane] * q < expf(s_lp[0][lane]))) stop = j0 + lane;
@@ -677,6 +693,8 @@ cudaError_t run(VerifyCall c, cudaStream_t s) {
   return e == cudaSuccess ? cudaLaunchKernelEx(&cfg, k_verify<T>, c) : e;
 }
 
+constexpr uint64_t kFallBytes = 16;  // of the workspace, before the rows' kept
+
 bool bad_word(const void* p) { return ((uintptr_t)p & 3) != 0; }
 bool bad_cuts(const mf_cuts_t& c) { return bad_word(c.temperature) || bad_word(c.top_p) || bad_word(c.min_p) || bad_word(c.top_k); }
 
@@ -688,7 +706,7 @@ using namespace mf;
 extern "C" int mf_verify_bytes(int n_seqs, int n_rows, int vocab, uint64_t* out) {
   if (!out || n_seqs < 0 || n_rows < 0 || n_seqs > (1 << 26) || n_rows > (1 << 26) || vocab < 1 || vocab > kMaxVocab) return MF_E_INVAL;
   const uint64_t units = ((uint64_t)vocab + kUnitEntries<float> + 2) / kUnitEntries<float>;
-  *out = (uint64_t)(n_rows > 0 ? n_rows : 1) * 2 * (sizeof(Kept) + units * sizeof(Piece));
+  *out = kFallBytes + (uint64_t)(n_rows > 0 ? n_rows : 1) * 2 * (sizeof(Kept) + units * sizeof(Piece));
   return MF_OK;
 }
 
@@ -711,13 +729,14 @@ extern "C" int mf_verify(const mf_verify_args_t* a, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   auto whole = [](const mf_cuts_t& c) { return !c.top_p && !c.min_p && !c.top_k; };
   const bool whole_p = whole(a->cuts), whole_q = whole(a->draft_cuts);
-  Kept* kept = static_cast<Kept*>(a->work);
+  int* fall = static_cast<int*>(a->work);
+  Kept* kept = reinterpret_cast<Kept*>(static_cast<unsigned char*>(a->work) + kFallBytes);
   const VerifyCall c = {a->logits, a->draft_logits, a->logits_stride, a->draft_stride, a->noise_stride, a->row_start, a->tokens, a->u, a->noise,
                         {a->cuts.temperature, a->draft_cuts.temperature}, a->token, a->accepted, a->logprob, kept,
-                        reinterpret_cast<Piece*>(kept + 2 * (int64_t)a->n_rows), {whole_p, whole_q}, a->n_seqs, a->n_rows, a->vocab, 0, 0, 0, sample_hold()};
+                        reinterpret_cast<Piece*>(kept + 2 * (int64_t)a->n_rows), fall, {whole_p, whole_q}, a->n_seqs, a->n_rows, a->vocab, 0, 0, 0, sample_hold()};
   cudaError_t e = cudaSuccess;
   if (a->n_rows > 0 && (!whole_p || (a->draft_logits && !whole_q))) {
-    const KeptRows rows = {a->logits,  whole_q ? nullptr : a->draft_logits, a->logits_stride, a->draft_stride, a->row_start, a->cuts, a->draft_cuts, kept,
+    const KeptRows rows = {a->logits,  whole_q ? nullptr : a->draft_logits, a->logits_stride, a->draft_stride, a->row_start, a->cuts, a->draft_cuts, kept, fall,
                            a->n_seqs, a->n_rows, a->vocab, a->dtype, !whole_p};
     e = launch_kept(rows, s);
   }

@@ -433,3 +433,40 @@ def test_copies_of_more_chunks_than_the_ring_holds_that_do_not_arrive(mf, model,
         mf.mf_sample_test_hold(0)
     assert all(torch.equal(p, q) for p, q in zip(want, got))
     assert all(torch.equal(p, q) for p, q in zip(want, b.run(mf)))
+
+
+def as_if_rising(starts, rows):
+    """Starts inside the rows, each the largest so far."""
+    at, out = 0, []
+    for x in starts:
+        at = max(at, min(max(x, 0), rows))
+        out.append(at)
+    return out
+
+
+@pytest.mark.parametrize("cut", [(), ("cuts",), ("draft_cuts",), ("cuts", "draft_cuts")])
+@pytest.mark.parametrize("starts", [[0, 5, 3, 4], [0, 5, 3, 11], [4, 2, 8, 12], [0, 2 ** 31 - 1, -2 ** 31, 6], [3, 0, 0, 12], [2, 6, 6, 5, 1, 9], [5, 4, 3, 2, 1]])
+def test_row_starts_that_fall(mf, starts, cut):
+    """Taken as the largest so far: a row has one sequence, whose settings and numbers it goes by; the others are not touched."""
+    n = len(starts) - 1
+    b = Batch([11] + [-1] * (n - 1), 300, torch.bfloat16)
+    for which in cut:
+        b.set(which, temperature=[0.7 + 0.1 * s for s in range(n)], top_k=[50 - 9 * s for s in range(n)], top_p=[0.9 - 0.05 * s for s in range(n)])
+    b.starts, b.row_start = as_if_rising(starts, b.rows), torch.tensor(starts, dtype=torch.int32, device="cuda")
+    token, accepted, lp = b.check(mf)
+    for row in list(range(b.starts[0])) + list(range(b.starts[-1], b.rows)):
+        assert token[row] == -7 and lp[row] == 7
+
+
+@pytest.mark.parametrize("cut", [False, True])
+def test_row_starts_of_many_sequences_that_fall(mf, cut):
+    """More sequences than are listed in shared memory, some of whose starts lie below earlier ones."""
+    n = 2500
+    b = Batch([1] * n, 9, torch.float32)
+    starts = list(b.starts)
+    for s in (3, 700, 701, 2300, n):
+        starts[s] -= 300
+    if cut:
+        b.set("cuts", temperature=[0.5 + 0.5 * (s % 3) for s in range(n)], top_k=[9 - s % 8 for s in range(n)])
+    b.starts, b.row_start = as_if_rising(starts, b.rows), torch.tensor(starts, dtype=torch.int32, device="cuda")
+    b.check(mf)
