@@ -136,7 +136,7 @@ class Shared(ctypes.Structure):
 
 class Cuts(ctypes.Structure):
     _fields_ = [("temperature", ctypes.c_void_p), ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p), ("top_k", ctypes.c_void_p)]
-    seqs = None  # sequences that all settings have, where it is known (cuts)
+    seqs = gpu = None  # sequences that all settings have, the GPU they are on (-1: several), where that is known (cuts)
 
 
 class _VerifyArgs(ctypes.Structure):
@@ -466,11 +466,13 @@ class _Types:
         cls.of = {code: dtype for dtype, code in cls.codes.items()}
 
 
-def _vector(t, dtype, n: int, where: str):
-    """Address of n elements of a contiguous tensor that the GPU can reach (None and plain addresses as they are)."""
+def _vector(t, dtype, n: int, where: str, device: int | None = None):
+    """Address of n elements of a contiguous tensor that the GPU can reach, of `device` where that is given (None and plain addresses
+    as they are)."""
     if t is None or isinstance(t, int):
         return t
-    if t.dtype is not dtype or t.numel() < n or (n > 1 and not t.is_contiguous()) or not (t.is_cuda or t.is_pinned()):
+    if t.dtype is not dtype or t.numel() < n or (n > 1 and not t.is_contiguous()) or \
+            not ((t.is_cuda if device is None else t.get_device() == device) or t.is_pinned()):
         raise MFError(MF_E_INVAL, where)
     return t.data_ptr()
 
@@ -713,6 +715,8 @@ def cuts(temperature=None, top_k=None, top_p=None, min_p=None) -> Cuts:
     _on_gpu(*given)
     c = Cuts(_addr(temperature), _addr(top_p), _addr(min_p), _addr(top_k))
     c.held, c.seqs = (temperature, top_k, top_p, min_p), min((t.shape[0] for t in given), default=None)
+    gpus = {t.get_device() for t in given if t.is_cuda}
+    c.gpu = (gpus.pop() if len(gpus) == 1 else -1) if gpus else None
     return c
 
 
@@ -728,9 +732,9 @@ _NO_CUTS = Cuts()
 
 def mf_verify(logits, row_start, tokens, u, noise, token, accepted, work, logprob=None, cuts: Cuts | None = None, draft_logits=None,
               draft_cuts: Cuts | None = None, stream=None) -> None:
-    """Drafted tokens taken or refused, and the token that ends each sequence (see mawforge.h).  logits and draft_logits [rows][vocab] of
-    one type on the current device, noise float32 [sequences][vocab], u and logprob float32, row_start, tokens, token and accepted
-    int32, work uint8."""
+    """Drafted tokens taken or refused, and the token that ends each sequence (see mawforge.h).  All tensors are on the current
+    device (or pinned), the settings' too: logits and draft_logits [rows][vocab] of one type, noise float32 [sequences][vocab], u and
+    logprob float32, row_start, tokens, token and accepted int32, work uint8."""
     w = "mf_verify"
     if not _Types.codes:
         _Types.load()
@@ -738,26 +742,31 @@ def mf_verify(logits, row_start, tokens, u, noise, token, accepted, work, logpro
     if dtype is None or logits.dim() != 2 or noise.dim() != 2 or noise.dtype is not f32 or noise.shape[1] != logits.shape[1]:
         raise MFError(MF_E_INVAL, w)
     (n, vocab), seqs = logits.shape, noise.shape[0]
+    if not (logits.is_cuda or logits.is_pinned()):
+        raise MFError(MF_E_INVAL, w)
+    here = _Types.device()
     draft, draft_stride = None, 0
     if draft_logits is not None:
         if draft_logits.dtype is not logits.dtype or draft_logits.shape != logits.shape or draft_logits.stride(1) != 1 or \
-                not (draft_logits.is_cuda or draft_logits.is_pinned()):
+                not (draft_logits.get_device() == here or draft_logits.is_pinned()):
             raise MFError(MF_E_INVAL, w)
         draft, draft_stride = draft_logits.data_ptr(), draft_logits.stride(0)
     ls, ns = logits.stride(), noise.stride()
-    if ls[1] != 1 or ns[1] != 1 or not ((logits.is_cuda or logits.is_pinned()) and (noise.is_cuda or noise.is_pinned())):
-        raise MFError(MF_E_INVAL, w)
-    if logits.is_cuda and logits.get_device() != _Types.device():
+    if ls[1] != 1 or ns[1] != 1 or not (logits.get_device() == here or logits.is_pinned()) or \
+            not (noise.get_device() == here or noise.is_pinned()):
         raise MFError(MF_E_INVAL, w)
     cuts, draft_cuts = cuts or _NO_CUTS, draft_cuts or _NO_CUTS
+    if cuts.gpu not in (None, here) or draft_cuts.gpu not in (None, here):
+        raise MFError(MF_E_INVAL, w)
     need = _u64()
     if any(c.seqs is not None and c.seqs < seqs for c in (cuts, draft_cuts)) or \
             _lib.mf_verify_bytes(seqs, n, vocab, ctypes.byref(need)) or work.numel() * work.element_size() < need.value or \
-            not work.is_contiguous() or not work.is_cuda:
+            not work.is_contiguous() or work.get_device() != here:
         raise MFError(MF_E_INVAL, w)
-    a = _VerifyArgs(logits.data_ptr(), draft, _vector(row_start, i32, seqs + 1, w), _vector(tokens, i32, n, w), _vector(u, f32, n, w),
-                    noise.data_ptr(), cuts, draft_cuts, _vector(token, i32, n, w), _vector(accepted, i32, seqs, w),
-                    _vector(logprob, f32, n, w), work.data_ptr(), ls[0], draft_stride, ns[0], seqs, n, vocab, dtype)
+    a = _VerifyArgs(logits.data_ptr(), draft, _vector(row_start, i32, seqs + 1, w, here), _vector(tokens, i32, n, w, here),
+                    _vector(u, f32, n, w, here), noise.data_ptr(), cuts, draft_cuts, _vector(token, i32, n, w, here),
+                    _vector(accepted, i32, seqs, w, here), _vector(logprob, f32, n, w, here), work.data_ptr(), ls[0], draft_stride, ns[0],
+                    seqs, n, vocab, dtype)
     rc = _lib.mf_verify(a, _stream(stream))
     if rc:
         _check(rc, w)

@@ -126,3 +126,65 @@ def test_descriptions_refuse_what_is_not_on_the_gpu(mf):
     with pytest.raises(mf.MFError) as e:
         mf.mf_verify(x, i, i, w[:2], x[:1], i, i, torch.zeros(4096, dtype=torch.uint8))
     assert e.value.status == mf.MF_E_INVAL
+
+
+class OnGpu:
+    """What the binding asks of a tensor, on a GPU that this machine need not have."""
+    is_cuda = True
+
+    def __init__(self, dtype, *shape, device=0):
+        self.dtype, self.shape, self.at = dtype, shape, device
+
+    def dim(self):
+        return len(self.shape)
+
+    def stride(self, i=None):
+        s = tuple(math.prod(self.shape[k + 1:]) for k in range(len(self.shape)))
+        return s if i is None else s[i]
+
+    def numel(self):
+        return math.prod(self.shape)
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def is_contiguous(self):
+        return True
+
+    def is_pinned(self):
+        return False
+
+    def get_device(self):
+        return self.at
+
+    def data_ptr(self):
+        return AT
+
+
+def test_verify_refuses_tensors_of_another_gpu(mf, monkeypatch):
+    """Every tensor of a call, settings too, has to be on the current device: the kernels would read another's addresses as their own."""
+    torch = pytest.importorskip("torch")
+    if not mf._Types.codes:
+        mf._Types.load()
+    calls = []
+    monkeypatch.setattr(mf._Types, "device", lambda: 0)
+    monkeypatch.setattr(mf, "_stream", lambda s: None)
+    monkeypatch.setattr(mf._lib, "mf_verify", lambda a, s: calls.append(a) or mf.MF_OK)
+    f32, i32, n, seqs, v = torch.float32, torch.int32, 5, 2, 300
+    good = dict(logits=(f32, n, v), draft_logits=(f32, n, v), noise=(f32, seqs, v), row_start=(i32, seqs + 1), tokens=(i32, n), u=(f32, n),
+                token=(i32, n), accepted=(i32, seqs), logprob=(f32, n), work=(torch.uint8, mf.mf_verify_bytes(seqs, n, v)))
+    sets = dict(temperature=(f32, seqs), top_k=(i32, seqs), top_p=(f32, seqs), min_p=(f32, seqs))
+
+    def call(other=None):
+        args = {k: OnGpu(*a, device=int(k == other)) for k, a in good.items()}
+        for which in ("cuts", "draft_cuts"):
+            args[which] = mf.cuts(**{k: OnGpu(*a, device=int((which, k) == other)) for k, a in sets.items()})
+        mf.mf_verify(**args)
+
+    call()
+    assert len(calls) == 1
+    for other in list(good) + [(w, k) for w in ("cuts", "draft_cuts") for k in sets]:
+        with pytest.raises(mf.MFError) as e:
+            call(other)
+        assert e.value.status == mf.MF_E_INVAL
+    assert len(calls) == 1
