@@ -223,3 +223,127 @@ def test_refusals(mf):
         mf.mf_kv_append_norm(at, cache, step, good, c.new_k[:, :1], c.new_v)
     assert mf.mf_attn_check(at) == 0
     mf.mf_attn_destroy(at)
+
+
+# ---- prompts: from eight blocks an SM on (1216 tokens), four tokens a block
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d,rot", [(64, 64), (64, None), (128, 128), (128, 48), (256, 64), (256, 256)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_prompts(mf, dtype, d, rot, interleaved):
+    """Sequences that begin and end inside a block's four tokens, a last block of three."""
+    check(mf, ref.Case([700, 1, 0, 511, 2, 1, 408], [0, 200, 9, 100, 16, 3, 31], 6, 2, d, dtype, page=24), rot, interleaved, offset=1.0,
+          w=[x - 1 for x in weights(ref.Case([1], [0], d=d, dtype=dtype))])
+
+
+@pytest.mark.parametrize("tokens", [1215, 1216, 1217, 1218, 1219, 2432])
+def test_prompts_of_any_length(mf, tokens):
+    check(mf, ref.Case([tokens - 50, 50], [3, 70], 4, 2, 128, page=16), 128, in_place=True)
+    check(mf, ref.Case([tokens], [0], 4, 2, 64, "f16", page=7), 64, with_q=False)
+
+
+@pytest.mark.parametrize("hq,hkv", [(1, 1), (3, 1), (5, 5), (40, 8), (64, 4), (96, 32)])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_heads_of_prompts(mf, hq, hkv, d):
+    """Heads of several tokens in a warp, and in one round of a block's threads."""
+    check(mf, ref.Case([1, 1218], [3, 0], hq, hkv, d), 64)
+
+
+@pytest.mark.parametrize("sections", [(8, 12, 12), (0, 32), (11, 10, 6, 5)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_axes_of_prompts(mf, sections, interleaved):
+    check(mf, ref.Case([7, 1300], [0, 5], 4, 4, 128, heads_first=True, row_pad=16), 64, interleaved, sections)
+
+
+@pytest.mark.parametrize("page", [1, 64])
+def test_single_tokens_of_many_sequences(mf, page):
+    """Every token of a block has a sequence of its own."""
+    check(mf, ref.Case([1] * 1301, [i % 50 for i in range(1301)], 4, 1, 128, page=page), 32)
+
+
+@pytest.mark.parametrize("which", [(True, False), (False, True), (False, False)])
+def test_prompts_with_one_norm_or_none(mf, which):
+    for f32, rot in ((True, 128), (False, None)):
+        c = ref.Case([1209, 9], [3, 64], 8, 2, 128)
+        check(mf, c, rot, w=[x if yes else None for x, yes in zip(weights(c, f32), which)])
+
+
+def test_sizes_of_x_in_prompts(mf):
+    """Rows whose squares' sum no float holds beside ordinary ones and zeros, in one warp too."""
+    c = ref.Case([1220], [0], 8, 2, 64)
+    for x in (c.q, c.new_k):
+        x[::3] = (x[::3] / x[::3].abs().amax(-1, keepdim=True).float() * 3e38).to(x.dtype)
+        x[1::3, ::2] = 0
+    check(mf, c, 64, eps=2.0 ** -100)
+
+
+def test_offsets_of_prompts_beyond_32_bits(mf):
+    base = 2 ** 31 // (64 * 2 * 128) + 1
+    check(mf, ref.Case([1216, 3], [200, 30], 8, 2, 128, page=64, base_page=base), 128)
+
+
+def test_prompt_tokens_and_pages_that_are_not_there(mf):
+    """Tokens of no sequence, which share blocks with others, store no key and no value; nor does one whose page is outside the pool.  All
+    others are right, and both are reported."""
+    c = ref.Case([1, 1300], [100, 7], 8, 2, 64)
+    norm, w = mf.qk_norm(*weights(c), 1e-6), weights(c)
+    pg = torch.cat([a[n - m:n] for (a, b), n, m in zip(c.lines, c.len, c.new)])
+    ln = torch.cat([b[n - m:n] for (a, b), n, m in zip(c.lines, c.len, c.new)])
+    at = mf.mf_attn_create(mf.AttnShape(8, 2, 64, mf.MF_BF16), 2, c.tokens + 8, 0)
+
+    def right(kc, vc, gone=None):
+        keep = torch.ones(c.tokens, dtype=torch.bool, device="cuda")
+        if gone is not None:
+            keep[gone] = False
+        want = norm64(c.new_k, w[1], 1e-6, 0.0)
+        assert ((c.k[pg, ln].double() - want).abs() <= (2.0 ** -8 + 24 * 2.0 ** -24) * 1.01 * want.abs())[keep].all()
+        assert torch.equal(c.v[pg, ln][keep], c.new_v[keep])
+        for got, was in ((c.k, kc), (c.v, vc)):
+            got[pg[keep], ln[keep]] = was[pg[keep], ln[keep]]
+            assert torch.equal(got.view(torch.int16), was.view(torch.int16))
+
+    kc, vc = c.k.clone(), c.v.clone()
+    for before, after in ((2, 2), (5, 0), (0, 7)):
+        q, k, v = (torch.cat((x[:before], x, x[:after])) for x in (c.q, c.new_k, c.new_v))
+        out = torch.empty(before + c.tokens + after, 8, 64, dtype=c.q.dtype, device="cuda")
+        step = mf.step(c.q_start + before, c.kv_len, c.pages, before + c.tokens + after, 1300)
+        mf.mf_kv_append_norm(at, mf.kv_cache(c.k, c.v), step, norm, k, v, q, out)
+        assert mf.mf_attn_check(at) == mf.MF_E_INVAL and mf.mf_attn_check(at) == 0
+        right(kc, vc)
+    page, bad = c.pages[1, 40].item(), (pg == c.pages[1, 40]).nonzero()[:, 0]
+    for x in (1 << 30, -3):
+        c.pages[1, 40] = x
+        mf.mf_kv_append_norm(at, mf.kv_cache(c.k, c.v), c.step(mf), norm, c.new_k, c.new_v)
+        assert mf.mf_attn_check(at) == mf.MF_E_INVAL
+        right(kc, vc, bad)
+    c.pages[1, 40] = page
+    mf.mf_attn_destroy(at)
+
+
+def test_prompts_on_another_stream_and_in_a_graph(mf):
+    c = ref.Case([1250, 1], [300, 20], 8, 2, 128)
+    at, cache, step = c.attn(mf), mf.kv_cache(c.k, c.v), c.step(mf)
+    qw, kw = weights(c)
+    norm, out, noise = mf.qk_norm(qw, kw, 1e-6), torch.empty_like(c.q.contiguous()), torch.randn_like(c.q)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+
+    def body():
+        c.q.add_(noise)
+        mf.mf_kv_append_norm(at, cache, step, norm, c.new_k, c.new_v, c.q, out)
+
+    with torch.cuda.stream(s):
+        body()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            body()
+        for lens in ([1550, 21], [1250, 1], [1401, 20]):
+            c.kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+            g.replay()
+            s.synchronize()
+            for got, x, w in ((out, c.q, qw), (torch.cat([c.k[a[n - m:n], b[n - m:n]] for (a, b), n, m in zip(c.lines, lens, c.new)]),
+                                               c.new_k, kw)):
+                want = norm64(x, w, 1e-6, 0.0)
+                assert ((got.double() - want).abs() <= (2.0 ** -8 + 2.0 ** -19) * want.abs()).all()
+    assert mf.mf_attn_check(at) == 0
+    mf.mf_attn_destroy(at)
