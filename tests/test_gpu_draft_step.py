@@ -44,3 +44,28 @@ def test_greedy_drafts(example):
     best = last.argmax(-1)
     rows = len(best)
     assert rows >= 3 and all(s[-1] in best.tolist() for s in said)
+
+
+@pytest.mark.parametrize("system", [16, 48, 150])
+@pytest.mark.parametrize("temperature", [0.8, 0.0])
+def test_steps_through_the_shared_kernels(example, monkeypatch, system, temperature):
+    """With page tables as wide as a server keeps them the streams' shared lines are read for the group (what narrow tables can hold, each
+    stream reads itself): the logits still equal those of one prefill, and the tokens are the same again."""
+    plain, widths = example.Server, []
+
+    class Wide(plain):
+        def __init__(self, streams, max_tokens, max_len, seed=0):
+            super().__init__(streams, max_tokens, max_len, seed)
+            line = streams * example.base.KV_HEADS * example.base.DIM * 4
+            more = int(128e6 / (line * example.base.PAGE)) + 2
+            self.pages = torch.nn.functional.pad(self.pages, (0, more)).contiguous()
+            widths.append(self.pages.shape[1] * example.base.PAGE * line)
+
+    monkeypatch.setattr(example, "Server", Wide)
+    prompt = [(11 * i) % 97 for i in range(system)]
+    questions = [[(7 * i + 13 * s) % example.base.VOCAB for i in range(n)] for s, n in enumerate((5, 40, 1, 23))]
+    said, (taken, offered), last, again = example.serve(prompt, questions, 9, temperature=temperature)
+    assert widths and min(widths) > 128e6
+    assert sum(map(len, said)) == 4 * 9 + taken <= 4 * 9 + offered
+    assert float(last.std()) > 0.5 and float((last - again).abs().max()) < 0.1
+    assert example.serve(prompt, questions, 9, temperature=temperature)[0] == said
