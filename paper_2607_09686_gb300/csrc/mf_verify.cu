@@ -519,14 +519,11 @@ __global__ void __launch_bounds__(kThreads + 32, 3) k_verify(const __grid_consta
     if (lane == 0) {
       int stage = 0;
       uint32_t phase = 1;  // (the first turn of the ring waits for nothing)
-      for (int k = 0; k < chunks && !s_lost; ++k) {
-        if (k >= stages && !mbar_wait(&s_free[stage], phase, kDefaultWaitNs)) {
-          s_lost = 1;
-          break;
-        }
-        if (s_lost) break;  // (let go without its copies, which may be on their way)
+      for (int k = 0; k < chunks; ++k) {
+        if (k >= stages && !mbar_wait(&s_free[stage], phase, kDefaultWaitNs)) s_lost = 1;
+        if (s_lost) break;  // (the stage may have been let go without its copies, which may be on their way)
         fill(k, stage);
-        ++filled;
+        filled = k + 1;
         if (++stage == stages) stage = 0, phase ^= 1;
       }
     }
