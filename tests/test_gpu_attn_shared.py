@@ -352,3 +352,13 @@ def test_many_sequences_that_share(mf, d, new):
     assert mf.mf_attn_check(at) == 0
     mf.mf_attn_destroy(at)
     assert (outs.view(torch.int16) == want.view(torch.int16)).all()
+
+
+@pytest.mark.parametrize("long", [False, True])
+def test_many_groups_of_several(mf, long):
+    """More groups than the plan holds in shared memory, each with lines in common, on the list of few rows and on that of many."""
+    n, per = 900, 3
+    lens = [16 * (1 + g % 5) + g % 3 for g in range(n // per)]
+    c = ref.Case([1 + 40 * (long and i % 90 == 4) for i in range(n)], [lens[i // per] + (i * 37) % 40 for i in range(n)], 4, 2, 64, "f16")
+    first = check(mf, c, list(range(0, n + 1, per)), lens)
+    assert torch.equal(first, check(mf, c, list(range(0, n + 1, per)), lens))
