@@ -2,7 +2,8 @@
 
 The system prompt is computed once; the streams' page tables name its pages.  Every step a stream adds its next token and a few drafts,
 looked up in what was said before.  On the layer that is: keys and queries normed head by head, rotated and appended to the
-paged cache in one pass, attention that reads the shared lines once for all streams, the routed experts, and the drafts verified
+paged cache in one pass, attention that shares the lines of the prompt among the streams (read once for all where the tables can hold
+enough for that to pay), the routed experts, and the drafts verified
 against the target's probabilities, with a token after the last that was taken.  Lines of drafts that were not taken are written over by the next
 step.  Weights are random; projections are plain torch.  ``python examples/draft_step.py`` prints the tokens and how many drafts were
 taken, and compares the logits of the last step with those of one pass over the whole sequences.

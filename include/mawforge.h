@@ -490,6 +490,8 @@ typedef struct mf_shared {
 int mf_attn_share(mf_attn_t* attn, int max_groups);
 
 /* mf_attn_forward for sequences that share their first lines: the same result, but for the order of sums.  args->window must be 0.
+ * Where sharing hardly pays (tables that hold at most 128 MB of lines, 80 MB with heads of 64; or sequences with rows, tokens times heads
+ * a kv head, for tiles of their own: 72 on the average, 256 with heads of 256) every sequence reads all lines from its own pages.
  * MF_E_STATE before mf_attn_share; errors else as for mf_attn_forward, and MF_E_INVAL for NULL pointers of a group, n_groups
  * below 0 or above max_groups. */
 int mf_attn_forward_shared(mf_attn_t* attn, const mf_kv_cache_t* cache, const mf_step_t* step, const mf_shared_t* shared,
@@ -558,7 +560,8 @@ typedef struct mf_cuts {
  * or NaN is not taken).  In the first row where it is not, the token is the entry with the largest log(p - q) + noise among those
  * with p > q (among those with p > 0 if there is none), in the last row, all drafts taken, the one with the largest log(p) + noise; the
  * lowest such index; noise (device float [n_seqs][vocab], row s at s * noise_stride) as in mf_sample.  So the tokens that are taken
- * are draws from the target.  Arithmetic in fp32, the kept as mf_sample finds them.
+ * are draws from the target.  Arithmetic in fp32, the kept as mf_sample finds them; what lies within 1e-5 of a border (u q of p, two
+ * keys) may fall on either side of it in another batch or at another alignment, the same call gives the same bits.
  *   token     device int32 [n_rows]: the drafts that were taken, then the new token (-1 where its row has no p), -1 in the rows after it
  *   accepted  device int32 [n_seqs]: the number of drafts taken
  *   logprob   device float [n_rows] or NULL: log p of each token in `token`, -inf beside -1

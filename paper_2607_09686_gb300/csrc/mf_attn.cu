@@ -406,7 +406,8 @@ extern "C" int mf_attn_share(mf_attn_t* attn, int max_groups) {
   unsigned char* ws = nullptr;
   // (the join counts its vectors in 32 bits)
   cudaError_t e = tiles < (1 << 30) && w.off < ((size_t)1 << 36) ? cudaMalloc(&ws, w.off) : cudaErrorMemoryAllocation;
-  // (runs that no call wrote, for lack of tiles where a step's bounds overlap, have no pieces)
+  // (runs that a step does not write, for lack of tiles where its bounds overlap, hold zeros or what an earlier step wrote: a wrong answer to a
+  // step that is reported, from inside the workspace)
   if (e == cudaSuccess) e = cudaMemset(ws + o_runs, 0, (size_t)tiles * sh.n_kv_heads * 8);
   if (e == cudaSuccess) e = cudaMemset(ws + o_fruns, 0, ((size_t)max_groups + attn->max_seqs) * sh.n_kv_heads * 8);
   if (e == cudaSuccess) e = cudaDeviceSynchronize();

@@ -165,14 +165,16 @@ __device__ __forceinline__ bool counter_wait(const unsigned long long* cnt, unsi
 // Programmatic dependent launch (PTX griddepcontrol).  pdl_wait: block until the grid this launch
 // depends on has completed and its memory operations are visible (returns at once when the
 // launch was not programmatic); everything before it may overlap the predecessor's tail and must
-// touch no global memory the predecessor or the caller's earlier work could write.
+// touch no global memory the predecessor or the caller's earlier work could write, but for what was
+// complete before the predecessor let this launch start.
 // pdl_trigger: allow the dependent launch to be scheduled (its blocks start as SMs free up).
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 // A launch whose blocks may be scheduled while the stream's previous kernel ends (every kernel launched
-// this way calls pdl_wait before it touches global memory; k_down_pipe's producer may fetch weights earlier, which
-// were complete before the kernel it follows began); a plain launch where that is refused or not
-// asked for (overlap false: after an event wait the predecessor is not a kernel of this stream).
+// this way calls pdl_wait before it touches global memory, but for what was complete before it could start:
+// k_down_pipe's producer may fetch weights earlier, written before the kernel it follows began; k_attn_few over shared
+// lines reads the plan, q and the cache, as the kernel before it triggers only after its own wait for the plan); a plain
+// launch where that is refused or not asked for (overlap false: after an event wait the predecessor is not a kernel of this stream).
 template <class... P, class... A>
 cudaError_t launch_pdl(bool overlap, void (*kern)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
                        A&&... args) {

@@ -8,9 +8,9 @@
 // What bounds it: reading the logits (k_rows), then of the rows that decide the logits again and the noise; few sequences, the
 // chain of launches and look-ups.  Where rows are cut, k_sample.
 //
-// Measured, in graphs: 64 sequences of up to 4 drafts and a drafter's rows, 131072 bf16, by temperature: 36.3 us, about 16 of them k_rows'
-// (79 MB, 5 TB/s); 64 of up to 8 drafts without a drafter, 50001 bf16: 22.3.  Cut rows: one sequence of 4 drafts, 131072 fp32: 20.4, of
-// them 12 k_sample's; 24 of up to 4, 200001 fp16: 77.4, of which k_sample, with 116 rows, has most (by itself 73, the caches cold).
+// Measured, in graphs: 64 sequences of up to 4 drafts and a drafter's rows, 131072 bf16, by temperature: 36.7 us, about 16 of them k_rows'
+// (79 MB, 5 TB/s); 64 of up to 8 drafts without a drafter, 50001 bf16: 22.3.  Cut rows: one sequence of 4 drafts, 131072 fp32: 20.8, of
+// them 12 k_sample's; 24 of up to 4, 200001 fp16: 77.6, of which k_sample, with 116 rows, has most (by itself 73, the caches cold).
 #include <cooperative_groups.h>
 
 #include <cfloat>
