@@ -140,9 +140,9 @@ __device__ __forceinline__ int64_t quick_div(int64_t a, int64_t b) {
 // all the group's tokens and the shared lines (whole pages of them), then the sequences, with what follows.  First the groups: bounds
 // that rise, lengths that all their sequences have; a group of one shares nothing.  p.groups and p.seqs say which of them are in the list
 // of this file's kernel, few_groups and few_seqs which are in that of few rows.  Two blocks, both of which find the groups: the first lays out this
-// file's list and says where its kernel's blocks begin, the second the other list, and what the join asks for.  Nothing orders the two: what both
-// write to one place (bounds, groups, first row tiles, of steps too large for shared memory) is written once, with the same value.  Its time is a chain of
-// loads and scans: 64 sequences, one group, 5 us (blocks of 512 threads; of 1024 a microsecond more, of 256 half of one).  Then the step of
+// file's list and says where its kernel's blocks begin, the second the other list, and what the join asks for.  Nothing orders the two: what
+// both write to one place (bounds, groups, first row tiles, of steps too large for shared memory) is written once, with the same value.
+// Its time is a chain of loads and scans: 64 sequences, one group, 5 us (blocks of 512 threads; of 1024 a microsecond more, of 256 half of one).  Then the step of
 // 64 tokens behind 16384 lines, 32/4 heads of 128: the group's 2048 jobs from 5.5 to 23 us (4.5 until the first scores, 13 for 13.5 jobs
 // a block), the sequences' own lines to 37 (few rows), the join to 46.
 constexpr int kPlanThreads = 512;

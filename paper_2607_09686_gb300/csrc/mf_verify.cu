@@ -730,11 +730,12 @@ extern "C" int mf_verify(const mf_verify_args_t* a, void* stream) {
   Kept* kept = reinterpret_cast<Kept*>(static_cast<unsigned char*>(a->work) + kFallBytes);
   const VerifyCall c = {a->logits, a->draft_logits, a->logits_stride, a->draft_stride, a->noise_stride, a->row_start, a->tokens, a->u, a->noise,
                         {a->cuts.temperature, a->draft_cuts.temperature}, a->token, a->accepted, a->logprob, kept,
-                        reinterpret_cast<Piece*>(kept + 2 * (int64_t)a->n_rows), fall, {whole_p, whole_q}, a->n_seqs, a->n_rows, a->vocab, 0, 0, 0, sample_hold()};
+                        reinterpret_cast<Piece*>(kept + 2 * (int64_t)a->n_rows), fall, {whole_p, whole_q}, a->n_seqs, a->n_rows, a->vocab, 0, 0, 0,
+                        sample_hold()};
   cudaError_t e = cudaSuccess;
   if (a->n_rows > 0 && (!whole_p || (a->draft_logits && !whole_q))) {
-    const KeptRows rows = {a->logits,  whole_q ? nullptr : a->draft_logits, a->logits_stride, a->draft_stride, a->row_start, a->cuts, a->draft_cuts, kept, fall,
-                           a->n_seqs, a->n_rows, a->vocab, a->dtype, !whole_p};
+    const KeptRows rows = {a->logits,  whole_q ? nullptr : a->draft_logits, a->logits_stride, a->draft_stride, a->row_start, a->cuts, a->draft_cuts,
+                           kept, fall, a->n_seqs, a->n_rows, a->vocab, a->dtype, !whole_p};
     e = launch_kept(rows, s);
   }
   if (e == cudaSuccess) e = a->dtype == MF_F32 ? run<float>(c, s) : a->dtype == MF_F16 ? run<__half>(c, s) : run<__nv_bfloat16>(c, s);

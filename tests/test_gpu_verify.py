@@ -461,7 +461,8 @@ def as_if_rising(starts, rows):
 
 
 @pytest.mark.parametrize("cut", [(), ("cuts",), ("draft_cuts",), ("cuts", "draft_cuts")])
-@pytest.mark.parametrize("starts", [[0, 5, 3, 4], [0, 5, 3, 11], [4, 2, 8, 12], [0, 2 ** 31 - 1, -2 ** 31, 6], [3, 0, 0, 12], [2, 6, 6, 5, 1, 9], [5, 4, 3, 2, 1]])
+@pytest.mark.parametrize("starts", [[0, 5, 3, 4], [0, 5, 3, 11], [4, 2, 8, 12], [0, 2 ** 31 - 1, -2 ** 31, 6], [3, 0, 0, 12],
+                                    [2, 6, 6, 5, 1, 9], [5, 4, 3, 2, 1]])
 def test_row_starts_that_fall(mf, starts, cut):
     """Taken as the largest so far: a row has one sequence, whose settings and numbers it goes by; the others are not touched."""
     n = len(starts) - 1
